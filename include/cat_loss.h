@@ -385,6 +385,104 @@ int cat_kd_loss_fwd_bwd(const cat_shape* shape, const cat_kd_desc* desc, const v
                         void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * Log probabilities of given tokens, with the entropy of each row's distribution and its most likely
+ * tokens, straight from hidden states and head (no counterpart in the paper; the general form of
+ * cat_conf_fwd, for scoring, policy-gradient training, serving, and for writing the lists that
+ * cat_topk_kd_loss_fwd_bwd distils from):
+ *     z[r, v]    = sum_i H[r, i] W[v, i],   lse[r] = log sum_v exp z[r, v],   p = exp(z - lse)
+ *     logp[r]    = z[r, y_r] - lse[r]                   0 if y_r is no token id
+ *     entropy[r] = - sum_v p[r, v] log p[r, v]
+ *     top_ids[r, :], top_logp[r, :]  the top_k largest z[r, v] - lse[r], in falling order
+ * The order of the alternatives is that of the logits as 64-bit sums of the exact products; equal logits go to the
+ * lower id.  Places past the vocabulary (top_k > V) hold id -1 and -infinity.
+ * A row with valid[r] == 0 gets logp = lse = entropy = 0, ids -1 and -infinity, whatever H holds there.  A row whose
+ * lse is not finite (an infinity or NaN in H or W) gets NaN, and ids -1; H and W must not overflow the fp32 logits.
+ * `shape`: T rows, d, V, in_dtype, ldH, ldW, slab_mib; K, dW_dtype and the weight mode are ignored.
+ *   H, W       [T, d], [V, d] of in_dtype                                        (device, in)
+ *   labels     [T] int64; NULL (then logp too) for alternatives and entropy alone  (device, in)
+ *   valid      [T] uint8 or NULL                                                   (device, in)
+ *   top_k      0 .. CAT_TOPK_MAX; 0 = no alternatives (top_ids, top_logp unused)      (host)
+ *   logp       [T] fp32, NULL exactly when labels is                                (device, out)
+ *   lse, entropy  [T] fp32                                                         (device, out)
+ *   top_ids    [T, top_k] int64;  top_logp  [T, top_k] fp32                        (device, out)
+ *   workspace  at least cat_logprob_workspace_bytes(shape, top_k, 0) bytes, 256-byte aligned
+ * With top_k > 0 the workspace holds one row slab of logits (fp16, or fp32 for CAT_F32) of at most about slab_mib
+ * MiB (default 3072), never more than T rows.  Two launches per slab and one memset.  The workspace's first int32 holds the
+ * device status.  Calls that may overlap on the GPU need a workspace each.  Returns CAT_OK or a negative cat_status.
+ */
+#define CAT_TOPK_MAX 256
+int cat_logprob_fwd(const cat_shape* shape, const void* H, const void* W, const int64_t* labels,
+                    const uint8_t* valid, int32_t top_k,
+                    float* logp, float* lse, float* entropy, int64_t* top_ids, float* top_logp,
+                    void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Gradients of sum_r (grad_logp[r] logp[r] + grad_entropy[r] entropy[r]) with respect to H and W:
+ *     dz[r, v] = grad_logp[r] ([v == y_r] - p[r, v]) - grad_entropy[r] p[r, v] (log p[r, v] + entropy[r]),
+ *     dH = dz W,   dW = dz^T H.
+ * The logits are recomputed per vocabulary slab, as in cat_loss_bwd; dz is rounded once to in_dtype.  Rows with
+ * valid[r] == 0 get a zero dH row and add nothing to dW, whatever H holds there; a label that is no token id
+ * contributes through the entropy only.  No gradient flows through the alternatives.
+ *   lse, entropy   [T] fp32 as written by cat_logprob_fwd; entropy may be NULL without grad_entropy   (device, in)
+ *   grad_logp      [T] fp32, or NULL (then labels may be NULL too)                 (device, in)
+ *   grad_entropy   [T] fp32, or NULL                                               (device, in)
+ *   dH [T, d] of in_dtype with pitch ldH;  dW [V, d] of dW_dtype with pitch ldW; accumulate_dW as in cat_loss_bwd
+ *   workspace      at least cat_logprob_workspace_bytes(shape, 0, 1) bytes, 256-byte aligned
+ */
+int cat_logprob_bwd(const cat_shape* shape, const void* H, const void* W, const int64_t* labels,
+                    const uint8_t* valid, const float* lse, const float* entropy,
+                    const float* grad_logp, const float* grad_entropy,
+                    void* dH, void* dW, int accumulate_dW,
+                    void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Scratch bytes: pass 0 = cat_logprob_fwd with this top_k, pass 1 = cat_logprob_bwd.  0 if anything is invalid. */
+size_t cat_logprob_workspace_bytes(const cat_shape* shape, int top_k, int pass);
+
+/*
+ * The loss of Eq. 12 with the distillation term taken over the teacher's stored top logits instead of its whole
+ * distribution (no target head or target hidden states at training time):
+ *     loss = (1/N) sum_r weight[r] * (beta * CE_r + KD_r),   KD_r = sum_i p_i (log p_i - log q_r[id_i])
+ * over the list (id_i, t_i), i < k, of the position row r predicts: t = block_start[b] + j for row (block b, position j),
+ * or t = r when block_start is NULL.  An entry counts iff 0 <= id_i < V and t_i > -infinity (so shorter lists
+ * are filled up with id -1); p_i = exp(t_i) (renormalize = 0: t_i are log probabilities, the tail is left out), or
+ * exp(t_i) / sum_j exp(t_j) (renormalize = 1: t_i may be logits up to a constant).  The same id twice adds up.  A list without
+ * entries has KD_r = 0.  Gradients, with the weights constant and none to the lists:
+ *     dz[r, v] = g * weight[r]/N * ((beta + sum_i p_i) q_r[v] - beta [v == y_r] - sum_i p_i [v == id_i]).
+ * A row takes part iff valid[r] != 0, 0 <= y_r < V and 0 <= t < L; H of the others may hold anything.  Confidences for the
+ * weights: conf_ext, or the draft's own (for the teacher's: exp(logp) of cat_logprob_fwd through cat_conf_window).
+ * Works in row slabs of whole draft blocks with the slab's logits kept (fp16, relative to the largest logit among
+ * the list's ids and the label; fp32 for CAT_F32), at most about slab_mib MiB (default 3072), turned into dz in place.
+ */
+typedef struct {
+    int64_t L;            /* positions the lists cover                                          */
+    int64_t ld;           /* row pitch of top_ids and top_logp in elements, >= k                */
+    int32_t k;            /* entries per list, 1 .. CAT_TOPK_MAX                                */
+    int32_t renormalize;  /* 1: softmax over the list's entries; 0: entries are log probabilities */
+    float   beta;         /* weight of the cross-entropy term, finite and >= 0                   */
+    int32_t reserved;
+} cat_topk_kd_desc;
+
+/* Scratch bytes of cat_topk_kd_loss_fwd_bwd (0 if anything is invalid). */
+size_t cat_topk_kd_workspace_bytes(const cat_shape* shape, const cat_topk_kd_desc* desc);
+
+/*
+ *   shape, H, W, labels, valid, conf_ext, grad_loss, lse, conf, weight, stats, dH, dW, accumulate_dW: as in cat_loss_fwd_bwd
+ *   desc         list sizes, beta, normalisation                                          (host, in)
+ *   top_ids      [L, k] int64, top_logp [L, k] fp32, row pitch desc->ld                    (device, in)
+ *   block_start  [T / K] int64, any order, or NULL                                        (device, in)
+ *   loss         [3] fp32: total, cross-entropy part, distillation part; total = beta * loss[1] + loss[2]  (device, out)
+ *   workspace    at least cat_topk_kd_workspace_bytes(...) bytes, 256-byte aligned         (device, scratch)
+ * Nothing is read on the host but shape and desc: the call may be captured into a graph.
+ */
+int cat_topk_kd_loss_fwd_bwd(const cat_shape* shape, const cat_topk_kd_desc* desc, const void* H, const void* W,
+                             const int64_t* labels, const uint8_t* valid,
+                             const int64_t* top_ids, const float* top_logp, const int64_t* block_start,
+                             const float* conf_ext, const float* grad_loss,
+                             float* loss, float* lse, float* conf, float* weight, cat_stats* stats,
+                             void* dH, void* dW, int accumulate_dW,
+                             void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Number of kernels of this library that the given pass (0 = cat_loss_fwd, 1 = cat_loss_bwd,
  * 2 = cat_loss_fwd_bwd) launches for this shape: the logits GEMM, the per-row kernels and the final reduction in
  * the forward pass; one set-up kernel plus three GEMMs per vocabulary slab in the backward

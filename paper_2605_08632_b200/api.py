@@ -5,9 +5,42 @@ C entry points.  No arithmetic of the method happens here.
 """
 from __future__ import annotations
 
+from typing import NamedTuple
+
 import torch
 
 from . import binding as B
+
+
+def _check(name, t, shape, dtype, device, rows_only=False):
+    """Refuses a tensor the kernels would misread: its type, its sizes, its device, its layout.  `rows_only`: the rows may lie
+    further apart than they are long."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    if rows_only and t.dim() == 2:
+        if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+            raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    elif not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _mask(valid):
+    """The kernels read one byte per row: a bool mask is the same bytes."""
+    return valid.view(torch.uint8) if valid is not None and valid.dtype == torch.bool else valid
+
+
+def _pitch(t):
+    """Row pitch of a 2-D tensor; the stride of a single row means nothing."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _device(device) -> torch.device:
+    dev = torch.device(device)
+    return torch.device("cuda", torch.cuda.current_device()) if dev.index is None else dev
 
 
 class CatLoss:
@@ -34,6 +67,7 @@ class CatLoss:
         self.ws_bwd = torch.empty(nb, dtype=torch.uint8, device=dev)
         self._ws_fused = None
         self._ws_kd = None
+        self._ws_topk = None
         self.loss3 = None
         self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
         self.lse = torch.empty(T, dtype=torch.float32, device=dev)
@@ -99,6 +133,44 @@ class CatLoss:
                               self._ws_kd)
         return self.loss3, self.dH, self.dW
 
+    def topk_kd_forward_backward(self, H, W, labels, valid, top_ids, top_logp, block_start=None, beta=0.1, renormalize=True,
+                                 conf_ext=None, grad_loss=None, accumulate_dW=False):
+        """cat_topk_kd_loss_fwd_bwd: Eq. 12 with the distillation term over the teacher's stored top lists `top_ids` [L, k] int64
+        and `top_logp` [L, k] fp32 (ids of -1 fill up short lists), as TokenLogProb.forward writes them, in the place of its head.
+        Row (block b, position j) reads list block_start[b] + j (int64 [T / K], on the device), or list b * K + j without it.
+        renormalize: softmax over the list's entries; otherwise their log probabilities as they are.
+        Returns (loss3, dH, dW) with loss3 = [total, cross-entropy part, distillation part]."""
+        dev, T, d, V = self.loss.device, self.T, self.d, self.V
+        valid = _mask(valid)
+        L, k = top_ids.shape
+        _check("H", H, (T, d), self.dtype, dev)
+        _check("W", W, (V, d), self.dtype, dev)
+        _check("labels", labels, (T,), torch.int64, dev)
+        _check("top_ids", top_ids, (L, k), torch.int64, dev, rows_only=True)
+        _check("top_logp", top_logp, (L, k), torch.float32, dev, rows_only=True)
+        if _pitch(top_ids) != _pitch(top_logp):
+            raise ValueError("top_ids and top_logp must have the same row pitch")
+        for name, t, shape, dtype in (("valid", valid, (T,), torch.uint8), ("block_start", block_start, (T // self.K,), torch.int64),
+                                      ("conf_ext", conf_ext, (T,), torch.float32), ("grad_loss", grad_loss, (1,), torch.float32)):
+            if t is not None:
+                _check(name, t, shape, dtype, dev)
+        desc = B.make_topk_kd_desc(L, k, float(beta), renormalize, ld=_pitch(top_ids))
+        n = B.cat_topk_kd_workspace_bytes(self.shape, desc)
+        if n == 0:
+            raise ValueError("invalid problem for cat_topk_kd_loss_fwd_bwd")
+        with torch.cuda.device(dev):
+            if self._ws_topk is None or self._ws_topk.numel() < n:
+                self._ws_topk = torch.empty(n, dtype=torch.uint8, device=dev)
+            if self.loss3 is None:
+                self.loss3 = torch.zeros(3, dtype=torch.float32, device=dev)
+            B.cat_topk_kd_loss_fwd_bwd(self.shape, desc, H, W, labels, valid, top_ids, top_logp, block_start, conf_ext, grad_loss,
+                                       self.loss3, self.lse, self.conf, self.weight, self.stats, self.dH, self.dW, accumulate_dW,
+                                       self._ws_topk)
+        return self.loss3, self.dH, self.dW
+
+    def topk_kd_status(self) -> int:
+        return int(self._ws_topk[:4].view(torch.int32).item())
+
     def kd_status(self) -> int:
         return int(self._ws_kd[:4].view(torch.int32).item())
 
@@ -142,6 +214,148 @@ class TargetConfidence:
 
     def status(self) -> int:
         return int(self.ws[:4].view(torch.int32).item())
+
+
+class LogProbs(NamedTuple):
+    """What TokenLogProb.forward returns.  logp is None without labels, top_ids and top_logp without alternatives."""
+    logp: torch.Tensor | None        # [T] fp32
+    lse: torch.Tensor                # [T] fp32
+    entropy: torch.Tensor            # [T] fp32
+    top_ids: torch.Tensor | None     # [T, top_k] int64
+    top_logp: torch.Tensor | None    # [T, top_k] fp32
+
+
+class TokenLogProb:
+    """Buffers and calls for cat_logprob_fwd / cat_logprob_bwd: log probabilities of given tokens, entropies and the top_k most
+    likely tokens of T rows, and the gradients of the first two.  The results are the engine's own buffers: the next
+    call overwrites them.  One engine serves one stream at a time."""
+
+    def __init__(self, T: int, d: int, V: int, top_k: int = 0, dtype: torch.dtype = torch.bfloat16,
+                 dW_dtype: torch.dtype = torch.float32, slab_mib: int = 0, device: str = "cuda"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("TokenLogProb needs a CUDA device; there is no CPU path")
+        code = {torch.bfloat16: B.CAT_BF16, torch.float32: B.CAT_F32}
+        if dtype not in code or dW_dtype not in code:
+            raise TypeError("TokenLogProb takes bfloat16 or float32")
+        self.T, self.d, self.V, self.top_k, self.dtype, self.dW_dtype, self.slab_mib = T, d, V, top_k, dtype, dW_dtype, slab_mib
+        self._code = (code[dtype], code[dW_dtype])
+        n = B.cat_logprob_workspace_bytes(self._shape(d, d), top_k, 0)
+        if n == 0:
+            raise ValueError("invalid shape for cat_logprob_fwd")
+        self.device = _device(device)
+        f32 = dict(dtype=torch.float32, device=self.device)
+        self.ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+        self._ws_bwd = self.dH = self.dW = None
+        self.logp, self.lse, self.entropy = torch.empty(T, **f32), torch.empty(T, **f32), torch.empty(T, **f32)
+        self.top_ids = torch.empty(T, top_k, dtype=torch.int64, device=self.device) if top_k else None
+        self.top_logp = torch.empty(T, top_k, **f32) if top_k else None
+
+    def _shape(self, ldH, ldW):
+        return B.make_shape(self.T, self.d, self.V, 1, *self._code, ldH=ldH, ldW=ldW, slab_mib=self.slab_mib)
+
+    def _inputs(self, H, W, labels, valid):
+        _check("H", H, (self.T, self.d), self.dtype, self.device, rows_only=True)
+        _check("W", W, (self.V, self.d), self.dtype, self.device, rows_only=True)
+        if labels is not None:
+            _check("labels", labels, (self.T,), torch.int64, self.device)
+        if valid is not None:
+            _check("valid", valid, (self.T,), torch.uint8, self.device)
+
+    def forward(self, H, W, labels=None, valid=None) -> LogProbs:
+        """Rows of H and W may lie further apart than d (multiples of 8 elements for bfloat16)."""
+        valid = _mask(valid)
+        self._inputs(H, W, labels, valid)
+        logp = None if labels is None else self.logp
+        with torch.cuda.device(self.device):
+            B.cat_logprob_fwd(self._shape(_pitch(H), _pitch(W)), H, W, labels, valid, self.top_k, logp, self.lse, self.entropy,
+                              self.top_ids, self.top_logp, self.ws)
+        return LogProbs(logp, self.lse, self.entropy, self.top_ids, self.top_logp)
+
+    def backward(self, H, W, labels=None, valid=None, grad_logp=None, grad_entropy=None, lse=None, entropy=None,
+                 accumulate_dW=False):
+        """(dH, dW) for the upstream gradients of logp and entropy (either may be None).  lse and entropy: those of the forward
+        pass on the same rows; the engine's own, of its last forward, unless given."""
+        valid = _mask(valid)
+        self._inputs(H, W, labels, valid)
+        if grad_logp is not None and labels is None:
+            raise ValueError("grad_logp needs labels")
+        lse = self.lse if lse is None else lse
+        entropy = self.entropy if entropy is None else entropy
+        for name, t in (("grad_logp", grad_logp), ("grad_entropy", grad_entropy), ("lse", lse), ("entropy", entropy)):
+            if t is not None:
+                _check(name, t, (self.T,), torch.float32, self.device)
+        if _pitch(H) != self.d or _pitch(W) != self.d:
+            raise ValueError("backward takes contiguous H and W: the gradients are laid out like them")
+        shape = self._shape(self.d, self.d)
+        with torch.cuda.device(self.device):
+            if self._ws_bwd is None:
+                n = B.cat_logprob_workspace_bytes(shape, 0, 1)
+                self._ws_bwd = torch.empty(n, dtype=torch.uint8, device=self.device)
+            if self.dH is None:
+                self.dH = torch.empty(self.T, self.d, dtype=self.dtype, device=self.device)
+            if self.dW is None:
+                if accumulate_dW:
+                    raise ValueError("accumulate_dW needs a dW to add to: set engine.dW, or run one backward without it")
+                self.dW = torch.empty(self.V, self.d, dtype=self.dW_dtype, device=self.device)
+            B.cat_logprob_bwd(shape, H, W, labels, valid, lse, entropy, grad_logp, grad_entropy, self.dH, self.dW, accumulate_dW,
+                              self._ws_bwd)
+        return self.dH, self.dW
+
+    def status(self) -> int:
+        return int(self.ws[:4].view(torch.int32).item())
+
+    def bwd_status(self) -> int:
+        return int(self._ws_bwd[:4].view(torch.int32).item())
+
+
+class _LogProbFn(torch.autograd.Function):
+    """autograd glue: cat_logprob_fwd in forward(), cat_logprob_bwd in backward().  What backward() needs from the forward (lse,
+    entropy) is copied out of the engine, and the gradient buffers it wrote leave with the graph node, so further calls
+    through the same engine cannot overwrite either."""
+
+    @staticmethod
+    def forward(ctx, H, W, labels, valid, engine):
+        r = engine.forward(H.detach(), W.detach(), labels, valid)
+        lse, entropy = r.lse.clone(), r.entropy.clone()
+        ctx.engine = engine
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(H, W, labels, valid, lse, entropy)
+        logp = None if r.logp is None else r.logp.clone()
+        ids, tl = (None, None) if r.top_ids is None else (r.top_ids.clone(), r.top_logp.clone())
+        ctx.mark_non_differentiable(*(t for t in (ids, tl) if t is not None))
+        return logp, entropy.clone(), ids, tl
+
+    @staticmethod
+    def backward(ctx, g_logp, g_entropy, _ids, _tl):
+        H, W, labels, valid, lse, entropy = ctx.saved_tensors
+        e = ctx.engine
+        e.dH = e.dW = None
+        dH, dW = e.backward(H.detach(), W.detach(), labels, valid, None if g_logp is None or labels is None else g_logp.contiguous(),
+                            None if g_entropy is None else g_entropy.contiguous(), lse=lse, entropy=entropy)
+        e.dH = e.dW = None
+        return dH, dW, None, None, None
+
+
+class LogProbModule(torch.nn.Module):
+    """Head of a scoring or policy-gradient loop: `logp, entropy, top_ids, top_logp = head(H, labels, valid)` with H [T, d] and
+    `weight` [V, d] as the LM head; logp and entropy carry gradients to H and the weight.  The gradient of the weight is formed in
+    the weight's type.  One engine is kept per distinct T."""
+
+    def __init__(self, weight: torch.Tensor, top_k: int = 0, slab_mib: int = 0):
+        super().__init__()
+        self.weight = weight if isinstance(weight, torch.nn.Parameter) else torch.nn.Parameter(weight)
+        self.top_k = top_k
+        self.slab_mib = slab_mib
+        self._engines = {}
+
+    def forward(self, H, labels=None, valid=None):
+        T, d = H.shape
+        key = (T, H.device, H.dtype)
+        eng = self._engines.get(key)
+        if eng is None:
+            eng = self._engines[key] = TokenLogProb(T, d, self.weight.shape[0], self.top_k, dtype=H.dtype, dW_dtype=self.weight.dtype,
+                                                    slab_mib=self.slab_mib, device=str(H.device))
+        return _LogProbFn.apply(H, self.weight, labels, valid, eng)
 
 
 class _CatLossFn(torch.autograd.Function):

@@ -38,6 +38,14 @@ class cat_kd_desc(ctypes.Structure):
 CAT_CONF_TARGET, CAT_CONF_DRAFT = 0, 1
 
 
+class cat_topk_kd_desc(ctypes.Structure):
+    _fields_ = [("L", ctypes.c_int64), ("ld", ctypes.c_int64), ("k", ctypes.c_int32), ("renormalize", ctypes.c_int32),
+                ("beta", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+CAT_TOPK_MAX = 256
+
+
 class CatError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -88,6 +96,16 @@ def lib() -> ctypes.CDLL:
         L.cat_kd_workspace_bytes.argtypes = [ctypes.POINTER(cat_shape), ctypes.POINTER(cat_kd_desc), vp]
         L.cat_kd_loss_fwd_bwd.restype = ctypes.c_int
         L.cat_kd_loss_fwd_bwd.argtypes = [ctypes.POINTER(cat_shape), ctypes.POINTER(cat_kd_desc)] + [vp] * 16 + [ctypes.c_int, vp, sz, vp]
+        L.cat_logprob_workspace_bytes.restype = sz
+        L.cat_logprob_workspace_bytes.argtypes = [ctypes.POINTER(cat_shape), ctypes.c_int, ctypes.c_int]
+        L.cat_logprob_fwd.restype = ctypes.c_int
+        L.cat_logprob_fwd.argtypes = [ctypes.POINTER(cat_shape)] + [vp] * 4 + [ctypes.c_int32] + [vp] * 5 + [vp, sz, vp]
+        L.cat_logprob_bwd.restype = ctypes.c_int
+        L.cat_logprob_bwd.argtypes = [ctypes.POINTER(cat_shape)] + [vp] * 10 + [ctypes.c_int, vp, sz, vp]
+        L.cat_topk_kd_workspace_bytes.restype = sz
+        L.cat_topk_kd_workspace_bytes.argtypes = [ctypes.POINTER(cat_shape), ctypes.POINTER(cat_topk_kd_desc)]
+        L.cat_topk_kd_loss_fwd_bwd.restype = ctypes.c_int
+        L.cat_topk_kd_loss_fwd_bwd.argtypes = [ctypes.POINTER(cat_shape), ctypes.POINTER(cat_topk_kd_desc)] + [vp] * 16 + [ctypes.c_int, vp, sz, vp]
         L.cat_die_map.restype = ctypes.c_int
         L.cat_die_map.argtypes = [vp, ctypes.c_int, vp, vp]
         L.cat_selftest_wait_timeout.restype = ctypes.c_int
@@ -267,6 +285,45 @@ def cat_kd_loss_fwd_bwd(shape, desc, H, W, labels, valid, Ht, Wt, block_start_ho
                                    workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
     if rc != CAT_OK:
         raise CatError(rc, "cat_kd_loss_fwd_bwd")
+
+
+def cat_logprob_workspace_bytes(shape, top_k: int, which: int) -> int:
+    return int(lib().cat_logprob_workspace_bytes(ctypes.byref(shape), int(top_k), int(which)))
+
+
+def cat_logprob_fwd(shape, H, W, labels, valid, top_k, logp, lse, entropy, top_ids, top_logp, workspace) -> None:
+    rc = lib().cat_logprob_fwd(ctypes.byref(shape), _ptr(H), _ptr(W), _ptr(labels), _ptr(valid), int(top_k), _ptr(logp), _ptr(lse),
+                               _ptr(entropy), _ptr(top_ids), _ptr(top_logp), _ptr(workspace),
+                               workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+    if rc != CAT_OK:
+        raise CatError(rc, "cat_logprob_fwd")
+
+
+def cat_logprob_bwd(shape, H, W, labels, valid, lse, entropy, grad_logp, grad_entropy, dH, dW, accumulate_dW, workspace) -> None:
+    rc = lib().cat_logprob_bwd(ctypes.byref(shape), _ptr(H), _ptr(W), _ptr(labels), _ptr(valid), _ptr(lse), _ptr(entropy),
+                               _ptr(grad_logp), _ptr(grad_entropy), _ptr(dH), _ptr(dW), int(bool(accumulate_dW)), _ptr(workspace),
+                               workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+    if rc != CAT_OK:
+        raise CatError(rc, "cat_logprob_bwd")
+
+
+def make_topk_kd_desc(L, k, beta, renormalize=True, ld=None) -> cat_topk_kd_desc:
+    return cat_topk_kd_desc(L, k if ld is None else ld, k, int(bool(renormalize)), beta, 0)
+
+
+def cat_topk_kd_workspace_bytes(shape, desc) -> int:
+    return int(lib().cat_topk_kd_workspace_bytes(ctypes.byref(shape), ctypes.byref(desc)))
+
+
+def cat_topk_kd_loss_fwd_bwd(shape, desc, H, W, labels, valid, top_ids, top_logp, block_start, conf_ext, grad_loss, loss, lse,
+                             conf, weight, stats, dH, dW, accumulate_dW, workspace) -> None:
+    rc = lib().cat_topk_kd_loss_fwd_bwd(ctypes.byref(shape), ctypes.byref(desc), _ptr(H), _ptr(W), _ptr(labels), _ptr(valid),
+                                        _ptr(top_ids), _ptr(top_logp), _ptr(block_start), _ptr(conf_ext), _ptr(grad_loss),
+                                        _ptr(loss), _ptr(lse), _ptr(conf), _ptr(weight), _ptr(stats), _ptr(dH), _ptr(dW),
+                                        int(bool(accumulate_dW)), _ptr(workspace),
+                                        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+    if rc != CAT_OK:
+        raise CatError(rc, "cat_topk_kd_loss_fwd_bwd")
 
 
 def cat_die_map():

@@ -16,9 +16,11 @@
 #include <mutex>
 
 #include "kd.cuh"
+#include "logprob.cuh"
 #include "rowops.cuh"
 #include "simt.cuh"
 #include "tc_gemm.cuh"
+#include "topk_kd.cuh"
 
 // ------------------------------------------------------------------------------------------
 // Forward pass with built-in scratch, for callers that may not allocate device memory.
@@ -188,14 +190,16 @@ struct FusedPlan {
 
 long long gcd_ll(long long a, long long b) { return b == 0 ? a : gcd_ll(b, a % b); }
 
-FusedPlan plan_fused(const cat_shape* s) {
+// `two_slabs`: a batch of more than one slab unit is cut in two at least, whatever the cap allows.
+FusedPlan plan_fused(const cat_shape* s, bool two_slabs = true) {
     FusedPlan p;
     p.ldz = cdiv(s->V, 256) * 256;
     const long long L = (static_cast<long long>(s->K) * tile_m()) / gcd_ll(s->K, tile_m());   // lcm(K, rows per m-tile)
     const long long mib = s->slab_mib > 0 ? s->slab_mib : kDefaultFusedSlabMiB;
     long long cap = ((mib << 20) / (p.ldz * 2) / L) * L;       // rows that fit the slab cap
     const long long most = ((s->T - 1) / L) * L;                // at least two slabs: the T x V logits never coexist
-    if (most >= L && cap > most) cap = most;
+    if (two_slabs && most >= L && cap > most) cap = most;
+    if (!two_slabs && cap > most + L) cap = most + L;
     if (cap < L) cap = L;
     // Among slab heights within the cap take the one that costs the three GEMMs the fewest tile-steps
     // (waves of the 74 tile-workers x k-slices per tile, summed over the slabs): the logits GEMM (items are
@@ -913,10 +917,20 @@ int cat_loss_fwd(const cat_shape* shape, const void* H, const void* W, const int
 
 // cat_loss_bwd / cat_loss_bwd_events: `slab_events` (host array of cudaEvent_t, one per vocabulary
 // slab, or NULL) are recorded on the stream as soon as a slab's rows of dW are final.
+// `lp`: the gradients of cat_logprob_bwd instead of the CAT loss's (another dz, no 1/N).
+struct LpArgs {
+    const float* entropy;
+    const float* grad_logp;
+    const float* grad_entropy;
+};
+static size_t lp_bwd_bytes(const cat_shape* s) {       // the plain backward's scratch and a copy of H without its masked rows
+    return align256(plan_bwd(s).total) + align256((s->in_dtype == CAT_BF16 ? 2 : 4) * static_cast<size_t>(s->T) * static_cast<size_t>(s->d));
+}
 static int bwd_core(const cat_shape* shape, const void* H, const void* W, const int64_t* labels, const uint8_t* valid,
                     const float* lse, const float* weight, const float* grad_loss, void* dH, void* dW, int accumulate_dW,
-                    void* workspace, size_t workspace_bytes, void* cuda_stream, void* const* slab_events) {
-    if (!shape || !H || !W || !labels || !lse || !weight || !dH || !dW) return CAT_ERR_NULL;
+                    void* workspace, size_t workspace_bytes, void* cuda_stream, void* const* slab_events, const LpArgs* lp = nullptr) {
+    if (!shape || !H || !W || !lse || !dH || !dW) return CAT_ERR_NULL;
+    if (lp ? (lp->grad_logp && !labels) || (lp->grad_entropy && !lp->entropy) : !labels || !weight) return CAT_ERR_NULL;
     const int sc = check_shape(shape);
     if (sc != CAT_OK) return sc;
     const bool bf16 = shape->in_dtype == CAT_BF16;
@@ -924,8 +938,9 @@ static int bwd_core(const cat_shape* shape, const void* H, const void* W, const 
     if (misaligned(H, in_al) || misaligned(W, in_al) || misaligned(dH, in_al) || misaligned(dW, 16) || misaligned(labels, 8) ||
         misaligned(lse, 4) || misaligned(weight, 4) || (grad_loss && misaligned(grad_loss, 4)))
         return CAT_ERR_ALIGN;
+    if (lp && (misaligned(lp->entropy, 4) || misaligned(lp->grad_logp, 4) || misaligned(lp->grad_entropy, 4))) return CAT_ERR_ALIGN;
     const BwdPlan plan = plan_bwd(shape);
-    if (!workspace || misaligned(workspace, 256) || workspace_bytes < plan.total) return CAT_ERR_WORKSPACE;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < (lp ? lp_bwd_bytes(shape) : plan.total)) return CAT_ERR_WORKSPACE;
     int sm_count = 0;
     const int dc = check_device(&sm_count);
     if (dc != CAT_OK) return dc;
@@ -937,15 +952,26 @@ static int bwd_core(const cat_shape* shape, const void* H, const void* W, const 
     const int T = static_cast<int>(shape->T), V = static_cast<int>(shape->V), d = static_cast<int>(shape->d);
     const long long* y = reinterpret_cast<const long long*>(labels);
 
+    // the right operand of dW: H, or a copy in which masked rows are zero whatever the caller left in them
+    const bool copy_H = lp && valid;
+    const void* Hw = copy_H ? static_cast<const void*>(ws + align256(plan.total)) : H;
+    const long long ldHw = copy_H ? shape->d : shape->ldH;
     // tensor maps that do not depend on the slab
     CUtensorMap tmH_k, tmH_mn;
     if (bf16) {
         if (tmap_a(&tmH_k, H, shape->T, shape->d, shape->ldH) != CAT_OK) return CAT_ERR_CUDA;
-        if (tmap_mn_major(&tmH_mn, H, shape->T, shape->d, shape->ldH) != CAT_OK) return CAT_ERR_CUDA;
+        if (tmap_mn_major(&tmH_mn, Hw, shape->T, shape->d, ldHw) != CAT_OK) return CAT_ERR_CUDA;
     }
     if (cudaMemsetAsync(ws, 0, kHeaderBytes, st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
-    rows::bwd_scale_kernel<<<1, 1024, 0, st>>>(y, valid, T, V, grad_loss, scale);
+    if (!lp) rows::bwd_scale_kernel<<<1, 1024, 0, st>>>(y, valid, T, V, grad_loss, scale);
+    else if (copy_H && bf16)
+        lp::masked_copy_kernel<<<static_cast<unsigned>(T), lp::THREADS, 0, st>>>(
+            static_cast<const __nv_bfloat16*>(H), shape->ldH, d, valid, reinterpret_cast<__nv_bfloat16*>(ws + align256(plan.total)));
+    else if (copy_H)
+        lp::masked_copy_kernel<<<static_cast<unsigned>(T), lp::THREADS, 0, st>>>(
+            static_cast<const float*>(H), shape->ldH, d, valid, reinterpret_cast<float*>(ws + align256(plan.total)));
     if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
+    if (lp) scale = nullptr;
 
     for (int sl = 0; sl < plan.n_slabs; ++sl) {
         const long long v0 = static_cast<long long>(sl) * plan.Vs;
@@ -964,12 +990,20 @@ static int bwd_core(const cat_shape* shape, const void* H, const void* W, const 
                 // same item shape as the forward pass: (m-tile, run of vocabulary tiles), so the per-row state
                 // (label, lse, weight) is loaded once per run
                 const tc::Sched sched = make_sched(shape->T, width, shape->d, fwd_splits(shape->T, width), band_tiles(shape->d), 0);
-                tc::EpiDz::Params ep;
-                ep.labels = y; ep.valid = valid; ep.lse = lse; ep.weight = weight; ep.dz = dz; ep.ld = plan.Vs;
-                ep.T = T; ep.V = V; ep.v0 = static_cast<int>(v0);
                 CUtensorMap tmDz_out;
                 if (tmap_out(&tmDz_out, dz, shape->T, width, plan.Vs) != CAT_OK) return CAT_ERR_CUDA;
-                const int rc = launch_tc<0, 0, tc::EpiDz>(tmH_k, tmW_k, sched, ep, status, sm_count, st, &tmDz_out);
+                int rc;
+                if (lp) {
+                    tc::EpiDzLp::Params ep;
+                    ep.labels = y; ep.valid = valid; ep.lse = lse; ep.entropy = lp->entropy; ep.grad_logp = lp->grad_logp;
+                    ep.grad_entropy = lp->grad_entropy; ep.T = T; ep.V = V; ep.v0 = static_cast<int>(v0);
+                    rc = launch_tc<0, 0, tc::EpiDzLp>(tmH_k, tmW_k, sched, ep, status, sm_count, st, &tmDz_out);
+                } else {
+                    tc::EpiDz::Params ep;
+                    ep.labels = y; ep.valid = valid; ep.lse = lse; ep.weight = weight; ep.dz = dz; ep.ld = plan.Vs;
+                    ep.T = T; ep.V = V; ep.v0 = static_cast<int>(v0);
+                    rc = launch_tc<0, 0, tc::EpiDz>(tmH_k, tmW_k, sched, ep, status, sm_count, st, &tmDz_out);
+                }
                 if (rc != CAT_OK) return rc;
             }
             {   // dW[v0 : v0 + width, :] = (g/N) dz^T H
@@ -1013,11 +1047,16 @@ static int bwd_core(const cat_shape* shape, const void* H, const void* W, const 
                 ep.labels = y; ep.valid = valid; ep.lse = lse; ep.weight = weight; ep.dz = dz; ep.ld_dz = plan.Vs;
                 ep.V = V; ep.v0 = static_cast<int>(v0);
                 const dim3 grid(static_cast<unsigned>(cdiv(T, simt::TM)), static_cast<unsigned>(op.n_groups));
-                simt::gemm_kernel<simt::MODE_DZ><<<grid, simt::THREADS, 0, st>>>(op, ep);
+                if (lp) {
+                    ep.entropy = lp->entropy; ep.grad_logp = lp->grad_logp; ep.grad_entropy = lp->grad_entropy;
+                    simt::gemm_kernel<simt::MODE_DZ_LP><<<grid, simt::THREADS, 0, st>>>(op, ep);
+                } else {
+                    simt::gemm_kernel<simt::MODE_DZ><<<grid, simt::THREADS, 0, st>>>(op, ep);
+                }
             }
             {   // dW slice = (g/N) dz^T H : A(m = v, k = r) = dz[r][v], B(k = r, n = i) = H[r][i]
                 simt::Operands op;
-                op.A = dz; op.sAm = 1; op.sAk = plan.Vs; op.B = Hf; op.sBk = shape->ldH; op.sBn = 1;
+                op.A = dz; op.sAm = 1; op.sAk = plan.Vs; op.B = static_cast<const float*>(Hw); op.sBk = ldHw; op.sBn = 1;
                 op.M = w; op.N = d; op.Kd = T; op.n_groups = static_cast<int>(cdiv(d, simt::TN));
                 simt::EpiParams ep;
                 memset(&ep, 0, sizeof(ep));
@@ -1247,3 +1286,5 @@ int cat_selftest_wait_timeout(int role, uint64_t short_ns, uint64_t long_ns, int
 }
 
 }  // extern "C"
+
+#include "head_ops.cuh"

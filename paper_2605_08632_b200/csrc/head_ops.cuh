@@ -1,0 +1,433 @@
+// Host side of the LM-head operators beside the CAT loss: cat_logprob_fwd / cat_logprob_bwd and
+// cat_topk_kd_loss_fwd_bwd.  Included at the end of cat_api.cu, whose planning, tensor-map and launch helpers it uses.
+#pragma once
+
+namespace {
+
+static_assert(CAT_TOPK_MAX == lp::MAX_TOP && lp::MAX_TOP == lp::THREADS, "one thread per list entry");
+
+// ------------------------------------------------------------------------------ log probabilities
+struct LpPlan {
+    long long Ts;          // rows per slab
+    long long ldz;         // row pitch of the logits slab
+    long long ld_g;        // row pitch of the group maxima
+    int group;             // columns per maximum
+    int n_slabs;
+    int S;                 // vocabulary splits of a full slab (the most any slab uses)
+    size_t off_m, off_l, off_u, off_g, off_z, total;
+};
+
+int simt_splits(long long rows, long long V) {
+    long long S = (2 * kPlanSMs) / cdiv(rows, simt::TM);
+    const long long num_n = cdiv(V, simt::TN);
+    if (S > num_n) S = num_n;
+    if (S > 64) S = 64;
+    return static_cast<int>(S < 1 ? 1 : S);
+}
+int head_splits(const cat_shape* s, long long rows) {
+    return s->in_dtype == CAT_BF16 ? fwd_splits(rows, s->V) : simt_splits(rows, s->V);
+}
+
+LpPlan plan_lp(const cat_shape* s, int top_k) {
+    LpPlan p;
+    const bool bf16 = s->in_dtype == CAT_BF16;
+    const long long tile = bf16 ? tile_m() : simt::TM;
+    p.group = bf16 ? tc::LP_GROUP : simt::TN;
+    p.ldz = cdiv(s->V, 256) * 256;
+    p.ld_g = bf16 ? cdiv(s->V, tc::BN) * (tc::BN / tc::LP_GROUP) : cdiv(s->V, simt::TN);
+    p.Ts = s->T;
+    if (top_k > 0) {
+        const long long mib = s->slab_mib > 0 ? s->slab_mib : kDefaultFusedSlabMiB;
+        long long cap = (mib << 20) / (p.ldz * (bf16 ? 2 : 4)) / tile * tile;
+        if (cap < tile) cap = tile;
+        if (cap < s->T) p.Ts = cdiv(cdiv(s->T, cdiv(s->T, cap)), tile) * tile;      // slabs of even height
+    }
+    p.n_slabs = static_cast<int>(cdiv(s->T, p.Ts));
+    p.S = head_splits(s, p.Ts);
+    const long long rest = s->T - (p.n_slabs - 1) * p.Ts;
+    if (head_splits(s, rest) > p.S) p.S = head_splits(s, rest);
+    size_t off = kHeaderBytes;
+    p.off_m = off; off = align256(off + sizeof(float) * p.S * p.Ts);
+    p.off_l = off; off = align256(off + sizeof(float) * p.S * p.Ts);
+    p.off_u = off; off = align256(off + sizeof(float) * p.S * p.Ts);
+    p.off_g = off; if (top_k > 0) off = align256(off + sizeof(float) * static_cast<size_t>(p.Ts) * p.ld_g);
+    p.off_z = off; if (top_k > 0) off = align256(off + (bf16 ? 2 : 4) * static_cast<size_t>(p.Ts) * p.ldz);
+    p.total = off;
+    return p;
+}
+
+template <class TI, class TZ, bool TOP>
+int launch_lp_rows(const cat_shape* s, const LpPlan& plan, const TI* H, const TI* W, long long r0, long long rws, int S, uint8_t* ws,
+                   const int64_t* labels, const uint8_t* valid, int top_k, float* logp, float* lse, float* entropy,
+                   int64_t* top_ids, float* top_logp, cudaStream_t st) {
+    lp::RowParams<TI, TZ> rp;
+    memset(&rp, 0, sizeof(rp));
+    rp.part_m = reinterpret_cast<float*>(ws + plan.off_m);
+    rp.part_l = reinterpret_cast<float*>(ws + plan.off_l);
+    rp.part_u = reinterpret_cast<float*>(ws + plan.off_u);
+    rp.part_stride = s->in_dtype == CAT_BF16 ? plan.Ts : rws;
+    rp.S = S;
+    rp.H = H; rp.W = W; rp.ldH = s->ldH; rp.ldW = s->ldW;
+    rp.d = static_cast<int>(s->d); rp.V = static_cast<int>(s->V);
+    rp.labels = labels ? reinterpret_cast<const long long*>(labels) + r0 : nullptr;
+    rp.valid = valid ? valid + r0 : nullptr;
+    rp.logp = logp ? logp + r0 : nullptr;
+    rp.lse = lse + r0;
+    rp.entropy = entropy + r0;
+    if (TOP) {
+        rp.zs = reinterpret_cast<const TZ*>(ws + plan.off_z);
+        rp.ldz = plan.ldz;
+        rp.gmax = reinterpret_cast<const float*>(ws + plan.off_g);
+        rp.ld_g = plan.ld_g;
+        rp.n_g = static_cast<int>(cdiv(s->V, plan.group));
+        rp.group = plan.group;
+        rp.k = top_k;
+        rp.top_ids = reinterpret_cast<long long*>(top_ids) + r0 * top_k;
+        rp.top_logp = top_logp + r0 * top_k;
+    }
+    lp::row_kernel<TI, TZ, TOP><<<static_cast<unsigned>(rws), lp::THREADS, 0, st>>>(rp);
+    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+}
+
+template <bool TOP>
+int lp_slab(const cat_shape* s, const LpPlan& plan, const CUtensorMap& tmW, const void* H, const void* W, long long r0, long long rws,
+            uint8_t* ws, const int64_t* labels, const uint8_t* valid, int top_k, float* logp, float* lse, float* entropy,
+            int64_t* top_ids, float* top_logp, int sm_count, cudaStream_t st) {
+    const int S = head_splits(s, rws);
+    float* part_m = reinterpret_cast<float*>(ws + plan.off_m);
+    float* part_l = reinterpret_cast<float*>(ws + plan.off_l);
+    float* part_u = reinterpret_cast<float*>(ws + plan.off_u);
+    if (s->in_dtype == CAT_BF16) {
+        const __nv_bfloat16* Hs = static_cast<const __nv_bfloat16*>(H) + r0 * s->ldH;
+        CUtensorMap tmH, tmZ;
+        if (tmap_a(&tmH, Hs, rws, s->d, s->ldH) != CAT_OK) return CAT_ERR_CUDA;
+        if (TOP && tmap_out(&tmZ, ws + plan.off_z, rws, s->V, plan.ldz) != CAT_OK) return CAT_ERR_CUDA;
+        const tc::Sched sched = make_sched(rws, s->V, s->d, S, band_tiles(s->d), 0);
+        typename tc::EpiLp<TOP>::Params ep;
+        ep.part_m = part_m; ep.part_l = part_l; ep.part_u = part_u; ep.part_stride = plan.Ts;
+        ep.gmax = reinterpret_cast<float*>(ws + plan.off_g); ep.ld_g = plan.ld_g;
+        ep.T = static_cast<int>(rws); ep.V = static_cast<int>(s->V);
+        const int rc = launch_tc<0, 0, tc::EpiLp<TOP>>(tmH, tmW, sched, ep, reinterpret_cast<int*>(ws), sm_count, st, TOP ? &tmZ : nullptr);
+        if (rc != CAT_OK) return rc;
+        return launch_lp_rows<__nv_bfloat16, __half, TOP>(s, plan, Hs, static_cast<const __nv_bfloat16*>(W), r0, rws, S, ws, labels, valid,
+                                                          top_k, logp, lse, entropy, top_ids, top_logp, st);
+    }
+    const float* Hs = static_cast<const float*>(H) + r0 * s->ldH;
+    simt::Operands op;
+    op.A = Hs; op.sAm = s->ldH; op.sAk = 1; op.B = static_cast<const float*>(W); op.sBk = 1; op.sBn = s->ldW;
+    op.M = static_cast<int>(rws); op.N = static_cast<int>(s->V); op.Kd = static_cast<int>(s->d); op.n_groups = S;
+    simt::EpiParams ep;
+    memset(&ep, 0, sizeof(ep));
+    ep.part_m = part_m; ep.part_l = part_l; ep.part_u = part_u; ep.V = static_cast<int>(s->V);
+    if (TOP) {
+        ep.zs = reinterpret_cast<float*>(ws + plan.off_z); ep.ld_z = plan.ldz;
+        ep.gmax = reinterpret_cast<float*>(ws + plan.off_g); ep.ld_g = plan.ld_g;
+    }
+    const dim3 grid(static_cast<unsigned>(cdiv(rws, simt::TM)), static_cast<unsigned>(S));
+    simt::gemm_kernel<simt::MODE_FWD_KEEP><<<grid, simt::THREADS, 0, st>>>(op, ep);
+    if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
+    return launch_lp_rows<float, float, TOP>(s, plan, Hs, static_cast<const float*>(W), r0, rws, S, ws, labels, valid, top_k, logp, lse,
+                                             entropy, top_ids, top_logp, st);
+}
+
+// ------------------------------------------------------------------------------ distillation from top logits
+int check_topk_kd(const cat_topk_kd_desc* k) {
+    if (!k) return CAT_ERR_NULL;
+    if (k->L <= 0 || k->L >= (1ll << 31) || k->k < 1 || k->k > CAT_TOPK_MAX || k->ld < k->k) return CAT_ERR_SHAPE;
+    if (!(k->beta >= 0.f && k->beta <= 3.0e38f)) return CAT_ERR_SHAPE;
+    if (k->renormalize != 0 && k->renormalize != 1) return CAT_ERR_SHAPE;
+    return CAT_OK;
+}
+
+struct TkPlan {
+    FusedPlan f;
+    int ld_zt;             // k + 1 logits per row: the list's and the label's
+    size_t off_valid, off_zt, off_kd_row, total;
+};
+
+TkPlan plan_tk(const cat_shape* s, int k) {
+    TkPlan p;
+    if (s->in_dtype == CAT_BF16) {
+        p.f = plan_fused(s, false);
+    } else {
+        FusedPlan& f = p.f;
+        memset(&f, 0, sizeof(f));
+        f.ldz = cdiv(s->V, 8) * 8;
+        const long long mib = s->slab_mib > 0 ? s->slab_mib : kDefaultFusedSlabMiB;
+        long long cap = (mib << 20) / (f.ldz * 4) / s->K * s->K;
+        if (cap < s->K) cap = s->K;
+        f.Ts = cap < s->T ? cap : s->T;
+        f.n_slabs = static_cast<int>(cdiv(s->T, f.Ts));
+        f.warp_scan = s->K <= 32 && (s->K & (s->K - 1)) == 0;
+        f.S_max = 1;
+        for (long long r0 = 0; r0 < s->T; r0 += f.Ts) {
+            const long long rws = (s->T - r0) < f.Ts ? (s->T - r0) : f.Ts;
+            const int S = simt_splits(rws, s->V);
+            if (S > f.S_max) f.S_max = S;
+            f.n_row_ctas += static_cast<int>(cdiv(f.warp_scan ? rws : rws / s->K, rows::ROW_THREADS));
+        }
+        size_t off = kHeaderBytes;
+        f.off_part_m = off;   off = align256(off + sizeof(float) * f.S_max * f.Ts);
+        f.off_part_l = off;   off = align256(off + sizeof(float) * f.S_max * f.Ts);
+        f.off_z_label = off;  off = align256(off + sizeof(float) * s->T);
+        f.off_row_ce = off;   off = align256(off + sizeof(float) * s->T);
+        f.off_partials = off; off = align256(off + sizeof(rows::CtaPartial) * f.n_row_ctas);
+        f.off_ref = off;      off = align256(off + sizeof(float) * s->T);
+        f.off_hs = off;       off = align256(off + sizeof(float) * static_cast<size_t>(f.Ts) * static_cast<size_t>(s->d));
+        f.off_z = off;        off = align256(off + sizeof(float) * static_cast<size_t>(f.Ts) * f.ldz);
+        f.total = off;
+    }
+    p.ld_zt = k + 1;
+    size_t off = align256(p.f.total);
+    p.off_valid = off;  off = align256(off + static_cast<size_t>(s->T));
+    p.off_zt = off;     off = align256(off + sizeof(float) * static_cast<size_t>(p.f.Ts) * p.ld_zt);
+    p.off_kd_row = off; off = align256(off + sizeof(float) * s->T);
+    p.total = off;
+    return p;
+}
+
+// dH[r0 : r0 + rws, :] = (g/N) dz W and dW (+)= (g/N) dz^T Hw of one row slab; Hw: the slab's rows of H with pitch ldHw.
+int slab_grads(const cat_shape* s, const FusedPlan& f, const void* W, const void* Hw, long long ldHw, void* zs, uint8_t* ws, long long r0,
+               long long rws, bool first, bool last, const float* scale, void* dH, void* dW, int accumulate_dW, int sm_count,
+               cudaStream_t st) {
+    const int V = static_cast<int>(s->V), d = static_cast<int>(s->d), R = static_cast<int>(rws);
+    if (s->in_dtype != CAT_BF16) {
+        float* dz = static_cast<float*>(zs);
+        simt::Operands op;
+        simt::EpiParams ep;
+        op.A = dz; op.sAm = f.ldz; op.sAk = 1; op.B = static_cast<const float*>(W); op.sBk = s->ldW; op.sBn = 1;
+        op.M = R; op.N = d; op.Kd = V; op.n_groups = static_cast<int>(cdiv(d, simt::TN));
+        memset(&ep, 0, sizeof(ep));
+        ep.alpha = scale; ep.out = static_cast<float*>(dH) + r0 * s->ldH; ep.ld_out = s->ldH;
+        simt::gemm_kernel<simt::MODE_OUT><<<dim3(static_cast<unsigned>(cdiv(R, simt::TM)), static_cast<unsigned>(op.n_groups)), simt::THREADS, 0, st>>>(op, ep);
+        op.A = dz; op.sAm = 1; op.sAk = f.ldz; op.B = static_cast<const float*>(Hw); op.sBk = ldHw; op.sBn = 1;
+        op.M = V; op.N = d; op.Kd = R;
+        ep.out = static_cast<float*>(dW); ep.ld_out = s->ldW;
+        if (!first || accumulate_dW) { ep.add = ep.out; ep.ld_add = s->ldW; }
+        simt::gemm_kernel<simt::MODE_OUT><<<dim3(static_cast<unsigned>(cdiv(V, simt::TM)), static_cast<unsigned>(op.n_groups)), simt::THREADS, 0, st>>>(op, ep);
+        return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+    }
+    int* status = reinterpret_cast<int*>(ws);
+    CUtensorMap tmZ_k, tmZ_mn, tmW_mn, tmH_mn;
+    if (tmap_a(&tmZ_k, zs, rws, s->V, f.ldz) != CAT_OK || tmap_mn_major(&tmZ_mn, zs, rws, s->V, f.ldz) != CAT_OK ||
+        tmap_mn_major(&tmW_mn, W, s->V, s->d, s->ldW) != CAT_OK || tmap_mn_major(&tmH_mn, Hw, rws, s->d, ldHw) != CAT_OK)
+        return CAT_ERR_CUDA;
+    tc::EpiOut::Params ep;
+    memset(&ep, 0, sizeof(ep));
+    ep.alpha = scale; ep.M = R; ep.N = d;
+    ep.out_bf16 = static_cast<__nv_bfloat16*>(dH) + r0 * s->ldH; ep.ld_out = s->ldH;
+    int rc = launch_out<0, 1>(tmZ_k, tmW_mn, make_sched(rws, s->d, s->V, 0, 1, 1), ep, status, sm_count, st);
+    if (rc != CAT_OK) return rc;
+    memset(&ep, 0, sizeof(ep));
+    ep.alpha = scale; ep.M = V; ep.N = d;
+    float* dw_acc = reinterpret_cast<float*>(ws + f.off_dw_acc);
+    if (s->dW_dtype == CAT_F32) {
+        ep.out_f32 = static_cast<float*>(dW); ep.ld_out = s->ldW;
+        if (!first || accumulate_dW) { ep.add_f32 = ep.out_f32; ep.ld_add = s->ldW; }
+    } else {        // bf16 dW: several slabs are summed in fp32 scratch and rounded once at the end
+        if (first) {
+            if (accumulate_dW) { ep.add_bf16 = static_cast<const __nv_bfloat16*>(dW); ep.ld_add = s->ldW; }
+        } else {
+            ep.add_f32 = dw_acc; ep.ld_add = s->d;
+        }
+        if (last) { ep.out_bf16 = static_cast<__nv_bfloat16*>(dW); ep.ld_out = s->ldW; }
+        else { ep.out_f32 = dw_acc; ep.ld_out = s->d; }
+    }
+    return launch_out<1, 1>(tmZ_mn, tmH_mn, make_sched(s->V, s->d, rws, 0, 1, 1), ep, status, sm_count, st);
+}
+
+template <class TI>
+int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan, const TI* H, const TI* W, const int64_t* labels,
+            const uint8_t* valid, const int64_t* top_ids, const float* top_logp, const int64_t* block_start, const float* conf_ext,
+            const float* grad_loss, float* loss, float* lse, float* conf, float* weight, cat_stats* stats, void* dH, void* dW,
+            int accumulate_dW, uint8_t* ws, int sm_count, cudaStream_t st) {
+    constexpr bool BF16 = sizeof(TI) == 2;
+    const FusedPlan& f = plan.f;
+    int* status = reinterpret_cast<int*>(ws);
+    float* scale = reinterpret_cast<float*>(ws + kScaleOffset);
+    float* part_m = reinterpret_cast<float*>(ws + f.off_part_m);
+    float* part_l = reinterpret_cast<float*>(ws + f.off_part_l);
+    float* z_label = reinterpret_cast<float*>(ws + f.off_z_label);
+    float* row_ce = reinterpret_cast<float*>(ws + f.off_row_ce);
+    float* ref = reinterpret_cast<float*>(ws + f.off_ref);
+    float* zt = reinterpret_cast<float*>(ws + plan.off_zt);
+    float* kd_row = reinterpret_cast<float*>(ws + plan.off_kd_row);
+    unsigned char* ok = ws + plan.off_valid;
+    TI* Hz = reinterpret_cast<TI*>(ws + f.off_hs);
+    rows::CtaPartial* partials = reinterpret_cast<rows::CtaPartial*>(ws + f.off_partials);
+    void* zs = ws + f.off_z;
+    const int T = static_cast<int>(s->T), V = static_cast<int>(s->V), d = static_cast<int>(s->d), K = s->K;
+    const long long* y = reinterpret_cast<const long long*>(labels);
+    tk::Lists lists;
+    lists.ids = reinterpret_cast<const long long*>(top_ids); lists.logp = top_logp;
+    lists.block_start = reinterpret_cast<const long long*>(block_start);
+    lists.ld = desc->ld; lists.k = desc->k; lists.K = K; lists.V = V; lists.renorm = desc->renormalize;
+
+    CUtensorMap tmW_k;
+    if (BF16 && tmap_b(&tmW_k, W, s->V, s->d, s->ldW) != CAT_OK) return CAT_ERR_CUDA;
+    if (cudaMemsetAsync(ws, 0, kHeaderBytes, st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
+    tk::prepare_kernel<<<static_cast<unsigned>(cdiv(T, tk::THREADS)), tk::THREADS, 0, st>>>(
+        y, valid, lists.block_start, T, K, V, desc->L, ok);
+    rows::bwd_scale_kernel<<<1, 1024, 0, st>>>(y, ok, T, V, grad_loss, scale);
+    if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
+    int cta0 = 0;
+    for (int sl = 0; sl < f.n_slabs; ++sl) {
+        const long long r0 = static_cast<long long>(sl) * f.Ts;
+        const long long rws = (s->T - r0) < f.Ts ? (s->T - r0) : f.Ts;
+        const int S = head_splits(s, rws);
+        const TI* Hs = H + r0 * s->ldH;
+        tk::gather_kernel<TI><<<static_cast<unsigned>(rws), tk::THREADS, 0, st>>>(Hs, s->ldH, W, s->ldW, d, y, ok, lists, r0, zt,
+                                                                                plan.ld_zt, ref);
+        // rows that take no part may hold anything: they meet dz = 0 in the dW contraction as zeros
+        lp::masked_copy_kernel<TI><<<static_cast<unsigned>(rws), lp::THREADS, 0, st>>>(Hs, s->ldH, d, ok + r0, Hz);
+        if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
+        rows::RowParams rp;
+        memset(&rp, 0, sizeof(rp));
+        if (BF16) {
+            CUtensorMap tmH_k, tmZ_out;
+            if (tmap_a(&tmH_k, Hs, rws, s->d, s->ldH) != CAT_OK || tmap_out(&tmZ_out, zs, rws, s->V, f.ldz) != CAT_OK) return CAT_ERR_CUDA;
+            tc::EpiFwdRef::Params ep;
+            ep.labels = y + r0; ep.part_m = part_m + r0; ep.part_l = part_l + r0; ep.z_label = z_label + r0; ep.ref = ref + r0;
+            ep.part_stride = T; ep.T = static_cast<int>(rws); ep.V = V;
+            const int rc = launch_tc<0, 0, tc::EpiFwdRef>(tmH_k, tmW_k, make_sched(rws, s->V, s->d, S, band_tiles(s->d), 0), ep, status,
+                                                          sm_count, st, &tmZ_out);
+            if (rc != CAT_OK) return rc;
+            rp.part_m = ep.part_m; rp.part_l = ep.part_l; rp.part_stride = T;
+        } else {
+            simt::Operands op;
+            op.A = reinterpret_cast<const float*>(Hs); op.sAm = s->ldH; op.sAk = 1;
+            op.B = reinterpret_cast<const float*>(W); op.sBk = 1; op.sBn = s->ldW;
+            op.M = static_cast<int>(rws); op.N = V; op.Kd = d; op.n_groups = S;
+            simt::EpiParams ep;
+            memset(&ep, 0, sizeof(ep));
+            ep.labels = y + r0; ep.part_m = part_m; ep.part_l = part_l; ep.z_label = z_label + r0; ep.V = V;
+            ep.zs = static_cast<float*>(zs); ep.ld_z = f.ldz;
+            simt::gemm_kernel<simt::MODE_FWD_KEEP><<<dim3(static_cast<unsigned>(cdiv(rws, simt::TM)), static_cast<unsigned>(S)), simt::THREADS, 0, st>>>(op, ep);
+            rp.part_m = part_m; rp.part_l = part_l; rp.part_stride = rws;
+        }
+        // lse, confidence (Eq. 9), CAT weights (Eq. 10), cross-entropy partials of the slab's blocks
+        rp.z_label = z_label + r0; rp.labels = y + r0; rp.valid = ok + r0; rp.conf_ext = conf_ext ? conf_ext + r0 : nullptr;
+        rp.lse = lse + r0; rp.conf = conf + r0; rp.weight = weight + r0; rp.row_ce = row_ce + r0; rp.partials = partials + cta0;
+        rp.T = static_cast<int>(rws); rp.V = V; rp.K = K; rp.S = S;
+        rp.fixed_decay = s->weight_mode == CAT_WEIGHT_FIXED_DECAY; rp.gamma = s->decay_gamma;
+        int n_ctas;
+        if (f.warp_scan) {
+            n_ctas = static_cast<int>(cdiv(rws, rows::ROW_THREADS));
+            rows::row_kernel<true><<<n_ctas, rows::ROW_THREADS, 0, st>>>(rp);
+        } else {
+            n_ctas = static_cast<int>(cdiv(rws / K, rows::ROW_THREADS));
+            rows::row_kernel<false><<<static_cast<unsigned>(cdiv(rws, rows::ROW_THREADS)), rows::ROW_THREADS, 0, st>>>(rp);
+            rows::block_scan_kernel<<<n_ctas, rows::ROW_THREADS, 0, st>>>(rp);
+        }
+        cta0 += n_ctas;
+        tk::dz_kernel<!BF16><<<static_cast<unsigned>(rws), tk::THREADS, 0, st>>>(zs, f.ldz, y, ok, lists, r0, lse, weight, zt, plan.ld_zt,
+                                                                               ref, desc->beta, kd_row, V);
+        if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
+        const int rc = slab_grads(s, f, W, Hz, s->d, zs, ws, r0, rws, sl == 0, sl == f.n_slabs - 1, scale, dH, dW, accumulate_dW,
+                                  sm_count, st);
+        if (rc != CAT_OK) return rc;
+    }
+    rows::finalize_kernel<<<1, rows::ROW_THREADS, 0, st>>>(partials, cta0, T / K, loss, reinterpret_cast<rows::StatsOut*>(stats), status);
+    kd::finalize_kernel<<<1, rows::ROW_THREADS, 0, st>>>(kd_row, ok, T, desc->beta, loss);
+    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t cat_logprob_workspace_bytes(const cat_shape* shape, int top_k, int pass) {
+    if (!shape) return 0;
+    cat_shape one = per_position_shape(shape);
+    one.dW_dtype = shape->dW_dtype;
+    if (check_shape(&one) != CAT_OK || top_k < 0 || top_k > CAT_TOPK_MAX) return 0;
+    if (pass == 0) return plan_lp(&one, top_k).total;
+    if (pass == 1) return lp_bwd_bytes(&one);
+    return 0;
+}
+
+int cat_logprob_fwd(const cat_shape* shape, const void* H, const void* W, const int64_t* labels, const uint8_t* valid, int32_t top_k,
+                    float* logp, float* lse, float* entropy, int64_t* top_ids, float* top_logp, void* workspace,
+                    size_t workspace_bytes, void* cuda_stream) {
+    if (!shape || !H || !W || !lse || !entropy || (labels == nullptr) != (logp == nullptr)) return CAT_ERR_NULL;
+    const cat_shape one = per_position_shape(shape);
+    const int sc = check_shape(&one);
+    if (sc != CAT_OK) return sc;
+    if (top_k < 0 || top_k > CAT_TOPK_MAX) return CAT_ERR_SHAPE;
+    if (top_k > 0 && (!top_ids || !top_logp)) return CAT_ERR_NULL;
+    const size_t in_al = one.in_dtype == CAT_BF16 ? 16 : 4;
+    if (misaligned(H, in_al) || misaligned(W, in_al) || misaligned(labels, 8) || misaligned(logp, 4) || misaligned(lse, 4) ||
+        misaligned(entropy, 4) || misaligned(top_ids, 8) || misaligned(top_logp, 4))
+        return CAT_ERR_ALIGN;
+    const LpPlan plan = plan_lp(&one, top_k);
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < plan.total) return CAT_ERR_WORKSPACE;
+    int sm_count = 0;
+    const int dc = check_device(&sm_count);
+    if (dc != CAT_OK) return dc;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    CUtensorMap tmW;
+    memset(&tmW, 0, sizeof(tmW));
+    if (one.in_dtype == CAT_BF16 && tmap_b(&tmW, W, one.V, one.d, one.ldW) != CAT_OK) return CAT_ERR_CUDA;
+    if (cudaMemsetAsync(ws, 0, kHeaderBytes, st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
+    for (int sl = 0; sl < plan.n_slabs; ++sl) {
+        const long long r0 = static_cast<long long>(sl) * plan.Ts;
+        const long long rws = (one.T - r0) < plan.Ts ? (one.T - r0) : plan.Ts;
+        const int rc = top_k > 0 ? lp_slab<true>(&one, plan, tmW, H, W, r0, rws, ws, labels, valid, top_k, logp, lse, entropy, top_ids,
+                                                 top_logp, sm_count, st)
+                                 : lp_slab<false>(&one, plan, tmW, H, W, r0, rws, ws, labels, valid, 0, logp, lse, entropy, nullptr,
+                                                  nullptr, sm_count, st);
+        if (rc != CAT_OK) return rc;
+    }
+    return CAT_OK;
+}
+
+int cat_logprob_bwd(const cat_shape* shape, const void* H, const void* W, const int64_t* labels, const uint8_t* valid, const float* lse,
+                    const float* entropy, const float* grad_logp, const float* grad_entropy, void* dH, void* dW, int accumulate_dW,
+                    void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (!shape) return CAT_ERR_NULL;
+    cat_shape one = per_position_shape(shape);
+    one.dW_dtype = shape->dW_dtype;
+    LpArgs a;
+    a.entropy = entropy; a.grad_logp = grad_logp; a.grad_entropy = grad_entropy;
+    return bwd_core(&one, H, W, labels, valid, lse, nullptr, nullptr, dH, dW, accumulate_dW, workspace, workspace_bytes, cuda_stream,
+                    nullptr, &a);
+}
+
+size_t cat_topk_kd_workspace_bytes(const cat_shape* shape, const cat_topk_kd_desc* desc) {
+    if (check_shape(shape) != CAT_OK || check_topk_kd(desc) != CAT_OK) return 0;
+    return plan_tk(shape, desc->k).total;
+}
+
+int cat_topk_kd_loss_fwd_bwd(const cat_shape* shape, const cat_topk_kd_desc* desc, const void* H, const void* W, const int64_t* labels,
+                             const uint8_t* valid, const int64_t* top_ids, const float* top_logp, const int64_t* block_start,
+                             const float* conf_ext, const float* grad_loss, float* loss, float* lse, float* conf, float* weight,
+                             cat_stats* stats, void* dH, void* dW, int accumulate_dW, void* workspace, size_t workspace_bytes,
+                             void* cuda_stream) {
+    if (!shape || !desc || !H || !W || !labels || !top_ids || !top_logp || !loss || !lse || !conf || !weight || !dH || !dW)
+        return CAT_ERR_NULL;
+    int rc = check_shape(shape);
+    if (rc == CAT_OK) rc = check_topk_kd(desc);
+    if (rc != CAT_OK) return rc;
+    const size_t in_al = shape->in_dtype == CAT_BF16 ? 16 : 4;
+    if (misaligned(H, in_al) || misaligned(W, in_al) || misaligned(dH, in_al) || misaligned(dW, 16) || misaligned(labels, 8) ||
+        misaligned(top_ids, 8) || misaligned(top_logp, 4) || misaligned(block_start, 8) || misaligned(conf_ext, 4) ||
+        misaligned(grad_loss, 4) || misaligned(loss, 4) || misaligned(lse, 4) || misaligned(conf, 4) || misaligned(weight, 4) ||
+        misaligned(stats, 8))
+        return CAT_ERR_ALIGN;
+    const TkPlan plan = plan_tk(shape, desc->k);
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < plan.total) return CAT_ERR_WORKSPACE;
+    int sm_count = 0;
+    rc = check_device(&sm_count);
+    if (rc != CAT_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    if (shape->in_dtype == CAT_BF16)
+        return tk_core<__nv_bfloat16>(shape, desc, plan, static_cast<const __nv_bfloat16*>(H), static_cast<const __nv_bfloat16*>(W), labels,
+                                      valid, top_ids, top_logp, block_start, conf_ext, grad_loss, loss, lse, conf, weight, stats, dH, dW,
+                                      accumulate_dW, ws, sm_count, st);
+    return tk_core<float>(shape, desc, plan, static_cast<const float*>(H), static_cast<const float*>(W), labels, valid, top_ids, top_logp,
+                          block_start, conf_ext, grad_loss, loss, lse, conf, weight, stats, dH, dW, accumulate_dW, ws, sm_count, st);
+}
+
+}  // extern "C"

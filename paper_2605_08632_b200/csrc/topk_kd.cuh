@@ -1,0 +1,285 @@
+// Distillation from a teacher's stored top logits, under the CAT weight: per draft row
+//   weight * (beta * CE + KD),   KD = sum_i p_i (log p_i - z[id_i] + lse)
+// over the row's list (id_i, log p_i), i < k, in the place of the full distribution of kd.cuh:
+//   dz[v] = weight ((beta + sum_i p_i) q_v - beta [v = y] - sum_i p_i [v = id_i]).
+// One row slab at a time: gather_kernel (the logits at the list's ids, fp32, and the slab's reference), the logits GEMM,
+// which keeps z - ref as fp16, the row kernel of rowops.cuh, dz_kernel (z -> dz in place) and the dH and dW contractions.
+//
+// Why the slab holds fp16 logits and is turned into dz by a pass of its own (4 bytes per logit, bound by HBM), although
+// cat_loss_fwd_bwd gets by without one: there the row's factor a[r] has to ride on H in the dW contraction, and
+// rounding a[r] H[r, :] to bf16 costs as much as rounding dz.  Here dz is rounded to bf16 once, and H not at all.
+#pragma once
+#include "logprob.cuh"
+
+namespace cat {
+namespace tc {
+
+// Softmax statistics (as EpiFwdT), the label's logit, and z - ref as fp16 (saturating).  ref is near the row's largest
+// logit when student and teacher agree, where fp16 is finest and softmax largest: a relative error of 2^-12 |z - ref|.
+struct EpiFwdRef {
+    struct Params {
+        const long long* labels;   // [T]
+        float* part_m;             // [n_groups][part_stride]
+        float* part_l;
+        float* z_label;            // [T]
+        const float* ref;          // [T]
+        long long part_stride;
+        int T;
+        int V;
+    };
+    struct State {
+        float m_run, l_run, ref;
+        int y;
+        int row;
+    };
+    __device__ static __forceinline__ void begin_item(const Params& p, State& s, int m_tile, int row_in_tile) {
+        s.row = m_tile * BM + row_in_tile;
+        s.m_run = LP_LOW;
+        s.l_run = 0.f;
+        s.ref = 0.f;
+        s.y = -1;
+        if (s.row < p.T) {
+            const long long y = p.labels[s.row];
+            if (y >= 0 && y < p.V) s.y = static_cast<int>(y);
+            s.ref = p.ref[s.row];
+        }
+    }
+    __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage& o) {
+        const int col0 = n_tile * BN;
+        const int ncols = min(BN, p.V - col0);
+#pragma unroll 1
+        for (int c = 0; c < BN / 32; ++c) {
+            if (c * 32 >= ncols) break;
+            if ((c & 1) == 0) o.begin();
+            uint32_t v[32];
+            ptx::tmem_ld_32x32(taddr + c * 32, v);
+            ptx::tmem_ld_wait();
+            float f[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
+            const int live = ncols - c * 32;
+            if (live < 32) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (i >= live) f[i] = LP_LOW;
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                o.put((c & 1) * 4 + q, ptx::pack_f16x2_sat(f[q * 8 + 0] - s.ref, f[q * 8 + 1] - s.ref),
+                      ptx::pack_f16x2_sat(f[q * 8 + 2] - s.ref, f[q * 8 + 3] - s.ref),
+                      ptx::pack_f16x2_sat(f[q * 8 + 4] - s.ref, f[q * 8 + 5] - s.ref),
+                      ptx::pack_f16x2_sat(f[q * 8 + 6] - s.ref, f[q * 8 + 7] - s.ref));
+            if ((c & 1) != 0 || (c + 1) * 32 >= ncols) o.flush(col0 + (c >> 1) * 64);
+            const int rel = s.y - (col0 + c * 32);
+            if (rel >= 0 && rel < 32) {
+                float zy = 0.f;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (i == rel) zy = f[i];
+                p.z_label[s.row] = zy;
+            }
+            float cmax = ptx::max3_f32(f[0], f[1], f[2]);
+#pragma unroll
+            for (int i = 3; i + 1 < 32; i += 2) cmax = ptx::max3_f32(cmax, f[i], f[i + 1]);
+            cmax = fmaxf(cmax, f[31]);
+            const float m_new = fmaxf(s.m_run, cmax);
+            const float mb = m_new * LOG2E;
+            const uint64_t l2e2 = ptx::pack_f32x2(LOG2E, LOG2E), nmb2 = ptx::pack_f32x2(-mb, -mb);
+            uint64_t sum2 = ptx::pack_f32x2(0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float x0, x1;
+                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(f[2 * i], f[2 * i + 1]), l2e2, nmb2), x0, x1);
+                sum2 = ptx::add_f32x2(sum2, ptx::pack_f32x2(ptx::ex2_approx(x0), ptx::ex2_approx(x1)));
+            }
+            float s0, s1;
+            ptx::unpack_f32x2(sum2, s0, s1);
+            s.l_run = fmaf(s.l_run, ptx::ex2_approx((s.m_run - m_new) * LOG2E), s0 + s1);
+            s.m_run = m_new;
+        }
+    }
+    __device__ static __forceinline__ int out_rows(const Params& p) { return p.T; }
+    __device__ static __forceinline__ void end_item(const Params& p, const State& s, int group) {
+        if (s.row < p.T) {
+            p.part_m[static_cast<size_t>(group) * p.part_stride + s.row] = s.m_run;
+            p.part_l[static_cast<size_t>(group) * p.part_stride + s.row] = s.l_run;
+        }
+    }
+};
+
+}  // namespace tc
+
+namespace tk {
+
+using lp::MAX_TOP;
+using lp::THREADS;
+using lp::WARPS;
+constexpr float LOG2E = 1.4426950408889634f;
+
+// A draft row takes part iff its mask bit is set, its label is a token id and its teacher position exists.
+__global__ void __launch_bounds__(THREADS) prepare_kernel(const long long* labels, const unsigned char* valid,
+                                                          const long long* block_start, int T, int K, int V, long long L,
+                                                          unsigned char* valid_eff) {
+    const int r = blockIdx.x * THREADS + threadIdx.x;
+    if (r >= T) return;
+    const long long y = labels[r];
+    const int b = r / K;
+    const long long t = block_start ? block_start[b] + (r - b * K) : r;
+    valid_eff[r] = ((valid == nullptr || valid[r] != 0) && y >= 0 && y < V && t >= 0 && t < L) ? 1 : 0;
+}
+
+// The teacher's lists: position t's entries are (ids[t * ld + i], logp[t * ld + i]), i < k.
+struct Lists {
+    const long long* ids;
+    const float* logp;
+    const long long* block_start;  // [T / K] or nullptr: row r reads position r
+    long long ld;
+    int k;
+    int K;
+    int V;
+    int renorm;
+    __device__ __forceinline__ long long position(long long r) const {
+        return block_start ? block_start[r / K] + (r - (r / K) * K) : r;
+    }
+    // entry i counts iff its id is a token and its log probability is above -infinity (NaN counts, and shows)
+    __device__ __forceinline__ bool entry(long long t, int i, long long& id, float& lp) const {
+        id = ids[t * ld + i];
+        lp = logp[t * ld + i];
+        return id >= 0 && id < V && !(lp == -INFINITY);
+    }
+};
+
+// One CTA per row of the slab: z[r, id_i] as fp32 for every counting entry of its list (one warp per dot product), and
+// ref[r], the largest of them and of the label's logit (0 for a row that takes no part).
+template <class TI>
+__global__ void __launch_bounds__(THREADS) gather_kernel(const TI* H, long long ldH, const TI* W, long long ldW, int d,
+                                                         const long long* labels, const unsigned char* valid_eff, Lists lists,
+                                                         long long row0, float* zt, int ld_zt, float* ref) {
+    __shared__ float s_max[WARPS];
+    const long long r = row0 + blockIdx.x;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (!valid_eff[r]) {
+        if (threadIdx.x == 0) ref[r] = 0.f;
+        return;
+    }
+    const long long t = lists.position(r);
+    const TI* h = H + static_cast<long long>(blockIdx.x) * ldH;
+    float mx = -INFINITY;
+    for (int i = warp; i <= lists.k; i += WARPS) {
+        long long id = -1;
+        float lp;
+        if (i == lists.k) id = labels[r];
+        else if (!lists.entry(t, i, id, lp)) continue;
+        const float z = static_cast<float>(lp::warp_dot(h, W + id * ldW, d, lane));
+        if (lane == 0) zt[static_cast<long long>(blockIdx.x) * ld_zt + i] = z;
+        mx = fmaxf(mx, z);
+    }
+    if (lane == 0) s_max[warp] = mx;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int i = 1; i < WARPS; ++i) mx = fmaxf(mx, s_max[i]);
+        ref[r] = fabsf(mx) < 1.0e30f ? mx : 0.f;
+    }
+}
+
+__device__ __forceinline__ float block_sum(float x, float* red) {
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
+    __syncthreads();
+    x = red[0];
+#pragma unroll
+    for (int i = 1; i < WARPS; ++i) x += red[i];
+    return x;
+}
+
+// One CTA per row of the slab: the row's KD value, and the stored logits turned into dz in place.  Dense part
+// weight (beta + sum p) q from the stored z - ref; the entries at the label and at the list's ids from their fp32
+// logits, an id that stands in the list twice with the sum of its probabilities.
+// fp32 slabs (fp32 inputs) hold z itself and leave as fp32 dz.
+template <bool F32>
+__global__ void __launch_bounds__(THREADS) dz_kernel(void* zs, long long ldz, const long long* labels, const unsigned char* valid_eff,
+                                                     Lists lists, long long row0, const float* lse, const float* weight,
+                                                     const float* zt, int ld_zt, const float* ref, float beta, float* kd_row,
+                                                     int V) {
+    __shared__ float s_red[WARPS];
+    __shared__ float s_p[MAX_TOP];
+    __shared__ int s_id[MAX_TOP];
+    const long long r = row0 + blockIdx.x;
+    uint4* row = reinterpret_cast<uint4*>(static_cast<unsigned short*>(zs) + static_cast<size_t>(blockIdx.x) * ldz);
+    float* row32 = static_cast<float*>(zs) + static_cast<size_t>(blockIdx.x) * ldz;
+    const int groups = static_cast<int>(ldz / 8);
+    if (!valid_eff[r]) {
+        if (F32) for (int v = threadIdx.x; v < V; v += THREADS) row32[v] = 0.f;
+        else for (int g = threadIdx.x; g < groups; g += THREADS) row[g] = make_uint4(0u, 0u, 0u, 0u);
+        if (threadIdx.x == 0) kd_row[r] = 0.f;
+        return;
+    }
+    const long long t = lists.position(r);
+    const float lse_r = lse[r], w = weight[r];
+    const int y = static_cast<int>(labels[r]);
+    const float* zr = zt + static_cast<long long>(blockIdx.x) * ld_zt;
+    // the list: thread i holds entry i (k <= MAX_TOP = THREADS)
+    const int i = threadIdx.x;
+    long long id = -1;
+    float lp = -INFINITY, z_i = 0.f;
+    const bool there = i < lists.k && lists.entry(t, i, id, lp);
+    if (there) z_i = zr[i];
+    if (lists.renorm) {
+        const float m = lp::block_max(there ? lp : -INFINITY, s_red);
+        const float l = block_sum(there ? expf(lp - m) : 0.f, s_red);
+        if (there) lp = lp - m - logf(l);
+    }
+    const float p_i = there ? expf(lp) : 0.f;
+    const float mass = block_sum(p_i, s_red);
+    // 0 (log 0 - ...) = 0: a probability that underflows adds nothing
+    const float kd = block_sum(there && p_i != 0.f ? p_i * (lp - (z_i - lse_r)) : 0.f, s_red);
+    if (i < MAX_TOP) {
+        s_p[i] = p_i;
+        s_id[i] = there ? static_cast<int>(id) : -1;
+    }
+    if (i == 0) kd_row[r] = w * kd;
+    const float wm = w * (beta + mass);
+    const float off = F32 ? 0.f : (ref[r] - lse_r) * LOG2E;
+    if (F32)
+        for (int v = threadIdx.x; v < V; v += THREADS) row32[v] = wm * expf(row32[v] - lse_r);
+    else for (int g = threadIdx.x; g < groups; g += THREADS) {
+        const uint4 in = __ldcs(row + g);
+        const uint32_t zw[4] = {in.x, in.y, in.z, in.w};
+        uint32_t o[4];
+        const int col = g * 8;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 z2 = __half22float2(*reinterpret_cast<const __half2*>(&zw[j]));
+            const float a = col + 2 * j < V ? wm * ptx::ex2_approx(fmaf(z2.x, LOG2E, off)) : 0.f;
+            const float b = col + 2 * j + 1 < V ? wm * ptx::ex2_approx(fmaf(z2.y, LOG2E, off)) : 0.f;
+            o[j] = ptx::pack_bf16x2(a, b);
+        }
+        row[g] = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+    __syncthreads();
+    auto put = [&](long long at, float x) {
+        if (F32) row32[at] = x;
+        else reinterpret_cast<__nv_bfloat16*>(row)[at] = __float2bfloat16_rn(x);
+    };
+    if (there) {
+        float sub = p_i;
+        bool first = true;
+        for (int j = 0; j < lists.k; ++j) {
+            if (j == i || s_id[j] != static_cast<int>(id)) continue;
+            first &= j > i;
+            sub += s_p[j];
+        }
+        if (id == y) sub += beta;
+        if (first) put(id, w * ((beta + mass) * expf(z_i - lse_r) - sub));
+    }
+    bool listed = false;
+    for (int j = threadIdx.x; j < lists.k; j += THREADS) listed |= s_id[j] == y;
+    if (!__syncthreads_or(listed ? 1 : 0) && threadIdx.x == 0)
+        put(y, w * ((beta + mass) * expf(zr[lists.k] - lse_r) - beta));
+}
+
+}  // namespace tk
+}  // namespace cat

@@ -1,0 +1,277 @@
+"""cat_logprob_fwd / cat_logprob_bwd against the fp64 oracle, through the public classes; bounds in head_ops_util."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from head_ops_util import U, check_grads, tolerances
+from oracle import head_ops_oracle as O
+from paper_2605_08632_b200 import binding as B
+from paper_2605_08632_b200.api import LogProbModule, TokenLogProb
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def make(T, d, V, dtype, seed=0, masked=0.2, sure=0.5):
+    g = torch.Generator().manual_seed(seed)
+    W = (0.02 * torch.randn(V, d, generator=g)).to(dtype)
+    H = torch.randn(T, d, generator=g)
+    y = torch.randint(0, V, (T,), generator=g)
+    amount = 12.0 * torch.rand(T, generator=g) * (torch.rand(T, generator=g) < sure)
+    Wy = W[y].float()
+    H = (H + Wy * (amount / (Wy * Wy).sum(1).clamp(min=1e-6)).unsqueeze(1)).to(dtype)
+    valid = (torch.rand(T, generator=g) >= masked).to(torch.uint8)
+    y = torch.where(torch.rand(T, generator=g) < 0.05, torch.full_like(y, V + 3), y)
+    return H, W, y, valid
+
+
+def np64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def check_forward(r, H, W, y, valid, k, bf16):
+    ref = O.logprob_forward(H, W, y, valid, k)
+    on = ref["on"]
+    tol_z, tol_l = tolerances(np64(H), np64(W), on, ref["z"], bf16)
+    lse = np64(r.lse)
+    tol = tol_z + tol_l + 8 * U * np.abs(ref["lse"])
+    assert np.all(np.abs(lse - ref["lse"]) <= tol)
+    V = W.shape[0]
+    assert np.all(np.abs(np64(r.entropy) - ref["entropy"]) <= 4 * (1 + math.log(V)) * (tol_z + tol_l))
+    if y is not None:
+        assert np.all(np.abs(np64(r.logp) - ref["logp"]) <= tol + 2 * U * np.abs(ref["logp"]))
+        assert not np64(r.logp)[~ref["known"]].any()
+    if k:
+        ids, tl = r.top_ids.cpu().numpy(), np64(r.top_logp)
+        assert np.array_equal(ids, ref["top_ids"])
+        there = ref["top_ids"] >= 0
+        assert np.all(np.isneginf(tl[~there]))
+        want = np.where(there, ref["top_logp"], 0.0)
+        assert np.all(np.abs(tl - want)[there] <= (tol[:, None] + 2 * U * np.abs(want))[there])
+    assert not lse[~on].any() and not np64(r.entropy)[~on].any()
+    return ref
+
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.mark.parametrize("T,d,V,k,dtype", [
+    (1, 64, 1, 1, BF), (1, 64, 3, 8, BF), (1, 512, 5003, 20, BF), (2, 8, 33, 33, BF), (3, 72, 256, 256, BF), (5, 128, 257, 1, BF),
+    (37, 256, 8191, 64, BF), (130, 136, 20011, 5, BF), (257, 256, 12000, 20, BF), (600, 128, 3000, 0, BF),
+    (1, 3, 1, 2, F32), (7, 5, 63, 64, F32), (65, 33, 129, 7, F32), (130, 100, 4097, 20, F32), (70, 64, 2500, 0, F32),
+])
+def test_forward_matches_oracle(T, d, V, k, dtype):
+    H, W, y, valid = make(T, d, V, dtype, seed=T + V)
+    e = TokenLogProb(T, d, V, top_k=k, dtype=dtype)
+    r = e.forward(H.to(DEV), W.to(DEV), y.to(DEV), valid.to(DEV))
+    check_forward(r, H, W, y, valid, k, dtype == BF)
+    assert e.status() == 0
+    # no mask, no labels: the other outputs alone
+    r = e.forward(H.to(DEV), W.to(DEV))
+    assert r.logp is None
+    check_forward(r, H, W, None, None, k, dtype == BF)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_row_slabs_give_the_same(dtype):
+    T, d, V, k = 1100, 64, 5000, 12
+    H, W, y, valid = (t.to(DEV) for t in make(T, d, V, dtype))
+    whole = TokenLogProb(T, d, V, k, dtype=dtype).forward(H, W, y, valid)
+    e = TokenLogProb(T, d, V, k, dtype=dtype, slab_mib=3)
+    cut = e.forward(H, W, y, valid)
+    assert e.ws.numel() < TokenLogProb(T, d, V, k, dtype=dtype).ws.numel()
+    assert torch.equal(whole.top_ids, cut.top_ids)
+    check_forward(cut, H.cpu(), W.cpu(), y.cpu(), valid.cpu(), k, dtype == BF)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_equal_logits_and_rows_of_zeros(dtype):
+    """Equal rows of W tie exactly; a zero row of H ties everything; a common offset crowds the stored logits' rounding."""
+    T, d, V, k = 6, 64, 6000, 40
+    H, W, y, _ = make(T, d, V, dtype, sure=0.0)
+    W[1000:3000] = W[7]                     # 2001 equal rows, more than are held at a time
+    H[0] = 0
+    H[1] = (W[7].float() * 30).to(dtype)    # ... and they are this row's largest
+    H[2] = -(W[7].float() * 30).to(dtype)
+    W[:, 0] = 1.0
+    H[3, 0] = 500.0                         # logits of 500 +- 1: the fp16 copies step by 0.25 to 0.5
+    H[4] = 0
+    H[4, 0] = 3.0                           # all equal, and not zero
+    r = TokenLogProb(T, d, V, k, dtype=dtype).forward(H.to(DEV), W.to(DEV), y.to(DEV))
+    ref = check_forward(r, H, W, y, None, k, dtype == BF)
+    assert ref["top_ids"][0].tolist() == list(range(k)) == ref["top_ids"][4].tolist()
+    assert ref["top_ids"][1].tolist() == [7] + list(range(1000, 1000 + k - 1))
+
+
+def test_padding_may_hold_anything_and_other_rows_are_untouched():
+    T, d, V, k = 70, 64, 1000, 9
+    for dtype in (BF, F32):
+        H, W, y, valid = make(T, d, V, dtype)
+        clean = H.clone()
+        clean[valid == 0] = 0
+        H[valid == 0] = float("nan")
+        H[int(np.nonzero(valid.numpy() == 0)[0][0])] = float("inf")
+        gl, ge = torch.randn(T), torch.randn(T)
+        e, f = (TokenLogProb(T, d, V, k, dtype=dtype) for _ in range(2))
+        a, b = e.forward(H.to(DEV), W.to(DEV), y.to(DEV), valid.to(DEV)), f.forward(clean.to(DEV), W.to(DEV), y.to(DEV), valid.to(DEV))
+        for x, z in zip(a, b):
+            assert torch.equal(x, z)
+        ga = e.backward(H.to(DEV), W.to(DEV), y.to(DEV), valid.to(DEV), gl.to(DEV), ge.to(DEV))
+        gb = f.backward(clean.to(DEV), W.to(DEV), y.to(DEV), valid.to(DEV), gl.to(DEV), ge.to(DEV))
+        assert torch.equal(ga[0], gb[0]) and torch.equal(ga[1], gb[1]) and bool(torch.isfinite(ga[1]).all())
+        assert not ga[0][valid.to(DEV) == 0].any()
+
+
+def test_rows_that_are_not_finite_say_so():
+    T, d, V, k = 5, 64, 700, 6
+    H, W, y, _ = make(T, d, V, BF)
+    H[1, 3] = float("nan")
+    H[3, 0] = float("inf")
+    r = TokenLogProb(T, d, V, k).forward(H.to(DEV), W.to(DEV), y.clamp(max=V - 1).to(DEV))
+    for i in range(T):
+        bad = i in (1, 3)
+        assert bool(torch.isnan(r.entropy[i])) == bad and bool(torch.isfinite(r.lse[i])) != bad
+        assert bool((r.top_ids[i] == -1).all()) == bad and bool(torch.isnan(r.top_logp[i]).all()) == bad
+
+
+@pytest.mark.parametrize("T,d,V,dtype,dW_dtype,slab_mib", [
+    (1, 64, 1, BF, F32, 0), (3, 64, 300, BF, BF, 0), (130, 136, 5003, BF, F32, 0), (300, 256, 3000, BF, BF, 1), (520, 64, 1111, BF, F32, 1),
+    (1, 3, 2, F32, F32, 0), (70, 33, 1025, F32, F32, 0), (200, 64, 2000, F32, F32, 1),
+])
+@pytest.mark.parametrize("which", ["logp", "entropy", "both"])
+def test_backward_matches_oracle(T, d, V, dtype, dW_dtype, slab_mib, which):
+    H, W, y, valid = make(T, d, V, dtype, seed=V)
+    g = torch.Generator().manual_seed(5)
+    gl = torch.randn(T, generator=g) if which != "entropy" else None
+    ge = 0.3 * torch.randn(T, generator=g) if which != "logp" else None
+    e = TokenLogProb(T, d, V, dtype=dtype, dW_dtype=dW_dtype, slab_mib=slab_mib)
+    dev = lambda t: None if t is None else t.to(DEV)  # noqa: E731
+    e.forward(dev(H), dev(W), dev(y), dev(valid))
+    dH, dW = e.backward(dev(H), dev(W), dev(y) if gl is not None else None, dev(valid), dev(gl), dev(ge))
+    assert e.bwd_status() == 0
+    on = O.logprob_forward(H, W, y, valid)["on"]
+    z = O.logprob_forward(H, W, y, valid)["z"]
+    tol_z, tol_l = tolerances(np64(H), np64(W), on, z, dtype == BF)
+    ref = O.logprob_backward(H, W, y if gl is not None else None, valid, gl, ge)
+    # p is off by the error of z - lse; the entropy's coefficient by that of log p + entropy, held against |log p| + entropy
+    tol = 2 * tol_z + tol_l + 16 * U * (1 + np.abs(z).max()) + 4 * (1 + math.log(V)) * (tol_z + tol_l)
+    Hc = np.where(on[:, None], np64(H), 0.0)
+    check_grads(np64(dH), np64(dW), ref, np64(W), Hc, tol, dtype == BF, dW_bf16=dW_dtype == BF)
+    # added to what dW holds
+    again = dW.clone()
+    dH2, dW2 = e.backward(dev(H), dev(W), dev(y) if gl is not None else None, dev(valid), dev(gl), dev(ge), accumulate_dW=True)
+    assert torch.allclose(dW2.float(), 2 * again.float(), rtol=2 ** -7 if dW_dtype == BF else 2 ** -22, atol=1e-30)
+
+
+def test_backward_against_differences():
+    """f(H + h D, W + h E) - f(H - h D, W - h E) over 2 h, f from the fp32 forward pass.  h = 2^-6: the third derivative's part is below
+    h^2, and the forward's error (a few 1e-6 a row, T rows) over 2 h below 3e-3."""
+    T, d, V = 40, 32, 500
+    H, W, y, _ = make(T, d, V, F32, sure=0.0)
+    y = y.clamp(max=V - 1)
+    g = torch.Generator().manual_seed(2)
+    gl, ge = torch.randn(T, generator=g), torch.randn(T, generator=g)
+    D, E = torch.randn(T, d, generator=g) / math.sqrt(T * d), torch.randn(V, d, generator=g) / math.sqrt(V * d)
+    e = TokenLogProb(T, d, V, dtype=F32)
+
+    def f(H, W):
+        r = e.forward(H.to(DEV), W.to(DEV), y.to(DEV))
+        return float((gl.double() * r.logp.cpu().double() + ge.double() * r.entropy.cpu().double()).sum())
+
+    h = 2.0 ** -6
+    slope = (f(H + h * D, W + h * E) - f(H - h * D, W - h * E)) / (2 * h)
+    e.forward(H.to(DEV), W.to(DEV), y.to(DEV))
+    dH, dW = e.backward(H.to(DEV), W.to(DEV), y.to(DEV), None, gl.to(DEV), ge.to(DEV))
+    got = float((dH.cpu().double() * D).sum() + (dW.cpu().double() * E).sum())
+    assert abs(got - slope) <= 3e-3 + h * h
+
+
+def test_strided_inputs_and_guarded_outputs():
+    T, d, V, k = 33, 64, 777, 5
+    H, W, y, valid = make(T, d, V, BF)
+    wide_H, wide_W = torch.full((T, d + 24), float("nan"), dtype=BF, device=DEV), torch.full((V, d + 8), float("nan"), dtype=BF, device=DEV)
+    wide_H[:, :d] = H.to(DEV)
+    wide_W[:, :d] = W.to(DEV)
+    e = TokenLogProb(T, d, V, k)
+    a = [t.clone() for t in e.forward(H.to(DEV), W.to(DEV), y.to(DEV), valid.to(DEV))]
+    b = e.forward(wide_H[:, :d], wide_W[:, :d], y.to(DEV), valid.to(DEV).bool())
+    for x, z in zip(a, b):
+        assert torch.equal(x, z)
+    with pytest.raises(ValueError):
+        e.backward(wide_H[:, :d], wide_W[:, :d], y.to(DEV), None, e.logp)
+    with pytest.raises(B.CatError) as err:      # a pitch that TMA cannot take
+        e.forward(torch.zeros(T, d + 4, dtype=BF, device=DEV)[:, :d], W.to(DEV))
+    assert err.value.code == -4
+    # nothing is written past the outputs
+    shape = B.make_shape(T, d, V, 1, B.CAT_BF16)
+    n = B.cat_logprob_workspace_bytes(shape, k, 0)
+    big = torch.full((n + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+    out = [torch.full((T + 8,), 7.0, device=DEV) for _ in range(3)]
+    ids, tl = torch.full((T + 8, k), 77, dtype=torch.int64, device=DEV), torch.full((T + 8, k), 7.0, device=DEV)
+    B.cat_logprob_fwd(shape, H.to(DEV), W.to(DEV), y.to(DEV), valid.to(DEV), k, out[0], out[1], out[2], ids, tl, big[:n])
+    torch.cuda.synchronize()
+    assert bool((big[n:] == 0xA5).all()) and all(bool((o[T:] == 7.0).all()) for o in out)
+    assert bool((ids[T:] == 77).all()) and bool((tl[T:] == 7.0).all())
+    assert torch.equal(out[0][:T], a[0]) and torch.equal(ids[:T], a[3])
+
+
+def test_refusals_of_the_python_layer():
+    e = TokenLogProb(8, 64, 100, 4)
+    H, W, y = torch.zeros(8, 64, dtype=BF, device=DEV), torch.zeros(100, 64, dtype=BF, device=DEV), torch.zeros(8, dtype=torch.int64, device=DEV)
+    for bad in (lambda: e.forward(H.float(), W, y), lambda: e.forward(H, W, y.int())):
+        with pytest.raises(TypeError):
+            bad()
+    for bad in (lambda: e.forward(H[:4], W, y), lambda: e.forward(H, W, y.cpu()), lambda: e.forward(H.cpu(), W, y),
+                lambda: e.backward(H, W, None, None, e.logp), lambda: e.backward(H, W, y, None, e.logp, accumulate_dW=True),
+                lambda: TokenLogProb(8, 60, 100), lambda: TokenLogProb(8, 64, 100, top_k=B.CAT_TOPK_MAX + 1)):
+        with pytest.raises(ValueError):
+            bad()
+
+
+def test_streams_graphs_and_repeatability():
+    T, d, V, k = 96, 128, 4000, 16
+    H, W, y, valid = (t.to(DEV) for t in make(T, d, V, BF))
+    gl, ge = torch.randn(T, device=DEV), torch.randn(T, device=DEV)
+    e = TokenLogProb(T, d, V, k)
+    first = [t.clone() for t in e.forward(H, W, y, valid)] + [t.clone() for t in e.backward(H, W, y, valid, gl, ge)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        second = [t.clone() for t in e.forward(H, W, y, valid)] + [t.clone() for t in e.backward(H, W, y, valid, gl, ge)]
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = e.forward(H, W, y, valid)
+        dH, dW = e.backward(H, W, y, valid, gl, ge)
+    for _ in range(2):
+        e.dH.zero_(), e.dW.zero_(), e.lse.zero_(), e.top_ids.zero_()
+        graph.replay()
+    torch.cuda.synchronize()
+    for a, b, c in zip(first, second, list(r) + [dH, dW]):
+        assert torch.equal(a, b) and torch.equal(a, c)
+    # new inputs in the captured buffers
+    H2 = make(T, d, V, BF, seed=9)[0]
+    H.copy_(H2)
+    graph.replay()
+    check_forward(r, H2, W.cpu(), y.cpu(), valid.cpu(), k, True)
+
+
+def test_module_gradients():
+    T, d, V = 50, 64, 900
+    H, W, y, valid = make(T, d, V, F32, sure=0.0)
+    head = LogProbModule(W.to(DEV), top_k=3)
+    h = H.to(DEV).requires_grad_()
+    logp, entropy, ids, tl = head(h, y.to(DEV), valid.to(DEV))
+    head(torch.zeros_like(h), y.to(DEV), valid.to(DEV))          # another call through the same engine before backward
+    gl, ge = torch.randn(T), torch.randn(T)
+    (logp * gl.to(DEV) + entropy * ge.to(DEV)).sum().backward()
+    dH, dW, *_ = O.logprob_backward(H, W, y, valid, gl, ge)
+    assert np.linalg.norm(np64(h.grad) - dH) <= 1e-5 * np.linalg.norm(dH)
+    assert np.linalg.norm(np64(head.weight.grad) - dW) <= 1e-5 * np.linalg.norm(dW)
+    assert not ids.requires_grad and not tl.requires_grad
+    h.grad = None
+    head(h, None, valid.to(DEV))[1].sum().backward()             # without labels: the entropy alone
+    dH, *_ = O.logprob_backward(H, W, None, valid, None, np.ones(T))
+    assert np.linalg.norm(np64(h.grad) - dH) <= 1e-5 * np.linalg.norm(dH)
