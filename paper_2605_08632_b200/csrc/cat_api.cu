@@ -188,6 +188,8 @@ struct FusedPlan {
     size_t off_part_m, off_part_l, off_z_label, off_row_ce, off_partials, off_ref, off_a, off_hs, off_z, off_dw_acc, total;
 };
 
+double dh_waves(long long rows, long long d, long long V);
+
 long long gcd_ll(long long a, long long b) { return b == 0 ? a : gcd_ll(b, a % b); }
 
 // `two_slabs`: a batch of more than one slab unit is cut in two at least, whatever the cap allows.
@@ -215,8 +217,11 @@ FusedPlan plan_fused(const cat_shape* s, bool two_slabs = true) {
             const long long num_m = cdiv(rws, tile_m());
             const long long S = fwd_splits(rws, s->V);
             cost += static_cast<double>(cdiv(num_m * S, plan_workers()) * cdiv(n_tiles_v, S)) * static_cast<double>(s->d);   // logits
-            cost += static_cast<double>(cdiv(num_m * n_tiles_n, plan_workers())) * static_cast<double>(s->V);               // dH
+            if (two_slabs) cost += static_cast<double>(cdiv(num_m * n_tiles_n, plan_workers())) * static_cast<double>(s->V);   // dH
+            else cost += dh_waves(rws, s->d, s->V) * static_cast<double>(s->V);
             cost += static_cast<double>(cdiv(n_tiles_v * n_tiles_n, plan_workers())) * static_cast<double>(rws);             // dW
+            // a further slab reads and writes dW's fp32 sum once more: 8 bytes at 6.4 TB/s, against 5.8 ns per tile and k
+            if (!two_slabs && r0 > 0) cost += 2.15e-4 * static_cast<double>(s->V) * static_cast<double>(s->d);
         }
         if (best_cost < 0.0 || cost < best_cost * (1.0 - 1e-9)) { best_cost = cost; best_ts = ts; }
     }
@@ -502,7 +507,8 @@ int launch_tc(const CUtensorMap& tmA, const CUtensorMap& tmB, const tc::Sched& s
 }
 
 // Launch of a GEMM with the plain-output epilogue: fp32 outputs that either overwrite or accumulate in
-// place (pitch a multiple of 4 elements) take the staged TMA store / reduce-add route.
+// place (pitch a multiple of 4 elements) take the staged TMA store / reduce-add route, bf16 outputs that
+// overwrite the staged TMA store.
 template <int A_MN, int B_MN>
 int launch_out(const CUtensorMap& tmA, const CUtensorMap& tmB, const tc::Sched& sched, tc::EpiOut::Params ep, int* status,
                int sm_count, cudaStream_t st) {
@@ -512,6 +518,9 @@ int launch_out(const CUtensorMap& tmA, const CUtensorMap& tmB, const tc::Sched& 
         !misaligned(ep.out_f32, 16)) {
         if (tmap_out_f32(&tmO, ep.out_f32, ep.M, ep.N, ep.ld_out) != CAT_OK) return CAT_ERR_CUDA;
         ep.staged = 1;
+    } else if (!ep.out_f32 && !ep.add_f32 && !ep.add_bf16 && ep.ld_out % 8 == 0 && !misaligned(ep.out_bf16, 16)) {
+        if (tmap_out(&tmO, ep.out_bf16, ep.M, ep.N, ep.ld_out) != CAT_OK) return CAT_ERR_CUDA;
+        ep.staged = 2;
     }
     return launch_tc<A_MN, B_MN, tc::EpiOut>(tmA, tmB, sched, ep, status, sm_count, st, ep.staged ? &tmO : nullptr);
 }
@@ -525,10 +534,61 @@ tc::Sched make_sched(long long M, long long N, long long Kd, int n_groups, int b
     s.band_m = band_m < 1 ? 1 : band_m;
     s.n_fastest = n_fastest;
     s.n_items = s.num_m_tiles * s.n_groups;
+    s.k_splits = 1;
+    s.m_real = s.num_m_tiles;
     s.wait_ns = tc::WAIT_LIMIT_NS;
     s.claims = nullptr;
     s.serial = 0;
     return s;
+}
+
+// Parts that the vocabulary contraction of dH = dz W is cut into when a batch has few output tiles for the 74 CTA pairs
+// (512 rows of d = 2048: 16 tiles).  Each part's fp32 sum goes to its own rows of a scratch array and one kernel adds them in
+// order, so the result does not depend on who finishes first.  Cost in whole-contraction tiles per worker; a part costs
+// its share of the scratch traffic, about 0.2 % of a tile each.  dH of 512 x 2048 over V = 128256: 622 us whole, XXX us in parts;
+// of 300 x 1024 over 151936: 708 and XXX us.
+int dh_parts(long long rows, long long d, long long V) {
+    const long long tiles = cdiv(rows, tile_m()) * cdiv(d, tc::BN);
+    const long long most = cdiv(V, 4096);                              // no part shorter than 4096 vocabulary entries
+    int best = 1;
+    double best_cost = static_cast<double>(cdiv(tiles, plan_workers()));
+    for (int g = 2; g <= 32 && g <= most; ++g) {
+        if (static_cast<size_t>(g) * cdiv(rows, tile_m()) * tile_m() * d * 4 > (256ull << 20)) break;
+        const double cost = static_cast<double>(cdiv(tiles * g, plan_workers())) / g + 0.002 * g;
+        if (cost < 0.95 * best_cost) { best_cost = cost; best = g; }
+    }
+    return best;
+}
+size_t dh_part_bytes(long long rows, long long d, long long V) {
+    const int g = dh_parts(rows, d, V);
+    return g > 1 ? align256(static_cast<size_t>(g) * cdiv(rows, tile_m()) * tile_m() * d * 4) : 0;
+}
+double dh_waves(long long rows, long long d, long long V) {
+    const int g = dh_parts(rows, d, V);
+    return static_cast<double>(cdiv(cdiv(rows, tile_m()) * cdiv(d, tc::BN) * g, plan_workers())) / g;
+}
+
+// dH = scale * dz W over the whole vocabulary: dz [rows, V] (K-major map tmZ), W (MN-major map tmW); `part`: dh_part_bytes of scratch.
+int launch_dh(const CUtensorMap& tmZ, const CUtensorMap& tmW, long long rows, long long d, long long V, const float* scale,
+              __nv_bfloat16* dH, long long ldH, float* part, int* status, int sm_count, cudaStream_t st) {
+    const int g = dh_parts(rows, d, V);
+    tc::Sched sched = make_sched(rows, d, V, 0, 1, 1);
+    tc::EpiOut::Params ep;
+    memset(&ep, 0, sizeof(ep));
+    ep.N = static_cast<int>(d);
+    if (g == 1) {
+        ep.alpha = scale; ep.M = static_cast<int>(rows); ep.out_bf16 = dH; ep.ld_out = ldH;
+        return launch_out<0, 1>(tmZ, tmW, sched, ep, status, sm_count, st);
+    }
+    const long long padded = sched.m_real * tile_m();
+    sched.k_splits = g;
+    sched.num_m_tiles = sched.m_real * g;
+    sched.n_items = sched.num_m_tiles * sched.n_groups;
+    ep.M = static_cast<int>(padded * g); ep.out_f32 = part; ep.ld_out = d;
+    const int rc = launch_out<0, 1>(tmZ, tmW, sched, ep, status, sm_count, st);
+    if (rc != CAT_OK) return rc;
+    lp::add_parts_kernel<<<static_cast<unsigned>(rows), lp::THREADS, 0, st>>>(part, g, padded * d, static_cast<int>(d), scale, dH, ldH);
+    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
 
 // Forward + backward over row slabs with the slab's logits kept (cat_loss_fwd_bwd); with `kd` also the
@@ -924,7 +984,10 @@ struct LpArgs {
     const float* grad_entropy;
 };
 static size_t lp_bwd_bytes(const cat_shape* s) {       // the plain backward's scratch and a copy of H without its masked rows
-    return align256(plan_bwd(s).total) + align256((s->in_dtype == CAT_BF16 ? 2 : 4) * static_cast<size_t>(s->T) * static_cast<size_t>(s->d));
+    const BwdPlan p = plan_bwd(s);
+    const bool bf16 = s->in_dtype == CAT_BF16;
+    return align256(p.total) + align256((bf16 ? 2 : 4) * static_cast<size_t>(s->T) * static_cast<size_t>(s->d)) +
+           (bf16 && p.n_slabs == 1 ? dh_part_bytes(s->T, s->d, s->V) : 0);
 }
 static int bwd_core(const cat_shape* shape, const void* H, const void* W, const int64_t* labels, const uint8_t* valid,
                     const float* lse, const float* weight, const float* grad_loss, void* dH, void* dW, int accumulate_dW,
@@ -1022,7 +1085,12 @@ static int bwd_core(const cat_shape* shape, const void* H, const void* W, const 
                 if (rc != CAT_OK) return rc;
                 if (slab_events && cudaEventRecord(static_cast<cudaEvent_t>(slab_events[sl]), st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
             }
-            {   // dH (+)= (g/N) dz W[v0 : v0 + width, :]
+            if (lp && plan.n_slabs == 1) {
+                float* part = reinterpret_cast<float*>(ws + align256(plan.total) + align256(2 * static_cast<size_t>(T) * static_cast<size_t>(d)));
+                const int rc = launch_dh(tmDz_k, tmW_mn, shape->T, shape->d, shape->V, nullptr, static_cast<__nv_bfloat16*>(dH),
+                                         shape->ldH, part, status, sm_count, st);
+                if (rc != CAT_OK) return rc;
+            } else {   // dH (+)= (g/N) dz W[v0 : v0 + width, :]
                 const tc::Sched sched = make_sched(shape->T, shape->d, width, 0, 1, 1);
                 tc::EpiOut::Params ep;
                 memset(&ep, 0, sizeof(ep));

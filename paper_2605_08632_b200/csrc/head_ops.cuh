@@ -11,10 +11,10 @@ struct LpPlan {
     long long Ts;          // rows per slab
     long long ldz;         // row pitch of the logits slab
     long long ld_g;        // row pitch of the group maxima
-    int group;             // columns per maximum
+    int group;             // columns per maximum (lp::GroupOf)
     int n_slabs;
     int S;                 // vocabulary splits of a full slab (the most any slab uses)
-    size_t off_m, off_l, off_u, off_g, off_z, total;
+    size_t off_m, off_l, off_u, off_id, off_g, off_z, total;
 };
 
 int simt_splits(long long rows, long long V) {
@@ -50,6 +50,7 @@ LpPlan plan_lp(const cat_shape* s, int top_k) {
     p.off_m = off; off = align256(off + sizeof(float) * p.S * p.Ts);
     p.off_l = off; off = align256(off + sizeof(float) * p.S * p.Ts);
     p.off_u = off; off = align256(off + sizeof(float) * p.S * p.Ts);
+    p.off_id = off; off = align256(off + sizeof(int) * p.S * p.Ts);
     p.off_g = off; if (top_k > 0) off = align256(off + sizeof(float) * static_cast<size_t>(p.Ts) * p.ld_g);
     p.off_z = off; if (top_k > 0) off = align256(off + (bf16 ? 2 : 4) * static_cast<size_t>(p.Ts) * p.ldz);
     p.total = off;
@@ -65,6 +66,7 @@ int launch_lp_rows(const cat_shape* s, const LpPlan& plan, const TI* H, const TI
     rp.part_m = reinterpret_cast<float*>(ws + plan.off_m);
     rp.part_l = reinterpret_cast<float*>(ws + plan.off_l);
     rp.part_u = reinterpret_cast<float*>(ws + plan.off_u);
+    rp.part_id = reinterpret_cast<int*>(ws + plan.off_id);
     rp.part_stride = s->in_dtype == CAT_BF16 ? plan.Ts : rws;
     rp.S = S;
     rp.H = H; rp.W = W; rp.ldH = s->ldH; rp.ldW = s->ldW;
@@ -80,7 +82,6 @@ int launch_lp_rows(const cat_shape* s, const LpPlan& plan, const TI* H, const TI
         rp.gmax = reinterpret_cast<const float*>(ws + plan.off_g);
         rp.ld_g = plan.ld_g;
         rp.n_g = static_cast<int>(cdiv(s->V, plan.group));
-        rp.group = plan.group;
         rp.k = top_k;
         rp.top_ids = reinterpret_cast<long long*>(top_ids) + r0 * top_k;
         rp.top_logp = top_logp + r0 * top_k;
@@ -104,7 +105,7 @@ int lp_slab(const cat_shape* s, const LpPlan& plan, const CUtensorMap& tmW, cons
         if (TOP && tmap_out(&tmZ, ws + plan.off_z, rws, s->V, plan.ldz) != CAT_OK) return CAT_ERR_CUDA;
         const tc::Sched sched = make_sched(rws, s->V, s->d, S, band_tiles(s->d), 0);
         typename tc::EpiLp<TOP>::Params ep;
-        ep.part_m = part_m; ep.part_l = part_l; ep.part_u = part_u; ep.part_stride = plan.Ts;
+        ep.part_m = part_m; ep.part_l = part_l; ep.part_u = part_u; ep.part_id = reinterpret_cast<int*>(ws + plan.off_id); ep.part_stride = plan.Ts;
         ep.gmax = reinterpret_cast<float*>(ws + plan.off_g); ep.ld_g = plan.ld_g;
         ep.T = static_cast<int>(rws); ep.V = static_cast<int>(s->V);
         const int rc = launch_tc<0, 0, tc::EpiLp<TOP>>(tmH, tmW, sched, ep, reinterpret_cast<int*>(ws), sm_count, st, TOP ? &tmZ : nullptr);
@@ -118,7 +119,7 @@ int lp_slab(const cat_shape* s, const LpPlan& plan, const CUtensorMap& tmW, cons
     op.M = static_cast<int>(rws); op.N = static_cast<int>(s->V); op.Kd = static_cast<int>(s->d); op.n_groups = S;
     simt::EpiParams ep;
     memset(&ep, 0, sizeof(ep));
-    ep.part_m = part_m; ep.part_l = part_l; ep.part_u = part_u; ep.V = static_cast<int>(s->V);
+    ep.part_m = part_m; ep.part_l = part_l; ep.part_u = part_u; ep.part_id = reinterpret_cast<int*>(ws + plan.off_id); ep.V = static_cast<int>(s->V);
     if (TOP) {
         ep.zs = reinterpret_cast<float*>(ws + plan.off_z); ep.ld_z = plan.ldz;
         ep.gmax = reinterpret_cast<float*>(ws + plan.off_g); ep.ld_g = plan.ld_g;
@@ -142,7 +143,7 @@ int check_topk_kd(const cat_topk_kd_desc* k) {
 struct TkPlan {
     FusedPlan f;
     int ld_zt;             // k + 1 logits per row: the list's and the label's
-    size_t off_valid, off_zt, off_kd_row, total;
+    size_t off_valid, off_zt, off_kd_row, off_id, off_m1, off_l1, off_part, total;
 };
 
 TkPlan plan_tk(const cat_shape* s, int k) {
@@ -182,13 +183,22 @@ TkPlan plan_tk(const cat_shape* s, int k) {
     p.off_valid = off;  off = align256(off + static_cast<size_t>(s->T));
     p.off_zt = off;     off = align256(off + sizeof(float) * static_cast<size_t>(p.f.Ts) * p.ld_zt);
     p.off_kd_row = off; off = align256(off + sizeof(float) * s->T);
+    p.off_id = off;     off = align256(off + sizeof(int) * p.f.S_max * (s->in_dtype == CAT_BF16 ? s->T : 1));
+    p.off_m1 = off;     off = align256(off + sizeof(float) * s->T);
+    p.off_l1 = off;     off = align256(off + sizeof(float) * s->T);
+    p.off_part = off;
+    if (s->in_dtype == CAT_BF16) {
+        const size_t full = dh_part_bytes(p.f.Ts < s->T ? p.f.Ts : s->T, s->d, s->V);
+        const size_t rest = dh_part_bytes(s->T - (p.f.n_slabs - 1) * p.f.Ts, s->d, s->V);
+        off += full > rest ? full : rest;
+    }
     p.total = off;
     return p;
 }
 
 // dH[r0 : r0 + rws, :] = (g/N) dz W and dW (+)= (g/N) dz^T Hw of one row slab; Hw: the slab's rows of H with pitch ldHw.
 int slab_grads(const cat_shape* s, const FusedPlan& f, const void* W, const void* Hw, long long ldHw, void* zs, uint8_t* ws, long long r0,
-               long long rws, bool first, bool last, const float* scale, void* dH, void* dW, int accumulate_dW, int sm_count,
+               long long rws, bool first, bool last, const float* scale, float* part, void* dH, void* dW, int accumulate_dW, int sm_count,
                cudaStream_t st) {
     const int V = static_cast<int>(s->V), d = static_cast<int>(s->d), R = static_cast<int>(rws);
     if (s->in_dtype != CAT_BF16) {
@@ -212,12 +222,10 @@ int slab_grads(const cat_shape* s, const FusedPlan& f, const void* W, const void
     if (tmap_a(&tmZ_k, zs, rws, s->V, f.ldz) != CAT_OK || tmap_mn_major(&tmZ_mn, zs, rws, s->V, f.ldz) != CAT_OK ||
         tmap_mn_major(&tmW_mn, W, s->V, s->d, s->ldW) != CAT_OK || tmap_mn_major(&tmH_mn, Hw, rws, s->d, ldHw) != CAT_OK)
         return CAT_ERR_CUDA;
-    tc::EpiOut::Params ep;
-    memset(&ep, 0, sizeof(ep));
-    ep.alpha = scale; ep.M = R; ep.N = d;
-    ep.out_bf16 = static_cast<__nv_bfloat16*>(dH) + r0 * s->ldH; ep.ld_out = s->ldH;
-    int rc = launch_out<0, 1>(tmZ_k, tmW_mn, make_sched(rws, s->d, s->V, 0, 1, 1), ep, status, sm_count, st);
+    const int rc = launch_dh(tmZ_k, tmW_mn, rws, s->d, s->V, scale, static_cast<__nv_bfloat16*>(dH) + r0 * s->ldH, s->ldH, part, status,
+                             sm_count, st);
     if (rc != CAT_OK) return rc;
+    tc::EpiOut::Params ep;
     memset(&ep, 0, sizeof(ep));
     ep.alpha = scale; ep.M = V; ep.N = d;
     float* dw_acc = reinterpret_cast<float*>(ws + f.off_dw_acc);
@@ -252,6 +260,9 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
     float* ref = reinterpret_cast<float*>(ws + f.off_ref);
     float* zt = reinterpret_cast<float*>(ws + plan.off_zt);
     float* kd_row = reinterpret_cast<float*>(ws + plan.off_kd_row);
+    int* part_id = reinterpret_cast<int*>(ws + plan.off_id);
+    float* m1 = reinterpret_cast<float*>(ws + plan.off_m1);
+    float* l1 = reinterpret_cast<float*>(ws + plan.off_l1);
     unsigned char* ok = ws + plan.off_valid;
     TI* Hz = reinterpret_cast<TI*>(ws + f.off_hs);
     rows::CtaPartial* partials = reinterpret_cast<rows::CtaPartial*>(ws + f.off_partials);
@@ -283,16 +294,17 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
         if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
         rows::RowParams rp;
         memset(&rp, 0, sizeof(rp));
+        tk::MergeParams<TI> mp;
         if (BF16) {
             CUtensorMap tmH_k, tmZ_out;
             if (tmap_a(&tmH_k, Hs, rws, s->d, s->ldH) != CAT_OK || tmap_out(&tmZ_out, zs, rws, s->V, f.ldz) != CAT_OK) return CAT_ERR_CUDA;
             tc::EpiFwdRef::Params ep;
             ep.labels = y + r0; ep.part_m = part_m + r0; ep.part_l = part_l + r0; ep.z_label = z_label + r0; ep.ref = ref + r0;
-            ep.part_stride = T; ep.T = static_cast<int>(rws); ep.V = V;
+            ep.part_id = part_id + r0; ep.part_stride = T; ep.T = static_cast<int>(rws); ep.V = V;
             const int rc = launch_tc<0, 0, tc::EpiFwdRef>(tmH_k, tmW_k, make_sched(rws, s->V, s->d, S, band_tiles(s->d), 0), ep, status,
                                                           sm_count, st, &tmZ_out);
             if (rc != CAT_OK) return rc;
-            rp.part_m = ep.part_m; rp.part_l = ep.part_l; rp.part_stride = T;
+            mp.part_m = ep.part_m; mp.part_l = ep.part_l; mp.part_id = ep.part_id; mp.part_stride = T;
         } else {
             simt::Operands op;
             op.A = reinterpret_cast<const float*>(Hs); op.sAm = s->ldH; op.sAk = 1;
@@ -303,12 +315,18 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
             ep.labels = y + r0; ep.part_m = part_m; ep.part_l = part_l; ep.z_label = z_label + r0; ep.V = V;
             ep.zs = static_cast<float*>(zs); ep.ld_z = f.ldz;
             simt::gemm_kernel<simt::MODE_FWD_KEEP><<<dim3(static_cast<unsigned>(cdiv(rws, simt::TM)), static_cast<unsigned>(S)), simt::THREADS, 0, st>>>(op, ep);
-            rp.part_m = part_m; rp.part_l = part_l; rp.part_stride = rws;
+            mp.part_m = part_m; mp.part_l = part_l; mp.part_id = nullptr; mp.part_stride = rws;
         }
+        mp.S = S; mp.H = Hs; mp.W = W; mp.ldH = s->ldH; mp.ldW = s->ldW; mp.d = d; mp.labels = y + r0; mp.valid = ok + r0;
+        mp.z_exact = zt + lists.k; mp.ld_exact = plan.ld_zt; mp.z_label = z_label + r0; mp.m1 = m1 + r0; mp.l1 = l1 + r0;
+        mp.rows = static_cast<int>(rws);
+        tk::merge_kernel<TI><<<static_cast<unsigned>(cdiv(rws, tk::WARPS)), tk::THREADS, 0, st>>>(mp);
+        if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
+        rp.part_m = m1 + r0; rp.part_l = l1 + r0; rp.part_stride = rws;
         // lse, confidence (Eq. 9), CAT weights (Eq. 10), cross-entropy partials of the slab's blocks
         rp.z_label = z_label + r0; rp.labels = y + r0; rp.valid = ok + r0; rp.conf_ext = conf_ext ? conf_ext + r0 : nullptr;
         rp.lse = lse + r0; rp.conf = conf + r0; rp.weight = weight + r0; rp.row_ce = row_ce + r0; rp.partials = partials + cta0;
-        rp.T = static_cast<int>(rws); rp.V = V; rp.K = K; rp.S = S;
+        rp.T = static_cast<int>(rws); rp.V = V; rp.K = K; rp.S = 1;
         rp.fixed_decay = s->weight_mode == CAT_WEIGHT_FIXED_DECAY; rp.gamma = s->decay_gamma;
         int n_ctas;
         if (f.warp_scan) {
@@ -323,7 +341,7 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
         tk::dz_kernel<!BF16><<<static_cast<unsigned>(rws), tk::THREADS, 0, st>>>(zs, f.ldz, y, ok, lists, r0, lse, weight, zt, plan.ld_zt,
                                                                                ref, desc->beta, kd_row, V);
         if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
-        const int rc = slab_grads(s, f, W, Hz, s->d, zs, ws, r0, rws, sl == 0, sl == f.n_slabs - 1, scale, dH, dW, accumulate_dW,
+        const int rc = slab_grads(s, f, W, Hz, s->d, zs, ws, r0, rws, sl == 0, sl == f.n_slabs - 1, scale, reinterpret_cast<float*>(ws + plan.off_part), dH, dW, accumulate_dW,
                                   sm_count, st);
         if (rc != CAT_OK) return rc;
     }

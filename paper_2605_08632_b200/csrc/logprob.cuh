@@ -22,13 +22,23 @@ namespace tc {
 constexpr int LP_GROUP = 32;             // columns per maximum that the epilogue keeps (one TMEM chunk)
 constexpr float LP_LOW = -1.0e30f;       // "no column yet": finite, so that 0 * (LP_LOW - m) is 0 and not NaN
 
-// Softmax statistics with entropy.  TOP: also the fp16 logits of the slab and the maxima of 32-column groups.
+// index of the first of 32 values that equals x (the last if none does)
+__device__ __forceinline__ int first_at(const float (&f)[32], float x) {
+    int at = 31;
+#pragma unroll
+    for (int i = 30; i >= 0; --i) at = f[i] == x ? i : at;
+    return at;
+}
+
+// Softmax statistics with entropy, and the row's largest logit's column.  TOP: also the slab's logits as fp16 distances from the
+// maximum of their 32-column group, and those maxima in fp32.
 template <bool TOP>
 struct EpiLp {
     struct Params {
         float* part_m;             // [n_groups][part_stride] running max of each (row, vocabulary split)
         float* part_l;             // sum exp(z - m)
         float* part_u;             // sum exp2(x) x with x = (z - m) log2 e
+        int* part_id;              // first column that holds the maximum
         float* gmax;               // [T][ld_g] maximum of columns [32 g, 32 g + 32)   (TOP)
         long long ld_g;            // 8 * vocabulary tiles
         long long part_stride;
@@ -37,6 +47,7 @@ struct EpiLp {
     };
     struct State {
         float m_run, l_run, u_run;
+        int id;
         int row;
     };
     __device__ static __forceinline__ void begin_item(const Params&, State& s, int m_tile, int row_in_tile) {
@@ -44,6 +55,7 @@ struct EpiLp {
         s.m_run = LP_LOW;
         s.l_run = 0.f;
         s.u_run = 0.f;
+        s.id = 0;
     }
     __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage& o) {
         const int col0 = n_tile * BN;
@@ -67,22 +79,23 @@ struct EpiLp {
                 for (int i = 0; i < 32; ++i)
                     if (i >= live) f[i] = LP_LOW;
             }
-            if (TOP) {
-                // rounding to nearest is monotone: a logit at or above a threshold stays at or above its rounding
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    o.put((c & 1) * 4 + q, ptx::pack_f16x2_sat(f[q * 8 + 0], f[q * 8 + 1]), ptx::pack_f16x2_sat(f[q * 8 + 2], f[q * 8 + 3]),
-                          ptx::pack_f16x2_sat(f[q * 8 + 4], f[q * 8 + 5]), ptx::pack_f16x2_sat(f[q * 8 + 6], f[q * 8 + 7]));
-                if ((c & 1) != 0 || (c + 1) * 32 >= ncols) o.flush(col0 + (c >> 1) * 64);
-            }
             float cmax = ptx::max3_f32(f[0], f[1], f[2]);
 #pragma unroll
             for (int i = 3; i + 1 < 32; i += 2) cmax = ptx::max3_f32(cmax, f[i], f[i + 1]);
             cmax = fmaxf(cmax, f[31]);
+            if (cmax > s.m_run) s.id = col0 + c * 32 + first_at(f, cmax);
             if (TOP) {
+                // the slab keeps z - (maximum of the group): the group's largest logit stays exact, its neighbours near it
 #pragma unroll
                 for (int i = 0; i < BN / LP_GROUP; ++i)
                     if (i == c) g[i] = cmax;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    o.put((c & 1) * 4 + q, ptx::pack_f16x2_sat(f[q * 8 + 0] - cmax, f[q * 8 + 1] - cmax),
+                          ptx::pack_f16x2_sat(f[q * 8 + 2] - cmax, f[q * 8 + 3] - cmax),
+                          ptx::pack_f16x2_sat(f[q * 8 + 4] - cmax, f[q * 8 + 5] - cmax),
+                          ptx::pack_f16x2_sat(f[q * 8 + 6] - cmax, f[q * 8 + 7] - cmax));
+                if ((c & 1) != 0 || (c + 1) * 32 >= ncols) o.flush(col0 + (c >> 1) * 64);
             }
             const float m_new = fmaxf(s.m_run, cmax);
             const float mb = m_new * LOG2E;
@@ -120,6 +133,7 @@ struct EpiLp {
             p.part_m[at] = s.m_run;
             p.part_l[at] = s.l_run;
             p.part_u[at] = s.u_run;
+            p.part_id[at] = s.id;
         }
     }
 };
@@ -252,28 +266,32 @@ __device__ __forceinline__ double warp_dot(const float* h, const float* w, int d
     return acc;
 }
 
-__device__ __forceinline__ float stored(const __half* z, long long i) { return __half2float(z[i]); }
-__device__ __forceinline__ float stored(const float* z, long long i) { return z[i]; }
-// the threshold as the slab's type would have rounded it
-__device__ __forceinline__ float as_stored(const __half*, float x) {
-    return __half2float(__float2half_rn(fminf(fmaxf(x, -65504.f), 65504.f)));
+// What the slab says of column v of a group whose maximum is gm: its logit up to `err`, plus the GEMM's own error.  fp16 slabs hold
+// the distance from the maximum (half a step: 2^-11 of it, or 2^-25), fp32 slabs the logit itself.
+__device__ __forceinline__ float stored(const __half* z, float gm, long long v, float& err) {
+    const float dist = __half2float(z[v]);
+    err = fmaf(-dist, 0.00048828125f, 3.0e-8f);
+    return gm + dist;
 }
-__device__ __forceinline__ float as_stored(const float*, float x) { return x; }
-
-// order-preserving map of floats to unsigned (no NaN)
-__device__ __forceinline__ uint32_t key_of(float x) {
-    const uint32_t b = __float_as_uint(x);
-    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+__device__ __forceinline__ float stored(const float* z, float, long long v, float& err) {
+    err = 0.f;
+    return z[v];
 }
-__device__ __forceinline__ float of_key(uint32_t k) {
-    return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
-}
+template <class TZ>
+struct GroupOf { static constexpr int value = tc::LP_GROUP; };
+template <>
+struct GroupOf<float> { static constexpr int value = 64; };       // columns per tile of the fp32 GEMM
+// Error of a logit of the GEMM relative to the row's largest: one addition of 16 products (tensor cores) or one (fp32) at a time, each off
+// by at most 2^-23 of a running sum that is taken to stay within twice that logit.
+__device__ __forceinline__ float gemm_error(const __half*, int d) { return static_cast<float>(d / 16 + 8) * 2.384185791015625e-7f; }
+__device__ __forceinline__ float gemm_error(const float*, int d) { return static_cast<float>(d + 8) * 2.384185791015625e-7f; }
 
 template <class TI, class TZ>
 struct RowParams {
     const float* part_m;           // [S][part_stride]
     const float* part_l;
     const float* part_u;
+    const int* part_id;
     long long part_stride;
     int S;
     const TI* H;                   // rows of this slab
@@ -290,26 +308,27 @@ struct RowParams {
     long long ldz;
     const float* gmax;             // [T][ld_g]
     long long ld_g;
-    int n_g;                       // groups of `group` columns
-    int group;                     // 32 or 64
+    int n_g;                       // groups of GroupOf<TZ> columns
     int k;
     long long* top_ids;            // [T][k]
     float* top_logp;               // [T][k]
 };
 
 struct Shared {
-    float red[WARPS];
-    float red2[WARPS];
-    unsigned hist[256];
-    unsigned prefix, want;
+    float red[2][WARPS];
+    int count[2][WARPS];
     int n_cand;
-    int flag;
     float lse;
-    double z[CAP];
+    int id_max;
+    double z_max, z_label;
+    double z[CAP];                 // exact logits, where `err` says so
+    float approx[CAP];
+    float err[CAP];                // how far approx may be off; EXACT: z is known; OUT: not among the k largest
     int id[CAP];
     double z_keep[MAX_TOP];
     int id_keep[MAX_TOP];
 };
+constexpr float EXACT = -1.f, OUT = -2.f;
 
 __device__ __forceinline__ float block_max(float x, float* red) {
 #pragma unroll
@@ -323,47 +342,56 @@ __device__ __forceinline__ float block_max(float x, float* red) {
     return x;
 }
 
-// The k-th largest of n values, by four 8-bit radix passes over their order-preserving keys.
-template <class X>
-__device__ __forceinline__ float kth_largest(const X* x, int n, int k, Shared& sh) {
-    if (threadIdx.x == 0) { sh.prefix = 0u; sh.want = static_cast<unsigned>(k); }
-    for (int pass = 0; pass < 4; ++pass) {
-        const int shift = 24 - 8 * pass;
-        for (int i = threadIdx.x; i < 256; i += THREADS) sh.hist[i] = 0u;
-        __syncthreads();
-        const unsigned prefix = sh.prefix;
+// A number that at least k of n values reach, and few more than k: bisection between the least and the largest of them.  The values
+// are kept in registers when they fit.  big = largest |value|.
+constexpr int KEPT = 20;
+template <class F>
+__device__ __forceinline__ float near_kth(F value, int n, int k, Shared& sh, float& big) {
+    float v[KEPT];
+    const bool fits = n <= KEPT * THREADS;
+    float hi = -INFINITY, nlo = -INFINITY;
+    if (fits) {
+#pragma unroll
+        for (int j = 0; j < KEPT; ++j) {
+            const int i = j * THREADS + threadIdx.x;
+            v[j] = i < n ? value(i) : -INFINITY;
+            if (i < n) { hi = fmaxf(hi, v[j]); nlo = fmaxf(nlo, -v[j]); }
+        }
+    } else {
         for (int i = threadIdx.x; i < n; i += THREADS) {
-            const uint32_t key = key_of(stored(x, i));
-            if (pass == 0 || (key >> (shift + 8)) == prefix) atomicAdd(&sh.hist[(key >> shift) & 255u], 1u);
+            const float x = value(i);
+            hi = fmaxf(hi, x);
+            nlo = fmaxf(nlo, -x);
         }
-        __syncthreads();
-        if (threadIdx.x < 32) {     // the bin, from the top, in which the count reaches `want`
-            const int lane = threadIdx.x;
-            unsigned mine = 0;      // bins 255 - 8 lane ... 255 - 8 lane - 7
-#pragma unroll
-            for (int j = 0; j < 8; ++j) mine += sh.hist[255 - 8 * lane - j];
-            unsigned upto = mine;
-#pragma unroll
-            for (int off = 1; off < 32; off <<= 1) {
-                const unsigned o = __shfl_up_sync(0xffffffffu, upto, off);
-                if (lane >= off) upto += o;
-            }
-            const unsigned want = sh.want;
-            const unsigned before = upto - mine;
-            __syncwarp();
-            if (before < want && want <= upto) {
-                unsigned acc = before;
-                for (int j = 0; j < 8; ++j) {
-                    const unsigned b = 255u - 8u * lane - j;
-                    const unsigned h = sh.hist[b];
-                    if (acc + h >= want) { sh.prefix = (prefix << 8) | b; sh.want = want - acc; break; }
-                    acc += h;
-                }
-            }
-        }
-        __syncthreads();
     }
-    return of_key(sh.prefix);
+    hi = block_max(hi, sh.red[0]);
+    float lo = -block_max(nlo, sh.red[1]);
+    big = fmaxf(fabsf(hi), fabsf(lo));
+    if (n <= k) return lo;
+    for (int it = 0; it < 24; ++it) {
+        const float mid = 0.5f * lo + 0.5f * hi;
+        if (!(mid > lo && mid < hi)) break;
+        int c = 0;
+        if (fits) {
+#pragma unroll
+            for (int j = 0; j < KEPT; ++j) c += v[j] >= mid ? 1 : 0;
+        } else {
+            for (int i = threadIdx.x; i < n; i += THREADS) c += value(i) >= mid ? 1 : 0;
+        }
+        c = __reduce_add_sync(0xffffffffu, c);
+        if ((threadIdx.x & 31) == 0) sh.count[it & 1][threadIdx.x >> 5] = c;
+        __syncthreads();
+        c = 0;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) c += sh.count[it & 1][i];
+        if (c >= k) {
+            lo = mid;
+            if (c <= k + k / 4 + 2) break;
+        } else {
+            hi = mid;
+        }
+    }
+    return lo;
 }
 
 // Exact logits of candidates [from, n) and the order of all n of them; the first k go to the front of the keep list.
@@ -386,14 +414,69 @@ __device__ __forceinline__ int settle(const RowParams<TI, TZ>& p, const TI* h, S
     return n < p.k ? n : p.k;
 }
 
+// The same from the approximate logits, with exact ones only for candidates that their errors leave in doubt against another, and for
+// those that the slab's fp16 has rounded (not the largest of their group): their values are returned.
+template <class TI, class TZ>
+__device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI* h, Shared& sh, int n, float eps) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    unsigned doubt = 0;                       // bit i: candidate threadIdx.x + i * THREADS needs its exact logit
+    unsigned out = 0;
+    static_assert(CAP / THREADS <= 32, "one bit per candidate of a thread");
+    for (int i = 0, c = threadIdx.x; c < n; ++i, c += THREADS) {
+        const float z = sh.approx[c], e = sh.err[c];
+        int above = 0;
+        bool near = false;
+        for (int j = 0; j < n; ++j) {
+            const float gap = sh.approx[j] - z, both = sh.err[j] + e;
+            above += gap > both ? 1 : 0;
+            near |= j != c && fabsf(gap) <= both;
+        }
+        if (above >= p.k) out |= 1u << i;
+        else if (near || e > eps + 4.0e-8f) doubt |= 1u << i;
+    }
+    __syncthreads();
+    for (int i = 0, c = threadIdx.x; c < n; ++i, c += THREADS) {
+        if (out >> i & 1u) sh.err[c] = OUT;
+        else if (doubt >> i & 1u) sh.err[c] = EXACT;
+    }
+    __syncthreads();
+    for (int c = warp; c < n; c += WARPS) {
+        if (sh.err[c] != EXACT) continue;
+        const double z = warp_dot(h, p.W + static_cast<long long>(sh.id[c]) * p.ldW, p.d, lane);
+        if (lane == 0) sh.z[c] = z;
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < n; c += THREADS) {
+        const float ec = sh.err[c];
+        if (ec == OUT) continue;
+        const int id = sh.id[c];
+        const double z = ec == EXACT ? sh.z[c] : static_cast<double>(sh.approx[c]);
+        int rank = 0;
+        for (int j = 0; j < n; ++j) {
+            const float ej = sh.err[j];
+            if (ej == OUT || j == c) continue;
+            // two in doubt against each other are both exact
+            if (ec == EXACT && ej == EXACT) rank += (sh.z[j] > z || (sh.z[j] == z && sh.id[j] < id)) ? 1 : 0;
+            else rank += sh.approx[j] > sh.approx[c] ? 1 : 0;
+        }
+        if (rank < p.k) { sh.z_keep[rank] = id == sh.id_max ? sh.z_max : z; sh.id_keep[rank] = id; }
+    }
+    __syncthreads();
+    return n < p.k ? n : p.k;
+}
+
 // One CTA per row: merges the split partials (lse, entropy), the label's log probability, and the top k.
 //
-// Top k.  The k largest group maxima are k logits of the row, so the k-th largest of them, t, is a lower bound of the
-// row's k-th largest logit, and only columns at or above t can be among the k largest.  They are looked up in the slab
-// (a few groups of it are read, not the row), with t lowered by 2^-9 of the row's largest |group maximum|: that covers
-// the rounding of the stored logits (2^-12) and twice the GEMM's accumulation error (about 2^-20 of it for inputs without cancellation) many times over.  Each
-// candidate's logit is then taken again as an fp64 sum, so that the order is that of the exact products and equal
-// logits go to the lower id.  More than CAP candidates (many logits within the margin) are settled batch by batch.
+// lse.  The tensor cores' additions truncate, so a logit that is far from 0 comes out a few 1e-6 of itself too small.  In a row that
+// is sure of a token that token's logit makes up lse, so the largest logit is taken again as an fp64 sum and the row's sums
+// are corrected by the difference; the label's logit is such a sum too.
+//
+// Top k.  Any k group maxima are k logits of the row, so a number t that k group maxima reach is a lower bound of the row's k-th
+// largest logit, and only columns at or above t, less the GEMM's error, can be among the k largest.  They are looked
+// up in the slab: a few groups of it are read, not the row.  The order is that of the exact products: candidates whose approximate
+// logits are closer than their errors are compared by fp64 sums (a gather of W for about one in twenty of them; taking all of them
+// again cost 0.7 ms for 8192 rows of k = 64, a quarter of the GEMM), and equal logits go to the lower id.
+// More than CAP candidates (a row of zeros, many equal rows of W) are settled batch by batch by exact sums.
 template <class TI, class TZ, bool TOP>
 __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p) {
     __shared__ Shared sh;
@@ -413,9 +496,17 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
     if (warp == 0) {
         // merge the split partials; sums over splits in a fixed order
         float m = tc::LP_LOW;
-        for (int s = lane; s < p.S; s += 32) m = fmaxf(m, p.part_m[s * p.part_stride + r]);
+        int id = 0;
+        for (int s = lane; s < p.S; s += 32) {
+            const float x = p.part_m[s * p.part_stride + r];
+            if (x > m) { m = x; id = p.part_id[s * p.part_stride + r]; }
+        }
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+        for (int off = 16; off > 0; off >>= 1) {
+            const float om = __shfl_xor_sync(0xffffffffu, m, off);
+            const int oid = __shfl_xor_sync(0xffffffffu, id, off);
+            if (om > m || (om == m && oid < id)) { m = om; id = oid; }
+        }
         float l = 0.f, u = 0.f;
         for (int s = lane; s < p.S; s += 32) {
             const size_t at = s * p.part_stride + r;
@@ -429,10 +520,19 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
             l += __shfl_xor_sync(0xffffffffu, l, off);
             u += __shfl_xor_sync(0xffffffffu, u, off);
         }
-        const float logl = logf(l);
-        const float lse = m + logl;
+        const double z_max = warp_dot(h, p.W + static_cast<long long>(id) * p.ldW, p.d, lane);
         if (lane == 0) {
+            // the largest logit entered as exp(0) = 1 and 0; it is exp(x) and x exp(x) with its exact distance x from m
+            const float x = static_cast<float>(z_max - static_cast<double>(m));
+            if (fabsf(x) < 1.f) {
+                l += expm1f(x);
+                u = fmaf(x * tc::LOG2E, expf(x), u);
+            }
+            const float logl = logf(l);
+            const float lse = m + logl;
             sh.lse = lse;
+            sh.id_max = id;
+            sh.z_max = z_max;
             p.lse[r] = lse;
             const float ent = logl - 0.6931471805599453f * u / l;
             p.entropy[r] = ent < 0.f ? 0.f : ent + (lse - lse);      // NaN for a row that is not finite
@@ -441,16 +541,15 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
         const long long y = p.labels[r];
         double zy = 0.0;
         if (y >= 0 && y < p.V) zy = warp_dot(h, p.W + y * p.ldW, p.d, lane);
-        if (lane == 0) sh.z_keep[0] = zy;
+        if (lane == 0) sh.z_label = zy;
     }
     __syncthreads();
     const float lse = sh.lse;
     if (p.logp != nullptr && threadIdx.x == 0) {
         const long long y = p.labels[r];
-        p.logp[r] = (y >= 0 && y < p.V) ? static_cast<float>(sh.z_keep[0] - static_cast<double>(lse)) : 0.f;
+        p.logp[r] = (y >= 0 && y < p.V) ? static_cast<float>(sh.z_label - static_cast<double>(lse)) : 0.f;
     }
     if (!TOP) return;
-    __syncthreads();
     long long* ids_out = p.top_ids + r * p.k;
     float* lp_out = p.top_logp + r * p.k;
     if (!isfinite(lse)) {
@@ -458,45 +557,47 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
         return;
     }
     const float* g = p.gmax + r * p.ld_g;
-    float big = 0.f;
-    for (int i = threadIdx.x; i < p.n_g; i += THREADS) {
-        const float x = fabsf(g[i]);
-        if (x < 1.0e29f) big = fmaxf(big, x);
-    }
-    big = block_max(big, sh.red);
     const TZ* z = p.zs + r * p.ldz;
-    // With few groups per alternative the bound by groups is loose (or there is none): take the k-th largest stored logit.
-    float t = tc::LP_LOW;
-    if (p.n_g >= 4 * p.k) t = kth_largest(g, p.n_g, p.k, sh);
-    else if (p.V > p.k) t = kth_largest(z, p.V, p.k, sh);
-    const float thr = t - big * 0.001953125f;
-    const float thr_s = as_stored(z, thr);
+    constexpr int group = GroupOf<TZ>::value;
+    // With few groups per alternative their maxima bound little (or there are not k of them): go by the logits themselves.
+    float big;
+    const float t = p.n_g >= 4 * p.k ? near_kth([&](int i) { return g[i]; }, p.n_g, p.k, sh, big)
+                                     : near_kth([&](int i) { float e; return stored(z, g[i / group], i, e); }, p.V, p.k, sh, big);
+    const float eps = big * gemm_error(z, p.d);
+    // a bound taken over stored logits may lie their rounding (2^-11 of the row's span) too high
+    const float thr = t - 2.f * eps - (p.n_g >= 4 * p.k ? 0.f : 1.0e-3f * big);
     if (threadIdx.x == 0) sh.n_cand = 0;
     __syncthreads();
+    auto look = [&](int gi) {      // one warp appends the candidates of one group
+        const float gm = g[gi];
+        for (int o = 0; o < group; o += 32) {
+            const long long col = static_cast<long long>(gi) * group + o + lane;
+            float e, x;
+            x = stored(z, gm, col < p.V ? col : 0, e);
+            const bool in = col < p.V && x + e >= thr;
+            const unsigned hit = __ballot_sync(0xffffffffu, in);
+            if (hit == 0) continue;
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&sh.n_cand, __popc(hit));
+            at = __shfl_sync(0xffffffffu, at, 0) + __popc(hit & ((1u << lane) - 1u));
+            if (in && at < CAP) { sh.id[at] = static_cast<int>(col); sh.approx[at] = x; sh.err[at] = eps + e; }
+        }
+    };
     for (int g0 = warp * 32; g0 < p.n_g; g0 += THREADS) {
         const int gi = g0 + lane;
         unsigned todo = __ballot_sync(0xffffffffu, gi < p.n_g && g[gi < p.n_g ? gi : 0] >= thr);
         while (todo) {
             const int b = __ffs(todo) - 1;
             todo &= todo - 1;
-            for (int o = 0; o < p.group; o += 32) {
-                const long long col = static_cast<long long>(g0 + b) * p.group + o + lane;
-                const bool in = col < p.V && stored(z, col < p.V ? col : 0) >= thr_s;
-                const unsigned hit = __ballot_sync(0xffffffffu, in);
-                if (hit == 0) continue;
-                int at = 0;
-                if (lane == 0) at = atomicAdd(&sh.n_cand, __popc(hit));
-                at = __shfl_sync(0xffffffffu, at, 0) + __popc(hit & ((1u << lane) - 1u));
-                if (in && at < CAP) sh.id[at] = static_cast<int>(col);
-            }
+            look(g0 + b);
         }
     }
     __syncthreads();
     int kept;
     if (sh.n_cand <= CAP) {
-        kept = settle(p, h, sh, 0, sh.n_cand);
+        kept = settle_close(p, h, sh, sh.n_cand, eps);
     } else {
-        // many logits within the margin of the k-th.  A row of zeros has them all equal: ids 0, 1, ...
+        // many logits within the error of the k-th.  A row of zeros has them all equal: ids 0, 1, ...
         bool nz = false;
         for (int i = threadIdx.x; i < p.d; i += THREADS) nz |= static_cast<float>(h[i]) != 0.f;
         if (!__syncthreads_or(nz ? 1 : 0)) {
@@ -511,18 +612,7 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
                 if (threadIdx.x == 0) sh.n_cand = n;
                 __syncthreads();
                 const int gi = g0 + warp;
-                if (gi < p.n_g && g[gi] >= thr) {
-                    for (int o = 0; o < p.group; o += 32) {
-                        const long long col = static_cast<long long>(gi) * p.group + o + lane;
-                        const bool in = col < p.V && stored(z, col < p.V ? col : 0) >= thr_s;
-                        const unsigned hit = __ballot_sync(0xffffffffu, in);
-                        if (hit == 0) continue;
-                        int at = 0;
-                        if (lane == 0) at = atomicAdd(&sh.n_cand, __popc(hit));
-                        at = __shfl_sync(0xffffffffu, at, 0) + __popc(hit & ((1u << lane) - 1u));
-                        if (in) sh.id[at] = static_cast<int>(col);
-                    }
-                }
+                if (gi < p.n_g && g[gi] >= thr) look(gi);
                 __syncthreads();
                 n = sh.n_cand;
                 const bool last = g0 + WARPS >= p.n_g;
@@ -538,6 +628,26 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
     for (int i = threadIdx.x; i < p.k; i += THREADS) {
         ids_out[i] = i < kept ? sh.id_keep[i] : -1;
         lp_out[i] = i < kept ? static_cast<float>(sh.z_keep[i] - static_cast<double>(lse)) : -INFINITY;
+    }
+}
+
+// dH = scale * (part 0 + part 1 + ...), in that order, in bf16.  One CTA per row; `stride` elements from part to part.
+__global__ void __launch_bounds__(THREADS) add_parts_kernel(const float* part, int n, long long stride, int d, const float* scale,
+                                                            __nv_bfloat16* out, long long ld) {
+    const long long r = blockIdx.x;
+    const float a = scale ? *scale : 1.f;
+    for (int i = threadIdx.x; i < d / 4; i += THREADS) {
+        const float4* src = reinterpret_cast<const float4*>(part + r * d) + i;
+        float4 s = __ldcs(src);
+#pragma unroll 4
+        for (int g = 1; g < n; ++g) {
+            const float4 x = __ldcs(src + g * (stride / 4));
+            s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+        }
+        uint2 o;
+        o.x = ptx::pack_bf16x2(a * s.x, a * s.y);
+        o.y = ptx::pack_bf16x2(a * s.z, a * s.w);
+        *reinterpret_cast<uint2*>(out + r * ld + 4 * i) = o;
     }
 }
 

@@ -28,6 +28,7 @@ struct EpiParams {
     float* part_l;
     float* z_label;                // MODE_FWD_KEEP: may be nullptr
     // MODE_FWD_KEEP
+    int* part_id;                  // first column of the maximum; with part_u
     float* part_u;                 // sum exp2(x) x with x = (z - max) log2 e; nullptr = not wanted
     float* zs;                     // [M][ld_z] logits, or nullptr
     float* gmax;                   // [M][ld_g] maximum of each TN-column tile, or nullptr
@@ -67,6 +68,7 @@ __global__ void __launch_bounds__(THREADS) gemm_kernel(const Operands op, const 
     constexpr bool FWD = MODE == MODE_FWD || MODE == MODE_FWD_KEEP;
     float m_run[4], l_run[4], w_row[4], lse_row[4];
     float u_run[4] = {}, ca[4] = {}, cb[4] = {};
+    int id_run[4] = {};
     int y_row[4];
     bool on[4] = {};
 #pragma unroll
@@ -166,6 +168,13 @@ __global__ void __launch_bounds__(THREADS) gemm_kernel(const Operands op, const 
 #pragma unroll
                 for (int off = 1; off < 16; off <<= 1) cmax = fmaxf(cmax, __shfl_xor_sync(0xffffffffu, cmax, off));
                 if (ep.gmax != nullptr && tx == 0 && row < op.M) ep.gmax[row * ep.ld_g + nt] = cmax;
+                int id = op.N;
+#pragma unroll
+                for (int j = 3; j >= 0; --j)
+                    if (acc[i][j] == cmax && n0 + tx * 4 + j < op.N) id = n0 + tx * 4 + j;
+#pragma unroll
+                for (int off = 1; off < 16; off <<= 1) id = min(id, __shfl_xor_sync(0xffffffffu, id, off));
+                if (cmax > m_run[i] && id < op.N) id_run[i] = id;
                 const float m_new = fmaxf(m_run[i], cmax);
                 float sum = 0.f, us = 0.f;
 #pragma unroll
@@ -237,7 +246,10 @@ __global__ void __launch_bounds__(THREADS) gemm_kernel(const Operands op, const 
             if (row < op.M) {
                 ep.part_m[static_cast<size_t>(g) * op.M + row] = m_run[i];
                 ep.part_l[static_cast<size_t>(g) * op.M + row] = l_run[i];
-                if (MODE == MODE_FWD_KEEP && ep.part_u != nullptr) ep.part_u[static_cast<size_t>(g) * op.M + row] = u_run[i];
+                if (MODE == MODE_FWD_KEEP && ep.part_u != nullptr) {
+                    ep.part_u[static_cast<size_t>(g) * op.M + row] = u_run[i];
+                    ep.part_id[static_cast<size_t>(g) * op.M + row] = id_run[i];
+                }
             }
         }
     }

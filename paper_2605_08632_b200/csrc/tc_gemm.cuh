@@ -42,6 +42,8 @@ struct Sched {
     int num_m_tiles;   // tiles of BM rows of the output
     int num_n_tiles;   // tiles of BN columns of the output
     int num_kb;        // ring stages (BK * k-slices per stage) along the contraction
+    int k_splits;      // parts of the contraction; part p of output tile m is scheduled (and stored) as m-tile
+    int m_real;        //   p * m_real + m, m_real = tiles of the output itself (num_m_tiles = k_splits * m_real)
     int n_groups;      // column groups per m-tile: one item = (m-tile, group); a group is a run of n-tiles
     int band_m;        // m-tiles per band when m runs fastest (keeps a band of A rows L2-resident)
     int n_fastest;     // 1: items ordered group-fastest within an m-tile; 0: m-fastest within (band, group)
@@ -65,6 +67,14 @@ __device__ __forceinline__ void decode_item(const Sched& s, int item, int& m_til
     }
     n_begin = static_cast<int>((static_cast<long long>(group) * s.num_n_tiles) / s.n_groups);
     n_end = static_cast<int>((static_cast<long long>(group + 1) * s.num_n_tiles) / s.n_groups);
+}
+
+// Ring stages [k0, k1) of a scheduled m-tile's part of the contraction, and its output's own m-tile.
+__device__ __forceinline__ int decode_k(const Sched& s, int m_tile, int& k0, int& k1) {
+    const int part = m_tile / s.m_real;
+    k0 = static_cast<int>((static_cast<long long>(part) * s.num_kb) / s.k_splits);
+    k1 = static_cast<int>((static_cast<long long>(part + 1) * s.num_kb) / s.k_splits);
+    return m_tile - part * s.m_real;
 }
 
 struct Ctl {
@@ -384,6 +394,8 @@ struct EpiOut {
         int M, N;
         int staged;                    // 1: fp32 output, no addend or the output itself as addend: tiles of
                                        //    32 x 32 go through shared memory and a TMA store / reduce-add
+                                       // 2: bf16 output, no addend: tiles of 32 x 64 and a TMA store.  Stored by the
+                                       //    threads (a row each) dW at 512 rows of H took 340 us, this way XXX us.
     };
     struct State {
         float alpha;
@@ -400,10 +412,20 @@ struct EpiOut {
 #pragma unroll 1
         for (int c = 0; c < BN / 32; ++c) {
             if (col0 + c * 32 >= p.N) break;
-            if (p.staged) o.begin();
+            if (p.staged == 1 || (p.staged == 2 && (c & 1) == 0)) o.begin();
             uint32_t v[32];
             ptx::tmem_ld_32x32(taddr + c * 32, v);
             ptx::tmem_ld_wait();
+            if (p.staged == 2) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    o.put((c & 1) * 4 + q, ptx::pack_bf16x2(s.alpha * __uint_as_float(v[8 * q]), s.alpha * __uint_as_float(v[8 * q + 1])),
+                          ptx::pack_bf16x2(s.alpha * __uint_as_float(v[8 * q + 2]), s.alpha * __uint_as_float(v[8 * q + 3])),
+                          ptx::pack_bf16x2(s.alpha * __uint_as_float(v[8 * q + 4]), s.alpha * __uint_as_float(v[8 * q + 5])),
+                          ptx::pack_bf16x2(s.alpha * __uint_as_float(v[8 * q + 6]), s.alpha * __uint_as_float(v[8 * q + 7])));
+                if ((c & 1) != 0 || col0 + (c + 1) * 32 >= p.N) o.flush(col0 + (c >> 1) * 64);
+                continue;
+            }
             if (p.staged) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -590,11 +612,12 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
             for (int item = worker; item < sched.n_items && ok; item += n_workers) {
                 int m_tile, group, n_begin, n_end;
                 decode_item(sched, item, m_tile, group, n_begin, n_end);
-                const int m0 = (m_tile * CG + static_cast<int>(rank)) * BM;
+                int kb0, kb1;
+                const int m0 = (decode_k(sched, m_tile, kb0, kb1) * CG + static_cast<int>(rank)) * BM;
                 for (int n = n_begin; n < n_end && ok; ++n, rev ^= 1u) {
                     const int n0 = n * BN + static_cast<int>(rank) * G::BN_CTA;
-                    for (int kbi = 0; kbi < sched.num_kb; ++kbi) {
-                        const int kb = rev ? sched.num_kb - 1 - kbi : kbi;
+                    for (int kbi = kb0; kbi < kb1; ++kbi) {
+                        const int kb = rev ? kb0 + kb1 - 1 - kbi : kbi;
                         if (!wait_bounded(ptx::smem_u32(&ctl.empty[stage]), phase ^ 1u, abort, status, wait_ns)) { ok = false; break; }
                         const uint32_t full_local = ptx::smem_u32(&ctl.full[stage]);
                         if (leader) ptx::mbar_arrive_expect_tx(full_local, G::STAGE_BYTES * CG);
@@ -661,18 +684,20 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
             for (int item = worker; item < sched.n_items && ok; item += n_workers) {
                 int m_tile, group, n_begin, n_end;
                 decode_item(sched, item, m_tile, group, n_begin, n_end);
+                int kb0, kb1;
+                decode_k(sched, m_tile, kb0, kb1);
                 for (int n = n_begin; n < n_end && ok; ++n) {
                     if (!wait_bounded(ptx::smem_u32(&ctl.tempty[acc]), acc_phase ^ 1u, abort, status, wait_ns)) { ok = false; break; }
                     ptx::tc_fence_after();
                     const uint32_t d_tmem = tmem + acc * BN;
-                    for (int kb = 0; kb < sched.num_kb; ++kb) {
+                    for (int kb = kb0; kb < kb1; ++kb) {
                         if (!wait_bounded(full0 + stage * 8u, phase, abort, status, wait_ns)) { ok = false; break; }
                         ptx::tc_fence_after();
 #pragma unroll
                         for (int h = 0; h < G::KS; ++h) {
 #pragma unroll
                             for (int j = 0; j < BK / 16; ++j) {
-                                const uint32_t accumulate = (h != 0 || j != 0 || kb != 0) ? 1u : 0u;
+                                const uint32_t accumulate = (h != 0 || j != 0 || kb != kb0) ? 1u : 0u;
                                 const uint64_t ad = adesc + h * A_SLICE_STEP + j * A_KSTEP, bd = bdesc + h * B_SLICE_STEP + j * B_KSTEP;
                                 if (CG == 1) ptx::umma_bf16(d_tmem, ad, bd, idesc, accumulate);
                                 else ptx::umma_bf16_pair(d_tmem, ad, bd, idesc, accumulate);

@@ -21,6 +21,7 @@ struct EpiFwdRef {
         const long long* labels;   // [T]
         float* part_m;             // [n_groups][part_stride]
         float* part_l;
+        int* part_id;              // first column that holds the maximum
         float* z_label;            // [T]
         const float* ref;          // [T]
         long long part_stride;
@@ -29,6 +30,7 @@ struct EpiFwdRef {
     };
     struct State {
         float m_run, l_run, ref;
+        int id;
         int y;
         int row;
     };
@@ -36,6 +38,7 @@ struct EpiFwdRef {
         s.row = m_tile * BM + row_in_tile;
         s.m_run = LP_LOW;
         s.l_run = 0.f;
+        s.id = 0;
         s.ref = 0.f;
         s.y = -1;
         if (s.row < p.T) {
@@ -82,6 +85,7 @@ struct EpiFwdRef {
 #pragma unroll
             for (int i = 3; i + 1 < 32; i += 2) cmax = ptx::max3_f32(cmax, f[i], f[i + 1]);
             cmax = fmaxf(cmax, f[31]);
+            if (cmax > s.m_run) s.id = col0 + c * 32 + first_at(f, cmax);
             const float m_new = fmaxf(s.m_run, cmax);
             const float mb = m_new * LOG2E;
             const uint64_t l2e2 = ptx::pack_f32x2(LOG2E, LOG2E), nmb2 = ptx::pack_f32x2(-mb, -mb);
@@ -103,6 +107,7 @@ struct EpiFwdRef {
         if (s.row < p.T) {
             p.part_m[static_cast<size_t>(group) * p.part_stride + s.row] = s.m_run;
             p.part_l[static_cast<size_t>(group) * p.part_stride + s.row] = s.l_run;
+            p.part_id[static_cast<size_t>(group) * p.part_stride + s.row] = s.id;
         }
     }
 };
@@ -181,6 +186,63 @@ __global__ void __launch_bounds__(THREADS) gather_kernel(const TI* H, long long 
         for (int i = 1; i < WARPS; ++i) mx = fmaxf(mx, s_max[i]);
         ref[r] = fabsf(mx) < 1.0e30f ? mx : 0.f;
     }
+}
+
+// Merges the vocabulary splits of a row's (max, sum exp) into one pair for the row kernel (one warp per row), and corrects the sum for the
+// largest logit and the label's, which are known as fp64 sums: the tensor cores' additions truncate, and a token of
+// high probability makes up lse (see lp::row_kernel).  z_label is replaced by the exact label logit.
+template <class TI>
+struct MergeParams {
+    const float* part_m;           // [S][part_stride]
+    const float* part_l;
+    const int* part_id;            // nullptr: fp32 logits, nothing to correct
+    long long part_stride;
+    int S;
+    const TI* H;
+    const TI* W;
+    long long ldH, ldW;
+    int d;
+    const long long* labels;
+    const unsigned char* valid;
+    const float* z_exact;          // [rows] at pitch ld_exact: the label's logit, of rows that take part
+    long long ld_exact;
+    float* z_label;                // [rows] the GEMM's on entry
+    float* m1;
+    float* l1;
+    int rows;
+};
+template <class TI>
+__global__ void __launch_bounds__(THREADS) merge_kernel(const MergeParams<TI> p) {
+    const int r = blockIdx.x * WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (r >= p.rows) return;
+    float m = -INFINITY;
+    int id = 0;
+    for (int s = lane; s < p.S; s += 32) {
+        const float x = p.part_m[s * p.part_stride + r];
+        if (x > m) { m = x; id = p.part_id ? p.part_id[s * p.part_stride + r] : 0; }
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        const float om = __shfl_xor_sync(0xffffffffu, m, off);
+        const int oid = __shfl_xor_sync(0xffffffffu, id, off);
+        if (om > m || (om == m && oid < id)) { m = om; id = oid; }
+    }
+    float l = 0.f;
+    for (int s = lane; s < p.S; s += 32) l = fmaf(expf(p.part_m[s * p.part_stride + r] - m), p.part_l[s * p.part_stride + r], l);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+    if (p.valid[r]) {
+        const float zy = p.z_exact[r * p.ld_exact];
+        if (p.part_id) {
+            const bool is_label = p.labels[r] == id;
+            const float z = is_label ? zy : static_cast<float>(lp::warp_dot(p.H + r * p.ldH, p.W + id * p.ldW, p.d, lane));
+            if (fabsf(z - m) < 1.f) l += expm1f(z - m);
+            if (!is_label && fabsf(zy - p.z_label[r]) < 1.f) l += expf(p.z_label[r] - m) * expm1f(zy - p.z_label[r]);
+        }
+        __syncwarp();
+        if (lane == 0) p.z_label[r] = zy;
+    }
+    if (lane == 0) { p.m1[r] = m; p.l1[r] = l; }
 }
 
 __device__ __forceinline__ float block_sum(float x, float* red) {
