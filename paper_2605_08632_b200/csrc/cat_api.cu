@@ -19,6 +19,7 @@
 #include "logprob.cuh"
 #include "rowops.cuh"
 #include "simt.cuh"
+#include "skinny.cuh"
 #include "tc_gemm.cuh"
 #include "topk_kd.cuh"
 

@@ -12,6 +12,7 @@ struct LpPlan {
     long long ldz;         // row pitch of the logits slab
     long long ld_g;        // row pitch of the group maxima
     int group;             // columns per maximum (lp::GroupOf)
+    bool skinny;           // few rows: the kernel of skinny.cuh
     int n_slabs;
     int S;                 // vocabulary splits of a full slab (the most any slab uses)
     size_t off_m, off_l, off_u, off_id, off_g, off_z, total;
@@ -28,6 +29,65 @@ int head_splits(const cat_shape* s, long long rows) {
     return s->in_dtype == CAT_BF16 ? fwd_splits(rows, s->V) : simt_splits(rows, s->V);
 }
 
+// Up to 128 rows go to the kernel of skinny.cuh.  Measured on 1024 x 151936: XXX
+bool use_skinny(const cat_shape* s) { return s->in_dtype == CAT_BF16 && s->T <= skinny::MAX_ROWS; }
+
+// Vocabulary entries per tile of that kernel: the height whose tiles, dealt to the SMs, leave the busiest the least to read.
+int skinny_tile_rows(long long V) {
+    int best = 128;
+    long long most = cdiv(cdiv(V, 128), kPlanSMs) * 128;
+    for (int r = 96; r >= 64; r -= 32) {
+        const long long x = cdiv(cdiv(V, r), kPlanSMs) * r;
+        if (x < most) { most = x; best = r; }
+    }
+    return best;
+}
+
+template <int TPW, int HALVES>
+int launch_skinny_as(const CUtensorMap& tmW, const CUtensorMap& tmH, const skinny::Params& p, int* status, int grid, cudaStream_t st) {
+    auto kern = skinny::logits_kernel<TPW, HALVES>;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, skinny::SMEM_BYTES) != cudaSuccess) {
+        cudaGetLastError();
+        return CAT_ERR_CUDA;
+    }
+    kern<<<static_cast<unsigned>(grid), 64 + 128 * HALVES, skinny::SMEM_BYTES, st>>>(tmW, tmH, p, status);
+    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+}
+
+// Logits of all T <= 128 rows: part_m/l/u [*n_parts][T], group maxima and slab.
+int launch_skinny(const cat_shape* s, const LpPlan& plan, const void* H, const void* W, bool top, uint8_t* ws, int sm_count, int* n_parts,
+                  cudaStream_t st) {
+    skinny::Params p;
+    memset(&p, 0, sizeof(p));
+    p.part_m = reinterpret_cast<float*>(ws + plan.off_m);
+    p.part_l = reinterpret_cast<float*>(ws + plan.off_l);
+    p.part_u = reinterpret_cast<float*>(ws + plan.off_u);
+    p.part_id = reinterpret_cast<int*>(ws + plan.off_id);
+    if (top) {
+        p.gmax = reinterpret_cast<float*>(ws + plan.off_g);
+        p.zs = reinterpret_cast<__half*>(ws + plan.off_z);
+    }
+    p.part_stride = plan.Ts; p.ld_g = plan.ld_g; p.ldz = plan.ldz;
+    p.T = static_cast<int>(s->T); p.V = static_cast<int>(s->V);
+    p.n = static_cast<int>(cdiv(s->T, 16) * 16);
+    p.tile_rows = skinny_tile_rows(s->V);
+    p.n_tiles = static_cast<int>(cdiv(s->V, p.tile_rows));
+    p.num_kb = static_cast<int>(cdiv(s->d, tc::BK));
+    p.stages = (skinny::SMEM_BYTES - 1024 - 8192) / ((p.tile_rows + p.n) * tc::BK * 2);
+    if (p.stages > skinny::MAX_STAGES) p.stages = skinny::MAX_STAGES;
+    p.wait_ns = tc::WAIT_LIMIT_NS;
+    CUtensorMap tmW, tmH;
+    if (tmap_k_major(&tmW, W, s->V, s->d, s->ldW, p.tile_rows) != CAT_OK) return CAT_ERR_CUDA;
+    if (tmap_k_major(&tmH, H, s->T, s->d, s->ldH, p.n) != CAT_OK) return CAT_ERR_CUDA;
+    int grid = sm_count < kPlanSMs ? sm_count : kPlanSMs;
+    if (p.n_tiles < grid) grid = p.n_tiles;
+    *n_parts = grid;
+    int* status = reinterpret_cast<int*>(ws);
+    if (s->T <= 32) return launch_skinny_as<32, 1>(tmW, tmH, p, status, grid, st);
+    if (s->T <= 64) return launch_skinny_as<32, 2>(tmW, tmH, p, status, grid, st);
+    return launch_skinny_as<64, 2>(tmW, tmH, p, status, grid, st);
+}
+
 LpPlan plan_lp(const cat_shape* s, int top_k) {
     LpPlan p;
     const bool bf16 = s->in_dtype == CAT_BF16;
@@ -42,10 +102,13 @@ LpPlan plan_lp(const cat_shape* s, int top_k) {
         if (cap < tile) cap = tile;
         if (cap < s->T) p.Ts = cdiv(cdiv(s->T, cdiv(s->T, cap)), tile) * tile;      // slabs of even height
     }
+    p.skinny = use_skinny(s);
+    if (p.skinny) p.Ts = s->T;
     p.n_slabs = static_cast<int>(cdiv(s->T, p.Ts));
     p.S = head_splits(s, p.Ts);
     const long long rest = s->T - (p.n_slabs - 1) * p.Ts;
     if (head_splits(s, rest) > p.S) p.S = head_splits(s, rest);
+    if (p.skinny) p.S = kPlanSMs;                // one part per CTA
     size_t off = kHeaderBytes;
     p.off_m = off; off = align256(off + sizeof(float) * p.S * p.Ts);
     p.off_l = off; off = align256(off + sizeof(float) * p.S * p.Ts);
@@ -100,6 +163,13 @@ int lp_slab(const cat_shape* s, const LpPlan& plan, const CUtensorMap& tmW, cons
     float* part_u = reinterpret_cast<float*>(ws + plan.off_u);
     if (s->in_dtype == CAT_BF16) {
         const __nv_bfloat16* Hs = static_cast<const __nv_bfloat16*>(H) + r0 * s->ldH;
+        if (plan.skinny) {
+            int n_parts = 0;
+            const int rc = launch_skinny(s, plan, H, W, TOP, ws, sm_count, &n_parts, st);
+            if (rc != CAT_OK) return rc;
+            return launch_lp_rows<__nv_bfloat16, __half, TOP>(s, plan, Hs, static_cast<const __nv_bfloat16*>(W), r0, rws, n_parts, ws,
+                                                              labels, valid, top_k, logp, lse, entropy, top_ids, top_logp, st);
+        }
         CUtensorMap tmH, tmZ;
         if (tmap_a(&tmH, Hs, rws, s->d, s->ldH) != CAT_OK) return CAT_ERR_CUDA;
         if (TOP && tmap_out(&tmZ, ws + plan.off_z, rws, s->V, plan.ldz) != CAT_OK) return CAT_ERR_CUDA;

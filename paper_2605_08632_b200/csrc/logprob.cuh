@@ -30,6 +30,44 @@ __device__ __forceinline__ int first_at(const float (&f)[32], float x) {
     return at;
 }
 
+__device__ __forceinline__ float max_of(const float (&f)[32]) {
+    float x = ptx::max3_f32(f[0], f[1], f[2]);
+#pragma unroll
+    for (int i = 3; i + 1 < 32; i += 2) x = ptx::max3_f32(x, f[i], f[i + 1]);
+    return fmaxf(x, f[31]);
+}
+
+// l = sum exp(z - m) and u = sum exp2(x) x, x = (z - m) log2 e, with m the largest logit so far.
+struct RunningSums {
+    float m, l, u;
+    __device__ __forceinline__ void clear() { m = LP_LOW; l = 0.f; u = 0.f; }
+    // 32 logits whose largest is cmax
+    __device__ __forceinline__ void add(const float (&f)[32], float cmax) {
+        const float m_new = fmaxf(m, cmax);
+        const float mb = m_new * LOG2E;
+        const uint64_t l2e2 = ptx::pack_f32x2(LOG2E, LOG2E), nmb2 = ptx::pack_f32x2(-mb, -mb);
+        uint64_t sum2 = ptx::pack_f32x2(0.f, 0.f), u2 = sum2;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint64_t x2 = ptx::fma_f32x2(ptx::pack_f32x2(f[2 * i], f[2 * i + 1]), l2e2, nmb2);
+            float x0, x1;
+            ptx::unpack_f32x2(x2, x0, x1);
+            const uint64_t e2 = ptx::pack_f32x2(ptx::ex2_approx(x0), ptx::ex2_approx(x1));
+            sum2 = ptx::add_f32x2(sum2, e2);
+            u2 = ptx::fma_f32x2(e2, x2, u2);
+        }
+        float s0, s1, u0, u1;
+        ptx::unpack_f32x2(sum2, s0, s1);
+        ptx::unpack_f32x2(u2, u0, u1);
+        // the sums so far, moved to the new maximum: u(m') = e^(m - m') (u(m) + (m - m') l(m))
+        const float dm = (m - m_new) * LOG2E;
+        const float sc = ptx::ex2_approx(dm);
+        u = fmaf(sc, fmaf(dm, l, u), u0 + u1);
+        l = fmaf(l, sc, s0 + s1);
+        m = m_new;
+    }
+};
+
 // Softmax statistics with entropy, and the row's largest logit's column.  TOP: also the slab's logits as fp16 distances from the
 // maximum of their 32-column group, and those maxima in fp32.
 template <bool TOP>
@@ -46,15 +84,13 @@ struct EpiLp {
         int V;
     };
     struct State {
-        float m_run, l_run, u_run;
+        RunningSums r;
         int id;
         int row;
     };
     __device__ static __forceinline__ void begin_item(const Params&, State& s, int m_tile, int row_in_tile) {
         s.row = m_tile * BM + row_in_tile;
-        s.m_run = LP_LOW;
-        s.l_run = 0.f;
-        s.u_run = 0.f;
+        s.r.clear();
         s.id = 0;
     }
     __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage& o) {
@@ -79,11 +115,8 @@ struct EpiLp {
                 for (int i = 0; i < 32; ++i)
                     if (i >= live) f[i] = LP_LOW;
             }
-            float cmax = ptx::max3_f32(f[0], f[1], f[2]);
-#pragma unroll
-            for (int i = 3; i + 1 < 32; i += 2) cmax = ptx::max3_f32(cmax, f[i], f[i + 1]);
-            cmax = fmaxf(cmax, f[31]);
-            if (cmax > s.m_run) s.id = col0 + c * 32 + first_at(f, cmax);
+            const float cmax = max_of(f);
+            if (cmax > s.r.m) s.id = col0 + c * 32 + first_at(f, cmax);
             if (TOP) {
                 // the slab keeps z - (maximum of the group): the group's largest logit stays exact, its neighbours near it
 #pragma unroll
@@ -97,28 +130,7 @@ struct EpiLp {
                           ptx::pack_f16x2_sat(f[q * 8 + 6] - cmax, f[q * 8 + 7] - cmax));
                 if ((c & 1) != 0 || (c + 1) * 32 >= ncols) o.flush(col0 + (c >> 1) * 64);
             }
-            const float m_new = fmaxf(s.m_run, cmax);
-            const float mb = m_new * LOG2E;
-            const uint64_t l2e2 = ptx::pack_f32x2(LOG2E, LOG2E), nmb2 = ptx::pack_f32x2(-mb, -mb);
-            uint64_t sum2 = ptx::pack_f32x2(0.f, 0.f), u2 = sum2;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint64_t x2 = ptx::fma_f32x2(ptx::pack_f32x2(f[2 * i], f[2 * i + 1]), l2e2, nmb2);
-                float x0, x1;
-                ptx::unpack_f32x2(x2, x0, x1);
-                const uint64_t e2 = ptx::pack_f32x2(ptx::ex2_approx(x0), ptx::ex2_approx(x1));
-                sum2 = ptx::add_f32x2(sum2, e2);
-                u2 = ptx::fma_f32x2(e2, x2, u2);
-            }
-            float s0, s1, u0, u1;
-            ptx::unpack_f32x2(sum2, s0, s1);
-            ptx::unpack_f32x2(u2, u0, u1);
-            // move the running sums to the new maximum: u(m') = e^(m - m') (u(m) + (m - m') l(m))
-            const float dm = (s.m_run - m_new) * LOG2E;
-            const float sc = ptx::ex2_approx(dm);
-            s.u_run = fmaf(sc, fmaf(dm, s.l_run, s.u_run), u0 + u1);
-            s.l_run = fmaf(s.l_run, sc, s0 + s1);
-            s.m_run = m_new;
+            s.r.add(f, cmax);
         }
         if (TOP && s.row < p.T) {
             float4* out = reinterpret_cast<float4*>(p.gmax + static_cast<size_t>(s.row) * p.ld_g + n_tile * (BN / LP_GROUP));
@@ -130,9 +142,9 @@ struct EpiLp {
     __device__ static __forceinline__ void end_item(const Params& p, const State& s, int group) {
         if (s.row < p.T) {
             const size_t at = static_cast<size_t>(group) * p.part_stride + s.row;
-            p.part_m[at] = s.m_run;
-            p.part_l[at] = s.l_run;
-            p.part_u[at] = s.u_run;
+            p.part_m[at] = s.r.m;
+            p.part_l[at] = s.r.l;
+            p.part_u[at] = s.r.u;
             p.part_id[at] = s.id;
         }
     }
@@ -277,6 +289,11 @@ __device__ __forceinline__ float stored(const float* z, float, long long v, floa
     err = 0.f;
     return z[v];
 }
+template <class TI>
+__device__ __forceinline__ void prefetch_row(const TI* row, int d, int lane) {
+    constexpr int LINE = 128 / sizeof(TI);
+    for (int i = lane * LINE; i < d; i += 32 * LINE) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + i));
+}
 template <class TZ>
 struct GroupOf { static constexpr int value = tc::LP_GROUP; };
 template <>
@@ -291,7 +308,7 @@ struct RowParams {
     const float* part_m;           // [S][part_stride]
     const float* part_l;
     const float* part_u;
-    const int* part_id;
+    const int* part_id;            // nullptr: the largest logit is found through gmax and zs
     long long part_stride;
     int S;
     const TI* H;                   // rows of this slab
@@ -317,8 +334,8 @@ struct RowParams {
 struct Shared {
     float red[2][WARPS];
     int count[2][WARPS];
-    int n_cand;
-    float lse;
+    int n_cand, n_near;
+    float m, l, u, lse;
     int id_max;
     double z_max, z_label;
     double z[CAP];                 // exact logits, where `err` says so
@@ -327,6 +344,9 @@ struct Shared {
     int id[CAP];
     double z_keep[MAX_TOP];
     int id_keep[MAX_TOP];
+    int near[CAP];                 // groups that may hold candidates; then the candidates in doubt
+    float near_max[CAP];           // those groups' maxima
+    int above[CAP], close[CAP];    // per candidate: others certainly above it, others within the errors
 };
 constexpr float EXACT = -1.f, OUT = -2.f;
 
@@ -342,42 +362,52 @@ __device__ __forceinline__ float block_max(float x, float* red) {
     return x;
 }
 
-// A number that at least k of n values reach, and few more than k: bisection between the least and the largest of them.  The values
-// are kept in registers when they fit.  big = largest |value|.
+// A number that at least k of n values reach, and few more than k: bisection between the least and the largest of them.  The first
+// KEPT * THREADS values come in registers (v, value j * THREADS + threadIdx.x, -infinity past n), the others by `value`.
+// big = largest |value|.  Up to k = 128 the bisection runs over the threads' own largest values only: any k of them are k of the
+// values, the bound is a little lower (k = 64 of 4008 values: 72 reach it instead of 64), and a step is one compare and one
+// barrier that counts.
 constexpr int KEPT = 20;
 template <class F>
-__device__ __forceinline__ float near_kth(F value, int n, int k, Shared& sh, float& big) {
-    float v[KEPT];
-    const bool fits = n <= KEPT * THREADS;
-    float hi = -INFINITY, nlo = -INFINITY;
-    if (fits) {
+__device__ __forceinline__ float near_kth(const float (&v)[KEPT], F value, int n, int k, Shared& sh, float& big) {
+    float mine = -INFINITY, nlo = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < KEPT; ++j) {
-            const int i = j * THREADS + threadIdx.x;
-            v[j] = i < n ? value(i) : -INFINITY;
-            if (i < n) { hi = fmaxf(hi, v[j]); nlo = fmaxf(nlo, -v[j]); }
-        }
-    } else {
-        for (int i = threadIdx.x; i < n; i += THREADS) {
-            const float x = value(i);
-            hi = fmaxf(hi, x);
-            nlo = fmaxf(nlo, -x);
-        }
+    for (int j = 0; j < KEPT; ++j) {
+        mine = fmaxf(mine, v[j]);
+        if (j * THREADS + threadIdx.x < n) nlo = fmaxf(nlo, -v[j]);
     }
-    hi = block_max(hi, sh.red[0]);
+    for (int i = KEPT * THREADS + threadIdx.x; i < n; i += THREADS) {
+        const float x = value(i);
+        mine = fmaxf(mine, x);
+        nlo = fmaxf(nlo, -x);
+    }
+    float hi = block_max(mine, sh.red[0]);
     float lo = -block_max(nlo, sh.red[1]);
     big = fmaxf(fabsf(hi), fabsf(lo));
     if (n <= k) return lo;
+    const int enough = k + k / 4 + 2;
+    if (k <= THREADS / 2 && n >= THREADS) {
+        lo = -block_max(-mine, sh.red[0]);          // every thread's value reaches it
+        for (int it = 0; it < 24; ++it) {
+            const float mid = 0.5f * lo + 0.5f * hi;
+            if (!(mid > lo && mid < hi)) break;
+            const int c = __syncthreads_count(mine >= mid);
+            if (c >= k) {
+                lo = mid;
+                if (c <= enough) break;
+            } else {
+                hi = mid;
+            }
+        }
+        return lo;
+    }
     for (int it = 0; it < 24; ++it) {
         const float mid = 0.5f * lo + 0.5f * hi;
         if (!(mid > lo && mid < hi)) break;
         int c = 0;
-        if (fits) {
 #pragma unroll
-            for (int j = 0; j < KEPT; ++j) c += v[j] >= mid ? 1 : 0;
-        } else {
-            for (int i = threadIdx.x; i < n; i += THREADS) c += value(i) >= mid ? 1 : 0;
-        }
+        for (int j = 0; j < KEPT; ++j) c += v[j] >= mid ? 1 : 0;
+        for (int i = KEPT * THREADS + threadIdx.x; i < n; i += THREADS) c += value(i) >= mid ? 1 : 0;
         c = __reduce_add_sync(0xffffffffu, c);
         if ((threadIdx.x & 31) == 0) sh.count[it & 1][threadIdx.x >> 5] = c;
         __syncthreads();
@@ -386,12 +416,50 @@ __device__ __forceinline__ float near_kth(F value, int n, int k, Shared& sh, flo
         for (int i = 0; i < WARPS; ++i) c += sh.count[it & 1][i];
         if (c >= k) {
             lo = mid;
-            if (c <= k + k / 4 + 2) break;
+            if (c <= enough) break;
         } else {
             hi = mid;
         }
     }
     return lo;
+}
+
+// lse and entropy from the merged sums and the exact largest logit, and the label's log probability; one thread.
+template <class TI, class TZ>
+__device__ __forceinline__ void finish_row(const RowParams<TI, TZ>& p, long long r, Shared& sh) {
+    // the largest logit entered as exp(0) = 1 and 0; it is exp(x) and x exp(x) with its exact distance x from m
+    float l = sh.l, u = sh.u;
+    const float x = static_cast<float>(sh.z_max - static_cast<double>(sh.m));
+    if (fabsf(x) < 1.f) {
+        l += expm1f(x);
+        u = fmaf(x * tc::LOG2E, expf(x), u);
+    }
+    const float logl = logf(l);
+    const float lse = sh.m + logl;
+    sh.lse = lse;
+    p.lse[r] = lse;
+    const float ent = logl - 0.6931471805599453f * u / l;
+    p.entropy[r] = ent < 0.f ? 0.f : ent + (lse - lse);      // NaN for a row that is not finite
+    if (p.logp != nullptr) {
+        const long long y = p.labels[r];
+        p.logp[r] = (y >= 0 && y < p.V) ? static_cast<float>((y == sh.id_max ? sh.z_max : sh.z_label) - static_cast<double>(lse)) : 0.f;
+    }
+}
+
+// The two logits of a row that are always taken exactly, by one warp each: which = 0 the largest, 1 the label's.
+template <class TI, class TZ>
+__device__ __forceinline__ void exact_one(const RowParams<TI, TZ>& p, const TI* h, long long r, Shared& sh, int which) {
+    const int lane = threadIdx.x & 31;
+    if (which == 0) {
+        const double z = warp_dot(h, p.W + static_cast<long long>(sh.id_max) * p.ldW, p.d, lane);
+        if (lane == 0) sh.z_max = z;
+    } else if (p.logp != nullptr) {
+        const long long y = p.labels[r];
+        if (y >= 0 && y < p.V && y != sh.id_max) {
+            const double z = warp_dot(h, p.W + y * p.ldW, p.d, lane);
+            if (lane == 0) sh.z_label = z;
+        }
+    }
 }
 
 // Exact logits of candidates [from, n) and the order of all n of them; the first k go to the front of the keep list.
@@ -417,47 +485,70 @@ __device__ __forceinline__ int settle(const RowParams<TI, TZ>& p, const TI* h, S
 // The same from the approximate logits, with exact ones only for candidates that their errors leave in doubt against another, and for
 // those that the slab's fp16 has rounded (not the largest of their group): their values are returned.
 template <class TI, class TZ>
-__device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI* h, Shared& sh, int n, float eps) {
+__device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI* h, long long r, Shared& sh, int n, float eps) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    unsigned doubt = 0;                       // bit i: candidate threadIdx.x + i * THREADS needs its exact logit
-    unsigned out = 0;
     static_assert(CAP / THREADS <= 32, "one bit per candidate of a thread");
-    for (int i = 0, c = threadIdx.x; c < n; ++i, c += THREADS) {
+    unsigned doubt = 0, out = 0;              // bit i: candidate threadIdx.x + i * THREADS needs its exact logit, is out
+    // Several threads share a candidate while there are threads to share: each looks at its part of the others.
+    const int parts = n <= THREADS / 2 ? THREADS / (n > 0 ? n : 1) : 1;
+    const int part = threadIdx.x / (n > 0 ? n : 1), per = (n + parts - 1) / parts;
+    for (int c = threadIdx.x; c < n; c += THREADS) { sh.above[c] = 0; sh.close[c] = 0; }
+    if (threadIdx.x == 0) sh.n_near = 0;
+    __syncthreads();
+    for (int c = parts > 1 ? threadIdx.x - part * n : threadIdx.x; c < n && (parts == 1 || part < parts); c += parts > 1 ? CAP : THREADS) {
         const float z = sh.approx[c], e = sh.err[c];
-        int above = 0;
-        bool near = false;
-        for (int j = 0; j < n; ++j) {
+        const int j0 = parts > 1 ? part * per : 0, j1 = parts > 1 ? min(n, j0 + per) : n;
+        int above = 0, near = 0;
+#pragma unroll 8
+        for (int j = j0; j < j1; ++j) {
             const float gap = sh.approx[j] - z, both = sh.err[j] + e;
             above += gap > both ? 1 : 0;
-            near |= j != c && fabsf(gap) <= both;
+            near += fabsf(gap) <= both ? 1 : 0;       // itself among them
         }
-        if (above >= p.k) out |= 1u << i;
-        else if (near || e > eps + 4.0e-8f) doubt |= 1u << i;
+        if (above) atomicAdd(&sh.above[c], above);
+        if (near) atomicAdd(&sh.close[c], near);
     }
     __syncthreads();
     for (int i = 0, c = threadIdx.x; c < n; ++i, c += THREADS) {
-        if (out >> i & 1u) sh.err[c] = OUT;
-        else if (doubt >> i & 1u) sh.err[c] = EXACT;
+        if (sh.above[c] >= p.k) out |= 1u << i;
+        else if (sh.close[c] > 1 || sh.err[c] > eps + 4.0e-8f) doubt |= 1u << i;
+        sh.above[c] = 0;
+        if (out >> i & 1u) { sh.err[c] = OUT; sh.approx[c] = -INFINITY; }
+        else if (doubt >> i & 1u) { sh.err[c] = EXACT; sh.near[atomicAdd(&sh.n_near, 1)] = c; }
     }
     __syncthreads();
-    for (int c = warp; c < n; c += WARPS) {
-        if (sh.err[c] != EXACT) continue;
-        const double z = warp_dot(h, p.W + static_cast<long long>(sh.id[c]) * p.ldW, p.d, lane);
-        if (lane == 0) sh.z[c] = z;
+    const int n_doubt = sh.n_near;
+    for (int i = warp; i < n_doubt + 2; i += WARPS) {
+        if (i < 2) {
+            exact_one(p, h, r, sh, i);
+        } else {
+            const int c = sh.near[i - 2];
+            const double z = warp_dot(h, p.W + static_cast<long long>(sh.id[c]) * p.ldW, p.d, lane);
+            if (lane == 0) sh.z[c] = z;
+        }
+    }
+    for (int c = parts > 1 ? threadIdx.x - part * n : threadIdx.x; c < n && (parts == 1 || part < parts); c += parts > 1 ? CAP : THREADS) {
+        const float zc = sh.approx[c];
+        const int j0 = parts > 1 ? part * per : 0, j1 = parts > 1 ? min(n, j0 + per) : n;
+        int rank = 0;
+#pragma unroll 8
+        for (int j = j0; j < j1; ++j) rank += sh.approx[j] > zc ? 1 : 0;
+        if (rank) atomicAdd(&sh.above[c], rank);
     }
     __syncthreads();
+    if (threadIdx.x == THREADS - 1) finish_row(p, r, sh);
     for (int c = threadIdx.x; c < n; c += THREADS) {
-        const float ec = sh.err[c];
+        const float ec = sh.err[c], zc = sh.approx[c];
         if (ec == OUT) continue;
         const int id = sh.id[c];
-        const double z = ec == EXACT ? sh.z[c] : static_cast<double>(sh.approx[c]);
-        int rank = 0;
-        for (int j = 0; j < n; ++j) {
-            const float ej = sh.err[j];
-            if (ej == OUT || j == c) continue;
-            // two in doubt against each other are both exact
-            if (ec == EXACT && ej == EXACT) rank += (sh.z[j] > z || (sh.z[j] == z && sh.id[j] < id)) ? 1 : 0;
-            else rank += sh.approx[j] > sh.approx[c] ? 1 : 0;
+        double z = static_cast<double>(zc);
+        int rank = sh.above[c];
+        if (ec == EXACT) {      // against others in doubt the exact logits count
+            z = sh.z[c];
+            for (int i = 0; i < n_doubt; ++i) {
+                const int j = sh.near[i];
+                rank += (sh.z[j] > z || (sh.z[j] == z && sh.id[j] < id) ? 1 : 0) - (sh.approx[j] > zc ? 1 : 0);
+            }
         }
         if (rank < p.k) { sh.z_keep[rank] = id == sh.id_max ? sh.z_max : z; sh.id_keep[rank] = id; }
     }
@@ -493,110 +584,143 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
         return;
     }
     const TI* h = p.H + r * p.ldH;
-    if (warp == 0) {
-        // merge the split partials; sums over splits in a fixed order
-        float m = tc::LP_LOW;
-        int id = 0;
-        for (int s = lane; s < p.S; s += 32) {
-            const float x = p.part_m[s * p.part_stride + r];
-            if (x > m) { m = x; id = p.part_id[s * p.part_stride + r]; }
-        }
+    constexpr int group = GroupOf<TZ>::value;
+    const float* g = p.gmax + r * p.ld_g;
+    const TZ* z = p.zs + r * p.ldz;
+    // With few groups per alternative their maxima bound little (or there are not k of them): go by the logits themselves.
+    const bool by_group = TOP && p.n_g >= 4 * p.k;
+    const int n_values = by_group ? p.n_g : p.V;
+    auto value = [&](int i) {
+        float e;
+        return by_group ? g[i] : stored(z, g[i / group], i, e);
+    };
+    float v[KEPT];
+    if (TOP) {      // asked for first: they are under way while warp 0 merges
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) {
-            const float om = __shfl_xor_sync(0xffffffffu, m, off);
-            const int oid = __shfl_xor_sync(0xffffffffu, id, off);
-            if (om > m || (om == m && oid < id)) { m = om; id = oid; }
+        for (int j = 0; j < KEPT; ++j) {
+            const int i = j * THREADS + threadIdx.x;
+            v[j] = i < n_values ? value(i) : -INFINITY;
         }
-        float l = 0.f, u = 0.f;
-        for (int s = lane; s < p.S; s += 32) {
-            const size_t at = s * p.part_stride + r;
-            const float dm = (p.part_m[at] - m) * tc::LOG2E;
-            const float e = exp2f(dm), ls = p.part_l[at];
-            l = fmaf(e, ls, l);
-            u = fmaf(e, fmaf(dm, ls, p.part_u[at]), u);
+    }
+    if (warp == 1) {      // the rows of W whose exact logits are wanted at the end
+        prefetch_row(h, p.d, lane);
+        const long long y = p.logp != nullptr ? p.labels[r] : -1;
+        if (y >= 0 && y < p.V) prefetch_row(p.W + y * p.ldW, p.d, lane);
+    }
+    if (warp == 0) {
+        // merge the split partials; sums over splits in a fixed order.  The loads of up to 160 splits are under way together.
+        constexpr int BATCH = 5;
+        float m = tc::LP_LOW, l = 0.f, u = 0.f;
+        int id = 0;
+        for (int s0 = 0; s0 < p.S; s0 += 32 * BATCH) {
+            float ms[BATCH], ls[BATCH], us[BATCH];
+            int is[BATCH];
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const int s = s0 + 32 * j + lane;
+                const size_t at = static_cast<size_t>(s < p.S ? s : 0) * p.part_stride + r;
+                ms[j] = p.part_m[at]; ls[j] = p.part_l[at]; us[j] = p.part_u[at]; is[j] = p.part_id[at];
+                if (s >= p.S) { ms[j] = tc::LP_LOW; ls[j] = us[j] = 0.f; }
+            }
+            float m_new = m;
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j)
+                if (ms[j] > m_new || (ms[j] == m_new && is[j] < id)) { m_new = ms[j]; id = is[j]; }
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) {
+                const float om = __shfl_xor_sync(0xffffffffu, m_new, off);
+                const int oid = __shfl_xor_sync(0xffffffffu, id, off);
+                if (om > m_new || (om == m_new && oid < id)) { m_new = om; id = oid; }
+            }
+            const float dm0 = (m - m_new) * tc::LOG2E, e0 = exp2f(dm0);
+            u = e0 * fmaf(dm0, l, u);
+            l *= e0;
+            m = m_new;
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const float dm = (ms[j] - m) * tc::LOG2E, e = exp2f(dm);
+                l = fmaf(e, ls[j], l);
+                u = fmaf(e, fmaf(dm, ls[j], us[j]), u);
+            }
         }
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) {
             l += __shfl_xor_sync(0xffffffffu, l, off);
             u += __shfl_xor_sync(0xffffffffu, u, off);
         }
-        const double z_max = warp_dot(h, p.W + static_cast<long long>(id) * p.ldW, p.d, lane);
+        prefetch_row(p.W + static_cast<long long>(id) * p.ldW, p.d, lane);
         if (lane == 0) {
-            // the largest logit entered as exp(0) = 1 and 0; it is exp(x) and x exp(x) with its exact distance x from m
-            const float x = static_cast<float>(z_max - static_cast<double>(m));
-            if (fabsf(x) < 1.f) {
-                l += expm1f(x);
-                u = fmaf(x * tc::LOG2E, expf(x), u);
-            }
-            const float logl = logf(l);
-            const float lse = m + logl;
-            sh.lse = lse;
+            sh.m = m; sh.l = l; sh.u = u;
             sh.id_max = id;
-            sh.z_max = z_max;
-            p.lse[r] = lse;
-            const float ent = logl - 0.6931471805599453f * u / l;
-            p.entropy[r] = ent < 0.f ? 0.f : ent + (lse - lse);      // NaN for a row that is not finite
+            sh.n_cand = sh.n_near = 0;
         }
-    } else if (warp == 1 && p.logp != nullptr) {
-        const long long y = p.labels[r];
-        double zy = 0.0;
-        if (y >= 0 && y < p.V) zy = warp_dot(h, p.W + y * p.ldW, p.d, lane);
-        if (lane == 0) sh.z_label = zy;
     }
     __syncthreads();
-    const float lse = sh.lse;
-    if (p.logp != nullptr && threadIdx.x == 0) {
-        const long long y = p.labels[r];
-        p.logp[r] = (y >= 0 && y < p.V) ? static_cast<float>(sh.z_label - static_cast<double>(lse)) : 0.f;
-    }
-    if (!TOP) return;
-    long long* ids_out = p.top_ids + r * p.k;
-    float* lp_out = p.top_logp + r * p.k;
-    if (!isfinite(lse)) {
-        for (int i = threadIdx.x; i < p.k; i += THREADS) { ids_out[i] = -1; lp_out[i] = NAN; }
+    if (!TOP) {
+        if (warp < 2) exact_one(p, h, r, sh, warp);
+        __syncthreads();
+        if (threadIdx.x == 0) finish_row(p, r, sh);
         return;
     }
-    const float* g = p.gmax + r * p.ld_g;
-    const TZ* z = p.zs + r * p.ldz;
-    constexpr int group = GroupOf<TZ>::value;
-    // With few groups per alternative their maxima bound little (or there are not k of them): go by the logits themselves.
+    long long* ids_out = p.top_ids + r * p.k;
+    float* lp_out = p.top_logp + r * p.k;
+    if (!isfinite(sh.m + logf(sh.l))) {
+        for (int i = threadIdx.x; i < p.k; i += THREADS) { ids_out[i] = -1; lp_out[i] = NAN; }
+        if (warp < 2) exact_one(p, h, r, sh, warp);
+        __syncthreads();
+        if (threadIdx.x == 0) finish_row(p, r, sh);
+        return;
+    }
     float big;
-    const float t = p.n_g >= 4 * p.k ? near_kth([&](int i) { return g[i]; }, p.n_g, p.k, sh, big)
-                                     : near_kth([&](int i) { float e; return stored(z, g[i / group], i, e); }, p.V, p.k, sh, big);
+    const float t = near_kth(v, value, n_values, p.k, sh, big);
     const float eps = big * gemm_error(z, p.d);
     // a bound taken over stored logits may lie their rounding (2^-11 of the row's span) too high
-    const float thr = t - 2.f * eps - (p.n_g >= 4 * p.k ? 0.f : 1.0e-3f * big);
-    if (threadIdx.x == 0) sh.n_cand = 0;
-    __syncthreads();
-    auto look = [&](int gi) {      // one warp appends the candidates of one group
-        const float gm = g[gi];
-        for (int o = 0; o < group; o += 32) {
-            const long long col = static_cast<long long>(gi) * group + o + lane;
-            float e, x;
-            x = stored(z, gm, col < p.V ? col : 0, e);
-            const bool in = col < p.V && x + e >= thr;
-            const unsigned hit = __ballot_sync(0xffffffffu, in);
-            if (hit == 0) continue;
-            int at = 0;
-            if (lane == 0) at = atomicAdd(&sh.n_cand, __popc(hit));
-            at = __shfl_sync(0xffffffffu, at, 0) + __popc(hit & ((1u << lane) - 1u));
-            if (in && at < CAP) { sh.id[at] = static_cast<int>(col); sh.approx[at] = x; sh.err[at] = eps + e; }
-        }
+    const float thr = t - 2.f * eps - (by_group ? 0.f : 1.0e-3f * big);
+    // the groups that reach the threshold, then their columns that do
+    auto keep_group = [&](int gi, float gm) {
+        const int at = atomicAdd(&sh.n_near, 1);
+        if (at < CAP) { sh.near[at] = gi; sh.near_max[at] = gm; }
     };
-    for (int g0 = warp * 32; g0 < p.n_g; g0 += THREADS) {
-        const int gi = g0 + lane;
-        unsigned todo = __ballot_sync(0xffffffffu, gi < p.n_g && g[gi < p.n_g ? gi : 0] >= thr);
-        while (todo) {
-            const int b = __ffs(todo) - 1;
-            todo &= todo - 1;
-            look(g0 + b);
+    if (by_group) {
+#pragma unroll
+        for (int j = 0; j < KEPT; ++j)
+            if (v[j] >= thr) keep_group(j * THREADS + threadIdx.x, v[j]);      // -infinity past n_g; thr is finite
+    }
+    for (int gi = (by_group ? KEPT * THREADS : 0) + threadIdx.x; gi < p.n_g; gi += THREADS)
+        if (g[gi] >= thr) keep_group(gi, g[gi]);
+    __syncthreads();
+    const int n_near = sh.n_near;
+    auto append = [&](bool in, long long col, float x, float e) {      // whole warps
+        const unsigned hit = __ballot_sync(0xffffffffu, in);
+        if (hit == 0) return;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&sh.n_cand, __popc(hit));
+        at = __shfl_sync(0xffffffffu, at, 0) + __popc(hit & ((1u << lane) - 1u));
+        if (in && at < CAP) { sh.id[at] = static_cast<int>(col); sh.approx[at] = x; sh.err[at] = eps + e; }
+    };
+    if (n_near <= CAP) {
+        const int n_el = n_near * group;
+        constexpr int BATCH = 4;      // loads under way together
+        for (int i0 = 0; i0 < n_el; i0 += BATCH * THREADS) {
+            float x[BATCH], e[BATCH];
+            long long col[BATCH];
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const int i = i0 + j * THREADS + threadIdx.x, at = i < n_el ? i / group : 0;
+                col[j] = static_cast<long long>(sh.near[at]) * group + (i & (group - 1));
+                x[j] = stored(z, sh.near_max[at], col[j] < p.V ? col[j] : 0, e[j]);
+                if (i >= n_el || col[j] >= p.V) x[j] = -INFINITY;
+            }
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) append(x[j] + e[j] >= thr, col[j], x[j], e[j]);
         }
     }
     __syncthreads();
     int kept;
-    if (sh.n_cand <= CAP) {
-        kept = settle_close(p, h, sh, sh.n_cand, eps);
+    if (n_near <= CAP && sh.n_cand <= CAP) {
+        kept = settle_close(p, h, r, sh, sh.n_cand, eps);
     } else {
+        if (warp < 2) exact_one(p, h, r, sh, warp);
         // many logits within the error of the k-th.  A row of zeros has them all equal: ids 0, 1, ...
         bool nz = false;
         for (int i = threadIdx.x; i < p.d; i += THREADS) nz |= static_cast<float>(h[i]) != 0.f;
@@ -612,7 +736,14 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
                 if (threadIdx.x == 0) sh.n_cand = n;
                 __syncthreads();
                 const int gi = g0 + warp;
-                if (gi < p.n_g && g[gi] >= thr) look(gi);
+                if (gi < p.n_g && g[gi] >= thr) {
+                    for (int o = 0; o < group; o += 32) {
+                        const long long col = static_cast<long long>(gi) * group + o + lane;
+                        float e;
+                        const float x = stored(z, g[gi], col < p.V ? col : 0, e);
+                        append(col < p.V && x + e >= thr, col, x, e);
+                    }
+                }
                 __syncthreads();
                 n = sh.n_cand;
                 const bool last = g0 + WARPS >= p.n_g;
@@ -624,7 +755,10 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
                 __syncthreads();
             }
         }
+        if (threadIdx.x == 0) finish_row(p, r, sh);
+        __syncthreads();
     }
+    const float lse = sh.lse;
     for (int i = threadIdx.x; i < p.k; i += THREADS) {
         ids_out[i] = i < kept ? sh.id_keep[i] : -1;
         lp_out[i] = i < kept ? static_cast<float>(sh.z_keep[i] - static_cast<double>(lse)) : -INFINITY;

@@ -60,6 +60,8 @@ BF, F32 = torch.bfloat16, torch.float32
 @pytest.mark.parametrize("T,d,V,k,dtype", [
     (1, 64, 1, 1, BF), (1, 64, 3, 8, BF), (1, 512, 5003, 20, BF), (2, 8, 33, 33, BF), (3, 72, 256, 256, BF), (5, 128, 257, 1, BF),
     (37, 256, 8191, 64, BF), (130, 136, 20011, 5, BF), (257, 256, 12000, 20, BF), (600, 128, 3000, 0, BF),
+    (32, 64, 30000, 20, BF), (33, 200, 20001, 8, BF), (64, 1024, 9473, 64, BF), (65, 64, 14209, 20, BF), (127, 72, 40000, 3, BF),
+    (128, 2048, 19000, 20, BF), (129, 64, 14209, 20, BF), (128, 64, 700, 0, BF), (16, 64, 18945, 0, BF),
     (1, 3, 1, 2, F32), (7, 5, 63, 64, F32), (65, 33, 129, 7, F32), (130, 100, 4097, 20, F32), (70, 64, 2500, 0, F32),
 ])
 def test_forward_matches_oracle(T, d, V, k, dtype):
