@@ -15,6 +15,7 @@
 #include <atomic>
 #include <mutex>
 
+#include "fp32_gemm.cuh"
 #include "kd.cuh"
 #include "logprob.cuh"
 #include "rowops.cuh"
@@ -592,6 +593,52 @@ int launch_dh(const CUtensorMap& tmZ, const CUtensorMap& tmW, long long rows, lo
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
 
+// fp32 products C[M, N] (+)= scale * A B over Kd: parts of the contraction when the output has few 64 x 64 tiles, so that about four
+// CTAs per SM have work; no part shorter than 256.
+int f32_parts(long long M, long long N, long long Kd) {
+    const long long tiles = cdiv(M, f32::TM) * cdiv(N, f32::TN);
+    long long p = (4 * kPlanSMs) / tiles;
+    if (p > Kd / 256) p = Kd / 256;
+    if (p > 32) p = 32;
+    return static_cast<int>(p < 1 ? 1 : p);
+}
+// scratch for the parts of any such product: parts * tiles <= 4 per SM whenever there is more than one part
+constexpr size_t kF32PartBytes = sizeof(float) * 4 * kPlanSMs * f32::TM * f32::TN;
+template <bool A_KC, bool B_KC>
+int launch_f32_out(const f32::Operands& op, const float* scale, float* out, long long ld, bool add, float* part, cudaStream_t st) {
+    const int parts = f32_parts(op.M, op.N, op.Kd);
+    f32::EpiParams ep;
+    memset(&ep, 0, sizeof(ep));
+    const dim3 grid(static_cast<unsigned>(cdiv(op.M, f32::TM)), static_cast<unsigned>(op.n_groups), static_cast<unsigned>(parts));
+    if (parts == 1) {
+        ep.alpha = scale; ep.out = out; ep.ld_out = ld;
+        if (add) { ep.add = out; ep.ld_add = ld; }
+        f32::gemm_kernel<f32::OUT, A_KC, B_KC><<<grid, f32::THREADS, 0, st>>>(op, ep);
+    } else {
+        ep.out = part; ep.ld_out = op.N; ep.part_stride = static_cast<long long>(op.M) * op.N;
+        f32::gemm_kernel<f32::OUT, A_KC, B_KC><<<grid, f32::THREADS, 0, st>>>(op, ep);
+        f32::add_kernel<<<static_cast<unsigned>(cdiv(ep.part_stride, 256)), 256, 0, st>>>(part, parts, ep.part_stride, op.M, op.N, scale,
+                                                                                       add ? out : nullptr, ld, out, ld);
+    }
+    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+}
+// dW [w, d] (+)= scale * dz^T H, dz [rows, w] with pitch ldz
+int launch_f32_dw(const float* dz, long long ldz, const float* H, long long ldH, int w, int d, int rows, const float* scale, float* dW,
+                  long long ldW, bool add, float* part, cudaStream_t st) {
+    f32::Operands op;
+    op.A = dz; op.sAm = 1; op.sAk = ldz; op.B = H; op.sBk = ldH; op.sBn = 1;
+    op.M = w; op.N = d; op.Kd = rows; op.n_groups = static_cast<int>(cdiv(d, f32::TN));
+    return launch_f32_out<false, false>(op, scale, dW, ldW, add, part, st);
+}
+// dH [rows, d] (+)= scale * dz W
+int launch_f32_dh(const float* dz, long long ldz, const float* W, long long ldW, int rows, int d, int w, const float* scale, float* dH,
+                  long long ldH, bool add, float* part, cudaStream_t st) {
+    f32::Operands op;
+    op.A = dz; op.sAm = ldz; op.sAk = 1; op.B = W; op.sBk = ldW; op.sBn = 1;
+    op.M = rows; op.N = d; op.Kd = w; op.n_groups = static_cast<int>(cdiv(d, f32::TN));
+    return launch_f32_out<true, false>(op, scale, dH, ldH, add, part, st);
+}
+
 // Forward + backward over row slabs with the slab's logits kept (cat_loss_fwd_bwd); with `kd` also the
 // distillation term of Eq. 12 (cat_kd_loss_fwd_bwd): per slab a second logits GEMM on the target
 // side, the target confidences of Eq. 9, and a dz that carries both terms.
@@ -988,7 +1035,7 @@ static size_t lp_bwd_bytes(const cat_shape* s) {       // the plain backward's s
     const BwdPlan p = plan_bwd(s);
     const bool bf16 = s->in_dtype == CAT_BF16;
     return align256(p.total) + align256((bf16 ? 2 : 4) * static_cast<size_t>(s->T) * static_cast<size_t>(s->d)) +
-           (bf16 && p.n_slabs == 1 ? dh_part_bytes(s->T, s->d, s->V) : 0);
+           (!bf16 ? kF32PartBytes : p.n_slabs == 1 ? dh_part_bytes(s->T, s->d, s->V) : 0);
 }
 static int bwd_core(const cat_shape* shape, const void* H, const void* W, const int64_t* labels, const uint8_t* valid,
                     const float* lse, const float* weight, const float* grad_loss, void* dH, void* dW, int accumulate_dW,
@@ -1107,6 +1154,23 @@ static int bwd_core(const cat_shape* shape, const void* H, const void* W, const 
             const float* Wf = static_cast<const float*>(W) + v0 * shape->ldW;
             float* dz = reinterpret_cast<float*>(ws + plan.off_dz);
             const int w = static_cast<int>(width);
+            if (lp) {
+                float* part = reinterpret_cast<float*>(ws + align256(plan.total) + align256(sizeof(float) * static_cast<size_t>(T) * static_cast<size_t>(d)));
+                f32::Operands op;
+                f32::EpiParams ep;
+                memset(&ep, 0, sizeof(ep));
+                op.A = Hf; op.sAm = shape->ldH; op.sAk = 1; op.B = Wf; op.sBk = 1; op.sBn = shape->ldW;
+                op.M = T; op.N = w; op.Kd = d; op.n_groups = static_cast<int>(cdiv(w, f32::TN));
+                ep.labels = y; ep.valid = valid; ep.lse = lse; ep.entropy = lp->entropy; ep.grad_logp = lp->grad_logp;
+                ep.grad_entropy = lp->grad_entropy; ep.dz = dz; ep.ld_dz = plan.Vs; ep.V = V; ep.v0 = static_cast<int>(v0);
+                f32::gemm_kernel<f32::DZ, true, true><<<dim3(static_cast<unsigned>(cdiv(T, f32::TM)), static_cast<unsigned>(op.n_groups)), f32::THREADS, 0, st>>>(op, ep);
+                if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
+                int rc = launch_f32_dw(dz, plan.Vs, static_cast<const float*>(Hw), ldHw, w, d, T, nullptr,
+                                       static_cast<float*>(dW) + v0 * shape->ldW, shape->ldW, accumulate_dW != 0, part, st);
+                if (rc == CAT_OK) rc = launch_f32_dh(dz, plan.Vs, Wf, shape->ldW, T, d, w, nullptr, static_cast<float*>(dH), shape->ldH, !first, part, st);
+                if (rc != CAT_OK) return rc;
+                continue;
+            }
             {
                 simt::Operands op;
                 op.A = Hf; op.sAm = shape->ldH; op.sAk = 1; op.B = Wf; op.sBk = 1; op.sBn = shape->ldW;
@@ -1116,16 +1180,11 @@ static int bwd_core(const cat_shape* shape, const void* H, const void* W, const 
                 ep.labels = y; ep.valid = valid; ep.lse = lse; ep.weight = weight; ep.dz = dz; ep.ld_dz = plan.Vs;
                 ep.V = V; ep.v0 = static_cast<int>(v0);
                 const dim3 grid(static_cast<unsigned>(cdiv(T, simt::TM)), static_cast<unsigned>(op.n_groups));
-                if (lp) {
-                    ep.entropy = lp->entropy; ep.grad_logp = lp->grad_logp; ep.grad_entropy = lp->grad_entropy;
-                    simt::gemm_kernel<simt::MODE_DZ_LP><<<grid, simt::THREADS, 0, st>>>(op, ep);
-                } else {
-                    simt::gemm_kernel<simt::MODE_DZ><<<grid, simt::THREADS, 0, st>>>(op, ep);
-                }
+                simt::gemm_kernel<simt::MODE_DZ><<<grid, simt::THREADS, 0, st>>>(op, ep);
             }
             {   // dW slice = (g/N) dz^T H : A(m = v, k = r) = dz[r][v], B(k = r, n = i) = H[r][i]
                 simt::Operands op;
-                op.A = dz; op.sAm = 1; op.sAk = plan.Vs; op.B = static_cast<const float*>(Hw); op.sBk = ldHw; op.sBn = 1;
+                op.A = dz; op.sAm = 1; op.sAk = plan.Vs; op.B = Hf; op.sBk = shape->ldH; op.sBn = 1;
                 op.M = w; op.N = d; op.Kd = T; op.n_groups = static_cast<int>(cdiv(d, simt::TN));
                 simt::EpiParams ep;
                 memset(&ep, 0, sizeof(ep));

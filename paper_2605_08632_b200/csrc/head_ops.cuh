@@ -18,15 +18,15 @@ struct LpPlan {
     size_t off_m, off_l, off_u, off_id, off_g, off_z, total;
 };
 
-int simt_splits(long long rows, long long V) {
-    long long S = (2 * kPlanSMs) / cdiv(rows, simt::TM);
-    const long long num_n = cdiv(V, simt::TN);
+// Vocabulary splits of the fp32 forward product: about four CTAs per SM.
+int f32_splits(long long rows, long long V) {
+    long long S = cdiv(4 * kPlanSMs, cdiv(rows, f32::TM));
+    const long long num_n = cdiv(V, f32::TN);
     if (S > num_n) S = num_n;
-    if (S > 64) S = 64;
-    return static_cast<int>(S < 1 ? 1 : S);
+    return static_cast<int>(S > kMaxSplits ? kMaxSplits : S);
 }
 int head_splits(const cat_shape* s, long long rows) {
-    return s->in_dtype == CAT_BF16 ? fwd_splits(rows, s->V) : simt_splits(rows, s->V);
+    return s->in_dtype == CAT_BF16 ? fwd_splits(rows, s->V) : f32_splits(rows, s->V);
 }
 
 // Up to 128 rows go to the kernel of skinny.cuh.  Measured on 1024 x 151936: XXX
@@ -91,10 +91,10 @@ int launch_skinny(const cat_shape* s, const LpPlan& plan, const void* H, const v
 LpPlan plan_lp(const cat_shape* s, int top_k) {
     LpPlan p;
     const bool bf16 = s->in_dtype == CAT_BF16;
-    const long long tile = bf16 ? tile_m() : simt::TM;
-    p.group = bf16 ? tc::LP_GROUP : simt::TN;
+    const long long tile = bf16 ? tile_m() : f32::TM;
+    p.group = bf16 ? tc::LP_GROUP : f32::TN;
     p.ldz = cdiv(s->V, 256) * 256;
-    p.ld_g = bf16 ? cdiv(s->V, tc::BN) * (tc::BN / tc::LP_GROUP) : cdiv(s->V, simt::TN);
+    p.ld_g = bf16 ? cdiv(s->V, tc::BN) * (tc::BN / tc::LP_GROUP) : cdiv(s->V, f32::TN);
     p.Ts = s->T;
     if (top_k > 0) {
         const long long mib = s->slab_mib > 0 ? s->slab_mib : kDefaultFusedSlabMiB;
@@ -184,18 +184,18 @@ int lp_slab(const cat_shape* s, const LpPlan& plan, const CUtensorMap& tmW, cons
                                                           top_k, logp, lse, entropy, top_ids, top_logp, st);
     }
     const float* Hs = static_cast<const float*>(H) + r0 * s->ldH;
-    simt::Operands op;
+    f32::Operands op;
     op.A = Hs; op.sAm = s->ldH; op.sAk = 1; op.B = static_cast<const float*>(W); op.sBk = 1; op.sBn = s->ldW;
     op.M = static_cast<int>(rws); op.N = static_cast<int>(s->V); op.Kd = static_cast<int>(s->d); op.n_groups = S;
-    simt::EpiParams ep;
+    f32::EpiParams ep;
     memset(&ep, 0, sizeof(ep));
     ep.part_m = part_m; ep.part_l = part_l; ep.part_u = part_u; ep.part_id = reinterpret_cast<int*>(ws + plan.off_id); ep.V = static_cast<int>(s->V);
     if (TOP) {
         ep.zs = reinterpret_cast<float*>(ws + plan.off_z); ep.ld_z = plan.ldz;
         ep.gmax = reinterpret_cast<float*>(ws + plan.off_g); ep.ld_g = plan.ld_g;
     }
-    const dim3 grid(static_cast<unsigned>(cdiv(rws, simt::TM)), static_cast<unsigned>(S));
-    simt::gemm_kernel<simt::MODE_FWD_KEEP><<<grid, simt::THREADS, 0, st>>>(op, ep);
+    const dim3 grid(static_cast<unsigned>(cdiv(rws, f32::TM)), static_cast<unsigned>(S));
+    f32::gemm_kernel<f32::FWD, true, true><<<grid, f32::THREADS, 0, st>>>(op, ep);
     if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
     return launch_lp_rows<float, float, TOP>(s, plan, Hs, static_cast<const float*>(W), r0, rws, S, ws, labels, valid, top_k, logp, lse,
                                              entropy, top_ids, top_logp, st);
@@ -233,7 +233,7 @@ TkPlan plan_tk(const cat_shape* s, int k) {
         f.S_max = 1;
         for (long long r0 = 0; r0 < s->T; r0 += f.Ts) {
             const long long rws = (s->T - r0) < f.Ts ? (s->T - r0) : f.Ts;
-            const int S = simt_splits(rws, s->V);
+            const int S = f32_splits(rws, s->V);
             if (S > f.S_max) f.S_max = S;
             f.n_row_ctas += static_cast<int>(cdiv(f.warp_scan ? rws : rws / s->K, rows::ROW_THREADS));
         }
@@ -261,6 +261,8 @@ TkPlan plan_tk(const cat_shape* s, int k) {
         const size_t full = dh_part_bytes(p.f.Ts < s->T ? p.f.Ts : s->T, s->d, s->V);
         const size_t rest = dh_part_bytes(s->T - (p.f.n_slabs - 1) * p.f.Ts, s->d, s->V);
         off += full > rest ? full : rest;
+    } else {
+        off += kF32PartBytes;
     }
     p.total = off;
     return p;
@@ -272,20 +274,11 @@ int slab_grads(const cat_shape* s, const FusedPlan& f, const void* W, const void
                cudaStream_t st) {
     const int V = static_cast<int>(s->V), d = static_cast<int>(s->d), R = static_cast<int>(rws);
     if (s->in_dtype != CAT_BF16) {
-        float* dz = static_cast<float*>(zs);
-        simt::Operands op;
-        simt::EpiParams ep;
-        op.A = dz; op.sAm = f.ldz; op.sAk = 1; op.B = static_cast<const float*>(W); op.sBk = s->ldW; op.sBn = 1;
-        op.M = R; op.N = d; op.Kd = V; op.n_groups = static_cast<int>(cdiv(d, simt::TN));
-        memset(&ep, 0, sizeof(ep));
-        ep.alpha = scale; ep.out = static_cast<float*>(dH) + r0 * s->ldH; ep.ld_out = s->ldH;
-        simt::gemm_kernel<simt::MODE_OUT><<<dim3(static_cast<unsigned>(cdiv(R, simt::TM)), static_cast<unsigned>(op.n_groups)), simt::THREADS, 0, st>>>(op, ep);
-        op.A = dz; op.sAm = 1; op.sAk = f.ldz; op.B = static_cast<const float*>(Hw); op.sBk = ldHw; op.sBn = 1;
-        op.M = V; op.N = d; op.Kd = R;
-        ep.out = static_cast<float*>(dW); ep.ld_out = s->ldW;
-        if (!first || accumulate_dW) { ep.add = ep.out; ep.ld_add = s->ldW; }
-        simt::gemm_kernel<simt::MODE_OUT><<<dim3(static_cast<unsigned>(cdiv(V, simt::TM)), static_cast<unsigned>(op.n_groups)), simt::THREADS, 0, st>>>(op, ep);
-        return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+        const int rc = launch_f32_dh(static_cast<float*>(zs), f.ldz, static_cast<const float*>(W), s->ldW, R, d, V, scale,
+                                     static_cast<float*>(dH) + r0 * s->ldH, s->ldH, false, part, st);
+        if (rc != CAT_OK) return rc;
+        return launch_f32_dw(static_cast<float*>(zs), f.ldz, static_cast<const float*>(Hw), ldHw, V, d, R, scale, static_cast<float*>(dW),
+                             s->ldW, !first || accumulate_dW, part, st);
     }
     int* status = reinterpret_cast<int*>(ws);
     CUtensorMap tmZ_k, tmZ_mn, tmW_mn, tmH_mn;
@@ -358,9 +351,7 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
         const int S = head_splits(s, rws);
         const TI* Hs = H + r0 * s->ldH;
         tk::gather_kernel<TI><<<static_cast<unsigned>(rws), tk::THREADS, 0, st>>>(Hs, s->ldH, W, s->ldW, d, y, ok, lists, r0, zt,
-                                                                                plan.ld_zt, ref);
-        // rows that take no part may hold anything: they meet dz = 0 in the dW contraction as zeros
-        lp::masked_copy_kernel<TI><<<static_cast<unsigned>(rws), lp::THREADS, 0, st>>>(Hs, s->ldH, d, ok + r0, Hz);
+                                                                                plan.ld_zt, ref, Hz);
         if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
         rows::RowParams rp;
         memset(&rp, 0, sizeof(rp));
@@ -376,15 +367,15 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
             if (rc != CAT_OK) return rc;
             mp.part_m = ep.part_m; mp.part_l = ep.part_l; mp.part_id = ep.part_id; mp.part_stride = T;
         } else {
-            simt::Operands op;
+            f32::Operands op;
             op.A = reinterpret_cast<const float*>(Hs); op.sAm = s->ldH; op.sAk = 1;
             op.B = reinterpret_cast<const float*>(W); op.sBk = 1; op.sBn = s->ldW;
             op.M = static_cast<int>(rws); op.N = V; op.Kd = d; op.n_groups = S;
-            simt::EpiParams ep;
+            f32::EpiParams ep;
             memset(&ep, 0, sizeof(ep));
             ep.labels = y + r0; ep.part_m = part_m; ep.part_l = part_l; ep.z_label = z_label + r0; ep.V = V;
             ep.zs = static_cast<float*>(zs); ep.ld_z = f.ldz;
-            simt::gemm_kernel<simt::MODE_FWD_KEEP><<<dim3(static_cast<unsigned>(cdiv(rws, simt::TM)), static_cast<unsigned>(S)), simt::THREADS, 0, st>>>(op, ep);
+            f32::gemm_kernel<f32::FWD, true, true><<<dim3(static_cast<unsigned>(cdiv(rws, f32::TM)), static_cast<unsigned>(S)), f32::THREADS, 0, st>>>(op, ep);
             mp.part_m = part_m; mp.part_l = part_l; mp.part_id = nullptr; mp.part_stride = rws;
         }
         mp.S = S; mp.H = Hs; mp.W = W; mp.ldH = s->ldH; mp.ldW = s->ldW; mp.d = d; mp.labels = y + r0; mp.valid = ok + r0;

@@ -278,6 +278,33 @@ __device__ __forceinline__ double warp_dot(const float* h, const float* w, int d
     return acc;
 }
 
+// The same as an fp32 sum (four chains per lane), for where nothing is ordered by it: converting every product to fp64 costs 16 lanes
+// a clock.
+__device__ __forceinline__ float warp_dot_f32(const __nv_bfloat16* h, const __nv_bfloat16* w, int d, int lane) {
+    const uint4* hv = reinterpret_cast<const uint4*>(h);
+    const uint4* wv = reinterpret_cast<const uint4*>(w);
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = lane; i < d / 8; i += 32) {
+        const uint4 a = __ldg(hv + i), b = __ldg(wv + i);
+        const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 fa = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&aw[j]));
+            const float2 fb = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&bw[j]));
+            acc[j] = fmaf(fa.x, fb.x, acc[j]);
+            acc[j] = fmaf(fa.y, fb.y, acc[j]);
+        }
+    }
+    float sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    return sum;
+}
+__device__ __forceinline__ float warp_dot_f32(const float* h, const float* w, int d, int lane) {
+    return static_cast<float>(warp_dot(h, w, d, lane));
+}
+
 // What the slab says of column v of a group whose maximum is gm: its logit up to `err`, plus the GEMM's own error.  fp16 slabs hold
 // the distance from the maximum (half a step: 2^-11 of it, or 2^-25), fp32 slabs the logit itself.
 __device__ __forceinline__ float stored(const __half* z, float gm, long long v, float& err) {
@@ -788,18 +815,18 @@ __global__ void __launch_bounds__(THREADS) add_parts_kernel(const float* part, i
 // Copy of H with the rows that take no part set to zero: the dW contraction meets them with dz = 0, and 0 times
 // whatever padding a caller left there (NaN, infinity) must add nothing.
 template <class TI>
-__global__ void __launch_bounds__(THREADS) masked_copy_kernel(const TI* H, long long ldH, int d, const unsigned char* valid,
-                                                              TI* out) {
-    const long long r = blockIdx.x;
-    const bool on = valid == nullptr || valid[r] != 0;
-    constexpr int PER = 16 / sizeof(TI);
+__device__ __forceinline__ void copy_row(const TI* src, TI* dst, int d, bool on) {
     if (sizeof(TI) == 2) {
-        const uint4* src = reinterpret_cast<const uint4*>(H + r * ldH);
-        uint4* dst = reinterpret_cast<uint4*>(out + r * d);
-        for (int i = threadIdx.x; i < d / PER; i += THREADS) dst[i] = on ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+        for (int i = threadIdx.x; i < d / 8; i += THREADS)
+            reinterpret_cast<uint4*>(dst)[i] = on ? __ldg(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0u, 0u, 0u, 0u);
     } else {
-        for (int i = threadIdx.x; i < d; i += THREADS) out[r * d + i] = on ? H[r * ldH + i] : static_cast<TI>(0);
+        for (int i = threadIdx.x; i < d; i += THREADS) dst[i] = on ? src[i] : static_cast<TI>(0);
     }
+}
+template <class TI>
+__global__ void __launch_bounds__(THREADS) masked_copy_kernel(const TI* H, long long ldH, int d, const unsigned char* valid, TI* out) {
+    const long long r = blockIdx.x;
+    copy_row(H + r * ldH, out + r * d, d, valid == nullptr || valid[r] != 0);
 }
 
 }  // namespace lp

@@ -19,24 +19,14 @@ struct Operands {
     int n_groups;     // gridDim.y; group g covers n-tiles [g*nt/n_groups, (g+1)*nt/n_groups)
 };
 
-enum { MODE_FWD = 0, MODE_DZ = 1, MODE_OUT = 2, MODE_FWD_KEEP = 3, MODE_DZ_LP = 4 };   // KEEP: logits, entropy sums and tile maxima too
+enum { MODE_FWD = 0, MODE_DZ = 1, MODE_OUT = 2 };
 
 struct EpiParams {
     // MODE_FWD
     const long long* labels;
     float* part_m;
     float* part_l;
-    float* z_label;                // MODE_FWD_KEEP: may be nullptr
-    // MODE_FWD_KEEP
-    int* part_id;                  // first column of the maximum; with part_u
-    float* part_u;                 // sum exp2(x) x with x = (z - max) log2 e; nullptr = not wanted
-    float* zs;                     // [M][ld_z] logits, or nullptr
-    float* gmax;                   // [M][ld_g] maximum of each TN-column tile, or nullptr
-    long long ld_z, ld_g;
-    // MODE_DZ_LP (dz = gl ([v = y] - p) - ge p (log p + entropy); rows with valid = 0 get zeros)
-    const float* entropy;
-    const float* grad_logp;
-    const float* grad_entropy;
+    float* z_label;
     // MODE_DZ
     const unsigned char* valid;
     const float* lse;
@@ -65,29 +55,16 @@ __global__ void __launch_bounds__(THREADS) gemm_kernel(const Operands op, const 
     const int nt_end = static_cast<int>((static_cast<long long>(g + 1) * n_tiles) / op.n_groups);
 
     // per-row state (rows ty*4 + i), replicated over the 16 threads that share a row
-    constexpr bool FWD = MODE == MODE_FWD || MODE == MODE_FWD_KEEP;
     float m_run[4], l_run[4], w_row[4], lse_row[4];
-    float u_run[4] = {}, ca[4] = {}, cb[4] = {};
-    int id_run[4] = {};
     int y_row[4];
-    bool on[4] = {};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int row = m0 + ty * 4 + i;
-        m_run[i] = MODE == MODE_FWD_KEEP ? -1.0e30f : -INFINITY; l_run[i] = 0.f; w_row[i] = 0.f; lse_row[i] = INFINITY; y_row[i] = -1;
-        if (MODE == MODE_DZ_LP && row < op.M) {
-            on[i] = ep.valid == nullptr || ep.valid[row] != 0;
-            if (on[i]) {
-                lse_row[i] = ep.lse[row];
-                const long long y = ep.grad_logp ? ep.labels[row] : -1;
-                if (y >= 0 && y < ep.V) { y_row[i] = static_cast<int>(y) - ep.v0; w_row[i] = ep.grad_logp[row]; ca[i] = -w_row[i]; }
-                if (ep.grad_entropy) { cb[i] = -ep.grad_entropy[row]; ca[i] = fmaf(cb[i], ep.entropy[row], ca[i]); }
-            }
-        }
-        if (MODE != MODE_OUT && MODE != MODE_DZ_LP && row < op.M && (MODE != MODE_FWD_KEEP || ep.labels != nullptr)) {
+        m_run[i] = -INFINITY; l_run[i] = 0.f; w_row[i] = 0.f; lse_row[i] = INFINITY; y_row[i] = -1;
+        if (MODE != MODE_OUT && row < op.M) {
             const long long y = ep.labels[row];
             const bool y_ok = y >= 0 && y < ep.V;
-            if (FWD) {
+            if (MODE == MODE_FWD) {
                 if (y_ok) y_row[i] = static_cast<int>(y);
             } else {
                 const bool ok = y_ok && (ep.valid == nullptr || ep.valid[row] != 0);
@@ -153,62 +130,6 @@ __global__ void __launch_bounds__(THREADS) gemm_kernel(const Operands op, const 
                 l_run[i] = l_run[i] * expf(m_run[i] - m_new) + sum;
                 m_run[i] = m_new;
             }
-        } else if (MODE == MODE_FWD_KEEP) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = m0 + ty * 4 + i;
-                float cmax = -1.0e30f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int col = n0 + tx * 4 + j;
-                    if (col < op.N) cmax = fmaxf(cmax, acc[i][j]);
-                    if (col == y_row[i] && ep.z_label != nullptr) ep.z_label[row] = acc[i][j];
-                    if (ep.zs != nullptr && row < op.M && col < op.N) ep.zs[row * ep.ld_z + col] = acc[i][j];
-                }
-#pragma unroll
-                for (int off = 1; off < 16; off <<= 1) cmax = fmaxf(cmax, __shfl_xor_sync(0xffffffffu, cmax, off));
-                if (ep.gmax != nullptr && tx == 0 && row < op.M) ep.gmax[row * ep.ld_g + nt] = cmax;
-                int id = op.N;
-#pragma unroll
-                for (int j = 3; j >= 0; --j)
-                    if (acc[i][j] == cmax && n0 + tx * 4 + j < op.N) id = n0 + tx * 4 + j;
-#pragma unroll
-                for (int off = 1; off < 16; off <<= 1) id = min(id, __shfl_xor_sync(0xffffffffu, id, off));
-                if (cmax > m_run[i] && id < op.N) id_run[i] = id;
-                const float m_new = fmaxf(m_run[i], cmax);
-                float sum = 0.f, us = 0.f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int col = n0 + tx * 4 + j;
-                    const float x = (acc[i][j] - m_new) * 1.4426950408889634f;
-                    const float e = expf(acc[i][j] - m_new);
-                    if (col < op.N) { sum += e; us = fmaf(e, x, us); }
-                }
-#pragma unroll
-                for (int off = 1; off < 16; off <<= 1) {
-                    sum += __shfl_xor_sync(0xffffffffu, sum, off);
-                    us += __shfl_xor_sync(0xffffffffu, us, off);
-                }
-                const float sc = expf(m_run[i] - m_new);
-                u_run[i] = sc * fmaf((m_run[i] - m_new) * 1.4426950408889634f, l_run[i], u_run[i]) + us;
-                l_run[i] = l_run[i] * sc + sum;
-                m_run[i] = m_new;
-            }
-        } else if (MODE == MODE_DZ_LP) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = m0 + ty * 4 + i;
-                if (row >= op.M) continue;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int col = n0 + tx * 4 + j;
-                    if (col >= op.N) continue;
-                    const float x = acc[i][j] - lse_row[i];
-                    float v = expf(x) * fmaf(cb[i], x, ca[i]);
-                    if (col == y_row[i]) v += w_row[i];
-                    ep.dz[row * ep.ld_dz + col] = on[i] ? v : 0.f;
-                }
-            }
         } else if (MODE == MODE_DZ) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -239,17 +160,13 @@ __global__ void __launch_bounds__(THREADS) gemm_kernel(const Operands op, const 
             }
         }
     }
-    if (FWD && tx == 0) {
+    if (MODE == MODE_FWD && tx == 0) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = m0 + ty * 4 + i;
             if (row < op.M) {
                 ep.part_m[static_cast<size_t>(g) * op.M + row] = m_run[i];
                 ep.part_l[static_cast<size_t>(g) * op.M + row] = l_run[i];
-                if (MODE == MODE_FWD_KEEP && ep.part_u != nullptr) {
-                    ep.part_u[static_cast<size_t>(g) * op.M + row] = u_run[i];
-                    ep.part_id[static_cast<size_t>(g) * op.M + row] = id_run[i];
-                }
             }
         }
     }

@@ -154,28 +154,30 @@ struct Lists {
     }
 };
 
-// One CTA per row of the slab: z[r, id_i] as fp32 for every counting entry of its list (one warp per dot product), and
-// ref[r], the largest of them and of the label's logit (0 for a row that takes no part).
+// One CTA per row of the slab: z[r, id_i] as fp32 for every counting entry of its list (one warp per dot product), ref[r],
+// the largest of them and of the label's logit (0 for a row that takes no part), and the row's copy in Hz: the dW contraction's
+// operand, in which a row that takes no part is zero whatever H holds there.
 template <class TI>
 __global__ void __launch_bounds__(THREADS) gather_kernel(const TI* H, long long ldH, const TI* W, long long ldW, int d,
                                                          const long long* labels, const unsigned char* valid_eff, Lists lists,
-                                                         long long row0, float* zt, int ld_zt, float* ref) {
+                                                         long long row0, float* zt, int ld_zt, float* ref, TI* Hz) {
     __shared__ float s_max[WARPS];
     const long long r = row0 + blockIdx.x;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const TI* h = H + static_cast<long long>(blockIdx.x) * ldH;
+    lp::copy_row(h, Hz + static_cast<long long>(blockIdx.x) * d, d, valid_eff[r] != 0);
     if (!valid_eff[r]) {
         if (threadIdx.x == 0) ref[r] = 0.f;
         return;
     }
     const long long t = lists.position(r);
-    const TI* h = H + static_cast<long long>(blockIdx.x) * ldH;
     float mx = -INFINITY;
     for (int i = warp; i <= lists.k; i += WARPS) {
         long long id = -1;
         float lp;
         if (i == lists.k) id = labels[r];
         else if (!lists.entry(t, i, id, lp)) continue;
-        const float z = static_cast<float>(lp::warp_dot(h, W + id * ldW, d, lane));
+        const float z = lp::warp_dot_f32(h, W + id * ldW, d, lane);
         if (lane == 0) zt[static_cast<long long>(blockIdx.x) * ld_zt + i] = z;
         mx = fmaxf(mx, z);
     }
@@ -189,7 +191,7 @@ __global__ void __launch_bounds__(THREADS) gather_kernel(const TI* H, long long 
 }
 
 // Merges the vocabulary splits of a row's (max, sum exp) into one pair for the row kernel (one warp per row), and corrects the sum for the
-// largest logit and the label's, which are known as fp64 sums: the tensor cores' additions truncate, and a token of
+// largest logit and the label's, which are known exactly (nearly: as fp32 sums): the tensor cores' additions truncate, and a token of
 // high probability makes up lse (see lp::row_kernel).  z_label is replaced by the exact label logit.
 template <class TI>
 struct MergeParams {
@@ -235,7 +237,7 @@ __global__ void __launch_bounds__(THREADS) merge_kernel(const MergeParams<TI> p)
         const float zy = p.z_exact[r * p.ld_exact];
         if (p.part_id) {
             const bool is_label = p.labels[r] == id;
-            const float z = is_label ? zy : static_cast<float>(lp::warp_dot(p.H + r * p.ldH, p.W + id * p.ldW, p.d, lane));
+            const float z = is_label ? zy : lp::warp_dot_f32(p.H + r * p.ldH, p.W + id * p.ldW, p.d, lane);
             if (fabsf(z - m) < 1.f) l += expm1f(z - m);
             if (!is_label && fabsf(zy - p.z_label[r]) < 1.f) l += expf(p.z_label[r] - m) * expm1f(zy - p.z_label[r]);
         }
