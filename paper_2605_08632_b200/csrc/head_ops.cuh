@@ -94,7 +94,7 @@ LpPlan plan_lp(const cat_shape* s, int top_k) {
     const long long tile = bf16 ? tile_m() : f32::TM;
     p.group = bf16 ? tc::LP_GROUP : f32::TN;
     p.ldz = cdiv(s->V, 256) * 256;
-    p.ld_g = bf16 ? cdiv(s->V, tc::BN) * (tc::BN / tc::LP_GROUP) : cdiv(s->V, f32::TN);
+    p.ld_g = bf16 ? cdiv(s->V, tc::BN) * (tc::BN / tc::LP_GROUP) : cdiv(cdiv(s->V, f32::TN), 4) * 4;
     p.Ts = s->T;
     if (top_k > 0) {
         const long long mib = s->slab_mib > 0 ? s->slab_mib : kDefaultFusedSlabMiB;
@@ -149,7 +149,7 @@ int launch_lp_rows(const cat_shape* s, const LpPlan& plan, const TI* H, const TI
         rp.top_ids = reinterpret_cast<long long*>(top_ids) + r0 * top_k;
         rp.top_logp = top_logp + r0 * top_k;
     }
-    lp::row_kernel<TI, TZ, TOP><<<static_cast<unsigned>(rws), lp::THREADS, 0, st>>>(rp);
+    lp::row_kernel<TI, TZ, TOP><<<static_cast<unsigned>(rws), lp::RT, 0, st>>>(rp);
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
 

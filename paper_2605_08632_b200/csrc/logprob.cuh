@@ -245,7 +245,9 @@ namespace lp {
 constexpr int THREADS = 256;
 constexpr int WARPS = THREADS / 32;
 constexpr int MAX_TOP = 256;            // CAT_TOPK_MAX
-constexpr int CAP = 1024;               // candidate columns held at a time
+constexpr int CAP = 512;                // candidate columns held at a time
+constexpr int RT = 128;                 // threads of the row kernel: its phases wait more than they work, so many small CTAs per SM
+constexpr int RW = RT / 32;
 
 // H[r, :] . W[v, :] by one warp, every lane gets the sum.  bf16 products are exact in fp32 (16 significant bits), fp32
 // products in fp64; the sums are taken in fp64 and always in the same order, so equal rows of W give equal logits.
@@ -325,8 +327,9 @@ template <class TZ>
 struct GroupOf { static constexpr int value = tc::LP_GROUP; };
 template <>
 struct GroupOf<float> { static constexpr int value = 64; };       // columns per tile of the fp32 GEMM
-// Error of a logit of the GEMM relative to the row's largest: one addition of 16 products (tensor cores) or one (fp32) at a time, each off
-// by at most 2^-23 of a running sum that is taken to stay within twice that logit.
+// Error of a logit of the GEMM relative to itself, or to the threshold where that is larger: one addition of 16 products (tensor cores) or
+// one (fp32) at a time, each off by at most 2^-23 of a running sum that is taken to stay within twice that.  (What was seen: 3e-6 of
+// a logit at d = 2048, against 3.2e-5 here.)
 __device__ __forceinline__ float gemm_error(const __half*, int d) { return static_cast<float>(d / 16 + 8) * 2.384185791015625e-7f; }
 __device__ __forceinline__ float gemm_error(const float*, int d) { return static_cast<float>(d + 8) * 2.384185791015625e-7f; }
 
@@ -359,8 +362,8 @@ struct RowParams {
 };
 
 struct Shared {
-    float red[2][WARPS];
-    int count[2][WARPS];
+    float red[2][RW];
+    int count[2][RW];
     int n_cand, n_near;
     float m, l, u, lse;
     int id_max;
@@ -385,62 +388,47 @@ __device__ __forceinline__ float block_max(float x, float* red) {
     __syncthreads();
     x = red[0];
 #pragma unroll
-    for (int i = 1; i < WARPS; ++i) x = fmaxf(x, red[i]);
+    for (int i = 1; i < RW; ++i) x = fmaxf(x, red[i]);
     return x;
 }
 
-// A number that at least k of n values reach, and few more than k: bisection between the least and the largest of them.  The first
-// KEPT * THREADS values come in registers (v, value j * THREADS + threadIdx.x, -infinity past n), the others by `value`.
-// big = largest |value|.  Up to k = 128 the bisection runs over the threads' own largest values only: any k of them are k of the
-// values, the bound is a little lower (k = 64 of 4008 values: 72 reach it instead of 64), and a step is one compare and one
-// barrier that counts.
-constexpr int KEPT = 20;
-template <class F>
-__device__ __forceinline__ float near_kth(const float (&v)[KEPT], F value, int n, int k, Shared& sh, float& big) {
-    float mine = -INFINITY, nlo = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < KEPT; ++j) {
-        mine = fmaxf(mine, v[j]);
-        if (j * THREADS + threadIdx.x < n) nlo = fmaxf(nlo, -v[j]);
-    }
-    for (int i = KEPT * THREADS + threadIdx.x; i < n; i += THREADS) {
-        const float x = value(i);
-        mine = fmaxf(mine, x);
-        nlo = fmaxf(nlo, -x);
-    }
+// A bound that at least k of the values reach, and few more than k, from the largest values of each thread's four shares of them (best,
+// -infinity for an empty share): any k of those are k of the values.  Bisection between the least and the largest, until at most
+// k + k / 16 + 1 shares reach it (k = 64 of 4008 values: about 75 values do).  LP_LOW when fewer than k shares hold a value.  big: largest |value| there is.
+__device__ __forceinline__ float near_kth(const float (&best)[4], float least, int k, Shared& sh, float& big) {
+    const float mine = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
     float hi = block_max(mine, sh.red[0]);
-    float lo = -block_max(nlo, sh.red[1]);
-    big = fmaxf(fabsf(hi), fabsf(lo));
-    if (n <= k) return lo;
-    const int enough = k + k / 4 + 2;
-    if (k <= THREADS / 2 && n >= THREADS) {
-        lo = -block_max(-mine, sh.red[0]);          // every thread's value reaches it
-        for (int it = 0; it < 24; ++it) {
-            const float mid = 0.5f * lo + 0.5f * hi;
-            if (!(mid > lo && mid < hi)) break;
-            const int c = __syncthreads_count(mine >= mid);
-            if (c >= k) {
-                lo = mid;
-                if (c <= enough) break;
-            } else {
-                hi = mid;
-            }
-        }
-        return lo;
+    big = fmaxf(fabsf(hi), fabsf(block_max(-least, sh.red[1])));
+    const bool one = k <= RT / 4;                   // the threads' own largest values will do
+    float low = mine;
+    if (!one) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) low = fminf(low, best[j]);
     }
-    for (int it = 0; it < 24; ++it) {
-        const float mid = 0.5f * lo + 0.5f * hi;
-        if (!(mid > lo && mid < hi)) break;
+    float lo = -block_max(-low, sh.red[0]);         // -infinity with an empty share: the loop below counts from LP_LOW then
+    lo = fmaxf(lo, tc::LP_LOW);
+    const int enough = k + k / 16 + 1;
+    auto count = [&](float x, int it) {
+        if (one) return __syncthreads_count(mine >= x);
         int c = 0;
 #pragma unroll
-        for (int j = 0; j < KEPT; ++j) c += v[j] >= mid ? 1 : 0;
-        for (int i = KEPT * THREADS + threadIdx.x; i < n; i += THREADS) c += value(i) >= mid ? 1 : 0;
+        for (int j = 0; j < 4; ++j) c += best[j] >= x ? 1 : 0;
         c = __reduce_add_sync(0xffffffffu, c);
         if ((threadIdx.x & 31) == 0) sh.count[it & 1][threadIdx.x >> 5] = c;
         __syncthreads();
         c = 0;
 #pragma unroll
-        for (int i = 0; i < WARPS; ++i) c += sh.count[it & 1][i];
+        for (int i = 0; i < RW; ++i) c += sh.count[it & 1][i];
+        return c;
+    };
+    if (lo == tc::LP_LOW) {      // some share is empty: are there k at all?
+        if (count(lo, 1) < k) return lo;
+        lo = fmaxf(lo, -big);
+    }
+    for (int it = 0; it < 24; ++it) {
+        const float mid = 0.5f * lo + 0.5f * hi;
+        if (!(mid > lo && mid < hi)) break;
+        const int c = count(mid, it);
         if (c >= k) {
             lo = mid;
             if (c <= enough) break;
@@ -493,12 +481,12 @@ __device__ __forceinline__ void exact_one(const RowParams<TI, TZ>& p, const TI* 
 template <class TI, class TZ>
 __device__ __forceinline__ int settle(const RowParams<TI, TZ>& p, const TI* h, Shared& sh, int from, int n) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int c = from + warp; c < n; c += WARPS) {
+    for (int c = from + warp; c < n; c += RW) {
         const double z = warp_dot(h, p.W + static_cast<long long>(sh.id[c]) * p.ldW, p.d, lane);
         if (lane == 0) sh.z[c] = z;
     }
     __syncthreads();
-    for (int c = threadIdx.x; c < n; c += THREADS) {
+    for (int c = threadIdx.x; c < n; c += RT) {
         const double z = sh.z[c];
         const int id = sh.id[c];
         int rank = 0;
@@ -512,17 +500,17 @@ __device__ __forceinline__ int settle(const RowParams<TI, TZ>& p, const TI* h, S
 // The same from the approximate logits, with exact ones only for candidates that their errors leave in doubt against another, and for
 // those that the slab's fp16 has rounded (not the largest of their group): their values are returned.
 template <class TI, class TZ>
-__device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI* h, long long r, Shared& sh, int n, float eps) {
+__device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI* h, long long r, Shared& sh, int n, float eps, float rel) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    static_assert(CAP / THREADS <= 32, "one bit per candidate of a thread");
-    unsigned doubt = 0, out = 0;              // bit i: candidate threadIdx.x + i * THREADS needs its exact logit, is out
+    static_assert(CAP / RT <= 32, "one bit per candidate of a thread");
+    unsigned doubt = 0, out = 0;              // bit i: candidate threadIdx.x + i * RT needs its exact logit, is out
     // Several threads share a candidate while there are threads to share: each looks at its part of the others.
-    const int parts = n <= THREADS / 2 ? THREADS / (n > 0 ? n : 1) : 1;
+    const int parts = n <= RT / 2 ? RT / (n > 0 ? n : 1) : 1;
     const int part = threadIdx.x / (n > 0 ? n : 1), per = (n + parts - 1) / parts;
-    for (int c = threadIdx.x; c < n; c += THREADS) { sh.above[c] = 0; sh.close[c] = 0; }
+    for (int c = threadIdx.x; c < n; c += RT) { sh.above[c] = 0; sh.close[c] = 0; }
     if (threadIdx.x == 0) sh.n_near = 0;
     __syncthreads();
-    for (int c = parts > 1 ? threadIdx.x - part * n : threadIdx.x; c < n && (parts == 1 || part < parts); c += parts > 1 ? CAP : THREADS) {
+    for (int c = parts > 1 ? threadIdx.x - part * n : threadIdx.x; c < n && (parts == 1 || part < parts); c += parts > 1 ? CAP : RT) {
         const float z = sh.approx[c], e = sh.err[c];
         const int j0 = parts > 1 ? part * per : 0, j1 = parts > 1 ? min(n, j0 + per) : n;
         int above = 0, near = 0;
@@ -536,16 +524,16 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
         if (near) atomicAdd(&sh.close[c], near);
     }
     __syncthreads();
-    for (int i = 0, c = threadIdx.x; c < n; ++i, c += THREADS) {
+    for (int i = 0, c = threadIdx.x; c < n; ++i, c += RT) {
         if (sh.above[c] >= p.k) out |= 1u << i;
-        else if (sh.close[c] > 1 || sh.err[c] > eps + 4.0e-8f) doubt |= 1u << i;
+        else if (sh.close[c] > 1 || sh.err[c] > fmaxf(eps, rel * fabsf(sh.approx[c])) + 4.0e-8f) doubt |= 1u << i;
         sh.above[c] = 0;
         if (out >> i & 1u) { sh.err[c] = OUT; sh.approx[c] = -INFINITY; }
         else if (doubt >> i & 1u) { sh.err[c] = EXACT; sh.near[atomicAdd(&sh.n_near, 1)] = c; }
     }
     __syncthreads();
     const int n_doubt = sh.n_near;
-    for (int i = warp; i < n_doubt + 2; i += WARPS) {
+    for (int i = warp; i < n_doubt + 2; i += RW) {
         if (i < 2) {
             exact_one(p, h, r, sh, i);
         } else {
@@ -554,7 +542,7 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
             if (lane == 0) sh.z[c] = z;
         }
     }
-    for (int c = parts > 1 ? threadIdx.x - part * n : threadIdx.x; c < n && (parts == 1 || part < parts); c += parts > 1 ? CAP : THREADS) {
+    for (int c = parts > 1 ? threadIdx.x - part * n : threadIdx.x; c < n && (parts == 1 || part < parts); c += parts > 1 ? CAP : RT) {
         const float zc = sh.approx[c];
         const int j0 = parts > 1 ? part * per : 0, j1 = parts > 1 ? min(n, j0 + per) : n;
         int rank = 0;
@@ -563,8 +551,8 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
         if (rank) atomicAdd(&sh.above[c], rank);
     }
     __syncthreads();
-    if (threadIdx.x == THREADS - 1) finish_row(p, r, sh);
-    for (int c = threadIdx.x; c < n; c += THREADS) {
+    if (threadIdx.x == RT - 1) finish_row(p, r, sh);
+    for (int c = threadIdx.x; c < n; c += RT) {
         const float ec = sh.err[c], zc = sh.approx[c];
         if (ec == OUT) continue;
         const int id = sh.id[c];
@@ -596,7 +584,7 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
 // again cost 0.7 ms for 8192 rows of k = 64, a quarter of the GEMM), and equal logits go to the lower id.
 // More than CAP candidates (a row of zeros, many equal rows of W) are settled batch by batch by exact sums.
 template <class TI, class TZ, bool TOP>
-__global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p) {
+__global__ void __launch_bounds__(RT, 8) row_kernel(const RowParams<TI, TZ> p) {
     __shared__ Shared sh;
     const long long r = blockIdx.x;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -607,7 +595,7 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
             if (p.logp) p.logp[r] = 0.f;
         }
         if (TOP)
-            for (int i = threadIdx.x; i < p.k; i += THREADS) { p.top_ids[r * p.k + i] = -1; p.top_logp[r * p.k + i] = -INFINITY; }
+            for (int i = threadIdx.x; i < p.k; i += RT) { p.top_ids[r * p.k + i] = -1; p.top_logp[r * p.k + i] = -INFINITY; }
         return;
     }
     const TI* h = p.H + r * p.ldH;
@@ -616,17 +604,27 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
     const TZ* z = p.zs + r * p.ldz;
     // With few groups per alternative their maxima bound little (or there are not k of them): go by the logits themselves.
     const bool by_group = TOP && p.n_g >= 4 * p.k;
-    const int n_values = by_group ? p.n_g : p.V;
-    auto value = [&](int i) {
-        float e;
-        return by_group ? g[i] : stored(z, g[i / group], i, e);
-    };
-    float v[KEPT];
-    if (TOP) {      // asked for first: they are under way while warp 0 merges
+    float best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, least = INFINITY;
+    if (TOP) {
+        auto see = [&](float x, int j) { best[j] = fmaxf(best[j], x); least = fminf(least, x); };
+        if (by_group) {
+#pragma unroll 4
+            for (int i = threadIdx.x; i < (p.n_g + 3) / 4; i += RT) {      // the pitch is a multiple of 4
+                const float4 x = reinterpret_cast<const float4*>(g)[i];
+                see(x.x, 0);
+                if (4 * i + 1 < p.n_g) see(x.y, 1);
+                if (4 * i + 2 < p.n_g) see(x.z, 2);
+                if (4 * i + 3 < p.n_g) see(x.w, 3);
+            }
+        } else {
+            for (int i = threadIdx.x; i < p.V; i += 4 * RT) {
 #pragma unroll
-        for (int j = 0; j < KEPT; ++j) {
-            const int i = j * THREADS + threadIdx.x;
-            v[j] = i < n_values ? value(i) : -INFINITY;
+                for (int j = 0; j < 4; ++j) {
+                    const int v = i + j * RT;
+                    float e;
+                    if (v < p.V) see(stored(z, g[v / group], v, e), j);
+                }
+            }
         }
     }
     if (warp == 1) {      // the rows of W whose exact logits are wanted at the end
@@ -692,29 +690,38 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
     long long* ids_out = p.top_ids + r * p.k;
     float* lp_out = p.top_logp + r * p.k;
     if (!isfinite(sh.m + logf(sh.l))) {
-        for (int i = threadIdx.x; i < p.k; i += THREADS) { ids_out[i] = -1; lp_out[i] = NAN; }
+        for (int i = threadIdx.x; i < p.k; i += RT) { ids_out[i] = -1; lp_out[i] = NAN; }
         if (warp < 2) exact_one(p, h, r, sh, warp);
         __syncthreads();
         if (threadIdx.x == 0) finish_row(p, r, sh);
         return;
     }
     float big;
-    const float t = near_kth(v, value, n_values, p.k, sh, big);
-    const float eps = big * gemm_error(z, p.d);
-    // a bound taken over stored logits may lie their rounding (2^-11 of the row's span) too high
-    const float thr = t - 2.f * eps - (by_group ? 0.f : 1.0e-3f * big);
+    const float t = near_kth(best, least, p.k, sh, big);
+    const float rel = gemm_error(z, p.d);
+    // k exact logits reach t - eps; a bound taken over stored logits may lie their rounding (2^-11 of the row's span) higher
+    const float eps = rel * fabsf(t);
+    const float thr = t - 2.2f * eps - (by_group ? 0.f : 1.0e-3f * big);
     // the groups that reach the threshold, then their columns that do
     auto keep_group = [&](int gi, float gm) {
         const int at = atomicAdd(&sh.n_near, 1);
         if (at < CAP) { sh.near[at] = gi; sh.near_max[at] = gm; }
     };
-    if (by_group) {
-#pragma unroll
-        for (int j = 0; j < KEPT; ++j)
-            if (v[j] >= thr) keep_group(j * THREADS + threadIdx.x, v[j]);      // -infinity past n_g; thr is finite
+    const int n_vec = by_group ? (p.n_g + 3) / 4 : 0;
+    // with one share per thread, a thread whose largest is below the threshold has nothing to look up
+    if (fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3])) >= thr) {
+#pragma unroll 4
+        for (int i = threadIdx.x; i < n_vec; i += RT) {
+            const float4 x = reinterpret_cast<const float4*>(g)[i];
+            if (x.x >= thr) keep_group(4 * i, x.x);
+            if (x.y >= thr && 4 * i + 1 < p.n_g) keep_group(4 * i + 1, x.y);
+            if (x.z >= thr && 4 * i + 2 < p.n_g) keep_group(4 * i + 2, x.z);
+            if (x.w >= thr && 4 * i + 3 < p.n_g) keep_group(4 * i + 3, x.w);
+        }
     }
-    for (int gi = (by_group ? KEPT * THREADS : 0) + threadIdx.x; gi < p.n_g; gi += THREADS)
-        if (g[gi] >= thr) keep_group(gi, g[gi]);
+    if (!by_group)
+        for (int gi = threadIdx.x; gi < p.n_g; gi += RT)
+            if (g[gi] >= thr) keep_group(gi, g[gi]);
     __syncthreads();
     const int n_near = sh.n_near;
     auto append = [&](bool in, long long col, float x, float e) {      // whole warps
@@ -723,17 +730,17 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
         int at = 0;
         if (lane == 0) at = atomicAdd(&sh.n_cand, __popc(hit));
         at = __shfl_sync(0xffffffffu, at, 0) + __popc(hit & ((1u << lane) - 1u));
-        if (in && at < CAP) { sh.id[at] = static_cast<int>(col); sh.approx[at] = x; sh.err[at] = eps + e; }
+        if (in && at < CAP) { sh.id[at] = static_cast<int>(col); sh.approx[at] = x; sh.err[at] = fmaxf(eps, rel * fabsf(x)) + e; }
     };
     if (n_near <= CAP) {
         const int n_el = n_near * group;
         constexpr int BATCH = 4;      // loads under way together
-        for (int i0 = 0; i0 < n_el; i0 += BATCH * THREADS) {
+        for (int i0 = 0; i0 < n_el; i0 += BATCH * RT) {
             float x[BATCH], e[BATCH];
             long long col[BATCH];
 #pragma unroll
             for (int j = 0; j < BATCH; ++j) {
-                const int i = i0 + j * THREADS + threadIdx.x, at = i < n_el ? i / group : 0;
+                const int i = i0 + j * RT + threadIdx.x, at = i < n_el ? i / group : 0;
                 col[j] = static_cast<long long>(sh.near[at]) * group + (i & (group - 1));
                 x[j] = stored(z, sh.near_max[at], col[j] < p.V ? col[j] : 0, e[j]);
                 if (i >= n_el || col[j] >= p.V) x[j] = -INFINITY;
@@ -745,21 +752,21 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
     __syncthreads();
     int kept;
     if (n_near <= CAP && sh.n_cand <= CAP) {
-        kept = settle_close(p, h, r, sh, sh.n_cand, eps);
+        kept = settle_close(p, h, r, sh, sh.n_cand, eps, rel);
     } else {
         if (warp < 2) exact_one(p, h, r, sh, warp);
         // many logits within the error of the k-th.  A row of zeros has them all equal: ids 0, 1, ...
         bool nz = false;
-        for (int i = threadIdx.x; i < p.d; i += THREADS) nz |= static_cast<float>(h[i]) != 0.f;
+        for (int i = threadIdx.x; i < p.d; i += RT) nz |= static_cast<float>(h[i]) != 0.f;
         if (!__syncthreads_or(nz ? 1 : 0)) {
             kept = p.k < p.V ? p.k : p.V;
-            for (int i = threadIdx.x; i < kept; i += THREADS) { sh.z_keep[i] = 0.0; sh.id_keep[i] = i; }
+            for (int i = threadIdx.x; i < kept; i += RT) { sh.z_keep[i] = 0.0; sh.id_keep[i] = i; }
             __syncthreads();
         } else {
             // otherwise batch by batch, one group per warp and step, the k best so far carried along
             kept = 0;
             int n = 0;
-            for (int g0 = 0; g0 < p.n_g; g0 += WARPS) {
+            for (int g0 = 0; g0 < p.n_g; g0 += RW) {
                 if (threadIdx.x == 0) sh.n_cand = n;
                 __syncthreads();
                 const int gi = g0 + warp;
@@ -773,10 +780,10 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
                 }
                 __syncthreads();
                 n = sh.n_cand;
-                const bool last = g0 + WARPS >= p.n_g;
-                if (n > CAP - WARPS * 64 || last) {
+                const bool last = g0 + RW >= p.n_g;
+                if (n > CAP - RW * 64 || last) {
                     kept = settle(p, h, sh, kept, n);
-                    for (int i = threadIdx.x; i < kept; i += THREADS) { sh.z[i] = sh.z_keep[i]; sh.id[i] = sh.id_keep[i]; }
+                    for (int i = threadIdx.x; i < kept; i += RT) { sh.z[i] = sh.z_keep[i]; sh.id[i] = sh.id_keep[i]; }
                     n = kept;
                 }
                 __syncthreads();
@@ -786,7 +793,7 @@ __global__ void __launch_bounds__(THREADS) row_kernel(const RowParams<TI, TZ> p)
         __syncthreads();
     }
     const float lse = sh.lse;
-    for (int i = threadIdx.x; i < p.k; i += THREADS) {
+    for (int i = threadIdx.x; i < p.k; i += RT) {
         ids_out[i] = i < kept ? sh.id_keep[i] : -1;
         lp_out[i] = i < kept ? static_cast<float>(sh.z_keep[i] - static_cast<double>(lse)) : -INFINITY;
     }

@@ -247,6 +247,17 @@ __global__ void __launch_bounds__(THREADS) merge_kernel(const MergeParams<TI> p)
     if (lane == 0) { p.m1[r] = m; p.l1[r] = l; }
 }
 
+__device__ __forceinline__ float block_max(float x, float* red) {
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
+    __syncthreads();
+    x = red[0];
+#pragma unroll
+    for (int i = 1; i < WARPS; ++i) x = fmaxf(x, red[i]);
+    return x;
+}
 __device__ __forceinline__ float block_sum(float x, float* red) {
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
@@ -292,7 +303,7 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(void* zs, long long ldz, co
     const bool there = i < lists.k && lists.entry(t, i, id, lp);
     if (there) z_i = zr[i];
     if (lists.renorm) {
-        const float m = lp::block_max(there ? lp : -INFINITY, s_red);
+        const float m = block_max(there ? lp : -INFINITY, s_red);
         const float l = block_sum(there ? expf(lp - m) : 0.f, s_red);
         if (there) lp = lp - m - logf(l);
     }
