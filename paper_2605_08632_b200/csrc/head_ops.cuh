@@ -43,9 +43,12 @@ int skinny_tile_rows(long long V) {
     return best;
 }
 
-template <int TPW, int HALVES>
-int launch_skinny_as(const CUtensorMap& tmW, const CUtensorMap& tmH, const skinny::Params& p, int* status, int grid, cudaStream_t st) {
-    auto kern = skinny::logits_kernel<TPW, HALVES>;
+template <int TPW, int HALVES, int SUB>
+int launch_skinny_as(const CUtensorMap& tmW, const CUtensorMap& tmH, const skinny::Params& plan, int* status, int grid, cudaStream_t st) {
+    skinny::Params p = plan;
+    p.stages = (skinny::SMEM_BYTES - 1024 - 8192) / ((SUB * p.tile_rows + p.n) * tc::BK * 2);
+    if (p.stages > skinny::MAX_STAGES) p.stages = skinny::MAX_STAGES;
+    auto kern = skinny::logits_kernel<TPW, HALVES, SUB>;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, skinny::SMEM_BYTES) != cudaSuccess) {
         cudaGetLastError();
         return CAT_ERR_CUDA;
@@ -73,8 +76,6 @@ int launch_skinny(const cat_shape* s, const LpPlan& plan, const void* H, const v
     p.tile_rows = skinny_tile_rows(s->V);
     p.n_tiles = static_cast<int>(cdiv(s->V, p.tile_rows));
     p.num_kb = static_cast<int>(cdiv(s->d, tc::BK));
-    p.stages = (skinny::SMEM_BYTES - 1024 - 8192) / ((p.tile_rows + p.n) * tc::BK * 2);
-    if (p.stages > skinny::MAX_STAGES) p.stages = skinny::MAX_STAGES;
     p.wait_ns = tc::WAIT_LIMIT_NS;
     CUtensorMap tmW, tmH;
     if (tmap_k_major(&tmW, W, s->V, s->d, s->ldW, p.tile_rows) != CAT_OK) return CAT_ERR_CUDA;
@@ -83,9 +84,9 @@ int launch_skinny(const cat_shape* s, const LpPlan& plan, const void* H, const v
     if (p.n_tiles < grid) grid = p.n_tiles;
     *n_parts = grid;
     int* status = reinterpret_cast<int*>(ws);
-    if (s->T <= 32) return launch_skinny_as<32, 1>(tmW, tmH, p, status, grid, st);
-    if (s->T <= 64) return launch_skinny_as<32, 2>(tmW, tmH, p, status, grid, st);
-    return launch_skinny_as<64, 2>(tmW, tmH, p, status, grid, st);
+    if (s->T <= 32) return launch_skinny_as<32, 1, 1>(tmW, tmH, p, status, grid, st);
+    if (s->T <= 64) return launch_skinny_as<32, 2, 2>(tmW, tmH, p, status, grid, st);
+    return launch_skinny_as<64, 2, 2>(tmW, tmH, p, status, grid, st);
 }
 
 LpPlan plan_lp(const cat_shape* s, int top_k) {
@@ -149,8 +150,18 @@ int launch_lp_rows(const cat_shape* s, const LpPlan& plan, const TI* H, const TI
         rp.top_ids = reinterpret_cast<long long*>(top_ids) + r0 * top_k;
         rp.top_logp = top_logp + r0 * top_k;
     }
-    lp::row_kernel<TI, TZ, TOP><<<static_cast<unsigned>(rws), lp::RT, 0, st>>>(rp);
-    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+    // launched ahead of the logits kernel's end, for which it waits: a decoding step is short enough for the 2 us to show
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(rws), 1, 1);
+    cfg.blockDim = dim3(lp::RT, 1, 1);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, lp::row_kernel<TI, TZ, TOP>, rp) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
+    return CAT_OK;
 }
 
 template <bool TOP>

@@ -588,6 +588,7 @@ __global__ void __launch_bounds__(RT, 8) row_kernel(const RowParams<TI, TZ> p) {
     __shared__ Shared sh;
     const long long r = blockIdx.x;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    asm volatile("griddepcontrol.wait;" ::: "memory");      // the logits kernel has finished (it may have been launched ahead of that)
     if (p.valid != nullptr && p.valid[r] == 0) {
         if (threadIdx.x == 0) {
             p.lse[r] = 0.f;

@@ -48,8 +48,9 @@ struct Params {
     unsigned long long wait_ns;
 };
 
-// TPW: hidden states a warp looks after; HALVES: sets of four epilogue warps (HALVES * TPW >= T).
-template <int TPW, int HALVES>
+// TPW: hidden states a warp looks after; HALVES: sets of four epilogue warps (HALVES * TPW >= T); SUB: W tiles that a slice of H is
+// loaded for.  With many rows the slices of H take as much of the ring as those of W; two tiles per slice of H leave more of it to W.
+template <int TPW, int HALVES, int SUB>
 __global__ void __launch_bounds__(64 + 128 * HALVES, 1)
 logits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmH, const Params p, int* status) {
     constexpr int COLS = TPW * HALVES;                       // accumulator columns (a power of two >= 32)
@@ -64,7 +65,7 @@ logits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
     // the slot of a W slice holds its tile_rows rows; the MMA reads 128, the last ones out of whatever follows, into accumulator
     // lanes that nobody looks at (the last slot is followed by 8 KB of slack)
     const uint32_t a_bytes = static_cast<uint32_t>(p.tile_rows) * BK * 2;
-    const uint32_t stage_bytes = a_bytes + b_bytes;
+    const uint32_t stage_bytes = SUB * a_bytes + b_bytes;
     if (threadIdx.x == 0) {
         ptx::prefetch_tmap(&tmW);
         ptx::prefetch_tmap(&tmH);
@@ -81,7 +82,7 @@ logits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
         ptx::fence_mbar_init();
     }
     if (warp == 1) {
-        ptx::tmem_alloc<2 * COLS>(ptx::smem_u32(&ctl.tmem_base));
+        ptx::tmem_alloc<2 * SUB * COLS>(ptx::smem_u32(&ctl.tmem_base));
         ptx::tmem_relinquish();
     }
     ptx::tc_fence_before();
@@ -95,13 +96,15 @@ logits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
             int stage = 0, issued = 0;
             uint32_t phase = 0;
             bool ok = true;
-            for (int t = blockIdx.x; t < p.n_tiles && ok; t += gridDim.x) {
+            for (int t = blockIdx.x; t < p.n_tiles && ok; t += SUB * gridDim.x) {
                 for (int kb = 0; kb < p.num_kb; ++kb) {
                     if (!tc::wait_bounded(ptx::smem_u32(&ctl.empty[stage]), phase ^ 1u, abort, status, p.wait_ns)) { ok = false; break; }
                     const uint32_t full = ptx::smem_u32(&ctl.full[stage]), dst = ring + stage * stage_bytes;
-                    ptx::mbar_arrive_expect_tx(full, stage_bytes);
-                    ptx::tma_load_2d(dst, &tmW, kb * BK, t * p.tile_rows, full);
-                    ptx::tma_load_2d(dst + a_bytes, &tmH, kb * BK, 0, full);
+                    const int n_sub = SUB == 1 || t + static_cast<int>(gridDim.x) >= p.n_tiles ? 1 : SUB;      // the last round may have one tile
+                    ptx::mbar_arrive_expect_tx(full, n_sub * a_bytes + b_bytes);
+                    for (int j = 0; j < n_sub; ++j)
+                        ptx::tma_load_2d(dst + j * a_bytes, &tmW, kb * BK, (t + j * static_cast<int>(gridDim.x)) * p.tile_rows, full);
+                    ptx::tma_load_2d(dst + SUB * a_bytes, &tmH, kb * BK, 0, full);
                     ++issued;
                     if (++stage == p.stages) { stage = 0; phase ^= 1u; }
                 }
@@ -121,16 +124,19 @@ logits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
             int stage = 0;
             uint32_t phase = 0, acc = 0, acc_phase = 0;
             bool ok = true;
-            for (int t = blockIdx.x; t < p.n_tiles && ok; t += gridDim.x) {
+            for (int t = blockIdx.x; t < p.n_tiles && ok; t += SUB * gridDim.x) {
                 if (!tc::wait_bounded(ptx::smem_u32(&ctl.tempty[acc]), acc_phase ^ 1u, abort, status, p.wait_ns)) { ok = false; break; }
                 ptx::tc_fence_after();
                 for (int kb = 0; kb < p.num_kb; ++kb) {
                     if (!tc::wait_bounded(ptx::smem_u32(&ctl.full[stage]), phase, abort, status, p.wait_ns)) { ok = false; break; }
                     ptx::tc_fence_after();
                     const uint32_t at = ring + stage * stage_bytes;
-                    const uint64_t ad = ptx::smem_desc_sw128(at, 16, 1024), bd = ptx::smem_desc_sw128(at + a_bytes, 16, 1024);
+                    const uint64_t ad = ptx::smem_desc_sw128(at, 16, 1024), bd = ptx::smem_desc_sw128(at + SUB * a_bytes, 16, 1024);
+                    const int n_sub = SUB == 1 || t + static_cast<int>(gridDim.x) >= p.n_tiles ? 1 : SUB;
+                    for (int i = 0; i < n_sub; ++i)
 #pragma unroll
-                    for (int j = 0; j < BK / 16; ++j) ptx::umma_bf16(tmem + acc * COLS, ad + 2 * j, bd + 2 * j, idesc, (kb | j) != 0 ? 1u : 0u);
+                        for (int j = 0; j < BK / 16; ++j)
+                            ptx::umma_bf16(tmem + (acc * SUB + i) * COLS, ad + i * (a_bytes >> 4) + 2 * j, bd + 2 * j, idesc, (kb | j) != 0 ? 1u : 0u);
                     ptx::umma_commit(ptx::smem_u32(&ctl.empty[stage]));
                     if (++stage == p.stages) { stage = 0; phase ^= 1u; }
                 }
@@ -156,44 +162,46 @@ logits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
         for (int i = 0; i < TPW / 32; ++i) { sums[i].clear(); id[i] = 0; }
         uint32_t acc = 0, acc_phase = 0;
         bool ok = true;
-        for (int t = blockIdx.x; t < p.n_tiles; t += gridDim.x) {
+        for (int t0 = blockIdx.x; t0 < p.n_tiles; t0 += SUB * gridDim.x) {
             ok = tc::wait_bounded(ptx::smem_u32(&ctl.tfull[acc]), acc_phase, abort, status, p.wait_ns);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             ptx::tc_fence_after();
-            const int v0 = t * p.tile_rows + quarter * 32;
-            const bool in_tile = quarter * 32 < p.tile_rows && v0 < p.V;        // the warp has vocabulary entries
+            for (int j = 0, t = t0; j < SUB && t < p.n_tiles; ++j, t += gridDim.x) {
+                const int v0 = t * p.tile_rows + quarter * 32;
+                const bool in_tile = quarter * 32 < p.tile_rows && v0 < p.V;        // the warp has vocabulary entries
 #pragma unroll
-            for (int c = 0; c < TPW / 32; ++c) {
-                const int tok = tok0 + c * 32;
-                if (!in_tile || tok >= p.T) continue;
-                uint32_t raw[32];
-                ptx::tmem_ld_32x32(lanes + acc * COLS + tok, raw);
-                ptx::tmem_ld_wait();
-                __syncwarp();
+                for (int c = 0; c < TPW / 32; ++c) {
+                    const int tok = tok0 + c * 32;
+                    if (!in_tile || tok >= p.T) continue;
+                    uint32_t raw[32];
+                    ptx::tmem_ld_32x32(lanes + (acc * SUB + j) * COLS + tok, raw);
+                    ptx::tmem_ld_wait();
+                    __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) turn[i * 33 + lane] = __uint_as_float(raw[i]);
-                __syncwarp();
-                float f[32];
+                    for (int i = 0; i < 32; ++i) turn[i * 33 + lane] = __uint_as_float(raw[i]);
+                    __syncwarp();
+                    float f[32];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) f[i] = turn[lane * 33 + i];
-                const int live = p.V - v0;
-                if (live < 32) {
+                    for (int i = 0; i < 32; ++i) f[i] = turn[lane * 33 + i];
+                    const int live = p.V - v0;
+                    if (live < 32) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (i >= live) f[i] = tc::LP_LOW;
-                }
-                const float g = tc::max_of(f);
-                if (g > sums[c].m) id[c] = v0 + tc::first_at(f, g);
-                sums[c].add(f, g);
-                if (p.gmax != nullptr && tok + lane < p.T) {
-                    p.gmax[static_cast<long long>(tok + lane) * p.ld_g + (v0 >> 5)] = g;
-                    // the pitch covers whole groups of 32 columns, so the last one may be written past the vocabulary
-                    uint4* out = reinterpret_cast<uint4*>(p.zs + static_cast<long long>(tok + lane) * p.ldz + v0);
+                        for (int i = 0; i < 32; ++i)
+                            if (i >= live) f[i] = tc::LP_LOW;
+                    }
+                    const float g = tc::max_of(f);
+                    if (g > sums[c].m) id[c] = v0 + tc::first_at(f, g);
+                    sums[c].add(f, g);
+                    if (p.gmax != nullptr && tok + lane < p.T) {
+                        p.gmax[static_cast<long long>(tok + lane) * p.ld_g + (v0 >> 5)] = g;
+                        // the pitch covers whole groups of 32 columns, so the last one may be written past the vocabulary
+                        uint4* out = reinterpret_cast<uint4*>(p.zs + static_cast<long long>(tok + lane) * p.ldz + v0);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        out[q] = make_uint4(ptx::pack_f16x2_sat(f[q * 8 + 0] - g, f[q * 8 + 1] - g), ptx::pack_f16x2_sat(f[q * 8 + 2] - g, f[q * 8 + 3] - g),
-                                            ptx::pack_f16x2_sat(f[q * 8 + 4] - g, f[q * 8 + 5] - g), ptx::pack_f16x2_sat(f[q * 8 + 6] - g, f[q * 8 + 7] - g));
+                        for (int q = 0; q < 4; ++q)
+                            out[q] = make_uint4(ptx::pack_f16x2_sat(f[q * 8 + 0] - g, f[q * 8 + 1] - g), ptx::pack_f16x2_sat(f[q * 8 + 2] - g, f[q * 8 + 3] - g),
+                                                ptx::pack_f16x2_sat(f[q * 8 + 4] - g, f[q * 8 + 5] - g), ptx::pack_f16x2_sat(f[q * 8 + 6] - g, f[q * 8 + 7] - g));
+                    }
                 }
             }
             ptx::tc_fence_before();
@@ -235,7 +243,7 @@ logits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
     __syncthreads();
     if (warp == 1) {
         ptx::tc_fence_after();
-        ptx::tmem_dealloc<2 * COLS>(tmem);
+        ptx::tmem_dealloc<2 * SUB * COLS>(tmem);
     }
 }
 
