@@ -67,7 +67,7 @@ class CatLoss:
         self.ws_bwd = torch.empty(nb, dtype=torch.uint8, device=dev)
         self._ws_fused = None
         self._ws_kd = None
-        self._ws_topk = None
+        self._ws_topk = self._topk_need = None      # workspace, and (k, its size)
         self.loss3 = None
         self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
         self.lse = torch.empty(T, dtype=torch.float32, device=dev)
@@ -155,8 +155,11 @@ class CatLoss:
             if t is not None:
                 _check(name, t, shape, dtype, dev)
         desc = B.make_topk_kd_desc(L, k, float(beta), renormalize, ld=_pitch(top_ids))
-        n = B.cat_topk_kd_workspace_bytes(self.shape, desc)
+        if self._topk_need is None or self._topk_need[0] != k or not 0.0 <= desc.beta < float("inf"):
+            self._topk_need = (k, B.cat_topk_kd_workspace_bytes(self.shape, desc))
+        n = self._topk_need[1]
         if n == 0:
+            self._topk_need = None
             raise ValueError("invalid problem for cat_topk_kd_loss_fwd_bwd")
         with torch.cuda.device(dev):
             if self._ws_topk is None or self._ws_topk.numel() < n:
@@ -326,6 +329,7 @@ class _LogProbFn(torch.autograd.Function):
         return logp, entropy.clone(), ids, tl
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, g_logp, g_entropy, _ids, _tl):
         H, W, labels, valid, lse, entropy = ctx.saved_tensors
         e = ctx.engine
@@ -339,7 +343,8 @@ class _LogProbFn(torch.autograd.Function):
 class LogProbModule(torch.nn.Module):
     """Head of a scoring or policy-gradient loop: `logp, entropy, top_ids, top_logp = head(H, labels, valid)` with H [T, d] and
     `weight` [V, d] as the LM head; logp and entropy carry gradients to H and the weight.  The gradient of the weight is formed in
-    the weight's type.  One engine is kept per distinct T."""
+    the weight's type.  One engine is kept per distinct T.  Not for stream capture with gradients: autograd may then wait for other
+    streams inside the capture; capture TokenLogProb.forward and backward instead."""
 
     def __init__(self, weight: torch.Tensor, top_k: int = 0, slab_mib: int = 0):
         super().__init__()
@@ -349,6 +354,8 @@ class LogProbModule(torch.nn.Module):
         self._engines = {}
 
     def forward(self, H, labels=None, valid=None):
+        if torch.is_grad_enabled() and (H.requires_grad or self.weight.requires_grad) and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("LogProbModule cannot be captured with gradients: capture TokenLogProb.forward and backward")
         T, d = H.shape
         key = (T, H.device, H.dtype)
         eng = self._engines.get(key)

@@ -389,7 +389,7 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
             f32::gemm_kernel<f32::FWD, true, true><<<dim3(static_cast<unsigned>(cdiv(rws, f32::TM)), static_cast<unsigned>(S)), f32::THREADS, 0, st>>>(op, ep);
             mp.part_m = part_m; mp.part_l = part_l; mp.part_id = nullptr; mp.part_stride = rws;
         }
-        mp.S = S; mp.H = Hs; mp.W = W; mp.ldH = s->ldH; mp.ldW = s->ldW; mp.d = d; mp.labels = y + r0; mp.valid = ok + r0;
+        mp.S = S; mp.H = Hs; mp.W = W; mp.ldH = s->ldH; mp.ldW = s->ldW; mp.d = d; mp.V = V; mp.labels = y + r0; mp.valid = ok + r0;
         mp.z_exact = zt + lists.k; mp.ld_exact = plan.ld_zt; mp.z_label = z_label + r0; mp.m1 = m1 + r0; mp.l1 = l1 + r0;
         mp.rows = static_cast<int>(rws);
         tk::merge_kernel<TI><<<static_cast<unsigned>(cdiv(rws, tk::WARPS)), tk::THREADS, 0, st>>>(mp);

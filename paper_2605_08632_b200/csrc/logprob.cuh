@@ -674,6 +674,7 @@ __global__ void __launch_bounds__(RT, 8) row_kernel(const RowParams<TI, TZ> p) {
             l += __shfl_xor_sync(0xffffffffu, l, off);
             u += __shfl_xor_sync(0xffffffffu, u, off);
         }
+        if (static_cast<unsigned>(id) >= static_cast<unsigned>(p.V)) id = 0;      // a logits kernel that timed out leaves anything here
         prefetch_row(p.W + static_cast<long long>(id) * p.ldW, p.d, lane);
         if (lane == 0) {
             sh.m = m; sh.l = l; sh.u = u;

@@ -203,7 +203,7 @@ struct MergeParams {
     const TI* H;
     const TI* W;
     long long ldH, ldW;
-    int d;
+    int d, V;
     const long long* labels;
     const unsigned char* valid;
     const float* z_exact;          // [rows] at pitch ld_exact: the label's logit, of rows that take part
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(THREADS) merge_kernel(const MergeParams<TI> p)
     for (int off = 16; off > 0; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
     if (p.valid[r]) {
         const float zy = p.z_exact[r * p.ld_exact];
-        if (p.part_id) {
+        if (p.part_id && static_cast<unsigned>(id) < static_cast<unsigned>(p.V)) {      // a GEMM that timed out leaves anything here
             const bool is_label = p.labels[r] == id;
             const float z = is_label ? zy : lp::warp_dot_f32(p.H + r * p.ldH, p.W + id * p.ldW, p.d, lane);
             if (fabsf(z - m) < 1.f) l += expm1f(z - m);

@@ -260,6 +260,77 @@ def test_streams_graphs_and_repeatability():
     check_forward(r, H2, W.cpu(), y.cpu(), valid.cpu(), k, True)
 
 
+def test_nothing_to_do_and_no_gradient():
+    T, d, V, k = 40, 64, 500, 4
+    for dtype in (BF, F32):
+        H, W, y, valid = (t.to(DEV) for t in make(T, d, V, dtype))
+        e = TokenLogProb(T, d, V, k, dtype=dtype)
+        r = e.forward(H, W, y, torch.zeros_like(valid))
+        assert not r.logp.any() and not r.lse.any() and not r.entropy.any()
+        assert bool((r.top_ids == -1).all()) and bool(torch.isneginf(r.top_logp).all())
+        g = torch.ones(T, device=DEV)
+        dH, dW = e.backward(H, W, y, torch.zeros_like(valid), g, g)
+        assert not dH.any() and not dW.any()
+        e.forward(H, W, y, valid)
+        dH, dW = e.backward(H, W, None, valid)
+        assert not dH.any() and not dW.any()
+
+
+def test_offsets_past_31_bits():
+    """A slab of more than 2^31 logits: the rows at its end against the oracle."""
+    T, d, V, k = 13500, 64, 160001, 3
+    H, W, y, _ = make(T, d, V, BF, sure=0.0)
+    y = y.clamp(max=V - 1)
+    e = TokenLogProb(T, d, V, k, slab_mib=8192)
+    r = e.forward(H.to(DEV), W.to(DEV), y.to(DEV))
+    rows = slice(T - 40, T)
+    part = type(r)(r.logp[rows], r.lse[rows], r.entropy[rows], r.top_ids[rows], r.top_logp[rows])
+    check_forward(part, H[rows], W, y[rows], None, k, True)
+    g = torch.zeros(T)
+    g[rows] = 1.0
+    dH, _ = e.backward(H.to(DEV), W.to(DEV), y.to(DEV), None, g.to(DEV))
+    ref = O.logprob_backward(H[rows], W, y[rows], None, np.ones(40))
+    assert not dH[: T - 40].any()
+    assert np.linalg.norm(np64(dH[rows]) - ref[0]) <= 2 * 2.0 ** -8 * np.linalg.norm(ref[0])
+
+
+def test_pitched_gradients_leave_the_gaps_alone():
+    T, d, V = 300, 72, 1000
+    for dtype, wdt in ((BF, BF), (BF, F32), (F32, F32)):
+        H, W, y, valid = make(T, d, V, dtype)
+        code = {BF: B.CAT_BF16, F32: B.CAT_F32}
+        ldH, ldW = d + 24, d + 8
+        shape = B.make_shape(T, d, V, 1, code[dtype], code[wdt], ldH=ldH, ldW=ldW)
+        wH, wW = torch.full((T, ldH), float("nan"), dtype=dtype, device=DEV), torch.full((V, ldW), float("nan"), dtype=dtype, device=DEV)
+        wH[:, :d], wW[:, :d] = H.to(DEV), W.to(DEV)
+        gl = torch.randn(T, device=DEV)
+        e = TokenLogProb(T, d, V, dtype=dtype, dW_dtype=wdt)
+        r = e.forward(H.to(DEV), W.to(DEV), y.to(DEV), valid.to(DEV))
+        dH, dW = e.backward(H.to(DEV), W.to(DEV), y.to(DEV), valid.to(DEV), gl, gl)
+        pH, pW = torch.full((T, ldH), 7.0, dtype=dtype, device=DEV), torch.full((V, ldW), 7.0, dtype=wdt, device=DEV)
+        ws = torch.empty(B.cat_logprob_workspace_bytes(shape, 0, 1), dtype=torch.uint8, device=DEV)
+        B.cat_logprob_bwd(shape, wH, wW, y.to(DEV), valid.to(DEV), r.lse, r.entropy, gl, gl, pH, pW, False, ws)
+        assert torch.equal(pH[:, :d], dH) and torch.equal(pW[:, :d], dW)
+        assert bool((pH[:, d:] == 7.0).all()) and bool((pW[:, d:] == 7.0).all())
+
+
+def test_two_engines_on_two_streams():
+    T, d, V, k = 64, 256, 20000, 8
+    a, b = make(T, d, V, BF, seed=1), make(T, d, V, BF, seed=2)
+    x, z = [t.to(DEV) for t in a], [t.to(DEV) for t in b]
+    e, f = TokenLogProb(T, d, V, k), TokenLogProb(T, d, V, k)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(20):
+        with torch.cuda.stream(s1):
+            r = e.forward(*x)
+        with torch.cuda.stream(s2):
+            q = f.forward(*z)
+    torch.cuda.synchronize()
+    check_forward(r, *a, k, True)
+    check_forward(q, *b, k, True)
+
+
 def test_module_gradients():
     T, d, V = 50, 64, 900
     H, W, y, valid = make(T, d, V, F32, sure=0.0)
@@ -273,6 +344,11 @@ def test_module_gradients():
     assert np.linalg.norm(np64(h.grad) - dH) <= 1e-5 * np.linalg.norm(dH)
     assert np.linalg.norm(np64(head.weight.grad) - dW) <= 1e-5 * np.linalg.norm(dW)
     assert not ids.requires_grad and not tl.requires_grad
+    on_dev = y.to(DEV), valid.to(DEV)
+    graph = torch.cuda.CUDAGraph()
+    with pytest.raises(RuntimeError, match="captured"):
+        with torch.cuda.graph(graph):
+            head(h, *on_dev)
     h.grad = None
     head(h, None, valid.to(DEV))[1].sum().backward()             # without labels: the entropy alone
     dH, *_ = O.logprob_backward(H, W, None, valid, None, np.ones(T))

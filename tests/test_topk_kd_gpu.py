@@ -168,6 +168,42 @@ def test_pitched_lists_and_refusals():
         eng.topk_kd_forward_backward(*g, beta=-1.0)
 
 
+def test_pitched_rows_leave_the_gaps_alone():
+    T, K, d, V, k = 264, 8, 72, 900, 5
+    for dtype, wdt in ((BF, BF), (BF, F32), (F32, F32)):
+        H, W, y, valid, ids, tl, start = (t.to(DEV) for t in make(T, K, d, V, k, dtype))
+        eng = CatLoss(T, d, V, K, dtype=dtype, dW_dtype=wdt)
+        loss3, dH, dW = eng.topk_kd_forward_backward(H, W, y, valid, ids, tl, start)
+        code = {BF: B.CAT_BF16, F32: B.CAT_F32}
+        ldH, ldW = d + 24, d + 8
+        shape = B.make_shape(T, d, V, K, code[dtype], code[wdt], ldH=ldH, ldW=ldW)
+        desc = B.make_topk_kd_desc(ids.shape[0], k, 0.1)
+        wH, wW = torch.full((T, ldH), float("nan"), dtype=dtype, device=DEV), torch.full((V, ldW), float("nan"), dtype=dtype, device=DEV)
+        wH[:, :d], wW[:, :d] = H, W
+        pH, pW = torch.full((T, ldH), 7.0, dtype=dtype, device=DEV), torch.full((V, ldW), 7.0, dtype=wdt, device=DEV)
+        n = B.cat_topk_kd_workspace_bytes(shape, desc)
+        ws = torch.full((n + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+        out = [torch.empty(3, device=DEV)] + [torch.empty(T, device=DEV) for _ in range(3)]
+        B.cat_topk_kd_loss_fwd_bwd(shape, desc, wH, wW, y, valid, ids, tl, start, None, None, *out, None, pH, pW, False, ws[:n])
+        assert torch.equal(out[0], loss3) and torch.equal(pH[:, :d], dH) and torch.equal(pW[:, :d], dW)
+        assert bool((pH[:, d:] == 7.0).all()) and bool((pW[:, d:] == 7.0).all()) and bool((ws[n:] == 0xA5).all())
+
+
+def test_offsets_past_31_bits():
+    """A slab of more than 2^31 logits: the blocks at its end against the oracle."""
+    T, K, d, V, k = 13504, 8, 64, 160001, 3
+    H, W, y, valid, ids, tl, start = make(T, K, d, V, k, BF)
+    eng = CatLoss(T, d, V, K, slab_mib=8192)
+    loss3, dH, _ = run(eng, H, W, y, valid, ids, tl, start, beta=0.3)
+    rows = slice(T - 40, T)
+    ref = O.topk_kd(H[rows], W, y[rows], valid[rows], K, ids, tl, start[-5:], beta=0.3)
+    n = eng.fwd_stats().n_valid
+    want = ref["dH"] * ref["n_valid"] / n
+    # roundings of dz and of the result (2^-8 each), of z - ref (2^-11 of at most about 16, on the smaller part of dz)
+    assert np.linalg.norm(np64(dH[rows]) - want) <= (2 * 2.0 ** -8 + 2.0 ** -7) * np.linalg.norm(want)
+    assert np.abs(np64(eng.lse[rows]) - ref["lse"])[ref["ok"]].max() <= 1e-4
+
+
 def test_repeatable_captured_and_on_another_stream():
     T, K, d, V, k = 256, 8, 128, 4000, 16
     x = [t.to(DEV) for t in make(T, K, d, V, k, BF)]
