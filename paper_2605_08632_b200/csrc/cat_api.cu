@@ -561,24 +561,33 @@ int dh_parts(long long rows, long long d, long long V) {
     }
     return best;
 }
-size_t dh_part_bytes(long long rows, long long d, long long V) {
+size_t dh_part_bytes(long long rows, long long d, long long V, bool two_terms = false) {
     const int g = dh_parts(rows, d, V);
-    return g > 1 ? align256(static_cast<size_t>(g) * cdiv(rows, tile_m()) * tile_m() * d * 4) : 0;
+    return g > 1 || two_terms ? align256(static_cast<size_t>(g) * cdiv(rows, tile_m()) * tile_m() * d * 4) : 0;
 }
+// Batches of up to this many rows hand dz to the contractions as two bf16 terms, dz = hi + lo, rows r and lo_rows + r.  The gradient of a
+// few rows is a few entries of dz (a row's label, its list's first entries), and the rounding of one such entry to bf16, up to 2^-8,
+// would be the error of whole rows of dW; in larger batches many independent roundings average out.  Both terms fit the row tile and
+// the k-slices that so few rows leave mostly empty, so they cost next to nothing.
+constexpr long long kTwoTermRows = 128;
+long long lo_rows_of(long long T) { return T <= kTwoTermRows ? cdiv(T, 32) * 32 : 0; }
+
 double dh_waves(long long rows, long long d, long long V) {
     const int g = dh_parts(rows, d, V);
     return static_cast<double>(cdiv(cdiv(rows, tile_m()) * cdiv(d, tc::BN) * g, plan_workers())) / g;
 }
 
 // dH = scale * dz W over the whole vocabulary: dz [rows, V] (K-major map tmZ), W (MN-major map tmW); `part`: dh_part_bytes of scratch.
+// lo > 0: dz comes as two bf16 terms, rows r and lo + r (see kTwoTermRows); their products are added in fp32.
 int launch_dh(const CUtensorMap& tmZ, const CUtensorMap& tmW, long long rows, long long d, long long V, const float* scale,
-              __nv_bfloat16* dH, long long ldH, float* part, int* status, int sm_count, cudaStream_t st) {
-    const int g = dh_parts(rows, d, V);
-    tc::Sched sched = make_sched(rows, d, V, 0, 1, 1);
+              __nv_bfloat16* dH, long long ldH, float* part, int* status, int sm_count, cudaStream_t st, long long lo = 0) {
+    const long long all = lo > 0 ? 2 * lo : rows;
+    const int g = dh_parts(all, d, V);
+    tc::Sched sched = make_sched(all, d, V, 0, 1, 1);
     tc::EpiOut::Params ep;
     memset(&ep, 0, sizeof(ep));
     ep.N = static_cast<int>(d);
-    if (g == 1) {
+    if (g == 1 && lo == 0) {
         ep.alpha = scale; ep.M = static_cast<int>(rows); ep.out_bf16 = dH; ep.ld_out = ldH;
         return launch_out<0, 1>(tmZ, tmW, sched, ep, status, sm_count, st);
     }
@@ -589,7 +598,7 @@ int launch_dh(const CUtensorMap& tmZ, const CUtensorMap& tmW, long long rows, lo
     ep.M = static_cast<int>(padded * g); ep.out_f32 = part; ep.ld_out = d;
     const int rc = launch_out<0, 1>(tmZ, tmW, sched, ep, status, sm_count, st);
     if (rc != CAT_OK) return rc;
-    lp::add_parts_kernel<<<static_cast<unsigned>(rows), lp::THREADS, 0, st>>>(part, g, padded * d, static_cast<int>(d), scale, dH, ldH);
+    lp::add_parts_kernel<<<static_cast<unsigned>(rows), lp::THREADS, 0, st>>>(part, g, padded * d, static_cast<int>(d), scale, dH, ldH, lo);
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
 
@@ -1025,23 +1034,10 @@ int cat_loss_fwd(const cat_shape* shape, const void* H, const void* W, const int
 
 // cat_loss_bwd / cat_loss_bwd_events: `slab_events` (host array of cudaEvent_t, one per vocabulary
 // slab, or NULL) are recorded on the stream as soon as a slab's rows of dW are final.
-// `lp`: the gradients of cat_logprob_bwd instead of the CAT loss's (another dz, no 1/N).
-struct LpArgs {
-    const float* entropy;
-    const float* grad_logp;
-    const float* grad_entropy;
-};
-static size_t lp_bwd_bytes(const cat_shape* s) {       // the plain backward's scratch and a copy of H without its masked rows
-    const BwdPlan p = plan_bwd(s);
-    const bool bf16 = s->in_dtype == CAT_BF16;
-    return align256(p.total) + align256((bf16 ? 2 : 4) * static_cast<size_t>(s->T) * static_cast<size_t>(s->d)) +
-           (!bf16 ? kF32PartBytes : p.n_slabs == 1 ? dh_part_bytes(s->T, s->d, s->V) : 0);
-}
 static int bwd_core(const cat_shape* shape, const void* H, const void* W, const int64_t* labels, const uint8_t* valid,
                     const float* lse, const float* weight, const float* grad_loss, void* dH, void* dW, int accumulate_dW,
-                    void* workspace, size_t workspace_bytes, void* cuda_stream, void* const* slab_events, const LpArgs* lp = nullptr) {
-    if (!shape || !H || !W || !lse || !dH || !dW) return CAT_ERR_NULL;
-    if (lp ? (lp->grad_logp && !labels) || (lp->grad_entropy && !lp->entropy) : !labels || !weight) return CAT_ERR_NULL;
+                    void* workspace, size_t workspace_bytes, void* cuda_stream, void* const* slab_events) {
+    if (!shape || !H || !W || !labels || !lse || !weight || !dH || !dW) return CAT_ERR_NULL;
     const int sc = check_shape(shape);
     if (sc != CAT_OK) return sc;
     const bool bf16 = shape->in_dtype == CAT_BF16;
@@ -1049,9 +1045,8 @@ static int bwd_core(const cat_shape* shape, const void* H, const void* W, const 
     if (misaligned(H, in_al) || misaligned(W, in_al) || misaligned(dH, in_al) || misaligned(dW, 16) || misaligned(labels, 8) ||
         misaligned(lse, 4) || misaligned(weight, 4) || (grad_loss && misaligned(grad_loss, 4)))
         return CAT_ERR_ALIGN;
-    if (lp && (misaligned(lp->entropy, 4) || misaligned(lp->grad_logp, 4) || misaligned(lp->grad_entropy, 4))) return CAT_ERR_ALIGN;
     const BwdPlan plan = plan_bwd(shape);
-    if (!workspace || misaligned(workspace, 256) || workspace_bytes < (lp ? lp_bwd_bytes(shape) : plan.total)) return CAT_ERR_WORKSPACE;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < plan.total) return CAT_ERR_WORKSPACE;
     int sm_count = 0;
     const int dc = check_device(&sm_count);
     if (dc != CAT_OK) return dc;
@@ -1063,26 +1058,15 @@ static int bwd_core(const cat_shape* shape, const void* H, const void* W, const 
     const int T = static_cast<int>(shape->T), V = static_cast<int>(shape->V), d = static_cast<int>(shape->d);
     const long long* y = reinterpret_cast<const long long*>(labels);
 
-    // the right operand of dW: H, or a copy in which masked rows are zero whatever the caller left in them
-    const bool copy_H = lp && valid;
-    const void* Hw = copy_H ? static_cast<const void*>(ws + align256(plan.total)) : H;
-    const long long ldHw = copy_H ? shape->d : shape->ldH;
     // tensor maps that do not depend on the slab
     CUtensorMap tmH_k, tmH_mn;
     if (bf16) {
         if (tmap_a(&tmH_k, H, shape->T, shape->d, shape->ldH) != CAT_OK) return CAT_ERR_CUDA;
-        if (tmap_mn_major(&tmH_mn, Hw, shape->T, shape->d, ldHw) != CAT_OK) return CAT_ERR_CUDA;
+        if (tmap_mn_major(&tmH_mn, H, shape->T, shape->d, shape->ldH) != CAT_OK) return CAT_ERR_CUDA;
     }
     if (cudaMemsetAsync(ws, 0, kHeaderBytes, st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
-    if (!lp) rows::bwd_scale_kernel<<<1, 1024, 0, st>>>(y, valid, T, V, grad_loss, scale);
-    else if (copy_H && bf16)
-        lp::masked_copy_kernel<<<static_cast<unsigned>(T), lp::THREADS, 0, st>>>(
-            static_cast<const __nv_bfloat16*>(H), shape->ldH, d, valid, reinterpret_cast<__nv_bfloat16*>(ws + align256(plan.total)));
-    else if (copy_H)
-        lp::masked_copy_kernel<<<static_cast<unsigned>(T), lp::THREADS, 0, st>>>(
-            static_cast<const float*>(H), shape->ldH, d, valid, reinterpret_cast<float*>(ws + align256(plan.total)));
+    rows::bwd_scale_kernel<<<1, 1024, 0, st>>>(y, valid, T, V, grad_loss, scale);
     if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
-    if (lp) scale = nullptr;
 
     for (int sl = 0; sl < plan.n_slabs; ++sl) {
         const long long v0 = static_cast<long long>(sl) * plan.Vs;
@@ -1101,20 +1085,12 @@ static int bwd_core(const cat_shape* shape, const void* H, const void* W, const 
                 // same item shape as the forward pass: (m-tile, run of vocabulary tiles), so the per-row state
                 // (label, lse, weight) is loaded once per run
                 const tc::Sched sched = make_sched(shape->T, width, shape->d, fwd_splits(shape->T, width), band_tiles(shape->d), 0);
+                tc::EpiDz::Params ep;
+                ep.labels = y; ep.valid = valid; ep.lse = lse; ep.weight = weight; ep.dz = dz; ep.ld = plan.Vs;
+                ep.T = T; ep.V = V; ep.v0 = static_cast<int>(v0);
                 CUtensorMap tmDz_out;
                 if (tmap_out(&tmDz_out, dz, shape->T, width, plan.Vs) != CAT_OK) return CAT_ERR_CUDA;
-                int rc;
-                if (lp) {
-                    tc::EpiDzLp::Params ep;
-                    ep.labels = y; ep.valid = valid; ep.lse = lse; ep.entropy = lp->entropy; ep.grad_logp = lp->grad_logp;
-                    ep.grad_entropy = lp->grad_entropy; ep.T = T; ep.V = V; ep.v0 = static_cast<int>(v0);
-                    rc = launch_tc<0, 0, tc::EpiDzLp>(tmH_k, tmW_k, sched, ep, status, sm_count, st, &tmDz_out);
-                } else {
-                    tc::EpiDz::Params ep;
-                    ep.labels = y; ep.valid = valid; ep.lse = lse; ep.weight = weight; ep.dz = dz; ep.ld = plan.Vs;
-                    ep.T = T; ep.V = V; ep.v0 = static_cast<int>(v0);
-                    rc = launch_tc<0, 0, tc::EpiDz>(tmH_k, tmW_k, sched, ep, status, sm_count, st, &tmDz_out);
-                }
+                const int rc = launch_tc<0, 0, tc::EpiDz>(tmH_k, tmW_k, sched, ep, status, sm_count, st, &tmDz_out);
                 if (rc != CAT_OK) return rc;
             }
             {   // dW[v0 : v0 + width, :] = (g/N) dz^T H
@@ -1133,12 +1109,7 @@ static int bwd_core(const cat_shape* shape, const void* H, const void* W, const 
                 if (rc != CAT_OK) return rc;
                 if (slab_events && cudaEventRecord(static_cast<cudaEvent_t>(slab_events[sl]), st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
             }
-            if (lp && plan.n_slabs == 1) {
-                float* part = reinterpret_cast<float*>(ws + align256(plan.total) + align256(2 * static_cast<size_t>(T) * static_cast<size_t>(d)));
-                const int rc = launch_dh(tmDz_k, tmW_mn, shape->T, shape->d, shape->V, nullptr, static_cast<__nv_bfloat16*>(dH),
-                                         shape->ldH, part, status, sm_count, st);
-                if (rc != CAT_OK) return rc;
-            } else {   // dH (+)= (g/N) dz W[v0 : v0 + width, :]
+            {   // dH (+)= (g/N) dz W[v0 : v0 + width, :]
                 const tc::Sched sched = make_sched(shape->T, shape->d, width, 0, 1, 1);
                 tc::EpiOut::Params ep;
                 memset(&ep, 0, sizeof(ep));
@@ -1154,23 +1125,6 @@ static int bwd_core(const cat_shape* shape, const void* H, const void* W, const 
             const float* Wf = static_cast<const float*>(W) + v0 * shape->ldW;
             float* dz = reinterpret_cast<float*>(ws + plan.off_dz);
             const int w = static_cast<int>(width);
-            if (lp) {
-                float* part = reinterpret_cast<float*>(ws + align256(plan.total) + align256(sizeof(float) * static_cast<size_t>(T) * static_cast<size_t>(d)));
-                f32::Operands op;
-                f32::EpiParams ep;
-                memset(&ep, 0, sizeof(ep));
-                op.A = Hf; op.sAm = shape->ldH; op.sAk = 1; op.B = Wf; op.sBk = 1; op.sBn = shape->ldW;
-                op.M = T; op.N = w; op.Kd = d; op.n_groups = static_cast<int>(cdiv(w, f32::TN));
-                ep.labels = y; ep.valid = valid; ep.lse = lse; ep.entropy = lp->entropy; ep.grad_logp = lp->grad_logp;
-                ep.grad_entropy = lp->grad_entropy; ep.dz = dz; ep.ld_dz = plan.Vs; ep.V = V; ep.v0 = static_cast<int>(v0);
-                f32::gemm_kernel<f32::DZ, true, true><<<dim3(static_cast<unsigned>(cdiv(T, f32::TM)), static_cast<unsigned>(op.n_groups)), f32::THREADS, 0, st>>>(op, ep);
-                if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
-                int rc = launch_f32_dw(dz, plan.Vs, static_cast<const float*>(Hw), ldHw, w, d, T, nullptr,
-                                       static_cast<float*>(dW) + v0 * shape->ldW, shape->ldW, accumulate_dW != 0, part, st);
-                if (rc == CAT_OK) rc = launch_f32_dh(dz, plan.Vs, Wf, shape->ldW, T, d, w, nullptr, static_cast<float*>(dH), shape->ldH, !first, part, st);
-                if (rc != CAT_OK) return rc;
-                continue;
-            }
             {
                 simt::Operands op;
                 op.A = Hf; op.sAm = shape->ldH; op.sAk = 1; op.B = Wf; op.sBk = 1; op.sBn = shape->ldW;

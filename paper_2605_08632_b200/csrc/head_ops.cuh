@@ -212,6 +212,134 @@ int lp_slab(const cat_shape* s, const LpPlan& plan, const CUtensorMap& tmW, cons
                                              entropy, top_ids, top_logp, st);
 }
 
+// ------------------------------------------------------------------------------ gradients of the log probabilities
+// As cat_loss_bwd: the vocabulary in slabs, per slab recomputed logits -> dz, dW of the slab, dH summed over the slabs.
+struct LpBwdPlan {
+    BwdPlan b;
+    long long lo;          // rows before the second terms of dz, or 0
+    size_t off_h, off_part, total;
+};
+
+LpBwdPlan plan_lp_bwd(const cat_shape* s) {
+    LpBwdPlan p;
+    const bool bf16 = s->in_dtype == CAT_BF16;
+    cat_shape t = *s;
+    p.lo = bf16 ? lo_rows_of(s->T) : 0;
+    if (p.lo > 0) {
+        t.T = 2 * p.lo;
+        p.b = plan_bwd(&t);
+        if (p.b.n_slabs > 1) { p.lo = 0; t.T = s->T; }       // a vocabulary of millions, or a small cap on the slab
+    }
+    if (p.lo == 0) p.b = plan_bwd(s);
+    size_t off = align256(p.b.total);
+    p.off_h = off;    off = align256(off + (bf16 ? 2 : 4) * static_cast<size_t>(t.T) * static_cast<size_t>(s->d));
+    p.off_part = off;
+    off += !bf16 ? kF32PartBytes : p.b.n_slabs == 1 ? dh_part_bytes(t.T, s->d, s->V, p.lo > 0) : 0;
+    p.total = off;
+    return p;
+}
+
+struct LpGrads {
+    const int64_t* labels;
+    const uint8_t* valid;
+    const float *lse, *entropy, *grad_logp, *grad_entropy;
+};
+
+int lp_bwd_bf16(const cat_shape* s, const LpBwdPlan& plan, const __nv_bfloat16* H, const __nv_bfloat16* W, const LpGrads& a,
+                __nv_bfloat16* dH, void* dW, int accumulate_dW, uint8_t* ws, int sm_count, cudaStream_t st) {
+    int* status = reinterpret_cast<int*>(ws);
+    __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + plan.b.off_dz);
+    __nv_bfloat16* Hz = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_h);
+    float* dh_acc = reinterpret_cast<float*>(ws + plan.b.off_dh_acc);
+    const int d = static_cast<int>(s->d);
+    const long long rows = plan.lo > 0 ? 2 * plan.lo : s->T;             // of dz
+    const bool copy_H = a.valid != nullptr || plan.lo > 0;
+    if (copy_H) {
+        lp::masked_copy_kernel<<<static_cast<unsigned>(rows), lp::THREADS, 0, st>>>(H, s->ldH, d, a.valid, static_cast<int>(s->T),
+                                                                                   static_cast<int>(plan.lo), Hz);
+        if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
+    }
+    CUtensorMap tmH_k, tmH_mn;
+    if (tmap_a(&tmH_k, H, s->T, s->d, s->ldH) != CAT_OK ||
+        tmap_mn_major(&tmH_mn, copy_H ? Hz : H, rows, s->d, copy_H ? s->d : s->ldH) != CAT_OK)
+        return CAT_ERR_CUDA;
+    for (int sl = 0; sl < plan.b.n_slabs; ++sl) {
+        const long long v0 = static_cast<long long>(sl) * plan.b.Vs;
+        const long long width = (s->V - v0) < plan.b.Vs ? (s->V - v0) : plan.b.Vs;
+        const bool first = sl == 0, last = sl == plan.b.n_slabs - 1;
+        const __nv_bfloat16* Wb = W + v0 * s->ldW;
+        CUtensorMap tmW_k, tmW_mn, tmDz_k, tmDz_mn, tmDz_out;
+        if (tmap_b(&tmW_k, Wb, width, s->d, s->ldW) != CAT_OK || tmap_mn_major(&tmW_mn, Wb, width, s->d, s->ldW) != CAT_OK ||
+            tmap_a(&tmDz_k, dz, rows, width, plan.b.Vs) != CAT_OK || tmap_mn_major(&tmDz_mn, dz, rows, width, plan.b.Vs) != CAT_OK ||
+            tmap_out(&tmDz_out, dz, rows, width, plan.b.Vs) != CAT_OK)
+            return CAT_ERR_CUDA;
+        tc::EpiDzLp::Params zp;
+        zp.labels = reinterpret_cast<const long long*>(a.labels); zp.valid = a.valid; zp.lse = a.lse; zp.entropy = a.entropy;
+        zp.grad_logp = a.grad_logp; zp.grad_entropy = a.grad_entropy; zp.T = static_cast<int>(s->T); zp.V = static_cast<int>(s->V);
+        zp.v0 = static_cast<int>(v0); zp.lo_rows = static_cast<int>(plan.lo);
+        int rc = launch_tc<0, 0, tc::EpiDzLp>(tmH_k, tmW_k, make_sched(s->T, width, s->d, fwd_splits(s->T, width), band_tiles(s->d), 0), zp,
+                                              status, sm_count, st, &tmDz_out);
+        if (rc != CAT_OK) return rc;
+        tc::EpiOut::Params ep;
+        memset(&ep, 0, sizeof(ep));
+        ep.M = static_cast<int>(width); ep.N = d; ep.ld_add = s->ldW; ep.ld_out = s->ldW;
+        if (s->dW_dtype == CAT_F32) {
+            ep.out_f32 = static_cast<float*>(dW) + v0 * s->ldW;
+            if (accumulate_dW) ep.add_f32 = ep.out_f32;
+        } else {
+            ep.out_bf16 = static_cast<__nv_bfloat16*>(dW) + v0 * s->ldW;
+            if (accumulate_dW) ep.add_bf16 = ep.out_bf16;
+        }
+        rc = launch_out<1, 1>(tmDz_mn, tmH_mn, make_sched(width, s->d, rows, 0, 1, 1), ep, status, sm_count, st);
+        if (rc != CAT_OK) return rc;
+        if (plan.b.n_slabs == 1) {
+            rc = launch_dh(tmDz_k, tmW_mn, s->T, s->d, s->V, nullptr, dH, s->ldH, reinterpret_cast<float*>(ws + plan.off_part), status, sm_count,
+                           st, plan.lo);
+        } else {
+            memset(&ep, 0, sizeof(ep));
+            ep.M = static_cast<int>(s->T); ep.N = d;
+            if (!first) { ep.add_f32 = dh_acc; ep.ld_add = s->d; }
+            if (last) { ep.out_bf16 = dH; ep.ld_out = s->ldH; }
+            else { ep.out_f32 = dh_acc; ep.ld_out = s->d; }
+            rc = launch_out<0, 1>(tmDz_k, tmW_mn, make_sched(s->T, s->d, width, 0, 1, 1), ep, status, sm_count, st);
+        }
+        if (rc != CAT_OK) return rc;
+    }
+    return CAT_OK;
+}
+
+int lp_bwd_f32(const cat_shape* s, const LpBwdPlan& plan, const float* H, const float* W, const LpGrads& a, float* dH, float* dW,
+               int accumulate_dW, uint8_t* ws, cudaStream_t st) {
+    float* dz = reinterpret_cast<float*>(ws + plan.b.off_dz);
+    float* Hz = reinterpret_cast<float*>(ws + plan.off_h);
+    float* part = reinterpret_cast<float*>(ws + plan.off_part);
+    const int T = static_cast<int>(s->T), d = static_cast<int>(s->d);
+    if (a.valid) {
+        lp::masked_copy_kernel<<<static_cast<unsigned>(T), lp::THREADS, 0, st>>>(H, s->ldH, d, a.valid, T, 0, Hz);
+        if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
+    }
+    for (int sl = 0; sl < plan.b.n_slabs; ++sl) {
+        const long long v0 = static_cast<long long>(sl) * plan.b.Vs;
+        const int w = static_cast<int>((s->V - v0) < plan.b.Vs ? (s->V - v0) : plan.b.Vs);
+        const float* Wf = W + v0 * s->ldW;
+        f32::Operands op;
+        f32::EpiParams ep;
+        memset(&ep, 0, sizeof(ep));
+        op.A = H; op.sAm = s->ldH; op.sAk = 1; op.B = Wf; op.sBk = 1; op.sBn = s->ldW;
+        op.M = T; op.N = w; op.Kd = d; op.n_groups = static_cast<int>(cdiv(w, f32::TN));
+        ep.labels = reinterpret_cast<const long long*>(a.labels); ep.valid = a.valid; ep.lse = a.lse; ep.entropy = a.entropy;
+        ep.grad_logp = a.grad_logp; ep.grad_entropy = a.grad_entropy; ep.dz = dz; ep.ld_dz = plan.b.Vs; ep.V = static_cast<int>(s->V);
+        ep.v0 = static_cast<int>(v0);
+        f32::gemm_kernel<f32::DZ, true, true><<<dim3(static_cast<unsigned>(cdiv(T, f32::TM)), static_cast<unsigned>(op.n_groups)), f32::THREADS, 0, st>>>(op, ep);
+        if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
+        int rc = launch_f32_dw(dz, plan.b.Vs, a.valid ? Hz : H, a.valid ? s->d : s->ldH, w, d, T, nullptr, dW + v0 * s->ldW, s->ldW,
+                               accumulate_dW != 0, part, st);
+        if (rc == CAT_OK) rc = launch_f32_dh(dz, plan.b.Vs, Wf, s->ldW, T, d, w, nullptr, dH, s->ldH, sl > 0, part, st);
+        if (rc != CAT_OK) return rc;
+    }
+    return CAT_OK;
+}
+
 // ------------------------------------------------------------------------------ distillation from top logits
 int check_topk_kd(const cat_topk_kd_desc* k) {
     if (!k) return CAT_ERR_NULL;
@@ -269,7 +397,8 @@ TkPlan plan_tk(const cat_shape* s, int k) {
     p.off_l1 = off;     off = align256(off + sizeof(float) * s->T);
     p.off_part = off;
     if (s->in_dtype == CAT_BF16) {
-        const size_t full = dh_part_bytes(p.f.Ts < s->T ? p.f.Ts : s->T, s->d, s->V);
+        const long long lo = lo_rows_of(s->T);
+        const size_t full = dh_part_bytes(lo > 0 ? 2 * lo : p.f.Ts < s->T ? p.f.Ts : s->T, s->d, s->V, lo > 0);
         const size_t rest = dh_part_bytes(s->T - (p.f.n_slabs - 1) * p.f.Ts, s->d, s->V);
         off += full > rest ? full : rest;
     } else {
@@ -279,9 +408,10 @@ TkPlan plan_tk(const cat_shape* s, int k) {
     return p;
 }
 
-// dH[r0 : r0 + rws, :] = (g/N) dz W and dW (+)= (g/N) dz^T Hw of one row slab; Hw: the slab's rows of H with pitch ldHw.
+// dH[r0 : r0 + rws, :] = (g/N) dz W and dW (+)= (g/N) dz^T Hw of one row slab; Hw: the slab's rows of H with pitch ldHw.  lo > 0: dz in
+// two terms (kTwoTermRows).
 int slab_grads(const cat_shape* s, const FusedPlan& f, const void* W, const void* Hw, long long ldHw, void* zs, uint8_t* ws, long long r0,
-               long long rws, bool first, bool last, const float* scale, float* part, void* dH, void* dW, int accumulate_dW, int sm_count,
+               long long rws, long long lo, bool first, bool last, const float* scale, float* part, void* dH, void* dW, int accumulate_dW, int sm_count,
                cudaStream_t st) {
     const int V = static_cast<int>(s->V), d = static_cast<int>(s->d), R = static_cast<int>(rws);
     if (s->in_dtype != CAT_BF16) {
@@ -293,11 +423,12 @@ int slab_grads(const cat_shape* s, const FusedPlan& f, const void* W, const void
     }
     int* status = reinterpret_cast<int*>(ws);
     CUtensorMap tmZ_k, tmZ_mn, tmW_mn, tmH_mn;
-    if (tmap_a(&tmZ_k, zs, rws, s->V, f.ldz) != CAT_OK || tmap_mn_major(&tmZ_mn, zs, rws, s->V, f.ldz) != CAT_OK ||
-        tmap_mn_major(&tmW_mn, W, s->V, s->d, s->ldW) != CAT_OK || tmap_mn_major(&tmH_mn, Hw, rws, s->d, ldHw) != CAT_OK)
+    const long long all = lo > 0 ? 2 * lo : rws;         // rows of dz, with its second terms
+    if (tmap_a(&tmZ_k, zs, all, s->V, f.ldz) != CAT_OK || tmap_mn_major(&tmZ_mn, zs, all, s->V, f.ldz) != CAT_OK ||
+        tmap_mn_major(&tmW_mn, W, s->V, s->d, s->ldW) != CAT_OK || tmap_mn_major(&tmH_mn, Hw, all, s->d, ldHw) != CAT_OK)
         return CAT_ERR_CUDA;
     const int rc = launch_dh(tmZ_k, tmW_mn, rws, s->d, s->V, scale, static_cast<__nv_bfloat16*>(dH) + r0 * s->ldH, s->ldH, part, status,
-                             sm_count, st);
+                             sm_count, st, lo);
     if (rc != CAT_OK) return rc;
     tc::EpiOut::Params ep;
     memset(&ep, 0, sizeof(ep));
@@ -315,7 +446,7 @@ int slab_grads(const cat_shape* s, const FusedPlan& f, const void* W, const void
         if (last) { ep.out_bf16 = static_cast<__nv_bfloat16*>(dW); ep.ld_out = s->ldW; }
         else { ep.out_f32 = dw_acc; ep.ld_out = s->d; }
     }
-    return launch_out<1, 1>(tmZ_mn, tmH_mn, make_sched(s->V, s->d, rws, 0, 1, 1), ep, status, sm_count, st);
+    return launch_out<1, 1>(tmZ_mn, tmH_mn, make_sched(s->V, s->d, all, 0, 1, 1), ep, status, sm_count, st);
 }
 
 template <class TI>
@@ -361,8 +492,10 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
         const long long rws = (s->T - r0) < f.Ts ? (s->T - r0) : f.Ts;
         const int S = head_splits(s, rws);
         const TI* Hs = H + r0 * s->ldH;
-        tk::gather_kernel<TI><<<static_cast<unsigned>(rws), tk::THREADS, 0, st>>>(Hs, s->ldH, W, s->ldW, d, y, ok, lists, r0, zt,
-                                                                                plan.ld_zt, ref, Hz);
+        const long long lo = BF16 ? lo_rows_of(s->T) : 0;
+        const unsigned grid_rows = static_cast<unsigned>(lo > 0 ? lo : rws);
+        tk::gather_kernel<TI><<<grid_rows, tk::THREADS, 0, st>>>(Hs, s->ldH, W, s->ldW, d, y, ok, lists, r0, static_cast<int>(rws),
+                                                                 static_cast<int>(lo), zt, plan.ld_zt, ref, Hz);
         if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
         rows::RowParams rp;
         memset(&rp, 0, sizeof(rp));
@@ -410,10 +543,10 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
             rows::block_scan_kernel<<<n_ctas, rows::ROW_THREADS, 0, st>>>(rp);
         }
         cta0 += n_ctas;
-        tk::dz_kernel<!BF16><<<static_cast<unsigned>(rws), tk::THREADS, 0, st>>>(zs, f.ldz, y, ok, lists, r0, lse, weight, zt, plan.ld_zt,
-                                                                               ref, desc->beta, kd_row, V);
+        tk::dz_kernel<!BF16><<<grid_rows, tk::THREADS, 0, st>>>(zs, f.ldz, y, ok, lists, r0, static_cast<int>(rws), static_cast<int>(lo), lse,
+                                                                weight, zt, plan.ld_zt, ref, desc->beta, kd_row, V);
         if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
-        const int rc = slab_grads(s, f, W, Hz, s->d, zs, ws, r0, rws, sl == 0, sl == f.n_slabs - 1, scale, reinterpret_cast<float*>(ws + plan.off_part), dH, dW, accumulate_dW,
+        const int rc = slab_grads(s, f, W, Hz, s->d, zs, ws, r0, rws, lo, sl == 0, sl == f.n_slabs - 1, scale, reinterpret_cast<float*>(ws + plan.off_part), dH, dW, accumulate_dW,
                                   sm_count, st);
         if (rc != CAT_OK) return rc;
     }
@@ -432,7 +565,7 @@ size_t cat_logprob_workspace_bytes(const cat_shape* shape, int top_k, int pass) 
     one.dW_dtype = shape->dW_dtype;
     if (check_shape(&one) != CAT_OK || top_k < 0 || top_k > CAT_TOPK_MAX) return 0;
     if (pass == 0) return plan_lp(&one, top_k).total;
-    if (pass == 1) return lp_bwd_bytes(&one);
+    if (pass == 1) return plan_lp_bwd(&one).total;
     return 0;
 }
 
@@ -475,13 +608,30 @@ int cat_logprob_fwd(const cat_shape* shape, const void* H, const void* W, const 
 int cat_logprob_bwd(const cat_shape* shape, const void* H, const void* W, const int64_t* labels, const uint8_t* valid, const float* lse,
                     const float* entropy, const float* grad_logp, const float* grad_entropy, void* dH, void* dW, int accumulate_dW,
                     void* workspace, size_t workspace_bytes, void* cuda_stream) {
-    if (!shape) return CAT_ERR_NULL;
+    if (!shape || !H || !W || !lse || !dH || !dW || (grad_logp && !labels) || (grad_entropy && !entropy)) return CAT_ERR_NULL;
     cat_shape one = per_position_shape(shape);
     one.dW_dtype = shape->dW_dtype;
-    LpArgs a;
-    a.entropy = entropy; a.grad_logp = grad_logp; a.grad_entropy = grad_entropy;
-    return bwd_core(&one, H, W, labels, valid, lse, nullptr, nullptr, dH, dW, accumulate_dW, workspace, workspace_bytes, cuda_stream,
-                    nullptr, &a);
+    const int sc = check_shape(&one);
+    if (sc != CAT_OK) return sc;
+    const bool bf16 = one.in_dtype == CAT_BF16;
+    const size_t in_al = bf16 ? 16 : 4;
+    if (misaligned(H, in_al) || misaligned(W, in_al) || misaligned(dH, in_al) || misaligned(dW, 16) || misaligned(labels, 8) ||
+        misaligned(lse, 4) || misaligned(entropy, 4) || misaligned(grad_logp, 4) || misaligned(grad_entropy, 4))
+        return CAT_ERR_ALIGN;
+    const LpBwdPlan plan = plan_lp_bwd(&one);
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < plan.total) return CAT_ERR_WORKSPACE;
+    int sm_count = 0;
+    const int dc = check_device(&sm_count);
+    if (dc != CAT_OK) return dc;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    if (cudaMemsetAsync(ws, 0, kHeaderBytes, st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
+    LpGrads a;
+    a.labels = labels; a.valid = valid; a.lse = lse; a.entropy = entropy; a.grad_logp = grad_logp; a.grad_entropy = grad_entropy;
+    return bf16 ? lp_bwd_bf16(&one, plan, static_cast<const __nv_bfloat16*>(H), static_cast<const __nv_bfloat16*>(W), a,
+                              static_cast<__nv_bfloat16*>(dH), dW, accumulate_dW, ws, sm_count, st)
+                : lp_bwd_f32(&one, plan, static_cast<const float*>(H), static_cast<const float*>(W), a, static_cast<float*>(dH),
+                             static_cast<float*>(dW), accumulate_dW, ws, st);
 }
 
 size_t cat_topk_kd_workspace_bytes(const cat_shape* shape, const cat_topk_kd_desc* desc) {

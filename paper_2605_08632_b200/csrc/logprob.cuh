@@ -162,6 +162,7 @@ struct EpiDzLp {
         int T;
         int V;
         int v0;
+        int lo_rows;                   // > 0: also what the rounding leaves, as row lo_rows + r (a multiple of 32, >= T)
     };
     struct State {
         float l2;                      // lse * log2 e
@@ -200,7 +201,10 @@ struct EpiDzLp {
 #pragma unroll 1
         for (int c = 0; c < BN / 32; ++c) {
             if (c * 32 >= ncols) break;
-            if ((c & 1) == 0) o.begin();
+            if ((c & 1) == 0) {
+                if (p.lo_rows == 0) o.begin();
+                else o.begin_both();
+            }
             uint32_t v[32];
             ptx::tmem_ld_32x32(taddr + c * 32, v);
             ptx::tmem_ld_wait();
@@ -227,14 +231,28 @@ struct EpiDzLp {
                 for (int i = 0; i < 32; ++i)
                     if (i >= live || !s.on) f[i] = 0.f;
             }
+            const bool closes = (c & 1) != 0 || (c + 1) * 32 >= ncols;
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                o.put((c & 1) * 4 + q, ptx::pack_bf16x2(f[q * 8 + 0], f[q * 8 + 1]), ptx::pack_bf16x2(f[q * 8 + 2], f[q * 8 + 3]),
-                      ptx::pack_bf16x2(f[q * 8 + 4], f[q * 8 + 5]), ptx::pack_bf16x2(f[q * 8 + 6], f[q * 8 + 7]));
-            if ((c & 1) != 0 || (c + 1) * 32 >= ncols) o.flush(col0 + (c >> 1) * 64);
+            for (int q = 0; q < 4; ++q) {
+                uint32_t hi[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) hi[i] = ptx::pack_bf16x2(f[q * 8 + 2 * i], f[q * 8 + 2 * i + 1]);
+                o.put((c & 1) * 4 + q, hi[0], hi[1], hi[2], hi[3]);
+                if (p.lo_rows > 0) {
+                    uint32_t lo[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        lo[i] = ptx::pack_bf16x2(f[q * 8 + 2 * i] - __uint_as_float(hi[i] << 16), f[q * 8 + 2 * i + 1] - __uint_as_float(hi[i] & 0xffff0000u));
+                    o.put_other((c & 1) * 4 + q, lo[0], lo[1], lo[2], lo[3]);
+                }
+            }
+            if (closes) {
+                if (p.lo_rows == 0) o.flush(col0 + (c >> 1) * 64);
+                else o.flush_both(col0 + (c >> 1) * 64, p.lo_rows);
+            }
         }
     }
-    __device__ static __forceinline__ int out_rows(const Params& p) { return p.T; }
+    __device__ static __forceinline__ int out_rows(const Params& p) { return p.lo_rows > 0 ? p.lo_rows : p.T; }
     __device__ static __forceinline__ void end_item(const Params&, const State&, int) {}
 };
 
@@ -801,9 +819,10 @@ __global__ void __launch_bounds__(RT, 8) row_kernel(const RowParams<TI, TZ> p) {
     }
 }
 
-// dH = scale * (part 0 + part 1 + ...), in that order, in bf16.  One CTA per row; `stride` elements from part to part.
+// dH = scale * (part 0 + part 1 + ...), in that order, in bf16.  One CTA per row; `stride` elements from part to part.  lo > 0: each part
+// has a second term in row lo + r.
 __global__ void __launch_bounds__(THREADS) add_parts_kernel(const float* part, int n, long long stride, int d, const float* scale,
-                                                            __nv_bfloat16* out, long long ld) {
+                                                            __nv_bfloat16* out, long long ld, long long lo) {
     const long long r = blockIdx.x;
     const float a = scale ? *scale : 1.f;
     for (int i = threadIdx.x; i < d / 4; i += THREADS) {
@@ -813,6 +832,12 @@ __global__ void __launch_bounds__(THREADS) add_parts_kernel(const float* part, i
         for (int g = 1; g < n; ++g) {
             const float4 x = __ldcs(src + g * (stride / 4));
             s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+        }
+        if (lo > 0) {
+            for (int g = 0; g < n; ++g) {
+                const float4 x = __ldcs(src + g * (stride / 4) + lo * d / 4);
+                s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+            }
         }
         uint2 o;
         o.x = ptx::pack_bf16x2(a * s.x, a * s.y);
@@ -832,10 +857,12 @@ __device__ __forceinline__ void copy_row(const TI* src, TI* dst, int d, bool on)
         for (int i = threadIdx.x; i < d; i += THREADS) dst[i] = on ? src[i] : static_cast<TI>(0);
     }
 }
+// Grid: rows of the copy.  lo > 0: rows T .. lo - 1 are zero and rows lo .. 2 lo - 1 a second copy, for dz in two terms.
 template <class TI>
-__global__ void __launch_bounds__(THREADS) masked_copy_kernel(const TI* H, long long ldH, int d, const unsigned char* valid, TI* out) {
-    const long long r = blockIdx.x;
-    copy_row(H + r * ldH, out + r * d, d, valid == nullptr || valid[r] != 0);
+__global__ void __launch_bounds__(THREADS) masked_copy_kernel(const TI* H, long long ldH, int d, const unsigned char* valid, int T, int lo,
+                                                              TI* out) {
+    const long long at = blockIdx.x, r = lo > 0 && at >= lo ? at - lo : at;
+    copy_row(H + (r < T ? r : 0) * ldH, out + at * d, d, r < T && (valid == nullptr || valid[r] != 0));
 }
 
 }  // namespace lp

@@ -151,6 +151,23 @@ struct OutStage {
         }
         sel ^= 1;
     }
+    // Both tiles at once, for rows that leave as two terms: the same columns of rows row0 and row0 + lo.
+    __device__ __forceinline__ void begin_both() {
+        if (lane == 0) ptx::tma_store_wait_read<0>();
+        __syncwarp();
+    }
+    __device__ __forceinline__ void put_other(int j, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+        ptx::st_shared_v4(buf + (sel ^ 1) * OUT_TILE_BYTES + lane * 128 + ((j ^ (lane & 7)) << 4), a, b, c, d);
+    }
+    __device__ __forceinline__ void flush_both(int x, int lo) {
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0 && row0 < n_rows) {
+            ptx::tma_store_2d(tm, buf + sel * OUT_TILE_BYTES, x, row0);
+            ptx::tma_store_2d(tm, buf + (sel ^ 1) * OUT_TILE_BYTES, x, row0 + lo);
+            ptx::tma_store_commit();
+        }
+    }
     __device__ __forceinline__ void finish() {
         if (lane == 0) ptx::tma_store_wait_all();
         __syncwarp();

@@ -160,12 +160,16 @@ struct Lists {
 template <class TI>
 __global__ void __launch_bounds__(THREADS) gather_kernel(const TI* H, long long ldH, const TI* W, long long ldW, int d,
                                                          const long long* labels, const unsigned char* valid_eff, Lists lists,
-                                                         long long row0, float* zt, int ld_zt, float* ref, TI* Hz) {
+                                                         long long row0, int rows, int lo, float* zt, int ld_zt, float* ref, TI* Hz) {
     __shared__ float s_max[WARPS];
     const long long r = row0 + blockIdx.x;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const TI* h = H + static_cast<long long>(blockIdx.x) * ldH;
-    lp::copy_row(h, Hz + static_cast<long long>(blockIdx.x) * d, d, valid_eff[r] != 0);
+    const bool pad = static_cast<int>(blockIdx.x) >= rows;            // dz in two terms: the grid goes on to `lo` rows
+    const TI* h = H + (pad ? 0 : static_cast<long long>(blockIdx.x)) * ldH;
+    const bool on = !pad && valid_eff[r] != 0;
+    lp::copy_row(h, Hz + static_cast<long long>(blockIdx.x) * d, d, on);
+    if (lo > 0) lp::copy_row(h, Hz + (static_cast<long long>(blockIdx.x) + lo) * d, d, on);
+    if (pad) return;
     if (!valid_eff[r]) {
         if (threadIdx.x == 0) ref[r] = 0.f;
         return;
@@ -276,7 +280,7 @@ __device__ __forceinline__ float block_sum(float x, float* red) {
 // fp32 slabs (fp32 inputs) hold z itself and leave as fp32 dz.
 template <bool F32>
 __global__ void __launch_bounds__(THREADS) dz_kernel(void* zs, long long ldz, const long long* labels, const unsigned char* valid_eff,
-                                                     Lists lists, long long row0, const float* lse, const float* weight,
+                                                     Lists lists, long long row0, int rows, int lo, const float* lse, const float* weight,
                                                      const float* zt, int ld_zt, const float* ref, float beta, float* kd_row,
                                                      int V) {
     __shared__ float s_red[WARPS];
@@ -286,10 +290,14 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(void* zs, long long ldz, co
     uint4* row = reinterpret_cast<uint4*>(static_cast<unsigned short*>(zs) + static_cast<size_t>(blockIdx.x) * ldz);
     float* row32 = static_cast<float*>(zs) + static_cast<size_t>(blockIdx.x) * ldz;
     const int groups = static_cast<int>(ldz / 8);
-    if (!valid_eff[r]) {
+    // what rounding to bf16 leaves, with dz in two terms
+    uint4* rest = lo > 0 ? row + static_cast<size_t>(lo) * (ldz / 8) : nullptr;
+    if (static_cast<int>(blockIdx.x) >= rows || !valid_eff[r]) {
+        if (lo > 0)
+            for (int g = threadIdx.x; g < groups; g += THREADS) rest[g] = make_uint4(0u, 0u, 0u, 0u);
         if (F32) for (int v = threadIdx.x; v < V; v += THREADS) row32[v] = 0.f;
         else for (int g = threadIdx.x; g < groups; g += THREADS) row[g] = make_uint4(0u, 0u, 0u, 0u);
-        if (threadIdx.x == 0) kd_row[r] = 0.f;
+        if (threadIdx.x == 0 && static_cast<int>(blockIdx.x) < rows) kd_row[r] = 0.f;
         return;
     }
     const long long t = lists.position(r);
@@ -323,7 +331,7 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(void* zs, long long ldz, co
     else for (int g = threadIdx.x; g < groups; g += THREADS) {
         const uint4 in = __ldcs(row + g);
         const uint32_t zw[4] = {in.x, in.y, in.z, in.w};
-        uint32_t o[4];
+        uint32_t o[4], left[4];
         const int col = g * 8;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -331,13 +339,19 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(void* zs, long long ldz, co
             const float a = col + 2 * j < V ? wm * ptx::ex2_approx(fmaf(z2.x, LOG2E, off)) : 0.f;
             const float b = col + 2 * j + 1 < V ? wm * ptx::ex2_approx(fmaf(z2.y, LOG2E, off)) : 0.f;
             o[j] = ptx::pack_bf16x2(a, b);
+            if (lo > 0) left[j] = ptx::pack_bf16x2(a - __uint_as_float(o[j] << 16), b - __uint_as_float(o[j] & 0xffff0000u));
         }
         row[g] = make_uint4(o[0], o[1], o[2], o[3]);
+        if (lo > 0) rest[g] = make_uint4(left[0], left[1], left[2], left[3]);
     }
     __syncthreads();
     auto put = [&](long long at, float x) {
         if (F32) row32[at] = x;
-        else reinterpret_cast<__nv_bfloat16*>(row)[at] = __float2bfloat16_rn(x);
+        else {
+            const __nv_bfloat16 hi = __float2bfloat16_rn(x);
+            reinterpret_cast<__nv_bfloat16*>(row)[at] = hi;
+            if (lo > 0) reinterpret_cast<__nv_bfloat16*>(rest)[at] = __float2bfloat16_rn(x - __bfloat162float(hi));
+        }
     };
     if (there) {
         float sub = p_i;
