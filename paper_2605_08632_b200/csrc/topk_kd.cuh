@@ -3,9 +3,9 @@
 // over the row's list (id_i, log p_i), i < k, in the place of the full distribution of kd.cuh:
 //   dz[v] = weight ((beta + sum_i p_i) q_v - beta [v = y] - sum_i p_i [v = id_i]).
 // One row slab at a time: gather_kernel (the logits at the list's ids, fp32, and the slab's reference), the logits GEMM,
-// which keeps z - ref as fp16, the row kernel of rowops.cuh, dz_kernel (z -> dz in place) and the dH and dW contractions.
+// which keeps z - ref in 16 bits, the row kernel of rowops.cuh, dz_kernel (z -> dz in place) and the dH and dW contractions.
 //
-// Why the slab holds fp16 logits and is turned into dz by a pass of its own (4 bytes per logit, bound by HBM), although
+// Why the slab holds logits and is turned into dz by a pass of its own (4 bytes per logit, bound by HBM), although
 // cat_loss_fwd_bwd gets by without one: there the row's factor a[r] has to ride on H in the dW contraction, and
 // rounding a[r] H[r, :] to bf16 costs as much as rounding dz.  Here dz is rounded to bf16 once, and H not at all.
 #pragma once
@@ -14,8 +14,19 @@
 namespace cat {
 namespace tc {
 
-// Softmax statistics (as EpiFwdT), the label's logit, and z - ref as fp16 (saturating).  ref is near the row's largest
-// logit when student and teacher agree, where fp16 is finest and softmax largest: a relative error of 2^-12 |z - ref|.
+// Softmax statistics (as EpiFwdT), the label's logit, and z - ref in 16 bits: a whole number of steps of 2^-9 nats around +16, from -48 to
+// +80.  ref is the largest of the logits that the list and the label name, so softmax is below e^-48 times a named token's where it is
+// cut off below, and above only logits that exceed every named one by 80 nats are cut.  The steps put a relative error of at most 2^-10
+// on softmax, 5.6e-4 rms, wherever it lies; fp16 would put 2^-12 |z - ref| there, 2.3e-3 rms in the bulk 8 to 16 nats below the top,
+// which is more than the rounding of dz.
+constexpr float STEPS = 512.f;           // per nat
+constexpr float CENTRE = 16.f;
+
+// two numbers of steps, rounded and clamped, into the halves of a word: adding 1.5 * 2^23 leaves a whole number in the low bits
+__device__ __forceinline__ uint32_t pack_steps(float a, float b) {
+    const float m = 12582912.f;
+    return __byte_perm(__float_as_uint(fminf(fmaxf(a, -32768.f), 32767.f) + m), __float_as_uint(fminf(fmaxf(b, -32768.f), 32767.f) + m), 0x5410);
+}
 struct EpiFwdRef {
     struct Params {
         const long long* labels;   // [T]
@@ -29,7 +40,8 @@ struct EpiFwdRef {
         int V;
     };
     struct State {
-        float m_run, l_run, ref;
+        float m_run, l_run;
+        float base;                // -(ref + CENTRE) in steps
         int id;
         int y;
         int row;
@@ -39,12 +51,12 @@ struct EpiFwdRef {
         s.m_run = LP_LOW;
         s.l_run = 0.f;
         s.id = 0;
-        s.ref = 0.f;
+        s.base = 0.f;
         s.y = -1;
         if (s.row < p.T) {
             const long long y = p.labels[s.row];
             if (y >= 0 && y < p.V) s.y = static_cast<int>(y);
-            s.ref = p.ref[s.row];
+            s.base = -(p.ref[s.row] + CENTRE) * STEPS;
         }
     }
     __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage& o) {
@@ -68,10 +80,10 @@ struct EpiFwdRef {
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                o.put((c & 1) * 4 + q, ptx::pack_f16x2_sat(f[q * 8 + 0] - s.ref, f[q * 8 + 1] - s.ref),
-                      ptx::pack_f16x2_sat(f[q * 8 + 2] - s.ref, f[q * 8 + 3] - s.ref),
-                      ptx::pack_f16x2_sat(f[q * 8 + 4] - s.ref, f[q * 8 + 5] - s.ref),
-                      ptx::pack_f16x2_sat(f[q * 8 + 6] - s.ref, f[q * 8 + 7] - s.ref));
+                o.put((c & 1) * 4 + q, pack_steps(fmaf(f[q * 8 + 0], STEPS, s.base), fmaf(f[q * 8 + 1], STEPS, s.base)),
+                      pack_steps(fmaf(f[q * 8 + 2], STEPS, s.base), fmaf(f[q * 8 + 3], STEPS, s.base)),
+                      pack_steps(fmaf(f[q * 8 + 4], STEPS, s.base), fmaf(f[q * 8 + 5], STEPS, s.base)),
+                      pack_steps(fmaf(f[q * 8 + 6], STEPS, s.base), fmaf(f[q * 8 + 7], STEPS, s.base)));
             if ((c & 1) != 0 || (c + 1) * 32 >= ncols) o.flush(col0 + (c >> 1) * 64);
             const int rel = s.y - (col0 + c * 32);
             if (rel >= 0 && rel < 32) {
@@ -325,7 +337,7 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(void* zs, long long ldz, co
     }
     if (i == 0) kd_row[r] = w * kd;
     const float wm = w * (beta + mass);
-    const float off = F32 ? 0.f : (ref[r] - lse_r) * LOG2E;
+    const float off = F32 ? 0.f : (ref[r] + tc::CENTRE - lse_r) * LOG2E;
     if (F32)
         for (int v = threadIdx.x; v < V; v += THREADS) row32[v] = wm * expf(row32[v] - lse_r);
     else for (int g = threadIdx.x; g < groups; g += THREADS) {
@@ -335,9 +347,11 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(void* zs, long long ldz, co
         const int col = g * 8;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float2 z2 = __half22float2(*reinterpret_cast<const __half2*>(&zw[j]));
-            const float a = col + 2 * j < V ? wm * ptx::ex2_approx(fmaf(z2.x, LOG2E, off)) : 0.f;
-            const float b = col + 2 * j + 1 < V ? wm * ptx::ex2_approx(fmaf(z2.y, LOG2E, off)) : 0.f;
+            // steps + 2^15 in the low bits of 2^23, taken off exactly
+            const float n0 = __uint_as_float(((zw[j] & 0xffffu) ^ 0x8000u) | 0x4b000000u) - 8421376.f;
+            const float n1 = __uint_as_float(((zw[j] >> 16) ^ 0x8000u) | 0x4b000000u) - 8421376.f;
+            const float a = col + 2 * j < V ? wm * ptx::ex2_approx(fmaf(n0, LOG2E / tc::STEPS, off)) : 0.f;
+            const float b = col + 2 * j + 1 < V ? wm * ptx::ex2_approx(fmaf(n1, LOG2E / tc::STEPS, off)) : 0.f;
             o[j] = ptx::pack_bf16x2(a, b);
             if (lo > 0) left[j] = ptx::pack_bf16x2(a - __uint_as_float(o[j] << 16), b - __uint_as_float(o[j] & 0xffff0000u));
         }

@@ -76,9 +76,8 @@ def check(eng, out, inputs, K, dW_bf16=False, fixed=None, **kw):
         slack = float((ref["weight"] * (err * (1 + mass) + 1.01 * K * (err + 4 * U) * np.abs(term))).sum() / n) + 4 * U * abs(want)
         assert abs(got - want) <= slack, (got, want, slack)
     assert abs(loss3[0] - (beta * loss3[1] + loss3[2])) <= 4 * U * (beta * abs(loss3[1]) + abs(loss3[2]))
-    # dz: the stored z - ref is off by half a step of fp16, 2^-11 of it; the weight by K err
-    span = float((ref["z"].max(axis=1) - ref["z"].min(axis=1)).max()) if ok.any() else 0.0
-    tol = 2 * err + 1.01 * K * (err + 4 * U) + (2.0 ** -11 * span if bf16 else 0.0)
+    # dz: the stored z - ref is off by half a step of 2^-9; the weight by K err
+    tol = 2 * err + 1.01 * K * (err + 4 * U) + (1.01 * 2.0 ** -10 if bf16 else 0.0)
     Hc = np.where(ok[:, None], np64(H), 0.0)
     check_grads(dH, dW, (ref["dH"], ref["dW"], ref["terms"]), np64(W), Hc, tol, bf16, dW_bf16=dW_bf16)
     assert not dH[~ok].any()
@@ -129,6 +128,23 @@ def test_without_block_start_every_row_has_its_own_list():
     eng = CatLoss(T, d, V, K)
     ref = check(eng, run(eng, *x), x, K)
     assert not ref["ok"][50:].any()
+
+
+def test_logits_far_from_the_named_ones():
+    """Rows whose largest logit is up to 70 nats above all that the list and the label name, and rows with all others 60 and more below."""
+    T, K, d, V, k = 160, 4, 64, 500, 3
+    H, W, y, valid, ids, tl, start = make(T, K, d, V, k, BF, masked=0.0)
+    far = torch.arange(T) % 2 == 0
+    named = torch.cat([ids[(start[:, None] + torch.arange(K)).reshape(-1)], y[:, None]], 1)
+    other = torch.tensor([next(v for v in range(V) if v not in named[r].tolist()) for r in range(T)])
+    token = torch.where(far, other, y)
+    Wy = W[token].float()
+    H = (H.float() + Wy * (70.0 * torch.rand(T, generator=torch.Generator().manual_seed(4)) / (Wy * Wy).sum(1)).unsqueeze(1)).to(BF)
+    x = (H, W, y, valid, ids, tl, start)
+    for renorm in (True, False):
+        eng = CatLoss(T, d, V, K)
+        conf = torch.full((T,), 0.9)
+        check(eng, run(eng, *x, beta=0.2, renormalize=renorm, conf_ext=conf), x, K, beta=0.2, renormalize=renorm, conf_ext=conf)
 
 
 def test_no_row_takes_part_and_padding_may_hold_anything():
@@ -199,8 +215,8 @@ def test_offsets_past_31_bits():
     ref = O.topk_kd(H[rows], W, y[rows], valid[rows], K, ids, tl, start[-5:], beta=0.3)
     n = eng.fwd_stats().n_valid
     want = ref["dH"] * ref["n_valid"] / n
-    # roundings of dz and of the result (2^-8 each), of z - ref (2^-11 of at most about 16, on the smaller part of dz)
-    assert np.linalg.norm(np64(dH[rows]) - want) <= (2 * 2.0 ** -8 + 2.0 ** -7) * np.linalg.norm(want)
+    # roundings of dz and of the result (2^-8 each), of z - ref (2^-10)
+    assert np.linalg.norm(np64(dH[rows]) - want) <= (2 * 2.0 ** -8 + 2.0 ** -10) * np.linalg.norm(want)
     assert np.abs(np64(eng.lse[rows]) - ref["lse"])[ref["ok"]].max() <= 1e-4
 
 
@@ -243,7 +259,7 @@ def test_lists_written_by_one_operator_train_the_other():
                                                                     start.to(DEV), beta=0.2, renormalize=False, conf_ext=conf))
     ref, oH, oW = C.cat_kd_forward_backward(H, W, y, None, K, Ht, Wt, start, 0.2, conf_ext=conf.cpu().numpy())
     assert abs(float(loss3[0]) - ref["loss"]) <= 1e-4 * ref["loss"]
-    # dz and the result are rounded to bf16 (2^-8 each), z - ref to fp16
+    # dz and the result are rounded to bf16 (2^-8 each), z - ref to steps of 2^-9
     assert np.linalg.norm(np64(dH) - oH) <= 2 ** -6 * np.linalg.norm(oH) and np.linalg.norm(np64(dW) - oW) <= 2 ** -6 * np.linalg.norm(oW)
     other = CatLoss(T, d, V, K)
     full3, fH, fW = other.kd_forward_backward(H.to(DEV), W.to(DEV), y.to(DEV), None, Ht.to(DEV), Wt.to(DEV), start, 0.2, conf_ext=conf)
