@@ -547,8 +547,8 @@ tc::Sched make_sched(long long M, long long N, long long Kd, int n_groups, int b
 // Parts that the vocabulary contraction of dH = dz W is cut into when a batch has few output tiles for the 74 CTA pairs
 // (512 rows of d = 2048: 16 tiles).  Each part's fp32 sum goes to its own rows of a scratch array and one kernel adds them in
 // order, so the result does not depend on who finishes first.  Cost in whole-contraction tiles per worker; a part costs
-// its share of the scratch traffic, about 0.2 % of a tile each.  dH of 512 x 2048 over V = 128256: 622 us whole, XXX us in parts;
-// of 300 x 1024 over 151936: 708 and XXX us.
+// its share of the scratch traffic, about 0.2 % of a tile each.  dH of 512 x 2048 over V = 128256: 622 us whole, 182 us in parts;
+// of 300 x 1024 over 151936: 708 and 104 us.
 int dh_parts(long long rows, long long d, long long V) {
     const long long tiles = cdiv(rows, tile_m()) * cdiv(d, tc::BN);
     const long long most = cdiv(V, 4096);                              // no part shorter than 4096 vocabulary entries

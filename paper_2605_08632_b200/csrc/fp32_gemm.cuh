@@ -8,7 +8,8 @@
 // and reached a sixth of the FFMA rate).  The sum over k is taken in runs of 256, added up in a second accumulator: the rounding of a
 // sum over 4096 vocabulary entries grows with 256 + 16 instead of 4096 terms.  Outputs with few tiles have their contraction cut into
 // parts (gridDim.z), summed in order by add_kernel.
-// Measured, 512 x 256 x 4096: XXX
+// Measured, 512 rows x 256 x 4096 (1.07 GFLOP a product): forward 52 us, dH 50 us, dW 45 us, 20 to 24 TFLOP/s: one or two CTAs' worth of
+// tiles per SM, so latency and not the FFMA rate (74 TFLOP/s) bounds them; simt.cuh's kernel takes 106, 880 and 127 us.
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>
