@@ -407,7 +407,8 @@ int cat_kd_loss_fwd_bwd(const cat_shape* shape, const cat_kd_desc* desc, const v
  *   top_ids    [T, top_k] int64;  top_logp  [T, top_k] fp32                        (device, out)
  *   workspace  at least cat_logprob_workspace_bytes(shape, top_k, 0) bytes, 256-byte aligned
  * With top_k > 0 the workspace holds one row slab of logits (fp16, or fp32 for CAT_F32) of at most about slab_mib
- * MiB (default 3072), never more than T rows.  Two launches per slab and one memset.  The workspace's first int32 holds the
+ * MiB (default 3072; up to 128 rows of bf16 are taken at once whatever it says), never more than T rows.  Two launches per
+ * slab and one memset.  The workspace's first int32 holds the
  * device status.  Calls that may overlap on the GPU need a workspace each.  Returns CAT_OK or a negative cat_status.
  */
 #define CAT_TOPK_MAX 256
@@ -420,7 +421,8 @@ int cat_logprob_fwd(const cat_shape* shape, const void* H, const void* W, const 
  * Gradients of sum_r (grad_logp[r] logp[r] + grad_entropy[r] entropy[r]) with respect to H and W:
  *     dz[r, v] = grad_logp[r] ([v == y_r] - p[r, v]) - grad_entropy[r] p[r, v] (log p[r, v] + entropy[r]),
  *     dH = dz W,   dW = dz^T H.
- * The logits are recomputed per vocabulary slab, as in cat_loss_bwd; dz is rounded once to in_dtype.  Rows with
+ * The logits are recomputed per vocabulary slab, as in cat_loss_bwd; dz is rounded once to in_dtype (for up to 128 bf16 rows
+ * kept as two terms, unless slab_mib cuts the vocabulary).  Rows with
  * valid[r] == 0 get a zero dH row and add nothing to dW, whatever H holds there; a label that is no token id
  * contributes through the entropy only.  No gradient flows through the alternatives.
  *   lse, entropy   [T] fp32 as written by cat_logprob_fwd; entropy may be NULL without grad_entropy   (device, in)

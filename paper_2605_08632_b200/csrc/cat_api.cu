@@ -191,6 +191,7 @@ struct FusedPlan {
 };
 
 double dh_waves(long long rows, long long d, long long V);
+long long lo_rows_of(long long T);
 
 long long gcd_ll(long long a, long long b) { return b == 0 ? a : gcd_ll(b, a % b); }
 
@@ -228,6 +229,10 @@ FusedPlan plan_fused(const cat_shape* s, bool two_slabs = true) {
         if (best_cost < 0.0 || cost < best_cost * (1.0 - 1e-9)) { best_cost = cost; best_ts = ts; }
     }
     p.Ts = best_ts;
+    if (!two_slabs && p.Ts >= s->T) {       // one slab: no taller than the batch, but with room for dz in two terms
+        const long long rows = cdiv(s->T, tile_m()) * tile_m(), terms = 2 * lo_rows_of(s->T);
+        p.Ts = rows > terms ? rows : terms;
+    }
     p.n_slabs = static_cast<int>(cdiv(s->T, p.Ts));
     p.warp_scan = s->K <= 32 && (s->K & (s->K - 1)) == 0;
     p.S_max = 1;

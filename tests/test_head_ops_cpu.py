@@ -1,6 +1,9 @@
 """The LM-head operators without a GPU: the oracle against hand examples and differences, argument refusals before any launch,
 workspace sizes, the binding's structure layout."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -12,6 +15,7 @@ from paper_2605_08632_b200 import api
 from paper_2605_08632_b200 import binding as B
 
 P = ctypes.c_void_p
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 # ------------------------------------------------------------------------------ the oracle
@@ -182,6 +186,23 @@ def test_workspaces_stay_bounded():
     assert B.cat_logprob_workspace_bytes(one, 20, 0) < 1 << 20
     small = B.make_shape(65536, 2048, 128256, 8, B.CAT_BF16, slab_mib=256)
     assert B.cat_logprob_workspace_bytes(small, 20, 0) < 300 << 20
+
+
+@pytest.mark.parametrize("pair", ["0", "1"])
+def test_one_slab_has_room_for_dz_in_two_terms(pair):
+    """Up to 128 rows, dz stands in the slab (and H in its copy) as two sets of rows, each rounded up to 32; the kernels without CTA
+    pairs plan in tiles of 128 rows, so that a slab of one tile would be too low.  A slab is no taller than its batch otherwise."""
+    code = ("from paper_2605_08632_b200 import binding as B\n"
+            "for T, K in ((1, 1), (66, 33), (70, 1), (128, 8), (128, 128)):\n"
+            "    s = B.make_shape(T, 512, 20000, K, B.CAT_BF16, B.CAT_BF16)\n"
+            "    print(T, B.cat_topk_kd_workspace_bytes(s, B.make_topk_kd_desc(T, 4, 0.1)), B.cat_logprob_workspace_bytes(s, 0, 1))\n")
+    out = subprocess.run([sys.executable, "-c", code], cwd=ROOT, env=dict(os.environ, CAT_LOSS_CTA_PAIR=pair), capture_output=True, text=True, check=True)
+    for line in out.stdout.splitlines():
+        T, kd, bwd = (int(x) for x in line.split())
+        rows = 2 * ((T + 31) // 32 * 32)
+        need = rows * (20000 * 2 + 512 * 2) + rows * 512 * 4           # slab, copy of H, dH's parts
+        assert need <= kd < need + (40 << 20), line
+        assert need <= bwd < need + (40 << 20), line
 
 
 def test_python_layer_refuses_what_the_kernels_would_misread():

@@ -1,4 +1,8 @@
 """cat_topk_kd_loss_fwd_bwd against the fp64 oracle, through CatLoss.topk_kd_forward_backward; bounds in head_ops_util."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -86,7 +90,7 @@ def check(eng, out, inputs, K, dW_bf16=False, fixed=None, **kw):
 
 @pytest.mark.parametrize("T,K,d,V,k,dtype", [
     (1, 1, 64, 1, 1, BF), (3, 3, 64, 2, 5, BF), (64, 8, 64, 500, 8, BF), (130, 5, 136, 3001, 16, BF), (264, 8, 128, 5003, 64, BF),
-    (320, 32, 64, 1000, 256, BF), (66, 33, 72, 900, 3, BF), (2, 1, 3, 5, 2, F32), (65, 5, 33, 700, 8, F32), (96, 16, 64, 2050, 64, F32),
+    (320, 32, 64, 1000, 256, BF), (66, 33, 72, 900, 3, BF), (128, 8, 64, 1000, 6, BF), (2, 1, 3, 5, 2, F32), (65, 5, 33, 700, 8, F32), (96, 16, 64, 2050, 64, F32),
 ])
 @pytest.mark.parametrize("renorm", [True, False])
 def test_matches_oracle(T, K, d, V, k, dtype, renorm):
@@ -267,3 +271,13 @@ def test_lists_written_by_one_operator_train_the_other():
     # a top-16 list keeps most of the teacher's mass: the step points the same way
     few = TokenLogProb(L, d, V, top_k=16).forward(Ht.to(DEV), Wt.to(DEV))
     assert torch.equal(few.top_ids, r.top_ids[:, :16])
+
+
+def test_without_cta_pairs():
+    """The one-CTA kernels (128-row tiles) in a process of their own: the choice is made once per process."""
+    here = os.path.dirname(os.path.abspath(__file__))
+    pick = "matches_oracle or slabs or guarded or pitched or padding"
+    r = subprocess.run([sys.executable, "-m", "pytest", "-q", "-x", "-p", "no:cacheprovider", os.path.join(here, "test_logprob_gpu.py"),
+                        os.path.join(here, "test_topk_kd_gpu.py"), "-k", pick], env=dict(os.environ, CAT_LOSS_CTA_PAIR="0"),
+                       capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-1000:]
