@@ -17,15 +17,25 @@ def _check(name, t, shape, dtype, device, rows_only=False):
     further apart than they are long."""
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.device != device:
         raise ValueError(f"{name} must be on {device}, got {t.device}")
-    if rows_only and t.dim() == 2:
-        if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-            raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    elif not t.is_contiguous():
+    if t.is_contiguous():
+        return
+    if not rows_only or t.dim() != 2:
         raise ValueError(f"{name} must be contiguous")
+    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{name} must have contiguous rows that do not overlap")
+
+
+def _on(device, call, *args):
+    """The call with `device` current, as the library wants it."""
+    if torch.cuda.current_device() == device.index:
+        call(*args)
+    else:
+        with torch.cuda.device(device):
+            call(*args)
 
 
 def _mask(valid):
@@ -161,14 +171,12 @@ class CatLoss:
         if n == 0:
             self._topk_need = None
             raise ValueError("invalid problem for cat_topk_kd_loss_fwd_bwd")
-        with torch.cuda.device(dev):
-            if self._ws_topk is None or self._ws_topk.numel() < n:
-                self._ws_topk = torch.empty(n, dtype=torch.uint8, device=dev)
-            if self.loss3 is None:
-                self.loss3 = torch.zeros(3, dtype=torch.float32, device=dev)
-            B.cat_topk_kd_loss_fwd_bwd(self.shape, desc, H, W, labels, valid, top_ids, top_logp, block_start, conf_ext, grad_loss,
-                                       self.loss3, self.lse, self.conf, self.weight, self.stats, self.dH, self.dW, accumulate_dW,
-                                       self._ws_topk)
+        if self._ws_topk is None or self._ws_topk.numel() < n:
+            self._ws_topk = torch.empty(n, dtype=torch.uint8, device=dev)
+        if self.loss3 is None:
+            self.loss3 = torch.zeros(3, dtype=torch.float32, device=dev)
+        _on(dev, B.cat_topk_kd_loss_fwd_bwd, self.shape, desc, H, W, labels, valid, top_ids, top_logp, block_start, conf_ext, grad_loss,
+            self.loss3, self.lse, self.conf, self.weight, self.stats, self.dH, self.dW, accumulate_dW, self._ws_topk)
         return self.loss3, self.dH, self.dW
 
     def topk_kd_status(self) -> int:
@@ -242,6 +250,7 @@ class TokenLogProb:
             raise TypeError("TokenLogProb takes bfloat16 or float32")
         self.T, self.d, self.V, self.top_k, self.dtype, self.dW_dtype, self.slab_mib = T, d, V, top_k, dtype, dW_dtype, slab_mib
         self._code = (code[dtype], code[dW_dtype])
+        self._shapes = {}
         n = B.cat_logprob_workspace_bytes(self._shape(d, d), top_k, 0)
         if n == 0:
             raise ValueError("invalid shape for cat_logprob_fwd")
@@ -254,7 +263,10 @@ class TokenLogProb:
         self.top_logp = torch.empty(T, top_k, **f32) if top_k else None
 
     def _shape(self, ldH, ldW):
-        return B.make_shape(self.T, self.d, self.V, 1, *self._code, ldH=ldH, ldW=ldW, slab_mib=self.slab_mib)
+        s = self._shapes.get((ldH, ldW))
+        if s is None:
+            s = self._shapes[ldH, ldW] = B.make_shape(self.T, self.d, self.V, 1, *self._code, ldH=ldH, ldW=ldW, slab_mib=self.slab_mib)
+        return s
 
     def _inputs(self, H, W, labels, valid):
         _check("H", H, (self.T, self.d), self.dtype, self.device, rows_only=True)
@@ -269,9 +281,8 @@ class TokenLogProb:
         valid = _mask(valid)
         self._inputs(H, W, labels, valid)
         logp = None if labels is None else self.logp
-        with torch.cuda.device(self.device):
-            B.cat_logprob_fwd(self._shape(_pitch(H), _pitch(W)), H, W, labels, valid, self.top_k, logp, self.lse, self.entropy,
-                              self.top_ids, self.top_logp, self.ws)
+        _on(self.device, B.cat_logprob_fwd, self._shape(_pitch(H), _pitch(W)), H, W, labels, valid, self.top_k, logp, self.lse, self.entropy,
+            self.top_ids, self.top_logp, self.ws)
         return LogProbs(logp, self.lse, self.entropy, self.top_ids, self.top_logp)
 
     def backward(self, H, W, labels=None, valid=None, grad_logp=None, grad_entropy=None, lse=None, entropy=None,
@@ -290,18 +301,17 @@ class TokenLogProb:
         if _pitch(H) != self.d or _pitch(W) != self.d:
             raise ValueError("backward takes contiguous H and W: the gradients are laid out like them")
         shape = self._shape(self.d, self.d)
-        with torch.cuda.device(self.device):
-            if self._ws_bwd is None:
-                n = B.cat_logprob_workspace_bytes(shape, 0, 1)
-                self._ws_bwd = torch.empty(n, dtype=torch.uint8, device=self.device)
-            if self.dH is None:
-                self.dH = torch.empty(self.T, self.d, dtype=self.dtype, device=self.device)
-            if self.dW is None:
-                if accumulate_dW:
-                    raise ValueError("accumulate_dW needs a dW to add to: set engine.dW, or run one backward without it")
-                self.dW = torch.empty(self.V, self.d, dtype=self.dW_dtype, device=self.device)
-            B.cat_logprob_bwd(shape, H, W, labels, valid, lse, entropy, grad_logp, grad_entropy, self.dH, self.dW, accumulate_dW,
-                              self._ws_bwd)
+        if self._ws_bwd is None:
+            n = B.cat_logprob_workspace_bytes(shape, 0, 1)
+            self._ws_bwd = torch.empty(n, dtype=torch.uint8, device=self.device)
+        if self.dH is None:
+            self.dH = torch.empty(self.T, self.d, dtype=self.dtype, device=self.device)
+        if self.dW is None:
+            if accumulate_dW:
+                raise ValueError("accumulate_dW needs a dW to add to: set engine.dW, or run one backward without it")
+            self.dW = torch.empty(self.V, self.d, dtype=self.dW_dtype, device=self.device)
+        _on(self.device, B.cat_logprob_bwd, shape, H, W, labels, valid, lse, entropy, grad_logp, grad_entropy, self.dH, self.dW, accumulate_dW,
+            self._ws_bwd)
         return self.dH, self.dW
 
     def status(self) -> int:

@@ -133,11 +133,13 @@ def cat_loss_launch_count(shape: cat_shape, which: int) -> int:
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    """An address for an argument declared c_void_p: ctypes takes a plain int, and makes it in a third of the time of c_void_p(...)."""
+    return None if t is None else t.data_ptr()
 
 
 def _stream():
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    """Handle of the current device's current stream (torch.cuda.current_stream() builds a Stream object for it: 3 us)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def cat_loss_fwd(shape, H, W, labels, valid, conf_ext, loss, lse, conf, weight, stats, workspace) -> None:

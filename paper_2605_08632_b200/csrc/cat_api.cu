@@ -467,6 +467,18 @@ unsigned next_launch_serial() {
     return v == 0 ? ++n & 0x7fffffffu : v;
 }
 
+// Dynamic shared memory above 48 KB is allowed to a kernel once per device; `done` (one per kernel) remembers where that has been done.
+template <class Kernel>
+bool allow_smem(Kernel kern, int bytes, std::atomic<unsigned long long>& done) {
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return false; }
+    const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0ull;
+    if (bit != 0 && (done.load(std::memory_order_relaxed) & bit) != 0) return true;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) { cudaGetLastError(); return false; }
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
+
 template <int A_MN, int B_MN, class Epi, int CG>
 int launch_tc_cg(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmOut, const tc::Sched& sched_in,
                  const typename Epi::Params& ep, int* status, int sm_count, cudaStream_t st) {
@@ -478,10 +490,8 @@ int launch_tc_cg(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorM
     }
     auto kern = tc::gemm_kernel<A_MN, B_MN, Epi, CG>;
     constexpr int smem = tc::Geo<CG>::SMEM_BYTES;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
-        cudaGetLastError();
-        return CAT_ERR_CUDA;
-    }
+    static std::atomic<unsigned long long> allowed{0};
+    if (!allow_smem(kern, smem, allowed)) return CAT_ERR_CUDA;
     const int workers = sm_count / CG;
     const int grid = CG * (sched.n_items < workers ? sched.n_items : workers);
     cudaLaunchConfig_t cfg = {};

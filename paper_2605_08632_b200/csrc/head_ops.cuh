@@ -50,10 +50,8 @@ int launch_skinny_as(const CUtensorMap& tmW, const CUtensorMap& tmH, const skinn
     p.stages = (skinny::SMEM_BYTES - 1024 - 8192) / ((SUB * p.tile_rows + p.n) * tc::BK * 2);
     if (p.stages > skinny::MAX_STAGES) p.stages = skinny::MAX_STAGES;
     auto kern = skinny::logits_kernel<TPW, HALVES, SUB>;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, skinny::SMEM_BYTES) != cudaSuccess) {
-        cudaGetLastError();
-        return CAT_ERR_CUDA;
-    }
+    static std::atomic<unsigned long long> allowed{0};
+    if (!allow_smem(kern, skinny::SMEM_BYTES, allowed)) return CAT_ERR_CUDA;
     kern<<<static_cast<unsigned>(grid), 64 + 128 * HALVES, skinny::SMEM_BYTES, st>>>(tmW, tmH, p, status);
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
@@ -482,10 +480,8 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
 
     CUtensorMap tmW_k;
     if (BF16 && tmap_b(&tmW_k, W, s->V, s->d, s->ldW) != CAT_OK) return CAT_ERR_CUDA;
-    if (cudaMemsetAsync(ws, 0, kHeaderBytes, st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
-    tk::prepare_kernel<<<static_cast<unsigned>(cdiv(T, tk::THREADS)), tk::THREADS, 0, st>>>(
-        y, valid, lists.block_start, T, K, V, desc->L, ok);
-    rows::bwd_scale_kernel<<<1, 1024, 0, st>>>(y, ok, T, V, grad_loss, scale);
+    tk::begin_kernel<<<1, 1024, 0, st>>>(y, valid, lists.block_start, T, K, V, desc->L, grad_loss, ok, scale, status,
+                                         static_cast<int>(kHeaderBytes / sizeof(int)));
     if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
     int cta0 = 0;
     for (int sl = 0; sl < f.n_slabs; ++sl) {
@@ -551,8 +547,7 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
                                   sm_count, st);
         if (rc != CAT_OK) return rc;
     }
-    rows::finalize_kernel<<<1, rows::ROW_THREADS, 0, st>>>(partials, cta0, T / K, loss, reinterpret_cast<rows::StatsOut*>(stats), status);
-    kd::finalize_kernel<<<1, rows::ROW_THREADS, 0, st>>>(kd_row, ok, T, desc->beta, loss);
+    tk::end_kernel<<<1, 1024, 0, st>>>(partials, cta0, T / K, kd_row, T, desc->beta, loss, reinterpret_cast<rows::StatsOut*>(stats), status);
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
 
