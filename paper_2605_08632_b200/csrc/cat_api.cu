@@ -561,17 +561,17 @@ tc::Sched make_sched(long long M, long long N, long long Kd, int n_groups, int b
 
 // Parts that the vocabulary contraction of dH = dz W is cut into when a batch has few output tiles for the 74 CTA pairs
 // (512 rows of d = 2048: 16 tiles).  Each part's fp32 sum goes to its own rows of a scratch array and one kernel adds them in
-// order, so the result does not depend on who finishes first.  Cost in whole-contraction tiles per worker; a part costs
-// its share of the scratch traffic, about 0.2 % of a tile each.  dH of 512 x 2048 over V = 128256: 622 us whole, 182 us in parts;
-// of 300 x 1024 over 151936: 708 and 104 us.
+// order, so the result does not depend on who finishes first.  Cost in us: 8 ns per tile and vocabulary entry, 2.5 us to write a part's
+// tile out, the scratch read back at 4 TB/s.  dH of 512 x 2048 over V = 128256: 622 us whole, 182 us in 9 parts; of 300 x 1024 over
+// 151936 708 and 104 us; of 64 x 1024 over 20000 XXX.
 int dh_parts(long long rows, long long d, long long V) {
     const long long tiles = cdiv(rows, tile_m()) * cdiv(d, tc::BN);
-    const long long most = cdiv(V, 4096);                              // no part shorter than 4096 vocabulary entries
+    const double whole = 8.0e-3 * static_cast<double>(V), back = static_cast<double>(rows) * static_cast<double>(d) * 1.0e-6;
     int best = 1;
-    double best_cost = static_cast<double>(cdiv(tiles, plan_workers()));
-    for (int g = 2; g <= 32 && g <= most; ++g) {
+    double best_cost = static_cast<double>(cdiv(tiles, plan_workers())) * (whole + 2.5);
+    for (int g = 2; g <= 32 && g * 512 <= V; ++g) {                    // no part shorter than 512 vocabulary entries
         if (static_cast<size_t>(g) * cdiv(rows, tile_m()) * tile_m() * d * 4 > (256ull << 20)) break;
-        const double cost = static_cast<double>(cdiv(tiles * g, plan_workers())) / g + 0.002 * g;
+        const double cost = static_cast<double>(cdiv(tiles * g, plan_workers())) * (whole / g + 2.5) + 3.0 + back * g;
         if (cost < 0.95 * best_cost) { best_cost = cost; best = g; }
     }
     return best;
