@@ -406,23 +406,35 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(void* zs, long long ldz, co
     const float off = F32 ? 0.f : (ref[r] + tc::CENTRE - lse_r) * LOG2E;
     if (F32)
         for (int v = threadIdx.x; v < V; v += THREADS) row32[v] = wm * expf(row32[v] - lse_r);
-    else for (int g = threadIdx.x; g < groups; g += THREADS) {
-        const uint4 in = __ldcs(row + g);
-        const uint32_t zw[4] = {in.x, in.y, in.z, in.w};
-        uint32_t o[4], left[4];
-        const int col = g * 8;
+    else {
+        // four loads in flight a thread: slabs of few rows fill the SMs with too few warps to cover the memory's latency with one
+        constexpr int AHEAD = 4;
+        for (int g0 = threadIdx.x; g0 < groups; g0 += AHEAD * THREADS) {
+            uint4 in[AHEAD];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            // steps + 2^15 in the low bits of 2^23, taken off exactly
-            const float n0 = __uint_as_float(((zw[j] & 0xffffu) ^ 0x8000u) | 0x4b000000u) - 8421376.f;
-            const float n1 = __uint_as_float(((zw[j] >> 16) ^ 0x8000u) | 0x4b000000u) - 8421376.f;
-            const float a = col + 2 * j < V ? wm * ptx::ex2_approx(fmaf(n0, LOG2E / tc::STEPS, off)) : 0.f;
-            const float b = col + 2 * j + 1 < V ? wm * ptx::ex2_approx(fmaf(n1, LOG2E / tc::STEPS, off)) : 0.f;
-            o[j] = ptx::pack_bf16x2(a, b);
-            if (lo > 0) left[j] = ptx::pack_bf16x2(a - __uint_as_float(o[j] << 16), b - __uint_as_float(o[j] & 0xffff0000u));
+            for (int u = 0; u < AHEAD; ++u)
+                if (g0 + u * THREADS < groups) in[u] = __ldcs(row + g0 + u * THREADS);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int g = g0 + u * THREADS;
+                if (g >= groups) break;
+                const uint32_t zw[4] = {in[u].x, in[u].y, in[u].z, in[u].w};
+                uint32_t o[4], left[4];
+                const int col = g * 8;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    // steps + 2^15 in the low bits of 2^23, taken off exactly
+                    const float n0 = __uint_as_float(((zw[j] & 0xffffu) ^ 0x8000u) | 0x4b000000u) - 8421376.f;
+                    const float n1 = __uint_as_float(((zw[j] >> 16) ^ 0x8000u) | 0x4b000000u) - 8421376.f;
+                    const float a = col + 2 * j < V ? wm * ptx::ex2_approx(fmaf(n0, LOG2E / tc::STEPS, off)) : 0.f;
+                    const float b = col + 2 * j + 1 < V ? wm * ptx::ex2_approx(fmaf(n1, LOG2E / tc::STEPS, off)) : 0.f;
+                    o[j] = ptx::pack_bf16x2(a, b);
+                    if (lo > 0) left[j] = ptx::pack_bf16x2(a - __uint_as_float(o[j] << 16), b - __uint_as_float(o[j] & 0xffff0000u));
+                }
+                row[g] = make_uint4(o[0], o[1], o[2], o[3]);
+                if (lo > 0) rest[g] = make_uint4(left[0], left[1], left[2], left[3]);
+            }
         }
-        row[g] = make_uint4(o[0], o[1], o[2], o[3]);
-        if (lo > 0) rest[g] = make_uint4(left[0], left[1], left[2], left[3]);
     }
     __syncthreads();
     auto put = [&](long long at, float x) {
