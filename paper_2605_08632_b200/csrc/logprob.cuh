@@ -30,11 +30,36 @@ __device__ __forceinline__ int first_at(const float (&f)[32], float x) {
     return at;
 }
 
+// (three chains: one alone is 16 dependent steps)
 __device__ __forceinline__ float max_of(const float (&f)[32]) {
-    float x = ptx::max3_f32(f[0], f[1], f[2]);
+    float a = ptx::max3_f32(f[0], f[1], f[2]), b = ptx::max3_f32(f[3], f[4], f[5]), c = ptx::max3_f32(f[6], f[7], f[8]);
 #pragma unroll
-    for (int i = 3; i + 1 < 32; i += 2) x = ptx::max3_f32(x, f[i], f[i + 1]);
-    return fmaxf(x, f[31]);
+    for (int i = 9; i + 5 < 32; i += 6) {
+        a = ptx::max3_f32(a, f[i], f[i + 1]);
+        b = ptx::max3_f32(b, f[i + 2], f[i + 3]);
+        c = ptx::max3_f32(c, f[i + 4], f[i + 5]);
+    }
+    a = ptx::max3_f32(a, f[27], f[28]);
+    b = ptx::max3_f32(b, f[29], f[30]);
+    return ptx::max3_f32(a, b, fmaxf(c, f[31]));
+}
+
+// A tile's accumulators in chunks of 32 columns, body(c, v) for each that holds columns below ncols: the next chunk is on its way
+// from tensor memory while the warp works on one.
+template <class F>
+__device__ __forceinline__ void walk_tile(uint32_t taddr, int ncols, F&& body) {
+    uint32_t a[32], b[32];
+    ptx::tmem_ld_32x32(taddr, a);
+#pragma unroll 1
+    for (int c = 0; c < BN / 32 && c * 32 < ncols; c += 2) {
+        ptx::tmem_ld_wait(a);
+        ptx::tmem_ld_32x32(taddr + (c + 1) * 32, b);
+        body(c, a);
+        ptx::tmem_ld_wait(b);
+        if (c + 2 < BN / 32) ptx::tmem_ld_32x32(taddr + (c + 2) * 32, a);
+        if ((c + 1) * 32 < ncols) body(c + 1, b);
+    }
+    ptx::tmem_ld_wait();
 }
 
 // l = sum exp(z - m) and u = sum exp2(x) x, x = (z - m) log2 e, with m the largest logit so far.
@@ -99,13 +124,8 @@ struct EpiLp {
         float g[BN / LP_GROUP];
 #pragma unroll
         for (int i = 0; i < BN / LP_GROUP; ++i) g[i] = LP_LOW;
-#pragma unroll 1
-        for (int c = 0; c < BN / 32; ++c) {
-            if (c * 32 >= ncols) break;
+        walk_tile(taddr, ncols, [&](int c, uint32_t (&v)[32]) {
             if (TOP && (c & 1) == 0) o.begin();
-            uint32_t v[32];
-            ptx::tmem_ld_32x32(taddr + c * 32, v);
-            ptx::tmem_ld_wait();
             float f[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
@@ -131,7 +151,7 @@ struct EpiLp {
                 if ((c & 1) != 0 || (c + 1) * 32 >= ncols) o.flush(col0 + (c >> 1) * 64);
             }
             s.r.add(f, cmax);
-        }
+        });
         if (TOP && s.row < p.T) {
             float4* out = reinterpret_cast<float4*>(p.gmax + static_cast<size_t>(s.row) * p.ld_g + n_tile * (BN / LP_GROUP));
             out[0] = make_float4(g[0], g[1], g[2], g[3]);
@@ -198,16 +218,11 @@ struct EpiDzLp {
     __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage& o) {
         const int col0 = n_tile * BN;
         const int ncols = min(BN, p.V - p.v0 - col0);
-#pragma unroll 1
-        for (int c = 0; c < BN / 32; ++c) {
-            if (c * 32 >= ncols) break;
+        walk_tile(taddr, ncols, [&](int c, uint32_t (&v)[32]) {
             if ((c & 1) == 0) {
                 if (p.lo_rows == 0) o.begin();
                 else o.begin_both();
             }
-            uint32_t v[32];
-            ptx::tmem_ld_32x32(taddr + c * 32, v);
-            ptx::tmem_ld_wait();
             float f[32];
             const int live = ncols - c * 32;
             const uint64_t l2e2 = ptx::pack_f32x2(LOG2E, LOG2E), nl2 = ptx::pack_f32x2(-s.l2, -s.l2);
@@ -250,7 +265,7 @@ struct EpiDzLp {
                 if (p.lo_rows == 0) o.flush(col0 + (c >> 1) * 64);
                 else o.flush_both(col0 + (c >> 1) * 64, p.lo_rows);
             }
-        }
+        });
     }
     __device__ static __forceinline__ int out_rows(const Params& p) { return p.lo_rows > 0 ? p.lo_rows : p.T; }
     __device__ static __forceinline__ void end_item(const Params&, const State&, int) {}

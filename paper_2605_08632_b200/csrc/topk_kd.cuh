@@ -17,18 +17,23 @@
 namespace cat {
 namespace tc {
 
-// Softmax statistics (as EpiFwdT), the label's logit, and z - ref in 16 bits: a whole number of steps of 2^-9 nats around +16, from -48 to
+// Softmax statistics (as EpiFwdT), the label's logit, and z - ref in 16 bits: a whole number of steps of 2^-9 nats from -48, up to
 // +80.  ref is the largest of the logits that the list and the label name, so softmax is below e^-48 times a named token's where it is
 // cut off below, and above only logits that exceed every named one by 80 nats are cut.  The steps put a relative error of at most 2^-10
 // on softmax, 5.6e-4 rms, wherever it lies; fp16 would put 2^-12 |z - ref| there, 2.3e-3 rms in the bulk 8 to 16 nats below the top,
 // which is more than the rounding of dz.
 constexpr float STEPS = 512.f;           // per nat
-constexpr float CENTRE = 16.f;
 
-// two numbers of steps, rounded and clamped, into the halves of a word: adding 1.5 * 2^23 leaves a whole number in the low bits
-__device__ __forceinline__ uint32_t pack_steps(float a, float b) {
-    const float m = 12582912.f;
-    return __byte_perm(__float_as_uint(fminf(fmaxf(a, -32768.f), 32767.f) + m), __float_as_uint(fminf(fmaxf(b, -32768.f), 32767.f) + m), 0x5410);
+constexpr float LOW_END = -48.f;         // the range's lower end: step 0
+constexpr float TOP_STEP = 65535.f;
+
+// two logits as steps, rounded and clamped, into the halves of a word.  The saturating fma clamps to the range as a share of it, and adding
+// 2^23 leaves the whole number of steps in the low bits: two instructions a logit on the fma pipe, where clamping by min and max takes
+// four, two of them at half the rate.  base = -(ref + LOW_END) STEPS / TOP_STEP.
+__device__ __forceinline__ uint32_t pack_steps(float a, float b, float base) {
+    const uint32_t x = __float_as_uint(fmaf(__saturatef(fmaf(a, STEPS / TOP_STEP, base)), TOP_STEP, 8388608.f));
+    const uint32_t y = __float_as_uint(fmaf(__saturatef(fmaf(b, STEPS / TOP_STEP, base)), TOP_STEP, 8388608.f));
+    return __byte_perm(x, y, 0x5410);
 }
 struct EpiFwdRef {
     struct Params {
@@ -44,7 +49,7 @@ struct EpiFwdRef {
     };
     struct State {
         float m_run, l_run;
-        float base;                // -(ref + CENTRE) in steps
+        float base;                // see pack_steps
         int id;
         int y;
         int row;
@@ -59,19 +64,14 @@ struct EpiFwdRef {
         if (s.row < p.T) {
             const long long y = p.labels[s.row];
             if (y >= 0 && y < p.V) s.y = static_cast<int>(y);
-            s.base = -(p.ref[s.row] + CENTRE) * STEPS;
+            s.base = -(p.ref[s.row] + LOW_END) * (STEPS / TOP_STEP);
         }
     }
     __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage& o) {
         const int col0 = n_tile * BN;
         const int ncols = min(BN, p.V - col0);
-#pragma unroll 1
-        for (int c = 0; c < BN / 32; ++c) {
-            if (c * 32 >= ncols) break;
+        walk_tile(taddr, ncols, [&](int c, uint32_t (&v)[32]) {
             if ((c & 1) == 0) o.begin();
-            uint32_t v[32];
-            ptx::tmem_ld_32x32(taddr + c * 32, v);
-            ptx::tmem_ld_wait();
             float f[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
@@ -83,10 +83,8 @@ struct EpiFwdRef {
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                o.put((c & 1) * 4 + q, pack_steps(fmaf(f[q * 8 + 0], STEPS, s.base), fmaf(f[q * 8 + 1], STEPS, s.base)),
-                      pack_steps(fmaf(f[q * 8 + 2], STEPS, s.base), fmaf(f[q * 8 + 3], STEPS, s.base)),
-                      pack_steps(fmaf(f[q * 8 + 4], STEPS, s.base), fmaf(f[q * 8 + 5], STEPS, s.base)),
-                      pack_steps(fmaf(f[q * 8 + 6], STEPS, s.base), fmaf(f[q * 8 + 7], STEPS, s.base)));
+                o.put((c & 1) * 4 + q, pack_steps(f[q * 8 + 0], f[q * 8 + 1], s.base), pack_steps(f[q * 8 + 2], f[q * 8 + 3], s.base),
+                      pack_steps(f[q * 8 + 4], f[q * 8 + 5], s.base), pack_steps(f[q * 8 + 6], f[q * 8 + 7], s.base));
             if ((c & 1) != 0 || (c + 1) * 32 >= ncols) o.flush(col0 + (c >> 1) * 64);
             const int rel = s.y - (col0 + c * 32);
             if (rel >= 0 && rel < 32) {
@@ -96,10 +94,7 @@ struct EpiFwdRef {
                     if (i == rel) zy = f[i];
                 p.z_label[s.row] = zy;
             }
-            float cmax = ptx::max3_f32(f[0], f[1], f[2]);
-#pragma unroll
-            for (int i = 3; i + 1 < 32; i += 2) cmax = ptx::max3_f32(cmax, f[i], f[i + 1]);
-            cmax = fmaxf(cmax, f[31]);
+            const float cmax = max_of(f);
             if (cmax > s.m_run) s.id = col0 + c * 32 + first_at(f, cmax);
             const float m_new = fmaxf(s.m_run, cmax);
             const float mb = m_new * LOG2E;
@@ -115,7 +110,7 @@ struct EpiFwdRef {
             ptx::unpack_f32x2(sum2, s0, s1);
             s.l_run = fmaf(s.l_run, ptx::ex2_approx((s.m_run - m_new) * LOG2E), s0 + s1);
             s.m_run = m_new;
-        }
+        });
     }
     __device__ static __forceinline__ int out_rows(const Params& p) { return p.T; }
     __device__ static __forceinline__ void end_item(const Params& p, const State& s, int group) {
@@ -403,7 +398,7 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(void* zs, long long ldz, co
     }
     if (i == 0) kd_row[r] = w * kd;
     const float wm = w * (beta + mass);
-    const float off = F32 ? 0.f : (ref[r] + tc::CENTRE - lse_r) * LOG2E;
+    const float off = F32 ? 0.f : (ref[r] + (tc::LOW_END + 64.f) - lse_r) * LOG2E;
     if (F32)
         for (int v = threadIdx.x; v < V; v += THREADS) row32[v] = wm * expf(row32[v] - lse_r);
     else {
@@ -423,9 +418,9 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(void* zs, long long ldz, co
                 const int col = g * 8;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    // steps + 2^15 in the low bits of 2^23, taken off exactly
-                    const float n0 = __uint_as_float(((zw[j] & 0xffffu) ^ 0x8000u) | 0x4b000000u) - 8421376.f;
-                    const float n1 = __uint_as_float(((zw[j] >> 16) ^ 0x8000u) | 0x4b000000u) - 8421376.f;
+                    // steps from the middle of the range: the low bits of 2^23, and that much taken off exactly
+                    const float n0 = __uint_as_float((zw[j] & 0xffffu) | 0x4b000000u) - 8421376.f;
+                    const float n1 = __uint_as_float((zw[j] >> 16) | 0x4b000000u) - 8421376.f;
                     const float a = col + 2 * j < V ? wm * ptx::ex2_approx(fmaf(n0, LOG2E / tc::STEPS, off)) : 0.f;
                     const float b = col + 2 * j + 1 < V ? wm * ptx::ex2_approx(fmaf(n1, LOG2E / tc::STEPS, off)) : 0.f;
                     o[j] = ptx::pack_bf16x2(a, b);
