@@ -120,6 +120,9 @@ LpPlan plan_lp(const cat_shape* s, int top_k) {
     return p;
 }
 
+// Rows of up to this many get the row kernel's large CTAs.
+constexpr long long kFewRows = 2 * kPlanSMs;
+
 template <class TI, class TZ, bool TOP>
 int launch_lp_rows(const cat_shape* s, const LpPlan& plan, const TI* H, const TI* W, long long r0, long long rws, int S, uint8_t* ws,
                    const int64_t* labels, const uint8_t* valid, int top_k, float* logp, float* lse, float* entropy,
@@ -152,14 +155,17 @@ int launch_lp_rows(const cat_shape* s, const LpPlan& plan, const TI* H, const TI
     // launched ahead of the logits kernel's end, for which it waits: a decoding step is short enough for the 2 us to show
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(rws), 1, 1);
-    cfg.blockDim = dim3(lp::RT, 1, 1);
+    const bool few = rws <= kFewRows;
+    cfg.blockDim = dim3(few ? lp::RT_FEW : lp::RT_MANY, 1, 1);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, lp::row_kernel<TI, TZ, TOP>, rp) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
+    const cudaError_t err = few ? cudaLaunchKernelEx(&cfg, lp::row_kernel<TI, TZ, TOP, lp::RT_FEW>, rp)
+                                : cudaLaunchKernelEx(&cfg, lp::row_kernel<TI, TZ, TOP, lp::RT_MANY>, rp);
+    if (err != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
     return CAT_OK;
 }
 

@@ -279,8 +279,9 @@ constexpr int THREADS = 256;
 constexpr int WARPS = THREADS / 32;
 constexpr int MAX_TOP = 256;            // CAT_TOPK_MAX
 constexpr int CAP = 512;                // candidate columns held at a time
-constexpr int RT = 128;                 // threads of the row kernel: its phases wait more than they work, so many small CTAs per SM
-constexpr int RW = RT / 32;
+// Threads RT of a row kernel's CTA: its phases wait more than they work, so with many rows small CTAs, eight to an SM; with rows for two CTAs
+// an SM at most, large ones, which have four times as many exact logits under way.
+constexpr int RT_MANY = 128, RT_FEW = 512;
 
 // H[r, :] . W[v, :] by one warp, every lane gets the sum.  bf16 products are exact in fp32 (16 significant bits), fp32
 // products in fp64; the sums are taken in fp64 and always in the same order, so equal rows of W give equal logits.
@@ -394,26 +395,29 @@ struct RowParams {
     float* top_logp;               // [T][k]
 };
 
+template <int RT>
 struct Shared {
+    static constexpr int RW = RT / 32;
     float red[2][RW];
     int count[2][RW];
-    int n_cand, n_near;
+    int n_cand, n_near, n_rest;
     float m, l, u, lse;
     int id_max;
     double z_max, z_label;
     double z[CAP];                 // exact logits, where `err` says so
     float approx[CAP];
-    float err[CAP];                // how far approx may be off; EXACT: z is known; OUT: not among the k largest
+    float err[CAP];                // how far approx may be off; EXACT, SUMMED: z is known; OUT: not among the k largest
     int id[CAP];
     double z_keep[MAX_TOP];
     int id_keep[MAX_TOP];
-    int near[CAP];                 // groups that may hold candidates; then the candidates in doubt
+    int near[CAP];                 // groups that may hold candidates; then the candidates in doubt, and from the end the others
     float near_max[CAP];           // those groups' maxima
     int above[CAP], close[CAP];    // per candidate: others certainly above it, others within the errors
 };
-constexpr float EXACT = -1.f, OUT = -2.f;
+constexpr float EXACT = -1.f, OUT = -2.f, SUMMED = -3.f;
 
-__device__ __forceinline__ float block_max(float x, float* red) {
+template <int RW>
+__device__ __forceinline__ float block_max(float x, float (&red)[RW]) {
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
     __syncthreads();
@@ -428,7 +432,9 @@ __device__ __forceinline__ float block_max(float x, float* red) {
 // A bound that at least k of the values reach, and few more than k, from the largest values of each thread's four shares of them (best,
 // -infinity for an empty share): any k of those are k of the values.  Bisection between the least and the largest, until at most
 // k + k / 16 + 1 shares reach it (k = 64 of 4008 values: about 75 values do).  LP_LOW when fewer than k shares hold a value.  big: largest |value| there is.
-__device__ __forceinline__ float near_kth(const float (&best)[4], float least, int k, Shared& sh, float& big) {
+template <int RT>
+__device__ __forceinline__ float near_kth(const float (&best)[4], float least, int k, Shared<RT>& sh, float& big) {
+    constexpr int RW = RT / 32;
     const float mine = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
     float hi = block_max(mine, sh.red[0]);
     big = fmaxf(fabsf(hi), fabsf(block_max(-least, sh.red[1])));
@@ -472,21 +478,32 @@ __device__ __forceinline__ float near_kth(const float (&best)[4], float least, i
     return lo;
 }
 
+// The share of itself that the row's largest logit came out too small, by which its other logits, bf16 sums of as many terms, are taken to be off
+// as well (their truncations add up to the same share of each within about a tenth).
+template <class TI, class S>
+__device__ __forceinline__ float off_share(const S& sh) {
+    const float x = static_cast<float>(sh.z_max - static_cast<double>(sh.m));
+    return sizeof(TI) == 2 && sh.m > 1.f && fabsf(x) < 1.f ? x / sh.m : 0.f;
+}
+
 // lse and entropy from the merged sums and the exact largest logit, and the label's log probability; one thread.
-template <class TI, class TZ>
-__device__ __forceinline__ void finish_row(const RowParams<TI, TZ>& p, long long r, Shared& sh) {
+template <class TI, class TZ, int RT>
+__device__ __forceinline__ void finish_row(const RowParams<TI, TZ>& p, long long r, Shared<RT>& sh) {
     // the largest logit entered as exp(0) = 1 and 0; it is exp(x) and x exp(x) with its exact distance x from m
     float l = sh.l, u = sh.u;
     const float x = static_cast<float>(sh.z_max - static_cast<double>(sh.m));
+    // l with the others' logits corrected too, to first order: the share times their sum of exp(z - m) z.  The entropy's two parts stay as
+    // they were summed: there the share cancels but for itself times the logits' variance.
+    float lc = fmaf(off_share<TI>(sh), fmaf(0.6931471805599453f, u, sh.m * (l - 1.f)), l);
     if (fabsf(x) < 1.f) {
+        lc += expm1f(x);
         l += expm1f(x);
         u = fmaf(x * tc::LOG2E, expf(x), u);
     }
-    const float logl = logf(l);
-    const float lse = sh.m + logl;
+    const float lse = sh.m + logf(lc);
     sh.lse = lse;
     p.lse[r] = lse;
-    const float ent = logl - 0.6931471805599453f * u / l;
+    const float ent = logf(l) - 0.6931471805599453f * u / l;
     p.entropy[r] = ent < 0.f ? 0.f : ent + (lse - lse);      // NaN for a row that is not finite
     if (p.logp != nullptr) {
         const long long y = p.labels[r];
@@ -495,8 +512,8 @@ __device__ __forceinline__ void finish_row(const RowParams<TI, TZ>& p, long long
 }
 
 // The two logits of a row that are always taken exactly, by one warp each: which = 0 the largest, 1 the label's.
-template <class TI, class TZ>
-__device__ __forceinline__ void exact_one(const RowParams<TI, TZ>& p, const TI* h, long long r, Shared& sh, int which) {
+template <class TI, class TZ, int RT>
+__device__ __forceinline__ void exact_one(const RowParams<TI, TZ>& p, const TI* h, long long r, Shared<RT>& sh, int which) {
     const int lane = threadIdx.x & 31;
     if (which == 0) {
         const double z = warp_dot(h, p.W + static_cast<long long>(sh.id_max) * p.ldW, p.d, lane);
@@ -511,8 +528,9 @@ __device__ __forceinline__ void exact_one(const RowParams<TI, TZ>& p, const TI* 
 }
 
 // Exact logits of candidates [from, n) and the order of all n of them; the first k go to the front of the keep list.
-template <class TI, class TZ>
-__device__ __forceinline__ int settle(const RowParams<TI, TZ>& p, const TI* h, Shared& sh, int from, int n) {
+template <class TI, class TZ, int RT>
+__device__ __forceinline__ int settle(const RowParams<TI, TZ>& p, const TI* h, Shared<RT>& sh, int from, int n) {
+    constexpr int RW = RT / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int c = from + warp; c < n; c += RW) {
         const double z = warp_dot(h, p.W + static_cast<long long>(sh.id[c]) * p.ldW, p.d, lane);
@@ -530,18 +548,24 @@ __device__ __forceinline__ int settle(const RowParams<TI, TZ>& p, const TI* h, S
     return n < p.k ? n : p.k;
 }
 
-// The same from the approximate logits, with exact ones only for candidates that their errors leave in doubt against another, and for
-// those that the slab's fp16 has rounded (not the largest of their group): their values are returned.
-template <class TI, class TZ>
-__device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI* h, long long r, Shared& sh, int n, float eps, float rel) {
+// The same, ordered by the approximate logits, with fp64 sums only for candidates that their errors leave in doubt against another.
+//
+// The values.  A bf16 logit of 20 that comes out 3e-6 of itself too small would be off by more than its log probability has
+// places for.  With few rows every value is an fp32 sum over d.  With many that is a gather of W for each (9240 rows of 1344 x 4906, k = 20: 178 -> 225 us;
+// 8192 of 2048 x 128256, k = 64: 3.18 -> 3.51 ms): there only values that the slab's fp16 has rounded (not the largest of their group) are
+// summed, and the others are corrected by the share of itself that the largest logit is off (see finish_row).
+template <class TI, class TZ, int RT>
+__device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI* h, long long r, Shared<RT>& sh, int n, float eps, float rel) {
+    constexpr int RW = RT / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    static_assert(CAP / RT <= 32, "one bit per candidate of a thread");
-    unsigned doubt = 0, out = 0;              // bit i: candidate threadIdx.x + i * RT needs its exact logit, is out
+    const long long y = p.logp != nullptr ? p.labels[r] : -1;
+    if (RT == RT_FEW)
+        for (int c = warp; c < n; c += RW) prefetch_row(p.W + static_cast<long long>(sh.id[c]) * p.ldW, p.d, lane);
     // Several threads share a candidate while there are threads to share: each looks at its part of the others.
     const int parts = n <= RT / 2 ? RT / (n > 0 ? n : 1) : 1;
     const int part = threadIdx.x / (n > 0 ? n : 1), per = (n + parts - 1) / parts;
     for (int c = threadIdx.x; c < n; c += RT) { sh.above[c] = 0; sh.close[c] = 0; }
-    if (threadIdx.x == 0) sh.n_near = 0;
+    if (threadIdx.x == 0) sh.n_near = sh.n_rest = 0;
     __syncthreads();
     for (int c = parts > 1 ? threadIdx.x - part * n : threadIdx.x; c < n && (parts == 1 || part < parts); c += parts > 1 ? CAP : RT) {
         const float z = sh.approx[c], e = sh.err[c];
@@ -557,21 +581,29 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
         if (near) atomicAdd(&sh.close[c], near);
     }
     __syncthreads();
-    for (int i = 0, c = threadIdx.x; c < n; ++i, c += RT) {
-        if (sh.above[c] >= p.k) out |= 1u << i;
-        else if (sh.close[c] > 1 || sh.err[c] > fmaxf(eps, rel * fabsf(sh.approx[c])) + 4.0e-8f) doubt |= 1u << i;
+    for (int c = threadIdx.x; c < n; c += RT) {
+        if (sh.above[c] >= p.k) {
+            sh.err[c] = OUT;
+            sh.approx[c] = -INFINITY;
+        } else if (sh.close[c] > 1) {
+            sh.err[c] = EXACT;
+            sh.near[atomicAdd(&sh.n_near, 1)] = c;
+        } else if (sizeof(TI) == 2 && sh.id[c] != sh.id_max && sh.id[c] != y &&
+                   (RT == RT_FEW || sh.err[c] > fmaxf(eps, rel * fabsf(sh.approx[c])) + 4.0e-8f)) {
+            sh.err[c] = SUMMED;
+            sh.near[CAP - 1 - atomicAdd(&sh.n_rest, 1)] = c;
+        }
         sh.above[c] = 0;
-        if (out >> i & 1u) { sh.err[c] = OUT; sh.approx[c] = -INFINITY; }
-        else if (doubt >> i & 1u) { sh.err[c] = EXACT; sh.near[atomicAdd(&sh.n_near, 1)] = c; }
     }
     __syncthreads();
-    const int n_doubt = sh.n_near;
-    for (int i = warp; i < n_doubt + 2; i += RW) {
+    const int n_doubt = sh.n_near, n_rest = sh.n_rest;
+    for (int i = warp; i < n_doubt + 2 + n_rest; i += RW) {
         if (i < 2) {
             exact_one(p, h, r, sh, i);
         } else {
-            const int c = sh.near[i - 2];
-            const double z = warp_dot(h, p.W + static_cast<long long>(sh.id[c]) * p.ldW, p.d, lane);
+            const int c = i < n_doubt + 2 ? sh.near[i - 2] : sh.near[CAP - 1 - (i - n_doubt - 2)];
+            const TI* w = p.W + static_cast<long long>(sh.id[c]) * p.ldW;
+            const double z = i < n_doubt + 2 ? warp_dot(h, w, p.d, lane) : static_cast<double>(warp_dot_f32(h, w, p.d, lane));
             if (lane == 0) sh.z[c] = z;
         }
     }
@@ -585,20 +617,20 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
     }
     __syncthreads();
     if (threadIdx.x == RT - 1) finish_row(p, r, sh);
+    const float share = off_share<TI>(sh);
     for (int c = threadIdx.x; c < n; c += RT) {
         const float ec = sh.err[c], zc = sh.approx[c];
         if (ec == OUT) continue;
         const int id = sh.id[c];
-        double z = static_cast<double>(zc);
+        const double z = ec < 0.f ? sh.z[c] : static_cast<double>(fmaf(share, zc, zc));
         int rank = sh.above[c];
         if (ec == EXACT) {      // against others in doubt the exact logits count
-            z = sh.z[c];
             for (int i = 0; i < n_doubt; ++i) {
                 const int j = sh.near[i];
                 rank += (sh.z[j] > z || (sh.z[j] == z && sh.id[j] < id) ? 1 : 0) - (sh.approx[j] > zc ? 1 : 0);
             }
         }
-        if (rank < p.k) { sh.z_keep[rank] = id == sh.id_max ? sh.z_max : z; sh.id_keep[rank] = id; }
+        if (rank < p.k) { sh.z_keep[rank] = id == sh.id_max ? sh.z_max : id == y ? sh.z_label : z; sh.id_keep[rank] = id; }
     }
     __syncthreads();
     return n < p.k ? n : p.k;
@@ -608,7 +640,7 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
 //
 // lse.  The tensor cores' additions truncate, so a logit that is far from 0 comes out a few 1e-6 of itself too small.  In a row that
 // is sure of a token that token's logit makes up lse, so the largest logit is taken again as an fp64 sum and the row's sums
-// are corrected by the difference; the label's logit is such a sum too.
+// are corrected by the difference; the label's logit is such a sum too, and so are the returned alternatives' (see settle_close).
 //
 // Top k.  Any k group maxima are k logits of the row, so a number t that k group maxima reach is a lower bound of the row's k-th
 // largest logit, and only columns at or above t, less the GEMM's error, can be among the k largest.  They are looked
@@ -618,9 +650,9 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
 // 12 us for one row, 256 us for 8192 rows of V = 128256, k = 64 (GEMM 2.85 ms): the bound 45, the list of groups 30, their look-up 78 (700
 // thousand 64-byte reads all over the slab), ranking about 45, exact sums the rest.
 // More than CAP candidates (a row of zeros, many equal rows of W) are settled batch by batch by exact sums.
-template <class TI, class TZ, bool TOP>
-__global__ void __launch_bounds__(RT, 8) row_kernel(const RowParams<TI, TZ> p) {
-    __shared__ Shared sh;
+template <class TI, class TZ, bool TOP, int RT>
+__global__ void __launch_bounds__(RT, 1024 / RT) row_kernel(const RowParams<TI, TZ> p) {
+    __shared__ Shared<RT> sh;
     const long long r = blockIdx.x;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     asm volatile("griddepcontrol.wait;" ::: "memory");      // the logits kernel has finished (it may have been launched ahead of that)
@@ -803,11 +835,12 @@ __global__ void __launch_bounds__(RT, 8) row_kernel(const RowParams<TI, TZ> p) {
             // otherwise batch by batch, one group per warp and step, the k best so far carried along
             kept = 0;
             int n = 0;
-            for (int g0 = 0; g0 < p.n_g; g0 += RW) {
+            constexpr int STEP = 4;          // at most 64 columns each: they fit beside MAX_TOP kept ones
+            for (int g0 = 0; g0 < p.n_g; g0 += STEP) {
                 if (threadIdx.x == 0) sh.n_cand = n;
                 __syncthreads();
                 const int gi = g0 + warp;
-                if (gi < p.n_g && g[gi] >= thr) {
+                if (warp < STEP && gi < p.n_g && g[gi] >= thr) {
                     for (int o = 0; o < group; o += 32) {
                         const long long col = static_cast<long long>(gi) * group + o + lane;
                         float e;
@@ -817,8 +850,8 @@ __global__ void __launch_bounds__(RT, 8) row_kernel(const RowParams<TI, TZ> p) {
                 }
                 __syncthreads();
                 n = sh.n_cand;
-                const bool last = g0 + RW >= p.n_g;
-                if (n > CAP - RW * 64 || last) {
+                const bool last = g0 + STEP >= p.n_g;
+                if (n > CAP - STEP * 64 || last) {
                     kept = settle(p, h, sh, kept, n);
                     for (int i = threadIdx.x; i < kept; i += RT) { sh.z[i] = sh.z_keep[i]; sh.id[i] = sh.id_keep[i]; }
                     n = kept;
