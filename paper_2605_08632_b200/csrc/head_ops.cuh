@@ -120,8 +120,9 @@ LpPlan plan_lp(const cat_shape* s, int top_k) {
     return p;
 }
 
-// Rows of up to this many get the row kernel's large CTAs.
-constexpr long long kFewRows = 2 * kPlanSMs;
+// Up to this many rows, with more than a few alternatives, get the row kernel's large CTAs (3 rows of 656 x 3936, one alternative: 18.8 us with
+// them, 17.2 without; 58 rows of 272 x 2915, twenty: 20.6 and 26.8).
+constexpr long long kFewRows = 2 * kPlanSMs, kFewAlternatives = 4;
 
 template <class TI, class TZ, bool TOP>
 int launch_lp_rows(const cat_shape* s, const LpPlan& plan, const TI* H, const TI* W, long long r0, long long rws, int S, uint8_t* ws,
@@ -155,7 +156,7 @@ int launch_lp_rows(const cat_shape* s, const LpPlan& plan, const TI* H, const TI
     // launched ahead of the logits kernel's end, for which it waits: a decoding step is short enough for the 2 us to show
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(rws), 1, 1);
-    const bool few = rws <= kFewRows;
+    const bool few = rws <= kFewRows && top_k > kFewAlternatives;
     cfg.blockDim = dim3(few ? lp::RT_FEW : lp::RT_MANY, 1, 1);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
