@@ -425,7 +425,8 @@ int cat_logprob_fwd(const cat_shape* shape, const void* H, const void* W, const 
  * kept as two terms, unless slab_mib cuts the vocabulary).  Rows with
  * valid[r] == 0 get a zero dH row and add nothing to dW, whatever H holds there; a label that is no token id
  * contributes through the entropy only.  No gradient flows through the alternatives.
- *   lse, entropy   [T] fp32 as written by cat_logprob_fwd; entropy may be NULL without grad_entropy   (device, in)
+ *   lse, entropy   [T] fp32 as written by cat_logprob_fwd for the same rows of H and the same W (a row's gradient by its
+ *                  logits is taken to sum to zero); entropy may be NULL without grad_entropy   (device, in)
  *   grad_logp      [T] fp32, or NULL (then labels may be NULL too)                 (device, in)
  *   grad_entropy   [T] fp32, or NULL                                               (device, in)
  *   dH [T, d] of in_dtype with pitch ldH;  dW [V, d] of dW_dtype with pitch ldW; accumulate_dW as in cat_loss_bwd

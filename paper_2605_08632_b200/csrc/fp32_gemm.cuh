@@ -50,6 +50,7 @@ struct EpiParams {
     const float* entropy;
     const float* grad_logp;
     const float* grad_entropy;
+    const float* dz_label;       // the label's entry, with grad_logp; nullptr: label_kernel writes it
     float* dz;
     long long ld_dz;
     int v0;
@@ -195,7 +196,7 @@ __global__ void __launch_bounds__(THREADS, 4) gemm_kernel(const Operands op, con
                     s_m[at] = m_new;
                 }
             } else if (row < op.M) {
-                float gl = 0.f, ca = 0.f, cb = 0.f, lse = 0.f;
+                float dz_y = 0.f, ca = 0.f, cb = 0.f, lse = 0.f;
                 int y = -1;
                 bool on = false;
                 if (MODE == DZ) {
@@ -203,7 +204,7 @@ __global__ void __launch_bounds__(THREADS, 4) gemm_kernel(const Operands op, con
                     if (on) {
                         lse = ep.lse[row];
                         const long long yy = ep.grad_logp ? ep.labels[row] : -1;
-                        if (yy >= 0 && yy < ep.V) { y = static_cast<int>(yy) - ep.v0; gl = ep.grad_logp[row]; ca = -gl; }
+                        if (yy >= 0 && yy < ep.V) { y = static_cast<int>(yy) - ep.v0; dz_y = ep.dz_label ? ep.dz_label[row] : 0.f; ca = -ep.grad_logp[row]; }
                         if (ep.grad_entropy) { cb = -ep.grad_entropy[row]; ca = fmaf(cb, ep.entropy[row], ca); }
                     }
                 }
@@ -213,8 +214,7 @@ __global__ void __launch_bounds__(THREADS, 4) gemm_kernel(const Operands op, con
                     if (col >= op.N) continue;
                     if (MODE == DZ) {
                         const float x = total[i][j] - lse;
-                        float v = expf(x) * fmaf(cb, x, ca);
-                        if (col == y) v += gl;
+                        const float v = col == y ? dz_y : expf(x) * fmaf(cb, x, ca);
                         ep.dz[row * ep.ld_dz + col] = on ? v : 0.f;
                     } else if (gridDim.z > 1) {
                         ep.out[blockIdx.z * ep.part_stride + row * ep.ld_out + col] = total[i][j];
@@ -238,6 +238,27 @@ __global__ void __launch_bounds__(THREADS, 4) gemm_kernel(const Operands op, con
             ep.part_l[at] = s_l[q];
             if (ep.part_u != nullptr) { ep.part_u[at] = s_u[q]; ep.part_id[at] = s_id[q]; }
         }
+    }
+}
+
+// The labels' entries of dz, one CTA per row.  A row of dz sums to zero, so its label's entry is the others' sum with the sign turned: as
+// exact as they are, where gl (1 - p) of a row that is sure of its label keeps the rounding of z and lse (1e-6 of lse) against 1 - p.
+__global__ void __launch_bounds__(256) label_kernel(float* dz, long long ld, int V, const long long* labels, const unsigned char* valid) {
+    __shared__ float s_sum[8];
+    const long long row = blockIdx.x;
+    const long long y = labels[row];
+    if ((valid != nullptr && valid[row] == 0) || y < 0 || y >= V) return;
+    float* z = dz + row * ld;
+    float sum = 0.f;
+    for (int v = threadIdx.x; v < V; v += 256) sum += v == y ? 0.f : z[v];
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int i = 1; i < 8; ++i) sum += s_sum[i];
+        z[y] = 0.f - sum;
     }
 }
 

@@ -223,7 +223,7 @@ int lp_slab(const cat_shape* s, const LpPlan& plan, const CUtensorMap& tmW, cons
 struct LpBwdPlan {
     BwdPlan b;
     long long lo;          // rows before the second terms of dz, or 0
-    size_t off_h, off_part, total;
+    size_t off_h, off_label, off_part, total;
 };
 
 LpBwdPlan plan_lp_bwd(const cat_shape* s) {
@@ -239,6 +239,7 @@ LpBwdPlan plan_lp_bwd(const cat_shape* s) {
     if (p.lo == 0) p.b = plan_bwd(s);
     size_t off = align256(p.b.total);
     p.off_h = off;    off = align256(off + (bf16 ? 2 : 4) * static_cast<size_t>(t.T) * static_cast<size_t>(s->d));
+    p.off_label = off; off = align256(off + sizeof(float) * static_cast<size_t>(s->T));
     p.off_part = off;
     off += !bf16 ? kF32PartBytes : p.b.n_slabs == 1 ? dh_part_bytes(t.T, s->d, s->V, p.lo > 0) : 0;
     p.total = off;
@@ -251,6 +252,21 @@ struct LpGrads {
     const float *lse, *entropy, *grad_logp, *grad_entropy;
 };
 
+// The rows of H as the dW contraction takes them (in `copy`), and the labels' entries of dz; NULL: not wanted.
+template <class TI>
+int launch_bwd_rows(const cat_shape* s, const TI* H, const TI* W, const LpGrads& a, long long rows, long long lo, TI* copy, float* dz_label,
+                    cudaStream_t st) {
+    if (copy == nullptr && (a.grad_logp == nullptr || dz_label == nullptr)) return CAT_OK;
+    lp::BwdRows<TI> p;
+    p.H = H; p.W = W; p.ldH = s->ldH; p.ldW = s->ldW;
+    p.d = static_cast<int>(s->d); p.T = static_cast<int>(s->T); p.V = static_cast<int>(s->V);
+    p.valid = a.valid; p.labels = reinterpret_cast<const long long*>(a.labels); p.lse = a.lse; p.entropy = a.entropy;
+    p.grad_logp = dz_label ? a.grad_logp : nullptr; p.grad_entropy = a.grad_entropy;
+    p.dz_label = dz_label; p.out = copy; p.lo = static_cast<int>(lo);
+    lp::bwd_rows_kernel<TI><<<static_cast<unsigned>(rows), lp::THREADS, 0, st>>>(p);
+    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+}
+
 int lp_bwd_bf16(const cat_shape* s, const LpBwdPlan& plan, const __nv_bfloat16* H, const __nv_bfloat16* W, const LpGrads& a,
                 __nv_bfloat16* dH, void* dW, int accumulate_dW, uint8_t* ws, int sm_count, cudaStream_t st) {
     int* status = reinterpret_cast<int*>(ws);
@@ -260,11 +276,9 @@ int lp_bwd_bf16(const cat_shape* s, const LpBwdPlan& plan, const __nv_bfloat16* 
     const int d = static_cast<int>(s->d);
     const long long rows = plan.lo > 0 ? 2 * plan.lo : s->T;             // of dz
     const bool copy_H = a.valid != nullptr || plan.lo > 0;
-    if (copy_H) {
-        lp::masked_copy_kernel<<<static_cast<unsigned>(rows), lp::THREADS, 0, st>>>(H, s->ldH, d, a.valid, static_cast<int>(s->T),
-                                                                                   static_cast<int>(plan.lo), Hz);
-        if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
-    }
+    float* dz_label = reinterpret_cast<float*>(ws + plan.off_label);
+    const int first_rc = launch_bwd_rows(s, H, W, a, rows, plan.lo, copy_H ? Hz : nullptr, dz_label, st);
+    if (first_rc != CAT_OK) return first_rc;
     CUtensorMap tmH_k, tmH_mn;
     if (tmap_a(&tmH_k, H, s->T, s->d, s->ldH) != CAT_OK ||
         tmap_mn_major(&tmH_mn, copy_H ? Hz : H, rows, s->d, copy_H ? s->d : s->ldH) != CAT_OK)
@@ -281,7 +295,7 @@ int lp_bwd_bf16(const cat_shape* s, const LpBwdPlan& plan, const __nv_bfloat16* 
             return CAT_ERR_CUDA;
         tc::EpiDzLp::Params zp;
         zp.labels = reinterpret_cast<const long long*>(a.labels); zp.valid = a.valid; zp.lse = a.lse; zp.entropy = a.entropy;
-        zp.grad_logp = a.grad_logp; zp.grad_entropy = a.grad_entropy; zp.T = static_cast<int>(s->T); zp.V = static_cast<int>(s->V);
+        zp.grad_logp = a.grad_logp; zp.grad_entropy = a.grad_entropy; zp.dz_label = dz_label; zp.T = static_cast<int>(s->T); zp.V = static_cast<int>(s->V);
         zp.v0 = static_cast<int>(v0); zp.lo_rows = static_cast<int>(plan.lo);
         int rc = launch_tc<0, 0, tc::EpiDzLp>(tmH_k, tmW_k, make_sched(s->T, width, s->d, fwd_splits(s->T, width), band_tiles(s->d), 0), zp,
                                               status, sm_count, st, &tmDz_out);
@@ -320,10 +334,10 @@ int lp_bwd_f32(const cat_shape* s, const LpBwdPlan& plan, const float* H, const 
     float* Hz = reinterpret_cast<float*>(ws + plan.off_h);
     float* part = reinterpret_cast<float*>(ws + plan.off_part);
     const int T = static_cast<int>(s->T), d = static_cast<int>(s->d);
-    if (a.valid) {
-        lp::masked_copy_kernel<<<static_cast<unsigned>(T), lp::THREADS, 0, st>>>(H, s->ldH, d, a.valid, T, 0, Hz);
-        if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
-    }
+    const bool whole = plan.b.n_slabs == 1 && a.grad_logp != nullptr;        // whole rows of dz at a time: see f32::label_kernel
+    float* dz_label = whole ? nullptr : reinterpret_cast<float*>(ws + plan.off_label);
+    const int first_rc = launch_bwd_rows(s, H, W, a, s->T, 0, a.valid ? Hz : nullptr, dz_label, st);
+    if (first_rc != CAT_OK) return first_rc;
     for (int sl = 0; sl < plan.b.n_slabs; ++sl) {
         const long long v0 = static_cast<long long>(sl) * plan.b.Vs;
         const int w = static_cast<int>((s->V - v0) < plan.b.Vs ? (s->V - v0) : plan.b.Vs);
@@ -334,9 +348,10 @@ int lp_bwd_f32(const cat_shape* s, const LpBwdPlan& plan, const float* H, const 
         op.A = H; op.sAm = s->ldH; op.sAk = 1; op.B = Wf; op.sBk = 1; op.sBn = s->ldW;
         op.M = T; op.N = w; op.Kd = d; op.n_groups = static_cast<int>(cdiv(w, f32::TN));
         ep.labels = reinterpret_cast<const long long*>(a.labels); ep.valid = a.valid; ep.lse = a.lse; ep.entropy = a.entropy;
-        ep.grad_logp = a.grad_logp; ep.grad_entropy = a.grad_entropy; ep.dz = dz; ep.ld_dz = plan.b.Vs; ep.V = static_cast<int>(s->V);
+        ep.grad_logp = a.grad_logp; ep.grad_entropy = a.grad_entropy; ep.dz_label = dz_label; ep.dz = dz; ep.ld_dz = plan.b.Vs; ep.V = static_cast<int>(s->V);
         ep.v0 = static_cast<int>(v0);
         f32::gemm_kernel<f32::DZ, true, true><<<dim3(static_cast<unsigned>(cdiv(T, f32::TM)), static_cast<unsigned>(op.n_groups)), f32::THREADS, 0, st>>>(op, ep);
+        if (whole) f32::label_kernel<<<static_cast<unsigned>(T), 256, 0, st>>>(dz, plan.b.Vs, w, ep.labels, a.valid);
         if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
         int rc = launch_f32_dw(dz, plan.b.Vs, a.valid ? Hz : H, a.valid ? s->d : s->ldH, w, d, T, nullptr, dW + v0 * s->ldW, s->ldW,
                                accumulate_dW != 0, part, st);
@@ -358,7 +373,7 @@ int check_topk_kd(const cat_topk_kd_desc* k) {
 struct TkPlan {
     FusedPlan f;
     int ld_zt;             // k + 1 logits per row: the list's and the label's
-    size_t off_valid, off_zt, off_kd_row, off_id, off_m1, off_l1, off_part, total;
+    size_t off_valid, off_zt, off_kd_row, off_id, off_u, off_m1, off_l1, off_part, total;
 };
 
 TkPlan plan_tk(const cat_shape* s, int k) {
@@ -399,6 +414,7 @@ TkPlan plan_tk(const cat_shape* s, int k) {
     p.off_zt = off;     off = align256(off + sizeof(float) * static_cast<size_t>(p.f.Ts) * p.ld_zt);
     p.off_kd_row = off; off = align256(off + sizeof(float) * s->T);
     p.off_id = off;     off = align256(off + sizeof(int) * p.f.S_max * (s->in_dtype == CAT_BF16 ? s->T : 1));
+    p.off_u = off;      off = align256(off + sizeof(float) * p.f.S_max * (s->in_dtype == CAT_BF16 ? s->T : 1));
     p.off_m1 = off;     off = align256(off + sizeof(float) * s->T);
     p.off_l1 = off;     off = align256(off + sizeof(float) * s->T);
     p.off_part = off;
@@ -472,6 +488,7 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
     float* zt = reinterpret_cast<float*>(ws + plan.off_zt);
     float* kd_row = reinterpret_cast<float*>(ws + plan.off_kd_row);
     int* part_id = reinterpret_cast<int*>(ws + plan.off_id);
+    float* part_u = reinterpret_cast<float*>(ws + plan.off_u);
     float* m1 = reinterpret_cast<float*>(ws + plan.off_m1);
     float* l1 = reinterpret_cast<float*>(ws + plan.off_l1);
     unsigned char* ok = ws + plan.off_valid;
@@ -509,11 +526,11 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
             if (tmap_a(&tmH_k, Hs, rws, s->d, s->ldH) != CAT_OK || tmap_out(&tmZ_out, zs, rws, s->V, f.ldz) != CAT_OK) return CAT_ERR_CUDA;
             tc::EpiFwdRef::Params ep;
             ep.labels = y + r0; ep.part_m = part_m + r0; ep.part_l = part_l + r0; ep.z_label = z_label + r0; ep.ref = ref + r0;
-            ep.part_id = part_id + r0; ep.part_stride = T; ep.T = static_cast<int>(rws); ep.V = V;
+            ep.part_u = part_u + r0; ep.part_id = part_id + r0; ep.part_stride = T; ep.T = static_cast<int>(rws); ep.V = V;
             const int rc = launch_tc<0, 0, tc::EpiFwdRef>(tmH_k, tmW_k, make_sched(rws, s->V, s->d, S, band_tiles(s->d), 0), ep, status,
                                                           sm_count, st, &tmZ_out);
             if (rc != CAT_OK) return rc;
-            mp.part_m = ep.part_m; mp.part_l = ep.part_l; mp.part_id = ep.part_id; mp.part_stride = T;
+            mp.part_m = ep.part_m; mp.part_l = ep.part_l; mp.part_u = ep.part_u; mp.part_id = ep.part_id; mp.part_stride = T;
         } else {
             f32::Operands op;
             op.A = reinterpret_cast<const float*>(Hs); op.sAm = s->ldH; op.sAk = 1;
@@ -524,7 +541,7 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
             ep.labels = y + r0; ep.part_m = part_m; ep.part_l = part_l; ep.z_label = z_label + r0; ep.V = V;
             ep.zs = static_cast<float*>(zs); ep.ld_z = f.ldz;
             f32::gemm_kernel<f32::FWD, true, true><<<dim3(static_cast<unsigned>(cdiv(rws, f32::TM)), static_cast<unsigned>(S)), f32::THREADS, 0, st>>>(op, ep);
-            mp.part_m = part_m; mp.part_l = part_l; mp.part_id = nullptr; mp.part_stride = rws;
+            mp.part_m = part_m; mp.part_l = part_l; mp.part_u = nullptr; mp.part_id = nullptr; mp.part_stride = rws;
         }
         mp.S = S; mp.H = Hs; mp.W = W; mp.ldH = s->ldH; mp.ldW = s->ldW; mp.d = d; mp.V = V; mp.labels = y + r0; mp.valid = ok + r0;
         mp.z_exact = zt + lists.k; mp.ld_exact = plan.ld_zt; mp.z_label = z_label + r0; mp.m1 = m1 + r0; mp.l1 = l1 + r0;

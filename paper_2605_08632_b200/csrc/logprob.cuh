@@ -179,6 +179,7 @@ struct EpiDzLp {
         const float* entropy;          // [T]; nullptr without grad_entropy
         const float* grad_logp;        // [T] or nullptr
         const float* grad_entropy;     // [T] or nullptr
+        const float* dz_label;         // [T] the label's entry, with grad_logp (see bwd_rows_kernel)
         int T;
         int V;
         int v0;
@@ -186,8 +187,8 @@ struct EpiDzLp {
     };
     struct State {
         float l2;                      // lse * log2 e
-        float ca, cb;                  // dz = p (ca + cb log2 p) + gl [v = y]
-        float gl;
+        float ca, cb;                  // dz = p (ca + cb log2 p), the label's entry apart
+        float dz_y;
         int y_rel;
         bool on;                       // the row takes part; one that does not gets zeros whatever its logits are
         int row;
@@ -195,7 +196,7 @@ struct EpiDzLp {
     __device__ static __forceinline__ void begin_item(const Params& p, State& s, int m_tile, int row_in_tile) {
         s.row = m_tile * BM + row_in_tile;
         s.l2 = 0.f;
-        s.ca = s.cb = s.gl = 0.f;
+        s.ca = s.cb = s.dz_y = 0.f;
         s.y_rel = -1;
         s.on = s.row < p.T && (p.valid == nullptr || p.valid[s.row] != 0);
         if (s.on) {
@@ -204,8 +205,8 @@ struct EpiDzLp {
                 const long long y = p.labels[s.row];
                 if (y >= 0 && y < p.V) {
                     s.y_rel = static_cast<int>(y) - p.v0;
-                    s.gl = p.grad_logp[s.row];
-                    s.ca = -s.gl;
+                    s.dz_y = p.dz_label[s.row];
+                    s.ca = -p.grad_logp[s.row];
                 }
             }
             if (p.grad_entropy) {
@@ -239,7 +240,7 @@ struct EpiDzLp {
             if (rel >= 0 && rel < 32) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    if (i == rel) f[i] += s.gl;
+                    if (i == rel) f[i] = s.dz_y;
             }
             if (live < 32 || !s.on) {
 #pragma unroll
@@ -401,7 +402,7 @@ struct Shared {
     float red[2][RW];
     int count[2][RW];
     int n_cand, n_near, n_rest;
-    float m, l, u, lse;
+    float m, l, u, logl;
     int id_max;
     double z_max, z_label;
     double z[CAP];                 // exact logits, where `err` says so
@@ -486,6 +487,12 @@ __device__ __forceinline__ float off_share(const S& sh) {
     return sizeof(TI) == 2 && sh.m > 1.f && fabsf(x) < 1.f ? x / sh.m : 0.f;
 }
 
+// z - lse.  In a row that is sure of its token this is the logarithm of 1 + a little, of which lse rounded to fp32 would leave few places.
+template <class S>
+__device__ __forceinline__ float log_prob(double z, const S& sh) {
+    return static_cast<float>((z - static_cast<double>(sh.m)) - static_cast<double>(sh.logl));
+}
+
 // lse and entropy from the merged sums and the exact largest logit, and the label's log probability; one thread.
 template <class TI, class TZ, int RT>
 __device__ __forceinline__ void finish_row(const RowParams<TI, TZ>& p, long long r, Shared<RT>& sh) {
@@ -500,14 +507,14 @@ __device__ __forceinline__ void finish_row(const RowParams<TI, TZ>& p, long long
         l += expm1f(x);
         u = fmaf(x * tc::LOG2E, expf(x), u);
     }
-    const float lse = sh.m + logf(lc);
-    sh.lse = lse;
+    const float logl = logf(lc), lse = sh.m + logl;
+    sh.logl = logl;
     p.lse[r] = lse;
     const float ent = logf(l) - 0.6931471805599453f * u / l;
     p.entropy[r] = ent < 0.f ? 0.f : ent + (lse - lse);      // NaN for a row that is not finite
     if (p.logp != nullptr) {
         const long long y = p.labels[r];
-        p.logp[r] = (y >= 0 && y < p.V) ? static_cast<float>((y == sh.id_max ? sh.z_max : sh.z_label) - static_cast<double>(lse)) : 0.f;
+        p.logp[r] = (y >= 0 && y < p.V) ? log_prob(y == sh.id_max ? sh.z_max : sh.z_label, sh) : 0.f;
     }
 }
 
@@ -862,10 +869,9 @@ __global__ void __launch_bounds__(RT, 1024 / RT) row_kernel(const RowParams<TI, 
         if (threadIdx.x == 0) finish_row(p, r, sh);
         __syncthreads();
     }
-    const float lse = sh.lse;
     for (int i = threadIdx.x; i < p.k; i += RT) {
         ids_out[i] = i < kept ? sh.id_keep[i] : -1;
-        lp_out[i] = i < kept ? static_cast<float>(sh.z_keep[i] - static_cast<double>(lse)) : -INFINITY;
+        lp_out[i] = i < kept ? log_prob(sh.z_keep[i], sh) : -INFINITY;
     }
 }
 
@@ -907,12 +913,42 @@ __device__ __forceinline__ void copy_row(const TI* src, TI* dst, int d, bool on)
         for (int i = threadIdx.x; i < d; i += THREADS) dst[i] = on ? src[i] : static_cast<TI>(0);
     }
 }
-// Grid: rows of the copy.  lo > 0: rows T .. lo - 1 are zero and rows lo .. 2 lo - 1 a second copy, for dz in two terms.
 template <class TI>
-__global__ void __launch_bounds__(THREADS) masked_copy_kernel(const TI* H, long long ldH, int d, const unsigned char* valid, int T, int lo,
-                                                              TI* out) {
-    const long long at = blockIdx.x, r = lo > 0 && at >= lo ? at - lo : at;
-    copy_row(H + (r < T ? r : 0) * ldH, out + at * d, d, r < T && (valid == nullptr || valid[r] != 0));
+struct BwdRows {
+    const TI* H;
+    const TI* W;
+    long long ldH, ldW;
+    int d, T, V;
+    const unsigned char* valid;        // [T] or nullptr
+    const long long* labels;           // [T], with grad_logp
+    const float* lse;
+    const float* entropy;
+    const float* grad_logp;            // [T] or nullptr
+    const float* grad_entropy;         // [T] or nullptr
+    float* dz_label;                   // [T]
+    TI* out;                           // the copy, or nullptr
+    int lo;
+};
+// First pass of the gradients, one CTA per row of the copy: the copy (lo > 0: rows T .. lo - 1 are zero and rows lo .. 2 lo - 1 a second one,
+// for dz in two terms), and the label's entry of dz from its exact logit,
+//   dz[y] = -gl (e^x - 1) - ge e^x (x + entropy),  x = z[y] - lse.
+// In a row that is sure of its label this is small against e^x, and the error of the GEMM's logit (3e-6 of it) would stand against
+// 1 - p: of the gradient of a token of p = 0.9999, half.
+template <class TI>
+__global__ void __launch_bounds__(THREADS) bwd_rows_kernel(const BwdRows<TI> p) {
+    const long long at = blockIdx.x, r = p.lo > 0 && at >= p.lo ? at - p.lo : at;
+    const bool on = r < p.T && (p.valid == nullptr || p.valid[r] != 0);
+    const TI* h = p.H + (r < p.T ? r : 0) * p.ldH;
+    if (p.out != nullptr) copy_row(h, p.out + at * p.d, p.d, on);
+    if (p.grad_logp == nullptr || threadIdx.x >= 32 || !on || at >= p.T) return;
+    const long long y = p.labels[r];
+    if (y < 0 || y >= p.V) return;
+    const double z = warp_dot(h, p.W + y * p.ldW, p.d, static_cast<int>(threadIdx.x));
+    if (threadIdx.x != 0) return;
+    const float x = static_cast<float>(z - static_cast<double>(p.lse[r]));
+    float v = -p.grad_logp[r] * expm1f(x);
+    if (p.grad_entropy != nullptr) v = fmaf(-p.grad_entropy[r] * expf(x), x + p.entropy[r], v);
+    p.dz_label[r] = v;
 }
 
 }  // namespace lp

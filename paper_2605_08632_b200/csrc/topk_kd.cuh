@@ -40,6 +40,7 @@ struct EpiFwdRef {
         const long long* labels;   // [T]
         float* part_m;             // [n_groups][part_stride]
         float* part_l;
+        float* part_u;             // see RunningSums
         int* part_id;              // first column that holds the maximum
         float* z_label;            // [T]
         const float* ref;          // [T]
@@ -48,7 +49,7 @@ struct EpiFwdRef {
         int V;
     };
     struct State {
-        float m_run, l_run;
+        RunningSums r;
         float base;                // see pack_steps
         int id;
         int y;
@@ -56,8 +57,7 @@ struct EpiFwdRef {
     };
     __device__ static __forceinline__ void begin_item(const Params& p, State& s, int m_tile, int row_in_tile) {
         s.row = m_tile * BM + row_in_tile;
-        s.m_run = LP_LOW;
-        s.l_run = 0.f;
+        s.r.clear();
         s.id = 0;
         s.base = 0.f;
         s.y = -1;
@@ -95,29 +95,18 @@ struct EpiFwdRef {
                 p.z_label[s.row] = zy;
             }
             const float cmax = max_of(f);
-            if (cmax > s.m_run) s.id = col0 + c * 32 + first_at(f, cmax);
-            const float m_new = fmaxf(s.m_run, cmax);
-            const float mb = m_new * LOG2E;
-            const uint64_t l2e2 = ptx::pack_f32x2(LOG2E, LOG2E), nmb2 = ptx::pack_f32x2(-mb, -mb);
-            uint64_t sum2 = ptx::pack_f32x2(0.f, 0.f);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float x0, x1;
-                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(f[2 * i], f[2 * i + 1]), l2e2, nmb2), x0, x1);
-                sum2 = ptx::add_f32x2(sum2, ptx::pack_f32x2(ptx::ex2_approx(x0), ptx::ex2_approx(x1)));
-            }
-            float s0, s1;
-            ptx::unpack_f32x2(sum2, s0, s1);
-            s.l_run = fmaf(s.l_run, ptx::ex2_approx((s.m_run - m_new) * LOG2E), s0 + s1);
-            s.m_run = m_new;
+            if (cmax > s.r.m) s.id = col0 + c * 32 + first_at(f, cmax);
+            s.r.add(f, cmax);
         });
     }
     __device__ static __forceinline__ int out_rows(const Params& p) { return p.T; }
     __device__ static __forceinline__ void end_item(const Params& p, const State& s, int group) {
         if (s.row < p.T) {
-            p.part_m[static_cast<size_t>(group) * p.part_stride + s.row] = s.m_run;
-            p.part_l[static_cast<size_t>(group) * p.part_stride + s.row] = s.l_run;
-            p.part_id[static_cast<size_t>(group) * p.part_stride + s.row] = s.id;
+            const size_t at = static_cast<size_t>(group) * p.part_stride + s.row;
+            p.part_m[at] = s.r.m;
+            p.part_l[at] = s.r.l;
+            p.part_u[at] = s.r.u;
+            p.part_id[at] = s.id;
         }
     }
 };
@@ -274,6 +263,7 @@ template <class TI>
 struct MergeParams {
     const float* part_m;           // [S][part_stride]
     const float* part_l;
+    const float* part_u;           // with part_id
     const int* part_id;            // nullptr: fp32 logits, nothing to correct
     long long part_stride;
     int S;
@@ -306,17 +296,32 @@ __global__ void __launch_bounds__(THREADS) merge_kernel(const MergeParams<TI> p)
         const int oid = __shfl_xor_sync(0xffffffffu, id, off);
         if (om > m || (om == m && oid < id)) { m = om; id = oid; }
     }
-    float l = 0.f;
-    for (int s = lane; s < p.S; s += 32) l = fmaf(expf(p.part_m[s * p.part_stride + r] - m), p.part_l[s * p.part_stride + r], l);
+    float l = 0.f, zl = 0.f;       // sum exp(z - m), and exp(z - m) z
+    for (int s = lane; s < p.S; s += 32) {
+        const float ms = p.part_m[s * p.part_stride + r], e = expf(ms - m), ls = p.part_l[s * p.part_stride + r];
+        l = fmaf(e, ls, l);
+        if (p.part_id) zl = fmaf(e, fmaf(0.6931471805599453f, p.part_u[s * p.part_stride + r], ms * ls), zl);
+    }
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+    for (int off = 16; off > 0; off >>= 1) {
+        l += __shfl_xor_sync(0xffffffffu, l, off);
+        zl += __shfl_xor_sync(0xffffffffu, zl, off);
+    }
     if (p.valid[r]) {
         const float zy = p.z_exact[r * p.ld_exact];
         if (p.part_id && static_cast<unsigned>(id) < static_cast<unsigned>(p.V)) {      // a GEMM that timed out leaves anything here
             const bool is_label = p.labels[r] == id;
             const float z = is_label ? zy : lp::warp_dot_f32(p.H + r * p.ldH, p.W + id * p.ldW, p.d, lane);
-            if (fabsf(z - m) < 1.f) l += expm1f(z - m);
-            if (!is_label && fabsf(zy - p.z_label[r]) < 1.f) l += expf(p.z_label[r] - m) * expm1f(zy - p.z_label[r]);
+            const float x = z - m, ly = p.z_label[r];
+            zl -= m;
+            if (fabsf(x) < 1.f) l += expm1f(x);
+            if (!is_label) {
+                const float e = expf(ly - m);
+                zl = fmaf(-e, ly, zl);
+                if (fabsf(zy - ly) < 1.f) l = fmaf(e, expm1f(zy - ly), l);
+            }
+            // the others, taken to be off by the same share of themselves as the largest (see lp::off_share)
+            if (m > 1.f && fabsf(x) < 1.f) l = fmaf(x / m, zl, l);
         }
         __syncwarp();
         if (lane == 0) p.z_label[r] = zy;
