@@ -353,3 +353,87 @@ def test_module_gradients():
     head(h, None, valid.to(DEV))[1].sum().backward()             # without labels: the entropy alone
     dH, *_ = O.logprob_backward(H, W, None, valid, None, np.ones(T))
     assert np.linalg.norm(np64(h.grad) - dH) <= 1e-5 * np.linalg.norm(dH)
+
+
+def sure_rows(T, d, V, dtype, seed, rest):
+    """Rows whose label has all but about `rest` of the probability."""
+    g = torch.Generator().manual_seed(seed)
+    W = (0.02 * torch.randn(V, d, generator=g)).to(dtype)
+    y = torch.randint(0, V, (T,), generator=g)
+    Wy = W[y].float()
+    H = 0.3 * torch.randn(T, d, generator=g)
+    up = math.log(V / rest) - (H * Wy).sum(1)
+    H = (H + Wy * (up / (Wy * Wy).sum(1)).unsqueeze(1)).to(dtype)
+    return H, W, y
+
+
+@pytest.mark.parametrize("d,V,dtype,rest", [(96, 700, F32, 1e-5), (320, 3001, F32, 1e-4), (128, 2500, BF, 1e-2), (512, 1111, BF, 1e-2)])
+def test_gradient_of_rows_that_are_sure_of_their_label(d, V, dtype, rest):
+    """1 - p of such a row is small against p: the label's entry may not be the difference of a rounded p from 1.
+
+    Every entry v != y of dz is p_v gl with p_v off by a factor exp(e), |e| <= tol_z (its logit) + tol_l (lse), and the label's entry, gl (1 - p), is
+    off by no more than they are (fp32: their sum) or, from its exact logit (bf16), by the error of lse against 1 - p: lse = m + log l
+    rounds to U |lse| and log l to 2 U, and l is off by tol_z of its part outside the largest logit, 1 - p of it.  dH is one row of products
+    of dz with W: sum |dz| |W| times that, V + 16 roundings of its sum, and for bf16 the rounding of the result.
+    """
+    T = 6
+    H, W, y = sure_rows(T, d, V, dtype, 3, rest)
+    e = TokenLogProb(T, d, V, dtype=dtype, dW_dtype=dtype)
+    f = e.forward(H.to(DEV), W.to(DEV), y.to(DEV))
+    gl = torch.linspace(0.5, 2.0, T)
+    dH, _ = e.backward(H.to(DEV), W.to(DEV), y.to(DEV), None, gl.to(DEV))
+    bf16 = dtype == BF
+    z = np64(H) @ np64(W).T
+    m = z.max(1, keepdims=True)
+    lse = m[:, 0] + np.log(np.exp(z - m).sum(1))
+    p = np.exp(z - lse[:, None])
+    at = np.arange(T), y.numpy()
+    q = p.copy()
+    q[at] = 0.0
+    left = q.sum(1)                      # 1 - p, without the difference
+    # the others' logits are normal with s = |label's logit| / sqrt(d), and exp of them averages e^(s^2 / 2): at most 5.5 for these sizes
+    assert (left < 50 * rest).all() and (left > 0).all()
+    dz = -np.asarray(gl)[:, None] * q
+    dz[at] = np64(gl) * left
+    tol_z, tol_l = tolerances(np64(H), np64(W), np.ones(T, bool), z, bf16)
+    rel = tol_z + tol_l + 8 * U * np.abs(lse)
+    label = rel + (((U * np.abs(lse) + 4 * U) / left + tol_z) if bf16 else 0.0)
+    err = (np.abs(dz) * rel[:, None])
+    err[at] = np64(gl) * left * label
+    want = dz @ np64(W)
+    tol = err @ np.abs(np64(W)) + (V + 16) * U * (np.abs(dz) @ np.abs(np64(W)))
+    if bf16:                             # dz in two terms (2^-16 of it), the result rounded once
+        tol = tol * 1.01 + 2.0 ** -16 * (np.abs(dz) @ np.abs(np64(W))) + 2.0 ** -8 * np.abs(want)
+    assert np.all(np.abs(np64(dH) - want) <= tol)
+    # and its log probability, the logarithm of 1 - (1 - p): off by rel of 1 - p, and by the roundings of l near 1 and of log l
+    assert np.all(np.abs(np64(f.logp) - np.log1p(-left)) <= rel * left + 6 * U)
+
+
+@pytest.mark.parametrize("T,dtype", [(5, BF), (400, BF), (70, F32)])
+def test_a_label_among_the_alternatives_has_one_log_probability(T, dtype):
+    """The two outputs take the label's logit from the same sum, whichever way the other alternatives' are taken."""
+    H, W, y, valid = make(T, 768, 3000, dtype, seed=9, sure=0.9)
+    e = TokenLogProb(T, 768, 3000, top_k=12, dtype=dtype)
+    r = e.forward(H.to(DEV), W.to(DEV), y.to(DEV), valid.to(DEV))
+    there = r.top_ids == y.to(DEV).unsqueeze(1)
+    rows = there.any(1)
+    assert rows.sum() > T // 4
+    same = r.top_logp[there] == r.logp[rows]
+    assert bool(same.all())
+
+
+def test_alternatives_are_as_exact_as_the_label():
+    """Few rows: alternatives are fp32 sums of d products (four chains of d / 128 a lane, and the lanes' five steps), lse is off by at most the
+    tensor cores' truncation of what lies outside the largest logit, a tenth of it after the correction, and by its rounding."""
+    T, d, V, k = 3, 3928, 2048, 20
+    H, W, y, _ = make(T, d, V, BF, seed=4, masked=0.0, sure=1.0)
+    r = TokenLogProb(T, d, V, top_k=k, dtype=BF).forward(H.to(DEV), W.to(DEV), None)
+    z = np64(H) @ np64(W).T
+    lse = z.max(1) + np.log(np.exp(z - z.max(1, keepdims=True)).sum(1))
+    ids = np.argsort(-z, axis=1, kind="stable")[:, :k]
+    assert np.array_equal(r.top_ids.cpu().numpy(), ids)
+    size = np.abs(np64(H)) @ np.abs(np64(W)).T
+    sums = (d / 128 + 8) * U * np.take_along_axis(size, ids, 1)
+    cut = (d / 16) * 2 * U * np.abs(z).max(1)           # d / 16 truncations of a sum that stays within the largest logit: up to 2 U each
+    tol = sums + 0.2 * cut[:, None] + 4 * U * np.abs(lse)[:, None]
+    assert np.all(np.abs(np64(r.top_logp) - (np.take_along_axis(z, ids, 1) - lse[:, None])) <= tol)
