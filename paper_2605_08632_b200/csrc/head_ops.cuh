@@ -223,7 +223,8 @@ int lp_slab(const cat_shape* s, const LpPlan& plan, const CUtensorMap& tmW, cons
 struct LpBwdPlan {
     BwdPlan b;
     long long lo;          // rows before the second terms of dz, or 0
-    size_t off_h, off_label, off_part, total;
+    bool rest;             // labels' entries of dz to more than bf16 (kLabelRestRows)
+    size_t off_h, off_label, off_rest, off_part, total;
 };
 
 LpBwdPlan plan_lp_bwd(const cat_shape* s) {
@@ -240,8 +241,10 @@ LpBwdPlan plan_lp_bwd(const cat_shape* s) {
     size_t off = align256(p.b.total);
     p.off_h = off;    off = align256(off + (bf16 ? 2 : 4) * static_cast<size_t>(t.T) * static_cast<size_t>(s->d));
     p.off_label = off; off = align256(off + sizeof(float) * static_cast<size_t>(s->T));
+    p.rest = bf16 && p.lo == 0 && s->T <= kLabelRestRows && p.b.n_slabs == 1;
+    p.off_rest = off;  if (p.rest) off = align256(off + 4 * sizeof(float) * static_cast<size_t>(s->T));
     p.off_part = off;
-    off += !bf16 ? kF32PartBytes : p.b.n_slabs == 1 ? dh_part_bytes(t.T, s->d, s->V, p.lo > 0) : 0;
+    off += !bf16 ? kF32PartBytes : p.b.n_slabs == 1 ? dh_part_bytes(t.T, s->d, s->V, p.lo > 0 || p.rest) : 0;
     p.total = off;
     return p;
 }
@@ -255,7 +258,7 @@ struct LpGrads {
 // The rows of H as the dW contraction takes them (in `copy`), and the labels' entries of dz; NULL: not wanted.
 template <class TI>
 int launch_bwd_rows(const cat_shape* s, const TI* H, const TI* W, const LpGrads& a, long long rows, long long lo, TI* copy, float* dz_label,
-                    cudaStream_t st) {
+                    float* rest, cudaStream_t st) {
     if (copy == nullptr && (a.grad_logp == nullptr || dz_label == nullptr)) return CAT_OK;
     lp::BwdRows<TI> p;
     p.H = H; p.W = W; p.ldH = s->ldH; p.ldW = s->ldW;
@@ -263,6 +266,7 @@ int launch_bwd_rows(const cat_shape* s, const TI* H, const TI* W, const LpGrads&
     p.valid = a.valid; p.labels = reinterpret_cast<const long long*>(a.labels); p.lse = a.lse; p.entropy = a.entropy;
     p.grad_logp = dz_label ? a.grad_logp : nullptr; p.grad_entropy = a.grad_entropy;
     p.dz_label = dz_label; p.out = copy; p.lo = static_cast<int>(lo);
+    p.rest = rest; p.key = reinterpret_cast<int*>(rest) + s->T; p.from = p.key + s->T; p.coef = rest + 3 * s->T;
     lp::bwd_rows_kernel<TI><<<static_cast<unsigned>(rows), lp::THREADS, 0, st>>>(p);
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
@@ -277,7 +281,8 @@ int lp_bwd_bf16(const cat_shape* s, const LpBwdPlan& plan, const __nv_bfloat16* 
     const long long rows = plan.lo > 0 ? 2 * plan.lo : s->T;             // of dz
     const bool copy_H = a.valid != nullptr || plan.lo > 0;
     float* dz_label = reinterpret_cast<float*>(ws + plan.off_label);
-    const int first_rc = launch_bwd_rows(s, H, W, a, rows, plan.lo, copy_H ? Hz : nullptr, dz_label, st);
+    float* rest = plan.rest && a.grad_logp ? reinterpret_cast<float*>(ws + plan.off_rest) : nullptr;
+    const int first_rc = launch_bwd_rows(s, H, W, a, rows, plan.lo, copy_H ? Hz : nullptr, dz_label, rest, st);
     if (first_rc != CAT_OK) return first_rc;
     CUtensorMap tmH_k, tmH_mn;
     if (tmap_a(&tmH_k, H, s->T, s->d, s->ldH) != CAT_OK ||
@@ -310,11 +315,23 @@ int lp_bwd_bf16(const cat_shape* s, const LpBwdPlan& plan, const __nv_bfloat16* 
             ep.out_bf16 = static_cast<__nv_bfloat16*>(dW) + v0 * s->ldW;
             if (accumulate_dW) ep.add_bf16 = ep.out_bf16;
         }
-        rc = launch_out<1, 1>(tmDz_mn, tmH_mn, make_sched(width, s->d, rows, 0, 1, 1), ep, status, sm_count, st);
+        const tc::Sched dw_sched = make_sched(width, s->d, rows, 0, 1, 1);
+        if (rest) {
+            tc::EpiOutT<true>::Params sp;
+            memset(&sp, 0, sizeof(sp));
+            sp.add_f32 = ep.add_f32; sp.add_bf16 = ep.add_bf16; sp.out_f32 = ep.out_f32; sp.out_bf16 = ep.out_bf16;
+            sp.ld_add = ep.ld_add; sp.ld_out = ep.ld_out; sp.M = ep.M; sp.N = ep.N;
+            sp.key = reinterpret_cast<int*>(rest) + s->T; sp.from = sp.key + s->T; sp.coef = rest + 3 * s->T;
+            sp.src = H; sp.ld_src = s->ldH; sp.n = static_cast<int>(s->T);
+            rc = launch_out<1, 1, true>(tmDz_mn, tmH_mn, dw_sched, sp, status, sm_count, st);
+        } else {
+            rc = launch_out<1, 1>(tmDz_mn, tmH_mn, dw_sched, ep, status, sm_count, st);
+        }
         if (rc != CAT_OK) return rc;
         if (plan.b.n_slabs == 1) {
+            const lp::LabelRest label{rest, reinterpret_cast<const long long*>(a.labels), W, s->ldW};
             rc = launch_dh(tmDz_k, tmW_mn, s->T, s->d, s->V, nullptr, dH, s->ldH, reinterpret_cast<float*>(ws + plan.off_part), status, sm_count,
-                           st, plan.lo);
+                           st, plan.lo, rest ? &label : nullptr);
         } else {
             memset(&ep, 0, sizeof(ep));
             ep.M = static_cast<int>(s->T); ep.N = d;
@@ -336,7 +353,7 @@ int lp_bwd_f32(const cat_shape* s, const LpBwdPlan& plan, const float* H, const 
     const int T = static_cast<int>(s->T), d = static_cast<int>(s->d);
     const bool whole = plan.b.n_slabs == 1 && a.grad_logp != nullptr;        // whole rows of dz at a time: see f32::label_kernel
     float* dz_label = whole ? nullptr : reinterpret_cast<float*>(ws + plan.off_label);
-    const int first_rc = launch_bwd_rows(s, H, W, a, s->T, 0, a.valid ? Hz : nullptr, dz_label, st);
+    const int first_rc = launch_bwd_rows(s, H, W, a, s->T, 0, a.valid ? Hz : nullptr, dz_label, nullptr, st);
     if (first_rc != CAT_OK) return first_rc;
     for (int sl = 0; sl < plan.b.n_slabs; ++sl) {
         const long long v0 = static_cast<long long>(sl) * plan.b.Vs;

@@ -875,12 +875,23 @@ __global__ void __launch_bounds__(RT, 1024 / RT) row_kernel(const RowParams<TI, 
     }
 }
 
+// What the rounding to bf16 left of the labels' entries of dz, for the result to have it all the same: rest[r] W[labels[r], :] in dH,
+// rest[r] H[r, :] in row labels[r] of dW (as tc::SparseTerms).
+struct LabelRest {
+    const float* rest;                 // [T], 0 in rows without a label; nullptr: not wanted
+    const long long* labels;
+    const __nv_bfloat16* W;
+    long long ldW;
+};
+
 // dH = scale * (part 0 + part 1 + ...), in that order, in bf16.  One CTA per row; `stride` elements from part to part.  lo > 0: each part
 // has a second term in row lo + r.
 __global__ void __launch_bounds__(THREADS) add_parts_kernel(const float* part, int n, long long stride, int d, const float* scale,
-                                                            __nv_bfloat16* out, long long ld, long long lo) {
+                                                            __nv_bfloat16* out, long long ld, long long lo, const LabelRest label) {
     const long long r = blockIdx.x;
     const float a = scale ? *scale : 1.f;
+    const float left = label.rest != nullptr ? label.rest[r] : 0.f;
+    const uint2* w = left != 0.f ? reinterpret_cast<const uint2*>(label.W + label.labels[r] * label.ldW) : nullptr;
     for (int i = threadIdx.x; i < d / 4; i += THREADS) {
         const float4* src = reinterpret_cast<const float4*>(part + r * d) + i;
         float4 s = __ldcs(src);
@@ -894,6 +905,11 @@ __global__ void __launch_bounds__(THREADS) add_parts_kernel(const float* part, i
                 const float4 x = __ldcs(src + g * (stride / 4) + lo * d / 4);
                 s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
             }
+        }
+        if (left != 0.f) {
+            const uint2 x = __ldg(w + i);
+            s.x = fmaf(left, __uint_as_float(x.x << 16), s.x); s.y = fmaf(left, __uint_as_float(x.x & 0xffff0000u), s.y);
+            s.z = fmaf(left, __uint_as_float(x.y << 16), s.z); s.w = fmaf(left, __uint_as_float(x.y & 0xffff0000u), s.w);
         }
         uint2 o;
         o.x = ptx::pack_bf16x2(a * s.x, a * s.y);
@@ -928,6 +944,11 @@ struct BwdRows {
     float* dz_label;                   // [T]
     TI* out;                           // the copy, or nullptr
     int lo;
+    // LabelRest, and the same sorted by label and row: [T] each, or nullptr (rows without a label: 0, and INT_MAX at the end)
+    float* rest;
+    int* key;
+    int* from;
+    float* coef;
 };
 // First pass of the gradients, one CTA per row of the copy: the copy (lo > 0: rows T .. lo - 1 are zero and rows lo .. 2 lo - 1 a second one,
 // for dz in two terms), and the label's entry of dz from its exact logit,
@@ -940,15 +961,32 @@ __global__ void __launch_bounds__(THREADS) bwd_rows_kernel(const BwdRows<TI> p) 
     const bool on = r < p.T && (p.valid == nullptr || p.valid[r] != 0);
     const TI* h = p.H + (r < p.T ? r : 0) * p.ldH;
     if (p.out != nullptr) copy_row(h, p.out + at * p.d, p.d, on);
-    if (p.grad_logp == nullptr || threadIdx.x >= 32 || !on || at >= p.T) return;
-    const long long y = p.labels[r];
-    if (y < 0 || y >= p.V) return;
-    const double z = warp_dot(h, p.W + y * p.ldW, p.d, static_cast<int>(threadIdx.x));
+    if (p.grad_logp == nullptr || at >= p.T) return;
+    auto label = [&](long long q) {
+        const long long y = p.labels[q];
+        return (p.valid == nullptr || p.valid[q] != 0) && y >= 0 && y < p.V ? static_cast<int>(y) : INT_MAX;
+    };
+    const int y = label(r);
+    int rank = 0;
+    if (p.rest != nullptr) {
+        for (int q0 = 0; q0 < p.T; q0 += THREADS) {
+            const int q = q0 + threadIdx.x, k = q < p.T ? label(q) : INT_MAX;
+            rank += __syncthreads_count(q < p.T && (k < y || (k == y && q < r)));
+        }
+        if (threadIdx.x == 0) {
+            p.key[rank] = y;
+            p.from[rank] = static_cast<int>(r);
+            if (y == INT_MAX) p.rest[r] = p.coef[rank] = 0.f;
+        }
+    }
+    if (threadIdx.x >= 32 || y == INT_MAX) return;
+    const double z = warp_dot(h, p.W + static_cast<long long>(y) * p.ldW, p.d, static_cast<int>(threadIdx.x));
     if (threadIdx.x != 0) return;
     const float x = static_cast<float>(z - static_cast<double>(p.lse[r]));
     float v = -p.grad_logp[r] * expm1f(x);
     if (p.grad_entropy != nullptr) v = fmaf(-p.grad_entropy[r] * expf(x), x + p.entropy[r], v);
     p.dz_label[r] = v;
+    if (p.rest != nullptr) p.rest[r] = p.coef[rank] = v - __bfloat162float(__float2bfloat16_rn(v));
 }
 
 }  // namespace lp

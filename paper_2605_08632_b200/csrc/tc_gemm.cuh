@@ -397,10 +397,26 @@ struct EpiDz {
     __device__ static __forceinline__ void end_item(const Params&, const State&, int) {}
 };
 
+// A few rows of another matrix for rows of an output, see EpiOutT.
+template <bool SPARSE>
+struct SparseTerms {};
+template <>
+struct SparseTerms<true> {
+    static constexpr int MAX_TERMS = 1024;
+    const int* key;                    // [n] rows of the output, rising
+    const int* from;                   // [n] rows of src
+    const float* coef;                 // [n]
+    const __nv_bfloat16* src;          // [..][ld_src], N columns
+    long long ld_src;
+    int n;
+};
+
 // Plain output: out = add + alpha * acc, fp32 or bf16, with optional fp32/bf16 addend
 // (dH accumulation across vocabulary slabs, accumulate_dW).
-struct EpiOut {
-    struct Params {
+// SPARSE: also out[key[i], :] += alpha coef[i] src[from[i], :], in the order of i, before the output is rounded.
+template <bool SPARSE>
+struct EpiOutT {
+    struct Params : SparseTerms<SPARSE> {
         const float* alpha;            // device scalar or nullptr (= 1)
         const float* row_scale;        // [M] per-output-row factor or nullptr (= 1)
         const float* add_f32;          // [M][ld_add] or nullptr
@@ -417,15 +433,71 @@ struct EpiOut {
     struct State {
         float alpha;
         int row;
+        int at, end, owner;            // SPARSE: the terms of the warp's rows; the lane and coefficient of the first
+        float coef;
     };
     __device__ static __forceinline__ void begin_item(const Params& p, State& s, int m_tile, int row_in_tile) {
         s.row = m_tile * BM + row_in_tile;
         s.alpha = p.alpha ? *p.alpha : 1.f;
         if (p.row_scale && s.row < p.M) s.alpha *= p.row_scale[s.row];
+        if constexpr (SPARSE) {
+            // the terms of the warp's 32 rows: the keys below the first, counted 32 apart and then one by one
+            const int lane = threadIdx.x & 31, row0 = s.row - lane;
+            const int step = (p.n + 31) >> 5;                       // n is at most MAX_TERMS, so at most 32
+            const bool below = lane * step < p.n && __ldg(p.key + lane * step) < row0;
+            const int n_below = __popc(__ballot_sync(0xffffffffu, below));
+            s.at = 0;
+            if (n_below > 0) {
+                const int i = (n_below - 1) * step + lane;
+                s.at = (n_below - 1) * step + __popc(__ballot_sync(0xffffffffu, lane < step && i < p.n && __ldg(p.key + i) < row0));
+            }
+            s.end = s.at;
+            while (s.end < p.n && __ldg(p.key + s.end) < min(row0 + 32, p.M)) ++s.end;
+            if (s.at < s.end) {
+                s.owner = __ldg(p.key + s.at) - row0;
+                s.coef = __ldg(p.coef + s.at);
+            }
+        }
+    }
+    // columns col0 + 8 lane .. + 7 of a term's row
+    __device__ static __forceinline__ uint4 term_row(const Params& p, int i, int col0) {
+        const int col = col0 + 8 * static_cast<int>(threadIdx.x & 31);
+        if constexpr (SPARSE)
+            if (col + 8 <= p.N) return __ldg(reinterpret_cast<const uint4*>(p.src + __ldg(p.from + i) * p.ld_src + col));
+        return make_uint4(0u, 0u, 0u, 0u);
+    }
+    // Chunk c of the tile's columns of the warp's terms.  A warp fetches a term's row of the tile in one load, a lane 8 columns, and hands them to
+    // the lane that has the term's output row.  (Lanes that read their own rows: dW of 300 rows of 1024 x 151936 176 us, this way 155,
+    // without terms 146.)
+    __device__ static __forceinline__ void add_terms(const Params& p, const State& s, int col0, int c, const uint4& first, uint32_t (&v)[32]) {
+        if constexpr (SPARSE) {
+            const int lane = threadIdx.x & 31;
+            for (int i = s.at; i < s.end; ++i) {
+                const uint4 x = i == s.at ? first : term_row(p, i, col0);
+                const int owner = i == s.at ? s.owner : __ldg(p.key + i) - (s.row - lane);
+                const float a = lane == owner ? (i == s.at ? s.coef : __ldg(p.coef + i)) : 0.f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t w[4] = {__shfl_sync(0xffffffffu, x.x, 4 * c + q), __shfl_sync(0xffffffffu, x.y, 4 * c + q),
+                                           __shfl_sync(0xffffffffu, x.z, 4 * c + q), __shfl_sync(0xffffffffu, x.w, 4 * c + q)};
+                    if (lane == owner) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            v[8 * q + 2 * j] = __float_as_uint(fmaf(a, __uint_as_float(w[j] << 16), __uint_as_float(v[8 * q + 2 * j])));
+                            v[8 * q + 2 * j + 1] =
+                                __float_as_uint(fmaf(a, __uint_as_float(w[j] & 0xffff0000u), __uint_as_float(v[8 * q + 2 * j + 1])));
+                        }
+                    }
+                }
+            }
+        }
     }
     __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage& o) {
         const int col0 = n_tile * BN;
         const bool row_ok = s.row < p.M;
+        uint4 first = make_uint4(0u, 0u, 0u, 0u);
+        if constexpr (SPARSE)
+            if (s.at < s.end) first = term_row(p, s.at, col0);
 #pragma unroll 1
         for (int c = 0; c < BN / 32; ++c) {
             if (col0 + c * 32 >= p.N) break;
@@ -433,6 +505,7 @@ struct EpiOut {
             uint32_t v[32];
             ptx::tmem_ld_32x32(taddr + c * 32, v);
             ptx::tmem_ld_wait();
+            add_terms(p, s, col0, c, first, v);
             if (p.staged == 2) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
@@ -497,6 +570,7 @@ struct EpiOut {
     __device__ static __forceinline__ int out_rows(const Params& p) { return p.staged ? p.M : 0; }
     __device__ static __forceinline__ void end_item(const Params&, const State&, int) {}
 };
+using EpiOut = EpiOutT<false>;
 
 // ------------------------------------------------------------------------------------------
 // The kernel.  tmA / tmB are 2-D tiled tensor maps with 128-byte swizzle:

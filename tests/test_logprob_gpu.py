@@ -437,3 +437,50 @@ def test_alternatives_are_as_exact_as_the_label():
     cut = (d / 16) * 2 * U * np.abs(z).max(1)           # d / 16 truncations of a sum that stays within the largest logit: up to 2 U each
     tol = sums + 0.2 * cut[:, None] + 4 * U * np.abs(lse)[:, None]
     assert np.all(np.abs(np64(r.top_logp) - (np.take_along_axis(z, ids, 1) - lse[:, None])) <= tol)
+
+
+@pytest.mark.parametrize("T,dW_dtype,accumulate,masked", [(129, BF, False, 0.3), (300, F32, False, 0.0), (300, BF, True, 0.2), (1024, F32, True, 0.1)])
+def test_labels_entries_of_dz_are_not_rounded(T, dW_dtype, accumulate, masked):
+    """Batches of 129 to 1024 bf16 rows: the label's entry of dz, nearly all of its row here, reaches both gradients unrounded, several rows of one
+    label among them.  What stays rounded (2^-8) is the rest of dz, p_v of about 1 / V each; fp32 sums add (T + 16) U; bf16
+    results are rounded once, 2^-8.  Were the labels' entries rounded, results would be off by up to 2^-8 more."""
+    d, V = 96, 2000
+    g = torch.Generator().manual_seed(T)
+    W = 0.01 * torch.randn(V, d, generator=g)
+    names = torch.tensor([3, 700, 701, 1280, V - 1])
+    W[names] *= 100.0
+    W = W.to(BF)
+    H = (0.01 * torch.randn(T, d, generator=g)).to(BF)
+    y = names[torch.randint(0, 5, (T,), generator=g)]
+    y[::17] = V + 1                                   # no token
+    valid = (torch.rand(T, generator=g) >= masked).to(torch.uint8)
+    gl = torch.randn(T, generator=g)
+    e = TokenLogProb(T, d, V, dtype=BF, dW_dtype=dW_dtype)
+    e.dW = torch.randn(V, d, generator=g).to(dW_dtype).to(DEV) if accumulate else None
+    before = np64(e.dW) if accumulate else 0.0
+    Hd = H.to(DEV)
+    Hd[(valid == 0).to(DEV)] = float("nan")
+    e.forward(Hd, W.to(DEV), y.to(DEV), valid.to(DEV))
+    dH, dW = e.backward(Hd, W.to(DEV), y.to(DEV), valid.to(DEV), gl.to(DEV), accumulate_dW=accumulate)
+    known = (valid.numpy() != 0) & (y.numpy() < V)
+    z = np64(H) @ np64(W).T
+    p = np.exp(z - z.max(1, keepdims=True))
+    p /= p.sum(1, keepdims=True)
+    c = np.where(known, np64(gl), 0.0)
+    rest = -c[:, None] * p
+    label = np.zeros_like(rest)
+    at = np.arange(T)[known], y.numpy()[known]
+    label[at] = c[known] * (1.0 - p[at])
+    rest[at] = 0.0
+    tol_z, tol_l = tolerances(np64(H), np64(W), known, z, True)
+    e_rest, e_label = 2.0 ** -8 + 2 * (tol_z + tol_l), 4 * (tol_z + tol_l) + (T + 16) * U
+    for got, want, size_rest, size_label, bf16 in (
+            (np64(dH), (rest + label) @ np64(W), np.abs(rest) @ np.abs(np64(W)), np.abs(label) @ np.abs(np64(W)), True),
+            (np64(dW), before + (rest + label).T @ np64(H), np.abs(rest).T @ np.abs(np64(H)), np.abs(label).T @ np.abs(np64(H)), dW_dtype == BF)):
+        tol = e_rest * size_rest + e_label * size_label + 4 * U * np.abs(want)
+        if bf16:
+            tol = tol * 1.01 + 2.0 ** -8 * np.abs(want)
+        assert np.all(np.abs(got - want) <= tol)
+    again = np64(dW)
+    if not accumulate:                                # in the order of the rows, whoever is first
+        assert np.array_equal(np64(e.backward(Hd, W.to(DEV), y.to(DEV), valid.to(DEV), gl.to(DEV))[1]), again)
