@@ -310,6 +310,8 @@ class TokenLogProb:
             if accumulate_dW:
                 raise ValueError("accumulate_dW needs a dW to add to: set engine.dW, or run one backward without it")
             self.dW = torch.empty(self.V, self.d, dtype=self.dW_dtype, device=self.device)
+        _check("dH", self.dH, (self.T, self.d), self.dtype, self.device)
+        _check("dW", self.dW, (self.V, self.d), self.dW_dtype, self.device)
         _on(self.device, B.cat_logprob_bwd, shape, H, W, labels, valid, lse, entropy, grad_logp, grad_entropy, self.dH, self.dW, accumulate_dW,
             self._ws_bwd)
         return self.dH, self.dW

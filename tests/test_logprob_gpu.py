@@ -484,3 +484,20 @@ def test_labels_entries_of_dz_are_not_rounded(T, dW_dtype, accumulate, masked):
     again = np64(dW)
     if not accumulate:                                # in the order of the rows, whoever is first
         assert np.array_equal(np64(e.backward(Hd, W.to(DEV), y.to(DEV), valid.to(DEV), gl.to(DEV))[1]), again)
+
+
+def test_gradient_buffers_of_the_user_are_checked():
+    T, d, V = 9, 64, 500
+    H, W, y, _ = make(T, d, V, BF, masked=0.0)
+    H, W, y = H.to(DEV), W.to(DEV), y.to(DEV)
+    e = TokenLogProb(T, d, V, dtype=BF, dW_dtype=BF)
+    e.forward(H, W, y)
+    g = torch.ones(T, device=DEV)
+    for bad in (torch.zeros(V, d, device=DEV), torch.zeros(V - 1, d, dtype=BF, device=DEV), torch.zeros(V, d, dtype=BF),
+                torch.zeros(d, V, dtype=BF, device=DEV).t()):
+        e.dW = bad
+        with pytest.raises((TypeError, ValueError), match="dW"):
+            e.backward(H, W, y, grad_logp=g)
+    e.dW, e.dH = None, torch.zeros(T + 1, d, dtype=BF, device=DEV)
+    with pytest.raises(ValueError, match="dH"):
+        e.backward(H, W, y, grad_logp=g)
