@@ -422,7 +422,7 @@ int cat_logprob_fwd(const cat_shape* shape, const void* H, const void* W, const 
  *     dz[r, v] = grad_logp[r] ([v == y_r] - p[r, v]) - grad_entropy[r] p[r, v] (log p[r, v] + entropy[r]),
  *     dH = dz W,   dW = dz^T H.
  * The logits are recomputed per vocabulary slab, as in cat_loss_bwd; dz is rounded once to in_dtype (for up to 128 bf16 rows
- * kept as two terms, unless slab_mib cuts the vocabulary).  Rows with
+ * kept as two terms, for up to 1024 the label's entry not rounded, unless slab_mib cuts the vocabulary).  Rows with
  * valid[r] == 0 get a zero dH row and add nothing to dW, whatever H holds there; a label that is no token id
  * contributes through the entropy only.  No gradient flows through the alternatives.
  *   lse, entropy   [T] fp32 as written by cat_logprob_fwd for the same rows of H and the same W (a row's gradient by its

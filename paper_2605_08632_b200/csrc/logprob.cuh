@@ -654,7 +654,7 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
 // up in the slab: a few groups of it are read, not the row.  The order is that of the exact products: candidates whose approximate
 // logits are closer than their errors are compared by fp64 sums (a gather of W for about one in twenty of them; taking all of them
 // again cost 0.7 ms for 8192 rows of k = 64, a quarter of the GEMM), and equal logits go to the lower id.
-// 12 us for one row, 256 us for 8192 rows of V = 128256, k = 64 (GEMM 2.85 ms): the bound 45, the list of groups 30, their look-up 78 (700
+// 14 us for one row of V = 128256, k = 20, 275 us for 8192 rows, k = 64 (GEMM 2.75 ms): the bound 45, the list of groups 30, their look-up 78 (700
 // thousand 64-byte reads all over the slab), ranking about 45, exact sums the rest.
 // More than CAP candidates (a row of zeros, many equal rows of W) are settled batch by batch by exact sums.
 template <class TI, class TZ, bool TOP, int RT>
