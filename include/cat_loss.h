@@ -407,7 +407,7 @@ int cat_kd_loss_fwd_bwd(const cat_shape* shape, const cat_kd_desc* desc, const v
  *   top_ids    [T, top_k] int64;  top_logp  [T, top_k] fp32                        (device, out)
  *   workspace  at least cat_logprob_workspace_bytes(shape, top_k, 0) bytes, 256-byte aligned
  * With top_k > 0 the workspace holds one row slab of logits (fp16, or fp32 for CAT_F32) of at most about slab_mib
- * MiB (default 3072; up to 128 rows of bf16 are taken at once whatever it says), never more than T rows.  Two launches per
+ * MiB (default 3 GiB; up to 128 rows of bf16 are taken at once whatever it says), never more than T rows.  Two launches per
  * slab and one memset.  The workspace's first int32 holds the
  * device status.  Calls that may overlap on the GPU need a workspace each.  Returns CAT_OK or a negative cat_status.
  */
@@ -454,7 +454,7 @@ size_t cat_logprob_workspace_bytes(const cat_shape* shape, int top_k, int pass);
  * A row takes part iff valid[r] != 0, 0 <= y_r < V and 0 <= t < L; H of the others may hold anything.  Confidences for the
  * weights: conf_ext, or the draft's own (for the teacher's: exp(logp) of cat_logprob_fwd through cat_conf_window).
  * Works in row slabs of whole draft blocks with the slab's logits kept (16 bits, relative to the largest logit among
- * the list's ids and the label; fp32 for CAT_F32), at most about slab_mib MiB (default 3072), turned into dz in place.
+ * the list's ids and the label; fp32 for CAT_F32), at most about slab_mib MiB (default 3 GiB), turned into dz in place.
  * bf16: a logit that lies more than 80 nats above every one that the row's list and label name enters dz as if 80 above
  * (the row's loss, lse and confidence are not affected).
  */

@@ -11,7 +11,8 @@
 //
 // Backward: the logits are recomputed per vocabulary slab and leave the GEMM as
 //   dz[v] = gl ([v = y] - p) - ge p (log p + entropy)
-// for upstream gradients gl (of logp) and ge (of the entropy); the dH and dW contractions follow.
+// for upstream gradients gl (of logp) and ge (of the entropy), the label's entry from its exact logit (bwd_rows_kernel); the dH and dW
+// contractions follow.
 #pragma once
 #include "rowops.cuh"
 #include "tc_gemm.cuh"
@@ -42,24 +43,6 @@ __device__ __forceinline__ float max_of(const float (&f)[32]) {
     a = ptx::max3_f32(a, f[27], f[28]);
     b = ptx::max3_f32(b, f[29], f[30]);
     return ptx::max3_f32(a, b, fmaxf(c, f[31]));
-}
-
-// A tile's accumulators in chunks of 32 columns, body(c, v) for each that holds columns below ncols: the next chunk is on its way
-// from tensor memory while the warp works on one.
-template <class F>
-__device__ __forceinline__ void walk_tile(uint32_t taddr, int ncols, F&& body) {
-    uint32_t a[32], b[32];
-    ptx::tmem_ld_32x32(taddr, a);
-#pragma unroll 1
-    for (int c = 0; c < BN / 32 && c * 32 < ncols; c += 2) {
-        ptx::tmem_ld_wait(a);
-        ptx::tmem_ld_32x32(taddr + (c + 1) * 32, b);
-        body(c, a);
-        ptx::tmem_ld_wait(b);
-        if (c + 2 < BN / 32) ptx::tmem_ld_32x32(taddr + (c + 2) * 32, a);
-        if ((c + 1) * 32 < ncols) body(c + 1, b);
-    }
-    ptx::tmem_ld_wait();
 }
 
 // l = sum exp(z - m) and u = sum exp2(x) x, x = (z - m) log2 e, with m the largest logit so far.

@@ -397,6 +397,24 @@ struct EpiDz {
     __device__ static __forceinline__ void end_item(const Params&, const State&, int) {}
 };
 
+// A tile's accumulators in chunks of 32 columns, body(c, v) for each that holds columns below ncols: the next chunk is on its way
+// from tensor memory while the warp works on one.
+template <class F>
+__device__ __forceinline__ void walk_tile(uint32_t taddr, int ncols, F&& body) {
+    uint32_t a[32], b[32];
+    ptx::tmem_ld_32x32(taddr, a);
+#pragma unroll 1
+    for (int c = 0; c < BN / 32 && c * 32 < ncols; c += 2) {
+        ptx::tmem_ld_wait(a);
+        ptx::tmem_ld_32x32(taddr + (c + 1) * 32, b);
+        body(c, a);
+        ptx::tmem_ld_wait(b);
+        if (c + 2 < BN / 32) ptx::tmem_ld_32x32(taddr + (c + 2) * 32, a);
+        if ((c + 1) * 32 < ncols) body(c + 1, b);
+    }
+    ptx::tmem_ld_wait();
+}
+
 // A few rows of another matrix for rows of an output, see EpiOutT.
 template <bool SPARSE>
 struct SparseTerms {};
@@ -468,7 +486,7 @@ struct EpiOutT {
     }
     // Chunk c of the tile's columns of the warp's terms.  A warp fetches a term's row of the tile in one load, a lane 8 columns, and hands them to
     // the lane that has the term's output row.  (Lanes that read their own rows: dW of 300 rows of 1024 x 151936 176 us, this way 155,
-    // without terms 146.)
+    // without terms 146; 142 since walk_tile reads ahead.)
     __device__ static __forceinline__ void add_terms(const Params& p, const State& s, int col0, int c, const uint4& first, uint32_t (&v)[32]) {
         if constexpr (SPARSE) {
             const int lane = threadIdx.x & 31;
@@ -498,15 +516,10 @@ struct EpiOutT {
         uint4 first = make_uint4(0u, 0u, 0u, 0u);
         if constexpr (SPARSE)
             if (s.at < s.end) first = term_row(p, s.at, col0);
-#pragma unroll 1
-        for (int c = 0; c < BN / 32; ++c) {
-            if (col0 + c * 32 >= p.N) break;
-            if (p.staged == 1 || (p.staged == 2 && (c & 1) == 0)) o.begin();
-            uint32_t v[32];
-            ptx::tmem_ld_32x32(taddr + c * 32, v);
-            ptx::tmem_ld_wait();
-            add_terms(p, s, col0, c, first, v);
-            if (p.staged == 2) {
+        if (p.staged == 2) {
+            walk_tile(taddr, p.N - col0, [&](int c, uint32_t (&v)[32]) {
+                if ((c & 1) == 0) o.begin();
+                add_terms(p, s, col0, c, first, v);
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     o.put((c & 1) * 4 + q, ptx::pack_bf16x2(s.alpha * __uint_as_float(v[8 * q]), s.alpha * __uint_as_float(v[8 * q + 1])),
@@ -514,8 +527,17 @@ struct EpiOutT {
                           ptx::pack_bf16x2(s.alpha * __uint_as_float(v[8 * q + 4]), s.alpha * __uint_as_float(v[8 * q + 5])),
                           ptx::pack_bf16x2(s.alpha * __uint_as_float(v[8 * q + 6]), s.alpha * __uint_as_float(v[8 * q + 7])));
                 if ((c & 1) != 0 || col0 + (c + 1) * 32 >= p.N) o.flush(col0 + (c >> 1) * 64);
-                continue;
-            }
+            });
+            return;
+        }
+#pragma unroll 1
+        for (int c = 0; c < BN / 32; ++c) {
+            if (col0 + c * 32 >= p.N) break;
+            if (p.staged) o.begin();
+            uint32_t v[32];
+            ptx::tmem_ld_32x32(taddr + c * 32, v);
+            ptx::tmem_ld_wait();
+            add_terms(p, s, col0, c, first, v);
             if (p.staged) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
