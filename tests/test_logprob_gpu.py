@@ -501,3 +501,35 @@ def test_gradient_buffers_of_the_user_are_checked():
     e.dW, e.dH = None, torch.zeros(T + 1, d, dtype=BF, device=DEV)
     with pytest.raises(ValueError, match="dH"):
         e.backward(H, W, y, grad_logp=g)
+
+
+@pytest.mark.parametrize("T", [1, 128, 129, 297, 1024, 1025])
+def test_captured_forward_and_backward_follow_new_inputs(T):
+    """Sizes on both sides of every rule on the number of rows: a replay gives what a plain call gives, bit for bit."""
+    d, V = 64, 1500
+
+    def inputs(seed):
+        H, W, y, valid = make(T, d, V, BF, seed=seed)
+        g = torch.Generator().manual_seed(seed)
+        return [t.to(DEV) for t in (H, W, y, valid, torch.randn(T, generator=g), 0.1 * torch.randn(T, generator=g))]
+
+    def both(e, H, W, y, valid, gl, ge):
+        return tuple(e.forward(H, W, y, valid)) + tuple(e.backward(H, W, y, valid, gl, ge))
+
+    e = TokenLogProb(T, d, V, top_k=6, dtype=BF, dW_dtype=BF)
+    held = inputs(1)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        both(e, *held)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            out = both(e, *held)
+    torch.cuda.synchronize()
+    new = inputs(2)
+    for a, b in zip(held, new):
+        a.copy_(b)
+    graph.replay()
+    torch.cuda.synchronize()
+    want = both(TokenLogProb(T, d, V, top_k=6, dtype=BF, dW_dtype=BF), *new)
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
