@@ -408,7 +408,7 @@ int cat_kd_loss_fwd_bwd(const cat_shape* shape, const cat_kd_desc* desc, const v
  *   workspace  at least cat_logprob_workspace_bytes(shape, top_k, 0) bytes, 256-byte aligned
  * With top_k > 0 the workspace holds one row slab of logits (fp16, or fp32 for CAT_F32) of at most about slab_mib
  * MiB (default 3 GiB; up to 128 rows of bf16 are taken at once whatever it says), never more than T rows.  Two launches per
- * slab and one memset.  The workspace's first int32 holds the
+ * slab, one that reads W once for more than 128 rows of bf16 with alternatives, and one memset.  The workspace's first int32 holds the
  * device status.  Calls that may overlap on the GPU need a workspace each.  Returns CAT_OK or a negative cat_status.
  */
 #define CAT_TOPK_MAX 256

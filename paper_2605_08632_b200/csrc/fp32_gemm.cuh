@@ -43,6 +43,7 @@ struct EpiParams {
     float* z_label;              // or nullptr
     float* zs;                   // [M][ld_z] logits, or nullptr
     float* gmax;                 // [M][ld_g] maxima of the tiles, or nullptr
+    int* w_sq;                   // raised to the largest sum of squares of a row of W (float bits), or nullptr
     long long ld_z, ld_g;
     // DZ: dz = gl ([v = y] - p) - ge p (log p + entropy); rows with valid = 0 get zeros
     const unsigned char* valid;
@@ -95,6 +96,10 @@ __global__ void __launch_bounds__(THREADS, 4) gemm_kernel(const Operands op, con
     const int ks0 = static_cast<int>((static_cast<long long>(blockIdx.z) * slices) / gridDim.z);
     const int ks1 = static_cast<int>((static_cast<long long>(blockIdx.z + 1) * slices) / gridDim.z);
 
+    // Sums of squares of B's columns (rows of W) as the slices pass: a thread's eight elements of a slice belong to columns 8 i + threadIdx.x / 16,
+    // and 16 lanes share a column.  By the first row tile's CTAs alone.
+    const bool squares = MODE == FWD && B_KC && ep.w_sq != nullptr && blockIdx.x == 0;
+    float most = 0.f;
     // running sums of the tile's rows over the group's tiles (kept here, not in registers: the 16 threads of a row all need them)
     __shared__ float s_m[TM], s_l[TM], s_u[TM];
     __shared__ int s_id[TM];
@@ -105,12 +110,19 @@ __global__ void __launch_bounds__(THREADS, 4) gemm_kernel(const Operands op, con
     for (int nt = nt0; nt < nt1; ++nt) {
         const int n0 = nt * TN;
         float total[8][4] = {}, acc[8][4] = {};
-        float av[8], bv[8];
+        float av[8], bv[8], sq[8] = {};
+        auto add_squares = [&] {
+            if (squares) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sq[i] = fmaf(bv[i], bv[i], sq[i]);
+            }
+        };
         fetch<A_KC>(op.A, op.sAm, op.sAk, m0, op.M, ks0 * TK, op.Kd, av);
         fetch<B_KC>(op.B, op.sBn, op.sBk, n0, op.N, ks0 * TK, op.Kd, bv);
         __syncthreads();              // the previous tile's last slice has been read
         put<A_KC>(As[0], av);
         put<B_KC>(Bs[0], bv);
+        add_squares();
         __syncthreads();
         for (int ks = ks0, run = 0; ks < ks1; ++ks) {
             const int buf = (ks - ks0) & 1;
@@ -142,7 +154,16 @@ __global__ void __launch_bounds__(THREADS, 4) gemm_kernel(const Operands op, con
             if (ks + 1 < ks1) {
                 put<A_KC>(As[buf ^ 1], av);
                 put<B_KC>(Bs[buf ^ 1], bv);
+                add_squares();
                 __syncthreads();
+            }
+        }
+        if (squares) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                for (int off = 1; off < 16; off <<= 1) sq[i] += __shfl_xor_sync(0xffffffffu, sq[i], off);
+                most = sq[i] <= most ? most : sq[i];        // NaN stays
             }
         }
 #pragma unroll
@@ -227,6 +248,7 @@ __global__ void __launch_bounds__(THREADS, 4) gemm_kernel(const Operands op, con
             }
         }
     }
+    if (squares && tx == 0) atomicMax(ep.w_sq, __float_as_int(most >= 0.f ? most : INFINITY));
     if (MODE == FWD && tx == 0) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {

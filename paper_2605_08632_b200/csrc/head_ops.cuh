@@ -52,7 +52,8 @@ int launch_skinny_as(const CUtensorMap& tmW, const CUtensorMap& tmH, const skinn
     auto kern = skinny::logits_kernel<TPW, HALVES, SUB>;
     static std::atomic<unsigned long long> allowed{0};
     if (!allow_smem(kern, skinny::SMEM_BYTES, allowed)) return CAT_ERR_CUDA;
-    kern<<<static_cast<unsigned>(grid), 64 + 128 * HALVES, skinny::SMEM_BYTES, st>>>(tmW, tmH, p, status);
+    const int threads = 64 + 128 * HALVES + (p.gmax != nullptr ? skinny::NORM_THREADS : 0);
+    kern<<<static_cast<unsigned>(grid), threads, skinny::SMEM_BYTES, st>>>(tmW, tmH, p, status);
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
 
@@ -68,6 +69,7 @@ int launch_skinny(const cat_shape* s, const LpPlan& plan, const void* H, const v
     if (top) {
         p.gmax = reinterpret_cast<float*>(ws + plan.off_g);
         p.zs = reinterpret_cast<__half*>(ws + plan.off_z);
+        p.w_sq = reinterpret_cast<int*>(ws + kNormOffset);
     }
     p.part_stride = plan.Ts; p.ld_g = plan.ld_g; p.ldz = plan.ldz;
     p.T = static_cast<int>(s->T); p.V = static_cast<int>(s->V);
@@ -144,6 +146,7 @@ int launch_lp_rows(const cat_shape* s, const LpPlan& plan, const TI* H, const TI
     rp.lse = lse + r0;
     rp.entropy = entropy + r0;
     if (TOP) {
+        rp.w_sq = reinterpret_cast<const int*>(ws + kNormOffset);
         rp.zs = reinterpret_cast<const TZ*>(ws + plan.off_z);
         rp.ldz = plan.ldz;
         rp.gmax = reinterpret_cast<const float*>(ws + plan.off_g);
@@ -170,6 +173,42 @@ int launch_lp_rows(const cat_shape* s, const LpPlan& plan, const TI* H, const TI
     return CAT_OK;
 }
 
+// The longest row of W, ahead of the logits GEMM or beside it (see lp::norm_kernel).
+template <bool BESIDE>
+int launch_norms(const cat_shape* s, const __nv_bfloat16* W, int n_groups, int* w_sq, int sm_count, cudaStream_t st) {
+    auto kern = lp::norm_kernel<BESIDE>;
+    if (BESIDE) {      // a kernel that prefers another split of shared memory and L1 than the GEMM's would wait for the GEMM's CTAs to leave their SMs
+        static std::atomic<unsigned long long> done{0};
+        int dev = -1;
+        if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
+        const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0ull;
+        if (bit == 0 || (done.load(std::memory_order_relaxed) & bit) == 0) {
+            if (cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess) {
+                cudaGetLastError();
+                return CAT_ERR_CUDA;
+            }
+            done.fetch_or(bit, std::memory_order_relaxed);
+        }
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(BESIDE ? sm_count : 2 * sm_count), 1, 1);
+    cfg.blockDim = dim3(lp::NORM_THREADS<BESIDE>, 1, 1);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = BESIDE ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, kern, W, static_cast<long long>(s->ldW), static_cast<int>(s->d), static_cast<int>(s->V), n_groups, w_sq) !=
+        cudaSuccess) {
+        cudaGetLastError();
+        return CAT_ERR_CUDA;
+    }
+    return CAT_OK;
+}
+// From this many rows on the GEMM takes longer than the pass beside it.
+constexpr long long kNormsBesideRows = 1024;
+
 template <bool TOP>
 int lp_slab(const cat_shape* s, const LpPlan& plan, const CUtensorMap& tmW, const void* H, const void* W, long long r0, long long rws,
             uint8_t* ws, const int64_t* labels, const uint8_t* valid, int top_k, float* logp, float* lse, float* entropy,
@@ -195,9 +234,15 @@ int lp_slab(const cat_shape* s, const LpPlan& plan, const CUtensorMap& tmW, cons
         ep.part_m = part_m; ep.part_l = part_l; ep.part_u = part_u; ep.part_id = reinterpret_cast<int*>(ws + plan.off_id); ep.part_stride = plan.Ts;
         ep.gmax = reinterpret_cast<float*>(ws + plan.off_g); ep.ld_g = plan.ld_g;
         ep.T = static_cast<int>(rws); ep.V = static_cast<int>(s->V);
-        const int rc = launch_tc<0, 0, tc::EpiLp<TOP>>(tmH, tmW, sched, ep, reinterpret_cast<int*>(ws), sm_count, st, TOP ? &tmZ : nullptr);
+        const __nv_bfloat16* Wb = static_cast<const __nv_bfloat16*>(W);
+        int* w_sq = reinterpret_cast<int*>(ws + kNormOffset);
+        const bool norms = TOP && r0 == 0, beside = rws >= kNormsBesideRows;
+        int rc = norms && !beside ? launch_norms<false>(s, Wb, S, w_sq, sm_count, st) : CAT_OK;
         if (rc != CAT_OK) return rc;
-        return launch_lp_rows<__nv_bfloat16, __half, TOP>(s, plan, Hs, static_cast<const __nv_bfloat16*>(W), r0, rws, S, ws, labels, valid,
+        rc = launch_tc<0, 0, tc::EpiLp<TOP>>(tmH, tmW, sched, ep, reinterpret_cast<int*>(ws), sm_count, st, TOP ? &tmZ : nullptr);
+        if (rc == CAT_OK && norms && beside) rc = launch_norms<true>(s, Wb, S, w_sq, sm_count, st);
+        if (rc != CAT_OK) return rc;
+        return launch_lp_rows<__nv_bfloat16, __half, TOP>(s, plan, Hs, Wb, r0, rws, S, ws, labels, valid,
                                                           top_k, logp, lse, entropy, top_ids, top_logp, st);
     }
     const float* Hs = static_cast<const float*>(H) + r0 * s->ldH;
@@ -210,6 +255,7 @@ int lp_slab(const cat_shape* s, const LpPlan& plan, const CUtensorMap& tmW, cons
     if (TOP) {
         ep.zs = reinterpret_cast<float*>(ws + plan.off_z); ep.ld_z = plan.ldz;
         ep.gmax = reinterpret_cast<float*>(ws + plan.off_g); ep.ld_g = plan.ld_g;
+        if (r0 == 0) ep.w_sq = reinterpret_cast<int*>(ws + kNormOffset);
     }
     const dim3 grid(static_cast<unsigned>(cdiv(rws, f32::TM)), static_cast<unsigned>(S));
     f32::gemm_kernel<f32::FWD, true, true><<<grid, f32::THREADS, 0, st>>>(op, ep);

@@ -153,6 +153,9 @@ struct EpiLp {
     }
 };
 
+template <>
+struct LetsNextStart<EpiLp<true>> { static constexpr bool value = true; };
+
 // Backward: dz of the current vocabulary slab, rounded to bf16 once (the operand type of the two contractions).
 struct EpiDzLp {
     struct Params {
@@ -345,11 +348,88 @@ template <class TZ>
 struct GroupOf { static constexpr int value = tc::LP_GROUP; };
 template <>
 struct GroupOf<float> { static constexpr int value = 64; };       // columns per tile of the fp32 GEMM
-// Error of a logit of the GEMM relative to itself, or to the threshold where that is larger: one addition of 16 products (tensor cores) or
-// one (fp32) at a time, each off by at most 2^-23 of a running sum that is taken to stay within twice that.  (What was seen: 3e-6 of
-// a logit at d = 2048, against 3.2e-5 here.)
-__device__ __forceinline__ float gemm_error(const __half*, int d) { return static_cast<float>(d / 16 + 8) * 2.384185791015625e-7f; }
-__device__ __forceinline__ float gemm_error(const float*, int d) { return static_cast<float>(d + 8) * 2.384185791015625e-7f; }
+// Error of a logit of the GEMM as a share of |h| |w|, the product of the norms, which no partial sum of h w exceeds.  (A share of the logit
+// itself bounds nothing where the sum cancels: with channels of +-1000 the sums pass through 1000 on their way to a logit of 1.)
+// Tensor cores: 16 products at a time, each of the 17 addends cut to 2^-25 of the power of two below the largest, the sum to 2^-23:
+// 21 * 2^-25 a step (seen on a B200 with sums of a large term and many small ones).  fp32: runs of 256, each addition rounded to 2^-24.
+// 8 steps more cover the roundings of what is made of the logits here.
+__device__ __forceinline__ float gemm_error(const __half*, int d) { return static_cast<float>(d / 16 + 9) * (21.f * 0x1p-25f); }
+__device__ __forceinline__ float gemm_error(const float*, int d) { return static_cast<float>(min(d, 256) + d / 256 + 9) * 0x1p-24f; }
+// The same of warp_dot_f32: four chains of 2 ceil(d / 256) additions a lane, seven more to join them.
+__device__ __forceinline__ float dot_error(int d) { return static_cast<float>(2 * ((d + 255) / 256) + 9) * 0x1p-24f; }
+// The norm of a vector of d elements from the fp32 sum of their squares, rounded up: what the squares lost below the range, d 2^-126 at most,
+// is added, and 1e-4 covers the roundings of the sum.  Squares past the range give infinity: then every candidate is in doubt.
+__device__ __forceinline__ float norm_above(float sum_sq, int d) {
+    const float x = sqrtf(fmaf(static_cast<float>(d), 0x1p-126f, sum_sq)) * 1.0001f;
+    return x >= 0.f ? x : INFINITY;
+}
+// acc + the squares of two bf16 numbers, from above: the upper one is taken with the lower one's bits behind its own, which makes its
+// square larger by up to 2^-6 of it and saves an instruction of four.
+__device__ __forceinline__ float add_squares(float acc, uint32_t two) {
+    const float a = __uint_as_float(two << 16), b = __uint_as_float(two);
+    return fmaf(b, b, fmaf(a, a, acc));
+}
+__device__ __forceinline__ float add_squares(float acc, const uint4& x) {
+    return add_squares(add_squares(add_squares(add_squares(acc, x.x), x.y), x.z), x.w);
+}
+// sum of the squares of a row, by one warp
+__device__ __forceinline__ float warp_squares(const __nv_bfloat16* row, int d, int lane) {
+    const uint4* v = reinterpret_cast<const uint4*>(row);
+    constexpr int BATCH = 8;      // loads under way together
+    const int n = d / 8;
+    float sum = 0.f;
+    int i = lane;
+    for (; i + 32 * (BATCH - 1) < n; i += 32 * BATCH) {
+        uint4 x[BATCH];
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) x[j] = __ldg(v + i + 32 * j);
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) sum += add_squares(0.f, x[j]);
+    }
+#pragma unroll 4
+    for (; i < n; i += 32) sum = add_squares(sum, __ldg(v + i));
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    return sum;
+}
+__device__ __forceinline__ float warp_squares(const float* row, int d, int lane) {
+    float sum = 0.f;
+#pragma unroll 4
+    for (int i = lane; i < d; i += 32) { const float x = __ldg(row + i); sum = fmaf(x, x, sum); }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    return sum;
+}
+// Raises *most, a float >= 0 held as its bits, to x; NaN counts as infinity.  The largest of many does not depend on their order.
+__device__ __forceinline__ void raise_to(int* most, float x) {
+    atomicMax(most, __float_as_int(x >= 0.f ? x : INFINITY));
+}
+
+// The largest sum of squares of a row of W, which row_kernel's bound wants.
+//   BESIDE: launched behind the logits GEMM, whose CTAs let it start as soon as they all run.  They leave it 2 KB of shared memory and 28 KB of L1,
+//     so that it reads at 1.7 TB/s: hidden behind a GEMM of many rows.  It ends after the GEMM, so that what follows may take its end for both.
+//   otherwise ahead of the GEMM, alone, at the rate of a copy.  Its CTAs walk the GEMM's vocabulary groups (n_groups of them, in tiles of BN)
+//     from back to front, so that what the GEMM reads first is in the L2.
+// Whole calls with k = 20, beside / ahead, in us: 129 rows of 2048 x 128256 386 / 217; 600 of 1024 x 151936 354 / 267.
+template <bool BESIDE>
+constexpr int NORM_THREADS = BESIDE ? 256 : 512;      // beside: what the registers that the GEMM leaves a quarter of an SM allow
+template <bool BESIDE>
+__global__ void __launch_bounds__(NORM_THREADS<BESIDE>) norm_kernel(const __nv_bfloat16* W, long long ldW, int d, int V, int n_groups, int* most) {
+    constexpr int WARPS = NORM_THREADS<BESIDE> / 32;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long n_tiles = (V + tc::BN - 1) / tc::BN;
+    float mx = 0.f;
+    for (int g = blockIdx.x % n_groups; g < n_groups; g += gridDim.x) {
+        const int sharers = gridDim.x <= n_groups ? 1 : (gridDim.x - g + n_groups - 1) / n_groups;       // CTAs of this group
+        const long long v0 = g * n_tiles / n_groups * tc::BN, v1 = min(static_cast<long long>(V), (g + 1) * n_tiles / n_groups * tc::BN);
+        for (long long v = v1 - 1 - (blockIdx.x / n_groups) * WARPS - warp; v >= v0; v -= sharers * WARPS) {
+            const float x = warp_squares(W + v * ldW, d, lane);
+            mx = x <= mx ? mx : x;         // NaN stays
+        }
+    }
+    if (lane == 0) raise_to(most, mx);
+    if (BESIDE) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
 
 template <class TI, class TZ>
 struct RowParams {
@@ -369,6 +449,7 @@ struct RowParams {
     float* lse;                    // [T]
     float* entropy;                // [T]
     // alternatives
+    const int* w_sq;               // largest sum of squares of a row of W (float bits)
     const TZ* zs;                  // [T][ldz] logits of the slab
     long long ldz;
     const float* gmax;             // [T][ld_g]
@@ -384,13 +465,14 @@ struct Shared {
     static constexpr int RW = RT / 32;
     float red[2][RW];
     int count[2][RW];
-    int n_cand, n_near, n_rest;
+    int n_cand, n_near, n_rest, n_tied;
     float m, l, u, logl;
+    float h_sq;                    // sum of the squares of the row of H
     int id_max;
     double z_max, z_label;
-    double z[CAP];                 // exact logits, where `err` says so
+    double z[CAP];                 // logits summed again, where `err` says so
     float approx[CAP];
-    float err[CAP];                // how far approx may be off; EXACT, SUMMED: z is known; OUT: not among the k largest
+    float err[CAP];                // how far approx may be off; DOUBT, SUMMED: z is known; OUT: not among the k largest
     int id[CAP];
     double z_keep[MAX_TOP];
     int id_keep[MAX_TOP];
@@ -398,7 +480,7 @@ struct Shared {
     float near_max[CAP];           // those groups' maxima
     int above[CAP], close[CAP];    // per candidate: others certainly above it, others within the errors
 };
-constexpr float EXACT = -1.f, OUT = -2.f, SUMMED = -3.f;
+constexpr float DOUBT = -1.f, OUT = -2.f, SUMMED = -3.f;
 
 template <int RW>
 __device__ __forceinline__ float block_max(float x, float (&red)[RW]) {
@@ -463,11 +545,14 @@ __device__ __forceinline__ float near_kth(const float (&best)[4], float least, i
 }
 
 // The share of itself that the row's largest logit came out too small, by which its other logits, bf16 sums of as many terms, are taken to be off
-// as well (their truncations add up to the same share of each within about a tenth).
+// as well (their truncations add up to the same share of each within about a tenth).  Only where truncation of that logit itself explains it: a
+// sum that passes through larger numbers is off by something else, which says nothing about the others.
+__device__ __forceinline__ float off_share(float off, float m, int d) {
+    return m > 1.f && off > 0.f && off <= gemm_error(static_cast<const __half*>(nullptr), d) * m ? off / m : 0.f;
+}
 template <class TI, class S>
-__device__ __forceinline__ float off_share(const S& sh) {
-    const float x = static_cast<float>(sh.z_max - static_cast<double>(sh.m));
-    return sizeof(TI) == 2 && sh.m > 1.f && fabsf(x) < 1.f ? x / sh.m : 0.f;
+__device__ __forceinline__ float off_share(const S& sh, int d) {
+    return sizeof(TI) == 2 ? off_share(static_cast<float>(sh.z_max - static_cast<double>(sh.m)), sh.m, d) : 0.f;
 }
 
 // z - lse.  In a row that is sure of its token this is the logarithm of 1 + a little, of which lse rounded to fp32 would leave few places.
@@ -484,7 +569,7 @@ __device__ __forceinline__ void finish_row(const RowParams<TI, TZ>& p, long long
     const float x = static_cast<float>(sh.z_max - static_cast<double>(sh.m));
     // l with the others' logits corrected too, to first order: the share times their sum of exp(z - m) z.  The entropy's two parts stay as
     // they were summed: there the share cancels but for itself times the logits' variance.
-    float lc = fmaf(off_share<TI>(sh), fmaf(0.6931471805599453f, u, sh.m * (l - 1.f)), l);
+    float lc = fmaf(off_share<TI>(sh, p.d), fmaf(0.6931471805599453f, u, sh.m * (l - 1.f)), l);
     if (fabsf(x) < 1.f) {
         lc += expm1f(x);
         l += expm1f(x);
@@ -538,14 +623,15 @@ __device__ __forceinline__ int settle(const RowParams<TI, TZ>& p, const TI* h, S
     return n < p.k ? n : p.k;
 }
 
-// The same, ordered by the approximate logits, with fp64 sums only for candidates that their errors leave in doubt against another.
+// The same, ordered by the approximate logits.  Candidates that their errors (eps and what the slab's rounding adds) leave in doubt against another
+// are summed again, in fp32 (off by eps32 at most); those still in doubt against each other, in fp64, which takes eight times as long.
 //
 // The values.  A bf16 logit of 20 that comes out 3e-6 of itself too small would be off by more than its log probability has
 // places for.  With few rows every value is an fp32 sum over d.  With many that is a gather of W for each (9240 rows of 1344 x 4906, k = 20: 178 -> 225 us;
 // 8192 of 2048 x 128256, k = 64: 3.18 -> 3.51 ms): there only values that the slab's fp16 has rounded (not the largest of their group) are
 // summed, and the others are corrected by the share of itself that the largest logit is off (see finish_row).
 template <class TI, class TZ, int RT>
-__device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI* h, long long r, Shared<RT>& sh, int n, float eps, float rel) {
+__device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI* h, long long r, Shared<RT>& sh, int n, float eps, float eps32) {
     constexpr int RW = RT / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long long y = p.logp != nullptr ? p.labels[r] : -1;
@@ -555,7 +641,7 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
     const int parts = n <= RT / 2 ? RT / (n > 0 ? n : 1) : 1;
     const int part = threadIdx.x / (n > 0 ? n : 1), per = (n + parts - 1) / parts;
     for (int c = threadIdx.x; c < n; c += RT) { sh.above[c] = 0; sh.close[c] = 0; }
-    if (threadIdx.x == 0) sh.n_near = sh.n_rest = 0;
+    if (threadIdx.x == 0) sh.n_near = sh.n_rest = sh.n_tied = 0;
     __syncthreads();
     for (int c = parts > 1 ? threadIdx.x - part * n : threadIdx.x; c < n && (parts == 1 || part < parts); c += parts > 1 ? CAP : RT) {
         const float z = sh.approx[c], e = sh.err[c];
@@ -576,10 +662,10 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
             sh.err[c] = OUT;
             sh.approx[c] = -INFINITY;
         } else if (sh.close[c] > 1) {
-            sh.err[c] = EXACT;
+            sh.err[c] = DOUBT;
             sh.near[atomicAdd(&sh.n_near, 1)] = c;
         } else if (sizeof(TI) == 2 && sh.id[c] != sh.id_max && sh.id[c] != y &&
-                   (RT == RT_FEW || sh.err[c] > fmaxf(eps, rel * fabsf(sh.approx[c])) + 4.0e-8f)) {
+                   (RT == RT_FEW || sh.err[c] - eps > 4.0e-8f)) {
             sh.err[c] = SUMMED;
             sh.near[CAP - 1 - atomicAdd(&sh.n_rest, 1)] = c;
         }
@@ -593,7 +679,24 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
         } else {
             const int c = i < n_doubt + 2 ? sh.near[i - 2] : sh.near[CAP - 1 - (i - n_doubt - 2)];
             const TI* w = p.W + static_cast<long long>(sh.id[c]) * p.ldW;
-            const double z = i < n_doubt + 2 ? warp_dot(h, w, p.d, lane) : static_cast<double>(warp_dot_f32(h, w, p.d, lane));
+            const double z = sizeof(TI) == 2 ? static_cast<double>(warp_dot_f32(h, w, p.d, lane)) : warp_dot(h, w, p.d, lane);
+            if (lane == 0) sh.z[c] = z;
+        }
+    }
+    if (sizeof(TI) == 2 && n_doubt > 1) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < n_doubt; i += RT) {
+            const int c = sh.near[i];
+            const float z = static_cast<float>(sh.z[c]);
+            bool tied = false;
+            for (int j = 0; j < n_doubt; ++j) tied |= j != i && fabsf(static_cast<float>(sh.z[sh.near[j]]) - z) <= 2.f * eps32;
+            if (tied) sh.close[atomicAdd(&sh.n_tied, 1)] = c;
+        }
+        __syncthreads();
+        const int n_tied = sh.n_tied;
+        for (int i = warp; i < n_tied; i += RW) {
+            const int c = sh.close[i];
+            const double z = warp_dot(h, p.W + static_cast<long long>(sh.id[c]) * p.ldW, p.d, lane);
             if (lane == 0) sh.z[c] = z;
         }
     }
@@ -607,14 +710,14 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
     }
     __syncthreads();
     if (threadIdx.x == RT - 1) finish_row(p, r, sh);
-    const float share = off_share<TI>(sh);
+    const float share = off_share<TI>(sh, p.d);
     for (int c = threadIdx.x; c < n; c += RT) {
         const float ec = sh.err[c], zc = sh.approx[c];
         if (ec == OUT) continue;
         const int id = sh.id[c];
         const double z = ec < 0.f ? sh.z[c] : static_cast<double>(fmaf(share, zc, zc));
         int rank = sh.above[c];
-        if (ec == EXACT) {      // against others in doubt the exact logits count
+        if (ec == DOUBT) {      // against others in doubt the sums count
             for (int i = 0; i < n_doubt; ++i) {
                 const int j = sh.near[i];
                 rank += (sh.z[j] > z || (sh.z[j] == z && sh.id[j] < id) ? 1 : 0) - (sh.approx[j] > zc ? 1 : 0);
@@ -635,10 +738,11 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
 // Top k.  Any k group maxima are k logits of the row, so a number t that k group maxima reach is a lower bound of the row's k-th
 // largest logit, and only columns at or above t, less the GEMM's error, can be among the k largest.  They are looked
 // up in the slab: a few groups of it are read, not the row.  The order is that of the exact products: candidates whose approximate
-// logits are closer than their errors are compared by fp64 sums (a gather of W for about one in twenty of them; taking all of them
-// again cost 0.7 ms for 8192 rows of k = 64, a quarter of the GEMM), and equal logits go to the lower id.
-// 14 us for one row of V = 128256, k = 20, 275 us for 8192 rows, k = 64 (GEMM 2.75 ms): the bound 45, the list of groups 30, their look-up 78 (700
-// thousand 64-byte reads all over the slab), ranking about 45, exact sums the rest.
+// logits are closer than their errors are summed again, and equal logits go to the lower id.  The errors are bounded by the norms of
+// the row of H and of the longest row of W (gemm_error), so they hold whatever the sums pass through.
+// 17 us for one row of V = 128256, k = 20, 525 us for 8192 rows, k = 64 (GEMM 2.82 ms): the bound 45, the list of groups 30, their look-up 78 (700
+// thousand 64-byte reads all over the slab), ranking about 45, sums the rest: the norms leave most of 64 candidates in doubt, whose rows of W
+// are 2 GB.  (Errors taken relative to the logit left one in twenty, 275 us, and wrong orders where sums cancel.)
 // More than CAP candidates (a row of zeros, many equal rows of W) are settled batch by batch by exact sums.
 template <class TI, class TZ, bool TOP, int RT>
 __global__ void __launch_bounds__(RT, 1024 / RT) row_kernel(const RowParams<TI, TZ> p) {
@@ -689,6 +793,10 @@ __global__ void __launch_bounds__(RT, 1024 / RT) row_kernel(const RowParams<TI, 
         prefetch_row(h, p.d, lane);
         const long long y = p.logp != nullptr ? p.labels[r] : -1;
         if (y >= 0 && y < p.V) prefetch_row(p.W + y * p.ldW, p.d, lane);
+    }
+    if (TOP && warp == 2) {
+        const float x = warp_squares(h, p.d, lane);
+        if (lane == 0) sh.h_sq = x;
     }
     if (warp == 0) {
         // merge the split partials; sums over splits in a fixed order.  The loads of up to 160 splits are under way together.
@@ -757,9 +865,9 @@ __global__ void __launch_bounds__(RT, 1024 / RT) row_kernel(const RowParams<TI, 
     }
     float big;
     const float t = near_kth(best, least, p.k, sh, big);
-    const float rel = gemm_error(z, p.d);
     // k exact logits reach t - eps; a bound taken over stored logits may lie their rounding (2^-11 of the row's span) higher
-    const float eps = rel * fabsf(t);
+    const float size = norm_above(sh.h_sq, p.d) * norm_above(__int_as_float(*p.w_sq), p.d);
+    const float eps = gemm_error(z, p.d) * size;
     const float thr = t - 2.2f * eps - (by_group ? 0.f : 1.0e-3f * big);
     // the groups that reach the threshold, then their columns that do
     auto keep_group = [&](int gi, float gm) {
@@ -789,7 +897,7 @@ __global__ void __launch_bounds__(RT, 1024 / RT) row_kernel(const RowParams<TI, 
         int at = 0;
         if (lane == 0) at = atomicAdd(&sh.n_cand, __popc(hit));
         at = __shfl_sync(0xffffffffu, at, 0) + __popc(hit & ((1u << lane) - 1u));
-        if (in && at < CAP) { sh.id[at] = static_cast<int>(col); sh.approx[at] = x; sh.err[at] = fmaxf(eps, rel * fabsf(x)) + e; }
+        if (in && at < CAP) { sh.id[at] = static_cast<int>(col); sh.approx[at] = x; sh.err[at] = eps + e; }
     };
     if (n_near <= CAP) {
         const int n_el = n_near * group;
@@ -811,7 +919,7 @@ __global__ void __launch_bounds__(RT, 1024 / RT) row_kernel(const RowParams<TI, 
     __syncthreads();
     int kept;
     if (n_near <= CAP && sh.n_cand <= CAP) {
-        kept = settle_close(p, h, r, sh, sh.n_cand, eps, rel);
+        kept = settle_close(p, h, r, sh, sh.n_cand, eps, dot_error(p.d) * size);
     } else {
         if (warp < 2) exact_one(p, h, r, sh, warp);
         // many logits within the error of the k-th.  A row of zeros has them all equal: ids 0, 1, ...

@@ -8,7 +8,9 @@
 //   * an accumulator lane is a vocabulary entry and a column a hidden state: a warp turns 32 x 32 logits over in shared memory, after
 //     which a thread holds 32 neighbouring logits of one hidden state and goes on like the epilogue of logprob.cuh.  (Reducing
 //     across the lanes instead, one redux and five shuffles per hidden state, took 125 us for 67 rows of 1024 x 151936;
-//     this way 61 us.)  Running sums stay in registers over all tiles of the CTA; warps and CTAs are merged at the end.
+//     this way 61 us.)  Running sums stay in registers over all tiles of the CTA; warps and CTAs are merged at the end;
+//   * with alternatives, four more warps sum the squares of W's rows as their slices pass, for the bound on the logits' errors
+//     (lp::gemm_error): the longest row is known without another pass over W.
 // Measured: one row of 2048 x 128256 (W 525 MB) 80.6 us, 6.5 TB/s, the rate of a plain copy; 67 rows of 1024 x 151936 (311 MB)
 // 61 us, 5.1 TB/s: the slices of H share the ring, and start and end of the launch are a sixth of it.
 #pragma once
@@ -39,6 +41,7 @@ struct Params {
     int* part_id;
     float* gmax;          // [T][ld_g] maxima of 32 neighbouring columns; nullptr (and zs) without alternatives
     __half* zs;           // [T][ldz] logits as distances from those maxima
+    int* w_sq;            // raised to the largest sum of squares of a row of W (float bits)
     long long part_stride, ld_g, ldz;
     int T, V;
     int n;                // rows of H in a tile of it: T rounded up to 16
@@ -51,8 +54,10 @@ struct Params {
 
 // TPW: hidden states a warp looks after; HALVES: sets of four epilogue warps (HALVES * TPW >= T); SUB: W tiles that a slice of H is
 // loaded for.  With many rows the slices of H take as much of the ring as those of W; two tiles per slice of H leave more of it to W.
+// Threads: 64 + 128 HALVES, and NORM_THREADS more with alternatives.
+constexpr int NORM_THREADS = 128;
 template <int TPW, int HALVES, int SUB>
-__global__ void __launch_bounds__(64 + 128 * HALVES, 1)
+__global__ void __launch_bounds__(64 + 128 * HALVES + NORM_THREADS, 1)
 logits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmH, const Params p, int* status) {
     constexpr int COLS = TPW * HALVES;                       // accumulator columns (a power of two >= 32)
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -72,7 +77,7 @@ logits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
         ptx::prefetch_tmap(&tmH);
         for (int i = 0; i < p.stages; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctl.full[i]), 1);
-            ptx::mbar_init(ptx::smem_u32(&ctl.empty[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&ctl.empty[i]), p.gmax != nullptr ? 1 + NORM_THREADS / 32 : 1);
         }
         for (int i = 0; i < 2; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctl.tfull[i]), 1);
@@ -152,6 +157,50 @@ logits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
             }
         }
         __syncwarp();
+    } else if (warp >= 2 + 4 * HALVES) {
+        // Squares of W's rows: the rows of a round's tiles lie one behind the other in the slot, and a thread takes every 128th.  A row's 16-byte
+        // pieces are read in an order of the lane's own, so that eight lanes meet eight different banks (the swizzle only moves pieces
+        // within a row).
+        const int i = threadIdx.x - (64 + 128 * HALVES);
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        float most = 0.f;
+        for (int t = blockIdx.x; t < p.n_tiles && ok; t += SUB * gridDim.x) {
+            float sq[SUB];
+#pragma unroll
+            for (int j = 0; j < SUB; ++j) sq[j] = 0.f;
+            const int n_rows = (SUB == 1 || t + static_cast<int>(gridDim.x) >= p.n_tiles ? 1 : SUB) * p.tile_rows;
+            for (int kb = 0; kb < p.num_kb; ++kb) {
+                ok = tc::wait_bounded(ptx::smem_u32(&ctl.full[stage]), phase, abort, status, p.wait_ns);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+#pragma unroll
+                for (int j = 0; j < SUB; ++j) {
+                    const int q = j * NORM_THREADS + i;
+                    if (q >= n_rows) break;
+                    const uint32_t row = ring + stage * stage_bytes + q * (BK * 2);
+                    uint4 x[8];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) ptx::ld_shared_v4(row + ((c ^ (lane & 7)) << 4), x[c]);
+                    float a[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) a[c & 3] = lp::add_squares(a[c & 3], x[c]);
+                    sq[j] += (a[0] + a[1]) + (a[2] + a[3]);
+                }
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl.empty[stage]));
+                if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+            }
+#pragma unroll
+            for (int j = 0; j < SUB; ++j) most = sq[j] <= most ? most : sq[j];        // NaN stays
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) {
+            const float o = __shfl_xor_sync(0xffffffffu, most, off);
+            most = o <= most ? most : o;
+        }
+        if (lane == 0) lp::raise_to(p.w_sq, most);
     } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         const int tok0 = half * TPW;

@@ -594,6 +594,10 @@ struct EpiOutT {
 };
 using EpiOut = EpiOutT<false>;
 
+// Whether a kernel behind the GEMM may run beside it (see lp::norm_kernel).
+template <class Epi>
+struct LetsNextStart { static constexpr bool value = false; };
+
 // ------------------------------------------------------------------------------------------
 // The kernel.  tmA / tmB are 2-D tiled tensor maps with 128-byte swizzle:
 //   K-major operand  [rows = M or N][cols = K]: box {BK, rows of the tile this CTA loads};
@@ -706,6 +710,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
         if (claimed && leader) ctl.worker = static_cast<uint32_t>(die::claim_worker(sched.claims, sched.serial, worker, n_workers));
     }
     cta_begin<CG>(ctl, G::STAGES, warp);
+    if constexpr (LetsNextStart<Epi>::value) ptx::launch_dependents();
     if (claimed) worker = static_cast<int>(leader ? ctl.worker : ptx::ld_shared_cluster_u32(ptx::mapa_shared(ptx::smem_u32(&ctl.worker), 0)));
     const uint32_t tmem = ctl.tmem_base;
     volatile int* abort = &ctl.abort;

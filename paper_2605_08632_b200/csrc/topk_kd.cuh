@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(THREADS) merge_kernel(const MergeParams<TI> p)
                 if (fabsf(zy - ly) < 1.f) l = fmaf(e, expm1f(zy - ly), l);
             }
             // the others, taken to be off by the same share of themselves as the largest (see lp::off_share)
-            if (m > 1.f && fabsf(x) < 1.f) l = fmaf(x / m, zl, l);
+            l = fmaf(lp::off_share(x, m, p.d), zl, l);
         }
         __syncwarp();
         if (lane == 0) p.z_label[r] = zy;
