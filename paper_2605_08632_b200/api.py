@@ -77,7 +77,7 @@ class CatLoss:
         self.ws_bwd = torch.empty(nb, dtype=torch.uint8, device=dev)
         self._ws_fused = None
         self._ws_kd = None
-        self._ws_topk = self._topk_need = None      # workspace, and (k, its size)
+        self._ws_topk = None
         self.loss3 = None
         self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
         self.lse = torch.empty(T, dtype=torch.float32, device=dev)
@@ -165,13 +165,13 @@ class CatLoss:
             if t is not None:
                 _check(name, t, shape, dtype, dev)
         desc = B.make_topk_kd_desc(L, k, float(beta), renormalize, ld=_pitch(top_ids))
-        if self._topk_need is None or self._topk_need[0] != k or not 0.0 <= desc.beta < float("inf"):
-            self._topk_need = (k, B.cat_topk_kd_workspace_bytes(self.shape, desc))
-        n = self._topk_need[1]
-        if n == 0:
-            self._topk_need = None
+        if not (1 <= k <= B.CAT_TOPK_MAX and L >= 1 and 0.0 <= desc.beta < float("inf")):
             raise ValueError("invalid problem for cat_topk_kd_loss_fwd_bwd")
-        if self._ws_topk is None or self._ws_topk.numel() < n:
+        if self._ws_topk is None:
+            # for lists of any length: a graph captured with one k holds this address while calls with another come and go
+            n = B.cat_topk_kd_workspace_bytes(self.shape, B.make_topk_kd_desc(1, B.CAT_TOPK_MAX, 0.0))
+            if n == 0:
+                raise ValueError("invalid problem for cat_topk_kd_loss_fwd_bwd")
             self._ws_topk = torch.empty(n, dtype=torch.uint8, device=dev)
         if self.loss3 is None:
             self.loss3 = torch.zeros(3, dtype=torch.float32, device=dev)

@@ -1,0 +1,48 @@
+"""What the engines of the LM-head operators keep between calls: workspaces that captured graphs hold, counters, autograd's buffers."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_08632_b200 import binding as B
+from paper_2605_08632_b200.api import CatLoss
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def lists(L, k, V, seed):
+    g = torch.Generator().manual_seed(seed)
+    ids = torch.stack([torch.randperm(V, generator=g)[:k] for _ in range(L)])
+    return ids.to(DEV), torch.log_softmax(torch.randn(L, k, generator=g), 1).to(DEV)
+
+
+def rows(T, d, V, seed, dtype=BF):
+    g = torch.Generator().manual_seed(seed)
+    H, W = torch.randn(T, d, generator=g).to(dtype), (0.05 * torch.randn(V, d, generator=g)).to(dtype)
+    return H.to(DEV), W.to(DEV), torch.randint(0, V, (T,), generator=g).to(DEV)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_captured_step_outlives_calls_with_longer_lists(dtype):
+    """Capture with short lists, call with long ones and with others, replay: the replay's workspace is still the engine's."""
+    T, K, d, V = 96, 8, 64, 700
+    eng = CatLoss(T, d, V, K, dtype=dtype)
+    H, W, y = rows(T, d, V, 0, dtype)
+    short, long = lists(T, 3, V, 1), lists(T, B.CAT_TOPK_MAX, V, 2)
+    eng.topk_kd_forward_backward(H, W, y, None, *short)
+    address = eng._ws_topk.data_ptr()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = eng.topk_kd_forward_backward(H, W, y, None, *short)
+    eng.topk_kd_forward_backward(H, W, y, None, *long)
+    eng.topk_kd_forward_backward(H, W, y, None, *lists(T, 200, V, 3))
+    others = [torch.full((1 << 22,), 0x5A, dtype=torch.uint8, device=DEV) for _ in range(8)]     # would take freed memory
+    assert eng._ws_topk.data_ptr() == address
+    H2, W2, _ = rows(T, d, V, 7, dtype)
+    H.copy_(H2), W.copy_(W2)
+    graph.replay()
+    torch.cuda.synchronize()
+    want = CatLoss(T, d, V, K, dtype=dtype).topk_kd_forward_backward(H, W, y, None, *short)
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+    assert all(bool((o == 0x5A).all()) for o in others)
