@@ -77,6 +77,7 @@ class CatLoss:
         self.ws_bwd = torch.empty(nb, dtype=torch.uint8, device=dev)
         self._ws_fused = None
         self._ws_kd = None
+        self._ws_captured = []      # workspaces that a captured graph holds, kept when a larger one takes their place
         self._ws_topk = None
         self.loss3 = None
         self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
@@ -136,6 +137,8 @@ class CatLoss:
             raise ValueError("invalid problem for cat_kd_loss_fwd_bwd")
         if self._ws_kd is None or self._ws_kd.numel() < n:
             self._ws_kd = torch.empty(n, dtype=torch.uint8, device=self.loss.device)
+        if torch.cuda.is_current_stream_capturing() and not any(w is self._ws_kd for w in self._ws_captured):
+            self._ws_captured.append(self._ws_kd)
         if self.loss3 is None:
             self.loss3 = torch.zeros(3, dtype=torch.float32, device=self.loss.device)
         B.cat_kd_loss_fwd_bwd(self.shape, desc, H, W, labels, valid, Ht, Wt, block_start_host, conf_ext, grad_loss,

@@ -46,3 +46,30 @@ def test_a_captured_step_outlives_calls_with_longer_lists(dtype):
     want = CatLoss(T, d, V, K, dtype=dtype).topk_kd_forward_backward(H, W, y, None, *short)
     assert all(torch.equal(a, b) for a, b in zip(out, want))
     assert all(bool((o == 0x5A).all()) for o in others)
+
+
+def test_a_captured_distillation_outlives_calls_with_more_positions():
+    """kd_forward_backward's workspace grows with the target positions a slab refers to; a captured call keeps the one it was given."""
+    T, K, d, V, L = 512, 8, 64, 700, 2000
+    eng = CatLoss(T, d, V, K)
+    H, W, y = rows(T, d, V, 0)
+    Ht, Wt, _ = rows(L, d, V, 1)
+    near, far = torch.arange(T // K), torch.arange(T // K) * 30
+    eng.kd_forward_backward(H, W, y, None, Ht, Wt, near, 0.2)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = eng.kd_forward_backward(H, W, y, None, Ht, Wt, near, 0.2)
+    held = eng._ws_kd
+    address, n = held.data_ptr(), held.numel()
+    del held
+    eng.kd_forward_backward(H, W, y, None, Ht, Wt, far, 0.2)
+    assert eng._ws_kd.numel() > n
+    others = [torch.full((n,), 0x5A, dtype=torch.uint8, device=DEV) for _ in range(4)]         # would take freed memory
+    assert all(o.data_ptr() != address for o in others)
+    H2, W2, _ = rows(T, d, V, 7)
+    H.copy_(H2), W.copy_(W2)
+    graph.replay()
+    torch.cuda.synchronize()
+    want = CatLoss(T, d, V, K).kd_forward_backward(H, W, y, None, Ht, Wt, near, 0.2)
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+    assert all(bool((o == 0x5A).all()) for o in others)
