@@ -41,6 +41,7 @@ constexpr int kPlanSMs = 148;            // B200: the static schedules are plann
 constexpr size_t kHeaderBytes = 1024;    // workspace header: int32 status at byte 0, fp32 g/N at byte 64, worker claims from byte 256
 constexpr size_t kClaimsOffset = 256;    // up to 192 ints: one per CTA pair of a GEMM launch
 constexpr size_t kScaleOffset = 64;
+constexpr size_t kBadOffset = 72;        // cat_topk_kd_loss_fwd_bwd: unmasked rows whose label is no token id
 constexpr size_t kNormOffset = 128;      // cat_logprob_fwd: largest sum of squares of a row of W
 constexpr int kMaxSplits = 128;
 constexpr long long kDefaultSlabMiB = 2048;

@@ -543,6 +543,7 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
     const FusedPlan& f = plan.f;
     int* status = reinterpret_cast<int*>(ws);
     float* scale = reinterpret_cast<float*>(ws + kScaleOffset);
+    int* n_bad = reinterpret_cast<int*>(ws + kBadOffset);
     float* part_m = reinterpret_cast<float*>(ws + f.off_part_m);
     float* part_l = reinterpret_cast<float*>(ws + f.off_part_l);
     float* z_label = reinterpret_cast<float*>(ws + f.off_z_label);
@@ -567,7 +568,7 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
 
     CUtensorMap tmW_k;
     if (BF16 && tmap_b(&tmW_k, W, s->V, s->d, s->ldW) != CAT_OK) return CAT_ERR_CUDA;
-    tk::begin_kernel<<<1, 1024, 0, st>>>(y, valid, lists.block_start, T, K, V, desc->L, grad_loss, ok, scale, status,
+    tk::begin_kernel<<<1, 1024, 0, st>>>(y, valid, lists.block_start, T, K, V, desc->L, grad_loss, ok, scale, n_bad, status,
                                          static_cast<int>(kHeaderBytes / sizeof(int)));
     if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
     int cta0 = 0;
@@ -634,7 +635,7 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
                                   sm_count, st);
         if (rc != CAT_OK) return rc;
     }
-    tk::end_kernel<<<1, 1024, 0, st>>>(partials, cta0, T / K, kd_row, T, desc->beta, loss, reinterpret_cast<rows::StatsOut*>(stats), status);
+    tk::end_kernel<<<1, 1024, 0, st>>>(partials, cta0, T / K, kd_row, T, desc->beta, loss, reinterpret_cast<rows::StatsOut*>(stats), n_bad, status);
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
 

@@ -121,28 +121,32 @@ using lp::WARPS;
 constexpr float LOG2E = 1.4426950408889634f;
 
 // First launch of a call, one CTA: the workspace header cleared, the rows that take part (mask bit set, label a token id, teacher position
-// exists), and g / N.
+// exists), g / N, and the unmasked rows whose label is no token id, counted (the kernels that follow know only the rows that take part).
 __global__ void __launch_bounds__(1024) begin_kernel(const long long* labels, const unsigned char* valid, const long long* block_start, int T,
                                                      int K, int V, long long L, const float* grad_loss, unsigned char* valid_eff,
-                                                     float* scale, int* header, int header_words) {
-    __shared__ int sh[32];
+                                                     float* scale, int* n_bad, int* header, int header_words) {
+    __shared__ int sh[32], sh_bad[32];
     for (int i = threadIdx.x; i < header_words; i += 1024) header[i] = 0;
-    int n = 0;
+    int n = 0, bad = 0;
 #pragma unroll 4
     for (int r = threadIdx.x; r < T; r += 1024) {
         const long long y = labels[r];
         const int b = r / K;
         const long long t = block_start ? block_start[b] + (r - b * K) : r;
-        const bool on = (valid == nullptr || valid[r] != 0) && y >= 0 && y < V && t >= 0 && t < L;
+        const bool mask = valid == nullptr || valid[r] != 0, token = y >= 0 && y < V;
+        const bool on = mask && token && t >= 0 && t < L;
         valid_eff[r] = on ? 1 : 0;
         n += on ? 1 : 0;
+        bad += mask && !token ? 1 : 0;
     }
     n = __reduce_add_sync(0xffffffffu, n);
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = n;
+    bad = __reduce_add_sync(0xffffffffu, bad);
+    if ((threadIdx.x & 31) == 0) { sh[threadIdx.x >> 5] = n; sh_bad[threadIdx.x >> 5] = bad; }
     __syncthreads();
     if (threadIdx.x == 0) {
-        int tot = 0;
-        for (int w = 0; w < 32; ++w) tot += sh[w];
+        int tot = 0, tot_bad = 0;
+        for (int w = 0; w < 32; ++w) { tot += sh[w]; tot_bad += sh_bad[w]; }
+        *n_bad = tot_bad;
         const float g = grad_loss ? *grad_loss : 1.f;
         *scale = tot > 0 ? g / static_cast<float>(tot) : 0.f;
     }
@@ -150,14 +154,14 @@ __global__ void __launch_bounds__(1024) begin_kernel(const long long* labels, co
 
 // Last launch, one CTA: loss = {beta ce + kd, ce, kd} with ce and kd the sums over rows over N (fp64, in a fixed order), and the statistics.
 __global__ void __launch_bounds__(1024) end_kernel(const rows::CtaPartial* partials, int n_partials, int n_blocks, const float* kd_row, int T,
-                                                   float beta, float* loss, rows::StatsOut* stats, const int* status) {
+                                                   float beta, float* loss, rows::StatsOut* stats, const int* n_bad, const int* status) {
     __shared__ double s_d[4][32];
-    __shared__ long long s_n[2][32];
+    __shared__ long long s_n[32];
     double d[4] = {0.0, 0.0, 0.0, 0.0};       // loss, weight, weight * conf, kd
-    long long n[2] = {0, 0};                  // valid rows, bad labels
+    long long n = 0;                          // valid rows
     for (int i = threadIdx.x; i < n_partials; i += 1024) {
         const rows::CtaPartial q = partials[i];
-        d[0] += q.loss; d[1] += q.sum_w; d[2] += q.sum_wc; n[0] += q.n_valid; n[1] += q.n_bad;
+        d[0] += q.loss; d[1] += q.sum_w; d[2] += q.sum_wc; n += q.n_valid;
     }
 #pragma unroll 4
     for (int r = threadIdx.x; r < T; r += 1024) d[3] += static_cast<double>(kd_row[r]);
@@ -165,28 +169,27 @@ __global__ void __launch_bounds__(1024) end_kernel(const rows::CtaPartial* parti
     for (int off = 16; off > 0; off >>= 1) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) d[j] += __shfl_down_sync(0xffffffffu, d[j], off);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) n[j] += __shfl_down_sync(0xffffffffu, n[j], off);
+        n += __shfl_down_sync(0xffffffffu, n, off);
     }
     const int warp = threadIdx.x >> 5;
     if ((threadIdx.x & 31) == 0) {
         for (int j = 0; j < 4; ++j) s_d[j][warp] = d[j];
-        for (int j = 0; j < 2; ++j) s_n[j][warp] = n[j];
+        s_n[warp] = n;
     }
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int w = 1; w < 32; ++w) {
             for (int j = 0; j < 4; ++j) d[j] += s_d[j][w];
-            for (int j = 0; j < 2; ++j) n[j] += s_n[j][w];
+            n += s_n[w];
         }
-        const double N = n[0] > 0 ? static_cast<double>(n[0]) : 1.0;
-        const float ce = n[0] > 0 ? static_cast<float>(d[0] / N) : 0.f, kd = n[0] > 0 ? static_cast<float>(d[3] / N) : 0.f;
+        const double N = n > 0 ? static_cast<double>(n) : 1.0;
+        const float ce = n > 0 ? static_cast<float>(d[0] / N) : 0.f, kd = n > 0 ? static_cast<float>(d[3] / N) : 0.f;
         loss[0] = beta * ce + kd;
         loss[1] = ce;
         loss[2] = kd;
         if (stats) {
-            stats->n_valid = n[0];
-            stats->n_bad_labels = n[1];
+            stats->n_valid = n;
+            stats->n_bad_labels = *n_bad;
             stats->sum_weight = static_cast<float>(d[1]);
             stats->est_accept_len = n_blocks > 0 ? static_cast<float>(d[2] / n_blocks) : 0.f;
             stats->device_status = *status;

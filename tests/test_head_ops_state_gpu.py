@@ -73,3 +73,35 @@ def test_a_captured_distillation_outlives_calls_with_more_positions():
     want = CatLoss(T, d, V, K).kd_forward_backward(H, W, y, None, Ht, Wt, near, 0.2)
     assert all(torch.equal(a, b) for a, b in zip(out, want))
     assert all(bool((o == 0x5A).all()) for o in others)
+
+
+def bad_labels(T, V, seed):
+    """Labels of which some are no token id, some of those in masked rows; and how many rows have one and are not masked."""
+    g = torch.Generator().manual_seed(seed)
+    y = torch.randint(0, V, (T,), generator=g)
+    where = torch.rand(T, generator=g)
+    for i, value in enumerate((-100, -1, V, V + 1, 2 ** 40, -(2 ** 62))):
+        y[(where >= 0.05 * i) & (where < 0.05 * (i + 1))] = value
+    valid = torch.rand(T, generator=g) < 0.7
+    bad = (y < 0) | (y >= V)
+    assert bool((bad & valid).any()) and bool((bad & ~valid).any())
+    return y.to(DEV), valid.to(DEV), bad, valid
+
+
+@pytest.mark.parametrize("dtype,slab_mib", [(BF, 0), (F32, 0), (BF, 1), (F32, 1)])
+def test_top_list_distillation_counts_labels_that_are_no_tokens(dtype, slab_mib):
+    """stats.n_bad_labels as in cat_loss_fwd_bwd: unmasked rows whose label is outside the vocabulary, whether they have a list or not."""
+    T, K, d, V, k = 600, 4, 64, 900, 5
+    H, W, _ = rows(T, d, V, 0, dtype)
+    y, valid, bad, mask = bad_labels(T, V, 1)
+    eng = CatLoss(T, d, V, K, dtype=dtype, slab_mib=slab_mib)
+    ids, tl = lists(T, k, V, 2)
+    for n_lists in (T, 400):                     # the last rows are without a list
+        for m in (valid, None):
+            eng.topk_kd_forward_backward(H, W, y, m, ids[:n_lists], tl[:n_lists])
+            on = mask if m is not None else torch.ones(T, dtype=torch.bool)
+            s = eng.fwd_stats()
+            assert s.n_bad_labels == int((on & bad).sum())
+            assert s.n_valid == int((on & ~bad)[:n_lists].sum())
+    eng.forward_backward(H, W, y, valid.to(torch.uint8))
+    assert eng.fwd_stats().n_bad_labels == int((mask & bad).sum())
