@@ -917,7 +917,9 @@ int fused_core(const cat_shape* shape, const void* H, const void* W, const int64
     rows::finalize_kernel<<<1, rows::ROW_THREADS, 0, st>>>(partials, cta0, T / shape->K, loss,
                                                          reinterpret_cast<rows::StatsOut*>(stats), status);
     mark(st);
-    if (kd) kd::finalize_kernel<<<1, rows::ROW_THREADS, 0, st>>>(kd_row, valid_eff, T, kd->desc->beta, loss);
+    if (kd)
+        kd::finalize_kernel<<<1, rows::ROW_THREADS, 0, st>>>(kd_row, valid_eff, y, valid_in, T, V, kd->desc->beta, loss,
+                                                           reinterpret_cast<rows::StatsOut*>(stats));
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
 

@@ -16,6 +16,7 @@ namespace cat {
 namespace kd {
 
 using rows::ROW_THREADS;
+using rows::StatsOut;
 constexpr float LOG2E = 1.4426950408889634f;
 
 // A draft row takes part iff its mask bit is set, its label is a token id and its target
@@ -151,24 +152,29 @@ __global__ void __launch_bounds__(ROW_THREADS) z_to_dz_kernel(void* zs, const vo
 
 // Single CTA: loss_kd = (1/N) sum_r weight_r KD_r in a fixed order (fp64), and the total of
 // Eq. 12, beta * loss_ce + loss_kd.  loss[0] holds loss_ce on entry (written by the forward's
-// finalize kernel); on exit loss = {total, loss_ce, loss_kd}.
-__global__ void __launch_bounds__(ROW_THREADS) finalize_kernel(const float* kd_row, const unsigned char* valid_eff, int T, float beta,
-                                                               float* loss) {
+// finalize kernel); on exit loss = {total, loss_ce, loss_kd}.  Also counts the unmasked rows whose label is no token id, which the
+// kernels before it know only as rows that take no part.
+__global__ void __launch_bounds__(ROW_THREADS) finalize_kernel(const float* kd_row, const unsigned char* valid_eff, const long long* labels,
+                                                               const unsigned char* valid, int T, int V, float beta, float* loss,
+                                                               StatsOut* stats) {
     __shared__ double s_sum[ROW_THREADS];
-    __shared__ long long s_n[ROW_THREADS];
+    __shared__ long long s_n[ROW_THREADS], s_bad[ROW_THREADS];
     double acc = 0.0;
-    long long n = 0;
+    long long n = 0, bad = 0;
     for (int r = threadIdx.x; r < T; r += ROW_THREADS) {
         acc += static_cast<double>(kd_row[r]);
         n += valid_eff[r] ? 1 : 0;
+        bad += (valid == nullptr || valid[r] != 0) && (labels[r] < 0 || labels[r] >= V) ? 1 : 0;
     }
     s_sum[threadIdx.x] = acc;
     s_n[threadIdx.x] = n;
+    s_bad[threadIdx.x] = bad;
     __syncthreads();
     for (int off = ROW_THREADS / 2; off > 0; off >>= 1) {
         if (threadIdx.x < off) {
             s_sum[threadIdx.x] += s_sum[threadIdx.x + off];
             s_n[threadIdx.x] += s_n[threadIdx.x + off];
+            s_bad[threadIdx.x] += s_bad[threadIdx.x + off];
         }
         __syncthreads();
     }
@@ -178,6 +184,7 @@ __global__ void __launch_bounds__(ROW_THREADS) finalize_kernel(const float* kd_r
         loss[1] = ce;
         loss[2] = kdl;
         loss[0] = beta * ce + kdl;
+        if (stats) stats->n_bad_labels = s_bad[0];
     }
 }
 

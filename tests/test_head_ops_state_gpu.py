@@ -105,3 +105,19 @@ def test_top_list_distillation_counts_labels_that_are_no_tokens(dtype, slab_mib)
             assert s.n_valid == int((on & ~bad)[:n_lists].sum())
     eng.forward_backward(H, W, y, valid.to(torch.uint8))
     assert eng.fwd_stats().n_bad_labels == int((mask & bad).sum())
+
+
+def test_distillation_from_a_head_counts_labels_that_are_no_tokens():
+    T, K, d, V, L = 600, 4, 64, 900, 160
+    H, W, _ = rows(T, d, V, 0)
+    Ht, Wt, _ = rows(L, d, V, 3)
+    y, valid, bad, mask = bad_labels(T, V, 1)
+    start = torch.arange(T // K) + 12            # the last blocks run past the target's positions
+    has = ((start[:, None] + torch.arange(K)).reshape(-1) < L)
+    eng = CatLoss(T, d, V, K)
+    for m in (valid.to(torch.uint8), None):
+        eng.kd_forward_backward(H, W, y, m, Ht, Wt, start, 0.2)
+        on = mask if m is not None else torch.ones(T, dtype=torch.bool)
+        s = eng.fwd_stats()
+        assert s.n_bad_labels == int((on & bad).sum())
+        assert s.n_valid == int((on & ~bad & has).sum())
