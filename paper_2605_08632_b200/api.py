@@ -327,57 +327,51 @@ class TokenLogProb:
 
 
 class _LogProbFn(torch.autograd.Function):
-    """autograd glue: cat_logprob_fwd in forward(), cat_logprob_bwd in backward().  What backward() needs from the forward (lse,
-    entropy) is copied out of the engine, and the gradient buffers it wrote leave with the graph node, so further calls
-    through the same engine cannot overwrite either."""
+    """autograd glue: cat_logprob_fwd in forward(), cat_logprob_bwd in backward(), through an engine of the call's own.  Its results are the
+    caller's; its workspaces go back to torch's allocator as soon as each pass is enqueued, which hands them on in the order of the
+    stream."""
 
     @staticmethod
     def forward(ctx, H, W, labels, valid, engine):
         r = engine.forward(H.detach(), W.detach(), labels, valid)
-        lse, entropy = r.lse.clone(), r.entropy.clone()
+        engine.ws = engine.logp = engine.lse = engine.entropy = engine.top_ids = engine.top_logp = None
         ctx.engine = engine
         ctx.set_materialize_grads(False)
-        ctx.save_for_backward(H, W, labels, valid, lse, entropy)
-        logp = None if r.logp is None else r.logp.clone()
-        ids, tl = (None, None) if r.top_ids is None else (r.top_ids.clone(), r.top_logp.clone())
-        ctx.mark_non_differentiable(*(t for t in (ids, tl) if t is not None))
-        return logp, entropy.clone(), ids, tl
+        # the caller may write to the entropies that are handed out
+        ctx.save_for_backward(H, W, labels, valid, r.lse, r.entropy.clone() if any(ctx.needs_input_grad) else r.entropy)
+        ctx.mark_non_differentiable(*(t for t in (r.top_ids, r.top_logp) if t is not None))
+        return r.logp, r.entropy, r.top_ids, r.top_logp
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, g_logp, g_entropy, _ids, _tl):
         H, W, labels, valid, lse, entropy = ctx.saved_tensors
         e = ctx.engine
-        e.dH = e.dW = None
         dH, dW = e.backward(H.detach(), W.detach(), labels, valid, None if g_logp is None or labels is None else g_logp.contiguous(),
                             None if g_entropy is None else g_entropy.contiguous(), lse=lse, entropy=entropy)
-        e.dH = e.dW = None
+        e.dH = e.dW = e._ws_bwd = None
         return dH, dW, None, None, None
 
 
 class LogProbModule(torch.nn.Module):
     """Head of a scoring or policy-gradient loop: `logp, entropy, top_ids, top_logp = head(H, labels, valid)` with H [T, d] and
     `weight` [V, d] as the LM head; logp and entropy carry gradients to H and the weight.  The gradient of the weight is formed in
-    the weight's type.  One engine is kept per distinct T.  Not for stream capture with gradients: autograd may then wait for other
-    streams inside the capture; capture TokenLogProb.forward and backward instead."""
+    the weight's type.  Calls share nothing: any lengths, streams and threads.  Not for stream capture with gradients: autograd may then
+    wait for other streams inside the capture; capture TokenLogProb.forward and backward instead."""
 
     def __init__(self, weight: torch.Tensor, top_k: int = 0, slab_mib: int = 0):
         super().__init__()
         self.weight = weight if isinstance(weight, torch.nn.Parameter) else torch.nn.Parameter(weight)
         self.top_k = top_k
         self.slab_mib = slab_mib
-        self._engines = {}
 
     def forward(self, H, labels=None, valid=None):
         if torch.is_grad_enabled() and (H.requires_grad or self.weight.requires_grad) and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("LogProbModule cannot be captured with gradients: capture TokenLogProb.forward and backward")
         T, d = H.shape
-        key = (T, H.device, H.dtype)
-        eng = self._engines.get(key)
-        if eng is None:
-            eng = self._engines[key] = TokenLogProb(T, d, self.weight.shape[0], self.top_k, dtype=H.dtype, dW_dtype=self.weight.dtype,
-                                                    slab_mib=self.slab_mib, device=str(H.device))
-        return _LogProbFn.apply(H, self.weight, labels, valid, eng)
+        engine = TokenLogProb(T, d, self.weight.shape[0], self.top_k, dtype=H.dtype, dW_dtype=self.weight.dtype, slab_mib=self.slab_mib,
+                              device=str(H.device))
+        return _LogProbFn.apply(H, self.weight, labels, valid, engine)
 
 
 class _CatLossFn(torch.autograd.Function):
