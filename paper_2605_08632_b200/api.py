@@ -357,7 +357,8 @@ class LogProbModule(torch.nn.Module):
     """Head of a scoring or policy-gradient loop: `logp, entropy, top_ids, top_logp = head(H, labels, valid)` with H [T, d] and
     `weight` [V, d] as the LM head; logp and entropy carry gradients to H and the weight.  The gradient of the weight is formed in
     the weight's type.  Calls share nothing: any lengths, streams and threads.  Not for stream capture with gradients: autograd may then
-    wait for other streams inside the capture; capture TokenLogProb.forward and backward instead."""
+    wait for other streams inside the capture; capture TokenLogProb.forward and backward instead.  With gradients the weight has to
+    be contiguous, and an H whose rows lie further apart is copied."""
 
     def __init__(self, weight: torch.Tensor, top_k: int = 0, slab_mib: int = 0):
         super().__init__()
@@ -366,8 +367,12 @@ class LogProbModule(torch.nn.Module):
         self.slab_mib = slab_mib
 
     def forward(self, H, labels=None, valid=None):
-        if torch.is_grad_enabled() and (H.requires_grad or self.weight.requires_grad) and torch.cuda.is_current_stream_capturing():
-            raise RuntimeError("LogProbModule cannot be captured with gradients: capture TokenLogProb.forward and backward")
+        if torch.is_grad_enabled() and (H.requires_grad or self.weight.requires_grad):
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("LogProbModule cannot be captured with gradients: capture TokenLogProb.forward and backward")
+            if not self.weight.is_contiguous():
+                raise ValueError("weight must be contiguous for gradients: theirs are laid out like it")
+            H = H.contiguous()
         T, d = H.shape
         engine = TokenLogProb(T, d, self.weight.shape[0], self.top_k, dtype=H.dtype, dW_dtype=self.weight.dtype, slab_mib=self.slab_mib,
                               device=str(H.device))

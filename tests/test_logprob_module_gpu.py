@@ -140,3 +140,20 @@ def test_captured_without_gradients_beside_eager_calls():
         e = TokenLogProb(T, d, V, 5)
         r = e.forward(new[0], W, y, valid)
         assert torch.equal(out[0], r.logp) and torch.equal(out[1], r.entropy) and torch.equal(out[2], r.top_ids) and torch.equal(out[3], r.top_logp)
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_pitched_hidden_states_get_their_gradient(dtype):
+    T, d, V = 50, 64, 900
+    H, W, y, valid = inputs(T, d, V, dtype, 1)
+    g = torch.randn(T, generator=torch.Generator().manual_seed(3)).to(DEV)
+    want = step(LogProbModule(W.clone()), H, y, valid, g, g)
+    wide = torch.zeros(T, d + 16, dtype=dtype, device=DEV)
+    wide[:, :d] = H
+    wide.requires_grad_()
+    head = LogProbModule(W.clone())
+    logp, entropy, _, _ = head(wide[:, :d], y, valid)
+    (logp * g + entropy * g).sum().backward()
+    assert torch.equal(wide.grad[:, :d], want[4]) and not wide.grad[:, d:].any()
+    assert torch.equal(head.weight.grad, want[5])
+    pitched = torch.zeros(V, d + 16, dtype=dtype, device=DEV)[:, :d]
+    with pytest.raises(ValueError, match="weight"):        # at once, not after the forward pass
+        LogProbModule(torch.nn.Parameter(pitched))(H, y, valid)
