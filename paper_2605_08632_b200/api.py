@@ -345,6 +345,8 @@ class _LogProbFn(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, g_logp, g_entropy, _ids, _tl):
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("LogProbModule's backward pass cannot be captured: capture TokenLogProb.forward and backward")
         H, W, labels, valid, lse, entropy = ctx.saved_tensors
         e = ctx.engine
         dH, dW = e.backward(H.detach(), W.detach(), labels, valid, None if g_logp is None or labels is None else g_logp.contiguous(),
