@@ -421,12 +421,13 @@ int cat_logprob_fwd(const cat_shape* shape, const void* H, const void* W, const 
  * Gradients of sum_r (grad_logp[r] logp[r] + grad_entropy[r] entropy[r]) with respect to H and W:
  *     dz[r, v] = grad_logp[r] ([v == y_r] - p[r, v]) - grad_entropy[r] p[r, v] (log p[r, v] + entropy[r]),
  *     dH = dz W,   dW = dz^T H.
- * The logits are recomputed per vocabulary slab, as in cat_loss_bwd; dz is rounded once to in_dtype (for up to 128 bf16 rows
- * kept as two terms, for up to 1024 the label's entry not rounded, unless slab_mib cuts the vocabulary).  Rows with
+ * The logits are recomputed per row slab (at most about slab_mib MiB of dz, default 3 GiB) and dz is rounded once to in_dtype (for up to
+ * 128 bf16 rows kept as two terms, for up to 1024 the label's entry not rounded).  A row's gradient by its logits sums to zero, and the entry
+ * of a token that has most of the probability is taken from that: as exact as the others, however near to 1 its probability is.  Rows with
  * valid[r] == 0 get a zero dH row and add nothing to dW, whatever H holds there; a label that is no token id
  * contributes through the entropy only.  No gradient flows through the alternatives.
- *   lse, entropy   [T] fp32 as written by cat_logprob_fwd for the same rows of H and the same W (a row's gradient by its
- *                  logits is taken to sum to zero); entropy may be NULL without grad_entropy   (device, in)
+ *   lse, entropy   [T] fp32 as written by cat_logprob_fwd for the same rows of H and the same W; entropy may be NULL without
+ *                  grad_entropy   (device, in)
  *   grad_logp      [T] fp32, or NULL (then labels may be NULL too)                 (device, in)
  *   grad_entropy   [T] fp32, or NULL                                               (device, in)
  *   dH [T, d] of in_dtype with pitch ldH;  dW [V, d] of dW_dtype with pitch ldW; accumulate_dW as in cat_loss_bwd
@@ -438,7 +439,8 @@ int cat_logprob_bwd(const cat_shape* shape, const void* H, const void* W, const 
                     void* dH, void* dW, int accumulate_dW,
                     void* workspace, size_t workspace_bytes, void* cuda_stream);
 
-/* Scratch bytes: pass 0 = cat_logprob_fwd with this top_k, pass 1 = cat_logprob_bwd.  0 if anything is invalid. */
+/* Scratch bytes: pass 0 = cat_logprob_fwd with this top_k, pass 1 = cat_logprob_bwd (a slab, and with several of them an fp32 sum of
+ * dW's size).  0 if anything is invalid. */
 size_t cat_logprob_workspace_bytes(const cat_shape* shape, int top_k, int pass);
 
 /*

@@ -20,6 +20,7 @@ namespace f32 {
 constexpr int TM = 64, TN = 64, TK = 16, THREADS = 128;
 constexpr int RUN = 256 / TK;            // slices per run of the sum
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr float CLOSING = -0.5f;         // log p from which on close_kernel writes the entry: at most one token of a row
 constexpr float LOW = -1.0e30f;          // "no column yet": finite, so that 0 * (LOW - m) is 0
 
 enum { FWD = 0, DZ = 1, OUT = 2 };
@@ -51,10 +52,9 @@ struct EpiParams {
     const float* entropy;
     const float* grad_logp;
     const float* grad_entropy;
-    const float* dz_label;       // the label's entry, with grad_logp; nullptr: label_kernel writes it
+    int* closing;                // [M] raised to the column of the entry that close_kernel writes; -1 on entry
     float* dz;
     long long ld_dz;
-    int v0;
     // OUT
     const float* alpha;          // device scalar or nullptr
     const float* add;            // or nullptr; only with one part
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(THREADS, 4) gemm_kernel(const Operands op, con
                     s_m[at] = m_new;
                 }
             } else if (row < op.M) {
-                float dz_y = 0.f, ca = 0.f, cb = 0.f, lse = 0.f;
+                float gl = 0.f, ca = 0.f, cb = 0.f, lse = 0.f;
                 int y = -1;
                 bool on = false;
                 if (MODE == DZ) {
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(THREADS, 4) gemm_kernel(const Operands op, con
                     if (on) {
                         lse = ep.lse[row];
                         const long long yy = ep.grad_logp ? ep.labels[row] : -1;
-                        if (yy >= 0 && yy < ep.V) { y = static_cast<int>(yy) - ep.v0; dz_y = ep.dz_label ? ep.dz_label[row] : 0.f; ca = -ep.grad_logp[row]; }
+                        if (yy >= 0 && yy < ep.V) { y = static_cast<int>(yy); gl = ep.grad_logp[row]; ca = -gl; }
                         if (ep.grad_entropy) { cb = -ep.grad_entropy[row]; ca = fmaf(cb, ep.entropy[row], ca); }
                     }
                 }
@@ -235,8 +235,9 @@ __global__ void __launch_bounds__(THREADS, 4) gemm_kernel(const Operands op, con
                     if (col >= op.N) continue;
                     if (MODE == DZ) {
                         const float x = total[i][j] - lse;
-                        const float v = col == y ? dz_y : expf(x) * fmaf(cb, x, ca);
+                        const float v = fmaf(expf(x), fmaf(cb, x, ca), col == y ? gl : 0.f);
                         ep.dz[row * ep.ld_dz + col] = on ? v : 0.f;
+                        if (on && x > CLOSING) atomicMax(ep.closing + row, col);
                     } else if (gridDim.z > 1) {
                         ep.out[blockIdx.z * ep.part_stride + row * ep.ld_out + col] = total[i][j];
                     } else {
@@ -263,13 +264,13 @@ __global__ void __launch_bounds__(THREADS, 4) gemm_kernel(const Operands op, con
     }
 }
 
-// The labels' entries of dz, one CTA per row.  A row of dz sums to zero, so its label's entry is the others' sum with the sign turned: as
-// exact as they are, where gl (1 - p) of a row that is sure of its label keeps the rounding of z and lse (1e-6 of lse) against 1 - p.
-__global__ void __launch_bounds__(256) label_kernel(float* dz, long long ld, int V, const long long* labels, const unsigned char* valid) {
+// The entry of a token that has most of its row's probability, one CTA per row.  A row of dz sums to zero, so it is the others' sum with the sign
+// turned: as exact as they are, where gl (1 - p) of a row that is sure of its label keeps the rounding of z and lse (1e-6 of lse) against 1 - p.
+__global__ void __launch_bounds__(256) close_kernel(float* dz, long long ld, int V, const int* closing) {
     __shared__ float s_sum[8];
     const long long row = blockIdx.x;
-    const long long y = labels[row];
-    if ((valid != nullptr && valid[row] == 0) || y < 0 || y >= V) return;
+    const int y = closing[row];
+    if (y < 0) return;
     float* z = dz + row * ld;
     float sum = 0.f;
     for (int v = threadIdx.x; v < V; v += 256) sum += v == y ? 0.f : z[v];

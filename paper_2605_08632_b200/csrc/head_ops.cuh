@@ -264,166 +264,6 @@ int lp_slab(const cat_shape* s, const LpPlan& plan, const CUtensorMap& tmW, cons
                                              entropy, top_ids, top_logp, st);
 }
 
-// ------------------------------------------------------------------------------ gradients of the log probabilities
-// As cat_loss_bwd: the vocabulary in slabs, per slab recomputed logits -> dz, dW of the slab, dH summed over the slabs.
-struct LpBwdPlan {
-    BwdPlan b;
-    long long lo;          // rows before the second terms of dz, or 0
-    bool rest;             // labels' entries of dz to more than bf16 (kLabelRestRows)
-    size_t off_h, off_label, off_rest, off_part, total;
-};
-
-LpBwdPlan plan_lp_bwd(const cat_shape* s) {
-    LpBwdPlan p;
-    const bool bf16 = s->in_dtype == CAT_BF16;
-    cat_shape t = *s;
-    p.lo = bf16 ? lo_rows_of(s->T) : 0;
-    if (p.lo > 0) {
-        t.T = 2 * p.lo;
-        p.b = plan_bwd(&t);
-        if (p.b.n_slabs > 1) { p.lo = 0; t.T = s->T; }       // a vocabulary of millions, or a small cap on the slab
-    }
-    if (p.lo == 0) p.b = plan_bwd(s);
-    size_t off = align256(p.b.total);
-    p.off_h = off;    off = align256(off + (bf16 ? 2 : 4) * static_cast<size_t>(t.T) * static_cast<size_t>(s->d));
-    p.off_label = off; off = align256(off + sizeof(float) * static_cast<size_t>(s->T));
-    p.rest = bf16 && p.lo == 0 && s->T <= kLabelRestRows && p.b.n_slabs == 1;
-    p.off_rest = off;  if (p.rest) off = align256(off + 4 * sizeof(float) * static_cast<size_t>(s->T));
-    p.off_part = off;
-    off += !bf16 ? kF32PartBytes : p.b.n_slabs == 1 ? dh_part_bytes(t.T, s->d, s->V, p.lo > 0 || p.rest) : 0;
-    p.total = off;
-    return p;
-}
-
-struct LpGrads {
-    const int64_t* labels;
-    const uint8_t* valid;
-    const float *lse, *entropy, *grad_logp, *grad_entropy;
-};
-
-// The rows of H as the dW contraction takes them (in `copy`), and the labels' entries of dz; NULL: not wanted.
-template <class TI>
-int launch_bwd_rows(const cat_shape* s, const TI* H, const TI* W, const LpGrads& a, long long rows, long long lo, TI* copy, float* dz_label,
-                    float* rest, cudaStream_t st) {
-    if (copy == nullptr && (a.grad_logp == nullptr || dz_label == nullptr)) return CAT_OK;
-    lp::BwdRows<TI> p;
-    p.H = H; p.W = W; p.ldH = s->ldH; p.ldW = s->ldW;
-    p.d = static_cast<int>(s->d); p.T = static_cast<int>(s->T); p.V = static_cast<int>(s->V);
-    p.valid = a.valid; p.labels = reinterpret_cast<const long long*>(a.labels); p.lse = a.lse; p.entropy = a.entropy;
-    p.grad_logp = dz_label ? a.grad_logp : nullptr; p.grad_entropy = a.grad_entropy;
-    p.dz_label = dz_label; p.out = copy; p.lo = static_cast<int>(lo);
-    p.rest = rest; p.key = reinterpret_cast<int*>(rest) + s->T; p.from = p.key + s->T; p.coef = rest + 3 * s->T;
-    lp::bwd_rows_kernel<TI><<<static_cast<unsigned>(rows), lp::THREADS, 0, st>>>(p);
-    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
-}
-
-int lp_bwd_bf16(const cat_shape* s, const LpBwdPlan& plan, const __nv_bfloat16* H, const __nv_bfloat16* W, const LpGrads& a,
-                __nv_bfloat16* dH, void* dW, int accumulate_dW, uint8_t* ws, int sm_count, cudaStream_t st) {
-    int* status = reinterpret_cast<int*>(ws);
-    __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + plan.b.off_dz);
-    __nv_bfloat16* Hz = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_h);
-    float* dh_acc = reinterpret_cast<float*>(ws + plan.b.off_dh_acc);
-    const int d = static_cast<int>(s->d);
-    const long long rows = plan.lo > 0 ? 2 * plan.lo : s->T;             // of dz
-    const bool copy_H = a.valid != nullptr || plan.lo > 0;
-    float* dz_label = reinterpret_cast<float*>(ws + plan.off_label);
-    float* rest = plan.rest && a.grad_logp ? reinterpret_cast<float*>(ws + plan.off_rest) : nullptr;
-    const int first_rc = launch_bwd_rows(s, H, W, a, rows, plan.lo, copy_H ? Hz : nullptr, dz_label, rest, st);
-    if (first_rc != CAT_OK) return first_rc;
-    CUtensorMap tmH_k, tmH_mn;
-    if (tmap_a(&tmH_k, H, s->T, s->d, s->ldH) != CAT_OK ||
-        tmap_mn_major(&tmH_mn, copy_H ? Hz : H, rows, s->d, copy_H ? s->d : s->ldH) != CAT_OK)
-        return CAT_ERR_CUDA;
-    for (int sl = 0; sl < plan.b.n_slabs; ++sl) {
-        const long long v0 = static_cast<long long>(sl) * plan.b.Vs;
-        const long long width = (s->V - v0) < plan.b.Vs ? (s->V - v0) : plan.b.Vs;
-        const bool first = sl == 0, last = sl == plan.b.n_slabs - 1;
-        const __nv_bfloat16* Wb = W + v0 * s->ldW;
-        CUtensorMap tmW_k, tmW_mn, tmDz_k, tmDz_mn, tmDz_out;
-        if (tmap_b(&tmW_k, Wb, width, s->d, s->ldW) != CAT_OK || tmap_mn_major(&tmW_mn, Wb, width, s->d, s->ldW) != CAT_OK ||
-            tmap_a(&tmDz_k, dz, rows, width, plan.b.Vs) != CAT_OK || tmap_mn_major(&tmDz_mn, dz, rows, width, plan.b.Vs) != CAT_OK ||
-            tmap_out(&tmDz_out, dz, rows, width, plan.b.Vs) != CAT_OK)
-            return CAT_ERR_CUDA;
-        tc::EpiDzLp::Params zp;
-        zp.labels = reinterpret_cast<const long long*>(a.labels); zp.valid = a.valid; zp.lse = a.lse; zp.entropy = a.entropy;
-        zp.grad_logp = a.grad_logp; zp.grad_entropy = a.grad_entropy; zp.dz_label = dz_label; zp.T = static_cast<int>(s->T); zp.V = static_cast<int>(s->V);
-        zp.v0 = static_cast<int>(v0); zp.lo_rows = static_cast<int>(plan.lo);
-        int rc = launch_tc<0, 0, tc::EpiDzLp>(tmH_k, tmW_k, make_sched(s->T, width, s->d, fwd_splits(s->T, width), band_tiles(s->d), 0), zp,
-                                              status, sm_count, st, &tmDz_out);
-        if (rc != CAT_OK) return rc;
-        tc::EpiOut::Params ep;
-        memset(&ep, 0, sizeof(ep));
-        ep.M = static_cast<int>(width); ep.N = d; ep.ld_add = s->ldW; ep.ld_out = s->ldW;
-        if (s->dW_dtype == CAT_F32) {
-            ep.out_f32 = static_cast<float*>(dW) + v0 * s->ldW;
-            if (accumulate_dW) ep.add_f32 = ep.out_f32;
-        } else {
-            ep.out_bf16 = static_cast<__nv_bfloat16*>(dW) + v0 * s->ldW;
-            if (accumulate_dW) ep.add_bf16 = ep.out_bf16;
-        }
-        const tc::Sched dw_sched = make_sched(width, s->d, rows, 0, 1, 1);
-        if (rest) {
-            tc::EpiOutT<true>::Params sp;
-            memset(&sp, 0, sizeof(sp));
-            sp.add_f32 = ep.add_f32; sp.add_bf16 = ep.add_bf16; sp.out_f32 = ep.out_f32; sp.out_bf16 = ep.out_bf16;
-            sp.ld_add = ep.ld_add; sp.ld_out = ep.ld_out; sp.M = ep.M; sp.N = ep.N;
-            sp.key = reinterpret_cast<int*>(rest) + s->T; sp.from = sp.key + s->T; sp.coef = rest + 3 * s->T;
-            sp.src = H; sp.ld_src = s->ldH; sp.n = static_cast<int>(s->T);
-            rc = launch_out<1, 1, true>(tmDz_mn, tmH_mn, dw_sched, sp, status, sm_count, st);
-        } else {
-            rc = launch_out<1, 1>(tmDz_mn, tmH_mn, dw_sched, ep, status, sm_count, st);
-        }
-        if (rc != CAT_OK) return rc;
-        if (plan.b.n_slabs == 1) {
-            const lp::LabelRest label{rest, reinterpret_cast<const long long*>(a.labels), W, s->ldW};
-            rc = launch_dh(tmDz_k, tmW_mn, s->T, s->d, s->V, nullptr, dH, s->ldH, reinterpret_cast<float*>(ws + plan.off_part), status, sm_count,
-                           st, plan.lo, rest ? &label : nullptr);
-        } else {
-            memset(&ep, 0, sizeof(ep));
-            ep.M = static_cast<int>(s->T); ep.N = d;
-            if (!first) { ep.add_f32 = dh_acc; ep.ld_add = s->d; }
-            if (last) { ep.out_bf16 = dH; ep.ld_out = s->ldH; }
-            else { ep.out_f32 = dh_acc; ep.ld_out = s->d; }
-            rc = launch_out<0, 1>(tmDz_k, tmW_mn, make_sched(s->T, s->d, width, 0, 1, 1), ep, status, sm_count, st);
-        }
-        if (rc != CAT_OK) return rc;
-    }
-    return CAT_OK;
-}
-
-int lp_bwd_f32(const cat_shape* s, const LpBwdPlan& plan, const float* H, const float* W, const LpGrads& a, float* dH, float* dW,
-               int accumulate_dW, uint8_t* ws, cudaStream_t st) {
-    float* dz = reinterpret_cast<float*>(ws + plan.b.off_dz);
-    float* Hz = reinterpret_cast<float*>(ws + plan.off_h);
-    float* part = reinterpret_cast<float*>(ws + plan.off_part);
-    const int T = static_cast<int>(s->T), d = static_cast<int>(s->d);
-    const bool whole = plan.b.n_slabs == 1 && a.grad_logp != nullptr;        // whole rows of dz at a time: see f32::label_kernel
-    float* dz_label = whole ? nullptr : reinterpret_cast<float*>(ws + plan.off_label);
-    const int first_rc = launch_bwd_rows(s, H, W, a, s->T, 0, a.valid ? Hz : nullptr, dz_label, nullptr, st);
-    if (first_rc != CAT_OK) return first_rc;
-    for (int sl = 0; sl < plan.b.n_slabs; ++sl) {
-        const long long v0 = static_cast<long long>(sl) * plan.b.Vs;
-        const int w = static_cast<int>((s->V - v0) < plan.b.Vs ? (s->V - v0) : plan.b.Vs);
-        const float* Wf = W + v0 * s->ldW;
-        f32::Operands op;
-        f32::EpiParams ep;
-        memset(&ep, 0, sizeof(ep));
-        op.A = H; op.sAm = s->ldH; op.sAk = 1; op.B = Wf; op.sBk = 1; op.sBn = s->ldW;
-        op.M = T; op.N = w; op.Kd = d; op.n_groups = static_cast<int>(cdiv(w, f32::TN));
-        ep.labels = reinterpret_cast<const long long*>(a.labels); ep.valid = a.valid; ep.lse = a.lse; ep.entropy = a.entropy;
-        ep.grad_logp = a.grad_logp; ep.grad_entropy = a.grad_entropy; ep.dz_label = dz_label; ep.dz = dz; ep.ld_dz = plan.b.Vs; ep.V = static_cast<int>(s->V);
-        ep.v0 = static_cast<int>(v0);
-        f32::gemm_kernel<f32::DZ, true, true><<<dim3(static_cast<unsigned>(cdiv(T, f32::TM)), static_cast<unsigned>(op.n_groups)), f32::THREADS, 0, st>>>(op, ep);
-        if (whole) f32::label_kernel<<<static_cast<unsigned>(T), 256, 0, st>>>(dz, plan.b.Vs, w, ep.labels, a.valid);
-        if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
-        int rc = launch_f32_dw(dz, plan.b.Vs, a.valid ? Hz : H, a.valid ? s->d : s->ldH, w, d, T, nullptr, dW + v0 * s->ldW, s->ldW,
-                               accumulate_dW != 0, part, st);
-        if (rc == CAT_OK) rc = launch_f32_dh(dz, plan.b.Vs, Wf, s->ldW, T, d, w, nullptr, dH, s->ldH, sl > 0, part, st);
-        if (rc != CAT_OK) return rc;
-    }
-    return CAT_OK;
-}
-
 // ------------------------------------------------------------------------------ distillation from top logits
 int check_topk_kd(const cat_topk_kd_desc* k) {
     if (!k) return CAT_ERR_NULL;
@@ -431,6 +271,38 @@ int check_topk_kd(const cat_topk_kd_desc* k) {
     if (!(k->beta >= 0.f && k->beta <= 3.0e38f)) return CAT_ERR_SHAPE;
     if (k->renormalize != 0 && k->renormalize != 1) return CAT_ERR_SHAPE;
     return CAT_OK;
+}
+
+// Row slabs of the fp32 operators: the logits of whole draft blocks, as many as the cap allows.
+FusedPlan plan_fused_f32(const cat_shape* s) {
+    FusedPlan f;
+    memset(&f, 0, sizeof(f));
+    f.ldz = cdiv(s->V, 8) * 8;
+    const long long mib = s->slab_mib > 0 ? s->slab_mib : kDefaultFusedSlabMiB;
+    long long cap = (mib << 20) / (f.ldz * 4) / s->K * s->K;
+    const long long least = cdiv(f32::TM, s->K) * s->K;          // whole blocks that fill a row tile
+    if (cap < least) cap = least;
+    f.Ts = cap < s->T ? cap : s->T;
+    f.n_slabs = static_cast<int>(cdiv(s->T, f.Ts));
+    f.warp_scan = s->K <= 32 && (s->K & (s->K - 1)) == 0;
+    f.S_max = 1;
+    for (long long r0 = 0; r0 < s->T; r0 += f.Ts) {
+        const long long rws = (s->T - r0) < f.Ts ? (s->T - r0) : f.Ts;
+        const int S = f32_splits(rws, s->V);
+        if (S > f.S_max) f.S_max = S;
+        f.n_row_ctas += static_cast<int>(cdiv(f.warp_scan ? rws : rws / s->K, rows::ROW_THREADS));
+    }
+    size_t off = kHeaderBytes;
+    f.off_part_m = off;   off = align256(off + sizeof(float) * f.S_max * f.Ts);
+    f.off_part_l = off;   off = align256(off + sizeof(float) * f.S_max * f.Ts);
+    f.off_z_label = off;  off = align256(off + sizeof(float) * s->T);
+    f.off_row_ce = off;   off = align256(off + sizeof(float) * s->T);
+    f.off_partials = off; off = align256(off + sizeof(rows::CtaPartial) * f.n_row_ctas);
+    f.off_ref = off;      off = align256(off + sizeof(float) * s->T);
+    f.off_hs = off;       off = align256(off + sizeof(float) * static_cast<size_t>(f.Ts) * static_cast<size_t>(s->d));
+    f.off_z = off;        off = align256(off + sizeof(float) * static_cast<size_t>(f.Ts) * f.ldz);
+    f.total = off;
+    return f;
 }
 
 struct TkPlan {
@@ -444,32 +316,7 @@ TkPlan plan_tk(const cat_shape* s, int k) {
     if (s->in_dtype == CAT_BF16) {
         p.f = plan_fused(s, false);
     } else {
-        FusedPlan& f = p.f;
-        memset(&f, 0, sizeof(f));
-        f.ldz = cdiv(s->V, 8) * 8;
-        const long long mib = s->slab_mib > 0 ? s->slab_mib : kDefaultFusedSlabMiB;
-        long long cap = (mib << 20) / (f.ldz * 4) / s->K * s->K;
-        if (cap < s->K) cap = s->K;
-        f.Ts = cap < s->T ? cap : s->T;
-        f.n_slabs = static_cast<int>(cdiv(s->T, f.Ts));
-        f.warp_scan = s->K <= 32 && (s->K & (s->K - 1)) == 0;
-        f.S_max = 1;
-        for (long long r0 = 0; r0 < s->T; r0 += f.Ts) {
-            const long long rws = (s->T - r0) < f.Ts ? (s->T - r0) : f.Ts;
-            const int S = f32_splits(rws, s->V);
-            if (S > f.S_max) f.S_max = S;
-            f.n_row_ctas += static_cast<int>(cdiv(f.warp_scan ? rws : rws / s->K, rows::ROW_THREADS));
-        }
-        size_t off = kHeaderBytes;
-        f.off_part_m = off;   off = align256(off + sizeof(float) * f.S_max * f.Ts);
-        f.off_part_l = off;   off = align256(off + sizeof(float) * f.S_max * f.Ts);
-        f.off_z_label = off;  off = align256(off + sizeof(float) * s->T);
-        f.off_row_ce = off;   off = align256(off + sizeof(float) * s->T);
-        f.off_partials = off; off = align256(off + sizeof(rows::CtaPartial) * f.n_row_ctas);
-        f.off_ref = off;      off = align256(off + sizeof(float) * s->T);
-        f.off_hs = off;       off = align256(off + sizeof(float) * static_cast<size_t>(f.Ts) * static_cast<size_t>(s->d));
-        f.off_z = off;        off = align256(off + sizeof(float) * static_cast<size_t>(f.Ts) * f.ldz);
-        f.total = off;
+        p.f = plan_fused_f32(s);
     }
     p.ld_zt = k + 1;
     size_t off = align256(p.f.total);
@@ -493,18 +340,20 @@ TkPlan plan_tk(const cat_shape* s, int k) {
     return p;
 }
 
-// dH[r0 : r0 + rws, :] = (g/N) dz W and dW (+)= (g/N) dz^T Hw of one row slab; Hw: the slab's rows of H with pitch ldHw.  lo > 0: dz in
-// two terms (kTwoTermRows).
+// dH[r0 : r0 + rws, :] = scale dz W and dW (+)= scale dz^T Hw of one row slab; Hw: the slab's rows of H with pitch ldHw.  lo > 0: dz in
+// two terms (kTwoTermRows).  rest, sparse: what the rounding left of the labels' entries (kLabelRestRows), without scale.  dw_sum: the sum over
+// the slabs goes there ([V, d], fp32) and dW is left alone.
 int slab_grads(const cat_shape* s, const FusedPlan& f, const void* W, const void* Hw, long long ldHw, void* zs, uint8_t* ws, long long r0,
                long long rws, long long lo, bool first, bool last, const float* scale, float* part, void* dH, void* dW, int accumulate_dW, int sm_count,
-               cudaStream_t st) {
+               cudaStream_t st, const lp::LabelRest* rest = nullptr, const tc::SparseTerms<true>* sparse = nullptr,
+               float* dw_sum = nullptr) {
     const int V = static_cast<int>(s->V), d = static_cast<int>(s->d), R = static_cast<int>(rws);
     if (s->in_dtype != CAT_BF16) {
         const int rc = launch_f32_dh(static_cast<float*>(zs), f.ldz, static_cast<const float*>(W), s->ldW, R, d, V, scale,
                                      static_cast<float*>(dH) + r0 * s->ldH, s->ldH, false, part, st);
         if (rc != CAT_OK) return rc;
-        return launch_f32_dw(static_cast<float*>(zs), f.ldz, static_cast<const float*>(Hw), ldHw, V, d, R, scale, static_cast<float*>(dW),
-                             s->ldW, !first || accumulate_dW, part, st);
+        return launch_f32_dw(static_cast<float*>(zs), f.ldz, static_cast<const float*>(Hw), ldHw, V, d, R, scale,
+                             dw_sum ? dw_sum : static_cast<float*>(dW), dw_sum ? s->d : s->ldW, !first || (accumulate_dW && !dw_sum), part, st);
     }
     int* status = reinterpret_cast<int*>(ws);
     CUtensorMap tmZ_k, tmZ_mn, tmW_mn, tmH_mn;
@@ -513,15 +362,15 @@ int slab_grads(const cat_shape* s, const FusedPlan& f, const void* W, const void
         tmap_mn_major(&tmW_mn, W, s->V, s->d, s->ldW) != CAT_OK || tmap_mn_major(&tmH_mn, Hw, all, s->d, ldHw) != CAT_OK)
         return CAT_ERR_CUDA;
     const int rc = launch_dh(tmZ_k, tmW_mn, rws, s->d, s->V, scale, static_cast<__nv_bfloat16*>(dH) + r0 * s->ldH, s->ldH, part, status,
-                             sm_count, st, lo);
+                             sm_count, st, lo, rest);
     if (rc != CAT_OK) return rc;
     tc::EpiOut::Params ep;
     memset(&ep, 0, sizeof(ep));
     ep.alpha = scale; ep.M = V; ep.N = d;
     float* dw_acc = reinterpret_cast<float*>(ws + f.off_dw_acc);
-    if (s->dW_dtype == CAT_F32) {
-        ep.out_f32 = static_cast<float*>(dW); ep.ld_out = s->ldW;
-        if (!first || accumulate_dW) { ep.add_f32 = ep.out_f32; ep.ld_add = s->ldW; }
+    if (dw_sum || s->dW_dtype == CAT_F32) {
+        ep.out_f32 = dw_sum ? dw_sum : static_cast<float*>(dW); ep.ld_out = dw_sum ? s->d : s->ldW;
+        if (!first || (accumulate_dW && !dw_sum)) { ep.add_f32 = ep.out_f32; ep.ld_add = ep.ld_out; }
     } else {        // bf16 dW: several slabs are summed in fp32 scratch and rounded once at the end
         if (first) {
             if (accumulate_dW) { ep.add_bf16 = static_cast<const __nv_bfloat16*>(dW); ep.ld_add = s->ldW; }
@@ -531,7 +380,14 @@ int slab_grads(const cat_shape* s, const FusedPlan& f, const void* W, const void
         if (last) { ep.out_bf16 = static_cast<__nv_bfloat16*>(dW); ep.ld_out = s->ldW; }
         else { ep.out_f32 = dw_acc; ep.ld_out = s->d; }
     }
-    return launch_out<1, 1>(tmZ_mn, tmH_mn, make_sched(s->V, s->d, all, 0, 1, 1), ep, status, sm_count, st);
+    const tc::Sched sched = make_sched(s->V, s->d, all, 0, 1, 1);
+    if (sparse == nullptr) return launch_out<1, 1>(tmZ_mn, tmH_mn, sched, ep, status, sm_count, st);
+    tc::EpiOutT<true>::Params sp;
+    memset(&sp, 0, sizeof(sp));
+    static_cast<tc::SparseTerms<true>&>(sp) = *sparse;
+    sp.add_f32 = ep.add_f32; sp.add_bf16 = ep.add_bf16; sp.out_f32 = ep.out_f32; sp.out_bf16 = ep.out_bf16;
+    sp.ld_add = ep.ld_add; sp.ld_out = ep.ld_out; sp.M = ep.M; sp.N = ep.N; sp.alpha = ep.alpha;
+    return launch_out<1, 1, true>(tmZ_mn, tmH_mn, sched, sp, status, sm_count, st);
 }
 
 template <class TI>
@@ -639,6 +495,135 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
 
+// ------------------------------------------------------------------------------ gradients of the log probabilities
+// By row slabs, as cat_topk_kd_loss_fwd_bwd: per slab recomputed logits -> dz, the closing entries (which need whole rows), dH of the slab's rows, dW
+// summed over the slabs.
+struct LpBwdPlan {
+    FusedPlan f;
+    long long lo;          // rows before the second terms of dz, or 0
+    bool rest;             // labels' entries of dz to more than bf16 (kLabelRestRows)
+    size_t off_rest, off_part, off_dw_sum, total;
+};
+
+LpBwdPlan plan_lp_bwd(const cat_shape* s) {
+    LpBwdPlan p;
+    const bool bf16 = s->in_dtype == CAT_BF16;
+    p.f = bf16 ? plan_fused(s, false) : plan_fused_f32(s);
+    p.lo = bf16 ? lo_rows_of(s->T) : 0;                  // a slab is never lower than 128 rows
+    p.rest = bf16 && p.lo == 0 && s->T <= kLabelRestRows;
+    size_t off = align256(p.f.total);
+    p.off_rest = off;  if (p.rest) off = align256(off + 4 * sizeof(float) * static_cast<size_t>(s->T));
+    p.off_part = off;
+    if (bf16) {
+        const size_t full = dh_part_bytes(p.lo > 0 ? 2 * p.lo : p.f.Ts < s->T ? p.f.Ts : s->T, s->d, s->V, p.lo > 0 || p.rest);
+        const size_t last = dh_part_bytes(s->T - (p.f.n_slabs - 1) * p.f.Ts, s->d, s->V, p.rest);
+        off += full > last ? full : last;
+    } else {
+        off += kF32PartBytes;
+    }
+    // what several slabs add to a dW that is accumulated into: summed first, so that dW takes one rounding whatever the slabs
+    off = align256(off);
+    p.off_dw_sum = p.f.dw_acc ? p.f.off_dw_acc : off;
+    if (p.f.n_slabs > 1 && !p.f.dw_acc) off = align256(off + sizeof(float) * static_cast<size_t>(s->V) * static_cast<size_t>(s->d));
+    p.total = off;
+    return p;
+}
+
+struct LpGrads {
+    const int64_t* labels;
+    const uint8_t* valid;
+    const float *lse, *entropy, *grad_logp, *grad_entropy;
+};
+
+template <class TI>
+int lp_bwd_core(const cat_shape* s, const LpBwdPlan& plan, const TI* H, const TI* W, const LpGrads& a, TI* dH, void* dW, int accumulate_dW,
+                uint8_t* ws, int sm_count, cudaStream_t st) {
+    constexpr bool BF16 = sizeof(TI) == 2;
+    const FusedPlan& f = plan.f;
+    int* status = reinterpret_cast<int*>(ws);
+    void* dz = ws + f.off_z;
+    TI* Hz = reinterpret_cast<TI*>(ws + f.off_hs);
+    float* part_sum = reinterpret_cast<float*>(ws + f.off_part_m);
+    int* part_col = reinterpret_cast<int*>(ws + f.off_part_l);
+    float* dz_label = reinterpret_cast<float*>(ws + f.off_z_label);
+    int* closing = reinterpret_cast<int*>(ws + f.off_ref);
+    const int d = static_cast<int>(s->d), V = static_cast<int>(s->V);
+    const bool copy_H = a.valid != nullptr || plan.lo > 0;
+    float* dw_sum = accumulate_dW && f.n_slabs > 1 ? reinterpret_cast<float*>(ws + plan.off_dw_sum) : nullptr;
+    CUtensorMap tmW_k;
+    if (BF16 && tmap_b(&tmW_k, W, s->V, s->d, s->ldW) != CAT_OK) return CAT_ERR_CUDA;
+    for (int sl = 0; sl < f.n_slabs; ++sl) {
+        const long long r0 = static_cast<long long>(sl) * f.Ts;
+        const long long rws = (s->T - r0) < f.Ts ? (s->T - r0) : f.Ts;
+        const long long all = plan.lo > 0 ? 2 * plan.lo : rws;             // rows of dz, with its second terms
+        const TI* Hs = H + r0 * s->ldH;
+        const long long* labels = a.labels ? reinterpret_cast<const long long*>(a.labels) + r0 : nullptr;
+        const uint8_t* valid = a.valid ? a.valid + r0 : nullptr;
+        const float *lse = a.lse + r0, *entropy = a.entropy ? a.entropy + r0 : nullptr;
+        const float *gl = a.grad_logp ? a.grad_logp + r0 : nullptr, *ge = a.grad_entropy ? a.grad_entropy + r0 : nullptr;
+        if (copy_H) {
+            lp::copy_rows_kernel<TI><<<static_cast<unsigned>(all), lp::THREADS, 0, st>>>(Hs, s->ldH, d, static_cast<int>(rws), valid,
+                                                                                         static_cast<int>(plan.lo), Hz);
+            if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
+        }
+        lp::LabelRest rest{nullptr, labels, nullptr, s->ldW};
+        tc::SparseTerms<true> sparse{};
+        if (BF16) {
+            const int S = fwd_splits(rws, s->V);
+            CUtensorMap tmH_k, tmDz_out;
+            if (tmap_a(&tmH_k, Hs, rws, s->d, s->ldH) != CAT_OK || tmap_out(&tmDz_out, dz, all, s->V, f.ldz) != CAT_OK) return CAT_ERR_CUDA;
+            tc::EpiDzLp::Params zp;
+            zp.labels = labels; zp.valid = valid; zp.lse = lse; zp.entropy = entropy; zp.grad_logp = gl; zp.grad_entropy = ge;
+            zp.part_sum = part_sum; zp.part_col = part_col; zp.part_stride = s->T; zp.dz_label = dz_label;
+            zp.T = static_cast<int>(rws); zp.V = V; zp.lo_rows = static_cast<int>(plan.lo);
+            const int rc = launch_tc<0, 0, tc::EpiDzLp>(tmH_k, tmW_k, make_sched(rws, s->V, s->d, S, band_tiles(s->d), 0), zp, status, sm_count, st,
+                                                        &tmDz_out);
+            if (rc != CAT_OK) return rc;
+            lp::CloseParams cp;
+            memset(&cp, 0, sizeof(cp));
+            cp.labels = labels; cp.valid = valid; cp.grad_logp = gl; cp.part_sum = part_sum; cp.part_col = part_col; cp.part_stride = s->T; cp.S = S;
+            cp.dz_label = dz_label; cp.dz = static_cast<__nv_bfloat16*>(dz); cp.ldz = f.ldz;
+            cp.T = static_cast<int>(rws); cp.V = V; cp.lo = static_cast<int>(plan.lo);
+            if (plan.rest && gl) {
+                cp.rest = reinterpret_cast<float*>(ws + plan.off_rest);
+                cp.key = reinterpret_cast<int*>(cp.rest + s->T); cp.from = cp.key + s->T; cp.coef = cp.rest + 3 * s->T;
+                rest.rest = cp.rest; rest.W = reinterpret_cast<const __nv_bfloat16*>(W);
+                sparse.key = cp.key; sparse.from = cp.from; sparse.coef = cp.coef;
+                sparse.src = reinterpret_cast<const __nv_bfloat16*>(Hs); sparse.ld_src = s->ldH; sparse.n = static_cast<int>(rws);
+            }
+            lp::close_kernel<<<static_cast<unsigned>(cdiv(rws, lp::WARPS)), lp::THREADS, 0, st>>>(cp);
+        } else {
+            f32::Operands op;
+            f32::EpiParams ep;
+            memset(&ep, 0, sizeof(ep));
+            op.A = reinterpret_cast<const float*>(Hs); op.sAm = s->ldH; op.sAk = 1;
+            op.B = reinterpret_cast<const float*>(W); op.sBk = 1; op.sBn = s->ldW;
+            op.M = static_cast<int>(rws); op.N = V; op.Kd = d;
+            op.n_groups = static_cast<int>(cdiv(V, f32::TN));
+            ep.labels = labels; ep.valid = valid; ep.lse = lse; ep.entropy = entropy; ep.grad_logp = gl; ep.grad_entropy = ge;
+            ep.closing = closing; ep.dz = static_cast<float*>(dz); ep.ld_dz = f.ldz; ep.V = V;
+            if (cudaMemsetAsync(closing, 0xFF, sizeof(int) * rws, st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
+            f32::gemm_kernel<f32::DZ, true, true><<<dim3(static_cast<unsigned>(cdiv(rws, f32::TM)), static_cast<unsigned>(op.n_groups)), f32::THREADS, 0, st>>>(op, ep);
+            f32::close_kernel<<<static_cast<unsigned>(rws), 256, 0, st>>>(static_cast<float*>(dz), f.ldz, V, closing);
+        }
+        if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
+        const int rc = slab_grads(s, f, W, copy_H ? Hz : Hs, copy_H ? s->d : s->ldH, dz, ws, r0, rws, plan.lo, sl == 0, sl == f.n_slabs - 1, nullptr,
+                                  reinterpret_cast<float*>(ws + plan.off_part), dH, dW, accumulate_dW, sm_count, st, rest.rest ? &rest : nullptr,
+                                  sparse.key ? &sparse : nullptr, dw_sum);
+        if (rc != CAT_OK) return rc;
+    }
+    if (dw_sum) {
+        const bool four = s->d % 4 == 0 && s->ldW % 4 == 0;
+        const long long ctas = cdiv(s->V * (four ? s->d / 4 : s->d), lp::THREADS * 4);
+        const unsigned grid = static_cast<unsigned>(ctas < 65535 ? ctas : 65535);
+        if (s->dW_dtype == CAT_BF16) lp::add_sum_kernel<4><<<grid, lp::THREADS, 0, st>>>(dw_sum, s->V, d, static_cast<__nv_bfloat16*>(dW), s->ldW);
+        else if (four) lp::add_sum_kernel<4><<<grid, lp::THREADS, 0, st>>>(dw_sum, s->V, d, static_cast<float*>(dW), s->ldW);
+        else lp::add_sum_kernel<1><<<grid, lp::THREADS, 0, st>>>(dw_sum, s->V, d, static_cast<float*>(dW), s->ldW);
+        if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
+    }
+    return CAT_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -712,10 +697,10 @@ int cat_logprob_bwd(const cat_shape* shape, const void* H, const void* W, const 
     if (cudaMemsetAsync(ws, 0, kHeaderBytes, st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
     LpGrads a;
     a.labels = labels; a.valid = valid; a.lse = lse; a.entropy = entropy; a.grad_logp = grad_logp; a.grad_entropy = grad_entropy;
-    return bf16 ? lp_bwd_bf16(&one, plan, static_cast<const __nv_bfloat16*>(H), static_cast<const __nv_bfloat16*>(W), a,
-                              static_cast<__nv_bfloat16*>(dH), dW, accumulate_dW, ws, sm_count, st)
-                : lp_bwd_f32(&one, plan, static_cast<const float*>(H), static_cast<const float*>(W), a, static_cast<float*>(dH),
-                             static_cast<float*>(dW), accumulate_dW, ws, st);
+    return bf16 ? lp_bwd_core<__nv_bfloat16>(&one, plan, static_cast<const __nv_bfloat16*>(H), static_cast<const __nv_bfloat16*>(W), a,
+                                             static_cast<__nv_bfloat16*>(dH), dW, accumulate_dW, ws, sm_count, st)
+                : lp_bwd_core<float>(&one, plan, static_cast<const float*>(H), static_cast<const float*>(W), a, static_cast<float*>(dH), dW,
+                                     accumulate_dW, ws, sm_count, st);
 }
 
 size_t cat_topk_kd_workspace_bytes(const cat_shape* shape, const cat_topk_kd_desc* desc) {

@@ -9,10 +9,10 @@
 // columns; row_kernel then finds the top k among the few columns that can be in it (see there).
 // Bound by the tensor cores for many rows and by reading W for few.
 //
-// Backward: the logits are recomputed per vocabulary slab and leave the GEMM as
+// Backward: the logits are recomputed per row slab and leave the GEMM as
 //   dz[v] = gl ([v = y] - p) - ge p (log p + entropy)
-// for upstream gradients gl (of logp) and ge (of the entropy), the label's entry from its exact logit (bwd_rows_kernel); the dH and dW
-// contractions follow.
+// for upstream gradients gl (of logp) and ge (of the entropy); close_kernel writes the entry of a token that has most of the row's probability, and
+// the dH and dW contractions follow.
 #pragma once
 #include "rowops.cuh"
 #include "tc_gemm.cuh"
@@ -156,7 +156,13 @@ struct EpiLp {
 template <>
 struct LetsNextStart<EpiLp<true>> { static constexpr bool value = true; };
 
-// Backward: dz of the current vocabulary slab, rounded to bf16 once (the operand type of the two contractions).
+// Backward: dz of the row slab, rounded to bf16 once (the operand type of the two contractions).
+//
+// The row's closing entry.  In a row that is sure of a token, that token's entry gl (1 - p) - ge p (log p + entropy) is small against its terms,
+// and the rounding of lse alone, 1e-6 of p, would be a tenth of it at 1 - p = 1e-5.  A row of dz sums to zero, so that entry is the others' sum with
+// the sign turned, as exact as they are.  It is left out here (at most one token has p above CLOSING), the others are summed per vocabulary
+// split, and close_kernel writes it.
+constexpr float CLOSING = -0.75f;        // log2 p
 struct EpiDzLp {
     struct Params {
         const long long* labels;       // [T]; nullptr without grad_logp
@@ -165,34 +171,38 @@ struct EpiDzLp {
         const float* entropy;          // [T]; nullptr without grad_entropy
         const float* grad_logp;        // [T] or nullptr
         const float* grad_entropy;     // [T] or nullptr
-        const float* dz_label;         // [T] the label's entry, with grad_logp (see bwd_rows_kernel)
+        float* part_sum;               // [n_groups][part_stride] sum of the entries but the closing one
+        int* part_col;                 // the closing entry's column, or -1
+        long long part_stride;
+        float* dz_label;               // [T] the label's entry before its rounding, unless it is the closing one
         int T;
         int V;
-        int v0;
         int lo_rows;                   // > 0: also what the rounding leaves, as row lo_rows + r (a multiple of 32, >= T)
     };
     struct State {
         float l2;                      // lse * log2 e
-        float ca, cb;                  // dz = p (ca + cb log2 p), the label's entry apart
-        float dz_y;
-        int y_rel;
+        float ca, cb;                  // dz = p (ca + cb log2 p), and gl more at the label
+        float gl;
+        float sum;
+        int col;
+        int y;
         bool on;                       // the row takes part; one that does not gets zeros whatever its logits are
         int row;
     };
     __device__ static __forceinline__ void begin_item(const Params& p, State& s, int m_tile, int row_in_tile) {
         s.row = m_tile * BM + row_in_tile;
         s.l2 = 0.f;
-        s.ca = s.cb = s.dz_y = 0.f;
-        s.y_rel = -1;
+        s.ca = s.cb = s.gl = s.sum = 0.f;
+        s.y = s.col = -1;
         s.on = s.row < p.T && (p.valid == nullptr || p.valid[s.row] != 0);
         if (s.on) {
             s.l2 = p.lse[s.row] * LOG2E;
             if (p.grad_logp) {
                 const long long y = p.labels[s.row];
                 if (y >= 0 && y < p.V) {
-                    s.y_rel = static_cast<int>(y) - p.v0;
-                    s.dz_y = p.dz_label[s.row];
-                    s.ca = -p.grad_logp[s.row];
+                    s.y = static_cast<int>(y);
+                    s.gl = p.grad_logp[s.row];
+                    s.ca = -s.gl;
                 }
             }
             if (p.grad_entropy) {
@@ -204,7 +214,7 @@ struct EpiDzLp {
     }
     __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage& o) {
         const int col0 = n_tile * BN;
-        const int ncols = min(BN, p.V - p.v0 - col0);
+        const int ncols = min(BN, p.V - col0);
         walk_tile(taddr, ncols, [&](int c, uint32_t (&v)[32]) {
             if ((c & 1) == 0) {
                 if (p.lo_rows == 0) o.begin();
@@ -214,25 +224,46 @@ struct EpiDzLp {
             const int live = ncols - c * 32;
             const uint64_t l2e2 = ptx::pack_f32x2(LOG2E, LOG2E), nl2 = ptx::pack_f32x2(-s.l2, -s.l2);
             const uint64_t ca2 = ptx::pack_f32x2(s.ca, s.ca), cb2 = ptx::pack_f32x2(s.cb, s.cb);
+            float xmax = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const uint64_t x2 = ptx::fma_f32x2(ptx::pack_f32x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), l2e2, nl2);
                 float x0, x1;
                 ptx::unpack_f32x2(x2, x0, x1);
+                xmax = ptx::max3_f32(xmax, x0, x1);
                 const uint64_t p2 = ptx::pack_f32x2(ptx::ex2_approx(x0), ptx::ex2_approx(x1));
                 ptx::unpack_f32x2(ptx::mul_f32x2(p2, ptx::fma_f32x2(cb2, x2, ca2)), f[2 * i], f[2 * i + 1]);
-            }
-            const int rel = s.y_rel - (col0 + c * 32);
-            if (rel >= 0 && rel < 32) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (i == rel) f[i] = s.dz_y;
             }
             if (live < 32 || !s.on) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
                     if (i >= live || !s.on) f[i] = 0.f;
             }
+            const int rel = s.y - (col0 + c * 32);
+            if (rel >= 0 && rel < 32) {
+                float at = 0.f;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (i == rel) at = f[i] += s.gl;
+                p.dz_label[s.row] = at;
+            }
+            if (xmax > CLOSING && s.on) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (i < live && fmaf(__uint_as_float(v[i]), LOG2E, -s.l2) > CLOSING && s.col < 0) {
+                        s.col = col0 + c * 32 + i;
+                        f[i] = 0.f;
+                    }
+            }
+            uint64_t sum2 = ptx::pack_f32x2(f[0], f[1]), sum2b = ptx::pack_f32x2(f[2], f[3]);
+#pragma unroll
+            for (int i = 4; i < 32; i += 4) {
+                sum2 = ptx::add_f32x2(sum2, ptx::pack_f32x2(f[i], f[i + 1]));
+                sum2b = ptx::add_f32x2(sum2b, ptx::pack_f32x2(f[i + 2], f[i + 3]));
+            }
+            float s0, s1;
+            ptx::unpack_f32x2(ptx::add_f32x2(sum2, sum2b), s0, s1);
+            s.sum += s0 + s1;
             const bool closes = (c & 1) != 0 || (c + 1) * 32 >= ncols;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -255,7 +286,13 @@ struct EpiDzLp {
         });
     }
     __device__ static __forceinline__ int out_rows(const Params& p) { return p.lo_rows > 0 ? p.lo_rows : p.T; }
-    __device__ static __forceinline__ void end_item(const Params&, const State&, int) {}
+    __device__ static __forceinline__ void end_item(const Params& p, const State& s, int group) {
+        if (s.row < p.T) {
+            const size_t at = static_cast<size_t>(group) * p.part_stride + s.row;
+            p.part_sum[at] = s.sum;
+            p.part_col[at] = s.col;
+        }
+    }
 };
 
 }  // namespace tc
@@ -1020,64 +1057,94 @@ __device__ __forceinline__ void copy_row(const TI* src, TI* dst, int d, bool on)
         for (int i = threadIdx.x; i < d; i += THREADS) dst[i] = on ? src[i] : static_cast<TI>(0);
     }
 }
+// One CTA per row of the copy.  lo > 0, for dz in two terms: rows T .. lo - 1 are zero and rows lo .. 2 lo - 1 a second copy.
 template <class TI>
-struct BwdRows {
-    const TI* H;
-    const TI* W;
-    long long ldH, ldW;
-    int d, T, V;
-    const unsigned char* valid;        // [T] or nullptr
+__global__ void __launch_bounds__(THREADS) copy_rows_kernel(const TI* H, long long ldH, int d, int T, const unsigned char* valid, int lo, TI* out) {
+    const long long at = blockIdx.x, r = lo > 0 && at >= lo ? at - lo : at;
+    const bool on = r < T && (valid == nullptr || valid[r] != 0);
+    copy_row(H + (r < T ? r : 0) * ldH, out + at * d, d, on);
+}
+
+// out += sum, sum [V][d] and out with pitch ld, N elements at a time (4: aligned so).
+__device__ __forceinline__ void add_to(float* to, const float* x) { *to += *x; }
+__device__ __forceinline__ void add_to4(float* to, const float* x) {
+    float4 a = *reinterpret_cast<float4*>(to);
+    const float4 b = __ldcs(reinterpret_cast<const float4*>(x));
+    a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+    *reinterpret_cast<float4*>(to) = a;
+}
+__device__ __forceinline__ void add_to4(__nv_bfloat16* to, const float* x) {
+    uint2 a = *reinterpret_cast<uint2*>(to);
+    const float4 b = __ldcs(reinterpret_cast<const float4*>(x));
+    a.x = ptx::pack_bf16x2(__uint_as_float(a.x << 16) + b.x, __uint_as_float(a.x & 0xffff0000u) + b.y);
+    a.y = ptx::pack_bf16x2(__uint_as_float(a.y << 16) + b.z, __uint_as_float(a.y & 0xffff0000u) + b.w);
+    *reinterpret_cast<uint2*>(to) = a;
+}
+template <int N, class T>
+__global__ void __launch_bounds__(THREADS) add_sum_kernel(const float* sum, long long V, int d, T* out, long long ld) {
+    const long long cols = d / N;
+    for (long long i = static_cast<long long>(blockIdx.x) * THREADS + threadIdx.x; i < V * cols; i += static_cast<long long>(gridDim.x) * THREADS) {
+        const long long v = i / cols, c = i - v * cols;
+        if constexpr (N == 4) add_to4(out + v * ld + 4 * c, sum + 4 * i);
+        else add_to(out + v * ld + c, sum + i);
+    }
+}
+
+// The closing entries of a slab of dz (see tc::EpiDzLp), one warp per row; and, with `rest`, what the rounding leaves of the labels' entries, as
+// LabelRest and sorted by label and row for tc::SparseTerms (rows without a label: 0, and INT_MAX at the end).
+struct CloseParams {
     const long long* labels;           // [T], with grad_logp
-    const float* lse;
-    const float* entropy;
+    const unsigned char* valid;        // [T] or nullptr
     const float* grad_logp;            // [T] or nullptr
-    const float* grad_entropy;         // [T] or nullptr
-    float* dz_label;                   // [T]
-    TI* out;                           // the copy, or nullptr
+    const float* part_sum;             // [S][part_stride]
+    const int* part_col;
+    long long part_stride;
+    int S;
+    const float* dz_label;             // [T]
+    __nv_bfloat16* dz;
+    long long ldz;
+    int T, V;
     int lo;
-    // LabelRest, and the same sorted by label and row: [T] each, or nullptr (rows without a label: 0, and INT_MAX at the end)
-    float* rest;
+    float* rest;                       // [T] each, or nullptr; only with grad_logp
     int* key;
     int* from;
     float* coef;
 };
-// First pass of the gradients, one CTA per row of the copy: the copy (lo > 0: rows T .. lo - 1 are zero and rows lo .. 2 lo - 1 a second one,
-// for dz in two terms), and the label's entry of dz from its exact logit,
-//   dz[y] = -gl (e^x - 1) - ge e^x (x + entropy),  x = z[y] - lse.
-// In a row that is sure of its label this is small against e^x, and the error of the GEMM's logit (3e-6 of it) would stand against
-// 1 - p: of the gradient of a token of p = 0.9999, half.
-template <class TI>
-__global__ void __launch_bounds__(THREADS) bwd_rows_kernel(const BwdRows<TI> p) {
-    const long long at = blockIdx.x, r = p.lo > 0 && at >= p.lo ? at - p.lo : at;
-    const bool on = r < p.T && (p.valid == nullptr || p.valid[r] != 0);
-    const TI* h = p.H + (r < p.T ? r : 0) * p.ldH;
-    if (p.out != nullptr) copy_row(h, p.out + at * p.d, p.d, on);
-    if (p.grad_logp == nullptr || at >= p.T) return;
-    auto label = [&](long long q) {
+__global__ void __launch_bounds__(THREADS) close_kernel(const CloseParams p) {
+    const int r = blockIdx.x * WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (r >= p.T) return;
+    float sum = 0.f;
+    int col = -1;
+    for (int s = lane; s < p.S; s += 32) {
+        sum += p.part_sum[s * p.part_stride + r];
+        col = max(col, p.part_col[s * p.part_stride + r]);
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    col = __reduce_max_sync(0xffffffffu, col);
+    if (static_cast<unsigned>(col) >= static_cast<unsigned>(p.V)) col = -1;      // a GEMM that timed out leaves anything here
+    const float entry = 0.f - sum;
+    if (col >= 0 && lane == 0) {
+        const __nv_bfloat16 hi = __float2bfloat16_rn(entry);
+        p.dz[r * p.ldz + col] = hi;
+        if (p.lo > 0) p.dz[(p.lo + r) * p.ldz + col] = __float2bfloat16_rn(entry - __bfloat162float(hi));
+    }
+    if (p.rest == nullptr) return;
+    auto label = [&](int q) {
         const long long y = p.labels[q];
         return (p.valid == nullptr || p.valid[q] != 0) && y >= 0 && y < p.V ? static_cast<int>(y) : INT_MAX;
     };
     const int y = label(r);
     int rank = 0;
-    if (p.rest != nullptr) {
-        for (int q0 = 0; q0 < p.T; q0 += THREADS) {
-            const int q = q0 + threadIdx.x, k = q < p.T ? label(q) : INT_MAX;
-            rank += __syncthreads_count(q < p.T && (k < y || (k == y && q < r)));
-        }
-        if (threadIdx.x == 0) {
-            p.key[rank] = y;
-            p.from[rank] = static_cast<int>(r);
-            if (y == INT_MAX) p.rest[r] = p.coef[rank] = 0.f;
-        }
+    for (int q0 = 0; q0 < p.T; q0 += 32) {
+        const int q = q0 + lane, k = q < p.T ? label(q) : INT_MAX;
+        rank += __popc(__ballot_sync(0xffffffffu, q < p.T && (k < y || (k == y && q < r))));
     }
-    if (threadIdx.x >= 32 || y == INT_MAX) return;
-    const double z = warp_dot(h, p.W + static_cast<long long>(y) * p.ldW, p.d, static_cast<int>(threadIdx.x));
-    if (threadIdx.x != 0) return;
-    const float x = static_cast<float>(z - static_cast<double>(p.lse[r]));
-    float v = -p.grad_logp[r] * expm1f(x);
-    if (p.grad_entropy != nullptr) v = fmaf(-p.grad_entropy[r] * expf(x), x + p.entropy[r], v);
-    p.dz_label[r] = v;
-    if (p.rest != nullptr) p.rest[r] = p.coef[rank] = v - __bfloat162float(__float2bfloat16_rn(v));
+    if (lane != 0) return;
+    const float v = y == INT_MAX ? 0.f : y == col ? entry : p.dz_label[r];
+    p.key[rank] = y;
+    p.from[rank] = r;
+    p.rest[r] = p.coef[rank] = v - __bfloat162float(__float2bfloat16_rn(v));
 }
 
 }  // namespace lp
