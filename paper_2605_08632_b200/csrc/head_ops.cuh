@@ -599,7 +599,7 @@ int lp_bwd_core(const cat_shape* s, const LpBwdPlan& plan, const TI* H, const TI
             op.A = reinterpret_cast<const float*>(Hs); op.sAm = s->ldH; op.sAk = 1;
             op.B = reinterpret_cast<const float*>(W); op.sBk = 1; op.sBn = s->ldW;
             op.M = static_cast<int>(rws); op.N = V; op.Kd = d;
-            op.n_groups = static_cast<int>(cdiv(V, f32::TN));
+            op.n_groups = static_cast<int>(cdiv(V, f32::TN) < 65535 ? cdiv(V, f32::TN) : 65535);       // a grid's second extent ends there
             ep.labels = labels; ep.valid = valid; ep.lse = lse; ep.entropy = entropy; ep.grad_logp = gl; ep.grad_entropy = ge;
             ep.closing = closing; ep.dz = static_cast<float*>(dz); ep.ld_dz = f.ldz; ep.V = V;
             if (cudaMemsetAsync(closing, 0xFF, sizeof(int) * rws, st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
