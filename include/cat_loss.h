@@ -457,8 +457,6 @@ size_t cat_logprob_workspace_bytes(const cat_shape* shape, int top_k, int pass);
  * weights: conf_ext, or the draft's own (for the teacher's: exp(logp) of cat_logprob_fwd through cat_conf_window).
  * Works in row slabs of whole draft blocks with the slab's logits kept (16 bits, relative to the largest logit among
  * the list's ids and the label; fp32 for CAT_F32), at most about slab_mib MiB (default 3 GiB), turned into dz in place.
- * bf16: a logit that lies more than 80 nats above every one that the row's list and label name enters dz as if 80 above
- * (the row's loss, lse and confidence are not affected).
  */
 typedef struct {
     int64_t L;            /* positions the lists cover                                          */

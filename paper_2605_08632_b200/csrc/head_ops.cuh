@@ -484,7 +484,7 @@ int tk_core(const cat_shape* s, const cat_topk_kd_desc* desc, const TkPlan& plan
             rows::block_scan_kernel<<<n_ctas, rows::ROW_THREADS, 0, st>>>(rp);
         }
         cta0 += n_ctas;
-        tk::dz_kernel<!BF16><<<grid_rows, tk::THREADS, 0, st>>>(zs, f.ldz, y, ok, lists, r0, static_cast<int>(rws), static_cast<int>(lo), lse,
+        tk::dz_kernel<!BF16><<<grid_rows, tk::THREADS, 0, st>>>(Hs, s->ldH, W, s->ldW, d, m1, zs, f.ldz, y, ok, lists, r0, static_cast<int>(rws), static_cast<int>(lo), lse,
                                                                 weight, zt, plan.ld_zt, ref, desc->beta, kd_row, V);
         if (cudaGetLastError() != cudaSuccess) return CAT_ERR_CUDA;
         const int rc = slab_grads(s, f, W, Hz, s->d, zs, ws, r0, rws, lo, sl == 0, sl == f.n_slabs - 1, scale, reinterpret_cast<float*>(ws + plan.off_part), dH, dW, accumulate_dW,

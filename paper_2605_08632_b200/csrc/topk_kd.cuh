@@ -13,13 +13,14 @@
 // takes all that the L2 can feed it, slowed down by three quarters of what the overlap saved.
 #pragma once
 #include "logprob.cuh"
+#include <type_traits>
 
 namespace cat {
 namespace tc {
 
 // Softmax statistics (as EpiFwdT), the label's logit, and z - ref in 16 bits: a whole number of steps of 2^-9 nats from -48, up to
 // +80.  ref is the largest of the logits that the list and the label name, so softmax is below e^-48 times a named token's where it is
-// cut off below, and above only logits that exceed every named one by 80 nats are cut.  The steps put a relative error of at most 2^-10
+// cut off below, and above only logits that exceed every named one by 80 nats are cut, which dz_kernel takes again.  The steps put a relative error of at most 2^-10
 // on softmax, 5.6e-4 rms, wherever it lies; fp16 would put 2^-12 |z - ref| there, 2.3e-3 rms in the bulk 8 to 16 nats below the top,
 // which is more than the rounding of dz.
 constexpr float STEPS = 512.f;           // per nat
@@ -358,9 +359,12 @@ __device__ __forceinline__ float block_sum(float x, float* red) {
 // One CTA per row of the slab: the row's KD value, and the stored logits turned into dz in place.  Dense part
 // weight (beta + sum p) q from the stored z - ref; the entries at the label and at the list's ids from their fp32
 // logits, an id that stands in the list twice with the sum of its probabilities.
-// fp32 slabs (fp32 inputs) hold z itself and leave as fp32 dz.
+// fp32 slabs (fp32 inputs) hold z itself and leave as fp32 dz.  In a row whose largest logit, m1, lies past the slab's range above all that the list
+// and the label name, the logits that were cut off there are summed again.
 template <bool F32>
-__global__ void __launch_bounds__(THREADS) dz_kernel(void* zs, long long ldz, const long long* labels, const unsigned char* valid_eff,
+__global__ void __launch_bounds__(THREADS) dz_kernel(const std::conditional_t<F32, float, __nv_bfloat16>* H, long long ldH,
+                                                     const std::conditional_t<F32, float, __nv_bfloat16>* W, long long ldW, int d, const float* m1,
+                                                     void* zs, long long ldz, const long long* labels, const unsigned char* valid_eff,
                                                      Lists lists, long long row0, int rows, int lo, const float* lse, const float* weight,
                                                      const float* zt, int ld_zt, const float* ref, float beta, float* kd_row,
                                                      int V) {
@@ -409,7 +413,45 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(void* zs, long long ldz, co
     const float off = F32 ? 0.f : (ref[r] + (tc::LOW_END + 64.f) - lse_r) * LOG2E;
     if (F32)
         for (int v = threadIdx.x; v < V; v += THREADS) row32[v] = wm * expf(row32[v] - lse_r);
-    else {
+    else if (m1[r] - ref[r] > tc::LOW_END + tc::TOP_STEP / tc::STEPS - 0.1f) {
+        if constexpr (!F32) {
+            const int lane = threadIdx.x & 31;
+            const __nv_bfloat16* h = H + static_cast<long long>(blockIdx.x) * ldH;
+            for (int g0 = threadIdx.x - lane; g0 < groups; g0 += THREADS) {      // whole warps
+                const int g = g0 + lane;
+                const uint4 in = g < groups ? row[g] : make_uint4(0u, 0u, 0u, 0u);
+                const uint32_t zw[4] = {in.x, in.y, in.z, in.w};
+                float x[8];
+                unsigned cut = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t n = j & 1 ? zw[j >> 1] >> 16 : zw[j >> 1] & 0xffffu;
+                    x[j] = g * 8 + j < V ? wm * ptx::ex2_approx(fmaf(__uint_as_float(n | 0x4b000000u) - 8421376.f, LOG2E / tc::STEPS, off)) : 0.f;
+                    cut |= n == 0xffffu && g * 8 + j < V ? 1u << j : 0u;
+                }
+                for (unsigned lanes = __ballot_sync(0xffffffffu, cut != 0); lanes != 0; lanes &= lanes - 1) {
+                    const int src = __ffs(lanes) - 1;
+                    for (unsigned at = __shfl_sync(0xffffffffu, cut, src); at != 0; at &= at - 1) {
+                        const int j = __ffs(at) - 1;
+                        const float z = lp::warp_dot_f32(h, W + (static_cast<long long>(g0 + src) * 8 + j) * ldW, d, lane);
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            if (lane == src && q == j) x[q] = wm * expf(z - lse_r);
+                    }
+                }
+                if (g < groups) {
+                    uint32_t o[4], left[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        o[j] = ptx::pack_bf16x2(x[2 * j], x[2 * j + 1]);
+                        left[j] = ptx::pack_bf16x2(x[2 * j] - __uint_as_float(o[j] << 16), x[2 * j + 1] - __uint_as_float(o[j] & 0xffff0000u));
+                    }
+                    row[g] = make_uint4(o[0], o[1], o[2], o[3]);
+                    if (lo > 0) rest[g] = make_uint4(left[0], left[1], left[2], left[3]);
+                }
+            }
+        }
+    } else {
         // four loads in flight a thread: slabs of few rows fill the SMs with too few warps to cover the memory's latency with one
         constexpr int AHEAD = 4;
         for (int g0 = threadIdx.x; g0 < groups; g0 += AHEAD * THREADS) {
