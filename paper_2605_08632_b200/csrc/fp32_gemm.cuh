@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(THREADS, 4) gemm_kernel(const Operands op, con
         auto add_squares = [&] {
             if (squares) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sq[i] = fmaf(bv[i], bv[i], sq[i]);
+                for (int i = 0; i < 8; ++i) sq[i] = fmaf(bv[i], bv[i], sq[i]) + (bv[i] != 0.f ? 0x1p-126f : 0.f);      // 0 for zeros alone
             }
         };
         fetch<A_KC>(op.A, op.sAm, op.sAk, m0, op.M, ks0 * TK, op.Kd, av);

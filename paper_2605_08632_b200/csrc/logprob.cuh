@@ -409,6 +409,10 @@ __device__ __forceinline__ float add_squares(float acc, uint32_t two) {
 __device__ __forceinline__ float add_squares(float acc, const uint4& x) {
     return add_squares(add_squares(add_squares(add_squares(acc, x.x), x.y), x.z), x.w);
 }
+// whether one of eight bf16 numbers is not zero
+__device__ __forceinline__ bool any_of(const uint4& x) { return ((x.x | x.y | x.z | x.w) & 0x7fff7fffu) != 0; }
+// The least sum of squares of a vector that is not zero, whatever its squares lose below the range: a sum of 0 means a vector of zeros.
+constexpr float NOT_ZERO = 0x1p-126f;
 // sum of the squares of a row, by one warp
 __device__ __forceinline__ float warp_squares(const __nv_bfloat16* row, int d, int lane) {
     const uint4* v = reinterpret_cast<const uint4*>(row);
@@ -427,12 +431,17 @@ __device__ __forceinline__ float warp_squares(const __nv_bfloat16* row, int d, i
     for (; i < n; i += 32) sum = add_squares(sum, __ldg(v + i));
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    if (sum == 0.f) {
+        bool any = false;
+        for (i = lane; i < n; i += 32) any |= any_of(__ldg(v + i));
+        if (__any_sync(0xffffffffu, any)) sum = NOT_ZERO;
+    }
     return sum;
 }
 __device__ __forceinline__ float warp_squares(const float* row, int d, int lane) {
     float sum = 0.f;
 #pragma unroll 4
-    for (int i = lane; i < d; i += 32) { const float x = __ldg(row + i); sum = fmaf(x, x, sum); }
+    for (int i = lane; i < d; i += 32) { const float x = __ldg(row + i); sum = fmaf(x, x, sum) + (x != 0.f ? NOT_ZERO : 0.f); }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
     return sum;
@@ -959,10 +968,8 @@ __global__ void __launch_bounds__(RT, 1024 / RT) row_kernel(const RowParams<TI, 
         kept = settle_close(p, h, r, sh, sh.n_cand, eps, dot_error(p.d) * size);
     } else {
         if (warp < 2) exact_one(p, h, r, sh, warp);
-        // many logits within the error of the k-th.  A row of zeros has them all equal: ids 0, 1, ...
-        bool nz = false;
-        for (int i = threadIdx.x; i < p.d; i += RT) nz |= static_cast<float>(h[i]) != 0.f;
-        if (!__syncthreads_or(nz ? 1 : 0)) {
+        // many logits within the error of the k-th.  A row of zeros, or a head of zeros, has them all equal: ids 0, 1, ...
+        if (sh.h_sq == 0.f || *p.w_sq == 0) {
             kept = p.k < p.V ? p.k : p.V;
             for (int i = threadIdx.x; i < kept; i += RT) { sh.z_keep[i] = 0.0; sh.id_keep[i] = i; }
             __syncthreads();

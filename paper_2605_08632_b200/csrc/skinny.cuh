@@ -186,7 +186,14 @@ logits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
                     float a[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int c = 0; c < 8; ++c) a[c & 3] = lp::add_squares(a[c & 3], x[c]);
-                    sq[j] += (a[0] + a[1]) + (a[2] + a[3]);
+                    const float sum = (a[0] + a[1]) + (a[2] + a[3]);
+                    sq[j] += sum;
+                    if (sum == 0.f) {
+                        bool any = false;
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) any |= lp::any_of(x[c]);
+                        if (any) sq[j] += lp::NOT_ZERO;
+                    }
                 }
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl.empty[stage]));
