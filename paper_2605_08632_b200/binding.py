@@ -137,9 +137,14 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+# torch's own short way to the handle; not part of its documented interface
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream():
     """Handle of the current device's current stream (torch.cuda.current_stream() builds a Stream object for it: 3 us)."""
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    dev = torch.cuda.current_device()
+    return torch.cuda.current_stream(dev).cuda_stream if _raw_stream is None else _raw_stream(dev)
 
 
 def cat_loss_fwd(shape, H, W, labels, valid, conf_ext, loss, lse, conf, weight, stats, workspace) -> None:

@@ -1,5 +1,8 @@
 """Sizes and rules behind what the LM-head operators' engines keep, without a GPU."""
+import types
+
 import pytest
+import torch
 
 from paper_2605_08632_b200 import binding as B
 
@@ -15,3 +18,12 @@ def test_the_longest_lists_workspace_serves_every_length(T, d, V, K, code, slab)
             assert B.cat_topk_kd_workspace_bytes(s, B.make_topk_kd_desc(L, k, 0.1)) <= most
     least = B.cat_topk_kd_workspace_bytes(s, B.make_topk_kd_desc(T, 1, 0.1))
     assert most - least <= (T + 255) // 256 * 256 * 4 * B.CAT_TOPK_MAX + 256       # a slab is whole tiles of 256 rows
+
+
+def test_stream_handle_without_the_undocumented_way(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev: types.SimpleNamespace(cuda_stream=1000 + dev))
+    monkeypatch.setattr(B, "_raw_stream", None)
+    assert B._stream() == 1003
+    monkeypatch.setattr(B, "_raw_stream", lambda dev: 2000 + dev)
+    assert B._stream() == 2003
