@@ -454,7 +454,8 @@ size_t cat_logprob_workspace_bytes(const cat_shape* shape, int top_k, int pass);
  * entries has KD_r = 0.  Gradients, with the weights constant and none to the lists:
  *     dz[r, v] = g * weight[r]/N * ((beta + sum_i p_i) q_r[v] - beta [v == y_r] - sum_i p_i [v == id_i]).
  * A row takes part iff valid[r] != 0, 0 <= y_r < V and 0 <= t < L; H of the others may hold anything.  Confidences for the
- * weights: conf_ext, or the draft's own (for the teacher's: exp(logp) of cat_logprob_fwd through cat_conf_window).
+ * weights: conf_ext, or the draft's own (for the teacher's: exp(logp) of cat_logprob_fwd through cat_conf_window).  A row of dz sums to
+ * zero, and the entry of a named token that has nearly all of the row's probability is taken from that.
  * Works in row slabs of whole draft blocks with the slab's logits kept (16 bits, relative to the largest logit among
  * the list's ids and the label; fp32 for CAT_F32), at most about slab_mib MiB (default 3 GiB), turned into dz in place.
  */

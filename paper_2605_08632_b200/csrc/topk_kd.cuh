@@ -361,6 +361,10 @@ __device__ __forceinline__ float block_sum(float x, float* red) {
 // logits, an id that stands in the list twice with the sum of its probabilities.
 // fp32 slabs (fp32 inputs) hold z itself and leave as fp32 dz.  In a row whose largest logit, m1, lies past the slab's range above all that the list
 // and the label name, the logits that were cut off there are summed again.
+//
+// The closing entry.  Where a named token has nearly all of the row's probability, its entry (beta + mass) q - sub is small against its terms, and
+// the rounding of lse, 1e-6 of q, stands against 1 - q.  A row of dz sums to zero (sum q = 1), so that entry is taken as the others' sum with
+// the sign turned, off by the same share as they are: 2^-10 at most for bf16, which is less than the rounding of lse from 1 - q = 2^-10 down.
 template <bool F32>
 __global__ void __launch_bounds__(THREADS) dz_kernel(const std::conditional_t<F32, float, __nv_bfloat16>* H, long long ldH,
                                                      const std::conditional_t<F32, float, __nv_bfloat16>* W, long long ldW, int d, const float* m1,
@@ -371,6 +375,8 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(const std::conditional_t<F3
     __shared__ float s_red[WARPS];
     __shared__ float s_p[MAX_TOP];
     __shared__ int s_id[MAX_TOP];
+    __shared__ int s_close;
+    constexpr float CLOSING = F32 ? -0.5f : -0.0009765625f;        // log q
     const long long r = row0 + blockIdx.x;
     uint4* row = reinterpret_cast<uint4*>(static_cast<unsigned short*>(zs) + static_cast<size_t>(blockIdx.x) * ldz);
     float* row32 = static_cast<float*>(zs) + static_cast<size_t>(blockIdx.x) * ldz;
@@ -395,6 +401,19 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(const std::conditional_t<F3
     float lp = -INFINITY, z_i = 0.f;
     const bool there = i < lists.k && lists.entry(t, i, id, lp);
     if (there) z_i = zr[i];
+    if (i == 0) s_close = -1;
+    __syncthreads();
+    if (there && z_i - lse_r > CLOSING) s_close = static_cast<int>(id);
+    if (i == 0 && zr[lists.k] - lse_r > CLOSING) s_close = y;
+    __syncthreads();
+    const int close = s_close;
+    // what the slab holds at the named tokens, for their part of the dense sum
+    float held = 0.f, held_y = 0.f;
+    if (close >= 0) {
+        auto at = [&](long long v) { return F32 ? row32[v] : static_cast<float>(reinterpret_cast<const unsigned short*>(row)[v]); };
+        if (there) held = at(id);
+        if (i == 0) held_y = at(y);
+    }
     if (lists.renorm) {
         const float m = block_max(there ? lp : -INFINITY, s_red);
         const float l = block_sum(there ? expf(lp - m) : 0.f, s_red);
@@ -411,8 +430,15 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(const std::conditional_t<F3
     if (i == 0) kd_row[r] = w * kd;
     const float wm = w * (beta + mass);
     const float off = F32 ? 0.f : (ref[r] + (tc::LOW_END + 64.f) - lse_r) * LOG2E;
+    // the dense part from what the slab holds: z, or steps from the lower end (less 2^15, the middle of the range)
+    auto dense = [&](float x) { return F32 ? wm * expf(x - lse_r) : wm * ptx::ex2_approx(fmaf(x - 32768.f, LOG2E / tc::STEPS, off)); };
+    float sum = 0.f;               // of the row's dense entries but the closing one, with one
     if (F32)
-        for (int v = threadIdx.x; v < V; v += THREADS) row32[v] = wm * expf(row32[v] - lse_r);
+        for (int v = threadIdx.x; v < V; v += THREADS) {
+            const float x = dense(row32[v]);
+            row32[v] = x;
+            if (v != close) sum += x;
+        }
     else if (m1[r] - ref[r] > tc::LOW_END + tc::TOP_STEP / tc::STEPS - 0.1f) {
         if constexpr (!F32) {
             const int lane = threadIdx.x & 31;
@@ -475,6 +501,7 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(const std::conditional_t<F3
                     const float b = col + 2 * j + 1 < V ? wm * ptx::ex2_approx(fmaf(n1, LOG2E / tc::STEPS, off)) : 0.f;
                     o[j] = ptx::pack_bf16x2(a, b);
                     if (lo > 0) left[j] = ptx::pack_bf16x2(a - __uint_as_float(o[j] << 16), b - __uint_as_float(o[j] & 0xffff0000u));
+                    if (close >= 0) sum += (col + 2 * j != close ? a : 0.f) + (col + 2 * j + 1 != close ? b : 0.f);
                 }
                 row[g] = make_uint4(o[0], o[1], o[2], o[3]);
                 if (lo > 0) rest[g] = make_uint4(left[0], left[1], left[2], left[3]);
@@ -499,12 +526,23 @@ __global__ void __launch_bounds__(THREADS) dz_kernel(const std::conditional_t<F3
             sub += s_p[j];
         }
         if (id == y) sub += beta;
-        if (first) put(id, w * ((beta + mass) * expf(z_i - lse_r) - sub));
+        if (first && id != close) {
+            const float x = w * ((beta + mass) * expf(z_i - lse_r) - sub);
+            put(id, x);
+            sum += x - dense(held);
+        }
     }
     bool listed = false;
     for (int j = threadIdx.x; j < lists.k; j += THREADS) listed |= s_id[j] == y;
-    if (!__syncthreads_or(listed ? 1 : 0) && threadIdx.x == 0)
-        put(y, w * ((beta + mass) * expf(zr[lists.k] - lse_r) - beta));
+    if (!__syncthreads_or(listed ? 1 : 0) && threadIdx.x == 0 && y != close) {
+        const float x = w * ((beta + mass) * expf(zr[lists.k] - lse_r) - beta);
+        put(y, x);
+        sum += x - dense(held_y);
+    }
+    if (close >= 0) {
+        sum = block_sum(sum, s_red);
+        if (threadIdx.x == 0) put(close, 0.f - sum);
+    }
 }
 
 }  // namespace tk
