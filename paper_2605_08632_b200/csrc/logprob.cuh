@@ -395,9 +395,10 @@ __device__ __forceinline__ float gemm_error(const float*, int d) { return static
 // The same of warp_dot_f32: four chains of 2 ceil(d / 256) additions a lane, seven more to join them.
 __device__ __forceinline__ float dot_error(int d) { return static_cast<float>(2 * ((d + 255) / 256) + 9) * 0x1p-24f; }
 // The norm of a vector of d elements from the fp32 sum of their squares, rounded up: what the squares lost below the range, d 2^-126 at most,
-// is added, and 1e-4 covers the roundings of the sum.  Squares past the range give infinity: then every candidate is in doubt.
+// is added, and 1e-3 covers the roundings of the sum (chains of up to 2^12 additions).  Squares past the range give infinity: then every
+// candidate is in doubt.
 __device__ __forceinline__ float norm_above(float sum_sq, int d) {
-    const float x = sqrtf(fmaf(static_cast<float>(d), 0x1p-126f, sum_sq)) * 1.0001f;
+    const float x = sqrtf(fmaf(static_cast<float>(d), 0x1p-126f, sum_sq)) * 1.001f;
     return x >= 0.f ? x : INFINITY;
 }
 // acc + the squares of two bf16 numbers, from above: the upper one is taken with the lower one's bits behind its own, which makes its
