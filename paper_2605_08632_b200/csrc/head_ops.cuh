@@ -29,8 +29,8 @@ int head_splits(const cat_shape* s, long long rows) {
     return s->in_dtype == CAT_BF16 ? fwd_splits(rows, s->V) : f32_splits(rows, s->V);
 }
 
-// Up to 128 rows go to the kernel of skinny.cuh.  Whole calls with 20 alternatives, GEMM of tc_gemm.cuh / that kernel, in us: 2048 x 128256
-// 183 / 99 for one row, 130 / 106 for 64, 143 / 120 for 128; 1024 x 151936 120 / 70, 88 / 75, 97 / 86.
+// Up to 128 rows go to the kernel of skinny.cuh.  Whole calls with 20 alternatives, GEMM of tc_gemm.cuh (and its pass over W for the norms) / that
+// kernel, in us: 2048 x 128256 267 / 101 for one row, 202 / 115 for 64, 213 / 131 for 128; 1024 x 151936 170 / 81, 145 / 87, 149 / 103.
 bool use_skinny(const cat_shape* s) { return s->in_dtype == CAT_BF16 && s->T <= skinny::MAX_ROWS; }
 
 // Vocabulary entries per tile of that kernel: the height whose tiles, dealt to the SMs, leave the busiest the least to read.
@@ -122,8 +122,9 @@ LpPlan plan_lp(const cat_shape* s, int top_k) {
     return p;
 }
 
-// Up to this many rows, with more than a few alternatives, get the row kernel's large CTAs (3 rows of 656 x 3936, one alternative: 18.8 us with
-// them, 17.2 without; 58 rows of 272 x 2915, twenty: 20.6 and 26.8).
+// Up to this many rows, with more than a few alternatives, get the row kernel's large CTAs.  Whole calls with them / with small ones, in us: 200 rows of
+// 2048 x 128256, k = 64: 228 / 278; 58 of 272 x 2915, 20: 21.0 / 23.0; 296 of 1024 x 20000, 20: 53.7 / 55.8, 297: 59.9 / 55.8; one of 2048 x 128256,
+// 4: 97.4 / 95.5; 200 of 1024 x 20000, 1: 45.1 / 43.6; 67 of 1024 x 151936, 4: 84.0 / 85.9.
 constexpr long long kFewRows = 2 * kPlanSMs, kFewAlternatives = 4;
 
 template <class TI, class TZ, bool TOP>
@@ -206,7 +207,7 @@ int launch_norms(const cat_shape* s, const __nv_bfloat16* W, int n_groups, int* 
     }
     return CAT_OK;
 }
-// From this many rows on the GEMM takes longer than the pass beside it.
+// From this many rows on the GEMM is long enough for the pass beside it (figures at lp::norm_kernel).
 constexpr long long kNormsBesideRows = 1024;
 
 template <bool TOP>

@@ -454,10 +454,11 @@ __device__ __forceinline__ void raise_to(int* most, float x) {
 
 // The largest sum of squares of a row of W, which row_kernel's bound wants.
 //   BESIDE: launched behind the logits GEMM, whose CTAs let it start as soon as they all run.  They leave it 2 KB of shared memory and 28 KB of L1,
-//     so that it reads at 1.7 TB/s: hidden behind a GEMM of many rows.  It ends after the GEMM, so that what follows may take its end for both.
+//     so that it reads at 1 to 1.7 TB/s: hidden behind a GEMM of many rows.  It ends after the GEMM, so that what follows may take its end for both.
 //   otherwise ahead of the GEMM, alone, at the rate of a copy.  Its CTAs walk the GEMM's vocabulary groups (n_groups of them, in tiles of BN)
 //     from back to front, so that what the GEMM reads first is in the L2.
-// Whole calls with k = 20, beside / ahead, in us: 129 rows of 2048 x 128256 386 / 217; 600 of 1024 x 151936 354 / 267.
+// Whole calls with k = 20, beside / ahead, in us: 129 rows of 2048 x 128256 503 / 204, 700 561 / 422, 1100 513 / 624, 4000 1610 / 1853; 600 of 1024 x 151936
+// 348 / 285, 1100 429 / 435, 2000 651 / 629.
 template <bool BESIDE>
 constexpr int NORM_THREADS = BESIDE ? 256 : 512;      // beside: what the registers that the GEMM leaves a quarter of an SM allow
 template <bool BESIDE>
@@ -674,9 +675,9 @@ __device__ __forceinline__ int settle(const RowParams<TI, TZ>& p, const TI* h, S
 // are summed again, in fp32 (off by eps32 at most); those still in doubt against each other, in fp64, which takes eight times as long.
 //
 // The values.  A bf16 logit of 20 that comes out 3e-6 of itself too small would be off by more than its log probability has
-// places for.  With few rows every value is an fp32 sum over d.  With many that is a gather of W for each (9240 rows of 1344 x 4906, k = 20: 178 -> 225 us;
-// 8192 of 2048 x 128256, k = 64: 3.18 -> 3.51 ms): there only values that the slab's fp16 has rounded (not the largest of their group) are
-// summed, and the others are corrected by the share of itself that the largest logit is off (see finish_row).
+// places for.  With few rows every value is an fp32 sum over d.  With many only values in doubt and values that the slab's fp16 has rounded (not
+// the largest of their group) are summed, each a gather of a row of W, and the others are corrected by the share of itself that the largest
+// logit is off (see finish_row).
 template <class TI, class TZ, int RT>
 __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI* h, long long r, Shared<RT>& sh, int n, float eps, float eps32) {
     constexpr int RW = RT / 32;

@@ -11,8 +11,9 @@
 //     this way 61 us.)  Running sums stay in registers over all tiles of the CTA; warps and CTAs are merged at the end;
 //   * with alternatives, four more warps sum the squares of W's rows as their slices pass, for the bound on the logits' errors
 //     (lp::gemm_error): the longest row is known without another pass over W.
-// Measured: one row of 2048 x 128256 (W 525 MB) 80.6 us, 6.5 TB/s, the rate of a plain copy; 67 rows of 1024 x 151936 (311 MB)
-// 61 us, 5.1 TB/s: the slices of H share the ring, and start and end of the launch are a sixth of it.
+// Measured, with alternatives: one row of 2048 x 128256 (W 525 MB) 82 us, 6.4 TB/s, the rate of a plain copy; 67 rows of 1024 x 151936 (311 MB)
+// 70 us, 4.4 TB/s: the slices of H share the ring, start and end of the launch are a seventh of it, and the squares hold every slice for
+// a while longer (61 us without them).
 #pragma once
 #include "logprob.cuh"
 
