@@ -690,6 +690,8 @@ __device__ __forceinline__ int settle_close(const RowParams<TI, TZ>& p, const TI
     const int part = threadIdx.x / (n > 0 ? n : 1), per = (n + parts - 1) / parts;
     for (int c = threadIdx.x; c < n; c += RT) { sh.above[c] = 0; sh.close[c] = 0; }
     if (threadIdx.x == 0) sh.n_near = sh.n_rest = sh.n_tied = 0;
+    // every place is written below, but where a logits kernel that timed out has left norms that bound nothing
+    for (int c = threadIdx.x; c < p.k; c += RT) { sh.z_keep[c] = -INFINITY; sh.id_keep[c] = -1; }
     __syncthreads();
     for (int c = parts > 1 ? threadIdx.x - part * n : threadIdx.x; c < n && (parts == 1 || part < parts); c += parts > 1 ? CAP : RT) {
         const float z = sh.approx[c], e = sh.err[c];
