@@ -489,6 +489,86 @@ int cat_topk_kd_loss_fwd_bwd(const cat_shape* shape, const cat_topk_kd_desc* des
                              void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * An LM head (or any projection) kept in 8 bits (no counterpart in the paper: drafts that share the target's frozen head train and
+ * answer through it).  A row x of d values is held as integers xq and one scale,
+ *     scale = max_i |x_i| / 127 (binary32),   xq_i = the integer nearest to 127 x_i / max |x|, halves to the even one,
+ * exactly so for every x; x_i is about scale * xq_i.  Rows of zeros have scale 0; a row that holds an infinity or NaN has scale NaN and zeros.
+ *   X      [rows, d] of dtype, row pitch ldX elements; any d >= 1, any alignment of its type     (device, in)
+ *   Xq     [rows, d] int8 with row pitch ldXq bytes; bytes past d are left as they are             (device, out)
+ *   scale  [rows] fp32                                                                            (device, out)
+ * One kernel, no workspace.  Returns CAT_OK or a negative cat_status.
+ */
+int cat_i8_quantize(const void* X, int32_t dtype, int64_t rows, int64_t d, int64_t ldX, int8_t* Xq, int64_t ldXq, float* scale,
+                    void* cuda_stream);
+
+/* Sizes of a call on an 8-bit head, read on the host. */
+typedef struct {
+    int64_t T;         /* rows of X: tokens                                                       */
+    int64_t d;         /* contraction length, <= 65536                                            */
+    int64_t V;         /* rows of Wq: channels, vocabulary entries                                */
+    int64_t ldX;       /* row pitch of X in elements, >= d                                        */
+    int64_t lddX;      /* row pitch of dX in elements, >= d, a multiple of 8 (dX 16-byte aligned); backward passes only */
+    int64_t ldW;       /* row pitch of Wq in bytes, >= d, a multiple of 16 (Wq 16-byte aligned)   */
+    int64_t ldY;       /* row pitch of Y and dY in elements, >= V, whole 16 bytes (Y, dY 16-byte aligned); linear passes only */
+    int32_t x_dtype;   /* cat_dtype of X; the backward passes are for CAT_BF16 (dX is CAT_BF16) with d % 8 == 0 */
+    int32_t y_dtype;   /* cat_dtype of Y; dY is CAT_BF16                                          */
+    int32_t slab_mib;  /* cap, in MiB, on the slab of cat_i8_ce_bwd; 0 = default (3072)            */
+    int32_t reserved;
+} cat_i8_shape;
+
+/* Scratch bytes: pass 0 = cat_i8_linear_fwd, 1 = cat_i8_linear_bwd, 2 = cat_i8_ce_fwd, 3 = cat_i8_ce_bwd.  0 if anything is invalid. */
+size_t cat_i8_workspace_bytes(const cat_i8_shape* shape, int pass);
+
+/*
+ * Matrix product in 8-bit integers with a scale for each token and each channel:
+ *     Y[t, v] = sx[t] w_scale[v] sum_i xq[t, i] Wq[v, i] + bias[v]
+ * with (xq, sx) the rows of X as cat_i8_quantize holds them (the call does that itself).  The sums are exact (int32 on the tensor
+ * cores); the scales and the bias are applied in binary32 and the result is rounded once to y_dtype.
+ *   X        [T, d] of x_dtype                                                     (device, in)
+ *   Wq       [V, d] int8 (-128 .. 127), pitch ldW bytes;  w_scale  [V] fp32          (device, in)
+ *   bias     [V] fp32 or NULL                                                       (device, in)
+ *   Y        [T, V] of y_dtype, pitch ldY; elements past V are left as they are       (device, out)
+ *   workspace  at least cat_i8_workspace_bytes(shape, 0) bytes, 256-byte aligned; its first int32 holds the device status after the call
+ * Calls that may overlap on the GPU need a workspace each.
+ */
+int cat_i8_linear_fwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, const float* w_scale, const float* bias, void* Y,
+                      void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Gradient of the product with respect to its tokens, the head frozen and the tokens' rounding passed straight through:
+ *     dX[t, i] = sum_v dY[t, v] w_scale[v] Wq[v, i].
+ *   dY  [T, V] bf16, pitch ldY (device, in);  dX  [T, d] bf16, pitch lddX (device, out)
+ * w_scale[v] Wq[v, :] is rounded to bf16 as the operand of the contraction, which is summed in binary32.
+ */
+int cat_i8_linear_bwd(const cat_i8_shape* shape, const void* dY, const int8_t* Wq, const float* w_scale, void* dX,
+                      void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Softmax cross entropy over an 8-bit head, in pieces of the vocabulary, without the logits being stored: with z = the product above
+ * (without bias),
+ *     lse[t] = log sum_v exp z[t, v],     nll[t] = lse[t] - z[t, y_t].
+ * nll is formed as log(1 + exp(lse over the other tokens - z[t, y_t])): as exact, relative to itself, for rows that are sure of their label as for others.
+ * A row with valid[t] == 0 has nll = lse = 0, whatever X holds there; one whose label is outside [0, V) has nll 0.  A row with an infinity or
+ * NaN has NaN.
+ *   labels   [T] int64;  valid  [T] uint8 or NULL;  nll, lse  [T] fp32
+ */
+int cat_i8_ce_fwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, const float* w_scale, const int64_t* labels,
+                  const uint8_t* valid, float* nll, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Gradient of sum_t grad_nll[t] nll[t] with respect to X, the head frozen, the tokens' rounding passed straight through:
+ *     dX[t, :] = grad_nll[t] sum_v (exp(z[t, v] - lse[t]) - [v == y_t]) w_scale[v] Wq[v, :].
+ * The logits are recomputed per row slab.  A row's terms are kept relative to 1 - p(y_t) and to the largest |w_scale|, in 11 bits of precision and down
+ * to 2^-39 of their largest, so that rows that are sure of their label keep theirs; p(y_t) is taken from nll.
+ * Rows that take no part (valid[t] == 0, a label outside [0, V)) get zeros.
+ *   nll, lse  [T] fp32 as written by cat_i8_ce_fwd for the same rows and head;  grad_nll  [T] fp32   (device, in)
+ *   dX        [T, d] bf16, pitch lddX                                                             (device, out)
+ */
+int cat_i8_ce_bwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, const float* w_scale, const int64_t* labels,
+                  const uint8_t* valid, const float* nll, const float* lse, const float* grad_nll, void* dX,
+                  void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Number of kernels of this library that the given pass (0 = cat_loss_fwd, 1 = cat_loss_bwd,
  * 2 = cat_loss_fwd_bwd) launches for this shape: the logits GEMM, the per-row kernels and the final reduction in
  * the forward pass; one set-up kernel plus three GEMMs per vocabulary slab in the backward

@@ -5,6 +5,7 @@ C entry points.  No arithmetic of the method happens here.
 """
 from __future__ import annotations
 
+import functools
 from typing import NamedTuple
 
 import torch
@@ -379,6 +380,219 @@ class LogProbModule(torch.nn.Module):
         engine = TokenLogProb(T, d, self.weight.shape[0], self.top_k, dtype=H.dtype, dW_dtype=self.weight.dtype, slab_mib=self.slab_mib,
                               device=str(H.device))
         return _LogProbFn.apply(H, self.weight, labels, valid, engine)
+
+
+_I8_CODE = {torch.bfloat16: B.CAT_BF16, torch.float32: B.CAT_F32}
+_I8_LINEAR, _I8_LINEAR_BWD, _I8_CE, _I8_CE_BWD = range(4)
+
+
+def _rows(name, t, dtypes, device=None):
+    """Refuses what is no matrix of one of the types with contiguous rows, on `device` or any GPU."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions, got {tuple(t.shape)}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a CUDA device; there is no CPU path")
+    _check(name, t, t.shape, t.dtype, t.device if device is None else device, rows_only=True)
+
+
+def quantize_rows(X):
+    """Rows of X [rows, d] as 8-bit integers with a scale each (cat_i8_quantize): (q [rows, d] int8, scale [rows] fp32), X about
+    q * scale.  bfloat16 or float32; the rows of q lie a multiple of 16 bytes apart, as the products want them."""
+    X = X.detach()
+    _rows("X", X, _I8_CODE)
+    rows, d = X.shape
+    if d == 0:
+        raise ValueError("X must have columns")
+    q = torch.empty(rows, (d + 15) // 16 * 16, dtype=torch.int8, device=X.device)
+    scale = torch.empty(rows, dtype=torch.float32, device=X.device)
+    if rows:
+        _on(X.device, B.cat_i8_quantize, X, _I8_CODE[X.dtype], rows, d, _pitch(X), q, q.shape[1], scale)
+    return q[:, :d], scale
+
+
+@functools.lru_cache(maxsize=512)
+def _i8_plan(which, T, d, V, ldX, ldY, x_dtype, y_dtype, slab_mib):
+    """The call's sizes and the bytes of its workspace."""
+    shape = B.make_i8_shape(T, d, V, ldX, None, None, ldY, x_dtype, y_dtype, slab_mib)
+    n = B.cat_i8_workspace_bytes(shape, which)
+    if n == 0:
+        raise ValueError("invalid shape or layout for an 8-bit head: at most 65536 columns; gradients want d, and the rows of dY, in whole 16 bytes")
+    return shape, n
+
+
+class Int8Head(torch.nn.Module):
+    """A frozen LM head (or any projection) kept in 8 bits, with a scale for each of its V rows, and what is computed with it from hidden states
+    X [T, d] (bfloat16 or float32), which each call holds in 8 bits with a scale for each token:
+
+        logits = head(X)                        the product, bfloat16 or float32, with `bias` [V] fp32 where there is one
+        nll = head.loss(X, labels, valid)       softmax cross entropy of each row (without the bias), in pieces of the vocabulary
+
+    Both carry gradients to bfloat16 X (the tokens' rounding is passed straight through).  Calls share nothing but the head: any lengths,
+    streams and threads.  Not for stream capture with gradients: autograd may then wait for other streams inside the capture; capture
+    loss_forward and loss_backward (or logits and logits_backward) instead.  `Int8Head(weight)` quantises a head, `Int8Head.from_quantized`
+    takes one that is in 8 bits already."""
+
+    def __init__(self, weight, bias=None, slab_mib: int = 0):
+        self._set(*quantize_rows(weight), bias, slab_mib)
+
+    @classmethod
+    def from_quantized(cls, q, scale, bias=None, slab_mib: int = 0):
+        """q [V, d] int8, scale [V] fp32.  A q whose rows lie whole 16 bytes apart is used where it is, another is copied."""
+        head = cls.__new__(cls)
+        head._set(q, scale, bias, slab_mib)
+        return head
+
+    def _set(self, q, scale, bias, slab_mib):
+        torch.nn.Module.__init__(self)
+        _rows("q", q, (torch.int8,))
+        self.V, self.d = q.shape
+        if self.V == 0 or self.d == 0:
+            raise ValueError("a head has rows and columns")
+        if bias is not None:
+            _check("bias", bias, (self.V,), torch.float32, q.device)
+        _check("scale", scale, (self.V,), torch.float32, q.device)
+        ld = (self.d + 15) // 16 * 16
+        in_place = _pitch(q) == ld and q.data_ptr() % 16 == 0 and q.storage_offset() + self.V * ld <= q.untyped_storage().nbytes()
+        if in_place:
+            padded = q.as_strided((self.V, ld), (ld, 1))
+        else:
+            padded = torch.zeros(self.V, ld, dtype=torch.int8, device=q.device)
+            padded[:, :self.d] = q
+        self.register_buffer("q", padded.detach())
+        self.register_buffer("scale", scale.detach())
+        self.register_buffer("bias", None if bias is None else bias.detach())
+        self.slab_mib = slab_mib
+
+    def _head(self, X, dtypes=tuple(_I8_CODE)):
+        """Checks the head as it is now (a module may have been moved or cast) and X against it."""
+        _check("q", self.q, (self.V, (self.d + 15) // 16 * 16), torch.int8, self.q.device)
+        _check("scale", self.scale, (self.V,), torch.float32, self.q.device)
+        if self.bias is not None:
+            _check("bias", self.bias, (self.V,), torch.float32, self.q.device)
+        _rows("X", X, dtypes, self.q.device)
+        if X.shape[1] != self.d:
+            raise ValueError(f"X must have {self.d} columns, got {X.shape[1]}")
+
+    def _call(self, which, entry, T, ldX, x_dtype, args, ldY=None, y_dtype=B.CAT_BF16):
+        if T == 0:
+            return
+        shape, n = _i8_plan(which, T, self.d, self.V, ldX, ldY, x_dtype, y_dtype, self.slab_mib)
+        _on(self.q.device, entry, shape, *args, torch.empty(n, dtype=torch.uint8, device=self.q.device))
+
+    def logits(self, X, out_dtype=None):
+        """[T, V] in out_dtype (X's unless given).  Where V is not in whole 16 bytes the rows lie further apart than V."""
+        self._head(X)
+        out_dtype = X.dtype if out_dtype is None else out_dtype
+        if out_dtype not in _I8_CODE:
+            raise TypeError("logits are bfloat16 or float32")
+        if torch.is_grad_enabled() and X.requires_grad:
+            self._refuse_capture(X)
+            return _Int8LogitsFn.apply(X, self, out_dtype)
+        return self._logits(X, out_dtype)
+
+    forward = logits
+
+    def _logits(self, X, out_dtype):
+        T, ldY = X.shape[0], (self.V + 7) // 8 * 8
+        Y = torch.empty(T, ldY, dtype=out_dtype, device=X.device)
+        self._call(_I8_LINEAR, B.cat_i8_linear_fwd, T, _pitch(X), _I8_CODE[X.dtype], (X, self.q, self.scale, self.bias, Y), ldY, _I8_CODE[out_dtype])
+        return Y if ldY == self.V else Y[:, :self.V]
+
+    def logits_backward(self, dY):
+        """dX [T, d] bfloat16 for the upstream gradient of the logits, [T, V] bfloat16.  Its rows have to lie whole 16 bytes apart."""
+        _rows("dY", dY, (torch.bfloat16,), self.q.device)
+        if dY.shape[1] != self.V:
+            raise ValueError(f"dY must have {self.V} columns, got {dY.shape[1]}")
+        T = dY.shape[0]
+        ldY = dY.stride(0) if T > 1 else (self.V + 7) // 8 * 8
+        dX = torch.empty(T, self.d, dtype=torch.bfloat16, device=dY.device)
+        self._call(_I8_LINEAR_BWD, B.cat_i8_linear_bwd, T, self.d, B.CAT_BF16, (dY, self.q, self.scale, dX), ldY)
+        return dX
+
+    def _rowwise(self, T, labels, valid, **f32):
+        _check("labels", labels, (T,), torch.int64, self.q.device)
+        if valid is not None:
+            _check("valid", valid, (T,), torch.uint8, self.q.device)
+        for name, t in f32.items():
+            _check(name, t, (T,), torch.float32, self.q.device)
+
+    def loss_forward(self, X, labels, valid=None):
+        """(nll [T], lse [T]) without a graph for autograd."""
+        valid, T = _mask(valid), X.shape[0]
+        self._head(X)
+        self._rowwise(T, labels, valid)
+        nll, lse = (torch.empty(T, dtype=torch.float32, device=X.device) for _ in range(2))
+        self._call(_I8_CE, B.cat_i8_ce_fwd, T, _pitch(X), _I8_CODE[X.dtype], (X, self.q, self.scale, labels, valid, nll, lse))
+        return nll, lse
+
+    def loss_backward(self, X, labels, valid, grad_nll, nll, lse):
+        """dX [T, d] for the upstream gradient of nll; nll and lse: those of loss_forward on the same rows."""
+        valid, T = _mask(valid), X.shape[0]
+        self._head(X, (torch.bfloat16,))
+        self._rowwise(T, labels, valid, grad_nll=grad_nll, nll=nll, lse=lse)
+        dX = torch.empty(T, self.d, dtype=X.dtype, device=X.device)
+        self._call(_I8_CE_BWD, B.cat_i8_ce_bwd, T, _pitch(X), B.CAT_BF16, (X, self.q, self.scale, labels, valid, nll, lse, grad_nll, dX))
+        return dX
+
+    def loss(self, X, labels, valid=None):
+        """nll [T] fp32: the cross entropy of each row with its label, 0 for rows that are masked or whose label is no token id.  What
+        is made of them (means, weights) is the caller's."""
+        if torch.is_grad_enabled() and X.requires_grad:
+            self._head(X, (torch.bfloat16,))
+            self._refuse_capture(X)
+            return _Int8LossFn.apply(X, labels, valid, self)
+        return self.loss_forward(X, labels, valid)[0]
+
+    @staticmethod
+    def _refuse_capture(X):
+        if X.dtype != torch.bfloat16:
+            raise TypeError(f"gradients are for bfloat16 X, got {X.dtype}")
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("Int8Head cannot be captured with gradients: capture loss_forward and loss_backward, or logits and logits_backward")
+
+    @staticmethod
+    def _refuse_capture_backward():
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("Int8Head's backward pass cannot be captured: capture loss_backward or logits_backward")
+
+
+class _Int8LogitsFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, X, head, out_dtype):
+        ctx.head = head
+        ctx.save_for_backward(head.q, head.scale)           # so that a head changed in between is noticed
+        return head._logits(X.detach(), out_dtype)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dY):
+        Int8Head._refuse_capture_backward()
+        ctx.saved_tensors
+        T, V = dY.shape
+        if dY.dtype != torch.bfloat16 or dY.stride(1) != 1 or (T > 1 and (dY.stride(0) < V or dY.stride(0) % 8)) or dY.data_ptr() % 16:
+            laid = torch.empty(T, (V + 7) // 8 * 8, dtype=torch.bfloat16, device=dY.device)[:, :V]
+            laid.copy_(dY)
+            dY = laid
+        return ctx.head.logits_backward(dY), None, None
+
+
+class _Int8LossFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, X, labels, valid, head):
+        nll, lse = head.loss_forward(X.detach(), labels, valid)
+        ctx.head = head
+        # the caller may write to the losses that are handed out
+        ctx.save_for_backward(X, labels, valid, nll.clone(), lse, head.q, head.scale)
+        return nll
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        Int8Head._refuse_capture_backward()
+        X, labels, valid, nll, lse = ctx.saved_tensors[:5]
+        return ctx.head.loss_backward(X.detach(), labels, valid, g.contiguous(), nll, lse), None, None, None
 
 
 class _CatLossFn(torch.autograd.Function):

@@ -46,6 +46,12 @@ class cat_topk_kd_desc(ctypes.Structure):
 CAT_TOPK_MAX = 256
 
 
+class cat_i8_shape(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("d", ctypes.c_int64), ("V", ctypes.c_int64), ("ldX", ctypes.c_int64), ("lddX", ctypes.c_int64),
+                ("ldW", ctypes.c_int64), ("ldY", ctypes.c_int64), ("x_dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32), ("slab_mib", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
 class CatError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -106,6 +112,14 @@ def lib() -> ctypes.CDLL:
         L.cat_topk_kd_workspace_bytes.argtypes = [ctypes.POINTER(cat_shape), ctypes.POINTER(cat_topk_kd_desc)]
         L.cat_topk_kd_loss_fwd_bwd.restype = ctypes.c_int
         L.cat_topk_kd_loss_fwd_bwd.argtypes = [ctypes.POINTER(cat_shape), ctypes.POINTER(cat_topk_kd_desc)] + [vp] * 16 + [ctypes.c_int, vp, sz, vp]
+        L.cat_i8_quantize.restype = ctypes.c_int
+        L.cat_i8_quantize.argtypes = [vp, ctypes.c_int32, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, vp, ctypes.c_int64, vp, vp]
+        L.cat_i8_workspace_bytes.restype = sz
+        L.cat_i8_workspace_bytes.argtypes = [ctypes.POINTER(cat_i8_shape), ctypes.c_int]
+        for name, n in (("cat_i8_linear_fwd", 5), ("cat_i8_linear_bwd", 4), ("cat_i8_ce_fwd", 7), ("cat_i8_ce_bwd", 9)):
+            f = getattr(L, name)
+            f.restype = ctypes.c_int
+            f.argtypes = [ctypes.POINTER(cat_i8_shape)] + [vp] * n + [vp, sz, vp]
         L.cat_die_map.restype = ctypes.c_int
         L.cat_die_map.argtypes = [vp, ctypes.c_int, vp, vp]
         L.cat_selftest_wait_timeout.restype = ctypes.c_int
@@ -331,6 +345,50 @@ def cat_topk_kd_loss_fwd_bwd(shape, desc, H, W, labels, valid, top_ids, top_logp
                                         workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
     if rc != CAT_OK:
         raise CatError(rc, "cat_topk_kd_loss_fwd_bwd")
+
+
+def cat_i8_quantize(X, dtype, rows, d, ldX, Xq, ldXq, scale) -> None:
+    rc = lib().cat_i8_quantize(_ptr(X), int(dtype), int(rows), int(d), int(ldX), _ptr(Xq), int(ldXq), _ptr(scale), _stream())
+    if rc != CAT_OK:
+        raise CatError(rc, "cat_i8_quantize")
+
+
+def make_i8_shape(T, d, V, ldX=None, lddX=None, ldW=None, ldY=None, x_dtype=CAT_BF16, y_dtype=CAT_BF16, slab_mib=0) -> cat_i8_shape:
+    return cat_i8_shape(T, d, V, d if ldX is None else ldX, d if lddX is None else lddX, (d + 15) // 16 * 16 if ldW is None else ldW,
+                        (V + 7) // 8 * 8 if ldY is None else ldY, x_dtype, y_dtype, slab_mib, 0)
+
+
+def cat_i8_workspace_bytes(shape, which: int) -> int:
+    return int(lib().cat_i8_workspace_bytes(ctypes.byref(shape), int(which)))
+
+
+def cat_i8_linear_fwd(shape, X, Wq, w_scale, bias, Y, workspace) -> None:
+    rc = lib().cat_i8_linear_fwd(ctypes.byref(shape), _ptr(X), _ptr(Wq), _ptr(w_scale), _ptr(bias), _ptr(Y), _ptr(workspace),
+                                 workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+    if rc != CAT_OK:
+        raise CatError(rc, "cat_i8_linear_fwd")
+
+
+def cat_i8_linear_bwd(shape, dY, Wq, w_scale, dX, workspace) -> None:
+    rc = lib().cat_i8_linear_bwd(ctypes.byref(shape), _ptr(dY), _ptr(Wq), _ptr(w_scale), _ptr(dX), _ptr(workspace),
+                                 workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+    if rc != CAT_OK:
+        raise CatError(rc, "cat_i8_linear_bwd")
+
+
+def cat_i8_ce_fwd(shape, X, Wq, w_scale, labels, valid, nll, lse, workspace) -> None:
+    rc = lib().cat_i8_ce_fwd(ctypes.byref(shape), _ptr(X), _ptr(Wq), _ptr(w_scale), _ptr(labels), _ptr(valid), _ptr(nll), _ptr(lse),
+                             _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+    if rc != CAT_OK:
+        raise CatError(rc, "cat_i8_ce_fwd")
+
+
+def cat_i8_ce_bwd(shape, X, Wq, w_scale, labels, valid, nll, lse, grad_nll, dX, workspace) -> None:
+    rc = lib().cat_i8_ce_bwd(ctypes.byref(shape), _ptr(X), _ptr(Wq), _ptr(w_scale), _ptr(labels), _ptr(valid), _ptr(nll), _ptr(lse),
+                             _ptr(grad_nll), _ptr(dX), _ptr(workspace),
+                             workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+    if rc != CAT_OK:
+        raise CatError(rc, "cat_i8_ce_bwd")
 
 
 def cat_die_map():

@@ -16,6 +16,7 @@
 #include <mutex>
 
 #include "fp32_gemm.cuh"
+#include "i8_head.cuh"
 #include "kd.cuh"
 #include "logprob.cuh"
 #include "rowops.cuh"
@@ -1396,3 +1397,4 @@ int cat_selftest_wait_timeout(int role, uint64_t short_ns, uint64_t long_ns, int
 }  // extern "C"
 
 #include "head_ops.cuh"
+#include "i8_ops.cuh"
