@@ -12,6 +12,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "logprob.cuh"
 #include "ptx.cuh"
 #include "tc_gemm.cuh"
 
@@ -56,11 +57,8 @@ __global__ void __launch_bounds__(THREADS) quantize_kernel(const T* X, long long
     if (threadIdx.x == 0) scale[r] = finite ? most / 127.f : __uint_as_float(0x7fc00000u);
 }
 
-// ------------------------------------------------------------------------------ a plain product, 64 x 64 outputs per CTA
-constexpr int TILE = 64;
-
 struct Head {
-    const int8_t* xq;      // [T][ldq], zeros past d
+    const int8_t* xq;      // [T][ldq]
     const float* sx;       // [T]
     const int8_t* wq;      // [V][ldw]
     const float* sw;       // [V]
@@ -68,90 +66,237 @@ struct Head {
     int T, V, d;
 };
 
-__device__ __forceinline__ int four_bytes(const int8_t* row, int k, int d) {
-    if (k + 4 <= d) return *reinterpret_cast<const int*>(row + k);
-    int v = 0;
-    for (int i = 0; i < 4; ++i)
-        if (k + i < d) v |= (static_cast<int>(row[k + i]) & 255) << (8 * i);
-    return v;
+// ------------------------------------------------------------------------------ epilogues of the 8-bit product
+// The GEMM of tc_gemm.cuh on integers (kind::i8, exact int32 sums, twice the bf16 rate).  A tile is done in half the time, so two sets of four
+// warps share its columns.
+using OutStage1 = tc::OutStageOf<1>;
+
+// Chunks of 32 columns of this warp's half of a tile, body(c, v) for each that holds columns below ncols: the next one is on its way from
+// tensor memory while the warp works on one.
+template <class F>
+__device__ __forceinline__ void walk_half(uint32_t taddr, int ncols, F&& body) {
+    const int c0 = ((threadIdx.x - 64) >> 7) * 4;
+    if (c0 * 32 >= ncols) return;
+    uint32_t a[32], b[32];
+    ptx::tmem_ld_32x32(taddr + c0 * 32, a);
+#pragma unroll 1
+    for (int c = c0; c < c0 + 4 && c * 32 < ncols; c += 2) {
+        ptx::tmem_ld_wait(a);
+        ptx::tmem_ld_32x32(taddr + (c + 1) * 32, b);
+        body(c, a);
+        ptx::tmem_ld_wait(b);
+        if (c + 2 < c0 + 4) ptx::tmem_ld_32x32(taddr + (c + 2) * 32, a);
+        if ((c + 1) * 32 < ncols) body(c + 1, b);
+    }
+    ptx::tmem_ld_wait();
 }
 
-__device__ __forceinline__ void tile_sums(const Head& h, int r0, int c0, int (&acc)[4][4]) {
-    __shared__ int sa[TILE][17], sb[TILE][17];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    for (int k0 = 0; k0 < h.d; k0 += 64) {
-        for (int i = threadIdx.x; i < TILE * 16; i += THREADS) {
-            const int row = i >> 4, w = i & 15, k = k0 + 4 * w;
-            sa[row][w] = r0 + row < h.T && k < h.d ? four_bytes(h.xq + (r0 + row) * h.ldq, k, h.d) : 0;
-            sb[row][w] = c0 + row < h.V && k < h.d ? four_bytes(h.wq + (c0 + row) * h.ldw, k, h.d) : 0;
+// 32 neighbouring values, the same for all lanes; zeros past the live ones
+__device__ __forceinline__ void values_at(const float* p, int live, float (&w)[32]) {
+    if (live >= 32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float4 x = __ldg(reinterpret_cast<const float4*>(p) + i);
+            w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
         }
-        __syncthreads();
-        for (int w = 0; w < 16; ++w)
+    } else {
 #pragma unroll
-            for (int a = 0; a < 4; ++a)
-#pragma unroll
-                for (int b = 0; b < 4; ++b) acc[a][b] = __dp4a(sa[ty * 4 + a][w], sb[tx * 4 + b][w], acc[a][b]);
-        __syncthreads();
+        for (int i = 0; i < 32; ++i) w[i] = i < live ? __ldg(p + i) : 0.f;
     }
 }
 
-__global__ void __launch_bounds__(THREADS) linear_kernel(const Head h, const float* bias, float* Yf, __nv_bfloat16* Yb, long long ldY) {
-    const int c0 = blockIdx.x * TILE, r0 = blockIdx.y * TILE;
-    int acc[4][4] = {};
-    tile_sums(h, r0, c0, acc);
-    for (int a = 0; a < 4; ++a)
-        for (int b = 0; b < 4; ++b) {
-            const int r = r0 + (threadIdx.x >> 4) * 4 + a, c = c0 + (threadIdx.x & 15) * 4 + b;
-            if (r >= h.T || c >= h.V) continue;
-            float y = __int2float_rn(acc[a][b]) * h.sw[c] * h.sx[r];
-            if (bias) y += bias[c];
-            if (Yf) Yf[r * ldY + c] = y;
-            else Yb[r * ldY + c] = __float2bfloat16(y);
-        }
+// integer sums times the channels' scales
+__device__ __forceinline__ void scaled(const uint32_t (&v)[32], const float (&w)[32], float (&f)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 2)
+        ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(__int2float_rn(static_cast<int>(v[i])), __int2float_rn(static_cast<int>(v[i + 1]))),
+                                         ptx::pack_f32x2(w[i], w[i + 1])), f[i], f[i + 1]);
 }
+
+// The product itself.  Whole chunks of 32 columns leave through shared memory and TMA stores (the tensor map ends with them: a store that is cut
+// off at the vocabulary's end would still write whole 16 bytes), the last ones from the threads.
+template <bool F32>
+struct EpiLinear {
+    struct Params {
+        const float* sx;       // [T]
+        const float* sw;       // [V]
+        const float* bias;     // [V] or nullptr
+        void* Y;               // [T][ldY]
+        long long ldY;
+        int T, V;
+    };
+    struct State {
+        float sx;
+        int row;
+    };
+    __device__ static __forceinline__ void begin_item(const Params& p, State& s, int m_tile, int row_in_tile) {
+        s.row = m_tile * tc::BM + row_in_tile;
+        s.sx = s.row < p.T ? p.sx[s.row] : 0.f;
+    }
+    __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage1& o) {
+        const int col0 = n_tile * tc::BN;
+        const int ncols = min(tc::BN, p.V - col0);
+        walk_half(taddr, ncols, [&](int c, uint32_t (&v)[32]) {
+            float w[32], f[32];
+            values_at(p.sw + col0 + c * 32, ncols - c * 32, w);
+            scaled(v, w, f);
+            if (p.bias != nullptr) {
+                values_at(p.bias + col0 + c * 32, ncols - c * 32, w);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) f[i] = __fadd_rn(__fmul_rn(f[i], s.sx), w[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) f[i] *= s.sx;
+            }
+            const int live = ncols - c * 32;
+            if (live < 32) {
+                if (!F32 && (c & 1) != 0) o.flush(col0 + (c >> 1) * 64);          // the chunk before, with whatever is beside it
+                if (s.row < p.T) {
+                    const long long at = s.row * p.ldY + col0 + c * 32;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        if (i >= live) continue;
+                        if (F32) static_cast<float*>(p.Y)[at + i] = f[i];
+                        else static_cast<__nv_bfloat16*>(p.Y)[at + i] = __float2bfloat16(f[i]);
+                    }
+                }
+                return;
+            }
+            if (F32) {
+                o.begin();
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    o.put(j, __float_as_uint(f[4 * j]), __float_as_uint(f[4 * j + 1]), __float_as_uint(f[4 * j + 2]), __float_as_uint(f[4 * j + 3]));
+                o.flush(col0 + c * 32);
+            } else {
+                if ((c & 1) == 0) o.begin();
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    o.put((c & 1) * 4 + q, ptx::pack_bf16x2(f[q * 8 + 0], f[q * 8 + 1]), ptx::pack_bf16x2(f[q * 8 + 2], f[q * 8 + 3]),
+                          ptx::pack_bf16x2(f[q * 8 + 4], f[q * 8 + 5]), ptx::pack_bf16x2(f[q * 8 + 6], f[q * 8 + 7]));
+                if ((c & 1) != 0 || live == 32) o.flush(col0 + (c >> 1) * 64);
+            }
+        });
+    }
+    __device__ static __forceinline__ int out_rows(const Params& p) { return p.T; }
+    __device__ static __forceinline__ void end_item(const Params&, const State&, int) {}
+};
 
 // log2 e times a row's scale; a row of zeros has logits 0 whatever this is, and -infinity times it has to stay -infinity.
 __device__ __forceinline__ float log2_scale(float sx) { return sx == 0.f ? tc::LOG2E : sx * tc::LOG2E; }
 
-// Largest logit but the label's and the sum relative to it, per row and tile of the vocabulary, in units of log2.
-__global__ void __launch_bounds__(THREADS) ce_kernel(const Head h, const long long* labels, float* part_m, float* part_l, float* z_label) {
-    const int c0 = blockIdx.x * TILE, r0 = blockIdx.y * TILE;
-    int acc[4][4] = {};
-    tile_sums(h, r0, c0, acc);
-    for (int a = 0; a < 4; ++a) {
-        const int r = r0 + (threadIdx.x >> 4) * 4 + a;
-        const float s = log2_scale(r < h.T ? h.sx[r] : 0.f);
-        const long long y = r < h.T ? labels[r] : -1;
-        float z[4], m = LOW2, l = 0.f;
-        for (int b = 0; b < 4; ++b) {
-            const int c = c0 + (threadIdx.x & 15) * 4 + b;
-            z[b] = c < h.V ? __int2float_rn(acc[a][b]) * h.sw[c] * s : -INFINITY;
-            if (r < h.T && c < h.V && c == y) { z_label[r] = z[b]; z[b] = -INFINITY; }
-            m = fmaxf(m, z[b]);
+// Largest logit but the label's and the sum of the exponentials relative to it, in units of log2, and the label's logit.
+struct RowSums {
+    float m, l;            // running maximum and sum
+    float a;               // log2 e times the row's scale
+    __device__ __forceinline__ void clear(float sx) { m = LOW2; l = 0.f; a = log2_scale(sx); }
+    // 32 columns (without the row's scale), those that are not to count at -infinity
+    __device__ __forceinline__ void add(const float (&f)[32]) {
+        const float m_new = fmaxf(m, tc::max_of(f) * a);
+        const uint64_t a2 = ptx::pack_f32x2(a, a), nm2 = ptx::pack_f32x2(-m_new, -m_new);
+        uint64_t sum2 = ptx::pack_f32x2(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float x0, x1;
+            ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(f[2 * i], f[2 * i + 1]), a2, nm2), x0, x1);
+            sum2 = ptx::add_f32x2(sum2, ptx::pack_f32x2(ptx::ex2_approx(x0), ptx::ex2_approx(x1)));
         }
-        for (int off = 8; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-        for (int b = 0; b < 4; ++b) l += exp2f(z[b] - m);
-        for (int off = 8; off > 0; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
-        if (r < h.T && (threadIdx.x & 15) == 0) {
-            part_m[static_cast<long long>(blockIdx.x) * h.T + r] = m;
-            part_l[static_cast<long long>(blockIdx.x) * h.T + r] = l;
-        }
+        float s0, s1;
+        ptx::unpack_f32x2(sum2, s0, s1);
+        l = fmaf(l, ptx::ex2_approx(m - m_new), s0 + s1);
+        m = m_new;
     }
-}
+};
 
-// The parts of each row in order, and what follows from them; z_label is read for rows with a label only.
+struct EpiCe {
+    struct Params {
+        const float* sx;           // [T]
+        const float* sw;           // [V]
+        const long long* labels;   // [T]
+        float* part_m;             // [2 n_groups][part_stride]
+        float* part_l;
+        float* z_label;            // [T], in units of log2
+        long long part_stride;
+        int T, V;
+    };
+    struct State {
+        RowSums r;
+        int y, row;
+    };
+    __device__ static __forceinline__ void begin_item(const Params& p, State& s, int m_tile, int row_in_tile) {
+        s.row = m_tile * tc::BM + row_in_tile;
+        s.y = -1;
+        float sx = 0.f;
+        if (s.row < p.T) {
+            sx = p.sx[s.row];
+            const long long y = p.labels[s.row];
+            if (y >= 0 && y < p.V) s.y = static_cast<int>(y);
+        }
+        s.r.clear(sx);
+    }
+    __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage1&) {
+        const int col0 = n_tile * tc::BN;
+        const int ncols = min(tc::BN, p.V - col0);
+        walk_half(taddr, ncols, [&](int c, uint32_t (&v)[32]) {
+            float w[32], f[32];
+            const int live = ncols - c * 32;
+            values_at(p.sw + col0 + c * 32, live, w);
+            scaled(v, w, f);
+            if (live < 32) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (i >= live) f[i] = -INFINITY;
+            }
+            const int rel = s.y - (col0 + c * 32);
+            if (rel >= 0 && rel < 32) {
+                float zy = 0.f;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (i == rel) { zy = f[i]; f[i] = -INFINITY; }
+                p.z_label[s.row] = zy * s.r.a;
+            }
+            s.r.add(f);
+        });
+    }
+    __device__ static __forceinline__ int out_rows(const Params&) { return 0; }
+    __device__ static __forceinline__ void end_item(const Params& p, const State& s, int group) {
+        if (s.row >= p.T) return;
+        const long long at = (2 * group + static_cast<int>((threadIdx.x - 64) >> 7)) * p.part_stride + s.row;
+        p.part_m[at] = s.r.m;
+        p.part_l[at] = s.r.l;
+    }
+};
+
+// The parts of each row and what follows from them; z_label is read for rows with a label only.  32 rows per CTA, the parts dealt to its warps
+// and joined in order.
+constexpr int MERGE_ROWS = 32;
 __global__ void __launch_bounds__(THREADS) merge_kernel(const float* part_m, const float* part_l, const float* z_label, int S, long long stride, int T, int V,
                                                         const long long* labels, const unsigned char* valid, float* nll, float* lse) {
-    const int r = blockIdx.x * THREADS + threadIdx.x;
-    if (r >= T) return;
+    __shared__ float s_m[THREADS / 32][MERGE_ROWS], s_l[THREADS / 32][MERGE_ROWS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int r = blockIdx.x * MERGE_ROWS + lane;
+    float m = LOW2, l = 0.f;
+    if (r < T) {
+#pragma unroll 4
+        for (int s = warp; s < S; s += THREADS / 32) {
+            const float pm = part_m[s * stride + r], pl = part_l[s * stride + r], m_new = fmaxf(m, pm);
+            l = fmaf(l, exp2f(m - m_new), pl * exp2f(pm - m_new));
+            m = m_new;
+        }
+    }
+    s_m[warp][lane] = m;
+    s_l[warp][lane] = l;
+    __syncthreads();
+    if (warp != 0 || r >= T) return;
     if (valid != nullptr && valid[r] == 0) {
         nll[r] = lse[r] = 0.f;
         return;
     }
-    float m = LOW2;
-    for (int s = 0; s < S; ++s) m = fmaxf(m, part_m[s * stride + r]);
-    float l = 0.f;
-    for (int s = 0; s < S; ++s) l = fmaf(part_l[s * stride + r], exp2f(part_m[s * stride + r] - m), l);
+#pragma unroll
+    for (int i = 1; i < THREADS / 32; ++i) m = fmaxf(m, s_m[i][lane]);
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; ++i) l = fmaf(s_l[i][lane], exp2f(s_m[i][lane] - m), l);
     constexpr double LN2 = 0.69314718055994530942;
     const double others = LN2 * (static_cast<double>(m) + log2(static_cast<double>(l)));
     const long long y = labels[r];
@@ -207,60 +352,130 @@ __device__ __forceinline__ RowGrad row_grad(int r, int T, int V, const long long
     return a;
 }
 
-// exp(z_v - o) sw_v 2^k, and -sw_y 2^k at the label, as fp16
-__global__ void __launch_bounds__(THREADS) ce_dz_kernel(const Head h, const long long* labels, const unsigned char* valid, const float* nll, const float* lse,
-                                                        const float* g, const int* most, __half* dz, long long ldz, float* factor) {
-    const int c0 = blockIdx.x * TILE, r0 = blockIdx.y * TILE;
-    int acc[4][4] = {};
-    tile_sums(h, r0, c0, acc);
-    float up, down;
-    fit_half(*most, up, down);
-    for (int a = 0; a < 4; ++a) {
-        const int r = r0 + (threadIdx.x >> 4) * 4 + a;
-        if (r >= h.T) continue;
-        const RowGrad q = row_grad(r, h.T, h.V, labels, valid, nll, lse, g);
-        const float s = log2_scale(h.sx[r]);
-        if (blockIdx.x == 0 && (threadIdx.x & 15) == 0) factor[r] = q.factor * down;
-        for (int b = 0; b < 4; ++b) {
-            const int c = c0 + (threadIdx.x & 15) * 4 + b;
-            if (c >= h.V) continue;
-            float x = 0.f;
-            if (q.on) x = c == q.y ? -h.sw[c] * up : exp2f(fmaf(__int2float_rn(acc[a][b]) * h.sw[c], s, -q.others2)) * (h.sw[c] * up);
-            dz[r * ldz + c] = __float2half(x);
+// exp(z_v - o) sw_v 2^k, and -sw_y 2^k at the label, as fp16: the rest of the row's factor is applied behind the contraction.  Half precision's 11 bits
+// keep the rounding of a row's few large terms below that of the bf16 result (bf16 terms: rows of dX off by up to 2^-8 more).
+struct EpiDz {
+    struct Params {
+        const float* sx;
+        const float* sw;
+        const long long* labels;
+        const unsigned char* valid;
+        const float* nll;
+        const float* lse;
+        const float* g;            // [T] upstream
+        const int* most;           // bits of the largest scale
+        float* factor;             // [T] out: g (1 - p_y) 2^-k
+        int T, V;
+    };
+    struct State {
+        RowGrad q;
+        float a, up, down;
+        int row;
+    };
+    __device__ static __forceinline__ void begin_item(const Params& p, State& s, int m_tile, int row_in_tile) {
+        s.row = m_tile * tc::BM + row_in_tile;
+        s.q = row_grad(s.row, p.T, p.V, p.labels, p.valid, p.nll, p.lse, p.g);
+        s.a = log2_scale(s.row < p.T ? p.sx[s.row] : 0.f);
+        fit_half(*p.most, s.up, s.down);
+    }
+    __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage1& o) {
+        const int col0 = n_tile * tc::BN;
+        const int ncols = min(tc::BN, p.V - col0);
+        const uint64_t a2 = ptx::pack_f32x2(s.a, s.a), no2 = ptx::pack_f32x2(-s.q.others2, -s.q.others2), up2 = ptx::pack_f32x2(s.up, s.up);
+        walk_half(taddr, ncols, [&](int c, uint32_t (&v)[32]) {
+            if ((c & 1) == 0) o.begin();
+            float w[32], f[32];
+            values_at(p.sw + col0 + c * 32, ncols - c * 32, w);
+            scaled(v, w, f);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint64_t w2 = ptx::mul_f32x2(ptx::pack_f32x2(w[2 * i], w[2 * i + 1]), up2);
+                float x0, x1;
+                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(f[2 * i], f[2 * i + 1]), a2, no2), x0, x1);
+                ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(ptx::ex2_approx(x0), ptx::ex2_approx(x1)), w2), f[2 * i], f[2 * i + 1]);
+                ptx::unpack_f32x2(w2, w[2 * i], w[2 * i + 1]);
+            }
+            const int rel = s.q.y - (col0 + c * 32);
+            if (rel >= 0 && rel < 32) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (i == rel) f[i] = -w[i];
+            }
+            if (!s.q.on) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) f[i] = 0.f;
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                o.put((c & 1) * 4 + q, ptx::pack_f16x2_sat(f[q * 8 + 0], f[q * 8 + 1]), ptx::pack_f16x2_sat(f[q * 8 + 2], f[q * 8 + 3]),
+                      ptx::pack_f16x2_sat(f[q * 8 + 4], f[q * 8 + 5]), ptx::pack_f16x2_sat(f[q * 8 + 6], f[q * 8 + 7]));
+            if ((c & 1) != 0 || (c + 1) * 32 >= ncols) o.flush(col0 + (c >> 1) * 64);
+        });
+    }
+    __device__ static __forceinline__ int out_rows(const Params& p) { return p.T; }
+    __device__ static __forceinline__ void end_item(const Params& p, const State& s, int group) {
+        if (group == 0 && threadIdx.x < 192 && s.row < p.T) p.factor[s.row] = s.q.factor * s.down;
+    }
+};
+
+// The head as the 16-bit operand of the gradient's contraction: its integers in fp16 (exact), or scale * integer in bf16.
+template <bool SCALED>
+__global__ void __launch_bounds__(THREADS) widen_kernel(const int8_t* wq, long long ldw, const float* sw, long long units, int per_row, int d, uint16_t* out) {
+    for (long long u = blockIdx.x * static_cast<long long>(THREADS) + threadIdx.x; u < units; u += static_cast<long long>(gridDim.x) * THREADS) {
+        const long long v = u / per_row;
+        const int i = static_cast<int>(u - v * per_row) * 8;              // 8 integers: d is a multiple of 8
+        const uint2 x = *reinterpret_cast<const uint2*>(wq + v * ldw + i);
+        uint32_t r[4];
+        const uint32_t b[2] = {x.x ^ 0x80808080u, x.y ^ 0x80808080u};    // 0 .. 255
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t pair = __byte_perm(b[j >> 1], 0x64646464u, (j & 1) ? 0x4342 : 0x4140);      // fp16 1024 + byte
+            __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&pair), __half2half2(__ushort_as_half(0x6480)));   // - 1152
+            if (SCALED) {
+                const float2 f = __half22float2(h);
+                const float s = sw[v];
+                r[j] = ptx::pack_bf16x2(f.x * s, f.y * s);
+            } else {
+                r[j] = *reinterpret_cast<const uint32_t*>(&h);
+            }
         }
+        *reinterpret_cast<uint4*>(out + v * d + i) = make_uint4(r[0], r[1], r[2], r[3]);
     }
 }
 
-// dX[r, i] = factor[r] sum_v A[r, v] wq[v, i]: A the fp16 terms above, or dY sw
-__global__ void __launch_bounds__(THREADS) dx_kernel(const __half* dz, const __nv_bfloat16* dY, long long ldA, const float* factor, const Head h,
-                                                     __nv_bfloat16* dX, long long ldX) {
-    __shared__ float sa[TILE][17], sb[16][TILE + 1];
-    const int c0 = blockIdx.x * TILE, r0 = blockIdx.y * TILE;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4] = {};
-    for (int k0 = 0; k0 < h.V; k0 += 16) {
-        for (int i = threadIdx.x; i < TILE * 16; i += THREADS) {
-            const int row = i >> 4, k = k0 + (i & 15);
-            float a = 0.f;
-            if (r0 + row < h.T && k < h.V) a = dz ? __half2float(dz[(r0 + row) * ldA + k]) : __bfloat162float(dY[(r0 + row) * ldA + k]) * h.sw[k];
-            sa[row][i & 15] = a;
-            const int kb = k0 + i / TILE, c = c0 + i % TILE;
-            sb[i / TILE][i % TILE] = kb < h.V && c < h.d ? static_cast<float>(h.wq[kb * h.ldw + c]) : 0.f;
+// Parts of a contraction, added in order; the row's factor; one rounding.
+__global__ void __launch_bounds__(THREADS) add_parts_kernel(const float* part, int g, long long stride, int d, const float* factor, __nv_bfloat16* out, long long ld) {
+    const long long r = blockIdx.x;
+    const float f = factor ? factor[r] : 1.f;
+    for (int i = threadIdx.x * 4; i < d; i += THREADS * 4) {
+        float4 s = *reinterpret_cast<const float4*>(part + r * d + i);
+        for (int k = 1; k < g; ++k) {
+            const float4 x = *reinterpret_cast<const float4*>(part + k * stride + r * d + i);
+            s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
         }
-        __syncthreads();
-        for (int k = 0; k < 16; ++k)
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-#pragma unroll
-                for (int b = 0; b < 4; ++b) acc[a][b] = fmaf(sa[ty * 4 + a][k], sb[k][tx * 4 + b], acc[a][b]);
-        __syncthreads();
+        *reinterpret_cast<uint2*>(out + r * ld + i) = make_uint2(ptx::pack_bf16x2(s.x * f, s.y * f), ptx::pack_bf16x2(s.z * f, s.w * f));
     }
-    for (int a = 0; a < 4; ++a)
-        for (int b = 0; b < 4; ++b) {
-            const int r = r0 + ty * 4 + a, c = c0 + tx * 4 + b;
-            if (r < h.T && c < h.d) dX[r * ldX + c] = __float2bfloat16(acc[a][b] * (factor ? factor[r] : 1.f));
-        }
 }
+
+// the plain output of a contraction of fp16 operands
+struct EpiOutHalf : tc::EpiOutT<false> {};
 
 }  // namespace i8
+
+namespace tc {
+template <bool F32>
+struct OperandOf<i8::EpiLinear<F32>> { static constexpr Operand value = Operand::I8; };
+template <>
+struct OperandOf<i8::EpiCe> { static constexpr Operand value = Operand::I8; };
+template <>
+struct OperandOf<i8::EpiDz> { static constexpr Operand value = Operand::I8; };
+template <>
+struct OperandOf<i8::EpiOutHalf> { static constexpr Operand value = Operand::F16; };
+template <bool F32>
+struct EpiSets<i8::EpiLinear<F32>> { static constexpr int value = 2; };
+template <>
+struct EpiSets<i8::EpiCe> { static constexpr int value = 2; };
+template <>
+struct EpiSets<i8::EpiDz> { static constexpr int value = 2; };
+}  // namespace tc
 }  // namespace cat

@@ -31,23 +31,24 @@ struct I8Plan {
     long long ldq;         // row pitch of the tokens' integers
     long long Ts;          // rows per slab
     long long ldz;
-    int S;                 // parts of the vocabulary
-    size_t off_q, off_s, off_m, off_l, off_zy, off_factor, off_z, total;
+    int S;                 // splits of the vocabulary
+    size_t off_q, off_s, off_m, off_l, off_zy, off_factor, off_w16, off_part, off_z, total;
 };
 
 I8Plan plan_i8(const cat_i8_shape* s, int pass) {
     I8Plan p;
     memset(&p, 0, sizeof(p));
     p.ldq = cdiv(s->d, 16) * 16;
-    p.S = static_cast<int>(cdiv(s->V, i8::TILE));
+    p.Ts = s->T;
     size_t off = kHeaderBytes;
     if (pass != kI8LinearBwd) {
         p.off_q = off; off = align256(off + static_cast<size_t>(s->T) * p.ldq);
         p.off_s = off; off = align256(off + sizeof(float) * s->T);
     }
     if (pass == kI8Ce) {
-        p.off_m = off; off = align256(off + sizeof(float) * p.S * s->T);
-        p.off_l = off; off = align256(off + sizeof(float) * p.S * s->T);
+        p.S = fwd_splits(s->T, s->V);
+        p.off_m = off; off = align256(off + sizeof(float) * 2 * p.S * s->T);
+        p.off_l = off; off = align256(off + sizeof(float) * 2 * p.S * s->T);
         p.off_zy = off; off = align256(off + sizeof(float) * s->T);
     }
     if (pass == kI8CeBwd) {
@@ -55,9 +56,14 @@ I8Plan plan_i8(const cat_i8_shape* s, int pass) {
         const long long mib = s->slab_mib > 0 ? s->slab_mib : kDefaultFusedSlabMiB;
         long long cap = (mib << 20) / (p.ldz * 2) / tile_m() * tile_m();
         if (cap < tile_m()) cap = tile_m();
-        p.Ts = cap < s->T ? cap : s->T;
+        if (cap < s->T) p.Ts = cdiv(cdiv(s->T, cdiv(s->T, cap)), tile_m()) * tile_m();       // slabs of even height
         p.off_factor = off; off = align256(off + sizeof(float) * s->T);
         p.off_z = off; off = align256(off + 2 * static_cast<size_t>(p.Ts) * p.ldz);
+    }
+    if (pass == kI8LinearBwd || pass == kI8CeBwd) {
+        p.off_w16 = off; off = align256(off + 2 * static_cast<size_t>(s->V) * s->d);
+        const size_t full = dh_part_bytes(p.Ts, s->d, s->V), rest = dh_part_bytes(s->T - (cdiv(s->T, p.Ts) - 1) * p.Ts, s->d, s->V);
+        p.off_part = off; off += full > rest ? full : rest;
     }
     p.total = off;
     return p;
@@ -78,7 +84,7 @@ int quantize(const void* X, int dtype, long long rows, long long d, long long ld
 // What every pass begins with: the checks that are alike, the header cleared, the tokens as integers.
 int begin_i8(const cat_i8_shape* s, int pass, const I8Plan& plan, const void* X, const int8_t* Wq, const float* w_scale, void* workspace,
              size_t workspace_bytes, int* sm_count, i8::Head* h, cudaStream_t st) {
-    if (misaligned(X, s->x_dtype == CAT_BF16 ? 2 : 4) || misaligned(Wq, 16) || misaligned(w_scale, 4)) return CAT_ERR_ALIGN;
+    if (misaligned(X, s->x_dtype == CAT_BF16 ? 2 : 4) || misaligned(Wq, 16) || misaligned(w_scale, 16)) return CAT_ERR_ALIGN;
     if (!workspace || misaligned(workspace, 256) || workspace_bytes < plan.total) return CAT_ERR_WORKSPACE;
     const int dc = check_device(sm_count);
     if (dc != CAT_OK) return dc;
@@ -93,7 +99,61 @@ int begin_i8(const cat_i8_shape* s, int pass, const I8Plan& plan, const void* X,
                     reinterpret_cast<float*>(ws + plan.off_s), st);
 }
 
-dim3 i8_grid(long long rows, long long cols) { return dim3(static_cast<unsigned>(cdiv(cols, i8::TILE)), static_cast<unsigned>(cdiv(rows, i8::TILE))); }
+// K-major 8-bit operand [rows][d] with row pitch ld bytes: boxes of 128 bytes x box_rows.
+int tmap_i8(CUtensorMap* m, const void* base, long long rows, long long d, long long ld, int box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return CAT_ERR_CUDA;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(ld)};
+    const cuuint32_t box[2] = {2 * tc::BK, static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
+    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? CAT_OK : CAT_ERR_CUDA;
+}
+
+// The product of h's tokens and head through epilogue Epi: n_groups runs of vocabulary tiles per row tile (0: every tile by itself).
+template <class Epi>
+int launch_i8(const i8::Head& h, const typename Epi::Params& ep, int n_groups, int* status, int sm_count, cudaStream_t st, const CUtensorMap* out) {
+    CUtensorMap tmX, tmW;
+    if (tmap_i8(&tmX, h.xq, h.T, h.d, h.ldq, tc::BM) != CAT_OK || tmap_i8(&tmW, h.wq, h.V, h.d, h.ldw, tc::BN / cta_group()) != CAT_OK) return CAT_ERR_CUDA;
+    const long long slices = cdiv(h.d, 2);             // a 64-wide slice of 16-bit operands is 128 integers
+    return launch_tc<0, 0, Epi>(tmX, tmW, make_sched(h.T, h.V, slices, n_groups, band_tiles(slices), 0), ep, status, sm_count, st, out);
+}
+
+// dX[r, :] = factor[r] sum_v A[r, v] W16[v, :], A [rows, V] and W16 [V, d] of the type Epi multiplies; the vocabulary in parts for few rows.
+template <class Epi>
+int launch_dx(const void* A, long long ldA, const uint16_t* w16, long long rows, long long d, long long V, const float* factor, __nv_bfloat16* dX, long long lddX,
+              float* part, int* status, int sm_count, cudaStream_t st) {
+    CUtensorMap tmA, tmW, tmO;
+    if (tmap_a(&tmA, A, rows, V, ldA) != CAT_OK || tmap_mn_major(&tmW, w16, V, d, d) != CAT_OK) return CAT_ERR_CUDA;
+    const int g = dh_parts(rows, d, V);
+    tc::Sched sched = make_sched(rows, d, V, 0, 1, 1);
+    typename Epi::Params ep;
+    memset(&ep, 0, sizeof(ep));
+    ep.N = static_cast<int>(d);
+    if (g == 1) {
+        ep.row_scale = factor; ep.M = static_cast<int>(rows); ep.out_bf16 = dX; ep.ld_out = lddX; ep.staged = 2;
+        if (tmap_out(&tmO, dX, rows, d, lddX) != CAT_OK) return CAT_ERR_CUDA;
+        return launch_tc<0, 1, Epi>(tmA, tmW, sched, ep, status, sm_count, st, &tmO);
+    }
+    const long long padded = sched.m_real * tile_m();
+    sched.k_splits = g;
+    sched.num_m_tiles = sched.m_real * g;
+    sched.n_items = sched.num_m_tiles * sched.n_groups;
+    ep.M = static_cast<int>(padded * g); ep.out_f32 = part; ep.ld_out = d; ep.staged = 1;
+    if (tmap_out_f32(&tmO, part, ep.M, d, d) != CAT_OK) return CAT_ERR_CUDA;
+    const int rc = launch_tc<0, 1, Epi>(tmA, tmW, sched, ep, status, sm_count, st, &tmO);
+    if (rc != CAT_OK) return rc;
+    i8::add_parts_kernel<<<static_cast<unsigned>(rows), i8::THREADS, 0, st>>>(part, g, padded * d, static_cast<int>(d), factor, dX, lddX);
+    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+}
+
+template <bool SCALED>
+int launch_widen(const i8::Head& h, uint16_t* w16, int sm_count, cudaStream_t st) {
+    const int per_row = h.d / 8;
+    i8::widen_kernel<SCALED><<<static_cast<unsigned>(8 * sm_count), i8::THREADS, 0, st>>>(h.wq, h.ldw, h.sw, static_cast<long long>(h.V) * per_row, per_row,
+                                                                                          h.d, w16);
+    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+}
 
 }  // namespace
 
@@ -121,17 +181,22 @@ int cat_i8_linear_fwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq
     if (!shape || !X || !Wq || !w_scale || !Y) return CAT_ERR_NULL;
     const int sc = check_i8(shape, kI8Linear);
     if (sc != CAT_OK) return sc;
-    if (misaligned(Y, 16) || misaligned(bias, 4)) return CAT_ERR_ALIGN;
+    if (misaligned(Y, 16) || misaligned(bias, 16)) return CAT_ERR_ALIGN;
     const I8Plan plan = plan_i8(shape, kI8Linear);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     int sm_count = 0;
     i8::Head h;
     const int rc = begin_i8(shape, kI8Linear, plan, X, Wq, w_scale, workspace, workspace_bytes, &sm_count, &h, st);
     if (rc != CAT_OK) return rc;
-    const bool f32 = shape->y_dtype == CAT_F32;
-    i8::linear_kernel<<<i8_grid(h.T, h.V), i8::THREADS, 0, st>>>(h, bias, f32 ? static_cast<float*>(Y) : nullptr,
-                                                                 f32 ? nullptr : static_cast<__nv_bfloat16*>(Y), shape->ldY);
-    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+    int* status = static_cast<int*>(workspace);
+    const long long whole = h.V >= 32 ? h.V / 32 * 32 : 8;        // nothing is sent where there is no whole chunk
+    CUtensorMap tmY;
+    if (shape->y_dtype == CAT_F32) {
+        if (tmap_out_f32(&tmY, Y, h.T, whole, shape->ldY) != CAT_OK) return CAT_ERR_CUDA;
+        return launch_i8<i8::EpiLinear<true>>(h, {h.sx, h.sw, bias, Y, shape->ldY, h.T, h.V}, 0, status, sm_count, st, &tmY);
+    }
+    if (tmap_out(&tmY, Y, h.T, whole, shape->ldY) != CAT_OK) return CAT_ERR_CUDA;
+    return launch_i8<i8::EpiLinear<false>>(h, {h.sx, h.sw, bias, Y, shape->ldY, h.T, h.V}, 0, status, sm_count, st, &tmY);
 }
 
 int cat_i8_linear_bwd(const cat_i8_shape* shape, const void* dY, const int8_t* Wq, const float* w_scale, void* dX,
@@ -146,9 +211,12 @@ int cat_i8_linear_bwd(const cat_i8_shape* shape, const void* dY, const int8_t* W
     i8::Head h;
     const int rc = begin_i8(shape, kI8LinearBwd, plan, nullptr, Wq, w_scale, workspace, workspace_bytes, &sm_count, &h, st);
     if (rc != CAT_OK) return rc;
-    i8::dx_kernel<<<i8_grid(h.T, h.d), i8::THREADS, 0, st>>>(nullptr, static_cast<const __nv_bfloat16*>(dY), shape->ldY, nullptr, h,
-                                                             static_cast<__nv_bfloat16*>(dX), shape->lddX);
-    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    uint16_t* w16 = reinterpret_cast<uint16_t*>(ws + plan.off_w16);
+    const int wc = launch_widen<true>(h, w16, sm_count, st);
+    if (wc != CAT_OK) return wc;
+    return launch_dx<tc::EpiOut>(dY, shape->ldY, w16, shape->T, shape->d, shape->V, nullptr, static_cast<__nv_bfloat16*>(dX), shape->lddX,
+                                 reinterpret_cast<float*>(ws + plan.off_part), reinterpret_cast<int*>(ws), sm_count, st);
 }
 
 int cat_i8_ce_fwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, const float* w_scale, const int64_t* labels,
@@ -167,8 +235,12 @@ int cat_i8_ce_fwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, co
     float *part_m = reinterpret_cast<float*>(ws + plan.off_m), *part_l = reinterpret_cast<float*>(ws + plan.off_l),
           *z_label = reinterpret_cast<float*>(ws + plan.off_zy);
     const long long* y = reinterpret_cast<const long long*>(labels);
-    i8::ce_kernel<<<i8_grid(h.T, h.V), i8::THREADS, 0, st>>>(h, y, part_m, part_l, z_label);
-    i8::merge_kernel<<<static_cast<unsigned>(cdiv(h.T, i8::THREADS)), i8::THREADS, 0, st>>>(part_m, part_l, z_label, plan.S, h.T, h.T, h.V, y, valid, nll, lse);
+    i8::EpiCe::Params ep;
+    ep.sx = h.sx; ep.sw = h.sw; ep.labels = y; ep.part_m = part_m; ep.part_l = part_l; ep.z_label = z_label; ep.part_stride = h.T; ep.T = h.T; ep.V = h.V;
+    const int gc = launch_i8<i8::EpiCe>(h, ep, plan.S, reinterpret_cast<int*>(ws), sm_count, st, nullptr);
+    if (gc != CAT_OK) return gc;
+    i8::merge_kernel<<<static_cast<unsigned>(cdiv(h.T, i8::MERGE_ROWS)), i8::THREADS, 0, st>>>(part_m, part_l, z_label, 2 * plan.S, h.T, h.T, h.V, y, valid,
+                                                                                               nll, lse);
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
 
@@ -190,17 +262,27 @@ int cat_i8_ce_bwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, co
     float* factor = reinterpret_cast<float*>(ws + plan.off_factor);
     __half* dz = reinterpret_cast<__half*>(ws + plan.off_z);
     const long long* y = reinterpret_cast<const long long*>(labels);
+    uint16_t* w16 = reinterpret_cast<uint16_t*>(ws + plan.off_w16);
+    float* part = reinterpret_cast<float*>(ws + plan.off_part);
     i8::largest_scale_kernel<<<static_cast<unsigned>(cdiv(h.V, 8 * i8::THREADS)), i8::THREADS, 0, st>>>(w_scale, h.V, most);
+    const int wc = launch_widen<false>(h, w16, sm_count, st);
+    if (wc != CAT_OK) return wc;
     for (long long r0 = 0; r0 < shape->T; r0 += plan.Ts) {
         i8::Head hs = h;
         hs.T = static_cast<int>(shape->T - r0 < plan.Ts ? shape->T - r0 : plan.Ts);
         hs.xq += r0 * plan.ldq; hs.sx += r0;
-        i8::ce_dz_kernel<<<i8_grid(hs.T, h.V), i8::THREADS, 0, st>>>(hs, y + r0, valid ? valid + r0 : nullptr, nll + r0, lse + r0, grad_nll + r0, most,
-                                                                     dz, plan.ldz, factor + r0);
-        i8::dx_kernel<<<i8_grid(hs.T, h.d), i8::THREADS, 0, st>>>(dz, nullptr, plan.ldz, factor + r0, hs,
-                                                                  static_cast<__nv_bfloat16*>(dX) + r0 * shape->lddX, shape->lddX);
+        CUtensorMap tmZ;
+        if (tmap_out(&tmZ, dz, hs.T, hs.V, plan.ldz) != CAT_OK) return CAT_ERR_CUDA;
+        i8::EpiDz::Params ep;
+        ep.sx = hs.sx; ep.sw = hs.sw; ep.labels = y + r0; ep.valid = valid ? valid + r0 : nullptr; ep.nll = nll + r0; ep.lse = lse + r0; ep.g = grad_nll + r0;
+        ep.most = most; ep.factor = factor + r0; ep.T = hs.T; ep.V = hs.V;
+        int gc = launch_i8<i8::EpiDz>(hs, ep, fwd_splits(hs.T, hs.V), reinterpret_cast<int*>(ws), sm_count, st, &tmZ);
+        if (gc != CAT_OK) return gc;
+        gc = launch_dx<i8::EpiOutHalf>(dz, plan.ldz, w16, hs.T, hs.d, hs.V, factor + r0, static_cast<__nv_bfloat16*>(dX) + r0 * shape->lddX, shape->lddX, part,
+                                       reinterpret_cast<int*>(ws), sm_count, st);
+        if (gc != CAT_OK) return gc;
     }
-    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+    return CAT_OK;
 }
 
 }  // extern "C"

@@ -125,8 +125,9 @@ __device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, vola
 // rows / columns outside the tensor.  Two tiles per warp alternate; a tile is reused once the
 // store issued from it has read it (cp.async.bulk.wait_group.read).
 constexpr int OUT_TILE_BYTES = 32 * 128;
-constexpr int OUT_STAGE_BYTES = 4 * 2 * OUT_TILE_BYTES;      // four epilogue warps, two tiles each
-struct OutStage {
+constexpr int OUT_STAGE_BYTES = 4 * 2 * OUT_TILE_BYTES;      // four epilogue warps, two tiles each, or eight with one
+template <int TILES>
+struct OutStageOf {
     const CUtensorMap* tm;
     uint32_t buf;      // shared-memory address of this warp's two tiles
     int row0;          // tensor row of this warp's lane 0
@@ -134,7 +135,7 @@ struct OutStage {
     int lane;
     int sel;
     __device__ __forceinline__ void begin() {
-        if (lane == 0) ptx::tma_store_wait_read<1>();     // the store before last (same tile) has read it
+        if (lane == 0) ptx::tma_store_wait_read<TILES - 1>();     // the last store from the same tile has read it
         __syncwarp();
     }
     // 16-byte piece `j` (0..7) of this lane's 128-byte row
@@ -149,7 +150,7 @@ struct OutStage {
             else ptx::tma_store_2d(tm, buf + sel * OUT_TILE_BYTES, x, row0);
             ptx::tma_store_commit();
         }
-        sel ^= 1;
+        if (TILES == 2) sel ^= 1;
     }
     // Both tiles at once, for rows that leave as two terms: the same columns of rows row0 and row0 + lo.
     __device__ __forceinline__ void begin_both() {
@@ -173,6 +174,7 @@ struct OutStage {
         __syncwarp();
     }
 };
+using OutStage = OutStageOf<2>;
 
 // ------------------------------------------------------------------------------------------
 // Epilogues.  Each epilogue thread owns output row (m_tile*BM + row_in_tile) and walks the
@@ -594,6 +596,17 @@ struct EpiOutT {
 };
 using EpiOut = EpiOutT<false>;
 
+// What an epilogue's GEMM multiplies.  I8: K-major 8-bit integers, int32 accumulators; a 128-byte slice of the contraction is 128 of them.
+enum class Operand { BF16, F16, I8 };
+template <class Epi>
+struct OperandOf { static constexpr Operand value = Operand::BF16; };
+
+// Sets of four epilogue warps: set i works on columns [i BN / sets, (i + 1) BN / sets) of each tile, one output row per thread.
+template <class Epi>
+struct EpiSets { static constexpr int value = 1; };
+template <class Epi>
+constexpr int THREADS_OF = NUM_THREADS + 128 * (EpiSets<Epi>::value - 1);
+
 // Whether a kernel behind the GEMM may run beside it (see lp::norm_kernel).
 template <class Epi>
 struct LetsNextStart { static constexpr bool value = false; };
@@ -642,7 +655,7 @@ struct Geo {
 
 // Set-up shared by every CTA of the kernels below: barriers, the abort flag, TMEM (warp 1 owns it).
 // On return the barriers exist in both CTAs of a pair and ctl.tmem_base is valid.
-template <int CG>
+template <int CG, int THREADS = NUM_THREADS>
 __device__ __forceinline__ void cta_begin(Ctl& ctl, int n_stages, int warp) {
     if (threadIdx.x == 0) {
         for (int i = 0; i < n_stages; ++i) {
@@ -651,7 +664,7 @@ __device__ __forceinline__ void cta_begin(Ctl& ctl, int n_stages, int warp) {
         }
         for (int i = 0; i < 2; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctl.tfull[i]), 1);
-            ptx::mbar_init(ptx::smem_u32(&ctl.tempty[i]), CG == 1 ? NUM_THREADS - 64 : 2 * (NUM_THREADS - 64) / 32);
+            ptx::mbar_init(ptx::smem_u32(&ctl.tempty[i]), CG == 1 ? THREADS - 64 : 2 * (THREADS - 64) / 32);
         }
         ptx::mbar_init(ptx::smem_u32(&ctl.drain), 1);
         ctl.abort = 0;
@@ -687,10 +700,13 @@ __device__ __forceinline__ void cta_end(int warp, uint32_t tmem) {
 }
 
 template <int A_MN, int B_MN, class Epi, int CG>
-__global__ void __launch_bounds__(NUM_THREADS, 1)
+__global__ void __launch_bounds__(THREADS_OF<Epi>, 1)
 gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
             const __grid_constant__ CUtensorMap tmOut, const Sched sched, const typename Epi::Params ep, int* status) {
     using G = Geo<CG>;
+    constexpr Operand OP = OperandOf<Epi>::value;
+    constexpr int SETS = EpiSets<Epi>::value;
+    static_assert(OP != Operand::I8 || (A_MN == 0 && B_MN == 0), "8-bit operands are K-major");
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ Ctl ctl;
     const uint32_t ring = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -709,7 +725,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
         // pairs are numbered die by die where the device's map is known (neighbouring workers share operand tiles)
         if (claimed && leader) ctl.worker = static_cast<uint32_t>(die::claim_worker(sched.claims, sched.serial, worker, n_workers));
     }
-    cta_begin<CG>(ctl, G::STAGES, warp);
+    cta_begin<CG, THREADS_OF<Epi>>(ctl, G::STAGES, warp);
     if constexpr (LetsNextStart<Epi>::value) ptx::launch_dependents();
     if (claimed) worker = static_cast<int>(leader ? ctl.worker : ptx::ld_shared_cluster_u32(ptx::mapa_shared(ptx::smem_u32(&ctl.worker), 0)));
     const uint32_t tmem = ctl.tmem_base;
@@ -744,7 +760,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
                         for (int h = 0; h < G::KS; ++h) {
                             const uint32_t a_dst = ring + stage * G::STAGE_BYTES + h * A_STAGE_BYTES;
                             const uint32_t b_dst = ring + stage * G::STAGE_BYTES + G::A_BYTES + h * G::B_SLICE_BYTES;
-                            const int k0 = (kb * G::KS + h) * BK;
+                            const int k0 = (kb * G::KS + h) * (OP == Operand::I8 ? 2 * BK : BK);
                             if (A_MN) {
 #pragma unroll
                                 for (int j = 0; j < BM / 64; ++j) load_box<CG>(a_dst + j * MN_ATOM_BYTES, &tmA, m0 + j * 64, k0, full_sig);
@@ -782,7 +798,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer (leader CTA only)
         if (lane == 0 && leader) {
-            constexpr uint32_t idesc = ptx::idesc_bf16_f32(BM * CG, BN, A_MN, B_MN);
+            constexpr uint32_t idesc = OP == Operand::I8 ? ptx::idesc_i8_s32(BM * CG, BN)
+                                       : OP == Operand::F16 ? ptx::idesc_f16_f32(BM * CG, BN, A_MN, B_MN) : ptx::idesc_bf16_f32(BM * CG, BN, A_MN, B_MN);
             // The tensor pipe takes only a few MMAs ahead of the one it executes, so the instructions between
             // two issues are on its critical path: the shared-memory descriptors of stage 0 are built once and
             // those of the other stages and k-slices follow by adding to the (address >> 4) field.
@@ -817,8 +834,13 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
                             for (int j = 0; j < BK / 16; ++j) {
                                 const uint32_t accumulate = (h != 0 || j != 0 || kb != kb0) ? 1u : 0u;
                                 const uint64_t ad = adesc + h * A_SLICE_STEP + j * A_KSTEP, bd = bdesc + h * B_SLICE_STEP + j * B_KSTEP;
-                                if (CG == 1) ptx::umma_bf16(d_tmem, ad, bd, idesc, accumulate);
-                                else ptx::umma_bf16_pair(d_tmem, ad, bd, idesc, accumulate);
+                                if (OP == Operand::I8) {
+                                    if (CG == 1) ptx::umma_i8(d_tmem, ad, bd, idesc, accumulate);
+                                    else ptx::umma_i8_pair(d_tmem, ad, bd, idesc, accumulate);
+                                } else {
+                                    if (CG == 1) ptx::umma_bf16(d_tmem, ad, bd, idesc, accumulate);
+                                    else ptx::umma_bf16_pair(d_tmem, ad, bd, idesc, accumulate);
+                                }
                             }
                         }
                         // frees the stage (in both CTAs of a pair) once these MMAs have read it
@@ -854,9 +876,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
         uint32_t acc = 0, acc_phase = 0;
         bool ok = true;
         typename Epi::State st;
-        OutStage out;
+        OutStageOf<SETS == 1 ? 2 : 1> out;
         out.tm = &tmOut;
-        out.buf = ring + G::RING_BYTES + static_cast<uint32_t>(quarter) * 2 * OUT_TILE_BYTES;
+        out.buf = ring + G::RING_BYTES + static_cast<uint32_t>(SETS == 1 ? 2 * quarter : warp - 2) * OUT_TILE_BYTES;
         out.lane = lane;
         out.sel = 0;
         out.row0 = 0;
