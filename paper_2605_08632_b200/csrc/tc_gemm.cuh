@@ -145,10 +145,12 @@ struct OutStageOf {
     __device__ __forceinline__ void flush(int x, bool add = false) {
         ptx::fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0 && row0 < n_rows) {
-            if (add) ptx::tma_reduce_add_2d(tm, buf + sel * OUT_TILE_BYTES, x, row0);
-            else ptx::tma_store_2d(tm, buf + sel * OUT_TILE_BYTES, x, row0);
-            ptx::tma_store_commit();
+        if (lane == 0) {
+            if (row0 < n_rows) {
+                if (add) ptx::tma_reduce_add_2d(tm, buf + sel * OUT_TILE_BYTES, x, row0);
+                else ptx::tma_store_2d(tm, buf + sel * OUT_TILE_BYTES, x, row0);
+            }
+            ptx::tma_store_commit();      // a tile that is not sent is a group too: begin() counts groups to know that the buffer's last store has read it
         }
         if (TILES == 2) sel ^= 1;
     }
