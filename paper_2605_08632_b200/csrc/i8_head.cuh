@@ -91,26 +91,28 @@ __device__ __forceinline__ void walk_half(uint32_t taddr, int ncols, F&& body) {
     ptx::tmem_ld_wait();
 }
 
-// 32 neighbouring values, the same for all lanes; zeros past the live ones
-__device__ __forceinline__ void values_at(const float* p, int live, float (&w)[32]) {
-    if (live >= 32) {
+// The scales (or biases) of the 128 columns of a warp's half of a tile, four to a lane: column 32 j + lane.  They are fetched one tile ahead and handed
+// round by shuffles; loads of the same addresses by all lanes, chunk by chunk, waited for L2 every time (loss of 300 x 1024 x 151936 85 us).
+struct Columns {
+    float x[4];
+    __device__ __forceinline__ void load(const float* p, int n_tile, int V) {
+        const int col = n_tile * tc::BN + static_cast<int>((threadIdx.x - 64) >> 7) * 128 + static_cast<int>(threadIdx.x & 31);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float4 x = __ldg(reinterpret_cast<const float4*>(p) + i);
-            w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) w[i] = i < live ? __ldg(p + i) : 0.f;
+        for (int j = 0; j < 4; ++j) x[j] = col + 32 * j < V ? __ldg(p + col + 32 * j) : 0.f;
     }
-}
+    // this lane's value of chunk c
+    __device__ __forceinline__ float chunk(int c) const {
+        const int j = c & 3;
+        return j < 2 ? (j == 0 ? x[0] : x[1]) : (j == 2 ? x[2] : x[3]);
+    }
+};
 
-// integer sums times the channels' scales
-__device__ __forceinline__ void scaled(const uint32_t (&v)[32], const float (&w)[32], float (&f)[32]) {
+// integer sums times the channels' scales, `mine` the lane's
+__device__ __forceinline__ void scaled(const uint32_t (&v)[32], float mine, float (&f)[32]) {
 #pragma unroll
     for (int i = 0; i < 32; i += 2)
         ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(__int2float_rn(static_cast<int>(v[i])), __int2float_rn(static_cast<int>(v[i + 1]))),
-                                         ptx::pack_f32x2(w[i], w[i + 1])), f[i], f[i + 1]);
+                                         ptx::pack_f32x2(__shfl_sync(0xffffffffu, mine, i), __shfl_sync(0xffffffffu, mine, i + 1))), f[i], f[i + 1]);
 }
 
 // The product itself.  Whole chunks of 32 columns leave through shared memory and TMA stores (the tensor map ends with them: a store that is cut
@@ -126,24 +128,30 @@ struct EpiLinear {
         int T, V;
     };
     struct State {
+        Columns w, b;
         float sx;
         int row;
     };
+    __device__ static __forceinline__ void ahead(const Params& p, State& s, int n_tile) {
+        s.w.load(p.sw, n_tile, p.V);
+        if (p.bias != nullptr) s.b.load(p.bias, n_tile, p.V);
+    }
     __device__ static __forceinline__ void begin_item(const Params& p, State& s, int m_tile, int row_in_tile) {
         s.row = m_tile * tc::BM + row_in_tile;
         s.sx = s.row < p.T ? p.sx[s.row] : 0.f;
     }
-    __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage1& o) {
+    __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, int n_next, uint32_t taddr, OutStage1& o) {
         const int col0 = n_tile * tc::BN;
         const int ncols = min(tc::BN, p.V - col0);
+        const Columns w = s.w, b = s.b;
+        ahead(p, s, n_next);
         walk_half(taddr, ncols, [&](int c, uint32_t (&v)[32]) {
-            float w[32], f[32];
-            values_at(p.sw + col0 + c * 32, ncols - c * 32, w);
-            scaled(v, w, f);
+            float f[32];
+            scaled(v, w.chunk(c), f);
             if (p.bias != nullptr) {
-                values_at(p.bias + col0 + c * 32, ncols - c * 32, w);
+                const float mine = b.chunk(c);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) f[i] = __fadd_rn(__fmul_rn(f[i], s.sx), w[i]);
+                for (int i = 0; i < 32; ++i) f[i] = __fadd_rn(__fmul_rn(f[i], s.sx), __shfl_sync(0xffffffffu, mine, i));
             } else {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) f[i] *= s.sx;
@@ -220,9 +228,11 @@ struct EpiCe {
         int T, V;
     };
     struct State {
+        Columns w;
         RowSums r;
         int y, row;
     };
+    __device__ static __forceinline__ void ahead(const Params& p, State& s, int n_tile) { s.w.load(p.sw, n_tile, p.V); }
     __device__ static __forceinline__ void begin_item(const Params& p, State& s, int m_tile, int row_in_tile) {
         s.row = m_tile * tc::BM + row_in_tile;
         s.y = -1;
@@ -234,14 +244,15 @@ struct EpiCe {
         }
         s.r.clear(sx);
     }
-    __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage1&) {
+    __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, int n_next, uint32_t taddr, OutStage1&) {
         const int col0 = n_tile * tc::BN;
         const int ncols = min(tc::BN, p.V - col0);
+        const Columns w = s.w;
+        ahead(p, s, n_next);
         walk_half(taddr, ncols, [&](int c, uint32_t (&v)[32]) {
-            float w[32], f[32];
+            float f[32];
             const int live = ncols - c * 32;
-            values_at(p.sw + col0 + c * 32, live, w);
-            scaled(v, w, f);
+            scaled(v, w.chunk(c), f);
             if (live < 32) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
@@ -368,38 +379,42 @@ struct EpiDz {
         int T, V;
     };
     struct State {
+        Columns w;
         RowGrad q;
         float a, up, down;
         int row;
     };
+    __device__ static __forceinline__ void ahead(const Params& p, State& s, int n_tile) { s.w.load(p.sw, n_tile, p.V); }
     __device__ static __forceinline__ void begin_item(const Params& p, State& s, int m_tile, int row_in_tile) {
         s.row = m_tile * tc::BM + row_in_tile;
         s.q = row_grad(s.row, p.T, p.V, p.labels, p.valid, p.nll, p.lse, p.g);
         s.a = log2_scale(s.row < p.T ? p.sx[s.row] : 0.f);
         fit_half(*p.most, s.up, s.down);
     }
-    __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, uint32_t taddr, OutStage1& o) {
+    __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, int n_next, uint32_t taddr, OutStage1& o) {
         const int col0 = n_tile * tc::BN;
         const int ncols = min(tc::BN, p.V - col0);
-        const uint64_t a2 = ptx::pack_f32x2(s.a, s.a), no2 = ptx::pack_f32x2(-s.q.others2, -s.q.others2), up2 = ptx::pack_f32x2(s.up, s.up);
+        const Columns w = s.w;
+        ahead(p, s, n_next);
+        const uint64_t a2 = ptx::pack_f32x2(s.a, s.a), no2 = ptx::pack_f32x2(-s.q.others2, -s.q.others2);
         walk_half(taddr, ncols, [&](int c, uint32_t (&v)[32]) {
             if ((c & 1) == 0) o.begin();
-            float w[32], f[32];
-            values_at(p.sw + col0 + c * 32, ncols - c * 32, w);
-            scaled(v, w, f);
+            const float mine = w.chunk(c), up = mine * s.up;
+            float f[32];
+            scaled(v, mine, f);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint64_t w2 = ptx::mul_f32x2(ptx::pack_f32x2(w[2 * i], w[2 * i + 1]), up2);
+            for (int i = 0; i < 32; i += 2) {
                 float x0, x1;
-                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(f[2 * i], f[2 * i + 1]), a2, no2), x0, x1);
-                ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(ptx::ex2_approx(x0), ptx::ex2_approx(x1)), w2), f[2 * i], f[2 * i + 1]);
-                ptx::unpack_f32x2(w2, w[2 * i], w[2 * i + 1]);
+                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(f[i], f[i + 1]), a2, no2), x0, x1);
+                ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(ptx::ex2_approx(x0), ptx::ex2_approx(x1)),
+                                                 ptx::pack_f32x2(__shfl_sync(0xffffffffu, up, i), __shfl_sync(0xffffffffu, up, i + 1))), f[i], f[i + 1]);
             }
             const int rel = s.q.y - (col0 + c * 32);
+            const float at_label = -__shfl_sync(0xffffffffu, up, rel & 31);
             if (rel >= 0 && rel < 32) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    if (i == rel) f[i] = -w[i];
+                    if (i == rel) f[i] = at_label;
             }
             if (!s.q.on) {
 #pragma unroll
@@ -473,6 +488,12 @@ template <>
 struct OperandOf<i8::EpiOutHalf> { static constexpr Operand value = Operand::F16; };
 template <bool F32>
 struct EpiSets<i8::EpiLinear<F32>> { static constexpr int value = 2; };
+template <bool F32>
+struct LooksAhead<i8::EpiLinear<F32>> { static constexpr bool value = true; };
+template <>
+struct LooksAhead<i8::EpiCe> { static constexpr bool value = true; };
+template <>
+struct LooksAhead<i8::EpiDz> { static constexpr bool value = true; };
 template <>
 struct EpiSets<i8::EpiCe> { static constexpr int value = 2; };
 template <>

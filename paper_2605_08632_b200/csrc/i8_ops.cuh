@@ -193,10 +193,10 @@ int cat_i8_linear_fwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq
     CUtensorMap tmY;
     if (shape->y_dtype == CAT_F32) {
         if (tmap_out_f32(&tmY, Y, h.T, whole, shape->ldY) != CAT_OK) return CAT_ERR_CUDA;
-        return launch_i8<i8::EpiLinear<true>>(h, {h.sx, h.sw, bias, Y, shape->ldY, h.T, h.V}, 0, status, sm_count, st, &tmY);
+        return launch_i8<i8::EpiLinear<true>>(h, {h.sx, h.sw, bias, Y, shape->ldY, h.T, h.V}, fwd_splits(h.T, h.V), status, sm_count, st, &tmY);
     }
     if (tmap_out(&tmY, Y, h.T, whole, shape->ldY) != CAT_OK) return CAT_ERR_CUDA;
-    return launch_i8<i8::EpiLinear<false>>(h, {h.sx, h.sw, bias, Y, shape->ldY, h.T, h.V}, 0, status, sm_count, st, &tmY);
+    return launch_i8<i8::EpiLinear<false>>(h, {h.sx, h.sw, bias, Y, shape->ldY, h.T, h.V}, fwd_splits(h.T, h.V), status, sm_count, st, &tmY);
 }
 
 int cat_i8_linear_bwd(const cat_i8_shape* shape, const void* dY, const int8_t* Wq, const float* w_scale, void* dX,

@@ -45,9 +45,11 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 
-// arrive on an mbarrier of another CTA of the cluster (address from mapa_shared)
+// Arrive on an mbarrier of another CTA of the cluster (address from mapa_shared), for what the two order by tcgen05 fences: no data
+// in memory is handed over.  (A release at cluster scope waits until all of the thread's global stores and loads have been performed: 2000 cycles
+// behind each tile of an epilogue.)
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 __device__ __forceinline__ void ld_shared_v4(uint32_t addr, uint4& v) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");

@@ -609,6 +609,11 @@ struct EpiSets { static constexpr int value = 1; };
 template <class Epi>
 constexpr int THREADS_OF = NUM_THREADS + 128 * (EpiSets<Epi>::value - 1);
 
+// Whether an epilogue fetches something for the columns of its next tile while it works on one: Epi::ahead(ep, st, n_tile) for the first tile, and
+// Epi::tile gets the next tile's index (its own where there is none).
+template <class Epi>
+struct LooksAhead { static constexpr bool value = false; };
+
 // Whether a kernel behind the GEMM may run beside it (see lp::norm_kernel).
 template <class Epi>
 struct LetsNextStart { static constexpr bool value = false; };
@@ -885,17 +890,33 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
         out.sel = 0;
         out.row0 = 0;
         out.n_rows = Epi::out_rows(ep);
+        if constexpr (LooksAhead<Epi>::value) {
+            if (worker < sched.n_items) {
+                int m_tile, group, n_begin, n_end;
+                decode_item(sched, worker, m_tile, group, n_begin, n_end);
+                Epi::ahead(ep, st, n_begin);
+            }
+        }
         for (int item = worker; item < sched.n_items && ok; item += n_workers) {
             int m_tile, group, n_begin, n_end;
             decode_item(sched, item, m_tile, group, n_begin, n_end);
             Epi::begin_item(ep, st, m_tile * CG + static_cast<int>(rank), row_in_tile);
             out.row0 = (m_tile * CG + static_cast<int>(rank)) * BM + quarter * 32;
             for (int n = n_begin; n < n_end; ++n) {
+                int n_next = n + 1;
+                if constexpr (LooksAhead<Epi>::value) {
+                    if (n_next == n_end) {
+                        int a, b, e;
+                        if (item + n_workers < sched.n_items) decode_item(sched, item + n_workers, a, b, n_next, e);
+                        else n_next = n;
+                    }
+                }
                 ok = wait_bounded(ptx::smem_u32(&ctl.tfull[acc]), acc_phase, abort, status, wait_ns);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 ptx::tc_fence_after();
-                Epi::tile(ep, st, n, lane_base + acc * BN, out);
+                if constexpr (LooksAhead<Epi>::value) Epi::tile(ep, st, n, n_next, lane_base + acc * BN, out);
+                else Epi::tile(ep, st, n, lane_base + acc * BN, out);
                 ptx::tc_fence_before();
                 if (CG == 1) {
                     ptx::mbar_arrive(ptx::smem_u32(&ctl.tempty[acc]));
