@@ -29,18 +29,56 @@ __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162f
 // 127 x / most to the nearest integer, halves to the even one, exactly: the binary32 product is off by less than 2^-16, and what lies
 // that near to a half is decided by the quotient in 64 bits (127 x is exact there, and no quotient of a 31-bit by a 24-bit number is
 // within 2^-53 of a half without being one).  inv = 127 / most, or 0 where that is out of range.
+__device__ __noinline__ int exact_steps(float x, float most) { return static_cast<int>(rint(127.0 * static_cast<double>(x) / static_cast<double>(most))); }
 __device__ __forceinline__ int steps_of(float x, float inv, float most) {
     const float t = x * inv;
     const float n = rintf(t);
-    if (inv != 0.f && fabsf(t - n) < 0.4999f) return static_cast<int>(n);
-    return static_cast<int>(rint(127.0 * static_cast<double>(x) / static_cast<double>(most)));
+    return inv != 0.f && fabsf(t - n) < 0.4999f ? static_cast<int>(n) : exact_steps(x, most);
 }
 
-// One CTA per row.
+// What else the kernel that makes a call's tokens into integers does: it clears the workspace's header and finds the largest finite |scale| of the
+// head, in MOST_PARTS parts.  Kept out of launches of their own: a small call is mostly the time between kernels.
+constexpr int MOST_PARTS = 32;
+struct CallSetup {
+    int* header;           // status and worker claims, or nullptr
+    int header_ints;
+    const float* sw;       // scales of the head, or nullptr: MOST_PARTS more CTAs
+    int V;
+    int* most;             // [MOST_PARTS] float bits, inside the header (not cleared)
+};
+__device__ __forceinline__ void set_up_call(const CallSetup& c, int part) {
+    if (part < 0) {
+        if (c.header != nullptr && blockIdx.x == 0)
+            for (int i = threadIdx.x; i < c.header_ints; i += THREADS) {
+                int* at = c.header + i;
+                if (c.most == nullptr || at < c.most || at >= c.most + MOST_PARTS) *at = 0;
+            }
+        return;
+    }
+    __shared__ unsigned s_part[THREADS / 32];
+    unsigned bits = 0;
+    for (long long v = static_cast<long long>(part) * THREADS + threadIdx.x; v < c.V; v += MOST_PARTS * THREADS) {
+        const unsigned x = __float_as_uint(c.sw[v]) & 0x7fffffffu;
+        if (x < 0x7f800000u) bits = max(bits, x);
+    }
+    bits = __reduce_max_sync(0xffffffffu, bits);
+    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = bits;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < THREADS / 32; ++i) bits = max(bits, s_part[i]);
+        c.most[part] = static_cast<int>(bits);
+    }
+}
+
+// Rows of any length and alignment, one CTA each.
 template <class T>
-__global__ void __launch_bounds__(THREADS) quantize_kernel(const T* X, long long ldX, int d, int8_t* Xq, long long ldq, int pad, float* scale) {
+__global__ void __launch_bounds__(THREADS) quantize_kernel(const T* X, long long ldX, int rows, int d, int8_t* Xq, long long ldq, int pad, float* scale,
+                                                           const CallSetup setup) {
     __shared__ unsigned s_most[THREADS / 32];
     const long long r = blockIdx.x;
+    ptx::launch_dependents();
+    set_up_call(setup, r < rows ? -1 : static_cast<int>(r) - rows);
+    if (r >= rows) return;
     const T* x = X + r * ldX;
     unsigned bits = 0;                      // of |x|: ordered like the values, infinities and NaN above them
     for (int i = threadIdx.x; i < d; i += THREADS) bits = max(bits, __float_as_uint(to_float(x[i])) & 0x7fffffffu);
@@ -55,6 +93,122 @@ __global__ void __launch_bounds__(THREADS) quantize_kernel(const T* X, long long
     int8_t* q = Xq + r * ldq;
     for (int i = threadIdx.x; i < pad; i += THREADS) q[i] = any && i < d ? static_cast<int8_t>(steps_of(to_float(x[i]), inv, most)) : 0;
     if (threadIdx.x == 0) scale[r] = finite ? most / 127.f : __uint_as_float(0x7fc00000u);
+}
+
+// Eight neighbouring values, 16 or 32 bytes.
+template <class T>
+struct Eight;
+template <>
+struct Eight<__nv_bfloat16> {
+    uint4 x;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { x = __ldg(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void clear() { x = make_uint4(0u, 0u, 0u, 0u); }
+    __device__ __forceinline__ unsigned most() const {          // of |x|, as float bits
+        const unsigned m = __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+        return max(m << 16, m & 0xffff0000u);
+    }
+    __device__ __forceinline__ void values(float (&f)[8]) const {
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+};
+template <>
+struct Eight<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p) {
+        a = __ldg(reinterpret_cast<const float4*>(p));
+        b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    }
+    __device__ __forceinline__ void clear() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void values(float (&f)[8]) const {
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+        f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    }
+    __device__ __forceinline__ unsigned most() const {
+        float f[8];
+        values(f);
+        unsigned m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
+        return m;
+    }
+};
+
+// steps_of for eight values.  x inv + 1.5 2^23 holds the nearest integer in its low bits; the distance to it says whether a half is near.
+__device__ __forceinline__ uint2 eight_steps(const float (&x)[8], float inv, float most) {
+    constexpr float MAGIC = 12582912.f;
+    uint32_t m[8];
+    float far = inv != 0.f ? 0.f : 1.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float t = fmaf(x[i], inv, MAGIC);
+        far = fmaxf(far, fabsf(fmaf(x[i], inv, -(t - MAGIC))));
+        m[i] = __float_as_uint(t);
+    }
+    if (far >= 0.4999f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float t = __uint_as_float(m[i]) - MAGIC;
+            if (inv == 0.f || fabsf(fmaf(x[i], inv, -t)) >= 0.4999f) m[i] = static_cast<uint32_t>(exact_steps(x[i], most));
+        }
+    }
+    return make_uint2(__byte_perm(__byte_perm(m[0], m[1], 0x0040), __byte_perm(m[2], m[3], 0x0040), 0x5410),
+                      __byte_perm(__byte_perm(m[4], m[5], 0x0040), __byte_perm(m[6], m[7], 0x0040), 0x5410));
+}
+
+// Rows of up to 2048 WARPS values in whole eights, on 16-byte boundaries: WARPS warps each, one pass, the values kept in registers.
+constexpr int EIGHTS = 8;                // per lane
+template <class T, int WARPS>
+__global__ void __launch_bounds__(THREADS) quantize_rows_kernel(const T* X, long long ldX, int rows, int d, int8_t* Xq, long long ldq, int pad, float* scale,
+                                                                const CallSetup setup) {
+    constexpr int PER_CTA = THREADS / 32 / WARPS;
+    __shared__ unsigned s_most[THREADS / 32];
+    const int row_ctas = (rows + PER_CTA - 1) / PER_CTA;
+    ptx::launch_dependents();
+    set_up_call(setup, static_cast<int>(blockIdx.x) < row_ctas ? -1 : static_cast<int>(blockIdx.x) - row_ctas);
+    if (static_cast<int>(blockIdx.x) >= row_ctas) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long r = static_cast<long long>(blockIdx.x) * PER_CTA + warp / WARPS;
+    const int first = (warp % WARPS) * 32 + lane, n = d >> 3;        // this lane's eights: first + 32 WARPS i
+    const bool on = r < rows;
+    Eight<T> x[EIGHTS];
+    unsigned bits = 0;
+#pragma unroll
+    for (int i = 0; i < EIGHTS; ++i) {
+        const int g = first + 32 * WARPS * i;
+        if (on && g < n) x[i].load(X + r * ldX + 8 * g);
+        else x[i].clear();
+    }
+#pragma unroll
+    for (int i = 0; i < EIGHTS; ++i) bits = max(bits, x[i].most());
+    bits = __reduce_max_sync(0xffffffffu, bits);
+    if (WARPS > 1) {
+        if (lane == 0) s_most[warp] = bits;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) bits = max(bits, s_most[warp / WARPS * WARPS + i]);
+    }
+    if (!on) return;
+    const float most = __uint_as_float(bits);
+    const bool finite = bits < 0x7f800000u, any = finite && bits != 0u;
+    const float inv = any && most > 1.0e-30f ? 127.f / most : 0.f;
+    int8_t* q = Xq + r * ldq;
+#pragma unroll
+    for (int i = 0; i < EIGHTS; ++i) {
+        const int g = first + 32 * WARPS * i;
+        if (g >= n) break;
+        float f[8];
+        x[i].values(f);
+        *reinterpret_cast<uint2*>(q + 8 * g) = any ? eight_steps(f, inv, most) : make_uint2(0u, 0u);
+    }
+    if (warp % WARPS == 0 && lane == 0) {
+        if (pad > d) *reinterpret_cast<uint2*>(q + d) = make_uint2(0u, 0u);          // the other half of 16 bytes
+        scale[r] = finite ? most / 127.f : __uint_as_float(0x7fc00000u);
+    }
 }
 
 struct Head {
@@ -286,6 +440,7 @@ __global__ void __launch_bounds__(THREADS) merge_kernel(const float* part_m, con
     __shared__ float s_m[THREADS / 32][MERGE_ROWS], s_l[THREADS / 32][MERGE_ROWS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int r = blockIdx.x * MERGE_ROWS + lane;
+    ptx::grid_dependency_wait();
     float m = LOW2, l = 0.f;
     if (r < T) {
 #pragma unroll 4
@@ -323,20 +478,10 @@ __global__ void __launch_bounds__(THREADS) merge_kernel(const float* part_m, con
 }
 
 // ------------------------------------------------------------------------------ gradient
-// Largest finite |scale| of the head, as float bits raised from 0.
-__global__ void __launch_bounds__(THREADS) largest_scale_kernel(const float* sw, int V, int* most) {
-    unsigned bits = 0;
-    for (int v = blockIdx.x * THREADS + threadIdx.x; v < V; v += gridDim.x * THREADS) {
-        const unsigned b = __float_as_uint(sw[v]) & 0x7fffffffu;
-        if (b < 0x7f800000u) bits = max(bits, b);
-    }
-    bits = __reduce_max_sync(0xffffffffu, bits);
-    if ((threadIdx.x & 31) == 0) atomicMax(most, static_cast<int>(bits));
-}
-
-// 2^k with most 2^k in [2^14, 2^15), and 2^-k
-__device__ __forceinline__ void fit_half(int most_bits, float& up, float& down) {
-    int e = most_bits >> 23;                            // biased exponent of the largest scale
+// 2^k with (largest scale) 2^k in [2^14, 2^15), and 2^-k.  All lanes of a warp.
+__device__ __forceinline__ void fit_half(const int* most, float& up, float& down) {
+    static_assert(MOST_PARTS == 32, "one part per lane");
+    int e = __reduce_max_sync(0xffffffffu, most[threadIdx.x & 31]) >> 23;       // its biased exponent
     e = e < 20 ? 20 : e > 250 ? 250 : e;
     up = __uint_as_float(static_cast<unsigned>(254 + 14 - e) << 23);
     down = __uint_as_float(static_cast<unsigned>(e - 14) << 23);
@@ -374,7 +519,7 @@ struct EpiDz {
         const float* nll;
         const float* lse;
         const float* g;            // [T] upstream
-        const int* most;           // bits of the largest scale
+        const int* most;           // [MOST_PARTS] bits of the largest scale
         float* factor;             // [T] out: g (1 - p_y) 2^-k
         int T, V;
     };
@@ -389,7 +534,7 @@ struct EpiDz {
         s.row = m_tile * tc::BM + row_in_tile;
         s.q = row_grad(s.row, p.T, p.V, p.labels, p.valid, p.nll, p.lse, p.g);
         s.a = log2_scale(s.row < p.T ? p.sx[s.row] : 0.f);
-        fit_half(*p.most, s.up, s.down);
+        fit_half(p.most, s.up, s.down);
     }
     __device__ static __forceinline__ void tile(const Params& p, State& s, int n_tile, int n_next, uint32_t taddr, OutStage1& o) {
         const int col0 = n_tile * tc::BN;
@@ -461,6 +606,7 @@ __global__ void __launch_bounds__(THREADS) widen_kernel(const int8_t* wq, long l
 // Parts of a contraction, added in order; the row's factor; one rounding.
 __global__ void __launch_bounds__(THREADS) add_parts_kernel(const float* part, int g, long long stride, int d, const float* factor, __nv_bfloat16* out, long long ld) {
     const long long r = blockIdx.x;
+    ptx::grid_dependency_wait();
     const float f = factor ? factor[r] : 1.f;
     for (int i = threadIdx.x * 4; i < d; i += THREADS * 4) {
         float4 s = *reinterpret_cast<const float4*>(part + r * d + i);

@@ -1,10 +1,14 @@
 // Host side of the operators on an 8-bit head: cat_i8_quantize, cat_i8_linear_fwd / _bwd and cat_i8_ce_fwd / _bwd.  Included at the end
 // of cat_api.cu, whose planning and launch helpers it uses.
 #pragma once
+#include "i8_grad.cuh"
+#include "i8_head.cuh"
+#include "i8_skinny.cuh"
 
 namespace {
 
-constexpr size_t kMostOffset = 64;       // header: largest scale of the head
+constexpr size_t kMostOffset = 64;       // header: largest scale of the head, in i8::MOST_PARTS parts
+static_assert(kMostOffset + sizeof(int) * i8::MOST_PARTS <= kClaimsOffset, "between the status and the claims");
 
 enum I8Pass { kI8Linear = 0, kI8LinearBwd = 1, kI8Ce = 2, kI8CeBwd = 3 };
 
@@ -32,14 +36,35 @@ struct I8Plan {
     long long Ts;          // rows per slab
     long long ldz;
     int S;                 // splits of the vocabulary
+    bool skinny;           // a few tokens: the kernel of i8_skinny.cuh
+    bool widen;            // gradient: from a widened copy of the head; else widened on its way (i8_grad.cuh)
     size_t off_q, off_s, off_m, off_l, off_zy, off_factor, off_w16, off_part, off_z, total;
 };
+
+// Parts of the vocabulary that grad_kernel's CTAs share out: about 340 ns per slice of the longest, four slices' worth for filling the ring, the tile written
+// out and read back.
+int grad_parts(long long rows, long long d, long long V) {
+    const long long tiles = cdiv(d, i8::GRAD_COLS), slices = cdiv(V, i8::GRAD_SLICE);
+    const double out = static_cast<double>(rows) * static_cast<double>(d) * 4.0e-6;           // slices' worth of time per part
+    int best = 1;
+    double best_cost = 1e300;
+    for (long long g = 1; g <= kPlanSMs && g <= slices; ++g) {
+        const double cost = static_cast<double>(cdiv(tiles * g, kPlanSMs)) * static_cast<double>(cdiv(slices, g) + 4) + out * static_cast<double>(g);
+        if (cost < best_cost) { best_cost = cost; best = static_cast<int>(g); }
+    }
+    return best;
+}
+size_t dx_part_bytes(long long rows, long long d, long long V, bool widen) {
+    return widen ? dh_part_bytes(rows, d, V) : align256(sizeof(float) * grad_parts(rows, d, V) * static_cast<size_t>(rows) * d);
+}
 
 I8Plan plan_i8(const cat_i8_shape* s, int pass) {
     I8Plan p;
     memset(&p, 0, sizeof(p));
     p.ldq = cdiv(s->d, 16) * 16;
     p.Ts = s->T;
+    p.skinny = s->T <= i8::SKINNY_ROWS;
+    p.widen = s->T > i8::GRAD_ROWS;
     size_t off = kHeaderBytes;
     if (pass != kI8LinearBwd) {
         p.off_q = off; off = align256(off + static_cast<size_t>(s->T) * p.ldq);
@@ -47,8 +72,9 @@ I8Plan plan_i8(const cat_i8_shape* s, int pass) {
     }
     if (pass == kI8Ce) {
         p.S = fwd_splits(s->T, s->V);
-        p.off_m = off; off = align256(off + sizeof(float) * 2 * p.S * s->T);
-        p.off_l = off; off = align256(off + sizeof(float) * 2 * p.S * s->T);
+        const size_t parts = p.skinny ? kPlanSMs : 2 * p.S;           // one per CTA, or two per split
+        p.off_m = off; off = align256(off + sizeof(float) * parts * s->T);
+        p.off_l = off; off = align256(off + sizeof(float) * parts * s->T);
         p.off_zy = off; off = align256(off + sizeof(float) * s->T);
     }
     if (pass == kI8CeBwd) {
@@ -61,24 +87,63 @@ I8Plan plan_i8(const cat_i8_shape* s, int pass) {
         p.off_z = off; off = align256(off + 2 * static_cast<size_t>(p.Ts) * p.ldz);
     }
     if (pass == kI8LinearBwd || pass == kI8CeBwd) {
-        p.off_w16 = off; off = align256(off + 2 * static_cast<size_t>(s->V) * s->d);
-        const size_t full = dh_part_bytes(p.Ts, s->d, s->V), rest = dh_part_bytes(s->T - (cdiv(s->T, p.Ts) - 1) * p.Ts, s->d, s->V);
+        p.off_w16 = off; if (p.widen) off = align256(off + 2 * static_cast<size_t>(s->V) * s->d);
+        const size_t full = dx_part_bytes(p.Ts, s->d, s->V, p.widen), rest = dx_part_bytes(s->T - (cdiv(s->T, p.Ts) - 1) * p.Ts, s->d, s->V, p.widen);
         p.off_part = off; off += full > rest ? full : rest;
     }
     p.total = off;
     return p;
 }
 
+// A launch that may start ahead of the end of the kernel before it, for which it waits itself.
+template <class... P, class... A>
+int launch_ahead(void (*kern)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads), 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kern, args...) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
+    return CAT_OK;
+}
+
+template <class T, int WARPS>
+void launch_quantize_rows(const T* X, long long rows, long long d, long long ldX, int8_t* Xq, long long ldq, long long pad, float* scale,
+                          const i8::CallSetup& setup, int more, cudaStream_t st) {
+    const long long ctas = cdiv(rows, i8::THREADS / 32 / WARPS);
+    i8::quantize_rows_kernel<T, WARPS><<<static_cast<unsigned>(ctas + more), i8::THREADS, 0, st>>>(X, ldX, static_cast<int>(rows), static_cast<int>(d), Xq, ldq,
+                                                                                                 static_cast<int>(pad), scale, setup);
+}
+
+// Rows of whole eights on 16-byte boundaries, up to 16384 long, are read once, by one warp each or, where they are long or few, by up to eight: the head of
+// 128256 x 2048 346 -> 155 us against a CTA per row that reads them twice.
 template <class T>
-int launch_quantize(const void* X, long long rows, long long d, long long ldX, int8_t* Xq, long long ldq, long long pad, float* scale, cudaStream_t st) {
-    i8::quantize_kernel<T><<<static_cast<unsigned>(rows), i8::THREADS, 0, st>>>(static_cast<const T*>(X), ldX, static_cast<int>(d), Xq, ldq,
-                                                                                static_cast<int>(pad), scale);
+int launch_quantize(const T* X, long long rows, long long d, long long ldX, int8_t* Xq, long long ldq, long long pad, float* scale, const i8::CallSetup& setup,
+                    cudaStream_t st) {
+    const int more = setup.sw ? i8::MOST_PARTS : 0;
+    const bool whole = d % 8 == 0 && d <= 8 * 256 * i8::EIGHTS && ldX * sizeof(T) % 16 == 0 && !misaligned(X, 16) && ldq % 8 == 0 && !misaligned(Xq, 8);
+    if (whole) {
+        int warps = 1;
+        while (warps < 8 && (d > 256 * i8::EIGHTS * warps || (rows * warps < 8 * kPlanSMs && d > 256 * warps))) warps *= 2;
+        if (warps == 1) launch_quantize_rows<T, 1>(X, rows, d, ldX, Xq, ldq, pad, scale, setup, more, st);
+        else if (warps == 2) launch_quantize_rows<T, 2>(X, rows, d, ldX, Xq, ldq, pad, scale, setup, more, st);
+        else if (warps == 4) launch_quantize_rows<T, 4>(X, rows, d, ldX, Xq, ldq, pad, scale, setup, more, st);
+        else launch_quantize_rows<T, 8>(X, rows, d, ldX, Xq, ldq, pad, scale, setup, more, st);
+    } else {
+        i8::quantize_kernel<T><<<static_cast<unsigned>(rows + more), i8::THREADS, 0, st>>>(X, ldX, static_cast<int>(rows), static_cast<int>(d), Xq, ldq,
+                                                                                           static_cast<int>(pad), scale, setup);
+    }
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
 int quantize(const void* X, int dtype, long long rows, long long d, long long ldX, int8_t* Xq, long long ldq, long long pad, float* scale,
-             cudaStream_t st) {
-    return dtype == CAT_BF16 ? launch_quantize<__nv_bfloat16>(X, rows, d, ldX, Xq, ldq, pad, scale, st)
-                             : launch_quantize<float>(X, rows, d, ldX, Xq, ldq, pad, scale, st);
+             const i8::CallSetup& setup, cudaStream_t st) {
+    return dtype == CAT_BF16 ? launch_quantize(static_cast<const __nv_bfloat16*>(X), rows, d, ldX, Xq, ldq, pad, scale, setup, st)
+                             : launch_quantize(static_cast<const float*>(X), rows, d, ldX, Xq, ldq, pad, scale, setup, st);
 }
 
 // What every pass begins with: the checks that are alike, the header cleared, the tokens as integers.
@@ -89,24 +154,31 @@ int begin_i8(const cat_i8_shape* s, int pass, const I8Plan& plan, const void* X,
     const int dc = check_device(sm_count);
     if (dc != CAT_OK) return dc;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    if (cudaMemsetAsync(ws, 0, kHeaderBytes, st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
     h->xq = reinterpret_cast<int8_t*>(ws + plan.off_q); h->ldq = plan.ldq;
     h->sx = reinterpret_cast<float*>(ws + plan.off_s);
     h->wq = Wq; h->sw = w_scale; h->ldw = s->ldW;
     h->T = static_cast<int>(s->T); h->V = static_cast<int>(s->V); h->d = static_cast<int>(s->d);
-    if (pass == kI8LinearBwd) return CAT_OK;
+    if (pass == kI8LinearBwd) {
+        if (cudaMemsetAsync(ws, 0, kHeaderBytes, st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
+        return CAT_OK;
+    }
+    i8::CallSetup setup = {};
+    setup.header = reinterpret_cast<int*>(ws);
+    setup.header_ints = kHeaderBytes / sizeof(int);
+    if (pass == kI8CeBwd) { setup.sw = w_scale; setup.V = h->V; setup.most = reinterpret_cast<int*>(ws + kMostOffset); }
     return quantize(X, s->x_dtype, s->T, s->d, s->ldX, reinterpret_cast<int8_t*>(ws + plan.off_q), plan.ldq, plan.ldq,
-                    reinterpret_cast<float*>(ws + plan.off_s), st);
+                    reinterpret_cast<float*>(ws + plan.off_s), setup, st);
 }
 
-// K-major 8-bit operand [rows][d] with row pitch ld bytes: boxes of 128 bytes x box_rows.
-int tmap_i8(CUtensorMap* m, const void* base, long long rows, long long d, long long ld, int box_rows) {
+// 8-bit operand [rows][d] with row pitch ld bytes: boxes of 128 bytes x box_rows, swizzled as the tensor cores want them or as they are.
+int tmap_i8(CUtensorMap* m, const void* base, long long rows, long long d, long long ld, int box_rows, bool swizzled = true) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return CAT_ERR_CUDA;
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(ld)};
     const cuuint32_t box[2] = {2 * tc::BK, static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
     const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                          swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? CAT_OK : CAT_ERR_CUDA;
 }
 
@@ -147,6 +219,66 @@ int launch_dx(const void* A, long long ldA, const uint16_t* w16, long long rows,
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
 
+template <int MODE, int TPW, int HALVES, int SUB>
+int launch_skinny_i8_as(const CUtensorMap& tmW, const CUtensorMap& tmX, i8::SkinnyParams p, int* status, int grid, cudaStream_t st) {
+    p.stages = (skinny::SMEM_BYTES - 1024 - 8192) / ((SUB * p.tile_rows + p.n) * 128);
+    if (p.stages > skinny::MAX_STAGES) p.stages = skinny::MAX_STAGES;
+    auto kern = i8::skinny_kernel<MODE, TPW, HALVES, SUB>;
+    static std::atomic<unsigned long long> allowed{0};
+    if (!allow_smem(kern, skinny::SMEM_BYTES, allowed)) return CAT_ERR_CUDA;
+    return launch_ahead(kern, dim3(static_cast<unsigned>(grid), 1, 1), 64 + 128 * HALVES, skinny::SMEM_BYTES, st, tmW, tmX, p, status);
+}
+
+// Up to 128 tokens against the head in the manner of MODE; p holds what that needs besides the sizes.
+template <int MODE>
+int launch_skinny_i8(i8::SkinnyParams p, int* status, int sm_count, int* n_parts, cudaStream_t st) {
+    p.n = static_cast<int>(cdiv(p.h.T, 16) * 16);
+    p.tile_rows = skinny_tile_rows(p.h.V);
+    p.n_tiles = static_cast<int>(cdiv(p.h.V, p.tile_rows));
+    p.num_kb = static_cast<int>(cdiv(p.h.d, 128));
+    p.wait_ns = tc::WAIT_LIMIT_NS;
+    CUtensorMap tmW, tmX;
+    if (tmap_i8(&tmW, p.h.wq, p.h.V, p.h.d, p.h.ldw, p.tile_rows) != CAT_OK || tmap_i8(&tmX, p.h.xq, p.h.T, p.h.d, p.h.ldq, p.n) != CAT_OK) return CAT_ERR_CUDA;
+    int grid = sm_count < kPlanSMs ? sm_count : kPlanSMs;
+    if (p.n_tiles < grid) grid = p.n_tiles;
+    if (n_parts) *n_parts = grid;
+    if (p.h.T <= 32) return launch_skinny_i8_as<MODE, 32, 1, 1>(tmW, tmX, p, status, grid, st);
+    if (p.h.T <= 64) return launch_skinny_i8_as<MODE, 32, 2, 2>(tmW, tmX, p, status, grid, st);
+    return launch_skinny_i8_as<MODE, 64, 2, 2>(tmW, tmX, p, status, grid, st);
+}
+
+template <bool SCALED, int TMEM>
+int launch_grad_as(const CUtensorMap& tmW, const CUtensorMap& tmA, const i8::GradParams& p, int* status, dim3 grid, cudaStream_t st) {
+    auto kern = i8::grad_kernel<SCALED, TMEM>;
+    static std::atomic<unsigned long long> allowed{0};
+    if (!allow_smem(kern, i8::GRAD_SMEM, allowed)) return CAT_ERR_CUDA;
+    return launch_ahead(kern, grid, i8::GRAD_THREADS, i8::GRAD_SMEM, st, tmW, tmA, p, status);
+}
+
+// dX[r, :] = factor[r] sum_v A[r, v] W[v, :] of up to 512 rows, the head widened on its way.
+template <bool SCALED>
+int launch_grad(const i8::Head& h, const void* A, long long ldA, const float* factor, __nv_bfloat16* dX, long long lddX, float* part, int* status, cudaStream_t st) {
+    i8::GradParams p;
+    p.sw = h.sw; p.part = part; p.T = h.T; p.V = h.V; p.d = h.d;
+    p.mmas = h.T > 256 ? 2 : 1;
+    p.n = static_cast<int>(cdiv(cdiv(h.T, p.mmas), 16) * 16);
+    p.num_kb = static_cast<int>(cdiv(h.V, i8::GRAD_SLICE));
+    p.stages = (i8::GRAD_SMEM - 1024 - i8::GRAD_WIDE * i8::GRAD_WIDE_BYTES) / (i8::GRAD_W_BYTES + p.mmas * p.n * 128);
+    if (p.stages > i8::GRAD_MAX_STAGES) p.stages = i8::GRAD_MAX_STAGES;
+    p.wait_ns = tc::WAIT_LIMIT_NS;
+    const int parts = grad_parts(h.T, h.d, h.V);
+    CUtensorMap tmW, tmA;
+    if (tmap_i8(&tmW, h.wq, h.V, h.d, h.ldw, i8::GRAD_SLICE, false) != CAT_OK || tmap_k_major(&tmA, A, h.T, h.V, ldA, p.n) != CAT_OK) return CAT_ERR_CUDA;
+    const dim3 grid(static_cast<unsigned>(cdiv(h.d, i8::GRAD_COLS)), static_cast<unsigned>(parts), 1);
+    const int cols = p.mmas * p.n;
+    const int rc = cols <= 32    ? launch_grad_as<SCALED, 32>(tmW, tmA, p, status, grid, st)
+                   : cols <= 128 ? launch_grad_as<SCALED, 128>(tmW, tmA, p, status, grid, st)
+                                 : launch_grad_as<SCALED, 512>(tmW, tmA, p, status, grid, st);
+    if (rc != CAT_OK) return rc;
+    return launch_ahead(i8::add_parts_kernel, dim3(static_cast<unsigned>(h.T), 1, 1), i8::THREADS, 0, st, static_cast<const float*>(part), parts,
+                        static_cast<long long>(h.T) * h.d, h.d, factor, dX, lddX);
+}
+
 template <bool SCALED>
 int launch_widen(const i8::Head& h, uint16_t* w16, int sm_count, cudaStream_t st) {
     const int per_row = h.d / 8;
@@ -168,7 +300,7 @@ int cat_i8_quantize(const void* X, int32_t dtype, int64_t rows, int64_t d, int64
     int sm_count = 0;
     const int dc = check_device(&sm_count);
     if (dc != CAT_OK) return dc;
-    return quantize(X, dtype, rows, d, ldX, Xq, ldXq, d, scale, static_cast<cudaStream_t>(cuda_stream));
+    return quantize(X, dtype, rows, d, ldX, Xq, ldXq, d, scale, i8::CallSetup{}, static_cast<cudaStream_t>(cuda_stream));
 }
 
 size_t cat_i8_workspace_bytes(const cat_i8_shape* shape, int pass) {
@@ -189,6 +321,13 @@ int cat_i8_linear_fwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq
     const int rc = begin_i8(shape, kI8Linear, plan, X, Wq, w_scale, workspace, workspace_bytes, &sm_count, &h, st);
     if (rc != CAT_OK) return rc;
     int* status = static_cast<int*>(workspace);
+    if (plan.skinny) {
+        i8::SkinnyParams p;
+        memset(&p, 0, sizeof(p));
+        p.h = h; p.bias = bias; p.Y = Y; p.ldY = shape->ldY;
+        return shape->y_dtype == CAT_F32 ? launch_skinny_i8<i8::SKINNY_F32>(p, status, sm_count, nullptr, st)
+                                         : launch_skinny_i8<i8::SKINNY_BF16>(p, status, sm_count, nullptr, st);
+    }
     const long long whole = h.V >= 32 ? h.V / 32 * 32 : 8;        // nothing is sent where there is no whole chunk
     CUtensorMap tmY;
     if (shape->y_dtype == CAT_F32) {
@@ -212,6 +351,9 @@ int cat_i8_linear_bwd(const cat_i8_shape* shape, const void* dY, const int8_t* W
     const int rc = begin_i8(shape, kI8LinearBwd, plan, nullptr, Wq, w_scale, workspace, workspace_bytes, &sm_count, &h, st);
     if (rc != CAT_OK) return rc;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
+    if (!plan.widen)
+        return launch_grad<true>(h, dY, shape->ldY, nullptr, static_cast<__nv_bfloat16*>(dX), shape->lddX, reinterpret_cast<float*>(ws + plan.off_part),
+                                 reinterpret_cast<int*>(ws), st);
     uint16_t* w16 = reinterpret_cast<uint16_t*>(ws + plan.off_w16);
     const int wc = launch_widen<true>(h, w16, sm_count, st);
     if (wc != CAT_OK) return wc;
@@ -235,13 +377,21 @@ int cat_i8_ce_fwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, co
     float *part_m = reinterpret_cast<float*>(ws + plan.off_m), *part_l = reinterpret_cast<float*>(ws + plan.off_l),
           *z_label = reinterpret_cast<float*>(ws + plan.off_zy);
     const long long* y = reinterpret_cast<const long long*>(labels);
-    i8::EpiCe::Params ep;
-    ep.sx = h.sx; ep.sw = h.sw; ep.labels = y; ep.part_m = part_m; ep.part_l = part_l; ep.z_label = z_label; ep.part_stride = h.T; ep.T = h.T; ep.V = h.V;
-    const int gc = launch_i8<i8::EpiCe>(h, ep, plan.S, reinterpret_cast<int*>(ws), sm_count, st, nullptr);
+    int* status = reinterpret_cast<int*>(ws);
+    int parts = 2 * plan.S, gc;
+    if (plan.skinny) {
+        i8::SkinnyParams p;
+        memset(&p, 0, sizeof(p));
+        p.h = h; p.labels = y; p.part_m = part_m; p.part_l = part_l; p.z_label = z_label;
+        gc = launch_skinny_i8<i8::SKINNY_CE>(p, status, sm_count, &parts, st);
+    } else {
+        i8::EpiCe::Params ep;
+        ep.sx = h.sx; ep.sw = h.sw; ep.labels = y; ep.part_m = part_m; ep.part_l = part_l; ep.z_label = z_label; ep.part_stride = h.T; ep.T = h.T; ep.V = h.V;
+        gc = launch_i8<i8::EpiCe>(h, ep, plan.S, status, sm_count, st, nullptr);
+    }
     if (gc != CAT_OK) return gc;
-    i8::merge_kernel<<<static_cast<unsigned>(cdiv(h.T, i8::MERGE_ROWS)), i8::THREADS, 0, st>>>(part_m, part_l, z_label, 2 * plan.S, h.T, h.T, h.V, y, valid,
-                                                                                               nll, lse);
-    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+    return launch_ahead(i8::merge_kernel, dim3(static_cast<unsigned>(cdiv(h.T, i8::MERGE_ROWS)), 1, 1), i8::THREADS, 0, st, static_cast<const float*>(part_m),
+                        static_cast<const float*>(part_l), static_cast<const float*>(z_label), parts, static_cast<long long>(h.T), h.T, h.V, y, valid, nll, lse);
 }
 
 int cat_i8_ce_bwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, const float* w_scale, const int64_t* labels,
@@ -264,22 +414,34 @@ int cat_i8_ce_bwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, co
     const long long* y = reinterpret_cast<const long long*>(labels);
     uint16_t* w16 = reinterpret_cast<uint16_t*>(ws + plan.off_w16);
     float* part = reinterpret_cast<float*>(ws + plan.off_part);
-    i8::largest_scale_kernel<<<static_cast<unsigned>(cdiv(h.V, 8 * i8::THREADS)), i8::THREADS, 0, st>>>(w_scale, h.V, most);
-    const int wc = launch_widen<false>(h, w16, sm_count, st);
-    if (wc != CAT_OK) return wc;
+    int* status = reinterpret_cast<int*>(ws);
+    if (plan.widen) {
+        const int wc = launch_widen<false>(h, w16, sm_count, st);
+        if (wc != CAT_OK) return wc;
+    }
     for (long long r0 = 0; r0 < shape->T; r0 += plan.Ts) {
         i8::Head hs = h;
         hs.T = static_cast<int>(shape->T - r0 < plan.Ts ? shape->T - r0 : plan.Ts);
         hs.xq += r0 * plan.ldq; hs.sx += r0;
-        CUtensorMap tmZ;
-        if (tmap_out(&tmZ, dz, hs.T, hs.V, plan.ldz) != CAT_OK) return CAT_ERR_CUDA;
-        i8::EpiDz::Params ep;
-        ep.sx = hs.sx; ep.sw = hs.sw; ep.labels = y + r0; ep.valid = valid ? valid + r0 : nullptr; ep.nll = nll + r0; ep.lse = lse + r0; ep.g = grad_nll + r0;
-        ep.most = most; ep.factor = factor + r0; ep.T = hs.T; ep.V = hs.V;
-        int gc = launch_i8<i8::EpiDz>(hs, ep, fwd_splits(hs.T, hs.V), reinterpret_cast<int*>(ws), sm_count, st, &tmZ);
+        const uint8_t* on = valid ? valid + r0 : nullptr;
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(dX) + r0 * shape->lddX;
+        int gc;
+        if (plan.skinny) {
+            i8::SkinnyParams p;
+            memset(&p, 0, sizeof(p));
+            p.h = hs; p.Y = dz; p.ldY = plan.ldz; p.labels = y; p.valid = on; p.nll = nll; p.lse = lse; p.g = grad_nll; p.most = most; p.factor = factor;
+            gc = launch_skinny_i8<i8::SKINNY_DZ>(p, status, sm_count, nullptr, st);
+        } else {
+            CUtensorMap tmZ;
+            if (tmap_out(&tmZ, dz, hs.T, hs.V, plan.ldz) != CAT_OK) return CAT_ERR_CUDA;
+            i8::EpiDz::Params ep;
+            ep.sx = hs.sx; ep.sw = hs.sw; ep.labels = y + r0; ep.valid = on; ep.nll = nll + r0; ep.lse = lse + r0; ep.g = grad_nll + r0;
+            ep.most = most; ep.factor = factor + r0; ep.T = hs.T; ep.V = hs.V;
+            gc = launch_i8<i8::EpiDz>(hs, ep, fwd_splits(hs.T, hs.V), status, sm_count, st, &tmZ);
+        }
         if (gc != CAT_OK) return gc;
-        gc = launch_dx<i8::EpiOutHalf>(dz, plan.ldz, w16, hs.T, hs.d, hs.V, factor + r0, static_cast<__nv_bfloat16*>(dX) + r0 * shape->lddX, shape->lddX, part,
-                                       reinterpret_cast<int*>(ws), sm_count, st);
+        gc = plan.widen ? launch_dx<i8::EpiOutHalf>(dz, plan.ldz, w16, hs.T, hs.d, hs.V, factor + r0, out, shape->lddX, part, status, sm_count, st)
+                        : launch_grad<false>(hs, dz, plan.ldz, factor + r0, out, shape->lddX, part, status, st);
         if (gc != CAT_OK) return gc;
     }
     return CAT_OK;
