@@ -21,19 +21,29 @@ namespace i8 {
 
 constexpr int THREADS = 256;
 constexpr float LOW2 = -1.0e30f;        // "no column yet", in units of log2: finite, so that LOW2 - LOW2 is 0
+constexpr float NEAR_HALF = 0.49998f;   // a distance from an integer that is 2^-16 short of a half, or more: what decides it is past binary32
 
 // ------------------------------------------------------------------------------ rows to integers
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// 127 x / most to the nearest integer, halves to the even one, exactly: the binary32 product is off by less than 2^-16, and what lies
-// that near to a half is decided by the quotient in 64 bits (127 x is exact there, and no quotient of a 31-bit by a 24-bit number is
-// within 2^-53 of a half without being one).  inv = 127 / most, or 0 where that is out of range.
+// 127 x / most to the nearest integer, halves to the even one, exactly.  inv = 127 / most; the product x inv is off by less than 2^-16, so only where it
+// comes that near to a half is more to be known: on which side of the odd number m = 2 (half) 254 x / most lies.  a + e is m most
+// exactly, and the fma's result is exact because its two sides nearly cancel.
+__device__ __forceinline__ float past_half(float x, float most, float n, float off) {
+    const float side = off < 0.f ? -1.f : 1.f, m = fmaf(2.f, n, side);
+    const float a = m * most, e = fmaf(m, most, -a), d = fmaf(254.f, x, -a);
+    const bool beyond = side > 0.f ? d > e : d < e, odd = (static_cast<int>(n) & 1) != 0;
+    return beyond || (d == e && odd) ? n + side : n;
+}
+// rows whose largest value is too small or too large for that: 127 x is exact in 64 bits, and no quotient of a 31-bit by a 24-bit number is within
+// 2^-53 of a half without being one
 __device__ __noinline__ int exact_steps(float x, float most) { return static_cast<int>(rint(127.0 * static_cast<double>(x) / static_cast<double>(most))); }
+__device__ __forceinline__ float inverse_step(float most) { return most > 1.0e-30f && most < 1.0e30f ? 127.f / most : 0.f; }
 __device__ __forceinline__ int steps_of(float x, float inv, float most) {
-    const float t = x * inv;
-    const float n = rintf(t);
-    return inv != 0.f && fabsf(t - n) < 0.4999f ? static_cast<int>(n) : exact_steps(x, most);
+    if (inv == 0.f) return exact_steps(x, most);
+    const float n = rintf(x * inv), off = fmaf(x, inv, -n);
+    return static_cast<int>(fabsf(off) < NEAR_HALF ? n : past_half(x, most, n, off));
 }
 
 // What else the kernel that makes a call's tokens into integers does: it clears the workspace's header and finds the largest finite |scale| of the
@@ -89,7 +99,7 @@ __global__ void __launch_bounds__(THREADS) quantize_kernel(const T* X, long long
     for (int i = 0; i < THREADS / 32; ++i) bits = max(bits, s_most[i]);
     const float most = __uint_as_float(bits);
     const bool finite = bits < 0x7f800000u, any = finite && bits != 0u;
-    const float inv = any && most > 1.0e-30f ? 127.f / most : 0.f;
+    const float inv = any ? inverse_step(most) : 0.f;
     int8_t* q = Xq + r * ldq;
     for (int i = threadIdx.x; i < pad; i += THREADS) q[i] = any && i < d ? static_cast<int8_t>(steps_of(to_float(x[i]), inv, most)) : 0;
     if (threadIdx.x == 0) scale[r] = finite ? most / 127.f : __uint_as_float(0x7fc00000u);
@@ -138,32 +148,52 @@ struct Eight<float> {
     }
 };
 
-// steps_of for eight values.  x inv + 1.5 2^23 holds the nearest integer in its low bits; the distance to it says whether a half is near.
-__device__ __forceinline__ uint2 eight_steps(const float (&x)[8], float inv, float most) {
+// steps_of for eight values, as far as binary32 goes; `open`: one of them is too near to a half for that.  Adding 1.5 2^23 rounds to the nearest integer,
+// halves to the even one, and leaves it in the low bits.
+//   bf16: with 8-bit significands, 127 x / most is a half exactly or off it by 1 / (254 * 255) of itself or more.  The binary32 product, off by 2^-22,
+//   is rounded to 20 bits first, which makes halves of all that are ones, and moves none of the others across one.
+//   fp32: the distance to the integer says whether a half is near.
+template <class T>
+__device__ __forceinline__ uint2 eight_steps(const float (&x)[8], float inv, bool& open) {
     constexpr float MAGIC = 12582912.f;
+    const uint64_t inv2 = ptx::pack_f32x2(inv, inv), magic2 = ptx::pack_f32x2(MAGIC, MAGIC), minus2 = ptx::pack_f32x2(-1.f, -1.f);
     uint32_t m[8];
-    float far = inv != 0.f ? 0.f : 1.f;
+    float far = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float t = fmaf(x[i], inv, MAGIC);
-        far = fmaxf(far, fabsf(fmaf(x[i], inv, -(t - MAGIC))));
-        m[i] = __float_as_uint(t);
-    }
-    if (far >= 0.4999f) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float t = __uint_as_float(m[i]) - MAGIC;
-            if (inv == 0.f || fabsf(fmaf(x[i], inv, -t)) >= 0.4999f) m[i] = static_cast<uint32_t>(exact_steps(x[i], most));
+    for (int i = 0; i < 8; i += 2) {
+        const uint64_t x2 = ptx::pack_f32x2(x[i], x[i + 1]);
+        uint64_t t2;
+        if (sizeof(T) == 2) {
+            const uint64_t p2 = ptx::mul_f32x2(x2, inv2), c2 = ptx::mul_f32x2(p2, ptx::pack_f32x2(17.f, 17.f));
+            const uint64_t hi2 = ptx::fma_f32x2(ptx::fma_f32x2(p2, minus2, c2), minus2, c2);          // c - (c - p): 20 bits of p
+            t2 = ptx::add_f32x2(hi2, magic2);
+        } else {
+            t2 = ptx::fma_f32x2(x2, inv2, magic2);
+            float off0, off1;
+            ptx::unpack_f32x2(ptx::fma_f32x2(x2, inv2, ptx::fma_f32x2(t2, minus2, magic2)), off0, off1);
+            far = ptx::max3_f32(far, fabsf(off0), fabsf(off1));
         }
+        float t0, t1;
+        ptx::unpack_f32x2(t2, t0, t1);
+        m[i] = __float_as_uint(t0);
+        m[i + 1] = __float_as_uint(t1);
     }
+    open = far >= NEAR_HALF;
     return make_uint2(__byte_perm(__byte_perm(m[0], m[1], 0x0040), __byte_perm(m[2], m[3], 0x0040), 0x5410),
                       __byte_perm(__byte_perm(m[4], m[5], 0x0040), __byte_perm(m[6], m[7], 0x0040), 0x5410));
 }
+// eight values that binary32 alone does not settle, read once more; a call of its own, so that its registers are not the kernel's
+template <class T>
+__device__ __noinline__ void settle_eight(const T* x, int8_t* q, float inv, float most) {
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) q[i] = static_cast<int8_t>(steps_of(to_float(x[i]), inv, most));
+}
 
-// Rows of up to 2048 WARPS values in whole eights, on 16-byte boundaries: WARPS warps each, one pass, the values kept in registers.
-constexpr int EIGHTS = 8;                // per lane
-template <class T, int WARPS>
-__global__ void __launch_bounds__(THREADS) quantize_rows_kernel(const T* X, long long ldX, int rows, int d, int8_t* Xq, long long ldq, int pad, float* scale,
+// Rows of up to 256 EIGHTS WARPS values in whole eights, on 16-byte boundaries: WARPS warps each, one pass, the values kept in registers.  Bound by HBM
+// where rows are many; four CTAs on an SM keep enough loads under way (128256 x 2048: 155 us with four, 177 with three, 184 with five).
+constexpr int MOST_EIGHTS = 8;           // per lane
+template <class T, int WARPS, int EIGHTS>
+__global__ void __launch_bounds__(THREADS, sizeof(T) == 2 || EIGHTS < MOST_EIGHTS ? 4 : 2) quantize_rows_kernel(const T* X, long long ldX, int rows, int d, int8_t* Xq, long long ldq, int pad, float* scale,
                                                                 const CallSetup setup) {
     constexpr int PER_CTA = THREADS / 32 / WARPS;
     __shared__ unsigned s_most[THREADS / 32];
@@ -195,15 +225,26 @@ __global__ void __launch_bounds__(THREADS) quantize_rows_kernel(const T* X, long
     if (!on) return;
     const float most = __uint_as_float(bits);
     const bool finite = bits < 0x7f800000u, any = finite && bits != 0u;
-    const float inv = any && most > 1.0e-30f ? 127.f / most : 0.f;
+    const float inv = any ? inverse_step(most) : 0.f;
     int8_t* q = Xq + r * ldq;
+    unsigned open = 0;                   // eights still to be settled
 #pragma unroll
     for (int i = 0; i < EIGHTS; ++i) {
         const int g = first + 32 * WARPS * i;
         if (g >= n) break;
         float f[8];
         x[i].values(f);
-        *reinterpret_cast<uint2*>(q + 8 * g) = any ? eight_steps(f, inv, most) : make_uint2(0u, 0u);
+        bool near;
+        const uint2 b = eight_steps<T>(f, inv, near);
+        *reinterpret_cast<uint2*>(q + 8 * g) = any ? b : make_uint2(0u, 0u);
+        open |= near || inv == 0.f ? 1u << i : 0u;
+    }
+    if (any) {
+        while (open != 0) {
+            const int g = first + 32 * WARPS * (__ffs(open) - 1);
+            open &= open - 1;
+            settle_eight(X + r * ldX + 8 * g, q + 8 * g, inv, most);
+        }
     }
     if (warp % WARPS == 0 && lane == 0) {
         if (pad > d) *reinterpret_cast<uint2*>(q + d) = make_uint2(0u, 0u);          // the other half of 16 bytes
