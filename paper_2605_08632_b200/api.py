@@ -387,29 +387,38 @@ _I8_LINEAR, _I8_LINEAR_BWD, _I8_CE, _I8_CE_BWD = range(4)
 
 
 def _rows(name, t, dtypes, device=None):
-    """Refuses what is no matrix of one of the types with contiguous rows, on `device` or any GPU."""
+    """Refuses what is no matrix of one of the types with contiguous rows, on `device` or any GPU; returns its row pitch."""
     if t.dim() != 2:
         raise ValueError(f"{name} must have two dimensions, got {tuple(t.shape)}")
     if t.dtype not in dtypes:
         raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be on a CUDA device; there is no CPU path")
-    _check(name, t, t.shape, t.dtype, t.device if device is None else device, rows_only=True)
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    (rows, cols), (pitch, step) = t.shape, t.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and pitch < cols):
+        raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    return pitch if rows > 1 else cols
 
 
 def quantize_rows(X):
     """Rows of X [rows, d] as 8-bit integers with a scale each (cat_i8_quantize): (q [rows, d] int8, scale [rows] fp32), X about
     q * scale.  bfloat16 or float32; the rows of q lie a multiple of 16 bytes apart, as the products want them."""
-    X = X.detach()
-    _rows("X", X, _I8_CODE)
+    pitch = _rows("X", X, _I8_CODE)
     rows, d = X.shape
     if d == 0:
         raise ValueError("X must have columns")
-    q = torch.empty(rows, (d + 15) // 16 * 16, dtype=torch.int8, device=X.device)
-    scale = torch.empty(rows, dtype=torch.float32, device=X.device)
+    dev, ld = X.device, (d + 15) // 16 * 16
+    q = torch.empty(rows, ld, dtype=torch.int8, device=dev)
+    scale = torch.empty(rows, dtype=torch.float32, device=dev)
     if rows:
-        _on(X.device, B.cat_i8_quantize, X, _I8_CODE[X.dtype], rows, d, _pitch(X), q, q.shape[1], scale)
-    return q[:, :d], scale
+        _on(dev, B.cat_i8_quantize, X, _I8_CODE[X.dtype], rows, d, pitch, q, ld, scale)
+    return q if ld == d else q[:, :d], scale
+
+
+def _on_16_bytes(t):
+    return t if t.data_ptr() % 16 == 0 else t.clone()
 
 
 @functools.lru_cache(maxsize=512)
@@ -454,40 +463,46 @@ class Int8Head(torch.nn.Module):
             _check("bias", bias, (self.V,), torch.float32, q.device)
         _check("scale", scale, (self.V,), torch.float32, q.device)
         ld = (self.d + 15) // 16 * 16
-        in_place = _pitch(q) == ld and q.data_ptr() % 16 == 0 and q.storage_offset() + self.V * ld <= q.untyped_storage().nbytes()
+        in_place = q.stride(0) == ld and q.data_ptr() % 16 == 0 and q.storage_offset() + self.V * ld <= q.untyped_storage().nbytes()
         if in_place:
             padded = q.as_strided((self.V, ld), (ld, 1))
         else:
             padded = torch.zeros(self.V, ld, dtype=torch.int8, device=q.device)
             padded[:, :self.d] = q
         self.register_buffer("q", padded.detach())
-        self.register_buffer("scale", scale.detach())
-        self.register_buffer("bias", None if bias is None else bias.detach())
+        self.register_buffer("scale", _on_16_bytes(scale.detach()))
+        self.register_buffer("bias", None if bias is None else _on_16_bytes(bias.detach()))
         self.slab_mib = slab_mib
 
-    def _head(self, X, dtypes=tuple(_I8_CODE)):
-        """Checks the head as it is now (a module may have been moved or cast) and X against it."""
-        _check("q", self.q, (self.V, (self.d + 15) // 16 * 16), torch.int8, self.q.device)
-        _check("scale", self.scale, (self.V,), torch.float32, self.q.device)
-        if self.bias is not None:
-            _check("bias", self.bias, (self.V,), torch.float32, self.q.device)
-        _rows("X", X, dtypes, self.q.device)
+    def _head(self):
+        """q, scale and bias as they are now: a module may have been moved or cast."""
+        held = self._buffers                    # (a module's attributes take their time)
+        q, scale, bias = held["q"], held["scale"], held["bias"]
+        dev = q.device
+        if q.dtype != torch.int8 or scale.dtype != torch.float32 or scale.device != dev or (
+                bias is not None and (bias.dtype != torch.float32 or bias.device != dev)):
+            raise TypeError("an 8-bit head is int8 with fp32 scales and biases on one device: it may be moved, not cast")
+        return q, scale, bias, dev
+
+    def _tokens(self, X, dev, dtypes=_I8_CODE):
+        """Checks X; its row pitch."""
+        pitch = _rows("X", X, dtypes, dev)
         if X.shape[1] != self.d:
             raise ValueError(f"X must have {self.d} columns, got {X.shape[1]}")
+        return pitch
 
-    def _call(self, which, entry, T, ldX, x_dtype, args, ldY=None, y_dtype=B.CAT_BF16):
+    def _call(self, which, entry, dev, T, ldX, x_dtype, args, ldY=None, y_dtype=B.CAT_BF16):
         if T == 0:
             return
         shape, n = _i8_plan(which, T, self.d, self.V, ldX, ldY, x_dtype, y_dtype, self.slab_mib)
-        _on(self.q.device, entry, shape, *args, torch.empty(n, dtype=torch.uint8, device=self.q.device))
+        _on(dev, entry, shape, *args, torch.empty(n, dtype=torch.uint8, device=dev))
 
     def logits(self, X, out_dtype=None):
         """[T, V] in out_dtype (X's unless given).  Where V is not in whole 16 bytes the rows lie further apart than V."""
-        self._head(X)
         out_dtype = X.dtype if out_dtype is None else out_dtype
         if out_dtype not in _I8_CODE:
             raise TypeError("logits are bfloat16 or float32")
-        if torch.is_grad_enabled() and X.requires_grad:
+        if X.requires_grad and torch.is_grad_enabled():
             self._refuse_capture(X)
             return _Int8LogitsFn.apply(X, self, out_dtype)
         return self._logits(X, out_dtype)
@@ -495,52 +510,60 @@ class Int8Head(torch.nn.Module):
     forward = logits
 
     def _logits(self, X, out_dtype):
-        T, ldY = X.shape[0], (self.V + 7) // 8 * 8
-        Y = torch.empty(T, ldY, dtype=out_dtype, device=X.device)
-        self._call(_I8_LINEAR, B.cat_i8_linear_fwd, T, _pitch(X), _I8_CODE[X.dtype], (X, self.q, self.scale, self.bias, Y), ldY, _I8_CODE[out_dtype])
-        return Y if ldY == self.V else Y[:, :self.V]
+        q, scale, bias, dev = self._head()
+        ldX = self._tokens(X, dev)
+        T, V = X.shape[0], self.V
+        ldY = (V + 7) // 8 * 8
+        Y = torch.empty(T, ldY, dtype=out_dtype, device=dev)
+        self._call(_I8_LINEAR, B.cat_i8_linear_fwd, dev, T, ldX, _I8_CODE[X.dtype], (X, q, scale, bias, Y), ldY, _I8_CODE[out_dtype])
+        return Y if ldY == V else Y[:, :V]
 
     def logits_backward(self, dY):
         """dX [T, d] bfloat16 for the upstream gradient of the logits, [T, V] bfloat16.  Its rows have to lie whole 16 bytes apart."""
-        _rows("dY", dY, (torch.bfloat16,), self.q.device)
+        q, scale, _, dev = self._head()
+        ldY = _rows("dY", dY, (torch.bfloat16,), dev)
         if dY.shape[1] != self.V:
             raise ValueError(f"dY must have {self.V} columns, got {dY.shape[1]}")
         T = dY.shape[0]
-        ldY = dY.stride(0) if T > 1 else (self.V + 7) // 8 * 8
-        dX = torch.empty(T, self.d, dtype=torch.bfloat16, device=dY.device)
-        self._call(_I8_LINEAR_BWD, B.cat_i8_linear_bwd, T, self.d, B.CAT_BF16, (dY, self.q, self.scale, dX), ldY)
+        ldY = ldY if T > 1 else (self.V + 7) // 8 * 8
+        dX = torch.empty(T, self.d, dtype=torch.bfloat16, device=dev)
+        self._call(_I8_LINEAR_BWD, B.cat_i8_linear_bwd, dev, T, self.d, B.CAT_BF16, (dY, q, scale, dX), ldY)
         return dX
 
-    def _rowwise(self, T, labels, valid, **f32):
-        _check("labels", labels, (T,), torch.int64, self.q.device)
+    @staticmethod
+    def _rowwise(T, dev, labels, valid, **f32):
+        shape = (T,)
+        _check("labels", labels, shape, torch.int64, dev)
         if valid is not None:
-            _check("valid", valid, (T,), torch.uint8, self.q.device)
+            _check("valid", valid, shape, torch.uint8, dev)
         for name, t in f32.items():
-            _check(name, t, (T,), torch.float32, self.q.device)
+            _check(name, t, shape, torch.float32, dev)
 
     def loss_forward(self, X, labels, valid=None):
         """(nll [T], lse [T]) without a graph for autograd."""
+        q, scale, _, dev = self._head()
+        ldX = self._tokens(X, dev)
         valid, T = _mask(valid), X.shape[0]
-        self._head(X)
-        self._rowwise(T, labels, valid)
-        nll, lse = (torch.empty(T, dtype=torch.float32, device=X.device) for _ in range(2))
-        self._call(_I8_CE, B.cat_i8_ce_fwd, T, _pitch(X), _I8_CODE[X.dtype], (X, self.q, self.scale, labels, valid, nll, lse))
+        self._rowwise(T, dev, labels, valid)
+        nll = torch.empty(T, dtype=torch.float32, device=dev)
+        lse = torch.empty(T, dtype=torch.float32, device=dev)
+        self._call(_I8_CE, B.cat_i8_ce_fwd, dev, T, ldX, _I8_CODE[X.dtype], (X, q, scale, labels, valid, nll, lse))
         return nll, lse
 
     def loss_backward(self, X, labels, valid, grad_nll, nll, lse):
         """dX [T, d] for the upstream gradient of nll; nll and lse: those of loss_forward on the same rows."""
+        q, scale, _, dev = self._head()
+        ldX = self._tokens(X, dev, (torch.bfloat16,))
         valid, T = _mask(valid), X.shape[0]
-        self._head(X, (torch.bfloat16,))
-        self._rowwise(T, labels, valid, grad_nll=grad_nll, nll=nll, lse=lse)
-        dX = torch.empty(T, self.d, dtype=X.dtype, device=X.device)
-        self._call(_I8_CE_BWD, B.cat_i8_ce_bwd, T, _pitch(X), B.CAT_BF16, (X, self.q, self.scale, labels, valid, nll, lse, grad_nll, dX))
+        self._rowwise(T, dev, labels, valid, grad_nll=grad_nll, nll=nll, lse=lse)
+        dX = torch.empty(T, self.d, dtype=torch.bfloat16, device=dev)
+        self._call(_I8_CE_BWD, B.cat_i8_ce_bwd, dev, T, ldX, B.CAT_BF16, (X, q, scale, labels, valid, nll, lse, grad_nll, dX))
         return dX
 
     def loss(self, X, labels, valid=None):
         """nll [T] fp32: the cross entropy of each row with its label, 0 for rows that are masked or whose label is no token id.  What
         is made of them (means, weights) is the caller's."""
-        if torch.is_grad_enabled() and X.requires_grad:
-            self._head(X, (torch.bfloat16,))
+        if X.requires_grad and torch.is_grad_enabled():
             self._refuse_capture(X)
             return _Int8LossFn.apply(X, labels, valid, self)
         return self.loss_forward(X, labels, valid)[0]

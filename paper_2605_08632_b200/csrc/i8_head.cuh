@@ -416,10 +416,10 @@ struct EpiCe {
         const float* sx;           // [T]
         const float* sw;           // [V]
         const long long* labels;   // [T]
-        float* part_m;             // [2 n_groups][part_stride]
+        float* part_m;             // [T][parts]
         float* part_l;
         float* z_label;            // [T], in units of log2
-        long long part_stride;
+        int parts;                 // 2 n_groups
         int T, V;
     };
     struct State {
@@ -467,55 +467,44 @@ struct EpiCe {
     __device__ static __forceinline__ int out_rows(const Params&) { return 0; }
     __device__ static __forceinline__ void end_item(const Params& p, const State& s, int group) {
         if (s.row >= p.T) return;
-        const long long at = (2 * group + static_cast<int>((threadIdx.x - 64) >> 7)) * p.part_stride + s.row;
+        const long long at = static_cast<long long>(s.row) * p.parts + 2 * group + static_cast<int>((threadIdx.x - 64) >> 7);
         p.part_m[at] = s.r.m;
         p.part_l[at] = s.r.l;
     }
 };
 
-// The parts of each row and what follows from them; z_label is read for rows with a label only.  32 rows per CTA, the parts dealt to its warps
-// and joined in order.
-constexpr int MERGE_ROWS = 32;
-__global__ void __launch_bounds__(THREADS) merge_kernel(const float* part_m, const float* part_l, const float* z_label, int S, long long stride, int T, int V,
+// The parts of each row, [T][S], and what follows from them; z_label is read for rows with a label only.  One warp per row: its lanes share the parts out
+// and are joined in a fixed order.
+__global__ void __launch_bounds__(THREADS) merge_kernel(const float* part_m, const float* part_l, const float* z_label, int S, int T, int V,
                                                         const long long* labels, const unsigned char* valid, float* nll, float* lse) {
-    __shared__ float s_m[THREADS / 32][MERGE_ROWS], s_l[THREADS / 32][MERGE_ROWS];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int r = blockIdx.x * MERGE_ROWS + lane;
+    const int lane = threadIdx.x & 31, r = blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
     ptx::grid_dependency_wait();
-    float m = LOW2, l = 0.f;
-    if (r < T) {
-#pragma unroll 4
-        for (int s = warp; s < S; s += THREADS / 32) {
-            const float pm = part_m[s * stride + r], pl = part_l[s * stride + r], m_new = fmaxf(m, pm);
-            l = fmaf(l, exp2f(m - m_new), pl * exp2f(pm - m_new));
-            m = m_new;
-        }
-    }
-    s_m[warp][lane] = m;
-    s_l[warp][lane] = l;
-    __syncthreads();
-    if (warp != 0 || r >= T) return;
+    if (r >= T) return;
+    const float *pm = part_m + static_cast<long long>(r) * S, *pl = part_l + static_cast<long long>(r) * S;
+    float m = LOW2;
+    for (int s = lane; s < S; s += 32) m = fmaxf(m, pm[s]);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+    float l = 0.f;
+    for (int s = lane; s < S; s += 32) l = fmaf(pl[s], exp2f(pm[s] - m), l);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+    if (lane != 0) return;
     if (valid != nullptr && valid[r] == 0) {
         nll[r] = lse[r] = 0.f;
         return;
     }
-#pragma unroll
-    for (int i = 1; i < THREADS / 32; ++i) m = fmaxf(m, s_m[i][lane]);
-    l = 0.f;
-#pragma unroll
-    for (int i = 0; i < THREADS / 32; ++i) l = fmaf(s_l[i][lane], exp2f(s_m[i][lane] - m), l);
-    constexpr double LN2 = 0.69314718055994530942;
-    const double others = LN2 * (static_cast<double>(m) + log2(static_cast<double>(l)));
+    constexpr float LN2 = 0.693147180559945309f;
     const long long y = labels[r];
     if (y < 0 || y >= V) {
         nll[r] = 0.f;
-        lse[r] = static_cast<float>(others);
+        lse[r] = LN2 * (m + log2f(l));
         return;
     }
-    const double zy = LN2 * static_cast<double>(z_label[r]), over = others - zy;
-    const double n = over > 0.0 ? over + log1p(exp(-over)) : log1p(exp(over));
-    nll[r] = static_cast<float>(n);
-    lse[r] = static_cast<float>(zy + n);
+    const float zy = z_label[r], over = LN2 * ((m - zy) + log2f(l));
+    const float n = over > 0.f ? over + log1pf(expf(-over)) : log1pf(expf(over));
+    nll[r] = n;
+    lse[r] = fmaf(LN2, zy, n);
 }
 
 // ------------------------------------------------------------------------------ gradient
@@ -651,6 +640,7 @@ __global__ void __launch_bounds__(THREADS) add_parts_kernel(const float* part, i
     const float f = factor ? factor[r] : 1.f;
     for (int i = threadIdx.x * 4; i < d; i += THREADS * 4) {
         float4 s = *reinterpret_cast<const float4*>(part + r * d + i);
+#pragma unroll 8
         for (int k = 1; k < g; ++k) {
             const float4 x = *reinterpret_cast<const float4*>(part + k * stride + r * d + i);
             s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;

@@ -386,12 +386,12 @@ int cat_i8_ce_fwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, co
         gc = launch_skinny_i8<i8::SKINNY_CE>(p, status, sm_count, &parts, st);
     } else {
         i8::EpiCe::Params ep;
-        ep.sx = h.sx; ep.sw = h.sw; ep.labels = y; ep.part_m = part_m; ep.part_l = part_l; ep.z_label = z_label; ep.part_stride = h.T; ep.T = h.T; ep.V = h.V;
+        ep.sx = h.sx; ep.sw = h.sw; ep.labels = y; ep.part_m = part_m; ep.part_l = part_l; ep.z_label = z_label; ep.parts = parts; ep.T = h.T; ep.V = h.V;
         gc = launch_i8<i8::EpiCe>(h, ep, plan.S, status, sm_count, st, nullptr);
     }
     if (gc != CAT_OK) return gc;
-    return launch_ahead(i8::merge_kernel, dim3(static_cast<unsigned>(cdiv(h.T, i8::MERGE_ROWS)), 1, 1), i8::THREADS, 0, st, static_cast<const float*>(part_m),
-                        static_cast<const float*>(part_l), static_cast<const float*>(z_label), parts, static_cast<long long>(h.T), h.T, h.V, y, valid, nll, lse);
+    return launch_ahead(i8::merge_kernel, dim3(static_cast<unsigned>(cdiv(h.T, i8::THREADS / 32)), 1, 1), i8::THREADS, 0, st, static_cast<const float*>(part_m),
+                        static_cast<const float*>(part_l), static_cast<const float*>(z_label), parts, h.T, h.V, y, valid, nll, lse);
 }
 
 int cat_i8_ce_bwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, const float* w_scale, const int64_t* labels,

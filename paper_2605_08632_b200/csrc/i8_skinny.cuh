@@ -26,7 +26,7 @@ struct SkinnyParams {
     const float *nll, *lse, *g;
     const int* most;
     float* factor;
-    float *part_m, *part_l, *z_label;      // [gridDim.x][T]
+    float *part_m, *part_l, *z_label;      // [T][gridDim.x] parts, [T]
     int n;                           // tokens rounded up to 16
     int tile_rows;                   // vocabulary entries per tile: 64, 96 or 128
     int n_tiles, num_kb, stages;
@@ -282,8 +282,8 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
                 for (int q = 1; q < 4; ++q) m = fmaxf(m, s_m[q][i]);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) l = fmaf(s_l[q][i], exp2f(s_m[q][i] - m), l);
-                p.part_m[static_cast<long long>(blockIdx.x) * T + i] = m;
-                p.part_l[static_cast<long long>(blockIdx.x) * T + i] = l;
+                p.part_m[i * gridDim.x + blockIdx.x] = m;
+                p.part_l[i * gridDim.x + blockIdx.x] = l;
             }
         }
     }
