@@ -41,21 +41,31 @@ struct I8Plan {
     size_t off_q, off_s, off_m, off_l, off_zy, off_factor, off_w16, off_part, off_z, total;
 };
 
-// Parts of the vocabulary that grad_kernel's CTAs share out: about 340 ns per slice of the longest, four slices' worth for filling the ring, the tile written
-// out and read back.
-int grad_parts(long long rows, long long d, long long V) {
-    const long long tiles = cdiv(d, i8::GRAD_COLS), slices = cdiv(V, i8::GRAD_SLICE);
-    const double out = static_cast<double>(rows) * static_cast<double>(d) * 4.0e-6;           // slices' worth of time per part
-    int best = 1;
+// How grad_kernel goes about its rows: units of columns per CTA, tiles of rows, and the parts its CTAs cut the vocabulary into: about 500 ns per slice of
+// the longest part, four slices' worth for filling the ring, the parts written out and read back.
+struct GradPlan {
+    bool head_m;
+    int units, tiles, n, num_kb, parts;
+};
+GradPlan plan_grad(long long rows, long long d, long long V) {
+    GradPlan p;
+    p.head_m = rows > 256;
+    p.units = p.head_m ? 1 : 2;
+    p.tiles = rows > 128 ? 2 : 1;
+    p.n = rows > 128 && !p.head_m ? 128 : static_cast<int>(cdiv(cdiv(rows, p.tiles), 16) * 16);
+    p.num_kb = static_cast<int>(cdiv(V, i8::GRAD_SLICE));
+    const long long tiles = cdiv(d, i8::GRAD_COLS * p.units);
+    const double out = static_cast<double>(rows) * static_cast<double>(d) * 3.0e-6;           // slices' worth of time per part
     double best_cost = 1e300;
-    for (long long g = 1; g <= kPlanSMs && g <= slices; ++g) {
-        const double cost = static_cast<double>(cdiv(tiles * g, kPlanSMs)) * static_cast<double>(cdiv(slices, g) + 4) + out * static_cast<double>(g);
-        if (cost < best_cost) { best_cost = cost; best = static_cast<int>(g); }
+    p.parts = 1;
+    for (long long g = 1; g <= kPlanSMs && g <= p.num_kb; ++g) {
+        const double cost = static_cast<double>(cdiv(tiles * g, kPlanSMs)) * static_cast<double>(cdiv(p.num_kb, g) + 4) + out * static_cast<double>(g);
+        if (cost < best_cost) { best_cost = cost; p.parts = static_cast<int>(g); }
     }
-    return best;
+    return p;
 }
 size_t dx_part_bytes(long long rows, long long d, long long V, bool widen) {
-    return widen ? dh_part_bytes(rows, d, V) : align256(sizeof(float) * grad_parts(rows, d, V) * static_cast<size_t>(rows) * d);
+    return widen ? dh_part_bytes(rows, d, V) : align256(sizeof(float) * plan_grad(rows, d, V).parts * static_cast<size_t>(rows) * d);
 }
 
 I8Plan plan_i8(const cat_i8_shape* s, int pass) {
@@ -247,9 +257,9 @@ int launch_skinny_i8(i8::SkinnyParams p, int* status, int sm_count, int* n_parts
     return launch_skinny_i8_as<MODE, 64, 2, 2>(tmW, tmX, p, status, grid, st);
 }
 
-template <bool SCALED, int TMEM>
+template <bool SCALED, int TMEM, int UNITS, bool HEAD_M>
 int launch_grad_as(const CUtensorMap& tmW, const CUtensorMap& tmA, const i8::GradParams& p, int* status, dim3 grid, cudaStream_t st) {
-    auto kern = i8::grad_kernel<SCALED, TMEM>;
+    auto kern = i8::grad_kernel<SCALED, TMEM, UNITS, HEAD_M>;
     static std::atomic<unsigned long long> allowed{0};
     if (!allow_smem(kern, i8::GRAD_SMEM, allowed)) return CAT_ERR_CUDA;
     return launch_ahead(kern, grid, i8::GRAD_THREADS, i8::GRAD_SMEM, st, tmW, tmA, p, status);
@@ -258,24 +268,22 @@ int launch_grad_as(const CUtensorMap& tmW, const CUtensorMap& tmA, const i8::Gra
 // dX[r, :] = factor[r] sum_v A[r, v] W[v, :] of up to 512 rows, the head widened on its way.
 template <bool SCALED>
 int launch_grad(const i8::Head& h, const void* A, long long ldA, const float* factor, __nv_bfloat16* dX, long long lddX, float* part, int* status, cudaStream_t st) {
+    const GradPlan plan = plan_grad(h.T, h.d, h.V);
     i8::GradParams p;
     p.sw = h.sw; p.part = part; p.T = h.T; p.V = h.V; p.d = h.d;
-    p.mmas = h.T > 256 ? 2 : 1;
-    p.n = static_cast<int>(cdiv(cdiv(h.T, p.mmas), 16) * 16);
-    p.num_kb = static_cast<int>(cdiv(h.V, i8::GRAD_SLICE));
-    p.stages = (i8::GRAD_SMEM - 1024 - i8::GRAD_WIDE * i8::GRAD_WIDE_BYTES) / (i8::GRAD_W_BYTES + p.mmas * p.n * 128);
+    p.n = plan.n; p.tiles = plan.tiles; p.num_kb = plan.num_kb;
+    const int a_bytes = plan.n * 128, slack = plan.n < 128 ? 128 * 128 - a_bytes : 0;           // the last slot's MMA reads 128 rows
+    p.stages = (i8::GRAD_SMEM - 1024 - i8::GRAD_WIDE_BYTES - slack) / (plan.units * i8::GRAD_UNIT_BYTES + plan.tiles * a_bytes);
     if (p.stages > i8::GRAD_MAX_STAGES) p.stages = i8::GRAD_MAX_STAGES;
     p.wait_ns = tc::WAIT_LIMIT_NS;
-    const int parts = grad_parts(h.T, h.d, h.V);
     CUtensorMap tmW, tmA;
     if (tmap_i8(&tmW, h.wq, h.V, h.d, h.ldw, i8::GRAD_SLICE, false) != CAT_OK || tmap_k_major(&tmA, A, h.T, h.V, ldA, p.n) != CAT_OK) return CAT_ERR_CUDA;
-    const dim3 grid(static_cast<unsigned>(cdiv(h.d, i8::GRAD_COLS)), static_cast<unsigned>(parts), 1);
-    const int cols = p.mmas * p.n;
-    const int rc = cols <= 32    ? launch_grad_as<SCALED, 32>(tmW, tmA, p, status, grid, st)
-                   : cols <= 128 ? launch_grad_as<SCALED, 128>(tmW, tmA, p, status, grid, st)
-                                 : launch_grad_as<SCALED, 512>(tmW, tmA, p, status, grid, st);
+    const dim3 grid(static_cast<unsigned>(cdiv(h.d, i8::GRAD_COLS * plan.units)), static_cast<unsigned>(plan.parts), 1);
+    const int rc = plan.head_m       ? launch_grad_as<SCALED, 512, 1, true>(tmW, tmA, p, status, grid, st)
+                   : plan.tiles == 2 ? launch_grad_as<SCALED, 512, 2, false>(tmW, tmA, p, status, grid, st)
+                                     : launch_grad_as<SCALED, 256, 2, false>(tmW, tmA, p, status, grid, st);
     if (rc != CAT_OK) return rc;
-    return launch_ahead(i8::add_parts_kernel, dim3(static_cast<unsigned>(h.T), 1, 1), i8::THREADS, 0, st, static_cast<const float*>(part), parts,
+    return launch_ahead(i8::add_parts_kernel, dim3(static_cast<unsigned>(h.T), 1, 1), i8::THREADS, 0, st, static_cast<const float*>(part), plan.parts,
                         static_cast<long long>(h.T) * h.d, h.d, factor, dX, lddX);
 }
 
