@@ -502,13 +502,15 @@ int launch_tc_cg(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorM
     cfg.blockDim = dim3(tc::THREADS_OF<Epi>, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = CG;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = tc::StartsAhead<Epi>::value ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, kern, tmA, tmB, tmOut, sched, ep, status) != cudaSuccess) {
         cudaGetLastError();
         return CAT_ERR_CUDA;

@@ -666,6 +666,14 @@ struct OperandOf<i8::EpiOutHalf> { static constexpr Operand value = Operand::F16
 template <bool F32>
 struct EpiSets<i8::EpiLinear<F32>> { static constexpr int value = 2; };
 template <bool F32>
+struct StartsAhead<i8::EpiLinear<F32>> { static constexpr bool value = true; };
+template <>
+struct StartsAhead<i8::EpiCe> { static constexpr bool value = true; };
+template <>
+struct StartsAhead<i8::EpiDz> { static constexpr bool value = true; };
+template <>
+struct LetsNextStart<i8::EpiCe> { static constexpr bool value = true; };       // merge_kernel
+template <bool F32>
 struct LooksAhead<i8::EpiLinear<F32>> { static constexpr bool value = true; };
 template <>
 struct LooksAhead<i8::EpiCe> { static constexpr bool value = true; };

@@ -614,6 +614,10 @@ constexpr int THREADS_OF = NUM_THREADS + 128 * (EpiSets<Epi>::value - 1);
 template <class Epi>
 struct LooksAhead { static constexpr bool value = false; };
 
+// Whether the GEMM is launched ahead of the end of the kernel before it, for which it then waits itself.
+template <class Epi>
+struct StartsAhead { static constexpr bool value = false; };
+
 // Whether a kernel behind the GEMM may run beside it (see lp::norm_kernel).
 template <class Epi>
 struct LetsNextStart { static constexpr bool value = false; };
@@ -729,6 +733,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
         ptx::prefetch_tmap(&tmA);
         ptx::prefetch_tmap(&tmB);
         ptx::prefetch_tmap(&tmOut);
+    }
+    if constexpr (StartsAhead<Epi>::value) ptx::grid_dependency_wait();
+    if (threadIdx.x == 0) {
         // pairs are numbered die by die where the device's map is known (neighbouring workers share operand tiles)
         if (claimed && leader) ctl.worker = static_cast<uint32_t>(die::claim_worker(sched.claims, sched.serial, worker, n_workers));
     }
