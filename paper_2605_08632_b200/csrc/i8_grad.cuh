@@ -44,6 +44,7 @@ struct GradParams {
     int tiles;             // boxes of them
     int num_kb;            // slices of the vocabulary
     int stages;            // 2 or more
+    int first;             // no kernel of the call runs before this one
     unsigned long long wait_ns;
 };
 
@@ -65,6 +66,8 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     const int n_iter = static_cast<int>((static_cast<long long>(blockIdx.y) + 1) * p.num_kb / gridDim.y) - kb0;
     const int col0 = blockIdx.x * N;
     if (threadIdx.x == 0) {
+        // where this is the call's first kernel, it clears the status: long before a wait of any CTA can run out
+        if (p.first && blockIdx.x == 0 && blockIdx.y == 0) *status = 0;
         ptx::prefetch_tmap(&tmW);
         ptx::prefetch_tmap(&tmA);
         for (int i = 0; i < p.stages; ++i) {

@@ -610,7 +610,10 @@ struct EpiDz {
 
 // The head as the 16-bit operand of the gradient's contraction: its integers in fp16 (exact), or scale * integer in bf16.
 template <bool SCALED>
-__global__ void __launch_bounds__(THREADS) widen_kernel(const int8_t* wq, long long ldw, const float* sw, long long units, int per_row, int d, uint16_t* out) {
+__global__ void __launch_bounds__(THREADS) widen_kernel(const int8_t* wq, long long ldw, const float* sw, long long units, int per_row, int d, uint16_t* out,
+                                                        const CallSetup setup) {
+    ptx::launch_dependents();
+    set_up_call(setup, -1);
     for (long long u = blockIdx.x * static_cast<long long>(THREADS) + threadIdx.x; u < units; u += static_cast<long long>(gridDim.x) * THREADS) {
         const long long v = u / per_row;
         const int i = static_cast<int>(u - v * per_row) * 8;              // 8 integers: d is a multiple of 8
@@ -649,8 +652,9 @@ __global__ void __launch_bounds__(THREADS) add_parts_kernel(const float* part, i
     }
 }
 
-// the plain output of a contraction of fp16 operands
+// the plain output of a contraction of fp16 operands, and of bf16 ones, behind other kernels of the call
 struct EpiOutHalf : tc::EpiOutT<false> {};
+struct EpiOutBehind : tc::EpiOutT<false> {};
 
 }  // namespace i8
 
@@ -665,6 +669,10 @@ template <>
 struct OperandOf<i8::EpiOutHalf> { static constexpr Operand value = Operand::F16; };
 template <bool F32>
 struct EpiSets<i8::EpiLinear<F32>> { static constexpr int value = 2; };
+template <>
+struct StartsAhead<i8::EpiOutHalf> { static constexpr bool value = true; };
+template <>
+struct StartsAhead<i8::EpiOutBehind> { static constexpr bool value = true; };
 template <bool F32>
 struct StartsAhead<i8::EpiLinear<F32>> { static constexpr bool value = true; };
 template <>

@@ -156,7 +156,14 @@ int quantize(const void* X, int dtype, long long rows, long long d, long long ld
                              : launch_quantize(static_cast<const float*>(X), rows, d, ldX, Xq, ldq, pad, scale, setup, st);
 }
 
-// What every pass begins with: the checks that are alike, the header cleared, the tokens as integers.
+i8::CallSetup header_setup(uint8_t* ws) {
+    i8::CallSetup setup = {};
+    setup.header = reinterpret_cast<int*>(ws);
+    setup.header_ints = kHeaderBytes / sizeof(int);
+    return setup;
+}
+
+// What every pass begins with: the checks that are alike, the header cleared and the tokens as integers where there are any.
 int begin_i8(const cat_i8_shape* s, int pass, const I8Plan& plan, const void* X, const int8_t* Wq, const float* w_scale, void* workspace,
              size_t workspace_bytes, int* sm_count, i8::Head* h, cudaStream_t st) {
     if (misaligned(X, s->x_dtype == CAT_BF16 ? 2 : 4) || misaligned(Wq, 16) || misaligned(w_scale, 16)) return CAT_ERR_ALIGN;
@@ -168,13 +175,8 @@ int begin_i8(const cat_i8_shape* s, int pass, const I8Plan& plan, const void* X,
     h->sx = reinterpret_cast<float*>(ws + plan.off_s);
     h->wq = Wq; h->sw = w_scale; h->ldw = s->ldW;
     h->T = static_cast<int>(s->T); h->V = static_cast<int>(s->V); h->d = static_cast<int>(s->d);
-    if (pass == kI8LinearBwd) {
-        if (cudaMemsetAsync(ws, 0, kHeaderBytes, st) != cudaSuccess) { cudaGetLastError(); return CAT_ERR_CUDA; }
-        return CAT_OK;
-    }
-    i8::CallSetup setup = {};
-    setup.header = reinterpret_cast<int*>(ws);
-    setup.header_ints = kHeaderBytes / sizeof(int);
+    if (pass == kI8LinearBwd) return CAT_OK;
+    i8::CallSetup setup = header_setup(ws);
     if (pass == kI8CeBwd) { setup.sw = w_scale; setup.V = h->V; setup.most = reinterpret_cast<int*>(ws + kMostOffset); }
     return quantize(X, s->x_dtype, s->T, s->d, s->ldX, reinterpret_cast<int8_t*>(ws + plan.off_q), plan.ldq, plan.ldq,
                     reinterpret_cast<float*>(ws + plan.off_s), setup, st);
@@ -262,12 +264,17 @@ int launch_grad_as(const CUtensorMap& tmW, const CUtensorMap& tmA, const i8::Gra
     auto kern = i8::grad_kernel<SCALED, TMEM, UNITS, HEAD_M>;
     static std::atomic<unsigned long long> allowed{0};
     if (!allow_smem(kern, i8::GRAD_SMEM, allowed)) return CAT_ERR_CUDA;
+    if (p.first) {           // what the head or dY comes from may still be running: no launch ahead of that
+        kern<<<grid, i8::GRAD_THREADS, i8::GRAD_SMEM, st>>>(tmW, tmA, p, status);
+        return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+    }
     return launch_ahead(kern, grid, i8::GRAD_THREADS, i8::GRAD_SMEM, st, tmW, tmA, p, status);
 }
 
 // dX[r, :] = factor[r] sum_v A[r, v] W[v, :] of up to 512 rows, the head widened on its way.
 template <bool SCALED>
 int launch_grad(const i8::Head& h, const void* A, long long ldA, const float* factor, __nv_bfloat16* dX, long long lddX, float* part, int* status, cudaStream_t st) {
+    const bool first = SCALED;           // dY and the head are the call's inputs
     const GradPlan plan = plan_grad(h.T, h.d, h.V);
     i8::GradParams p;
     p.sw = h.sw; p.part = part; p.T = h.T; p.V = h.V; p.d = h.d;
@@ -275,6 +282,7 @@ int launch_grad(const i8::Head& h, const void* A, long long ldA, const float* fa
     const int a_bytes = plan.n * 128, slack = plan.n < 128 ? 128 * 128 - a_bytes : 0;           // the last slot's MMA reads 128 rows
     p.stages = (i8::GRAD_SMEM - 1024 - i8::GRAD_WIDE_BYTES - slack) / (plan.units * i8::GRAD_UNIT_BYTES + plan.tiles * a_bytes);
     if (p.stages > i8::GRAD_MAX_STAGES) p.stages = i8::GRAD_MAX_STAGES;
+    p.first = first;
     p.wait_ns = tc::WAIT_LIMIT_NS;
     CUtensorMap tmW, tmA;
     if (tmap_i8(&tmW, h.wq, h.V, h.d, h.ldw, i8::GRAD_SLICE, false) != CAT_OK || tmap_k_major(&tmA, A, h.T, h.V, ldA, p.n) != CAT_OK) return CAT_ERR_CUDA;
@@ -288,10 +296,10 @@ int launch_grad(const i8::Head& h, const void* A, long long ldA, const float* fa
 }
 
 template <bool SCALED>
-int launch_widen(const i8::Head& h, uint16_t* w16, int sm_count, cudaStream_t st) {
+int launch_widen(const i8::Head& h, uint16_t* w16, const i8::CallSetup& setup, int sm_count, cudaStream_t st) {
     const int per_row = h.d / 8;
     i8::widen_kernel<SCALED><<<static_cast<unsigned>(8 * sm_count), i8::THREADS, 0, st>>>(h.wq, h.ldw, h.sw, static_cast<long long>(h.V) * per_row, per_row,
-                                                                                          h.d, w16);
+                                                                                          h.d, w16, setup);
     return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
 }
 
@@ -363,9 +371,9 @@ int cat_i8_linear_bwd(const cat_i8_shape* shape, const void* dY, const int8_t* W
         return launch_grad<true>(h, dY, shape->ldY, nullptr, static_cast<__nv_bfloat16*>(dX), shape->lddX, reinterpret_cast<float*>(ws + plan.off_part),
                                  reinterpret_cast<int*>(ws), st);
     uint16_t* w16 = reinterpret_cast<uint16_t*>(ws + plan.off_w16);
-    const int wc = launch_widen<true>(h, w16, sm_count, st);
+    const int wc = launch_widen<true>(h, w16, header_setup(ws), sm_count, st);
     if (wc != CAT_OK) return wc;
-    return launch_dx<tc::EpiOut>(dY, shape->ldY, w16, shape->T, shape->d, shape->V, nullptr, static_cast<__nv_bfloat16*>(dX), shape->lddX,
+    return launch_dx<i8::EpiOutBehind>(dY, shape->ldY, w16, shape->T, shape->d, shape->V, nullptr, static_cast<__nv_bfloat16*>(dX), shape->lddX,
                                  reinterpret_cast<float*>(ws + plan.off_part), reinterpret_cast<int*>(ws), sm_count, st);
 }
 
@@ -424,7 +432,7 @@ int cat_i8_ce_bwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, co
     float* part = reinterpret_cast<float*>(ws + plan.off_part);
     int* status = reinterpret_cast<int*>(ws);
     if (plan.widen) {
-        const int wc = launch_widen<false>(h, w16, sm_count, st);
+        const int wc = launch_widen<false>(h, w16, i8::CallSetup{}, sm_count, st);
         if (wc != CAT_OK) return wc;
     }
     for (long long r0 = 0; r0 < shape->T; r0 += plan.Ts) {

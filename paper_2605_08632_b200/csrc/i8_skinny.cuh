@@ -148,7 +148,8 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
         __syncwarp();
     } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2;
-        const int tok0 = half * TPW, T = p.h.T;
+        const int T = p.h.T;
+        const auto token = [&](int c) { return (c * HALVES + half) * 32; };      // first token of this warp's chunk c: dealt in turn, so that no set idles
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
         ptx::grid_dependency_wait();
         float up = 0.f, down = 0.f;
@@ -172,14 +173,14 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
             s_tok[t] = v;
         }
         asm volatile("bar.sync 1, %0;" ::"n"(128 * HALVES) : "memory");
-        RowSums sums[TPW / 32];          // of token tok0 + 32 c + lane, over this warp's vocabulary entries
+        RowSums sums[TPW / 32];          // of token token(c) + lane, over this warp's vocabulary entries
         int label[TPW / 32];
         if (MODE == SKINNY_CE) {
 #pragma unroll
             for (int c = 0; c < TPW / 32; ++c) {
-                const float4 v = s_tok[tok0 + c * 32 + lane];
+                const float4 v = s_tok[token(c) + lane];
                 sums[c].m = LOW2; sums[c].l = 0.f; sums[c].a = v.x;
-                label[c] = tok0 + c * 32 + lane < T ? __float_as_int(v.y) : -1;
+                label[c] = token(c) + lane < T ? __float_as_int(v.y) : -1;
             }
         }
         uint32_t acc = 0, acc_phase = 0;
@@ -214,7 +215,7 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
                 const bool in_tile = t < p.n_tiles && quarter * 32 < p.tile_rows && v0 < p.h.V;        // the warp has vocabulary entries
 #pragma unroll
                 for (int c = 0; c < TPW / 32; ++c) {
-                    const int tok = tok0 + c * 32;
+                    const int tok = token(c);
                     if (!in_tile || tok >= T) continue;
                     uint32_t raw[32];
                     ptx::tmem_ld_32x32(lanes + (acc * SUB + j) * COLS + tok, raw);
@@ -271,8 +272,8 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
         if (MODE == SKINNY_CE) {
 #pragma unroll
             for (int c = 0; c < TPW / 32; ++c) {
-                s_m[quarter][tok0 + c * 32 + lane] = sums[c].m;
-                s_l[quarter][tok0 + c * 32 + lane] = sums[c].l;
+                s_m[quarter][token(c) + lane] = sums[c].m;
+                s_l[quarter][token(c) + lane] = sums[c].l;
             }
             asm volatile("bar.sync 1, %0;" ::"n"(128 * HALVES) : "memory");
             const int i = threadIdx.x - 64;
