@@ -344,7 +344,7 @@ int cat_i8_linear_fwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq
         return shape->y_dtype == CAT_F32 ? launch_skinny_i8<i8::SKINNY_F32>(p, status, sm_count, nullptr, st)
                                          : launch_skinny_i8<i8::SKINNY_BF16>(p, status, sm_count, nullptr, st);
     }
-    const long long whole = h.V >= 32 ? h.V / 32 * 32 : 8;        // nothing is sent where there is no whole chunk
+    const long long whole = h.V >= 32 ? h.V / 32 * 32 : 4;        // nothing is sent where there is no whole chunk
     CUtensorMap tmY;
     if (shape->y_dtype == CAT_F32) {
         if (tmap_out_f32(&tmY, Y, h.T, whole, shape->ldY) != CAT_OK) return CAT_ERR_CUDA;

@@ -1,4 +1,8 @@
 """cat_i8_quantize, cat_i8_linear_fwd / _bwd and cat_i8_ce_fwd / _bwd against the fp64 oracle, through the public classes; bounds in i8_util."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -95,6 +99,16 @@ def test_logits_match_oracle(T, d, V, x, y, bias):
     b = torch.randn(V, generator=torch.Generator().manual_seed(9)) if bias else None
     h = Int8Head.from_quantized(q.to(DEV), scale.to(DEV), None if b is None else b.to(DEV))
     check_logits(h.logits(X.to(DEV), y), X, q, scale, b, y)
+
+
+@pytest.mark.parametrize("T,V", [(200, 3), (300, 31), (129, 33), (140, 8), (600, 1)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_narrow_outputs_of_many_rows(T, V, dtype):
+    d = 72
+    q, scale = head(V, d)
+    X = tokens(T, d, BF)
+    b = torch.randn(V, generator=torch.Generator().manual_seed(9))
+    check_logits(Int8Head.from_quantized(q.to(DEV), scale.to(DEV), b.to(DEV)).logits(X.to(DEV), dtype), X, q, scale, b, dtype)
 
 
 def test_extreme_integers_add_up_exactly():
@@ -451,6 +465,49 @@ def test_captured_calls_follow_new_inputs(T):
             assert all(torch.equal(a, b) for a, b in zip(out, want))
 
 
+@pytest.mark.parametrize("T", [1, 70, 300, 900])
+def test_inputs_written_just_before_a_call(T):
+    """Weights, tokens and upstream gradients that the kernel right before a call writes: the call's kernels may not start on what was there."""
+    d, V, n = 512, 20000, 6
+    g = torch.Generator().manual_seed(1)
+    Ws = [(0.02 * torch.randn(V, d, generator=g)).to(BF).to(DEV) for _ in range(2)]
+    Xs = [torch.randn(T, d, generator=g).to(BF).to(DEV) for _ in range(2)]
+    dYs = [torch.randn(T, V, generator=g).to(BF).to(DEV) for _ in range(2)]
+    y = torch.randint(0, V, (T,), generator=g).to(DEV)
+    fresh = [Int8Head(W) for W in Ws]
+    want = []
+    for i in range(2):
+        nll, lse = fresh[i].loss_forward(Xs[i], y)
+        want.append((fresh[i].logits(Xs[i]), nll, lse, fresh[i].loss_backward(Xs[i], y, None, nll, nll, lse), fresh[i].logits_backward(dYs[i])))
+    torch.cuda.synchronize()
+    h = Int8Head(Ws[0])
+    X, dY = Xs[0].clone(), dYs[0].clone()
+
+    def requantise(i):
+        B.cat_i8_quantize(Ws[i], B.CAT_BF16, V, d, d, h.q, d, h.scale)
+
+    for k in range(n):
+        i = k % 2
+        requantise(1 - i)
+        requantise(i)
+        a = h.logits(Xs[i])
+        requantise(1 - i)
+        requantise(i)
+        b = h.logits_backward(dYs[i])
+        X.copy_(Xs[i])
+        nll, lse = h.loss_forward(X, y)
+        X.zero_()
+        X.copy_(Xs[i])
+        requantise(1 - i)
+        requantise(i)
+        c = h.loss_backward(X, y, None, nll, nll, lse)
+        dY.zero_()
+        dY.copy_(dYs[i])
+        e = h.logits_backward(dY)
+        for got, ref in zip((a, nll, lse, c, b, e), (*want[i][:4], want[i][4], want[i][4])):
+            assert torch.equal(got, ref)
+
+
 def test_capture_with_gradients_is_refused():
     q, scale = head(300, 64)
     h = Int8Head.from_quantized(q.to(DEV), scale.to(DEV))
@@ -485,3 +542,28 @@ def test_two_streams_at_once():
     for i in range(2):
         for r in got[i]:
             assert all(torch.equal(a, b) for a, b in zip(r, want[i]))
+
+
+def test_without_cta_pairs():
+    """The one-CTA form of the products (read once per process): a short run of its own."""
+    code = """
+import torch
+from oracle import i8_oracle as O
+import numpy as np
+import sys
+sys.path.insert(0, "tests")
+from test_i8_gpu import check_logits, check_problem, problem, DEV, BF
+from paper_2605_08632_b200.api import Int8Head
+for T, d, V in ((300, 264, 3001), (700, 128, 5000)):
+    q, scale, X, y, valid, g = problem(T, d, V)
+    h = Int8Head.from_quantized(q.to(DEV), scale.to(DEV))
+    check_problem(h, q, scale, X, y, valid, g)
+    check_logits(h.logits(X.to(DEV)), X, q, scale, None, BF)
+    dY = torch.ones(T, (V + 7) // 8 * 8, dtype=BF, device=DEV)[:, :V]
+    want = np.tile((q.double() * scale.double()[:, None]).sum(0).numpy(), (T, 1))
+    got = h.logits_backward(dY).double().cpu().numpy()
+    assert np.linalg.norm(got - want) <= 2.0 ** -7 * np.linalg.norm(want)
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, env=dict(os.environ, CAT_LOSS_CTA_PAIR="0", PYTHONPATH=root), capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout[-1000:] + r.stderr[-2000:]
