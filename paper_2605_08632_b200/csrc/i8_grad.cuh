@@ -43,7 +43,7 @@ struct GradParams {
     int n;                 // rows of A per box, a multiple of 16: up to 128, or with the head as M side up to 256
     int tiles;             // boxes of them
     int num_kb;            // slices of the vocabulary
-    int stages;            // 2 or more
+    int stages;            // 2 or more with the head as M side, else 3 or more
     int first;             // no kernel of the call runs before this one
     unsigned long long wait_ns;
 };
@@ -56,6 +56,9 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     static_assert(!HEAD_M || UNITS == 1, "128 columns are an M side");
     constexpr int WIDE = GRAD_WIDE_BYTES / (UNITS * 2 * GRAD_UNIT_BYTES);      // buffers of a stage's widened units
     static_assert(WIDE == 2 || WIDE == 4, "each group of warps has buffers of its own");
+    // With more stages than widened buffers the barrier that frees the stage a buffer was made from frees the buffer as well (it cannot complete again
+    // before the buffer is filled anew); a commit by itself costs the issuing thread 170 cycles.
+    constexpr bool SHORT_RING = HEAD_M;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ GradCtl ctl;
     const uint32_t wide = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, ring = wide + GRAD_WIDE_BYTES;
@@ -103,8 +106,7 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
                 const uint32_t full = ptx::smem_u32(&ctl.full[s]);
                 const int v = (kb0 + i) * GRAD_SLICE;
                 ptx::mbar_arrive_expect_tx(full, stage_bytes);
-#pragma unroll
-                for (int u = 0; u < UNITS; ++u) ptx::tma_load_2d(dst + u * GRAD_UNIT_BYTES, &tmW, col0 + u * GRAD_COLS, v, full);
+                ptx::tma_load_2d(dst, &tmW, col0, v, full);
                 if (i == 0) ptx::grid_dependency_wait();        // A comes from the kernel before this one
                 for (int j = 0; j < p.tiles; ++j) ptx::tma_load_2d(dst + UNITS * GRAD_UNIT_BYTES + j * a_bytes, &tmA, v, j * (HEAD_M ? p.n : 128), full);
                 ++issued;
@@ -140,8 +142,8 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
                         ptx::umma_bf16(tmem + m * (HEAD_M ? p.n : N), HEAD_M ? w_at : a_at, HEAD_M ? a_at : w_at, idesc, (i | j) != 0 ? 1u : 0u);
                     }
                 }
-                ptx::umma_commit(ptx::smem_u32(&ctl.wide_empty[w]));
                 ptx::umma_commit(ptx::smem_u32(&ctl.empty[s]));
+                if (SHORT_RING) ptx::umma_commit(ptx::smem_u32(&ctl.wide_empty[w]));
                 a += stage_bytes;
                 if (++s == p.stages) { s = 0; phase ^= 1u; a = ring + UNITS * GRAD_UNIT_BYTES; }
                 if (++w == WIDE) { w = 0; w_phase ^= 1u; }
@@ -156,7 +158,7 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
         // A lane's 16 columns are 16-byte pieces 2 (piece & 3) and the one after it of a 128-byte row, swizzled by the row (the same for all of its rows); the
         // second half of the lanes begins with the odd one, so that eight lanes write to eight different banks.
         const int odd = piece >> 2, c = 2 * (piece & 3);
-        const uint32_t from = row0 * GRAD_COLS + piece * 16, to = odd * tc::MN_ATOM_BYTES + row0 * 128;
+        const uint32_t from = row0 * N + piece * 16, to = odd * tc::MN_ATOM_BYTES + row0 * 128;
         const uint32_t first = to + (((c + odd) ^ (row0 & 7)) << 4), second = to + (((c + 1 - odd) ^ (row0 & 7)) << 4);
         bool ok = true;
         float next[4];
@@ -170,6 +172,7 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
         if (SCALED) scales_of(group);
         int s = group, w = group;
         uint32_t phase = 0, w_phase = 1;
+        uint32_t free_bar = 0, free_phase = 0;              // !SHORT_RING: of the stage that this group's buffer was last made from
         for (int i = group; i < n_iter; i += 2) {
             float scale[4];
             if (SCALED) {
@@ -177,16 +180,19 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
                 for (int q = 0; q < 4; ++q) scale[q] = next[q];
                 scales_of(i + 2);
             }
-            ok = tc::wait_bounded(ptx::smem_u32(&ctl.full[s]), phase, abort, status, p.wait_ns) &&
-                 tc::wait_bounded(ptx::smem_u32(&ctl.wide_empty[w]), w_phase, abort, status, p.wait_ns);
+            ok = tc::wait_bounded(ptx::smem_u32(&ctl.full[s]), phase, abort, status, p.wait_ns);
+            if (SHORT_RING) ok = ok && tc::wait_bounded(ptx::smem_u32(&ctl.wide_empty[w]), w_phase, abort, status, p.wait_ns);
+            else if (i >= 2) ok = ok && tc::wait_bounded(free_bar, free_phase, abort, status, p.wait_ns);
+            free_bar = ptx::smem_u32(&ctl.empty[s]);
+            free_phase = phase;
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
-                const uint32_t src = ring + s * stage_bytes + u * GRAD_UNIT_BYTES + from, dst = wide + (w * UNITS + u) * (2 * GRAD_UNIT_BYTES);
+                const uint32_t src = ring + s * stage_bytes + u * GRAD_COLS + from, dst = wide + (w * UNITS + u) * (2 * GRAD_UNIT_BYTES);
                 uint4 x[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) ptx::ld_shared_v4(src + q * 16 * GRAD_COLS, x[q]);
+                for (int q = 0; q < 4; ++q) ptx::ld_shared_v4(src + q * 16 * N, x[q]);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const uint32_t in[4] = {x[q].x ^ 0x80808080u, x[q].y ^ 0x80808080u, x[q].z ^ 0x80808080u, x[q].w ^ 0x80808080u};     // 0 .. 255

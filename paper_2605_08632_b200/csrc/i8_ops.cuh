@@ -182,14 +182,14 @@ int begin_i8(const cat_i8_shape* s, int pass, const I8Plan& plan, const void* X,
                     reinterpret_cast<float*>(ws + plan.off_s), setup, st);
 }
 
-// 8-bit operand [rows][d] with row pitch ld bytes: boxes of 128 bytes x box_rows, swizzled as the tensor cores want them or as they are.
-int tmap_i8(CUtensorMap* m, const void* base, long long rows, long long d, long long ld, int box_rows, bool swizzled = true) {
+// 8-bit operand [rows][d] with row pitch ld bytes: boxes of 128 bytes x box_rows, swizzled as the tensor cores want them, or of any width as they are.
+int tmap_i8(CUtensorMap* m, const void* base, long long rows, long long d, long long ld, int box_rows, int as_is = 0) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return CAT_ERR_CUDA;
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(ld)};
-    const cuuint32_t box[2] = {2 * tc::BK, static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(as_is > 0 ? as_is : 2 * tc::BK), static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
     const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          as_is > 0 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? CAT_OK : CAT_ERR_CUDA;
 }
@@ -285,7 +285,7 @@ int launch_grad(const i8::Head& h, const void* A, long long ldA, const float* fa
     p.first = first;
     p.wait_ns = tc::WAIT_LIMIT_NS;
     CUtensorMap tmW, tmA;
-    if (tmap_i8(&tmW, h.wq, h.V, h.d, h.ldw, i8::GRAD_SLICE, false) != CAT_OK || tmap_k_major(&tmA, A, h.T, h.V, ldA, p.n) != CAT_OK) return CAT_ERR_CUDA;
+    if (tmap_i8(&tmW, h.wq, h.V, h.d, h.ldw, i8::GRAD_SLICE, i8::GRAD_COLS * plan.units) != CAT_OK || tmap_k_major(&tmA, A, h.T, h.V, ldA, p.n) != CAT_OK) return CAT_ERR_CUDA;
     const dim3 grid(static_cast<unsigned>(cdiv(h.d, i8::GRAD_COLS * plan.units)), static_cast<unsigned>(plan.parts), 1);
     const int rc = plan.head_m       ? launch_grad_as<SCALED, 512, 1, true>(tmW, tmA, p, status, grid, st)
                    : plan.tiles == 2 ? launch_grad_as<SCALED, 512, 2, false>(tmW, tmA, p, status, grid, st)
