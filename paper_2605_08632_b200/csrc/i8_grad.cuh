@@ -10,7 +10,7 @@
 //   * the fp32 tile of rows x columns stays in tensor memory over the whole part; the parts are added in order by add_parts_kernel.
 // Up to 256 rows: they are the M side, in tiles of 128 however few there are, and the head the N side, 256 columns (an MMA with 128 columns of the head
 // as M side and a few rows as N side takes as long: 16 rows of 1024 x 151936 68 us that way, 63 this).  Above, where A leaves room for 128 columns
-// only, those are the M side and the rows the N side of two MMAs, in steps of 32 rows (300 rows 117 us, with rows as M side 169).
+// only, those are the M side and the rows the N side of two MMAs, in steps of 32 rows (300 rows 106 us, with rows as M side 169).
 // Bound by the handshakes around each 64 entries (barriers, commits) rather than by memory or the tensor cores: about 1000 cycles per slice.
 #pragma once
 #include "i8_head.cuh"
@@ -22,15 +22,14 @@ constexpr int GRAD_ROWS = 512;
 constexpr int GRAD_SLICE = 64;                       // vocabulary entries of a stage
 constexpr int GRAD_COLS = 128;                       // columns of dX of a unit
 constexpr int GRAD_UNIT_BYTES = GRAD_SLICE * GRAD_COLS;
-constexpr int GRAD_WIDE_BYTES = 64 * 1024;           // widened units in flight
-constexpr int GRAD_MAX_WIDE = 4;
+constexpr int GRAD_WIDE = 2;                         // buffers of a stage's widened units, one for each group of warps
 constexpr int GRAD_MAX_STAGES = 8;
 constexpr int GRAD_SMEM = 226 * 1024;
 constexpr int GRAD_THREADS = 320;
 
 struct GradCtl {
     unsigned long long full[GRAD_MAX_STAGES], empty[GRAD_MAX_STAGES];
-    unsigned long long wide_full[GRAD_MAX_WIDE], wide_empty[GRAD_MAX_WIDE];
+    unsigned long long wide_full[GRAD_WIDE], wide_empty[GRAD_WIDE];
     unsigned long long done, drain;
     uint32_t tmem_base;
     volatile int abort;
@@ -54,14 +53,13 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1)
 grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA, const GradParams p, int* status) {
     constexpr int N = UNITS * GRAD_COLS;           // columns of dX
     static_assert(!HEAD_M || UNITS == 1, "128 columns are an M side");
-    constexpr int WIDE = GRAD_WIDE_BYTES / (UNITS * 2 * GRAD_UNIT_BYTES);      // buffers of a stage's widened units
-    static_assert(WIDE == 2 || WIDE == 4, "each group of warps has buffers of its own");
+    constexpr int WIDE_BYTES = GRAD_WIDE * UNITS * 2 * GRAD_UNIT_BYTES;
     // With more stages than widened buffers the barrier that frees the stage a buffer was made from frees the buffer as well (it cannot complete again
     // before the buffer is filled anew); a commit by itself costs the issuing thread 170 cycles.
     constexpr bool SHORT_RING = HEAD_M;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ GradCtl ctl;
-    const uint32_t wide = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, ring = wide + GRAD_WIDE_BYTES;
+    const uint32_t wide = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, ring = wide + WIDE_BYTES;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // the slot of a tile of A holds its n rows; as M side the MMA reads 128, the last ones out of whatever follows, into accumulator lanes that nobody looks at
     const uint32_t a_bytes = static_cast<uint32_t>(p.n) * 128, stage_bytes = UNITS * GRAD_UNIT_BYTES + p.tiles * a_bytes;
@@ -77,7 +75,7 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
             ptx::mbar_init(ptx::smem_u32(&ctl.full[i]), 1);
             ptx::mbar_init(ptx::smem_u32(&ctl.empty[i]), 1);
         }
-        for (int i = 0; i < WIDE; ++i) {
+        for (int i = 0; i < GRAD_WIDE; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctl.wide_full[i]), 4);
             ptx::mbar_init(ptx::smem_u32(&ctl.wide_empty[i]), 1);
         }
@@ -146,7 +144,7 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
                 if (SHORT_RING) ptx::umma_commit(ptx::smem_u32(&ctl.wide_empty[w]));
                 a += stage_bytes;
                 if (++s == p.stages) { s = 0; phase ^= 1u; a = ring + UNITS * GRAD_UNIT_BYTES; }
-                if (++w == WIDE) { w = 0; w_phase ^= 1u; }
+                if (++w == GRAD_WIDE) { w = 0; w_phase ^= 1u; }
             }
             ptx::umma_commit(ok ? ptx::smem_u32(&ctl.done) : ptx::smem_u32(&ctl.drain));
             if (!ok) tc::wait_bounded<true>(ptx::smem_u32(&ctl.drain), 0, abort, status, tc::DRAIN_LIMIT_NS);      // no MMA may be in flight when TMEM is freed
@@ -170,7 +168,8 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
             }
         };
         if (SCALED) scales_of(group);
-        int s = group, w = group;
+        const int w = group;
+        int s = group;
         uint32_t phase = 0, w_phase = 1;
         uint32_t free_bar = 0, free_phase = 0;              // !SHORT_RING: of the stage that this group's buffer was last made from
         for (int i = group; i < n_iter; i += 2) {
@@ -217,8 +216,7 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
             if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl.wide_full[w]));
             s += 2;
             if (s >= p.stages) { s -= p.stages; phase ^= 1u; }
-            w += 2;
-            if (w >= WIDE) { w = group; w_phase ^= 1u; }
+            w_phase ^= 1u;
         }
         if (ok) {
             ok = tc::wait_bounded(ptx::smem_u32(&ctl.done), 0, abort, status, p.wait_ns);
@@ -242,19 +240,24 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
                     }
                 }
             }
+            // a lane is a row: 32 x 32 are turned over in the memory of the widened units (64 KB there), so that a store covers 128 bytes of one row
+            float* turn = reinterpret_cast<float*>(smem_raw + (wide - ptx::smem_u32(smem_raw))) + (warp - 2) * (32 * 33);
             for (int m = 0; !HEAD_M && m < p.tiles; ++m) {
-                const int r = m * 128 + quarter * 32 + lane;
-                float* out = p.part + (static_cast<long long>(blockIdx.y) * p.T + r) * p.d + col0;
+                const int r0 = m * 128 + quarter * 32, rows = min(32, p.T - r0);
+                float* out = p.part + (static_cast<long long>(blockIdx.y) * p.T + r0) * p.d + col0 + lane;
 #pragma unroll 1
-                for (int c = group * (N / 2); c < (group + 1) * (N / 2); c += 32) {
+                for (int c = group * (N / 2); c < (group + 1) * (N / 2) && col0 + c < p.d && rows > 0; c += 32) {
                     uint32_t v[32];
                     ptx::tmem_ld_32x32(lanes + m * N + c, v);
                     ptx::tmem_ld_wait(v);
+                    __syncwarp();
 #pragma unroll
-                    for (int q = 0; q < 32; q += 4)                 // d is a multiple of 8
-                        if (r < p.T && col0 + c + q < p.d)
-                            *reinterpret_cast<float4*>(out + c + q) = make_float4(__uint_as_float(v[q]), __uint_as_float(v[q + 1]), __uint_as_float(v[q + 2]),
-                                                                                  __uint_as_float(v[q + 3]));
+                    for (int q = 0; q < 32; ++q) turn[lane * 33 + q] = __uint_as_float(v[q]);
+                    __syncwarp();
+                    if (col0 + c + lane < p.d) {
+#pragma unroll 8
+                        for (int q = 0; q < rows; ++q) out[static_cast<long long>(q) * p.d + c] = turn[q * 33 + lane];
+                    }
                 }
             }
         }

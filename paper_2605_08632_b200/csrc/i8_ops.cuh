@@ -64,6 +64,14 @@ GradPlan plan_grad(long long rows, long long d, long long V) {
     }
     return p;
 }
+// Whether the gradient goes by a widened copy of the head: for more rows than grad_kernel takes, and where its rows leave it little room and the copy is small.
+// dX in us, copy / widened on its way: 512 rows of 1024 x 8000 21 / 31, of 1024 x 32000 53 / 55, of 2048 x 32000 96 / 90, of 1024 x 151936 205 / 186; 400 rows 22 / 25,
+// 54 / 39, 97 / 62, 198 / 125; 300 rows 20 / 20, 51 / 33, 95 / 52, 194 / 106; 16 rows 19 / 13, 42 / 21, 74 / 32, 154 / 61.
+bool use_widened_copy(long long rows, long long d, long long V) {
+    const long long weights = d * V;
+    return rows > i8::GRAD_ROWS || (rows > 440 && weights <= (1ll << 25)) || (rows > 300 && weights <= (1ll << 23));
+}
+
 size_t dx_part_bytes(long long rows, long long d, long long V, bool widen) {
     return widen ? dh_part_bytes(rows, d, V) : align256(sizeof(float) * plan_grad(rows, d, V).parts * static_cast<size_t>(rows) * d);
 }
@@ -74,7 +82,7 @@ I8Plan plan_i8(const cat_i8_shape* s, int pass) {
     p.ldq = cdiv(s->d, 16) * 16;
     p.Ts = s->T;
     p.skinny = s->T <= i8::SKINNY_ROWS;
-    p.widen = s->T > i8::GRAD_ROWS;
+    p.widen = use_widened_copy(s->T, s->d, s->V);
     size_t off = kHeaderBytes;
     if (pass != kI8LinearBwd) {
         p.off_q = off; off = align256(off + static_cast<size_t>(s->T) * p.ldq);
@@ -254,7 +262,6 @@ int launch_skinny_i8(i8::SkinnyParams p, int* status, int sm_count, int* n_parts
     int grid = sm_count < kPlanSMs ? sm_count : kPlanSMs;
     if (p.n_tiles < grid) grid = p.n_tiles;
     if (n_parts) *n_parts = grid;
-    if (p.h.T <= 32) return launch_skinny_i8_as<MODE, 32, 1, 1>(tmW, tmX, p, status, grid, st);
     if (p.h.T <= 64) return launch_skinny_i8_as<MODE, 32, 2, 2>(tmW, tmX, p, status, grid, st);
     return launch_skinny_i8_as<MODE, 64, 2, 2>(tmW, tmX, p, status, grid, st);
 }
@@ -280,7 +287,7 @@ int launch_grad(const i8::Head& h, const void* A, long long ldA, const float* fa
     p.sw = h.sw; p.part = part; p.T = h.T; p.V = h.V; p.d = h.d;
     p.n = plan.n; p.tiles = plan.tiles; p.num_kb = plan.num_kb;
     const int a_bytes = plan.n * 128, slack = plan.n < 128 ? 128 * 128 - a_bytes : 0;           // the last slot's MMA reads 128 rows
-    p.stages = (i8::GRAD_SMEM - 1024 - i8::GRAD_WIDE_BYTES - slack) / (plan.units * i8::GRAD_UNIT_BYTES + plan.tiles * a_bytes);
+    p.stages = (i8::GRAD_SMEM - 1024 - i8::GRAD_WIDE * plan.units * 2 * i8::GRAD_UNIT_BYTES - slack) / (plan.units * i8::GRAD_UNIT_BYTES + plan.tiles * a_bytes);
     if (p.stages > i8::GRAD_MAX_STAGES) p.stages = i8::GRAD_MAX_STAGES;
     p.first = first;
     p.wait_ns = tc::WAIT_LIMIT_NS;

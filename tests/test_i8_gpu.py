@@ -176,7 +176,8 @@ def test_nothing_finite_in_a_row_or_channel():
         assert not Y[3][~bad[3]].any() and not Y[:, 9][~bad[:, 9]].any()
 
 
-@pytest.mark.parametrize("T,d,V", [(1, 8, 1), (1, 2048, 5000), (3, 64, 100), (40, 200, 3001), (130, 264, 20000), (300, 1024, 2056), (700, 72, 513), (257, 512, 777)])
+@pytest.mark.parametrize("T,d,V", [(1, 8, 1), (1, 2048, 5000), (3, 64, 100), (40, 200, 3001), (130, 264, 20000), (300, 1024, 2056), (700, 72, 513), (257, 512, 777), (400, 72, 513),
+                                   (480, 256, 70000), (336, 128, 70001), (129, 520, 1003)])
 def test_logits_gradient_matches_oracle(T, d, V):
     q, scale = head(V, d, seed=V)
     g = torch.Generator().manual_seed(T)
@@ -221,7 +222,7 @@ def check_problem(h, q, scale, X, y, valid, g):
 
 
 CE_SIZES = [(1, 8, 1), (1, 64, 2), (1, 2048, 5003), (2, 8, 33), (3, 72, 256), (5, 128, 257), (37, 256, 8191), (130, 136, 20011), (257, 256, 12000),
-            (600, 128, 3000), (64, 1024, 9473), (300, 1024, 2056), (1025, 48, 300), (128, 2048, 19000), (17, 64, 30000)]
+            (600, 128, 3000), (64, 1024, 9473), (300, 1024, 2056), (1025, 48, 300), (128, 2048, 19000), (17, 64, 30000), (400, 72, 513), (450, 1032, 9000), (33, 1288, 700)]
 
 
 @pytest.mark.parametrize("T,d,V", CE_SIZES)
