@@ -531,20 +531,19 @@ class Int8Head(torch.nn.Module):
         return dX
 
     @staticmethod
-    def _rowwise(T, dev, labels, valid, **f32):
-        shape = (T,)
-        _check("labels", labels, shape, torch.int64, dev)
+    def _labels(T, dev, labels, valid):
+        _check("labels", labels, (T,), torch.int64, dev)
         if valid is not None:
-            _check("valid", valid, shape, torch.uint8, dev)
-        for name, t in f32.items():
-            _check(name, t, shape, torch.float32, dev)
+            valid = _mask(valid)
+            _check("valid", valid, (T,), torch.uint8, dev)
+        return valid
 
     def loss_forward(self, X, labels, valid=None):
         """(nll [T], lse [T]) without a graph for autograd."""
         q, scale, _, dev = self._head()
         ldX = self._tokens(X, dev)
-        valid, T = _mask(valid), X.shape[0]
-        self._rowwise(T, dev, labels, valid)
+        T = X.shape[0]
+        valid = self._labels(T, dev, labels, valid)
         nll = torch.empty(T, dtype=torch.float32, device=dev)
         lse = torch.empty(T, dtype=torch.float32, device=dev)
         self._call(_I8_CE, B.cat_i8_ce_fwd, dev, T, ldX, _I8_CODE[X.dtype], (X, q, scale, labels, valid, nll, lse))
@@ -554,8 +553,10 @@ class Int8Head(torch.nn.Module):
         """dX [T, d] for the upstream gradient of nll; nll and lse: those of loss_forward on the same rows."""
         q, scale, _, dev = self._head()
         ldX = self._tokens(X, dev, (torch.bfloat16,))
-        valid, T = _mask(valid), X.shape[0]
-        self._rowwise(T, dev, labels, valid, grad_nll=grad_nll, nll=nll, lse=lse)
+        T = X.shape[0]
+        valid = self._labels(T, dev, labels, valid)
+        for name, t in (("grad_nll", grad_nll), ("nll", nll), ("lse", lse)):
+            _check(name, t, (T,), torch.float32, dev)
         dX = torch.empty(T, self.d, dtype=torch.bfloat16, device=dev)
         self._call(_I8_CE_BWD, B.cat_i8_ce_bwd, dev, T, ldX, B.CAT_BF16, (X, q, scale, labels, valid, nll, lse, grad_nll, dX))
         return dX

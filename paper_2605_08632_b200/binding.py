@@ -362,33 +362,28 @@ def cat_i8_workspace_bytes(shape, which: int) -> int:
     return int(lib().cat_i8_workspace_bytes(ctypes.byref(shape), int(which)))
 
 
-def cat_i8_linear_fwd(shape, X, Wq, w_scale, bias, Y, workspace) -> None:
-    rc = lib().cat_i8_linear_fwd(ctypes.byref(shape), _ptr(X), _ptr(Wq), _ptr(w_scale), _ptr(bias), _ptr(Y), _ptr(workspace),
-                                 workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+def _i8_call(entry, shape, workspace, *tensors) -> None:
+    """The calls on an 8-bit head differ in their pointers only."""
+    rc = getattr(_lib or lib(), entry)(ctypes.byref(shape), *[None if t is None else t.data_ptr() for t in tensors],
+                                       None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, _stream())
     if rc != CAT_OK:
-        raise CatError(rc, "cat_i8_linear_fwd")
+        raise CatError(rc, entry)
+
+
+def cat_i8_linear_fwd(shape, X, Wq, w_scale, bias, Y, workspace) -> None:
+    _i8_call("cat_i8_linear_fwd", shape, workspace, X, Wq, w_scale, bias, Y)
 
 
 def cat_i8_linear_bwd(shape, dY, Wq, w_scale, dX, workspace) -> None:
-    rc = lib().cat_i8_linear_bwd(ctypes.byref(shape), _ptr(dY), _ptr(Wq), _ptr(w_scale), _ptr(dX), _ptr(workspace),
-                                 workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
-    if rc != CAT_OK:
-        raise CatError(rc, "cat_i8_linear_bwd")
+    _i8_call("cat_i8_linear_bwd", shape, workspace, dY, Wq, w_scale, dX)
 
 
 def cat_i8_ce_fwd(shape, X, Wq, w_scale, labels, valid, nll, lse, workspace) -> None:
-    rc = lib().cat_i8_ce_fwd(ctypes.byref(shape), _ptr(X), _ptr(Wq), _ptr(w_scale), _ptr(labels), _ptr(valid), _ptr(nll), _ptr(lse),
-                             _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
-    if rc != CAT_OK:
-        raise CatError(rc, "cat_i8_ce_fwd")
+    _i8_call("cat_i8_ce_fwd", shape, workspace, X, Wq, w_scale, labels, valid, nll, lse)
 
 
 def cat_i8_ce_bwd(shape, X, Wq, w_scale, labels, valid, nll, lse, grad_nll, dX, workspace) -> None:
-    rc = lib().cat_i8_ce_bwd(ctypes.byref(shape), _ptr(X), _ptr(Wq), _ptr(w_scale), _ptr(labels), _ptr(valid), _ptr(nll), _ptr(lse),
-                             _ptr(grad_nll), _ptr(dX), _ptr(workspace),
-                             workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
-    if rc != CAT_OK:
-        raise CatError(rc, "cat_i8_ce_bwd")
+    _i8_call("cat_i8_ce_bwd", shape, workspace, X, Wq, w_scale, labels, valid, nll, lse, grad_nll, dX)
 
 
 def cat_die_map():
