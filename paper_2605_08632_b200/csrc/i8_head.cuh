@@ -636,20 +636,32 @@ __global__ void __launch_bounds__(THREADS) widen_kernel(const int8_t* wq, long l
     }
 }
 
-// Parts of a contraction, added in order; the row's factor; one rounding.
+// Parts of a contraction, added in a fixed order; the row's factor; one rounding.  A CTA has 256 columns of a row, four threads share the parts of four of them:
+// one by one they are mostly waited for (37 parts of 64 x 1024: 12 us by a thread each).
+constexpr int PART_COLS = 256, PART_SHARES = 4;
 __global__ void __launch_bounds__(THREADS) add_parts_kernel(const float* part, int g, long long stride, int d, const float* factor, __nv_bfloat16* out, long long ld) {
+    __shared__ float4 s_sum[PART_SHARES - 1][PART_COLS / 4];
     const long long r = blockIdx.x;
+    const int t = threadIdx.x & (PART_COLS / 4 - 1), share = threadIdx.x / (PART_COLS / 4), i = blockIdx.y * PART_COLS + t * 4;
     ptx::grid_dependency_wait();
-    const float f = factor ? factor[r] : 1.f;
-    for (int i = threadIdx.x * 4; i < d; i += THREADS * 4) {
-        float4 s = *reinterpret_cast<const float4*>(part + r * d + i);
-#pragma unroll 8
-        for (int k = 1; k < g; ++k) {
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i < d) {
+#pragma unroll 4
+        for (int k = share; k < g; k += PART_SHARES) {
             const float4 x = *reinterpret_cast<const float4*>(part + k * stride + r * d + i);
             s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
         }
-        *reinterpret_cast<uint2*>(out + r * ld + i) = make_uint2(ptx::pack_bf16x2(s.x * f, s.y * f), ptx::pack_bf16x2(s.z * f, s.w * f));
     }
+    if (share > 0) s_sum[share - 1][t] = s;
+    __syncthreads();
+    if (share > 0 || i >= d) return;
+#pragma unroll
+    for (int k = 0; k < PART_SHARES - 1; ++k) {
+        const float4 x = s_sum[k][t];
+        s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+    }
+    const float f = factor ? factor[r] : 1.f;
+    *reinterpret_cast<uint2*>(out + r * ld + i) = make_uint2(ptx::pack_bf16x2(s.x * f, s.y * f), ptx::pack_bf16x2(s.z * f, s.w * f));
 }
 
 // the plain output of a contraction of fp16 operands, and of bf16 ones, behind other kernels of the call

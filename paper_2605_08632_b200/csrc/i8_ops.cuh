@@ -211,6 +211,11 @@ int launch_i8(const i8::Head& h, const typename Epi::Params& ep, int n_groups, i
     return launch_tc<0, 0, Epi>(tmX, tmW, make_sched(h.T, h.V, slices, n_groups, band_tiles(slices), 0), ep, status, sm_count, st, out);
 }
 
+int launch_add_parts(const float* part, int g, long long stride, long long rows, long long d, const float* factor, __nv_bfloat16* dX, long long lddX, cudaStream_t st) {
+    return launch_ahead(i8::add_parts_kernel, dim3(static_cast<unsigned>(rows), static_cast<unsigned>(cdiv(d, i8::PART_COLS)), 1), i8::THREADS, 0, st, part, g, stride,
+                        static_cast<int>(d), factor, dX, lddX);
+}
+
 // dX[r, :] = factor[r] sum_v A[r, v] W16[v, :], A [rows, V] and W16 [V, d] of the type Epi multiplies; the vocabulary in parts for few rows.
 template <class Epi>
 int launch_dx(const void* A, long long ldA, const uint16_t* w16, long long rows, long long d, long long V, const float* factor, __nv_bfloat16* dX, long long lddX,
@@ -235,8 +240,7 @@ int launch_dx(const void* A, long long ldA, const uint16_t* w16, long long rows,
     if (tmap_out_f32(&tmO, part, ep.M, d, d) != CAT_OK) return CAT_ERR_CUDA;
     const int rc = launch_tc<0, 1, Epi>(tmA, tmW, sched, ep, status, sm_count, st, &tmO);
     if (rc != CAT_OK) return rc;
-    i8::add_parts_kernel<<<static_cast<unsigned>(rows), i8::THREADS, 0, st>>>(part, g, padded * d, static_cast<int>(d), factor, dX, lddX);
-    return cudaGetLastError() == cudaSuccess ? CAT_OK : CAT_ERR_CUDA;
+    return launch_add_parts(part, g, padded * d, rows, d, factor, dX, lddX, st);
 }
 
 template <int MODE, int TPW, int HALVES, int SUB>
@@ -298,8 +302,7 @@ int launch_grad(const i8::Head& h, const void* A, long long ldA, const float* fa
                    : plan.tiles == 2 ? launch_grad_as<SCALED, 512, 2, false>(tmW, tmA, p, status, grid, st)
                                      : launch_grad_as<SCALED, 256, 2, false>(tmW, tmA, p, status, grid, st);
     if (rc != CAT_OK) return rc;
-    return launch_ahead(i8::add_parts_kernel, dim3(static_cast<unsigned>(h.T), 1, 1), i8::THREADS, 0, st, static_cast<const float*>(part), plan.parts,
-                        static_cast<long long>(h.T) * h.d, h.d, factor, dX, lddX);
+    return launch_add_parts(part, plan.parts, static_cast<long long>(h.T) * h.d, h.T, h.d, factor, dX, lddX, st);
 }
 
 template <bool SCALED>
