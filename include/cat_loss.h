@@ -525,11 +525,12 @@ size_t cat_i8_workspace_bytes(const cat_i8_shape* shape, int pass);
  * with (xq, sx) the rows of X as cat_i8_quantize holds them (the call does that itself).  The sums are exact (int32 on the tensor
  * cores); the scales and the bias are applied in binary32 and the result is rounded once to y_dtype.
  *   X        [T, d] of x_dtype                                                     (device, in)
- *   Wq       [V, d] int8 (-128 .. 127), pitch ldW bytes;  w_scale  [V] fp32          (device, in)
- *   bias     [V] fp32 or NULL                                                       (device, in)
+ *   Wq       [V, d] int8 (-128 .. 127), pitch ldW bytes;  w_scale  [V] fp32, 16-byte aligned   (device, in)
+ *   bias     [V] fp32, 16-byte aligned, or NULL                                      (device, in)
  *   Y        [T, V] of y_dtype, pitch ldY; elements past V are left as they are       (device, out)
  *   workspace  at least cat_i8_workspace_bytes(shape, 0) bytes, 256-byte aligned; its first int32 holds the device status after the call
- * Calls that may overlap on the GPU need a workspace each.
+ * Two kernels.  Nothing is read on the host but shape, here and in the calls below: all may be captured into graphs.  Calls that may overlap
+ * on the GPU need a workspace each.
  */
 int cat_i8_linear_fwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, const float* w_scale, const float* bias, void* Y,
                       void* workspace, size_t workspace_bytes, void* cuda_stream);
@@ -538,7 +539,8 @@ int cat_i8_linear_fwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq
  * Gradient of the product with respect to its tokens, the head frozen and the tokens' rounding passed straight through:
  *     dX[t, i] = sum_v dY[t, v] w_scale[v] Wq[v, i].
  *   dY  [T, V] bf16, pitch ldY (device, in);  dX  [T, d] bf16, pitch lddX (device, out)
- * w_scale[v] Wq[v, :] is rounded to bf16 as the operand of the contraction, which is summed in binary32.
+ * w_scale[v] Wq[v, :] is rounded to bf16 as the operand of the contraction, which is summed in binary32.  For more than a few hundred rows the workspace
+ * holds the head in 16 bits (2 V d bytes), as it does in cat_i8_ce_bwd.
  */
 int cat_i8_linear_bwd(const cat_i8_shape* shape, const void* dY, const int8_t* Wq, const float* w_scale, void* dX,
                       void* workspace, size_t workspace_bytes, void* cuda_stream);

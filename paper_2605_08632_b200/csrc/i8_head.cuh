@@ -190,7 +190,8 @@ __device__ __noinline__ void settle_eight(const T* x, int8_t* q, float inv, floa
 }
 
 // Rows of up to 256 EIGHTS WARPS values in whole eights, on 16-byte boundaries: WARPS warps each, one pass, the values kept in registers.  Bound by HBM
-// where rows are many; four CTAs on an SM keep enough loads under way (128256 x 2048: 155 us with four, 177 with three, 184 with five).
+// where rows are many; four CTAs on an SM keep enough loads under way (128256 x 2048: 113 us, 7.0 TB/s; before halves were settled
+// without a branch 155 with four, 177 with three, 184 with five).
 constexpr int MOST_EIGHTS = 8;           // per lane
 template <class T, int WARPS, int EIGHTS>
 __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 || EIGHTS < MOST_EIGHTS ? 4 : 2) quantize_rows_kernel(const T* X, long long ldX, int rows, int d, int8_t* Xq, long long ldq, int pad, float* scale,
@@ -310,7 +311,7 @@ __device__ __forceinline__ void scaled(const uint32_t (&v)[32], float mine, floa
                                          ptx::pack_f32x2(__shfl_sync(0xffffffffu, mine, i), __shfl_sync(0xffffffffu, mine, i + 1))), f[i], f[i + 1]);
 }
 
-// The product itself.  Whole chunks of 32 columns leave through shared memory and TMA stores (the tensor map ends with them: a store that is cut
+// The product itself.  Bound by the traffic between L2 and the SMs where outputs are large: 1000 x 1024 x 151936 139 us, without stores 111.  Whole chunks of 32 columns leave through shared memory and TMA stores (the tensor map ends with them: a store that is cut
 // off at the vocabulary's end would still write whole 16 bytes), the last ones from the threads.
 template <bool F32>
 struct EpiLinear {
@@ -411,6 +412,7 @@ struct RowSums {
     }
 };
 
+// Cross entropy.  8192 x 2048 x 128256: 1240 us, 3.5 P operations a second, 2 % above the product without an epilogue; 8192 x 1024 x 151936: 846 us, 14 %.
 struct EpiCe {
     struct Params {
         const float* sx;           // [T]
@@ -608,7 +610,9 @@ struct EpiDz {
     }
 };
 
-// The head as the 16-bit operand of the gradient's contraction: its integers in fp16 (exact), or scale * integer in bf16.
+// The head as the 16-bit operand of the gradient's contraction: its integers in fp16 (exact), or scale * integer in bf16.  Bound by HBM: 86 us for
+// 1024 x 151936 (466 MB), 120 for 2048 x 128256.  (Beside the product of the gradient's terms, on what that leaves of the SMs, it does not fit: the step of
+// 4096 rows 2.8 -> 3.4 ms.)
 template <bool SCALED>
 __global__ void __launch_bounds__(THREADS) widen_kernel(const int8_t* wq, long long ldw, const float* sw, long long units, int per_row, int d, uint16_t* out,
                                                         const CallSetup setup) {

@@ -139,7 +139,7 @@ void launch_quantize_rows(const T* X, long long rows, long long d, long long ldX
 }
 
 // Rows of whole eights on 16-byte boundaries, up to 16384 long, are read once, by one warp each or, where they are long or few, by up to eight: the head of
-// 128256 x 2048 346 -> 155 us against a CTA per row that reads them twice.
+// 128256 x 2048 113 us, by a CTA per row that reads them twice 346.
 template <class T>
 int launch_quantize(const T* X, long long rows, long long d, long long ldX, int8_t* Xq, long long ldq, long long pad, float* scale, const i8::CallSetup& setup,
                     cudaStream_t st) {
