@@ -202,7 +202,7 @@ int tmap_i8(CUtensorMap* m, const void* base, long long rows, long long d, long 
     return r == CUDA_SUCCESS ? CAT_OK : CAT_ERR_CUDA;
 }
 
-// The product of h's tokens and head through epilogue Epi: n_groups runs of vocabulary tiles per row tile (0: every tile by itself).
+// The product of h's tokens and head through epilogue Epi: n_groups runs of vocabulary tiles per row tile.
 template <class Epi>
 int launch_i8(const i8::Head& h, const typename Epi::Params& ep, int n_groups, int* status, int sm_count, cudaStream_t st, const CUtensorMap* out) {
     CUtensorMap tmX, tmW;
@@ -243,14 +243,14 @@ int launch_dx(const void* A, long long ldA, const uint16_t* w16, long long rows,
     return launch_add_parts(part, g, padded * d, rows, d, factor, dX, lddX, st);
 }
 
-template <int MODE, int TPW, int HALVES, int SUB>
+template <int MODE, int TPW>
 int launch_skinny_i8_as(const CUtensorMap& tmW, const CUtensorMap& tmX, i8::SkinnyParams p, int* status, int grid, cudaStream_t st) {
-    p.stages = (skinny::SMEM_BYTES - 1024 - 8192) / ((SUB * p.tile_rows + p.n) * 128);
+    p.stages = (skinny::SMEM_BYTES - 1024 - 8192) / ((i8::SUB * p.tile_rows + p.n) * 128);
     if (p.stages > skinny::MAX_STAGES) p.stages = skinny::MAX_STAGES;
-    auto kern = i8::skinny_kernel<MODE, TPW, HALVES, SUB>;
+    auto kern = i8::skinny_kernel<MODE, TPW>;
     static std::atomic<unsigned long long> allowed{0};
     if (!allow_smem(kern, skinny::SMEM_BYTES, allowed)) return CAT_ERR_CUDA;
-    return launch_ahead(kern, dim3(static_cast<unsigned>(grid), 1, 1), 64 + 128 * HALVES, skinny::SMEM_BYTES, st, tmW, tmX, p, status);
+    return launch_ahead(kern, dim3(static_cast<unsigned>(grid), 1, 1), i8::SKINNY_THREADS, skinny::SMEM_BYTES, st, tmW, tmX, p, status);
 }
 
 // Up to 128 tokens against the head in the manner of MODE; p holds what that needs besides the sizes.
@@ -266,8 +266,8 @@ int launch_skinny_i8(i8::SkinnyParams p, int* status, int sm_count, int* n_parts
     int grid = sm_count < kPlanSMs ? sm_count : kPlanSMs;
     if (p.n_tiles < grid) grid = p.n_tiles;
     if (n_parts) *n_parts = grid;
-    if (p.h.T <= 64) return launch_skinny_i8_as<MODE, 32, 2, 2>(tmW, tmX, p, status, grid, st);
-    return launch_skinny_i8_as<MODE, 64, 2, 2>(tmW, tmX, p, status, grid, st);
+    if (p.h.T <= 64) return launch_skinny_i8_as<MODE, 32>(tmW, tmX, p, status, grid, st);
+    return launch_skinny_i8_as<MODE, 64>(tmW, tmX, p, status, grid, st);
 }
 
 template <bool SCALED, int TMEM, int UNITS, bool HEAD_M>

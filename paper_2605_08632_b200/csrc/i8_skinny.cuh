@@ -33,10 +33,12 @@ struct SkinnyParams {
     unsigned long long wait_ns;
 };
 
-// TPW, HALVES, SUB as in skinny::logits_kernel (two tiles of the head per slice of the tokens even for one token: 32 us for 1 x 1024 x 151936 with one,
-// 29 with two).  Threads: 64 + 128 HALVES.
-template <int MODE, int TPW, int HALVES, int SUB>
-__global__ void __launch_bounds__(64 + 128 * HALVES, 1)
+// TPW: tokens a warp looks after, a multiple of 32; HALVES sets of four epilogue warps; SUB tiles of the head per slice of the tokens, even for one token (32 us
+// for 1 x 1024 x 151936 with one tile and one set, 29 with two).
+constexpr int HALVES = 2, SUB = 2;
+constexpr int SKINNY_THREADS = 64 + 128 * HALVES;
+template <int MODE, int TPW>
+__global__ void __launch_bounds__(SKINNY_THREADS, 1)
 skinny_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const SkinnyParams p, int* status) {
     constexpr int COLS = TPW * HALVES;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -82,7 +84,7 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
             // slice `kb` of round t: the head's part, the tokens' part
             const auto load_w = [&](int t, int kb, int s) {
                 const uint32_t full = ptx::smem_u32(&ctl.full[s]), dst = ring + s * stage_bytes;
-                const int n_sub = SUB == 1 || t + static_cast<int>(gridDim.x) >= p.n_tiles ? 1 : SUB;      // the last round may have one tile
+                const int n_sub = t + static_cast<int>(gridDim.x) >= p.n_tiles ? 1 : SUB;      // the last round may have one tile
                 ptx::mbar_arrive_expect_tx(full, n_sub * a_bytes + b_bytes);
                 for (int j = 0; j < n_sub; ++j) ptx::tma_load_2d(dst + j * a_bytes, &tmW, kb * 128, (t + j * static_cast<int>(gridDim.x)) * p.tile_rows, full);
             };
@@ -128,7 +130,7 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
                     ptx::tc_fence_after();
                     const uint32_t at = ring + stage * stage_bytes;
                     const uint64_t ad = ptx::smem_desc_sw128(at, 16, 1024), bd = ptx::smem_desc_sw128(at + SUB * a_bytes, 16, 1024);
-                    const int n_sub = SUB == 1 || t + static_cast<int>(gridDim.x) >= p.n_tiles ? 1 : SUB;
+                    const int n_sub = t + static_cast<int>(gridDim.x) >= p.n_tiles ? 1 : SUB;
                     for (int i = 0; i < n_sub; ++i)
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
