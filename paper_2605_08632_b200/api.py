@@ -436,7 +436,7 @@ class Int8Head(torch.nn.Module):
     X [T, d] (bfloat16 or float32), which each call holds in 8 bits with a scale for each token:
 
         logits = head(X)                        the product, bfloat16 or float32, with `bias` [V] fp32 where there is one
-        nll = head.loss(X, labels, valid)       softmax cross entropy of each row (without the bias), in pieces of the vocabulary
+        nll = head.loss(X, labels, valid)       softmax cross entropy of each row, in pieces of the vocabulary (heads without a bias)
 
     Both carry gradients to bfloat16 X (the tokens' rounding is passed straight through).  Calls share nothing but the head: any lengths,
     streams and threads.  Not for stream capture with gradients: autograd may then wait for other streams inside the capture; capture
@@ -483,6 +483,12 @@ class Int8Head(torch.nn.Module):
                 bias is not None and (bias.dtype != torch.float32 or bias.device != dev)):
             raise TypeError("an 8-bit head is int8 with fp32 scales and biases on one device: it may be moved, not cast")
         return q, scale, bias, dev
+
+    def _without_bias(self):
+        q, scale, bias, dev = self._head()
+        if bias is not None:
+            raise ValueError("the loss is for heads without a bias")
+        return q, scale, dev
 
     def _tokens(self, X, dev, dtypes=_I8_CODE):
         """Checks X; its row pitch."""
@@ -540,7 +546,7 @@ class Int8Head(torch.nn.Module):
 
     def loss_forward(self, X, labels, valid=None):
         """(nll [T], lse [T]) without a graph for autograd."""
-        q, scale, _, dev = self._head()
+        q, scale, dev = self._without_bias()
         ldX = self._tokens(X, dev)
         T = X.shape[0]
         valid = self._labels(T, dev, labels, valid)
@@ -551,7 +557,7 @@ class Int8Head(torch.nn.Module):
 
     def loss_backward(self, X, labels, valid, grad_nll, nll, lse):
         """dX [T, d] for the upstream gradient of nll; nll and lse: those of loss_forward on the same rows."""
-        q, scale, _, dev = self._head()
+        q, scale, dev = self._without_bias()
         ldX = self._tokens(X, dev, (torch.bfloat16,))
         T = X.shape[0]
         valid = self._labels(T, dev, labels, valid)

@@ -113,6 +113,7 @@ struct Eight<__nv_bfloat16> {
     uint4 x;
     __device__ __forceinline__ void load(const __nv_bfloat16* p) { x = __ldg(reinterpret_cast<const uint4*>(p)); }
     __device__ __forceinline__ void clear() { x = make_uint4(0u, 0u, 0u, 0u); }
+    __device__ __forceinline__ void set(const uint32_t* w) { x = make_uint4(w[0], w[1], w[2], w[3]); }
     __device__ __forceinline__ unsigned most() const {          // of |x|, as float bits
         const unsigned m = __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
         return max(m << 16, m & 0xffff0000u);
@@ -134,6 +135,10 @@ struct Eight<float> {
         b = __ldg(reinterpret_cast<const float4*>(p) + 1);
     }
     __device__ __forceinline__ void clear() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void set(const uint32_t* w) {
+        a = make_float4(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3]));
+        b = make_float4(__uint_as_float(w[4]), __uint_as_float(w[5]), __uint_as_float(w[6]), __uint_as_float(w[7]));
+    }
     __device__ __forceinline__ void values(float (&f)[8]) const {
         f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
         f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
@@ -147,6 +152,56 @@ struct Eight<float> {
         return m;
     }
 };
+
+// Eight values at any address of their type: the whole 16-byte pieces around them, moved into place.  [lo, hi): the matrix; a piece that reaches past it (at
+// its first and last value only) is put together value by value.  Values from `count` on are zero.
+template <class T>
+__device__ __forceinline__ Eight<T> eight_at(const T* x, int count, uintptr_t lo, uintptr_t hi) {
+    constexpr int WORDS = 2 * sizeof(T), PIECES = WORDS / 4 + 1;          // of the eight; 16-byte pieces that they may touch
+    const uintptr_t at = reinterpret_cast<uintptr_t>(x), base = at & ~static_cast<uintptr_t>(15);
+    const unsigned shift = static_cast<unsigned>(at - base);
+    uint32_t w[4 * PIECES];
+#pragma unroll
+    for (int g = 0; g < PIECES; ++g) {
+        const uintptr_t p = base + 16 * g;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (p < at + count * sizeof(T)) {
+            if (p >= lo && p + 16 <= hi) {
+                v = __ldg(reinterpret_cast<const uint4*>(p));
+            } else {
+                uint32_t part[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+                for (int j = 0; j < static_cast<int>(16 / sizeof(T)); ++j) {
+                    const uintptr_t e = p + j * sizeof(T);
+                    if (e >= lo && e < hi) {
+                        if (sizeof(T) == 4) part[j & 3] = __ldg(reinterpret_cast<const uint32_t*>(e));
+                        else part[(j >> 1) & 3] |= static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t*>(e))) << (16 * (j & 1));
+                    }
+                }
+                v = make_uint4(part[0], part[1], part[2], part[3]);
+            }
+        }
+        w[4 * g] = v.x; w[4 * g + 1] = v.y; w[4 * g + 2] = v.z; w[4 * g + 3] = v.w;
+    }
+#pragma unroll
+    for (int k = 8; k >= 4; k -= 4)                                       // by two words, by one
+        if (shift & k) {
+#pragma unroll
+            for (int j = 0; j + k / 4 < 4 * PIECES; ++j) w[j] = w[j + k / 4];
+        }
+    if (sizeof(T) == 2 && (shift & 2)) {
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) w[j] = __funnelshift_r(w[j], w[j + 1], 16);
+    }
+#pragma unroll
+    for (int j = 0; j < WORDS; ++j) {
+        if (sizeof(T) == 4) w[j] = j < count ? w[j] : 0u;
+        else w[j] = 2 * j + 1 < count ? w[j] : 2 * j < count ? w[j] & 0xffffu : 0u;
+    }
+    Eight<T> r;
+    r.set(w);
+    return r;
+}
 
 // steps_of for eight values, as far as binary32 goes; `open`: one of them is too near to a half for that.  Adding 1.5 2^23 rounds to the nearest integer,
 // halves to the even one, and leaves it in the low bits.
@@ -184,16 +239,17 @@ __device__ __forceinline__ uint2 eight_steps(const float (&x)[8], float inv, boo
 }
 // eight values that binary32 alone does not settle, read once more; a call of its own, so that its registers are not the kernel's
 template <class T>
-__device__ __noinline__ void settle_eight(const T* x, int8_t* q, float inv, float most) {
+__device__ __noinline__ void settle_eight(const T* x, int8_t* q, int count, float inv, float most) {
 #pragma unroll 1
-    for (int i = 0; i < 8; ++i) q[i] = static_cast<int8_t>(steps_of(to_float(x[i]), inv, most));
+    for (int i = 0; i < count; ++i) q[i] = static_cast<int8_t>(steps_of(to_float(x[i]), inv, most));
 }
 
-// Rows of up to 256 EIGHTS WARPS values in whole eights, on 16-byte boundaries: WARPS warps each, one pass, the values kept in registers.  Bound by HBM
+// Rows of up to 256 EIGHTS WARPS values: WARPS warps each, one pass, the values kept in registers.  ANY: of any length and at any address, else whole eights
+// on 16-byte boundaries.  The integers' rows begin on 8-byte boundaries.  Bound by HBM
 // where rows are many; four CTAs on an SM keep enough loads under way (128256 x 2048: 113 us, 7.0 TB/s; before halves were settled
 // without a branch 155 with four, 177 with three, 184 with five).
 constexpr int MOST_EIGHTS = 8;           // per lane
-template <class T, int WARPS, int EIGHTS>
+template <class T, int WARPS, int EIGHTS, bool ANY>
 __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 || EIGHTS < MOST_EIGHTS ? 4 : 2) quantize_rows_kernel(const T* X, long long ldX, int rows, int d, int8_t* Xq, long long ldq, int pad, float* scale,
                                                                 const CallSetup setup) {
     constexpr int PER_CTA = THREADS / 32 / WARPS;
@@ -204,15 +260,17 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 || EIGHTS < MOST_EIGHT
     if (static_cast<int>(blockIdx.x) >= row_ctas) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long r = static_cast<long long>(blockIdx.x) * PER_CTA + warp / WARPS;
-    const int first = (warp % WARPS) * 32 + lane, n = d >> 3;        // this lane's eights: first + 32 WARPS i
+    const int first = (warp % WARPS) * 32 + lane, n = ANY ? (d + 7) >> 3 : d >> 3;        // this lane's eights: first + 32 WARPS i
     const bool on = r < rows;
     Eight<T> x[EIGHTS];
     unsigned bits = 0;
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(X), hi = reinterpret_cast<uintptr_t>(X + (rows - 1) * ldX + d);
 #pragma unroll
     for (int i = 0; i < EIGHTS; ++i) {
         const int g = first + 32 * WARPS * i;
-        if (on && g < n) x[i].load(X + r * ldX + 8 * g);
-        else x[i].clear();
+        if (!on || g >= n) x[i].clear();
+        else if (!ANY) x[i].load(X + r * ldX + 8 * g);
+        else x[i] = eight_at(X + r * ldX + 8 * g, min(8, d - 8 * g), lo, hi);
     }
 #pragma unroll
     for (int i = 0; i < EIGHTS; ++i) bits = max(bits, x[i].most());
@@ -236,19 +294,26 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 || EIGHTS < MOST_EIGHT
         float f[8];
         x[i].values(f);
         bool near;
-        const uint2 b = eight_steps<T>(f, inv, near);
-        *reinterpret_cast<uint2*>(q + 8 * g) = any ? b : make_uint2(0u, 0u);
+        uint2 b = eight_steps<T>(f, inv, near);
+        if (!any) b = make_uint2(0u, 0u);
+        if (!ANY || 8 * g + 8 <= pad) {
+            *reinterpret_cast<uint2*>(q + 8 * g) = b;
+        } else {                         // the last ones of a row whose padding is not to be written
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+                if (8 * g + j < d) q[8 * g + j] = static_cast<int8_t>((j < 4 ? b.x >> (8 * j) : b.y >> (8 * j - 32)) & 255u);
+        }
         open |= near || inv == 0.f ? 1u << i : 0u;
     }
     if (any) {
         while (open != 0) {
             const int g = first + 32 * WARPS * (__ffs(open) - 1);
             open &= open - 1;
-            settle_eight(X + r * ldX + 8 * g, q + 8 * g, inv, most);
+            settle_eight(X + r * ldX + 8 * g, q + 8 * g, ANY ? min(8, d - 8 * g) : 8, inv, most);
         }
     }
     if (warp % WARPS == 0 && lane == 0) {
-        if (pad > d) *reinterpret_cast<uint2*>(q + d) = make_uint2(0u, 0u);          // the other half of 16 bytes
+        if (pad > 8 * n) *reinterpret_cast<uint2*>(q + 8 * n) = make_uint2(0u, 0u);          // the other half of 16 bytes
         scale[r] = finite ? most / 127.f : __uint_as_float(0x7fc00000u);
     }
 }

@@ -132,26 +132,29 @@ int launch_ahead(void (*kern)(P...), dim3 grid, int threads, size_t smem, cudaSt
 
 template <class T, int WARPS>
 void launch_quantize_rows(const T* X, long long rows, long long d, long long ldX, int8_t* Xq, long long ldq, long long pad, float* scale,
-                          const i8::CallSetup& setup, int more, cudaStream_t st) {
+                          const i8::CallSetup& setup, int more, bool whole, cudaStream_t st) {
+    constexpr int FEW = i8::MOST_EIGHTS / 2;
     const unsigned ctas = static_cast<unsigned>(cdiv(rows, i8::THREADS / 32 / WARPS) + more);
-    auto kern = d > 128 * i8::MOST_EIGHTS * WARPS ? i8::quantize_rows_kernel<T, WARPS, i8::MOST_EIGHTS> : i8::quantize_rows_kernel<T, WARPS, i8::MOST_EIGHTS / 2>;
+    auto kern = !whole                   ? i8::quantize_rows_kernel<T, WARPS, FEW, true>
+                : d > 256 * FEW * WARPS ? i8::quantize_rows_kernel<T, WARPS, i8::MOST_EIGHTS, false> : i8::quantize_rows_kernel<T, WARPS, FEW, false>;
     kern<<<ctas, i8::THREADS, 0, st>>>(X, ldX, static_cast<int>(rows), static_cast<int>(d), Xq, ldq, static_cast<int>(pad), scale, setup);
 }
 
-// Rows of whole eights on 16-byte boundaries, up to 16384 long, are read once, by one warp each or, where they are long or few, by up to eight: the head of
-// 128256 x 2048 113 us, by a CTA per row that reads them twice 346.
+// Rows of whole eights on 16-byte boundaries, up to 16384 long, and others up to 8192 long are read once, by one warp each or, where they are long or few, by
+// up to eight: the head of 128256 x 2048 113 us, by a CTA per row that reads them twice 346; 151936 rows of 1003 bf16 values 144 and 414.
 template <class T>
 int launch_quantize(const T* X, long long rows, long long d, long long ldX, int8_t* Xq, long long ldq, long long pad, float* scale, const i8::CallSetup& setup,
                     cudaStream_t st) {
     const int more = setup.sw ? i8::MOST_PARTS : 0;
-    const bool whole = d % 8 == 0 && d <= 8 * 256 * i8::MOST_EIGHTS && ldX * sizeof(T) % 16 == 0 && !misaligned(X, 16) && ldq % 8 == 0 && !misaligned(Xq, 8);
-    if (whole) {
+    const bool whole = d % 8 == 0 && ldX * sizeof(T) % 16 == 0 && !misaligned(X, 16);
+    const long long per_warp = 256 * (whole ? i8::MOST_EIGHTS : i8::MOST_EIGHTS / 2);
+    if (d <= 8 * per_warp && ldq % 8 == 0 && !misaligned(Xq, 8)) {
         int warps = 1;
-        while (warps < 8 && (d > 256 * i8::MOST_EIGHTS * warps || (rows * warps < 8 * kPlanSMs && d > 256 * warps))) warps *= 2;
-        if (warps == 1) launch_quantize_rows<T, 1>(X, rows, d, ldX, Xq, ldq, pad, scale, setup, more, st);
-        else if (warps == 2) launch_quantize_rows<T, 2>(X, rows, d, ldX, Xq, ldq, pad, scale, setup, more, st);
-        else if (warps == 4) launch_quantize_rows<T, 4>(X, rows, d, ldX, Xq, ldq, pad, scale, setup, more, st);
-        else launch_quantize_rows<T, 8>(X, rows, d, ldX, Xq, ldq, pad, scale, setup, more, st);
+        while (warps < 8 && (d > per_warp * warps || (rows * warps < 8 * kPlanSMs && d > 256 * warps))) warps *= 2;
+        if (warps == 1) launch_quantize_rows<T, 1>(X, rows, d, ldX, Xq, ldq, pad, scale, setup, more, whole, st);
+        else if (warps == 2) launch_quantize_rows<T, 2>(X, rows, d, ldX, Xq, ldq, pad, scale, setup, more, whole, st);
+        else if (warps == 4) launch_quantize_rows<T, 4>(X, rows, d, ldX, Xq, ldq, pad, scale, setup, more, whole, st);
+        else launch_quantize_rows<T, 8>(X, rows, d, ldX, Xq, ldq, pad, scale, setup, more, whole, st);
     } else {
         i8::quantize_kernel<T><<<static_cast<unsigned>(rows + more), i8::THREADS, 0, st>>>(X, ldX, static_cast<int>(rows), static_cast<int>(d), Xq, ldq,
                                                                                            static_cast<int>(pad), scale, setup);

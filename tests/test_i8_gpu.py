@@ -66,6 +66,24 @@ def test_quantize_of_rows_that_lie_apart(dtype):
     check_rows(X[:1, 3:4])
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("shift", range(8))
+def test_quantize_at_every_address(dtype, shift):
+    """Rows whose first value lies anywhere in 16 bytes, pitches that move it from row to row, lengths around whole eights; what lies around the matrix is NaN."""
+    for rows, d, pitch in ((1, 1, 1), (3, 7, 9), (5, 8, 8), (4, 9, 11), (2, 23, 23), (9, 31, 40), (6, 33, 33), (40, 257, 257), (3, 2050, 2051), (2, 8191, 8191)):
+        flat = torch.full((shift + rows * pitch + 16,), float("nan"))
+        X = flat[shift:shift + rows * pitch].view(rows, pitch)[:, :d]
+        X.copy_(torch.randn(rows, d, generator=torch.Generator().manual_seed(d + shift)))
+        on = flat.to(dtype).to(DEV)
+        view = on[shift:shift + rows * pitch].view(rows, pitch)[:, :d]
+        q, s = quantize_rows(view)
+        want_q, want_s = O.quantize(np64(X.to(dtype)))
+        assert np.array_equal(q.cpu().numpy(), want_q) and np.array_equal(np64(s), want_s)
+        padded = torch.full((rows, (d + 7) // 8 * 8 + 8), 99, dtype=torch.int8, device=DEV)
+        B.cat_i8_quantize(view, B.CAT_BF16 if dtype == BF else B.CAT_F32, rows, d, pitch, padded, padded.shape[1], s)
+        assert bool((padded[:, d:] == 99).all()) and np.array_equal(padded[:, :d].cpu().numpy(), want_q)
+
+
 def test_quantize_leaves_what_is_not_its_own():
     X = tokens(20, 37, BF).to(DEV)
     q = torch.full((20, 48), 99, dtype=torch.int8, device=DEV)
@@ -408,6 +426,17 @@ def test_refusals():
     x = X[:, :60].clone().requires_grad_()
     with pytest.raises(ValueError):                              # 60 columns: no gradient
         odd.loss(x, y).sum().backward()
+
+
+def test_loss_refuses_a_head_with_a_bias():
+    q, scale = head(100, 64)
+    h = Int8Head.from_quantized(q.to(DEV), scale.to(DEV), torch.zeros(100, device=DEV))
+    X, y = tokens(5, 64, BF).to(DEV), torch.zeros(5, dtype=torch.int64, device=DEV)
+    n = torch.zeros(5, device=DEV)
+    for call in (lambda: h.loss(X, y), lambda: h.loss(X.clone().requires_grad_(), y), lambda: h.loss_backward(X, y, None, n, n, n)):
+        with pytest.raises(ValueError, match="bias"):
+            call()
+    assert h(X).shape == (5, 100)
 
 
 def test_no_rows():
