@@ -43,7 +43,8 @@ def quantize(X):
 
 
 def product(xq, sx, wq, sw, bias=None):
-    z = (xq.astype(np.int64) @ wq.astype(np.int64).T).astype(np.float64) * sx[:, None] * sw[None, :]
+    # whole numbers below 2^53, whatever the order of the sum: exact
+    z = (xq.astype(np.float64) @ wq.astype(np.float64).T) * sx[:, None] * sw[None, :]
     return z if bias is None else z + bias
 
 
