@@ -1,4 +1,4 @@
-// Gradient of the tokens of a small batch through the 8-bit head: dX[t, i] = sum_v A[t, v] W[v, i], A the 16-bit terms of the cross entropy's
+// Gradient of the tokens of a small batch (up to 448 rows a pass) through the 8-bit head: dX[t, i] = sum_v A[t, v] W[v, i], A the 16-bit terms of the cross entropy's
 // gradient (fp16, W the integers) or an upstream dY (bf16, W = scale * integer rounded to bf16).
 //
 // The tensor cores multiply no 8-bit by 16-bit operands, so the head has to be widened; a copy of it in memory (widen_kernel) is written and read again for
@@ -10,7 +10,8 @@
 //   * the fp32 tile of rows x columns stays in tensor memory over the whole part; the parts are added in order by add_parts_kernel.
 // Up to 256 rows: they are the M side, in tiles of 128 however few there are, and the head the N side, 256 columns (an MMA with 128 columns of the head
 // as M side and a few rows as N side takes as long: 16 rows of 1024 x 151936 68 us that way, 63 this).  Above, where A leaves room for 128 columns
-// only, those are the M side and the rows the N side of two MMAs, in steps of 32 rows (300 rows 106 us, with rows as M side 169).
+// only, those are the M side and the rows the N side of two MMAs, in steps of 32 rows (300 rows 106 us, with rows as M side 169).  More rows than fit
+// three stages go in two passes.
 // Bound by the handshakes around each 64 entries (barriers, commits) rather than by memory or the tensor cores: about 1000 cycles per slice.
 #pragma once
 #include "i8_head.cuh"
@@ -18,7 +19,7 @@
 namespace cat {
 namespace i8 {
 
-constexpr int GRAD_ROWS = 512;
+constexpr int GRAD_ROWS = 448;                       // a stage of 128 columns and so many rows fits three times
 constexpr int GRAD_SLICE = 64;                       // vocabulary entries of a stage
 constexpr int GRAD_COLS = 128;                       // columns of dX of a unit
 constexpr int GRAD_UNIT_BYTES = GRAD_SLICE * GRAD_COLS;
@@ -29,7 +30,7 @@ constexpr int GRAD_THREADS = 320;
 
 struct GradCtl {
     unsigned long long full[GRAD_MAX_STAGES], empty[GRAD_MAX_STAGES];
-    unsigned long long wide_full[GRAD_WIDE], wide_empty[GRAD_WIDE];
+    unsigned long long wide_full[GRAD_WIDE];
     unsigned long long done, drain;
     uint32_t tmem_base;
     volatile int abort;
@@ -42,7 +43,7 @@ struct GradParams {
     int n;                 // rows of A per box, a multiple of 16: up to 128, or with the head as M side up to 256
     int tiles;             // boxes of them
     int num_kb;            // slices of the vocabulary
-    int stages;            // 2 or more with the head as M side, else 3 or more
+    int stages;            // 3 or more: see the widened buffers
     int first;             // no kernel of the call runs before this one
     unsigned long long wait_ns;
 };
@@ -54,9 +55,6 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     constexpr int N = UNITS * GRAD_COLS;           // columns of dX
     static_assert(!HEAD_M || UNITS == 1, "128 columns are an M side");
     constexpr int WIDE_BYTES = GRAD_WIDE * UNITS * 2 * GRAD_UNIT_BYTES;
-    // With more stages than widened buffers the barrier that frees the stage a buffer was made from frees the buffer as well (it cannot complete again
-    // before the buffer is filled anew); a commit by itself costs the issuing thread 170 cycles.
-    constexpr bool SHORT_RING = HEAD_M;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ GradCtl ctl;
     const uint32_t wide = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, ring = wide + WIDE_BYTES;
@@ -75,10 +73,7 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
             ptx::mbar_init(ptx::smem_u32(&ctl.full[i]), 1);
             ptx::mbar_init(ptx::smem_u32(&ctl.empty[i]), 1);
         }
-        for (int i = 0; i < GRAD_WIDE; ++i) {
-            ptx::mbar_init(ptx::smem_u32(&ctl.wide_full[i]), 4);
-            ptx::mbar_init(ptx::smem_u32(&ctl.wide_empty[i]), 1);
-        }
+        for (int i = 0; i < GRAD_WIDE; ++i) ptx::mbar_init(ptx::smem_u32(&ctl.wide_full[i]), 4);
         ptx::mbar_init(ptx::smem_u32(&ctl.done), 1);
         ptx::mbar_init(ptx::smem_u32(&ctl.drain), 1);
         ctl.abort = 0;
@@ -141,7 +136,6 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
                     }
                 }
                 ptx::umma_commit(ptx::smem_u32(&ctl.empty[s]));
-                if (SHORT_RING) ptx::umma_commit(ptx::smem_u32(&ctl.wide_empty[w]));
                 a += stage_bytes;
                 if (++s == p.stages) { s = 0; phase ^= 1u; a = ring + UNITS * GRAD_UNIT_BYTES; }
                 if (++w == GRAD_WIDE) { w = 0; w_phase ^= 1u; }
@@ -170,8 +164,10 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
         if (SCALED) scales_of(group);
         const int w = group;
         int s = group;
-        uint32_t phase = 0, w_phase = 1;
-        uint32_t free_bar = 0, free_phase = 0;              // !SHORT_RING: of the stage that this group's buffer was last made from
+        uint32_t phase = 0;
+        // A widened buffer is free again when the stage that it was made from is: with more stages than buffers that barrier cannot complete once more before
+        // the buffer is filled anew.  (A commit of its own costs the issuing thread 170 cycles.)
+        uint32_t free_bar = 0, free_phase = 0;
         for (int i = group; i < n_iter; i += 2) {
             float scale[4];
             if (SCALED) {
@@ -180,8 +176,7 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
                 scales_of(i + 2);
             }
             ok = tc::wait_bounded(ptx::smem_u32(&ctl.full[s]), phase, abort, status, p.wait_ns);
-            if (SHORT_RING) ok = ok && tc::wait_bounded(ptx::smem_u32(&ctl.wide_empty[w]), w_phase, abort, status, p.wait_ns);
-            else if (i >= 2) ok = ok && tc::wait_bounded(free_bar, free_phase, abort, status, p.wait_ns);
+            if (i >= 2) ok = ok && tc::wait_bounded(free_bar, free_phase, abort, status, p.wait_ns);
             free_bar = ptx::smem_u32(&ctl.empty[s]);
             free_phase = phase;
             ok = __all_sync(0xffffffffu, ok);
@@ -216,7 +211,6 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
             if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl.wide_full[w]));
             s += 2;
             if (s >= p.stages) { s -= p.stages; phase ^= 1u; }
-            w_phase ^= 1u;
         }
         if (ok) {
             ok = tc::wait_bounded(ptx::smem_u32(&ctl.done), 0, abort, status, p.wait_ns);

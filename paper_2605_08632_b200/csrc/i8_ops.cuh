@@ -64,16 +64,26 @@ GradPlan plan_grad(long long rows, long long d, long long V) {
     }
     return p;
 }
-// Whether the gradient goes by a widened copy of the head: for more rows than grad_kernel takes, and where its rows leave it little room and the copy is small.
-// dX in us, copy / widened on its way: 512 rows of 1024 x 8000 21 / 31, of 1024 x 32000 53 / 55, of 2048 x 32000 96 / 90, of 1024 x 151936 205 / 186; 400 rows 22 / 25,
-// 54 / 39, 97 / 62, 198 / 125; 300 rows 20 / 20, 51 / 33, 95 / 52, 194 / 106; 16 rows 19 / 13, 42 / 21, 74 / 32, 154 / 61.
+// Rows of a pass of it: one pass, or two of even height.
+long long grad_pass_rows(long long rows) { return rows <= i8::GRAD_ROWS ? rows : cdiv(cdiv(rows, 2), 16) * 16; }
+
+// Whether the gradient goes by a widened copy of the head: for more rows than two passes take, and where the copy is small against the rows' work.
+// dX in us, copy / widened on its way.  One pass, heads of 1024 x 8000, 1024 x 32000, 2048 x 32000, 1024 x 151936: 16 rows 19 / 13, 42 / 21, 74 / 32, 154 / 61; 300 rows
+// 20 / 20, 51 / 33, 95 / 52, 194 / 106; 400 rows 22 / 25, 54 / 39, 97 / 62, 198 / 125.  Two passes: 512 rows of 1024 x 8000 21 / 39, of 1024 x 32000 54 / 62, of
+// 1024 x 50000 79 / 78, of 2048 x 32000 96 / 86, of 1024 x 151936 204 / 166; 600 rows of 2048 x 32000 109 / 103; 768 rows of 2048 x 32000 112 / 121, of 2048 x 64000
+// 211 / 205, of 1024 x 151936 253 / 241; 860 rows of 1024 x 151936 294 / 259, of 4096 x 128000 1000 / 808.
 bool use_widened_copy(long long rows, long long d, long long V) {
     const long long weights = d * V;
-    return rows > i8::GRAD_ROWS || (rows > 440 && weights <= (1ll << 25)) || (rows > 300 && weights <= (1ll << 23));
+    return rows > 2 * i8::GRAD_ROWS || (rows > 640 && weights <= 100'000'000) || (rows > i8::GRAD_ROWS && weights <= 50'000'000) ||
+           (rows > 300 && weights <= (1ll << 23));
 }
 
 size_t dx_part_bytes(long long rows, long long d, long long V, bool widen) {
-    return widen ? dh_part_bytes(rows, d, V) : align256(sizeof(float) * plan_grad(rows, d, V).parts * static_cast<size_t>(rows) * d);
+    if (widen) return dh_part_bytes(rows, d, V);
+    const long long most = grad_pass_rows(rows);
+    const size_t full = sizeof(float) * plan_grad(most, d, V).parts * static_cast<size_t>(most) * d;
+    const size_t rest = rows > most ? sizeof(float) * plan_grad(rows - most, d, V).parts * static_cast<size_t>(rows - most) * d : 0;
+    return align256(full > rest ? full : rest);
 }
 
 I8Plan plan_i8(const cat_i8_shape* s, int pass) {
@@ -285,10 +295,10 @@ int launch_grad_as(const CUtensorMap& tmW, const CUtensorMap& tmA, const i8::Gra
     return launch_ahead(kern, grid, i8::GRAD_THREADS, i8::GRAD_SMEM, st, tmW, tmA, p, status);
 }
 
-// dX[r, :] = factor[r] sum_v A[r, v] W[v, :] of up to 512 rows, the head widened on its way.
+// dX[r, :] = factor[r] sum_v A[r, v] W[v, :] of one pass, the head widened on its way.  first: the call's inputs are all that it reads.
 template <bool SCALED>
-int launch_grad(const i8::Head& h, const void* A, long long ldA, const float* factor, __nv_bfloat16* dX, long long lddX, float* part, int* status, cudaStream_t st) {
-    const bool first = SCALED;           // dY and the head are the call's inputs
+int launch_grad_pass(const i8::Head& h, const void* A, long long ldA, const float* factor, __nv_bfloat16* dX, long long lddX, float* part, bool first, int* status,
+                     cudaStream_t st) {
     const GradPlan plan = plan_grad(h.T, h.d, h.V);
     i8::GradParams p;
     p.sw = h.sw; p.part = part; p.T = h.T; p.V = h.V; p.d = h.d;
@@ -306,6 +316,19 @@ int launch_grad(const i8::Head& h, const void* A, long long ldA, const float* fa
                                      : launch_grad_as<SCALED, 256, 2, false>(tmW, tmA, p, status, grid, st);
     if (rc != CAT_OK) return rc;
     return launch_add_parts(part, plan.parts, static_cast<long long>(h.T) * h.d, h.T, h.d, factor, dX, lddX, st);
+}
+
+template <bool SCALED>
+int launch_grad(const i8::Head& h, const void* A, long long ldA, const float* factor, __nv_bfloat16* dX, long long lddX, float* part, int* status, cudaStream_t st) {
+    const long long step = grad_pass_rows(h.T);
+    for (long long r0 = 0; r0 < h.T; r0 += step) {
+        i8::Head hp = h;
+        hp.T = static_cast<int>(h.T - r0 < step ? h.T - r0 : step);
+        const int rc = launch_grad_pass<SCALED>(hp, static_cast<const uint16_t*>(A) + r0 * ldA, ldA, factor ? factor + r0 : nullptr, dX + r0 * lddX, lddX, part,
+                                                SCALED && r0 == 0, status, st);
+        if (rc != CAT_OK) return rc;
+    }
+    return CAT_OK;
 }
 
 template <bool SCALED>

@@ -211,6 +211,12 @@ def test_logits_gradient_matches_oracle(T, d, V):
     assert np.linalg.norm(dX - want) <= 2 * E * np.linalg.norm(want) + 2.0 ** -100
 
 
+# More rows than one pass over the head takes, heads so large that no widened copy is made: two passes that share the parts' workspace.
+@pytest.mark.parametrize("T,d,V", [(449, 2048, 25001), (513, 2056, 25003), (895, 4104, 25000)])
+def test_logits_gradient_in_two_passes(T, d, V):
+    test_logits_gradient_matches_oracle(T, d, V)
+
+
 # ------------------------------------------------------------------------------ cross entropy
 def problem(T, d, V, masked=0.2, spread=1.0, most=40.0):
     q, scale = head(V, d, seed=T + V, spread=spread)
@@ -315,6 +321,25 @@ def test_slabs_change_nothing(T, d, V, mib):
     a = Int8Head.from_quantized(q.to(DEV), scale.to(DEV), slab_mib=mib)
     assert B.cat_i8_workspace_bytes(B.make_i8_shape(T, d, V, slab_mib=mib), 3) < B.cat_i8_workspace_bytes(B.make_i8_shape(T, d, V), 3)
     check_problem(a, q, scale, X, y, valid, g)
+
+
+@pytest.mark.parametrize("T", [449, 601])
+def test_loss_gradient_in_two_passes(T):
+    d, V = 2048, 25001
+    q, scale, X, y, valid, g = problem(T, d, V)
+    h = Int8Head.from_quantized(q.to(DEV), scale.to(DEV))
+    check_problem(h, q, scale, X, y, valid, g)
+    args = [t.to(DEV) for t in (X, y, valid, g)]
+    nll, lse = h.loss_forward(*args[:3])
+    dX = h.loss_backward(*args, nll, lse)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        again = h.loss_backward(*args, nll, lse)
+    again.fill_(float("nan"))
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(again, dX)
 
 
 def test_loss_takes_fp32_tokens():
