@@ -485,10 +485,10 @@ class Int8Head(torch.nn.Module):
         return q, scale, bias, dev
 
     def _without_bias(self):
-        q, scale, bias, dev = self._head()
+        q, scale, bias, _ = self._head()
         if bias is not None:
             raise ValueError("the loss is for heads without a bias")
-        return q, scale, dev
+        return q, scale
 
     def _tokens(self, X, dev, dtypes=_I8_CODE):
         """Checks X; its row pitch."""
@@ -515,8 +515,8 @@ class Int8Head(torch.nn.Module):
 
     forward = logits
 
-    def _logits(self, X, out_dtype):
-        q, scale, bias, dev = self._head()
+    def _logits(self, X, out_dtype, held=None):
+        q, scale, bias, dev = held or self._head()
         ldX = self._tokens(X, dev)
         T, V = X.shape[0], self.V
         ldY = (V + 7) // 8 * 8
@@ -526,7 +526,10 @@ class Int8Head(torch.nn.Module):
 
     def logits_backward(self, dY):
         """dX [T, d] bfloat16 for the upstream gradient of the logits, [T, V] bfloat16.  Its rows have to lie whole 16 bytes apart."""
-        q, scale, _, dev = self._head()
+        return self._logits_backward(dY, *self._head()[:2])
+
+    def _logits_backward(self, dY, q, scale):
+        dev = q.device
         ldY = _rows("dY", dY, (torch.bfloat16,), dev)
         if dY.shape[1] != self.V:
             raise ValueError(f"dY must have {self.V} columns, got {dY.shape[1]}")
@@ -546,7 +549,10 @@ class Int8Head(torch.nn.Module):
 
     def loss_forward(self, X, labels, valid=None):
         """(nll [T], lse [T]) without a graph for autograd."""
-        q, scale, dev = self._without_bias()
+        return self._loss_forward(X, labels, valid, *self._without_bias())
+
+    def _loss_forward(self, X, labels, valid, q, scale):
+        dev = q.device
         ldX = self._tokens(X, dev)
         T = X.shape[0]
         valid = self._labels(T, dev, labels, valid)
@@ -557,7 +563,10 @@ class Int8Head(torch.nn.Module):
 
     def loss_backward(self, X, labels, valid, grad_nll, nll, lse):
         """dX [T, d] for the upstream gradient of nll; nll and lse: those of loss_forward on the same rows."""
-        q, scale, dev = self._without_bias()
+        return self._loss_backward(X, labels, valid, grad_nll, nll, lse, *self._without_bias())
+
+    def _loss_backward(self, X, labels, valid, grad_nll, nll, lse, q, scale):
+        dev = q.device
         ldX = self._tokens(X, dev, (torch.bfloat16,))
         T = X.shape[0]
         valid = self._labels(T, dev, labels, valid)
@@ -591,38 +600,40 @@ class Int8Head(torch.nn.Module):
 class _Int8LogitsFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, head, out_dtype):
+        held = head._head()
         ctx.head = head
-        ctx.save_for_backward(head.q, head.scale)           # so that a head changed in between is noticed
-        return head._logits(X.detach(), out_dtype)
+        ctx.save_for_backward(*held[:2])        # the backward pass is of these: the module's buffers may be others by then
+        return head._logits(X.detach(), out_dtype, held)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dY):
         Int8Head._refuse_capture_backward()
-        ctx.saved_tensors
+        q, scale = ctx.saved_tensors
         T, V = dY.shape
         if dY.dtype != torch.bfloat16 or dY.stride(1) != 1 or (T > 1 and (dY.stride(0) < V or dY.stride(0) % 8)) or dY.data_ptr() % 16:
             laid = torch.empty(T, (V + 7) // 8 * 8, dtype=torch.bfloat16, device=dY.device)[:, :V]
             laid.copy_(dY)
             dY = laid
-        return ctx.head.logits_backward(dY), None, None
+        return ctx.head._logits_backward(dY, q, scale), None, None
 
 
 class _Int8LossFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, labels, valid, head):
-        nll, lse = head.loss_forward(X.detach(), labels, valid)
+        q, scale = head._without_bias()
+        nll, lse = head._loss_forward(X.detach(), labels, valid, q, scale)
         ctx.head = head
-        # the caller may write to the losses that are handed out
-        ctx.save_for_backward(X, labels, valid, nll.clone(), lse, head.q, head.scale)
+        # the caller may write to the losses that are handed out, and give the module other buffers
+        ctx.save_for_backward(X, labels, valid, nll.clone(), lse, q, scale)
         return nll
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, g):
         Int8Head._refuse_capture_backward()
-        X, labels, valid, nll, lse = ctx.saved_tensors[:5]
-        return ctx.head.loss_backward(X.detach(), labels, valid, g.contiguous(), nll, lse), None, None, None
+        X, labels, valid, nll, lse, q, scale = ctx.saved_tensors
+        return ctx.head._loss_backward(X.detach(), labels, valid, g.contiguous(), nll, lse, q, scale), None, None, None
 
 
 class _CatLossFn(torch.autograd.Function):

@@ -1,0 +1,52 @@
+"""Gradients through Int8Head as autograd asks for them, beside what test_i8_gpu holds."""
+import pytest
+import torch
+
+from i8_util import head, tokens
+from paper_2605_08632_b200.api import Int8Head
+from test_i8_gpu import BF, DEV, problem
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------ a head that is replaced
+def replace(h, how, q, scale):
+    """Other weights in the module's buffers, without writing to the tensors that were there."""
+    if how == "scale":
+        h.scale = scale
+    elif how == "q":
+        h.q = q
+    else:
+        h.load_state_dict({"q": q, "scale": scale}, assign=True)
+
+
+@pytest.mark.parametrize("T", [40, 300])
+@pytest.mark.parametrize("how", ["scale", "q", "assign"])
+def test_backward_is_of_the_head_that_the_forward_pass_saw(T, how):
+    d, V = 64, 1001
+    q, scale, X, y, valid, g = (t.to(DEV) for t in problem(T, d, V))
+    q2, scale2 = (t.to(DEV) for t in head(V, d, seed=77))
+    dY = torch.randn(T, 1008, device=DEV).to(BF)[:, :V]
+    fixed = Int8Head.from_quantized(q, scale)
+    nll, lse = fixed.loss_forward(X, y, valid)
+    want_logits, want_loss = fixed.logits_backward(dY), fixed.loss_backward(X, y, valid, g, nll, lse)
+    h = Int8Head.from_quantized(q.clone(), scale.clone())
+    for call, up, want in ((lambda x: h(x), dY, want_logits), (lambda x: h.loss(x, y, valid), g, want_loss)):
+        x = X.clone().requires_grad_()
+        out = call(x)
+        replace(h, how, q2.clone(), 3.0 * scale2)
+        out.backward(up)
+        assert torch.equal(x.grad, want)
+        replace(h, "assign", q.clone(), scale.clone())
+
+
+@pytest.mark.parametrize("call", [lambda h, x, y: h(x), lambda h, x, y: h.loss(x, y)])
+def test_a_head_written_to_in_between_is_noticed(call):
+    q, scale = (t.to(DEV) for t in head(300, 64))
+    for write in (lambda h: h.scale.mul_(2.0), lambda h: h.q.zero_()):
+        h = Int8Head.from_quantized(q.clone(), scale.clone())
+        x = tokens(20, 64, BF).to(DEV).requires_grad_()
+        out = call(h, x, torch.zeros(20, dtype=torch.int64, device=DEV))
+        write(h)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            out.sum().backward()
