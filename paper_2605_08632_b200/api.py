@@ -475,13 +475,23 @@ class Int8Head(torch.nn.Module):
         self.slab_mib = slab_mib
 
     def _head(self):
-        """q, scale and bias as they are now: a module may have been moved or cast."""
+        """q, scale and bias as they are now: a module may have been moved, cast or given other buffers."""
         held = self._buffers                    # (a module's attributes take their time)
-        q, scale, bias = held["q"], held["scale"], held["bias"]
+        return self._checked(held["q"], held["scale"], held["bias"])
+
+    def _checked(self, q, scale, bias):
+        """Refuses buffers that the kernels would misread, with their device."""
         dev = q.device
         if q.dtype != torch.int8 or scale.dtype != torch.float32 or scale.device != dev or (
                 bias is not None and (bias.dtype != torch.float32 or bias.device != dev)):
             raise TypeError("an 8-bit head is int8 with fp32 scales and biases on one device: it may be moved, not cast")
+        V = (self.V,)
+        if q.shape != (self.V, (self.d + 15) // 16 * 16) or scale.shape != V or (bias is not None and bias.shape != V):
+            raise ValueError(f"the head's buffers must be q [{self.V}, {(self.d + 15) // 16 * 16}] and scale and bias [{self.V}], as they were made")
+        if not q.is_contiguous() or not scale.is_contiguous() or (bias is not None and not bias.is_contiguous()):
+            raise ValueError("the head's buffers must be contiguous")
+        if q.data_ptr() % 16 or scale.data_ptr() % 16 or (bias is not None and bias.data_ptr() % 16):
+            raise ValueError("the head's buffers must lie on 16-byte boundaries")
         return q, scale, bias, dev
 
     def _without_bias(self):
@@ -609,7 +619,7 @@ class _Int8LogitsFn(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dY):
         Int8Head._refuse_capture_backward()
-        q, scale = ctx.saved_tensors
+        q, scale = ctx.head._checked(*ctx.saved_tensors, None)[:2]          # which hooks may have laid out anew
         T, V = dY.shape
         if dY.dtype != torch.bfloat16 or dY.stride(1) != 1 or (T > 1 and (dY.stride(0) < V or dY.stride(0) % 8)) or dY.data_ptr() % 16:
             laid = torch.empty(T, (V + 7) // 8 * 8, dtype=torch.bfloat16, device=dY.device)[:, :V]
@@ -632,7 +642,8 @@ class _Int8LossFn(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, g):
         Int8Head._refuse_capture_backward()
-        X, labels, valid, nll, lse, q, scale = ctx.saved_tensors
+        X, labels, valid, nll, lse, *held = ctx.saved_tensors
+        q, scale = ctx.head._checked(*held, None)[:2]
         return ctx.head._loss_backward(X.detach(), labels, valid, g.contiguous(), nll, lse, q, scale), None, None, None
 
 
