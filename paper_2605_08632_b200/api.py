@@ -9,6 +9,7 @@ import functools
 from typing import NamedTuple
 
 import torch
+from torch.autograd.forward_ad import unpack_dual
 
 from . import binding as B
 
@@ -438,7 +439,7 @@ class Int8Head(torch.nn.Module):
         logits = head(X)                        the product, bfloat16 or float32, with `bias` [V] fp32 where there is one
         nll = head.loss(X, labels, valid)       softmax cross entropy of each row, in pieces of the vocabulary (heads without a bias)
 
-    Both carry gradients to bfloat16 X (the tokens' rounding is passed straight through).  Calls share nothing but the head: any lengths,
+    Both carry gradients to bfloat16 X (the tokens' rounding is passed straight through), in backward mode only.  Calls share nothing but the head: any lengths,
     streams and threads.  Not for stream capture with gradients: autograd may then wait for other streams inside the capture; capture
     loss_forward and loss_backward (or logits and logits_backward) instead.  `Int8Head(weight)` quantises a head, `Int8Head.from_quantized`
     takes one that is in 8 bits already."""
@@ -518,7 +519,7 @@ class Int8Head(torch.nn.Module):
         out_dtype = X.dtype if out_dtype is None else out_dtype
         if out_dtype not in _I8_CODE:
             raise TypeError("logits are bfloat16 or float32")
-        if X.requires_grad and torch.is_grad_enabled():
+        if self._differentiated(X):
             self._refuse_capture(X)
             return _Int8LogitsFn.apply(X, self, out_dtype)
         return self._logits(X, out_dtype)
@@ -589,10 +590,15 @@ class Int8Head(torch.nn.Module):
     def loss(self, X, labels, valid=None):
         """nll [T] fp32: the cross entropy of each row with its label, 0 for rows that are masked or whose label is no token id.  What
         is made of them (means, weights) is the caller's."""
-        if X.requires_grad and torch.is_grad_enabled():
+        if self._differentiated(X):
             self._refuse_capture(X)
             return _Int8LossFn.apply(X, labels, valid, self)
         return self.loss_forward(X, labels, valid)[0]
+
+    @staticmethod
+    def _differentiated(X):
+        """Whether the call has to go through autograd, in its backward mode or, to be refused there, in its forward one."""
+        return (X.requires_grad and torch.is_grad_enabled()) or unpack_dual(X).tangent is not None
 
     @staticmethod
     def _refuse_capture(X):

@@ -1,6 +1,7 @@
 """Gradients through Int8Head as autograd asks for them, beside what test_i8_gpu holds."""
 import pytest
 import torch
+import torch.autograd.forward_ad as forward_ad
 
 from i8_util import head, tokens
 from paper_2605_08632_b200.api import Int8Head
@@ -50,3 +51,19 @@ def test_a_head_written_to_in_between_is_noticed(call):
         write(h)
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             out.sum().backward()
+
+
+# ------------------------------------------------------------------------------ forward mode
+@pytest.mark.parametrize("needs_grad", [False, True])
+@pytest.mark.parametrize("T", [20, 300])
+def test_tangents_are_refused_not_dropped(T, needs_grad):
+    q, scale = (t.to(DEV) for t in head(300, 64))
+    h, X, y = Int8Head.from_quantized(q, scale), tokens(T, 64, BF).to(DEV), torch.zeros(T, dtype=torch.int64, device=DEV)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(X.clone().requires_grad_(needs_grad), torch.ones_like(X))
+        for call in (lambda: h(dual), lambda: h.loss(dual, y)):
+            with pytest.raises(NotImplementedError):
+                call()
+            with torch.no_grad(), pytest.raises(NotImplementedError):         # which does not switch tangents off
+                call()
+        assert h(X).shape == (T, 300) and bool(h.loss(X, y).isfinite().all())
