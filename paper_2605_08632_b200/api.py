@@ -439,8 +439,8 @@ class Int8Head(torch.nn.Module):
         logits = head(X)                        the product, bfloat16 or float32, with `bias` [V] fp32 where there is one
         nll = head.loss(X, labels, valid)       softmax cross entropy of each row, in pieces of the vocabulary (heads without a bias)
 
-    Both carry gradients to bfloat16 X (the tokens' rounding is passed straight through), in backward mode only.  Calls share nothing but the head: any lengths,
-    streams and threads.  Not for stream capture with gradients: autograd may then wait for other streams inside the capture; capture
+    Both carry gradients to bfloat16 X where d is a multiple of 8 (the tokens' rounding is passed straight through), in backward mode only.  Calls
+    share nothing but the head: any lengths, streams and threads.  Not for stream capture with gradients: autograd may then wait for other streams inside the capture; capture
     loss_forward and loss_backward (or logits and logits_backward) instead.  `Int8Head(weight)` quantises a head, `Int8Head.from_quantized`
     takes one that is in 8 bits already."""
 
@@ -520,7 +520,7 @@ class Int8Head(torch.nn.Module):
         if out_dtype not in _I8_CODE:
             raise TypeError("logits are bfloat16 or float32")
         if self._differentiated(X):
-            self._refuse_capture(X)
+            self._refuse(X)
             return _Int8LogitsFn.apply(X, self, out_dtype)
         return self._logits(X, out_dtype)
 
@@ -591,7 +591,7 @@ class Int8Head(torch.nn.Module):
         """nll [T] fp32: the cross entropy of each row with its label, 0 for rows that are masked or whose label is no token id.  What
         is made of them (means, weights) is the caller's."""
         if self._differentiated(X):
-            self._refuse_capture(X)
+            self._refuse(X)
             return _Int8LossFn.apply(X, labels, valid, self)
         return self.loss_forward(X, labels, valid)[0]
 
@@ -600,10 +600,12 @@ class Int8Head(torch.nn.Module):
         """Whether the call has to go through autograd, in its backward mode or, to be refused there, in its forward one."""
         return (X.requires_grad and torch.is_grad_enabled()) or unpack_dual(X).tangent is not None
 
-    @staticmethod
-    def _refuse_capture(X):
+    def _refuse(self, X):
+        """What has no gradient is refused before the forward pass."""
         if X.dtype != torch.bfloat16:
             raise TypeError(f"gradients are for bfloat16 X, got {X.dtype}")
+        if self.d % 8:
+            raise ValueError(f"gradients are for heads whose columns are a multiple of 8, got {self.d}")
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("Int8Head cannot be captured with gradients: capture loss_forward and loss_backward, or logits and logits_backward")
 

@@ -67,3 +67,16 @@ def test_tangents_are_refused_not_dropped(T, needs_grad):
             with torch.no_grad(), pytest.raises(NotImplementedError):         # which does not switch tangents off
                 call()
         assert h(X).shape == (T, 300) and bool(h.loss(X, y).isfinite().all())
+
+
+# ------------------------------------------------------------------------------ refusals
+def test_columns_without_a_gradient_are_refused_before_the_forward_pass():
+    """Heads whose rows are no whole 16 bytes of bf16."""
+    q, scale = (t.to(DEV) for t in head(100, 60))
+    h, y = Int8Head.from_quantized(q, scale), torch.zeros(10, dtype=torch.int64, device=DEV)
+    x = tokens(10, 60, BF).to(DEV).requires_grad_()
+    for call in (lambda: h(x), lambda: h.loss(x, y)):
+        with pytest.raises(ValueError, match="multiple of 8"):
+            call()
+        with torch.no_grad():
+            assert call().shape[0] == 10
