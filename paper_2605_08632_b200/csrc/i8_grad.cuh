@@ -175,8 +175,12 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
                 for (int q = 0; q < 4; ++q) scale[q] = next[q];
                 scales_of(i + 2);
             }
-            ok = tc::wait_bounded(ptx::smem_u32(&ctl.full[s]), phase, abort, status, p.wait_ns);
-            if (i >= 2) ok = ok && tc::wait_bounded(free_bar, free_phase, abort, status, p.wait_ns);
+            // In this order.  A wait names one of two phases, so it holds only where the phase before has completed for sure; with an odd number of stages the
+            // slot's last slice was the other group's, whose copy may still be under way when this group comes here.  Once the MMAs of slice i - 2 are
+            // done, so are those of i - stages, which waited for that copy.  (The other way round a group could take a slot for filled that still held
+            // slice i - 3, and widened that: seen in one call in 30 to 150 with 449 rows of 2048 x 25001.)
+            if (i >= 2) ok = tc::wait_bounded(free_bar, free_phase, abort, status, p.wait_ns);
+            ok = ok && tc::wait_bounded(ptx::smem_u32(&ctl.full[s]), phase, abort, status, p.wait_ns);
             free_bar = ptx::smem_u32(&ctl.empty[s]);
             free_phase = phase;
             ok = __all_sync(0xffffffffu, ok);
