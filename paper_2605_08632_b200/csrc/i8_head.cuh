@@ -451,8 +451,10 @@ struct EpiLinear {
     __device__ static __forceinline__ void end_item(const Params&, const State&, int) {}
 };
 
-// log2 e times a row's scale; a row of zeros has logits 0 whatever this is, and -infinity times it has to stay -infinity.
-__device__ __forceinline__ float log2_scale(float sx) { return sx == 0.f ? tc::LOG2E : sx * tc::LOG2E; }
+// log2 e times a row's scale.  Columns that are not to count are at -infinity, and times this have to stay there: where the scale is 0 (rows of zeros, and rows
+// whose largest value is so small that its 127th rounds to 0, with integers up to 127) it is the smallest number that is not, which leaves logits of 0 to within
+// 2^-149 of their integer sums times the channel's scale.
+__device__ __forceinline__ float log2_scale(float sx) { return sx == 0.f ? __uint_as_float(1u) : sx * tc::LOG2E; }
 
 // Largest logit but the label's and the sum of the exponentials relative to it, in units of log2, and the label's logit.
 struct RowSums {
