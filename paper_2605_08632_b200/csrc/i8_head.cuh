@@ -456,14 +456,15 @@ struct EpiLinear {
 // 2^-149 of their integer sums times the channel's scale.
 __device__ __forceinline__ float log2_scale(float sx) { return sx == 0.f ? __uint_as_float(1u) : sx * tc::LOG2E; }
 
-// Largest logit but the label's and the sum of the exponentials relative to it, in units of log2, and the label's logit.
+// Largest logit but the label's and the sum of the exponentials relative to it, in units of log2, and the label's logit.  The largest is rounded up, so
+// that no exponent is above 0: rounded to nearest, a logit of 1e10 has one of up to 500 itself.
 struct RowSums {
     float m, l;            // running maximum and sum
     float a;               // log2 e times the row's scale
     __device__ __forceinline__ void clear(float sx) { m = LOW2; l = 0.f; a = log2_scale(sx); }
     // 32 columns (without the row's scale), those that are not to count at -infinity
     __device__ __forceinline__ void add(const float (&f)[32]) {
-        const float m_new = fmaxf(m, tc::max_of(f) * a);
+        const float m_new = fmaxf(m, __fmul_ru(tc::max_of(f), a));
         const uint64_t a2 = ptx::pack_f32x2(a, a), nm2 = ptx::pack_f32x2(-m_new, -m_new);
         uint64_t sum2 = ptx::pack_f32x2(0.f, 0.f);
 #pragma unroll
@@ -559,6 +560,7 @@ __global__ void __launch_bounds__(THREADS) merge_kernel(const float* part_m, con
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
     if (lane != 0) return;
+    if (m > LOW2 && l < 0x1p-126f) l = 0x1p-126f;          // past 1e9 the largest logit may lie so far below its rounded value that its own exponential is 0
     if (valid != nullptr && valid[r] == 0) {
         nll[r] = lse[r] = 0.f;
         return;

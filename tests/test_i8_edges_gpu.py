@@ -6,7 +6,7 @@ import torch
 from i8_util import check_ce, head, np64, tokens
 from oracle import i8_oracle as O
 from paper_2605_08632_b200.api import Int8Head
-from test_i8_gpu import DEV, F32, check_logits
+from test_i8_gpu import BF, DEV, F32, check_logits
 
 pytestmark = pytest.mark.gpu
 
@@ -26,4 +26,26 @@ def test_rows_whose_scale_rounds_to_zero(T):
     check_logits(h(X.to(DEV)), X, q, scale, None, F32)
     nll, lse = h.loss_forward(X.to(DEV), y.to(DEV))
     z = O.product(xq, xs, q.numpy(), np64(scale))
+    check_ce(np64(nll), np64(lse), z, O.cross_entropy(z, y.numpy()))
+
+
+@pytest.mark.parametrize("T", [5, 200])
+@pytest.mark.parametrize("size", [1e7, 1e10, 1e28])
+@pytest.mark.parametrize("sign", [-1.0, 1.0, 0.0])
+def test_logits_of_any_size(T, size, sign):
+    """All below -size, all above size, or on both sides: what rounding leaves of the largest logit's own exponent, many units above 1e9, is cut off."""
+    d, V = 64, 3000
+    g = torch.Generator().manual_seed(T)
+    q = torch.randint(1, 128, (V, d), generator=g)
+    if sign == 0.0:
+        q = torch.where(torch.rand(V, d, generator=g) < 0.5, q, -q)
+    q = q.to(torch.int8)
+    scale = (0.02 / 40.0) * (1.0 + torch.rand(V, generator=g))
+    X = ((sign or 1.0) * size * (1.0 + torch.rand(T, d, generator=g))).to(BF)
+    y = torch.randint(0, V, (T,), generator=g)
+    y[0] = -100
+    nll, lse = Int8Head.from_quantized(q.to(DEV), scale.to(DEV)).loss_forward(X.to(DEV), y.to(DEV))
+    xq, xs = O.quantize(np64(X))
+    z = O.product(xq, xs, q.numpy(), np64(scale))
+    assert sign == 0.0 or (sign * z).min() > size           # 64 products of 1 .. 2 sizes with 5e-4 .. 0.13
     check_ce(np64(nll), np64(lse), z, O.cross_entropy(z, y.numpy()))
