@@ -20,7 +20,7 @@ namespace cat {
 namespace i8 {
 
 constexpr int THREADS = 256;
-constexpr float LOW2 = -1.0e30f;        // "no column yet", in units of log2: finite, so that LOW2 - LOW2 is 0
+constexpr float LOW2 = -3.4028234664e38f;        // "no column yet", in units of log2: finite, so that LOW2 - LOW2 is 0, and below every logit
 constexpr float NEAR_HALF = 0.49998f;   // a distance from an integer that is 2^-16 short of a half, or more: what decides it is past binary32
 
 // ------------------------------------------------------------------------------ rows to integers

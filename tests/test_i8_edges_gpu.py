@@ -49,3 +49,10 @@ def test_logits_of_any_size(T, size, sign):
     z = O.product(xq, xs, q.numpy(), np64(scale))
     assert sign == 0.0 or (sign * z).min() > size           # 64 products of 1 .. 2 sizes with 5e-4 .. 0.13
     check_ce(np64(nll), np64(lse), z, O.cross_entropy(z, y.numpy()))
+
+
+@pytest.mark.parametrize("T", [5, 200])
+@pytest.mark.parametrize("size", [1e32, 3e34])
+def test_rows_whose_logits_are_all_far_below_zero(T, size):
+    """No fixed number stands for "no logit yet"."""
+    test_logits_of_any_size(T, size, -1.0)
