@@ -254,7 +254,7 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ C
                                     float x = ptx::ex2_approx(fmaf(f, s.x, s.z)) * (w[j] * up);
                                     if (__float_as_int(s.y) == v) x = -w[j] * up;
                                     if (s.w == 0.f) x = 0.f;
-                                    static_cast<__half*>(p.Y)[at] = __float2half_rn(x);
+                                    static_cast<uint16_t*>(p.Y)[at] = static_cast<uint16_t>(ptx::pack_f16x2_sat(x, 0.f));
                                 } else {
                                     const float y = __fadd_rn(__fmul_rn(f, s_tok[tok + i].x), b[j]);
                                     if (MODE == SKINNY_F32) static_cast<float*>(p.Y)[at] = y;

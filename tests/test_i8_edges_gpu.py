@@ -56,3 +56,17 @@ def test_logits_of_any_size(T, size, sign):
 def test_rows_whose_logits_are_all_far_below_zero(T, size):
     """No fixed number stands for "no logit yet"."""
     test_logits_of_any_size(T, size, -1.0)
+
+
+@pytest.mark.parametrize("T", [60, 120, 300])
+def test_gradients_of_huge_logits_stay_finite(T):
+    """Logits of 1e8, where lse's own rounding is several units: the terms exp(z - lse) are cut off at half precision's largest value whatever the number of rows."""
+    d, V = 64, 1000
+    q, scale = (t.to(DEV) for t in head(V, d, spread=0.0))
+    X = (tokens(T, d, F32) * 3e8).to(BF).to(DEV)
+    y = (torch.arange(T) * 7 % V).to(DEV)
+    h = Int8Head.from_quantized(q, scale)
+    nll, lse = h.loss_forward(X, y)
+    assert bool(nll.isfinite().all()) and float(nll.max()) > 1e7
+    dX = h.loss_backward(X, y, None, torch.ones(T, device=DEV), nll, lse)
+    assert bool(dX.isfinite().all())
