@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 || EIGHTS < MOST_EIGHT
                                                                 const CallSetup setup) {
     constexpr int PER_CTA = THREADS / 32 / WARPS;
     __shared__ unsigned s_most[THREADS / 32];
-    const int row_ctas = (rows + PER_CTA - 1) / PER_CTA;
+    const int row_ctas = static_cast<int>((static_cast<unsigned>(rows) + PER_CTA - 1u) / PER_CTA);
     ptx::launch_dependents();
     set_up_call(setup, static_cast<int>(blockIdx.x) < row_ctas ? -1 : static_cast<int>(blockIdx.x) - row_ctas);
     if (static_cast<int>(blockIdx.x) >= row_ctas) return;

@@ -5,6 +5,7 @@ import torch
 
 from i8_util import check_ce, head, np64, tokens
 from oracle import i8_oracle as O
+from paper_2605_08632_b200 import binding as B
 from paper_2605_08632_b200.api import Int8Head
 from test_i8_gpu import BF, DEV, F32, check_logits
 
@@ -70,3 +71,28 @@ def test_gradients_of_huge_logits_stay_finite(T):
     assert bool(nll.isfinite().all()) and float(nll.max()) > 1e7
     dX = h.loss_backward(X, y, None, torch.ones(T, device=DEV), nll, lse)
     assert bool(dX.isfinite().all())
+
+
+# ------------------------------------------------------------------------------ the largest sizes of rows to integers
+def quantize_large(rows, d, pitch, at):
+    """Zeros but for one value in each of the places `at`."""
+    X = torch.zeros(rows, d, dtype=BF, device=DEV)
+    q = torch.full((rows, pitch), 9, dtype=torch.int8, device=DEV)
+    s = torch.full((rows,), 7.0, device=DEV)
+    for n, (r, i) in enumerate(at):
+        X[r, i] = float(n + 1)
+    B.cat_i8_quantize(X, B.CAT_BF16, rows, d, d, q, pitch, s)
+    return q, s
+
+
+def test_quantize_of_the_most_rows():
+    rows = 2 ** 31 - 1
+    at = [(0, 0), (5, 0), (2 ** 30 + 1, 0), (rows - 9, 0), (rows - 1, 0)]
+    q, s = quantize_large(rows, 1, 8, at)
+    for n, (r, _) in enumerate(at):
+        assert int(q[r, 0]) == 127 and float(s[r]) == float(torch.tensor((n + 1) / 127.0))
+        s[r] = 0.0
+        q[r, 0] = 0
+    assert int(torch.count_nonzero(s)) == 0
+    for i in range(0, rows, 1 << 28):
+        assert not bool(q[i:i + (1 << 28), 0].any()) and bool((q[i:i + (1 << 28), 1:] == 9).all())
