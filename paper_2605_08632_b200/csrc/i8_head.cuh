@@ -91,7 +91,8 @@ __global__ void __launch_bounds__(THREADS) quantize_kernel(const T* X, long long
     if (r >= rows) return;
     const T* x = X + r * ldX;
     unsigned bits = 0;                      // of |x|: ordered like the values, infinities and NaN above them
-    for (int i = threadIdx.x; i < d; i += THREADS) bits = max(bits, __float_as_uint(to_float(x[i])) & 0x7fffffffu);
+    const unsigned n = static_cast<unsigned>(d), n_out = static_cast<unsigned>(pad);          // an index may step past 2^31
+    for (unsigned i = threadIdx.x; i < n; i += THREADS) bits = max(bits, __float_as_uint(to_float(x[i])) & 0x7fffffffu);
     bits = __reduce_max_sync(0xffffffffu, bits);
     if ((threadIdx.x & 31) == 0) s_most[threadIdx.x >> 5] = bits;
     __syncthreads();
@@ -101,7 +102,7 @@ __global__ void __launch_bounds__(THREADS) quantize_kernel(const T* X, long long
     const bool finite = bits < 0x7f800000u, any = finite && bits != 0u;
     const float inv = any ? inverse_step(most) : 0.f;
     int8_t* q = Xq + r * ldq;
-    for (int i = threadIdx.x; i < pad; i += THREADS) q[i] = any && i < d ? static_cast<int8_t>(steps_of(to_float(x[i]), inv, most)) : 0;
+    for (unsigned i = threadIdx.x; i < n_out; i += THREADS) q[i] = any && i < n ? static_cast<int8_t>(steps_of(to_float(x[i]), inv, most)) : 0;
     if (threadIdx.x == 0) scale[r] = finite ? most / 127.f : __uint_as_float(0x7fc00000u);
 }
 

@@ -96,3 +96,12 @@ def test_quantize_of_the_most_rows():
     assert int(torch.count_nonzero(s)) == 0
     for i in range(0, rows, 1 << 28):
         assert not bool(q[i:i + (1 << 28), 0].any()) and bool((q[i:i + (1 << 28), 1:] == 9).all())
+
+
+def test_quantize_of_the_longest_row():
+    d = 2 ** 31 - 1
+    q, s = quantize_large(1, d, d, [(0, 0), (0, 255), (0, 2 ** 30), (0, d - 300), (0, d - 1)])
+    assert float(s[0]) == float(torch.tensor(5 / 127.0))
+    for i, n in ((0, 25), (255, 51), (2 ** 30, 76), (d - 300, 102), (d - 1, 127)):          # 25.4, 50.8, 76.2, 101.6
+        assert int(q[0, i]) == n
+    assert int(torch.count_nonzero(q)) == 5
