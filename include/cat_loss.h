@@ -616,6 +616,15 @@ int cat_die_map(int32_t* worker_of_tpc, int capacity, int32_t* n_first_die, void
 int cat_selftest_wait_timeout(int role, uint64_t short_ns, uint64_t long_ns, int32_t* status,
                               uint64_t* elapsed_ns, void* cuda_stream);
 
+/*
+ * Status of the current device: CAT_OK, or CAT_ERR_TIMEOUT if a wait inside any kernel of this library has run out on it since the library was loaded or the
+ * status was cleared.  For callers that do not keep the workspaces whose first word holds the status of a single call, and for replayed graphs: results
+ * formed in between may be wrong.  WAITS for `cuda_stream`, whose kernels it covers (others as far as they have run); refused (CAT_ERR_CUDA) while that
+ * is being captured.
+ *   status   HOST int32 (host, out);  clear != 0: back to CAT_OK
+ */
+int cat_device_status(int32_t* status, int clear, void* cuda_stream);
+
 /* Static, NUL-terminated description of a cat_status value (host pointer, never freed). */
 const char* cat_status_string(int status);
 

@@ -514,6 +514,12 @@ class Int8Head(torch.nn.Module):
         shape, n = _i8_plan(which, T, self.d, self.V, ldX, ldY, x_dtype, y_dtype, self.slab_mib)
         _on(dev, entry, shape, *args, torch.empty(n, dtype=torch.uint8, device=dev))
 
+    def status(self, clear: bool = False) -> int:
+        """0, or a negative status if a wait inside a kernel of the library has run out on the head's device since the status was last cleared: what was
+        computed in between may be wrong.  The calls keep no workspace to hold a status of their own.  Waits for the current stream."""
+        with torch.cuda.device(self.q.device):
+            return B.cat_device_status(clear)
+
     def logits(self, X, out_dtype=None):
         """[T, V] in out_dtype (X's unless given).  Where V is not in whole 16 bytes the rows lie further apart than V."""
         out_dtype = X.dtype if out_dtype is None else out_dtype

@@ -122,6 +122,8 @@ def lib() -> ctypes.CDLL:
             f.argtypes = [ctypes.POINTER(cat_i8_shape)] + [vp] * n + [vp, sz, vp]
         L.cat_die_map.restype = ctypes.c_int
         L.cat_die_map.argtypes = [vp, ctypes.c_int, vp, vp]
+        L.cat_device_status.restype = ctypes.c_int
+        L.cat_device_status.argtypes = [ctypes.POINTER(ctypes.c_int32), ctypes.c_int, vp]
         L.cat_selftest_wait_timeout.restype = ctypes.c_int
         L.cat_selftest_wait_timeout.argtypes = [ctypes.c_int, ctypes.c_uint64, ctypes.c_uint64, vp, vp, vp]
         _lib = L
@@ -395,6 +397,16 @@ def cat_die_map():
     if n < 0:
         raise CatError(n, "cat_die_map")
     return list(arr[:n]), int(n0.value)
+
+
+def cat_device_status(clear: bool = False) -> int:
+    """CAT_OK, or CAT_ERR_TIMEOUT if a wait of any kernel of the library has run out on the current device since this was last cleared.
+    Waits for the current stream."""
+    status = ctypes.c_int32(0)
+    rc = lib().cat_device_status(ctypes.byref(status), int(bool(clear)), _stream())
+    if rc != CAT_OK:
+        raise CatError(rc, "cat_device_status")
+    return int(status.value)
 
 
 def cat_selftest_wait_timeout(role: int, short_ns: int, long_ns: int, status, elapsed_ns) -> None:

@@ -1354,6 +1354,26 @@ int cat_die_map(int32_t* worker_of_tpc, int capacity, int32_t* n_first_die, void
 
 }  // extern "C"
 
+extern "C" int cat_device_status(int32_t* status, int clear, void* cuda_stream) {
+    if (!status) return CAT_ERR_NULL;
+    int sms = 0;
+    const int dc = check_device(&sms);
+    if (dc != CAT_OK) return dc;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &cap) != cudaSuccess || cap != cudaStreamCaptureStatusNone) { cudaGetLastError(); return CAT_ERR_CUDA; }
+    int32_t now = 0;
+    const int32_t none = 0;
+    bool ok = cudaMemcpyFromSymbolAsync(&now, tc::g_wait_status, sizeof(now), 0, cudaMemcpyDeviceToHost, st) == cudaSuccess &&
+              cudaStreamSynchronize(st) == cudaSuccess;
+    if (ok && clear && now != 0)
+        ok = cudaMemcpyToSymbolAsync(tc::g_wait_status, &none, sizeof(none), 0, cudaMemcpyHostToDevice, st) == cudaSuccess &&
+             cudaStreamSynchronize(st) == cudaSuccess;
+    if (!ok) { cudaGetLastError(); return CAT_ERR_CUDA; }
+    *status = now;
+    return CAT_OK;
+}
+
 // Self-test of the kernels' time-out path: one CTA (or one CTA pair, as the GEMMs are configured) runs the
 // GEMM kernel's set-up, role split and teardown around waits that nothing will ever satisfy.
 template <int CG>

@@ -88,8 +88,12 @@ struct Ctl {
     volatile int abort;
 };
 
+// CAT_ERR_TIMEOUT from the first wait on that ran out on this device, whichever call it was of: also where nobody keeps the call's own status word
+// (cat_device_status).
+__device__ int g_wait_status = 0;
+
 // Waits for phase `parity` of an mbarrier, at most `limit_ns`.  A wait that runs out raises the CTA's abort
-// flag and records CAT_ERR_TIMEOUT; a wait that sees the flag raised by another role gives up at once.
+// flag and records CAT_ERR_TIMEOUT, for the call and for the device; a wait that sees the flag raised by another role gives up at once.
 // DRAIN = true is for the clean-up after an abort: the flag is already up, so it is neither heeded nor
 // set, and the wait simply ends when the barrier completes or the limit passes.
 template <bool DRAIN = false>
@@ -109,6 +113,7 @@ __device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, vola
                 if (!DRAIN) {
                     *abort = 1;
                     atomicExch(status, STATUS_TIMEOUT);
+                    atomicExch(&g_wait_status, STATUS_TIMEOUT);
                 }
                 return false;
             }
