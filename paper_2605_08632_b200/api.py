@@ -423,9 +423,9 @@ def _on_16_bytes(t):
 
 
 @functools.lru_cache(maxsize=512)
-def _i8_plan(which, T, d, V, ldX, ldY, x_dtype, y_dtype, slab_mib):
+def _i8_plan(which, T, d, V, ldX, ldW, ldY, x_dtype, y_dtype, slab_mib):
     """The call's sizes and the bytes of its workspace."""
-    shape = B.make_i8_shape(T, d, V, ldX, None, None, ldY, x_dtype, y_dtype, slab_mib)
+    shape = B.make_i8_shape(T, d, V, ldX, None, ldW, ldY, x_dtype, y_dtype, slab_mib)
     n = B.cat_i8_workspace_bytes(shape, which)
     if n == 0:
         raise ValueError("invalid shape or layout for an 8-bit head: at most 65536 columns; gradients want d, and the rows of dY, in whole 16 bytes")
@@ -463,13 +463,15 @@ class Int8Head(torch.nn.Module):
         if bias is not None:
             _check("bias", bias, (self.V,), torch.float32, q.device)
         _check("scale", scale, (self.V,), torch.float32, q.device)
-        ld = (self.d + 15) // 16 * 16
-        in_place = q.stride(0) == ld and q.data_ptr() % 16 == 0 and q.storage_offset() + self.V * ld <= q.untyped_storage().nbytes()
+        ld, pitch = (self.d + 15) // 16 * 16, q.stride(0)
+        in_place = pitch >= ld and pitch % 16 == 0 and q.data_ptr() % 16 == 0 and (
+            q.storage_offset() + (self.V - 1) * pitch + ld <= q.untyped_storage().nbytes())
         if in_place:
-            padded = q.as_strided((self.V, ld), (ld, 1))
+            padded = q.as_strided((self.V, ld), (pitch, 1))
         else:
             padded = torch.zeros(self.V, ld, dtype=torch.int8, device=q.device)
             padded[:, :self.d] = q
+        self._sizes = padded.shape, scale.shape
         self.register_buffer("q", padded.detach())
         self.register_buffer("scale", _on_16_bytes(scale.detach()))
         self.register_buffer("bias", None if bias is None else _on_16_bytes(bias.detach()))
@@ -486,12 +488,15 @@ class Int8Head(torch.nn.Module):
         if q.dtype != torch.int8 or scale.dtype != torch.float32 or scale.device != dev or (
                 bias is not None and (bias.dtype != torch.float32 or bias.device != dev)):
             raise TypeError("an 8-bit head is int8 with fp32 scales and biases on one device: it may be moved, not cast")
-        V = (self.V,)
-        if q.shape != (self.V, (self.d + 15) // 16 * 16) or scale.shape != V or (bias is not None and bias.shape != V):
-            raise ValueError(f"the head's buffers must be q [{self.V}, {(self.d + 15) // 16 * 16}] and scale and bias [{self.V}], as they were made")
-        if not q.is_contiguous() or not scale.is_contiguous() or (bias is not None and not bias.is_contiguous()):
-            raise ValueError("the head's buffers must be contiguous")
-        if q.data_ptr() % 16 or scale.data_ptr() % 16 or (bias is not None and bias.data_ptr() % 16):
+        wide, long = self._sizes
+        if q.shape != wide or scale.shape != long or (bias is not None and bias.shape != long):
+            raise ValueError(f"the head's buffers must be q {list(wide)} and scale and bias {list(long)}, as they were made")
+        pitch, step = q.stride()
+        if step != 1 or pitch % 16 or pitch < wide[1]:
+            raise ValueError("the rows of q must be contiguous and lie whole 16 bytes apart")
+        if not scale.is_contiguous() or (bias is not None and not bias.is_contiguous()):
+            raise ValueError("scale and bias must be contiguous")
+        if (q.data_ptr() | scale.data_ptr()) % 16 or (bias is not None and bias.data_ptr() % 16):
             raise ValueError("the head's buffers must lie on 16-byte boundaries")
         return q, scale, bias, dev
 
@@ -511,7 +516,7 @@ class Int8Head(torch.nn.Module):
     def _call(self, which, entry, dev, T, ldX, x_dtype, args, ldY=None, y_dtype=B.CAT_BF16):
         if T == 0:
             return
-        shape, n = _i8_plan(which, T, self.d, self.V, ldX, ldY, x_dtype, y_dtype, self.slab_mib)
+        shape, n = _i8_plan(which, T, self.d, self.V, ldX, args[1].stride(0), ldY, x_dtype, y_dtype, self.slab_mib)         # args[1] is q
         _on(dev, entry, shape, *args, torch.empty(n, dtype=torch.uint8, device=dev))
 
     def status(self, clear: bool = False) -> int:

@@ -7,7 +7,7 @@ from i8_util import check_ce, head, np64, tokens
 from oracle import i8_oracle as O
 from paper_2605_08632_b200 import binding as B
 from paper_2605_08632_b200.api import Int8Head
-from test_i8_gpu import BF, DEV, F32, check_logits
+from test_i8_gpu import BF, DEV, F32, check_logits, check_problem, problem
 
 pytestmark = pytest.mark.gpu
 
@@ -105,3 +105,35 @@ def test_quantize_of_the_longest_row():
     for i, n in ((0, 25), (255, 51), (2 ** 30, 76), (d - 300, 102), (d - 1, 127)):          # 25.4, 50.8, 76.2, 101.6
         assert int(q[0, i]) == n
     assert int(torch.count_nonzero(q)) == 5
+
+
+# ------------------------------------------------------------------------------ heads that lie in wider rows
+@pytest.mark.parametrize("T", [5, 200, 600])
+@pytest.mark.parametrize("d,pitch", [(64, 96), (64, 64), (72, 208), (56, 64)])
+def test_a_head_is_used_where_it_is(T, d, pitch):
+    V = 1500
+    q, scale, X, y, valid, g = problem(T, d, V)
+    wide = torch.full((V, pitch), 99, dtype=torch.int8, device=DEV)
+    wide[:, :d] = q.to(DEV)
+    h = Int8Head.from_quantized(wide[:, :d], scale.to(DEV))
+    assert h.q.data_ptr() == wide.data_ptr() and h.q.stride(0) == pitch
+    check_problem(h, q, scale, X, y, valid, g)
+    check_logits(h(X.to(DEV)), X, q, scale, None, BF)
+    dY = torch.randn(T, V + 4, device=DEV).to(BF)[:, :V]
+    same = Int8Head.from_quantized(q.to(DEV), scale.to(DEV))
+    assert torch.equal(h.logits_backward(dY), same.logits_backward(dY))
+    assert torch.equal(h.to("cpu").to(DEV)(X.to(DEV)), same(X.to(DEV)))
+    assert bool((wide[:, d:] == 99).all())
+
+
+def test_other_layouts_are_copied():
+    V, d = 300, 64
+    q, scale = (t.to(DEV) for t in head(V, d))
+    X = tokens(9, d, BF).to(DEV)
+    want = Int8Head.from_quantized(q, scale)(X)
+    for pitch, shift in ((72, 0), (80, 8), (64, 4)):
+        flat = torch.zeros(V * pitch + 16, dtype=torch.int8, device=DEV)
+        at = flat[shift:shift + V * pitch].view(V, pitch)[:, :d]
+        at.copy_(q)
+        h = Int8Head.from_quantized(at, scale)
+        assert h.q.data_ptr() != at.data_ptr() and h.q.data_ptr() % 16 == 0 and torch.equal(h(X), want)
