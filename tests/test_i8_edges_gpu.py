@@ -137,3 +137,15 @@ def test_other_layouts_are_copied():
         at.copy_(q)
         h = Int8Head.from_quantized(at, scale)
         assert h.q.data_ptr() != at.data_ptr() and h.q.data_ptr() % 16 == 0 and torch.equal(h(X), want)
+
+
+# ------------------------------------------------------------------------------ row slabs and the gradient that widens the head on its way
+@pytest.mark.parametrize("T,d,V,mib", [(300, 1024, 9001, 1), (500, 2056, 25001, 20), (700, 2056, 50001, 48)])
+def test_slabs_of_a_few_rows(T, d, V, mib):
+    q, scale, X, y, valid, g = problem(T, d, V)
+    need = B.cat_i8_workspace_bytes(B.make_i8_shape(T, d, V, slab_mib=mib), 3)
+    assert need < B.cat_i8_workspace_bytes(B.make_i8_shape(T, d, V), 3) and need < 2 * d * V + (mib << 20)          # several slabs, no widened copy
+    h = Int8Head.from_quantized(q.to(DEV), scale.to(DEV), slab_mib=mib)
+    nll, lse, dX = check_problem(h, q, scale, X, y, valid, g)
+    for _ in range(3):
+        assert torch.equal(h.loss_backward(X.to(DEV), y.to(DEV), valid.to(DEV), g.to(DEV), nll, lse), dX)
