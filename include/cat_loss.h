@@ -560,8 +560,11 @@ int cat_i8_ce_fwd(const cat_i8_shape* shape, const void* X, const int8_t* Wq, co
 /*
  * Gradient of sum_t grad_nll[t] nll[t] with respect to X, the head frozen, the tokens' rounding passed straight through:
  *     dX[t, :] = grad_nll[t] sum_v (exp(z[t, v] - lse[t]) - [v == y_t]) w_scale[v] Wq[v, :].
- * The logits are recomputed per row slab.  A row's terms are kept relative to 1 - p(y_t) and to the largest |w_scale|, in 11 bits of precision and down
- * to 2^-39 of their largest, so that rows that are sure of their label keep theirs; p(y_t) is taken from nll.
+ * The logits are recomputed per row slab.  A row's terms, the other tokens' probabilities among themselves times w_scale, are kept relative to 1 - p(y_t), which
+ * is taken from nll (rows that are sure of their label keep theirs), as half precision numbers relative to the largest |w_scale| of the head: with 11
+ * bits down to 2^-28 of that, below with an error of up to 2^-39 of it.  Probability and scale count together: in a row that is flat over 2^17 tokens
+ * channels of less than 2^-11 of the largest scale lose bits, so one outlier among the scales costs all flat rows.  The exponents carry the binary32 rounding
+ * of the logits and of lse: relative errors of about 1e-7 of their size, and no more than the range of half precision.
  * Rows that take no part (valid[t] == 0, a label outside [0, V)) get zeros.
  *   nll, lse  [T] fp32 as written by cat_i8_ce_fwd for the same rows and head;  grad_nll  [T] fp32   (device, in)
  *   dX        [T, d] bf16, pitch lddX                                                             (device, out)

@@ -611,7 +611,8 @@ __device__ __forceinline__ RowGrad row_grad(int r, int T, int V, const long long
 }
 
 // exp(z_v - o) sw_v 2^k, and -sw_y 2^k at the label, as fp16: the rest of the row's factor is applied behind the contraction.  Half precision's 11 bits
-// keep the rounding of a row's few large terms below that of the bf16 result (bf16 terms: rows of dX off by up to 2^-8 more).
+// keep the rounding of a row's few large terms below that of the bf16 result (bf16 terms: rows of dX off by up to 2^-8 more).  With the largest scale at
+// 2^14 or more, terms from 2^-28 of it up have those bits; smaller ones are off by up to 2^-39 of it.
 struct EpiDz {
     struct Params {
         const float* sx;

@@ -149,3 +149,15 @@ def test_slabs_of_a_few_rows(T, d, V, mib):
     nll, lse, dX = check_problem(h, q, scale, X, y, valid, g)
     for _ in range(3):
         assert torch.equal(h.loss_backward(X.to(DEV), y.to(DEV), valid.to(DEV), g.to(DEV), nll, lse), dX)
+
+
+# ------------------------------------------------------------------------------ one outlier among the scales
+@pytest.mark.parametrize("T", [20, 200])
+@pytest.mark.parametrize("power", [12, 14, 16])
+def test_one_large_scale_beside_flat_rows(T, power):
+    """Every term of a row whose probabilities are all about 1 / V is so small then that it is off by up to 2^-39 of the largest scale."""
+    d, V = 128, 40000
+    q, scale, X, y, valid, g = problem(T, d, V, spread=0.0, most=0.0)
+    scale[123] *= 2.0 ** power
+    X = (X.float() * 2.0 ** (-power - 4)).to(BF)
+    check_problem(Int8Head.from_quantized(q.to(DEV), scale.to(DEV)), q, scale, X, y, valid, g)
