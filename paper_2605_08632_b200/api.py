@@ -405,7 +405,7 @@ def _rows(name, t, dtypes, device=None):
 
 def quantize_rows(X):
     """Rows of X [rows, d] as 8-bit integers with a scale each (cat_i8_quantize): (q [rows, d] int8, scale [rows] fp32), X about
-    q * scale.  bfloat16 or float32; the rows of q lie a multiple of 16 bytes apart, as the products want them."""
+    q * scale.  bfloat16 or float32; the rows of q lie a multiple of 16 bytes apart, as the products want them.  No graph for autograd."""
     pitch = _rows("X", X, _I8_CODE)
     rows, d = X.shape
     if d == 0:
@@ -439,8 +439,9 @@ class Int8Head(torch.nn.Module):
         logits = head(X)                        the product, bfloat16 or float32, with `bias` [V] fp32 where there is one
         nll = head.loss(X, labels, valid)       softmax cross entropy of each row, in pieces of the vocabulary (heads without a bias)
 
-    Both carry gradients to bfloat16 X where d is a multiple of 8 (the tokens' rounding is passed straight through), in backward mode only.  Calls
-    share nothing but the head: any lengths, streams and threads.  Not for stream capture with gradients: autograd may then wait for other streams inside the capture; capture
+    Both carry gradients to bfloat16 X where d is a multiple of 8 (the tokens' rounding is passed straight through), in backward mode only;
+    upstream gradients of float32 logits are rounded to bfloat16, which the contraction takes.  Calls share nothing but the head: any lengths,
+    streams and threads.  Not for stream capture with gradients: autograd may then wait for other streams inside the capture; capture
     loss_forward and loss_backward (or logits and logits_backward) instead.  `Int8Head(weight)` quantises a head, `Int8Head.from_quantized`
     takes one that is in 8 bits already."""
 

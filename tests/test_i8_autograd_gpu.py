@@ -5,7 +5,7 @@ import torch.autograd.forward_ad as forward_ad
 
 from i8_util import head, tokens
 from paper_2605_08632_b200.api import Int8Head
-from test_i8_gpu import BF, DEV, problem
+from test_i8_gpu import BF, DEV, F32, problem
 
 pytestmark = pytest.mark.gpu
 
@@ -80,3 +80,16 @@ def test_columns_without_a_gradient_are_refused_before_the_forward_pass():
             call()
         with torch.no_grad():
             assert call().shape[0] == 10
+
+
+# ------------------------------------------------------------------------------ fp32 logits
+def test_upstream_gradients_of_fp32_logits_are_rounded_once():
+    """The contraction takes bf16: fp32 upstream gradients are rounded to it, halves to even, and nothing else is."""
+    T, d, V = 70, 64, 1001
+    q, scale = (t.to(DEV) for t in head(V, d))
+    h, x = Int8Head.from_quantized(q, scale), tokens(T, d, BF).to(DEV).requires_grad_()
+    up = torch.randn(T, V, device=DEV) * torch.rand(T, 1, device=DEV)
+    h(x, F32).backward(up)
+    laid = torch.zeros(T, 1008, dtype=BF, device=DEV)
+    laid[:, :V] = up.to(BF)
+    assert torch.equal(x.grad, h.logits_backward(laid[:, :V]))
