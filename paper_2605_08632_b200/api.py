@@ -9,7 +9,7 @@ import functools
 from typing import NamedTuple
 
 import torch
-from torch.autograd.forward_ad import unpack_dual
+from torch.autograd import forward_ad
 
 from . import binding as B
 
@@ -484,7 +484,7 @@ class Int8Head(torch.nn.Module):
         return self._checked(held["q"], held["scale"], held["bias"])
 
     def _checked(self, q, scale, bias):
-        """Refuses buffers that the kernels would misread, with their device."""
+        """Refuses buffers that the kernels would misread; (q, scale, bias, their device, the row pitch of q), as the calls below take a head."""
         dev = q.device
         if q.dtype != torch.int8 or scale.dtype != torch.float32 or scale.device != dev or (
                 bias is not None and (bias.dtype != torch.float32 or bias.device != dev)):
@@ -499,13 +499,13 @@ class Int8Head(torch.nn.Module):
             raise ValueError("scale and bias must be contiguous")
         if (q.data_ptr() | scale.data_ptr()) % 16 or (bias is not None and bias.data_ptr() % 16):
             raise ValueError("the head's buffers must lie on 16-byte boundaries")
-        return q, scale, bias, dev
+        return q, scale, bias, dev, pitch
 
     def _without_bias(self):
-        q, scale, bias, _ = self._head()
-        if bias is not None:
+        held = self._head()
+        if held[2] is not None:
             raise ValueError("the loss is for heads without a bias")
-        return q, scale
+        return held
 
     def _tokens(self, X, dev, dtypes=_I8_CODE):
         """Checks X; its row pitch."""
@@ -514,10 +514,10 @@ class Int8Head(torch.nn.Module):
             raise ValueError(f"X must have {self.d} columns, got {X.shape[1]}")
         return pitch
 
-    def _call(self, which, entry, dev, T, ldX, x_dtype, args, ldY=None, y_dtype=B.CAT_BF16):
+    def _call(self, which, entry, dev, T, ldX, ldW, x_dtype, args, ldY=None, y_dtype=B.CAT_BF16):
         if T == 0:
             return
-        shape, n = _i8_plan(which, T, self.d, self.V, ldX, args[1].stride(0), ldY, x_dtype, y_dtype, self.slab_mib)         # args[1] is q
+        shape, n = _i8_plan(which, T, self.d, self.V, ldX, ldW, ldY, x_dtype, y_dtype, self.slab_mib)
         _on(dev, entry, shape, *args, torch.empty(n, dtype=torch.uint8, device=dev))
 
     def status(self, clear: bool = False) -> int:
@@ -539,27 +539,27 @@ class Int8Head(torch.nn.Module):
     forward = logits
 
     def _logits(self, X, out_dtype, held=None):
-        q, scale, bias, dev = held or self._head()
+        q, scale, bias, dev, ldW = held or self._head()
         ldX = self._tokens(X, dev)
         T, V = X.shape[0], self.V
         ldY = (V + 7) // 8 * 8
         Y = torch.empty(T, ldY, dtype=out_dtype, device=dev)
-        self._call(_I8_LINEAR, B.cat_i8_linear_fwd, dev, T, ldX, _I8_CODE[X.dtype], (X, q, scale, bias, Y), ldY, _I8_CODE[out_dtype])
+        self._call(_I8_LINEAR, B.cat_i8_linear_fwd, dev, T, ldX, ldW, _I8_CODE[X.dtype], (X, q, scale, bias, Y), ldY, _I8_CODE[out_dtype])
         return Y if ldY == V else Y[:, :V]
 
     def logits_backward(self, dY):
         """dX [T, d] bfloat16 for the upstream gradient of the logits, [T, V] bfloat16.  Its rows have to lie whole 16 bytes apart."""
-        return self._logits_backward(dY, *self._head()[:2])
+        return self._logits_backward(dY, self._head())
 
-    def _logits_backward(self, dY, q, scale):
-        dev = q.device
+    def _logits_backward(self, dY, held):
+        q, scale, _, dev, ldW = held
         ldY = _rows("dY", dY, (torch.bfloat16,), dev)
         if dY.shape[1] != self.V:
             raise ValueError(f"dY must have {self.V} columns, got {dY.shape[1]}")
         T = dY.shape[0]
         ldY = ldY if T > 1 else (self.V + 7) // 8 * 8
         dX = torch.empty(T, self.d, dtype=torch.bfloat16, device=dev)
-        self._call(_I8_LINEAR_BWD, B.cat_i8_linear_bwd, dev, T, self.d, B.CAT_BF16, (dY, q, scale, dX), ldY)
+        self._call(_I8_LINEAR_BWD, B.cat_i8_linear_bwd, dev, T, self.d, ldW, B.CAT_BF16, (dY, q, scale, dX), ldY)
         return dX
 
     @staticmethod
@@ -572,31 +572,31 @@ class Int8Head(torch.nn.Module):
 
     def loss_forward(self, X, labels, valid=None):
         """(nll [T], lse [T]) without a graph for autograd."""
-        return self._loss_forward(X, labels, valid, *self._without_bias())
+        return self._loss_forward(X, labels, valid, self._without_bias())
 
-    def _loss_forward(self, X, labels, valid, q, scale):
-        dev = q.device
+    def _loss_forward(self, X, labels, valid, held):
+        q, scale, _, dev, ldW = held
         ldX = self._tokens(X, dev)
         T = X.shape[0]
         valid = self._labels(T, dev, labels, valid)
         nll = torch.empty(T, dtype=torch.float32, device=dev)
         lse = torch.empty(T, dtype=torch.float32, device=dev)
-        self._call(_I8_CE, B.cat_i8_ce_fwd, dev, T, ldX, _I8_CODE[X.dtype], (X, q, scale, labels, valid, nll, lse))
+        self._call(_I8_CE, B.cat_i8_ce_fwd, dev, T, ldX, ldW, _I8_CODE[X.dtype], (X, q, scale, labels, valid, nll, lse))
         return nll, lse
 
     def loss_backward(self, X, labels, valid, grad_nll, nll, lse):
         """dX [T, d] for the upstream gradient of nll; nll and lse: those of loss_forward on the same rows."""
-        return self._loss_backward(X, labels, valid, grad_nll, nll, lse, *self._without_bias())
+        return self._loss_backward(X, labels, valid, grad_nll, nll, lse, self._without_bias())
 
-    def _loss_backward(self, X, labels, valid, grad_nll, nll, lse, q, scale):
-        dev = q.device
+    def _loss_backward(self, X, labels, valid, grad_nll, nll, lse, held):
+        q, scale, _, dev, ldW = held
         ldX = self._tokens(X, dev, (torch.bfloat16,))
         T = X.shape[0]
         valid = self._labels(T, dev, labels, valid)
         for name, t in (("grad_nll", grad_nll), ("nll", nll), ("lse", lse)):
             _check(name, t, (T,), torch.float32, dev)
         dX = torch.empty(T, self.d, dtype=torch.bfloat16, device=dev)
-        self._call(_I8_CE_BWD, B.cat_i8_ce_bwd, dev, T, ldX, B.CAT_BF16, (X, q, scale, labels, valid, nll, lse, grad_nll, dX))
+        self._call(_I8_CE_BWD, B.cat_i8_ce_bwd, dev, T, ldX, ldW, B.CAT_BF16, (X, q, scale, labels, valid, nll, lse, grad_nll, dX))
         return dX
 
     def loss(self, X, labels, valid=None):
@@ -610,7 +610,10 @@ class Int8Head(torch.nn.Module):
     @staticmethod
     def _differentiated(X):
         """Whether the call has to go through autograd, in its backward mode or, to be refused there, in its forward one."""
-        return (X.requires_grad and torch.is_grad_enabled()) or unpack_dual(X).tangent is not None
+        if X.requires_grad and torch.is_grad_enabled():
+            return True
+        # (outside of all dual levels, which is where calls are made, no tensor has a tangent, and to ask one takes its time)
+        return getattr(forward_ad, "_current_level", 0) >= 0 and forward_ad.unpack_dual(X).tangent is not None
 
     def _refuse(self, X):
         """What has no gradient is refused before the forward pass."""
@@ -639,32 +642,32 @@ class _Int8LogitsFn(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dY):
         Int8Head._refuse_capture_backward()
-        q, scale = ctx.head._checked(*ctx.saved_tensors, None)[:2]          # which hooks may have laid out anew
+        held = ctx.head._checked(*ctx.saved_tensors, None)          # which hooks may have laid out anew
         T, V = dY.shape
         if dY.dtype != torch.bfloat16 or dY.stride(1) != 1 or (T > 1 and (dY.stride(0) < V or dY.stride(0) % 8)) or dY.data_ptr() % 16:
             laid = torch.empty(T, (V + 7) // 8 * 8, dtype=torch.bfloat16, device=dY.device)[:, :V]
             laid.copy_(dY)
             dY = laid
-        return ctx.head._logits_backward(dY, q, scale), None, None
+        return ctx.head._logits_backward(dY, held), None, None
 
 
 class _Int8LossFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, labels, valid, head):
-        q, scale = head._without_bias()
-        nll, lse = head._loss_forward(X.detach(), labels, valid, q, scale)
+        held = head._without_bias()
+        nll, lse = head._loss_forward(X.detach(), labels, valid, held)
         ctx.head = head
         # the caller may write to the losses that are handed out, and give the module other buffers
-        ctx.save_for_backward(X, labels, valid, nll.clone(), lse, q, scale)
+        ctx.save_for_backward(X, labels, valid, nll.clone(), lse, *held[:2])
         return nll
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, g):
         Int8Head._refuse_capture_backward()
-        X, labels, valid, nll, lse, *held = ctx.saved_tensors
-        q, scale = ctx.head._checked(*held, None)[:2]
-        return ctx.head._loss_backward(X.detach(), labels, valid, g.contiguous(), nll, lse, q, scale), None, None, None
+        X, labels, valid, nll, lse, q, scale = ctx.saved_tensors
+        held = ctx.head._checked(q, scale, None)
+        return ctx.head._loss_backward(X.detach(), labels, valid, g.contiguous(), nll, lse, held), None, None, None
 
 
 class _CatLossFn(torch.autograd.Function):
