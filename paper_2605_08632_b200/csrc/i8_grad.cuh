@@ -1,5 +1,5 @@
 // Gradient of the tokens of a small batch (up to 448 rows a pass) through the 8-bit head: dX[t, i] = sum_v A[t, v] W[v, i], A the 16-bit terms of the cross entropy's
-// gradient (fp16, W the integers) or an upstream dY (bf16, W = scale * integer rounded to bf16).
+// gradient (fp16, W the integers) or an upstream dY (bf16, W = scale * integer rounded to bf16: why, at widen_kernel).
 //
 // The tensor cores multiply no 8-bit by 16-bit operands, so the head has to be widened; a copy of it in memory (widen_kernel) is written and read again for
 // 4 bytes per weight, against 1 to read it as it is.  With few rows that copy costs more than the product, so here the head is widened on its way:
@@ -197,8 +197,7 @@ grad_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
                     uint32_t r[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const uint32_t pair = __byte_perm(in[j >> 1], 0x64646464u, (j & 1) ? 0x4342 : 0x4140);                          // fp16 1024 + byte
-                        const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&pair), __half2half2(__ushort_as_half(0x6480)));         // - 1152
+                        const __half2 h = widened(in[j >> 1], j & 1);
                         if (SCALED) {
                             const float2 f = __half22float2(h);
                             r[j] = ptx::pack_bf16x2(f.x * scale[q], f.y * scale[q]);

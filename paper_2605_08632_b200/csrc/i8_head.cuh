@@ -207,7 +207,7 @@ __device__ __forceinline__ Eight<T> eight_at(const T* x, int count, uintptr_t lo
 // steps_of for eight values, as far as binary32 goes; `open`: one of them is too near to a half for that.  Adding 1.5 2^23 rounds to the nearest integer,
 // halves to the even one, and leaves it in the low bits.
 //   bf16: with 8-bit significands, 127 x / most is a half exactly or off it by 1 / (254 * 255) of itself or more.  The binary32 product, off by 2^-22,
-//   is rounded to 20 bits first, which makes halves of all that are ones, and moves none of the others across one.
+//   is rounded to 20 bits first (Veltkamp's splitting), which makes halves of all that are ones, and moves none of the others across one.
 //   fp32: the distance to the integer says whether a half is near.
 template <class T>
 __device__ __forceinline__ uint2 eight_steps(const float (&x)[8], float inv, bool& open) {
@@ -681,9 +681,18 @@ struct EpiDz {
     }
 };
 
-// The head as the 16-bit operand of the gradient's contraction: its integers in fp16 (exact), or scale * integer in bf16.  Bound by HBM: 86 us for
-// 1024 x 151936 (466 MB), 120 for 2048 x 128256.  (Beside the product of the gradient's terms, on what that leaves of the SMs, it does not fit: the step of
-// 4096 rows 2.8 -> 3.4 ms.)
+// Two neighbouring ones of four integers, which come with 128 added (0 .. 255), as fp16: a byte behind 0x64 is 1024 + byte, the widely published way to widen bytes.
+__device__ __forceinline__ __half2 widened(uint32_t biased, int pair) {
+    const uint32_t w = __byte_perm(biased, 0x64646464u, pair ? 0x4342 : 0x4140);
+    return __hsub2(*reinterpret_cast<const __half2*>(&w), __half2half2(__ushort_as_half(0x6480)));       // - 1152
+}
+
+// The head as the 16-bit operand of the gradient's contraction: its integers in fp16 (exact; the cross entropy's terms are fp16 with the scale in them), or
+// scale * integer in bf16, as an upstream dY is.  That rounding is a choice: dX is 2.4e-3 off, 1.7e-3 of it dX's own rounding.  Terms dY * scale in fp16, relative to
+// each row's largest, would leave 1.7e-3, at a pass over dY for those maxima and a copy of it (some 140 us more at the rate of memory for 1000 x 151936, beside
+// 360), and lose what lies far below the largest; bf16 holds upstream gradients of any range.
+// 86 us for 1024 x 151936 (466 MB, 5.4 TB/s), 120 for 2048 x 128256 (6.6 TB/s): one load under way per thread, and divisions, keep shorter rows off the rate
+// of memory.  (Beside the product of the gradient's terms, on what that leaves of the SMs, it does not fit: the step of 4096 rows 2.8 -> 3.4 ms.)
 template <bool SCALED>
 __global__ void __launch_bounds__(THREADS) widen_kernel(const int8_t* wq, long long ldw, const float* sw, long long units, int per_row, int d, uint16_t* out,
                                                         const CallSetup setup) {
@@ -697,8 +706,7 @@ __global__ void __launch_bounds__(THREADS) widen_kernel(const int8_t* wq, long l
         const uint32_t b[2] = {x.x ^ 0x80808080u, x.y ^ 0x80808080u};    // 0 .. 255
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t pair = __byte_perm(b[j >> 1], 0x64646464u, (j & 1) ? 0x4342 : 0x4140);      // fp16 1024 + byte
-            __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&pair), __half2half2(__ushort_as_half(0x6480)));   // - 1152
+            const __half2 h = widened(b[j >> 1], j & 1);
             if (SCALED) {
                 const float2 f = __half22float2(h);
                 const float s = sw[v];

@@ -71,7 +71,9 @@ long long grad_pass_rows(long long rows) { return rows <= i8::GRAD_ROWS ? rows :
 // dX in us, copy / widened on its way.  One pass, heads of 1024 x 8000, 1024 x 32000, 2048 x 32000, 1024 x 151936: 16 rows 19 / 13, 42 / 21, 74 / 32, 154 / 61; 300 rows
 // 20 / 20, 51 / 33, 95 / 52, 194 / 106; 400 rows 22 / 25, 54 / 39, 97 / 62, 198 / 125.  Two passes: 512 rows of 1024 x 8000 21 / 39, of 1024 x 32000 54 / 62, of
 // 1024 x 50000 79 / 78, of 2048 x 32000 96 / 86, of 1024 x 151936 204 / 166; 600 rows of 2048 x 32000 109 / 103; 768 rows of 2048 x 32000 112 / 121, of 2048 x 64000
-// 211 / 205, of 1024 x 151936 253 / 241; 860 rows of 1024 x 151936 294 / 259, of 4096 x 128000 1000 / 808.
+// 211 / 205, of 1024 x 151936 253 / 241; 860 rows of 1024 x 151936 294 / 259, of 4096 x 128000 1000 / 808.  Around the limit of 100 M weights, heads of 1024 x 80000,
+// 1024 x 100000, 1024 x 120000: 656 rows 136 / 129, 169 / 158, 198 / 180; 704 rows 137 / 138, 171 / 170, 200 / 194; 768 rows 139 / 141, 173 / 174, 203 / 198; 832 rows of
+// the first two 163 / 146, 203 / 180.  (The limit holds for 700 to 768 rows; below and above, smaller heads would gain 5 to 10 % from the two passes.)
 bool use_widened_copy(long long rows, long long d, long long V) {
     const long long weights = d * V;
     return rows > 2 * i8::GRAD_ROWS || (rows > 640 && weights <= 100'000'000) || (rows > i8::GRAD_ROWS && weights <= 50'000'000) ||
