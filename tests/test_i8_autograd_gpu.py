@@ -1,7 +1,10 @@
 """Gradients through Int8Head as autograd asks for them, beside what test_i8_gpu holds."""
+import copy
+
 import pytest
 import torch
 import torch.autograd.forward_ad as forward_ad
+import torch.utils.checkpoint
 
 from i8_util import head, tokens
 from paper_2605_08632_b200.api import Int8Head
@@ -93,3 +96,35 @@ def test_upstream_gradients_of_fp32_logits_are_rounded_once():
     laid = torch.zeros(T, 1008, dtype=BF, device=DEV)
     laid[:, :V] = up.to(BF)
     assert torch.equal(x.grad, h.logits_backward(laid[:, :V]))
+
+
+# ------------------------------------------------------------------------------ what is kept for the backward pass
+def test_kept_tensors_may_be_packed_away():
+    """Hooks that lay the kept tensors out anew, a head in wider rows among them, and a forward pass that is run again."""
+    T, d, V = 60, 64, 1001
+    q, scale, X, y, valid, g = (t.to(DEV) for t in problem(T, d, V))
+    wide = torch.zeros(V, 96, dtype=torch.int8, device=DEV)
+    wide[:, :d] = q
+    for h in (Int8Head.from_quantized(q, scale), Int8Head.from_quantized(wide[:, :d], scale)):
+        for call, up in ((lambda x: h.loss(x, y, valid), g), (lambda x: h(x), torch.randn(T, V, device=DEV).to(BF))):
+            plain, packed, again = (X.clone().requires_grad_() for _ in range(3))
+            call(plain).backward(up)
+            with torch.autograd.graph.save_on_cpu():
+                out = call(packed)
+            out.backward(up)
+            torch.utils.checkpoint.checkpoint(call, again, use_reentrant=False).backward(up)
+            assert torch.equal(packed.grad, plain.grad) and torch.equal(again.grad, plain.grad)
+
+
+def test_copies_of_a_head():
+    T, d, V = 20, 60, 300
+    q, scale = (t.to(DEV) for t in head(V, d))
+    wide = torch.full((V, 96), 55, dtype=torch.int8, device=DEV)
+    wide[:, :d] = q
+    X = tokens(T, d, BF).to(DEV)
+    h = Int8Head.from_quantized(wide[:, :d], scale)
+    want = h(X)
+    for other in (copy.deepcopy(h), Int8Head.from_quantized(torch.zeros_like(q), torch.zeros_like(scale)), Int8Head.from_quantized(h.q[:, :d], h.scale)):
+        other.load_state_dict(h.state_dict())
+        assert torch.equal(other(X), want)
+    assert bool((wide[:, d:] == 55).all())
